@@ -43,6 +43,8 @@ extern "C" {
 #define STMOE_F32 0
 #define STMOE_BF16 1
 #define STMOE_FP8_E4M3 2 /* e4m3 codes + one bf16 scale per output channel */
+#define STMOE_MX4 3      /* e2m1 codes + one e8m0 scale per 32 elements of a row (see stmoe_mx4_quantize) */
+#define STMOE_F16 4      /* element type of the MX4 and balance operators only */
 
 /* predictor_mode: which sources feed Algorithm 2 (tables evolve identically) */
 #define STMOE_PRED_OFF 0
@@ -367,6 +369,79 @@ size_t stmoe_expert_ffn_dense_scratch_bytes(int m, int hidden, int inter);
 int stmoe_expert_ffn_dense(const float *h, const float *inv_rms, const void *image, int m, int hidden,
                            int inter, float *y, uint32_t *flags, void *scratch, size_t scratch_bytes,
                            void *cuda_stream);
+
+/* ---- microscaled 4-bit floating point (MX4) ------------------------------------------------
+ *
+ * A row of `cols` elements is cut into blocks of 32 (nb = ceil(cols / 32), the last one filled up
+ * with zeros).  A block is 16 bytes of e2m1 codes, two to a byte, the even element in the low
+ * half (values 0, .5, 1, 1.5, 2, 3, 4, 6; bit 3 of a code is the sign), and one e8m0 scale byte
+ * worth 2^(byte-127); byte 255 means that the block is NaN.  Codes are [rows][nb*16] bytes,
+ * scales [rows][nb] bytes; row strides are free. */
+
+/* x [rows][cols] -> codes, scales.  byte = clamp(floor(log2 amax) - 2 + 127, 0, 254), amax the block's
+ * largest magnitude (0 for a block of zeros, 255 for a block that holds a NaN or an infinity);
+ * code = x / 2^(byte-127) to the nearest value, ties to the even code, magnitudes above 6 to 6.
+ *   dtype: STMOE_F32, STMOE_BF16 or STMOE_F16.  x_stride in elements, >= cols; code_stride (a
+ *   multiple of 4, codes 4-byte aligned) and scale_stride in bytes.  rows may be 0.  All pointers
+ *   device; asynchronous on cuda_stream.  16-byte aligned rows of x are read 16 bytes at a time,
+ *   others element by element. */
+int stmoe_mx4_quantize(const void *x, int dtype, int64_t rows, int64_t cols, int64_t x_stride, uint8_t *codes,
+                       int64_t code_stride, uint8_t *scales, int64_t scale_stride, void *cuda_stream);
+/* The reverse: x [rows][cols] = value(code) * 2^(byte-127), rounded once to dtype (exact for fp32 and
+ * bf16 unless it overflows).  Elements of x behind column `cols` stay as they were. */
+int stmoe_mx4_dequantize(const uint8_t *codes, int64_t code_stride, const uint8_t *scales, int64_t scale_stride, int64_t rows,
+                         int64_t cols, void *x, int dtype, int64_t x_stride, void *cuda_stream);
+
+/* out[t][i] = sum_k a[t][k] * b_g(t)[i][k], both operands MX4, on the tensor cores' block-scaled
+ * 4-bit form: products exact, sums fp32, one rounding to out_dtype.
+ *   a        [m] rows (tokens), sorted by group; k_blocks scale blocks each
+ *   b        [n_groups][n] rows of k_blocks blocks (the experts' matrices, one after the other)
+ *   counts   device int32 [n_groups]: rows of a that belong to each group, in order (the counts of
+ *            stmoe_router_balance); rows of a behind their sum have no group, and their rows of out stay
+ *            as they were.  Counts below 0 read as 0, and counts that lead past m are cut.
+ *            NULL: one group (n_groups = 1) with all m rows.
+ *   out      [m][n] in out_dtype (STMOE_F32, STMOE_BF16, STMOE_F16), out_stride in elements
+ *   flags    device uint32, caller-zeroed, or NULL; set to 1 when a bounded wait inside the kernel ran
+ *            out (the affected outputs are then NaN)
+ * Codes 16-byte aligned with strides that are multiples of 16; scale strides are free (rows on
+ * 8-byte boundaries are read fastest).  The part of a row's last block behind its end has to hold
+ * zero codes, as stmoe_mx4_quantize writes them.  A block with scale 255 makes every sum it enters
+ * NaN.  n <= 2^24, n_groups <= 256, n_groups * n < 2^31; m may be 0.  The same call gives the same
+ * bits every time.  No workspace; asynchronous on cuda_stream. */
+int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_t *a_scales, int64_t a_scale_stride, int64_t m,
+                     const uint8_t *b_codes, int64_t b_code_stride, const uint8_t *b_scales, int64_t b_scale_stride,
+                     int n_groups, int n, int k_blocks, const int32_t *counts, void *out, int out_dtype,
+                     int64_t out_stride, uint32_t *flags, void *cuda_stream);
+
+/* ---- router statistics over many tokens ----------------------------------------------------- */
+
+/* Balance loss, z loss and per-expert counts of a router (the gating network of Section 2):
+ *   p_t = softmax(logits_t), lse_t = log sum exp logits_t, over the n rows that count;
+ *   counts[e] = how often e stands in ids of those rows;  f_e = counts[e] / (n top_k);
+ *   loss[0] = n_experts * sum_e f_e * (1/n) sum_t p_te;   loss[1] = (1/n) sum_t lse_t^2.
+ * A row does not count where its mask byte is 0 (it may then hold anything, NaN included) or where
+ * all its logits are -infinity.  With n = 0 everything is 0.
+ *   logits   [tokens][n_experts] in dtype (STMOE_F32, STMOE_BF16, STMOE_F16), stride in elements
+ *   ids      int32 [tokens][top_k]; entries outside [0, n_experts) (-1 for a dropped choice) are not
+ *            counted, an expert that stands twice in a row counts twice
+ *   mask     uint8 [tokens] or NULL
+ *   loss     fp32 [2], counts int32 [n_experts], rows int32 [1] (= n): written
+ *   scratch  stmoe_router_balance_scratch_bytes(n_experts) bytes, 4-byte aligned, contents free;
+ *            calls that can overlap need scratch of their own
+ * All pointers device.  n_experts <= 256, top_k <= n_experts, tokens * top_k < 2^31; tokens may be 0.  The same call
+ * gives the same bits every time.  Asynchronous on cuda_stream. */
+size_t stmoe_router_balance_scratch_bytes(int n_experts);
+int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const int32_t *ids, const uint8_t *mask, int64_t tokens,
+                         int n_experts, int top_k, float *loss, int32_t *counts, int32_t *rows, void *scratch,
+                         size_t scratch_bytes, void *cuda_stream);
+/* Gradient of grad_loss[0] * loss[0] + grad_loss[1] * loss[1] with respect to the logits (counts held
+ * constant), from the forward call's counts and rows:
+ *   grad_logits[t][e] = g0 E/n p_te (f_e - sum_j f_j p_tj) + g1 2/n lse_t p_te,
+ * 0 in rows that do not count.  grad_loss: device fp32 [2].  grad_logits: dtype as the logits,
+ * [tokens][n_experts], every element written; the two may not overlap. */
+int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride, const uint8_t *mask, int64_t tokens,
+                                  int n_experts, int top_k, const int32_t *counts, const int32_t *rows, const float *grad_loss,
+                                  void *grad_logits, int64_t grad_stride, void *cuda_stream);
 
 #ifdef __cplusplus
 }

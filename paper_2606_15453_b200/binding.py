@@ -15,6 +15,7 @@ import torch
 from . import build as _build
 
 DTYPE = {"f32": 0, "bf16": 1, "fp8": 2}
+WEIGHT_DTYPE = {**DTYPE, "mx4": 3}      # expert weights of the FFN entry points and of a stack
 MODE = {"off": 0, "temporal": 1, "spatial": 2, "st": 3}
 FLAG_RENORM_TOPK = 1
 FLAG_NO_PERSISTENT = 2
@@ -91,6 +92,13 @@ def lib():
         L.stmoe_expert_ffn_dense_scratch_bytes.restype = sz
         L.stmoe_expert_ffn_dense_scratch_bytes.argtypes = [i32, i32, i32]
         L.stmoe_expert_ffn_dense.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.stmoe_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
+        L.stmoe_mx4_dequantize.argtypes = [vp, i64, vp, i64, i64, i64, vp, i32, i64, vp]
+        L.stmoe_mx4_matmul.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, i64, i32, i32, i32, vp, vp, i32, i64, vp, vp]
+        L.stmoe_router_balance_scratch_bytes.restype = sz
+        L.stmoe_router_balance_scratch_bytes.argtypes = [i32]
+        L.stmoe_router_balance.argtypes = [vp, i32, i64, vp, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.stmoe_router_balance_backward.argtypes = [vp, i32, i64, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -308,3 +316,182 @@ def expert_ffn_dense(h, inv_rms, image, hidden, inter, stream=None):
                                         _dev(y), _dev(flags), _dev(scratch), scratch.numel(), _stream(stream)),
            "stmoe_expert_ffn_dense")
     return y, flags
+
+
+# ---- microscaled 4-bit floating point and router statistics --------------------------------------
+
+_ELEM = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 4}
+
+
+def _need(ok, what: str) -> None:
+    if not ok:
+        raise StmoeError(what)
+
+
+def _rows2(t, what: str, dtype=None):
+    """A CUDA matrix whose rows are contiguous; any row stride."""
+    _need(t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{what}: expected a 2-D CUDA tensor with contiguous rows")
+    _need(dtype is None or t.dtype == dtype, f"{what}: expected {dtype}, got {t.dtype}")
+    return t
+
+
+def _same_device(first, *rest) -> None:
+    _need(all(t is None or t.device == first.device for t in rest), "all tensors have to be on one CUDA device")
+
+
+def _on_device(ref, stream, call):
+    """call(stream handle) with ref's device current; tensors it allocates belong to that stream."""
+    if stream is None and ref.device.index == torch.cuda.current_device():
+        return call(torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(ref.device):
+        s = stream if stream is not None else torch.cuda.current_stream()
+        _need(s.device == ref.device, "the stream belongs to another device than the tensors")
+        with torch.cuda.stream(s):
+            return call(s.cuda_stream)
+
+
+def mx4_quantize(x, codes=None, scales=None, stream=None):
+    """stmoe_mx4_quantize: x [rows][cols] (fp32, bf16 or fp16, any row stride) -> (codes uint8
+    [rows][ceil(cols/32)*16], scales uint8 [rows][ceil(cols/32)]), into given tensors or new ones."""
+    _rows2(x, "x")
+    _need(x.dtype in _ELEM, f"x: fp32, bf16 or fp16, got {x.dtype}")
+    rows, cols = x.shape
+    _need(cols >= 1, "x has no columns")
+    nb = (cols + 31) // 32
+    _same_device(x, codes, scales)
+    if codes is not None:
+        _need(tuple(_rows2(codes, "codes", torch.uint8).shape) == (rows, nb * 16), f"codes: expected {(rows, nb * 16)}")
+    if scales is not None:
+        _need(tuple(_rows2(scales, "scales", torch.uint8).shape) == (rows, nb), f"scales: expected {(rows, nb)}")
+
+    def call(st):
+        c = torch.empty(rows, nb * 16, dtype=torch.uint8, device=x.device) if codes is None else codes
+        s = torch.empty(rows, nb, dtype=torch.uint8, device=x.device) if scales is None else scales
+        if rows:
+            _check(lib().stmoe_mx4_quantize(x.data_ptr(), _ELEM[x.dtype], rows, cols, x.stride(0), c.data_ptr(), c.stride(0),
+                                            s.data_ptr(), s.stride(0), st), "stmoe_mx4_quantize")
+        return c, s
+    return _on_device(x, stream, call)
+
+
+def mx4_dequantize(codes, scales, cols, dtype=torch.float32, out=None, stream=None):
+    """stmoe_mx4_dequantize: the first `cols` values of every row, in dtype (or in out's)."""
+    _rows2(codes, "codes", torch.uint8), _rows2(scales, "scales", torch.uint8)
+    rows, nb = scales.shape
+    _need(tuple(codes.shape) == (rows, nb * 16) and cols >= 1 and (cols + 31) // 32 == nb,
+          "codes, scales and cols do not belong together")
+    _same_device(codes, scales, out)
+    if out is not None:
+        _need(tuple(_rows2(out, "out").shape) == (rows, cols), f"out: expected {(rows, cols)}")
+        dtype = out.dtype
+    _need(dtype in _ELEM, f"fp32, bf16 or fp16, got {dtype}")
+
+    def call(st):
+        y = torch.empty(rows, cols, dtype=dtype, device=codes.device) if out is None else out
+        if rows:
+            _check(lib().stmoe_mx4_dequantize(codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0), rows, cols,
+                                              y.data_ptr(), _ELEM[dtype], y.stride(0), st), "stmoe_mx4_dequantize")
+        return y
+    return _on_device(codes, stream, call)
+
+
+def mx4_matmul(a, b, counts=None, dtype=torch.bfloat16, out=None, flags=None, stream=None):
+    """stmoe_mx4_matmul: out[t] = a[t] b_g(t)^T for MX4 operands (codes, scales) as mx4_quantize
+    returns them.  a: [m] rows; b: [n] rows, or [groups][n] rows with counts (int32 [groups], on the
+    device: how many rows of a belong to each group, in order; rows behind their sum are not written).
+    flags: optional int32 [1], caller-zeroed; non-zero = a bounded wait inside the kernel ran out."""
+    a_codes, a_scales = _rows2(a[0], "a codes", torch.uint8), _rows2(a[1], "a scales", torch.uint8)
+    b_codes, b_scales = b
+    _need(b_codes.dim() == b_scales.dim() and b_codes.dim() in (2, 3), "b: codes and scales of [n] or [groups][n] rows")
+    groups = 1
+    if b_codes.dim() == 3:
+        groups, n = b_codes.shape[:2]
+        _need(groups >= 1 and n >= 1, "b has no rows")
+        for t in (b_codes, b_scales):
+            _need(groups == 1 or t.stride(0) == n * t.stride(1), "b: the groups' rows have to follow one another")
+        _need(b_scales.shape[:2] == b_codes.shape[:2], "b: codes and scales do not belong together")
+        b_codes, b_scales = b_codes[0], b_scales[0]
+    _rows2(b_codes, "b codes", torch.uint8), _rows2(b_scales, "b scales", torch.uint8)
+    m, nb = a_scales.shape
+    n = b_scales.shape[0]
+    _need(tuple(a_codes.shape) == (m, nb * 16) and tuple(b_codes.shape) == (n, nb * 16) and b_scales.shape[1] == nb and n >= 1 and nb >= 1,
+          "the operands' shapes do not belong together")
+    _same_device(a_codes, a_scales, b_codes, b_scales, counts, out, flags)
+    _need(counts is not None or groups == 1, "several groups need counts")
+    if counts is not None:
+        _need(counts.dtype == torch.int32 and counts.is_contiguous() and counts.numel() == groups, "counts: contiguous int32 [groups]")
+    if out is not None:
+        _need(tuple(_rows2(out, "out").shape) == (m, n), f"out: expected {(m, n)}")
+        dtype = out.dtype
+    _need(dtype in _ELEM, f"fp32, bf16 or fp16, got {dtype}")
+    _need(flags is None or (flags.dtype == torch.int32 and flags.numel() >= 1), "flags: int32")
+
+    def call(st):
+        y = torch.empty(m, n, dtype=dtype, device=a_codes.device) if out is None else out
+        if m:
+            _check(lib().stmoe_mx4_matmul(a_codes.data_ptr(), a_codes.stride(0), a_scales.data_ptr(), a_scales.stride(0), m,
+                                          b_codes.data_ptr(), b_codes.stride(0), b_scales.data_ptr(), b_scales.stride(0),
+                                          groups, n, nb, None if counts is None else counts.data_ptr(), y.data_ptr(),
+                                          _ELEM[dtype], y.stride(0), None if flags is None else flags.data_ptr(), st),
+                   "stmoe_mx4_matmul")
+        return y
+    return _on_device(a_codes, stream, call)
+
+
+def _balance_args(logits, mask):
+    _rows2(logits, "logits")
+    _need(logits.dtype in _ELEM, f"logits: fp32, bf16 or fp16, got {logits.dtype}")
+    T, E = logits.shape
+    if mask is not None:
+        _need(mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and mask.numel() == T, "mask: contiguous bool [tokens]")
+    return T, E
+
+
+def router_balance(logits, ids, mask=None, stream=None):
+    """stmoe_router_balance: losses and per-expert counts for logits [tokens][n_experts] and the
+    chosen experts ids int32 [tokens][top_k] (-1: dropped); mask [tokens]: rows that count.
+    Returns dict(loss fp32 [2] = balance, z; counts int32 [n_experts]; rows int32 [1]; top_k)."""
+    T, E = _balance_args(logits, mask)
+    _need(ids.is_cuda and ids.dtype == torch.int32 and ids.dim() == 2 and ids.is_contiguous() and ids.shape[0] == T,
+          "ids: contiguous int32 CUDA tensor [tokens][top_k]")
+    _same_device(logits, ids, mask)
+    K = ids.shape[1]
+
+    def call(st):
+        n = lib().stmoe_router_balance_scratch_bytes(E)
+        _need(n > 0, f"{E} experts are out of range")
+        scratch = torch.empty(n, dtype=torch.uint8, device=logits.device)
+        loss = torch.empty(2, dtype=torch.float32, device=logits.device)
+        ints = torch.empty(E + 1, dtype=torch.int32, device=logits.device)
+        counts, rows = ints[:E], ints[E:]
+        # an empty tensor has no address; nothing of it is read
+        src, idp = (logits.data_ptr(), ids.data_ptr()) if T else (scratch.data_ptr(), scratch.data_ptr())
+        _check(lib().stmoe_router_balance(src, _ELEM[logits.dtype], logits.stride(0), idp,
+                                          None if mask is None else mask.data_ptr(), T, E, K, loss.data_ptr(), counts.data_ptr(),
+                                          rows.data_ptr(), scratch.data_ptr(), n, st), "stmoe_router_balance")
+        return dict(loss=loss, counts=counts, rows=rows, top_k=K)
+    return _on_device(logits, stream, call)
+
+
+def router_balance_backward(logits, forward, grad_loss, mask=None, out=None, stream=None):
+    """stmoe_router_balance_backward: gradient of grad_loss . loss with respect to the logits, from
+    the dict that router_balance returned for the same logits and mask; grad_loss: fp32 [2]."""
+    T, E = _balance_args(logits, mask)
+    counts, rows = forward["counts"], forward["rows"]
+    _need(counts.dtype == torch.int32 and counts.numel() == E and counts.is_contiguous() and rows.dtype == torch.int32,
+          "forward does not belong to these logits")
+    _need(grad_loss.is_cuda and grad_loss.dtype == torch.float32 and grad_loss.numel() == 2 and grad_loss.is_contiguous(),
+          "grad_loss: fp32 CUDA tensor [2]")
+    _same_device(logits, mask, counts, rows, grad_loss, out)
+    if out is not None:
+        _need(tuple(_rows2(out, "out", logits.dtype).shape) == (T, E), f"out: expected {(T, E)}")
+
+    def call(st):
+        d = torch.empty(T, E, dtype=logits.dtype, device=logits.device) if out is None else out
+        if T:
+            _check(lib().stmoe_router_balance_backward(logits.data_ptr(), _ELEM[logits.dtype], logits.stride(0),
+                                                       None if mask is None else mask.data_ptr(), T, E, forward["top_k"],
+                                                       counts.data_ptr(), rows.data_ptr(), grad_loss.data_ptr(), d.data_ptr(),
+                                                       d.stride(0), st), "stmoe_router_balance_backward")
+        return d
+    return _on_device(logits, stream, call)

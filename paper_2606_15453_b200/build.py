@@ -8,7 +8,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libstmoe.so")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "--use_fast_math=false", "-Xcompiler", "-fPIC", "-shared"]
+              "--use_fast_math=false", "-Xcompiler", "-fPIC", "-shared",
+              "-t", "0"]                      # the sources are compiled side by side
 
 
 def sources():

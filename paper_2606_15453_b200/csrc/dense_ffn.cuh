@@ -19,6 +19,7 @@
 
 #include "device_utils.cuh"
 #include "ffn.cuh"
+#include "tcgen05_utils.cuh"
 
 namespace stmoe_dev {
 
@@ -27,46 +28,8 @@ constexpr int kDenseThreads = 160;       // 4 load/epilogue warps + 1 MMA warp
 constexpr int kDenseRows = 128;          // weight rows per CTA = MMA M
 constexpr int kDenseKStep = 64;          // reduction columns per stage
 constexpr int kDenseMaxTokens = 64;
-constexpr int kDenseSpinLimit = 1 << 22;
 constexpr int kDenseTmemCols = 128;      // gate accumulators in columns [0,64), up in [64,128)
 
-__device__ __forceinline__ uint32_t dsmem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void dmbar_init(uint64_t *bar, int count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(dsmem_u32(bar)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void dmbar_arrive(uint64_t *bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(dsmem_u32(bar)) : "memory");
-}
-// bounded wait on a phase parity; false when the limit ran out or another thread gave up
-__device__ __forceinline__ bool dmbar_wait(uint64_t *bar, uint32_t parity, volatile int *dead,
-                                           int spin_limit = kDenseSpinLimit)
-{
-    for (int spins = 0; spins < spin_limit; ++spins) {
-        uint32_t done;
-        asm volatile(
-            "{.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;}"
-            : "=r"(done)
-            : "r"(dsmem_u32(bar)), "r"(parity)
-            : "memory");
-        if (done) return true;
-        if (*dead) return false;
-    }
-    *dead = 1;
-    return false;
-}
-
-// K-major, no-swizzle shared-memory matrix descriptor: 8-row groups `sbo` bytes apart, the two
-// 16-byte K chunks of one MMA `lbo` bytes apart (descriptor version 1 = sm_100).
-__device__ __forceinline__ uint64_t umma_desc(uint32_t smem_addr, uint32_t lbo, uint32_t sbo)
-{
-    return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) |
-           ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) | (1ull << 46);
-}
 // bf16 x bf16 -> fp32, both operands K-major, M = 128, N = n
 __host__ __device__ constexpr uint32_t umma_idesc_bf16(int n)
 {
@@ -82,22 +45,6 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t a, uint64_t 
         : "r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
         : "memory");
 }
-__device__ __forceinline__ void umma_commit(uint64_t *bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(dsmem_u32(bar))
-                 : "memory");
-}
-__device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&v)[8])
-{
-    uint32_t r[8];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
-}
-
 struct DenseArgs {
     const __nv_bfloat16 *W0;   // [rows][kd] gate (or down) weights, row-major
     const __nv_bfloat16 *W1;   // [rows][kd] up weights (NMAT = 2), else unused

@@ -151,8 +151,6 @@ struct GroupArgs {
     int scale_off;         // element offset of this projection's scales in the image's scale vector
 };
 
-__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async;" ::: "memory"); }
-
 // Bounded wait (one thread) until a counter that other CTAs raise with release semantics reaches
 // `target`; false when the limit ran out or another thread of the CTA gave up.
 __device__ __forceinline__ bool group_wait_counter(const unsigned *counter, unsigned target, volatile int *dead,
@@ -206,32 +204,6 @@ __device__ __forceinline__ void split_e5m2x3(float v, uint8_t (&t)[3])
     }
 }
 
-__device__ __forceinline__ void dmbar_expect_tx(uint64_t *bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(dsmem_u32(bar)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, uint64_t *bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-        ::"r"(dsmem_u32(dst)), "l"(map), "r"(dsmem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
-        : "memory");
-}
-__device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, int c0, int c1, uint64_t *bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-        ::"r"(dsmem_u32(dst)), "l"(map), "r"(dsmem_u32(bar)), "r"(c0), "r"(c1)
-        : "memory");
-}
-// K-major operand tile in the 128-byte swizzled layout (rows of 128 bytes, 8-row groups 1024
-// bytes apart, tile base 1024-byte aligned); kstep = which 32-byte slice of the row (one MMA's
-// reduction depth: 16 two-byte or 32 one-byte elements).
-__device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t smem_addr, int kstep)
-{
-    return (uint64_t)(((smem_addr + kstep * 32) >> 4) & 0x3FFFu) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
-}
 __device__ __forceinline__ float tmem_ld1(uint32_t addr)
 {
     uint32_t r;

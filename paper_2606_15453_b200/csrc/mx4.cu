@@ -1,0 +1,198 @@
+// C entry points of the MX4 operators (mx4.cuh, mx4_matmul.cuh).
+#include "../../include/stmoe.h"
+
+#include <algorithm>
+
+#include "mx4.cuh"
+#include "mx4_matmul.cuh"
+
+using namespace stmoe_dev;
+
+namespace {
+
+#define CU_TRY(expr)                                  \
+    do {                                              \
+        cudaError_t e_ = (expr);                      \
+        if (e_ != cudaSuccess) {                      \
+            (void)cudaGetLastError();                 \
+            return e_ == cudaErrorMemoryAllocation ? STMOE_ERR_OOM : STMOE_ERR_CUDA; \
+        }                                             \
+    } while (0)
+
+constexpr int kMaxDevices = 64;
+
+// SMs of the current device, asked once per device ordinal (a racing fill writes the same value)
+int sm_count(int *dev_out)
+{
+    static int sms[kMaxDevices];
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    *dev_out = dev;
+    if (!sms[dev]) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return 0;
+        }
+        sms[dev] = n;
+    }
+    return sms[dev];
+}
+
+bool elem_type(int dtype) { return dtype == STMOE_F32 || dtype == STMOE_BF16 || dtype == STMOE_F16; }
+long long elem_bytes(int dtype) { return dtype == STMOE_F32 ? 4 : 2; }
+
+int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int64_t x_stride, uint8_t *codes,
+             int64_t code_stride, uint8_t *scales, int64_t scale_stride, void *cuda_stream)
+{
+    if (!x || !codes || !scales || !elem_type(dtype) || rows < 0 || cols < 1) return STMOE_ERR_BAD_ARG;
+    const int64_t nb = (cols - 1) / kMxBlock + 1;
+    if ((rows > 1 && (x_stride < cols || code_stride < nb * 16 || code_stride % 4 || scale_stride < nb)) ||
+        ((uintptr_t)codes & 3) || ((uintptr_t)x & (elem_bytes(dtype) - 1)))
+        return STMOE_ERR_BAD_ARG;
+    if (rows == 0) return STMOE_OK;
+    int dev = 0;
+    const int sms = sm_count(&dev);
+    if (!sms) return STMOE_ERR_CUDA;
+    Mx4Rows a{};
+    a.x = x, a.codes = codes, a.scales = scales, a.rows = rows, a.cols = cols;
+    a.x_stride = x_stride, a.code_stride = code_stride, a.scale_stride = scale_stride;
+    // rows without gaps whose blocks do not straddle them are one long row: short rows then fill
+    // their warps (a warp takes 1024 elements)
+    if (rows > 1 && cols % kMxBlock == 0 && x_stride == cols && code_stride == nb * 16 && scale_stride == nb)
+        a.rows = 1, a.cols = rows * cols;
+    a.vec = ((uintptr_t)x & 15) == 0 && (a.rows == 1 || (x_stride * elem_bytes(dtype)) % 16 == 0);
+    const int64_t tasks = a.rows * ((a.cols - 1) / kMxSeg + 1), warps = kMxThreads / kWarp;
+    const int grid = (int)std::min<int64_t>((tasks + warps - 1) / warps, (int64_t)sms * 8);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (quantize) {
+        if (dtype == STMOE_F32) mx4_quantize_kernel<0><<<grid, kMxThreads, 0, st>>>(a);
+        else if (dtype == STMOE_BF16) mx4_quantize_kernel<1><<<grid, kMxThreads, 0, st>>>(a);
+        else mx4_quantize_kernel<4><<<grid, kMxThreads, 0, st>>>(a);
+    } else {
+        if (dtype == STMOE_F32) mx4_dequantize_kernel<0><<<grid, kMxThreads, 0, st>>>(a);
+        else if (dtype == STMOE_BF16) mx4_dequantize_kernel<1><<<grid, kMxThreads, 0, st>>>(a);
+        else mx4_dequantize_kernel<4><<<grid, kMxThreads, 0, st>>>(a);
+    }
+    CU_TRY(cudaGetLastError());
+    return STMOE_OK;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn()
+{
+    static EncodeTiledFn fn = nullptr;
+    if (!fn) {
+        void *sym = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = (EncodeTiledFn)sym;
+        (void)cudaGetLastError();
+    }
+    return fn;
+}
+
+// codes [rows][row_bytes]: boxes of 128 bytes x box_rows rows, 128-byte swizzle, zeros outside
+int encode_codes(EncodeTiledFn fn, CUtensorMap *m, const uint8_t *base, int64_t rows, int64_t row_bytes, int64_t stride, int box_rows)
+{
+    const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, es[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void *)base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? STMOE_OK
+               : STMOE_ERR_CUDA;
+}
+
+template <int ODT>
+int launch_matmul(const CUtensorMap &ma, const CUtensorMap &mb, const Mx4MatmulArgs &a, int grid, int dev, cudaStream_t st)
+{
+    static bool ready[kMaxDevices];
+    if (!ready[dev]) {
+        CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<ODT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        ready[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(kMmThreads), cfg.dynamicSmemBytes = kMmSmemBytes, cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = a.splits, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = 1;
+    CU_TRY(cudaLaunchKernelEx(&cfg, mx4_matmul_kernel<ODT>, ma, mb, a));
+    return STMOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int stmoe_mx4_quantize(const void *x, int dtype, int64_t rows, int64_t cols, int64_t x_stride, uint8_t *codes,
+                       int64_t code_stride, uint8_t *scales, int64_t scale_stride, void *cuda_stream)
+{
+    return mx4_rows(true, (void *)x, dtype, rows, cols, x_stride, codes, code_stride, scales, scale_stride, cuda_stream);
+}
+
+int stmoe_mx4_dequantize(const uint8_t *codes, int64_t code_stride, const uint8_t *scales, int64_t scale_stride, int64_t rows,
+                         int64_t cols, void *x, int dtype, int64_t x_stride, void *cuda_stream)
+{
+    return mx4_rows(false, x, dtype, rows, cols, x_stride, (uint8_t *)codes, code_stride, (uint8_t *)scales, scale_stride,
+                    cuda_stream);
+}
+
+int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_t *a_scales, int64_t a_scale_stride, int64_t m,
+                     const uint8_t *b_codes, int64_t b_code_stride, const uint8_t *b_scales, int64_t b_scale_stride,
+                     int n_groups, int n, int k_blocks, const int32_t *counts, void *out, int out_dtype,
+                     int64_t out_stride, uint32_t *flags, void *cuda_stream)
+{
+    const int64_t row_bytes = (int64_t)k_blocks * 16;
+    if (!a_codes || !a_scales || !b_codes || !b_scales || !out || !elem_type(out_dtype) || m < 0 || m > INT32_MAX - 256 ||
+        n < 1 || n > (1 << 24) || k_blocks < 1 || k_blocks > (1 << 20) || n_groups < 1 || n_groups > kMmMaxGroups ||
+        (n_groups > 1 && !counts) || (int64_t)n_groups * n > INT32_MAX - 256 || ((uintptr_t)a_codes & 15) ||
+        ((uintptr_t)b_codes & 15) || (m > 1 && (a_code_stride % 16 || a_code_stride < row_bytes)) ||
+        ((int64_t)n_groups * n > 1 && (b_code_stride % 16 || b_code_stride < row_bytes)) || (m > 1 && a_scale_stride < k_blocks) ||
+        ((int64_t)n_groups * n > 1 && b_scale_stride < k_blocks) || (m > 1 && out_stride < n) || ((uintptr_t)out & (elem_bytes(out_dtype) - 1)))
+        return STMOE_ERR_BAD_ARG;
+    if (m == 0) return STMOE_OK;
+    int dev = 0;
+    const int sms = sm_count(&dev);
+    EncodeTiledFn fn = encode_fn();
+    if (!sms || !fn) return STMOE_ERR_CUDA;
+
+    Mx4MatmulArgs a{};
+    a.a_scales = a_scales, a.b_scales = b_scales, a.a_scale_stride = a_scale_stride, a.b_scale_stride = b_scale_stride;
+    a.counts = counts, a.groups = n_groups, a.m = (int)m, a.n = n, a.blocks = k_blocks;
+    a.out = out, a.out_stride = out_stride, a.err = flags;
+    a.a_vec = ((uintptr_t)a_scales & 7) == 0 && a_scale_stride % 8 == 0;
+    a.b_vec = ((uintptr_t)b_scales & 7) == 0 && b_scale_stride % 8 == 0;
+    const int64_t mean = (m + n_groups - 1) / n_groups;
+    a.bn = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 ? 64 : mean <= 128 ? 128 : kMmMaxTokens;
+    const int64_t row_tiles = (n + kMmRows - 1) / kMmRows;
+    // token tiles: at most one part-filled tile per group beyond the full ones
+    const int64_t tok_tiles = std::min<int64_t>(m, m / a.bn + n_groups);
+    const int64_t tasks = row_tiles * tok_tiles;
+    if (tasks > INT32_MAX - 4096) return STMOE_ERR_TOO_LARGE;
+    const int steps = (k_blocks + kMmStageBlocks - 1) / kMmStageBlocks;
+    // too few tiles for the SMs: split the reduction over a cluster
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({sms / std::max<int64_t>(tasks, 1), steps, kMmMaxSplits}));
+    if (a.bn > 64) a.splits = 1;
+    const int grid = a.splits > 1 ? (int)tasks * a.splits : (int)std::min<int64_t>(tasks, sms);
+
+    CUtensorMap ma, mb;
+    // a single row has no stride
+    const int64_t b_rows = (int64_t)n_groups * n;
+    if (encode_codes(fn, &ma, a_codes, m, row_bytes, m > 1 ? a_code_stride : row_bytes, a.bn) != STMOE_OK ||
+        encode_codes(fn, &mb, b_codes, b_rows, row_bytes, b_rows > 1 ? b_code_stride : row_bytes, kMmRows) != STMOE_OK)
+        return STMOE_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (out_dtype == STMOE_F32) return launch_matmul<0>(ma, mb, a, grid, dev, st);
+    if (out_dtype == STMOE_BF16) return launch_matmul<1>(ma, mb, a, grid, dev, st);
+    return launch_matmul<4>(ma, mb, a, grid, dev, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,203 @@
+// Microscaled 4-bit floating point (MX4): a row is cut into blocks of 32 elements; a block holds
+// 32 e2m1 codes (two to a byte, the even element in the low half) under one e8m0 scale byte.
+//
+//   amax = max |x| over the block
+//   byte = clamp(floor(log2 amax) - 2 + 127, 0, 254)   (6 = 1.5 * 2^2 is the largest e2m1 value)
+//          255 where the block holds a NaN or an infinity: the whole block reads back as NaN
+//   code = x / 2^(byte-127) rounded to the nearest of {0, .5, 1, 1.5, 2, 3, 4, 6} with its sign, ties
+//          to the even code, values above 6 to 6
+//
+// A row's last block is filled up with zeros, so a row of codes is a multiple of 16 bytes.
+//
+// Both directions are bound by HBM: one pass, 16-byte loads of the wide side, 4-byte accesses of
+// the codes.  A lane owns 8 consecutive elements of a block, so the block maximum is two shuffles;
+// a warp takes 1024 elements of a row at a time, four independent groups per lane, which keeps
+// enough loads in flight.  The arithmetic is exact: the scale is a power of two, its exponent is
+// read from the bits of amax, and the only rounding is the conversion to e2m1.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "device_utils.cuh"
+
+namespace stmoe_dev {
+
+constexpr int kMxBlock = 32;        // elements under one scale
+constexpr int kMxSeg = 1024;        // elements of a row that a warp takes at a time
+constexpr int kMxGroups = kMxSeg / (kWarp * 8);
+constexpr int kMxThreads = 256;
+
+// 8 fp32 -> 8 e2m1 codes, element i in bits 4i
+__device__ __forceinline__ uint32_t e2m1_pack8(const float (&v)[8])
+{
+    uint32_t r;
+    asm("{.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};}"
+        : "=r"(r)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+
+// 8 codes -> four f16 pairs (exact), element 2i in the low half of h[i]
+__device__ __forceinline__ void e2m1_unpack8(uint32_t w, uint32_t (&h)[4])
+{
+    asm("{.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+}
+
+// 2^(byte-127) as fp32: the byte is the exponent field, except at its ends
+__device__ __forceinline__ float e8m0_value(uint32_t byte)
+{
+    return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fffffffu : byte << 23);
+}
+
+// element types of the wide side: 0 fp32, 1 bf16, 4 f16 (the codes of the C boundary)
+template <int DT> struct Elem;
+template <> struct Elem<0> {
+    using T = float;
+    static constexpr int kVec = 4;   // elements of a 16-byte access
+    __device__ static __forceinline__ float to_f32(T v) { return v; }
+    __device__ static __forceinline__ T from_f32(float v) { return v; }
+};
+template <> struct Elem<1> {
+    using T = __nv_bfloat16;
+    static constexpr int kVec = 8;
+    __device__ static __forceinline__ float to_f32(T v) { return __bfloat162float(v); }
+    __device__ static __forceinline__ T from_f32(float v) { return __float2bfloat16_rn(v); }
+};
+template <> struct Elem<4> {
+    using T = __half;
+    static constexpr int kVec = 8;
+    __device__ static __forceinline__ float to_f32(T v) { return __half2float(v); }
+    __device__ static __forceinline__ T from_f32(float v) { return __float2half_rn(v); }
+};
+
+// 8 elements from p (valid: how many exist, the others read as 0); vec: p is 16-byte aligned
+template <int DT> __device__ __forceinline__ void load8(const typename Elem<DT>::T *p, int valid, bool vec, float (&v)[8])
+{
+    using E = Elem<DT>;
+    typename E::T t[8];
+    if (vec && valid >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8 / E::kVec; ++i)
+            *reinterpret_cast<uint4 *>(t + i * E::kVec) = ld_stream16(p + i * E::kVec);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = E::to_f32(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < valid ? E::to_f32(p[i]) : 0.f;
+    }
+}
+
+template <int DT> __device__ __forceinline__ void store8(typename Elem<DT>::T *p, int valid, bool vec, const float (&v)[8])
+{
+    using E = Elem<DT>;
+    typename E::T t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = E::from_f32(v[i]);
+    if (vec && valid >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8 / E::kVec; ++i)
+            *reinterpret_cast<uint4 *>(p + i * E::kVec) = *reinterpret_cast<const uint4 *>(t + i * E::kVec);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i] = t[i];
+    }
+}
+
+struct Mx4Rows {
+    void *x;                  // wide side [rows][cols]
+    uint8_t *codes, *scales;  // [rows][ceil(cols/32)*16], [rows][ceil(cols/32)]
+    long long rows, cols;
+    long long x_stride;       // elements
+    long long code_stride, scale_stride;  // bytes
+    bool vec;                 // rows of x start on 16-byte boundaries
+};
+
+template <int DT> __global__ void __launch_bounds__(kMxThreads) mx4_quantize_kernel(const Mx4Rows a)
+{
+    using T = typename Elem<DT>::T;
+    const int lane = threadIdx.x % kWarp;
+    const long long segs = (a.cols + kMxSeg - 1) / kMxSeg, tasks = a.rows * segs;
+    const long long nw = (long long)gridDim.x * (kMxThreads / kWarp);
+    for (long long task = (long long)blockIdx.x * (kMxThreads / kWarp) + threadIdx.x / kWarp; task < tasks; task += nw) {
+        const long long row = task / segs, c0 = (task - row * segs) * kMxSeg + lane * 8;
+        const T *x = reinterpret_cast<const T *>(a.x) + row * a.x_stride;
+        float v[kMxGroups][8];
+        const long long padded = (a.cols + kMxBlock - 1) / kMxBlock * kMxBlock;
+#pragma unroll
+        for (int g = 0; g < kMxGroups; ++g) {
+            const long long c = c0 + g * (kWarp * 8);
+            load8<DT>(x + c, (int)max(0ll, min(8ll, a.cols - c)), a.vec, v[g]);
+        }
+#pragma unroll
+        for (int g = 0; g < kMxGroups; ++g) {
+            const long long c = c0 + g * (kWarp * 8);
+            // the bits of |x| order like the values, with infinity and NaN on top
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[g][i]) & 0x7fffffffu);
+            m = max(m, __shfl_xor_sync(kFull, m, 1));
+            m = max(m, __shfl_xor_sync(kFull, m, 2));
+            const int e = (int)(m >> 23);
+            const uint32_t byte = e == 255 ? 255u : (uint32_t)max(e - 2, 0);
+            const float inv = __uint_as_float((254u - min(byte, 253u)) << 23);  // 2^-(byte-127), always normal
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[g][i] *= inv;
+            if (c < padded) {
+                *reinterpret_cast<uint32_t *>(a.codes + row * a.code_stride + c / 2) = e2m1_pack8(v[g]);
+                if (lane % 4 == 0) a.scales[row * a.scale_stride + c / kMxBlock] = (uint8_t)byte;
+            }
+        }
+    }
+}
+
+template <int DT> __global__ void __launch_bounds__(kMxThreads) mx4_dequantize_kernel(const Mx4Rows a)
+{
+    using T = typename Elem<DT>::T;
+    const int lane = threadIdx.x % kWarp;
+    const long long segs = (a.cols + kMxSeg - 1) / kMxSeg, tasks = a.rows * segs;
+    const long long nw = (long long)gridDim.x * (kMxThreads / kWarp);
+    for (long long task = (long long)blockIdx.x * (kMxThreads / kWarp) + threadIdx.x / kWarp; task < tasks; task += nw) {
+        const long long row = task / segs, c0 = (task - row * segs) * kMxSeg + lane * 8;
+        T *x = reinterpret_cast<T *>(a.x) + row * a.x_stride;
+        uint32_t w[kMxGroups], byte[kMxGroups];
+#pragma unroll
+        for (int g = 0; g < kMxGroups; ++g) {
+            const long long c = c0 + g * (kWarp * 8);
+            w[g] = byte[g] = 0;
+            if (c < a.cols) {
+                w[g] = __ldg(reinterpret_cast<const uint32_t *>(a.codes + row * a.code_stride + c / 2));
+                byte[g] = __ldg(a.scales + row * a.scale_stride + c / kMxBlock);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < kMxGroups; ++g) {
+            const long long c = c0 + g * (kWarp * 8);
+            if (c >= a.cols) break;
+            uint32_t h[4];
+            e2m1_unpack8(w[g], h);
+            const float s = e8m0_value(byte[g]);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[i]));
+                v[2 * i] = f.x * s, v[2 * i + 1] = f.y * s;
+            }
+            store8<DT>(x + c, (int)min(8ll, a.cols - c), a.vec, v);
+        }
+    }
+}
+
+}  // namespace stmoe_dev

@@ -1,0 +1,390 @@
+// MX4 product on the tensor cores (tcgen05.mma kind::mxf4, block scales in tensor memory):
+//
+//   out[t][i] = sum_k a[t][k] * b_e(t)[i][k]
+//
+// with both operands in MX4 (mx4.cuh).  The rows of a (tokens) are sorted by expert: counts[e] rows
+// belong to matrix e of b, in order; without counts there is one matrix and every row belongs to it.
+// The products of codes and scales are exact, sums are fp32 in tensor memory, the result is rounded
+// once.
+//
+// The rows of b are the MMA's M (128 a tile), the tokens its N (a tile of up to 192, multiples of
+// 16), and a stage holds 256 elements of the reduction: 128 bytes of codes a row, the width of the
+// swizzled operand layout, four MMAs of depth 64.
+//   warp 0      one thread loads the code tiles by TMA
+//   warp 1      one thread copies a stage's scales into tensor memory (tcgen05.cp), issues its four
+//               MMAs and frees the stage; the warp owns the tensor-memory allocation
+//   warps 2-5   epilogue, from two accumulator buffers
+//   warps 6-9   scales: a thread reads a row's eight scale bytes of a stage (four stages ahead, in
+//               registers) and writes them where the copy expects them: for 128 rows and four blocks
+//               512 bytes, row r at (r % 32) * 16 + (r / 32) * 4
+// The scales of a stage have their own columns in tensor memory, as many sets as there are stages:
+// a set is rewritten only after the commit that frees its stage, so no copy can overtake an MMA
+// that still reads the set.
+//
+// Few tokens: the product is bound by reading b, and one tile per SM leaves SMs idle, so the
+// reduction is split over a cluster of CTAs that exchange their partial sums through distributed
+// shared memory and add them in the order of the ranks (no workspace, no atomics, the same bits
+// every time).
+// Every wait is bounded; where one runs out the error word is set and the affected outputs are NaN.
+#pragma once
+#include "mx4.cuh"
+#include "tcgen05_utils.cuh"
+
+namespace stmoe_dev {
+
+constexpr int kMmThreads = 320;
+constexpr int kMmRows = 128;              // rows of b in a tile (MMA M)
+constexpr int kMmMaxTokens = 192;         // tokens in a tile (MMA N)
+constexpr int kMmStageBlocks = 8;         // scale blocks of a stage (256 elements, 128 bytes of codes)
+constexpr int kMmABytes = kMmRows * 128;
+constexpr int kMmMaxStages = 12;
+constexpr int kMmMaxSplits = 8;           // portable cluster size
+constexpr int kMmMaxGroups = 256;
+constexpr int kMmSmemBytes = 224 * 1024;  // dynamic; one CTA per SM
+constexpr int kMmAccStride = kMmMaxTokens;
+constexpr int kMmScaleCol = 2 * kMmAccStride;   // scale sets start behind the accumulators
+
+// rows of 128 tokens whose scales a stage copies, bytes and tensor-memory columns of a stage
+__host__ __device__ constexpr int mm_token_atoms(int bn) { return (bn + 127) / 128; }
+__host__ __device__ constexpr int mm_stage_bytes(int bn) { return kMmABytes + bn * 128 + 1024 + 1024 * mm_token_atoms(bn); }
+__host__ __device__ constexpr int mm_scale_cols(int bn) { return 8 + 8 * mm_token_atoms(bn); }
+__host__ __device__ constexpr int mm_slot_bytes(int bn) { return (mm_stage_bytes(bn) + 1023) / 1024 * 1024; }
+__host__ __device__ constexpr int mm_stages(int bn)
+{
+    const int by_smem = (kMmSmemBytes - 1024) / mm_slot_bytes(bn), by_tmem = (512 - kMmScaleCol) / mm_scale_cols(bn);
+    const int n = by_smem < by_tmem ? by_smem : by_tmem;
+    return n < kMmMaxStages ? n : kMmMaxStages;
+}
+
+struct Mx4MatmulArgs {
+    const uint8_t *a_scales, *b_scales;
+    long long a_scale_stride, b_scale_stride;  // bytes
+    const int *counts;      // [groups] rows of a per matrix of b, or nullptr
+    int groups, m, n;
+    int blocks;             // scale blocks of a row (reduction length / 32)
+    int bn, splits;
+    void *out;
+    long long out_stride;   // elements
+    unsigned *err;          // may be nullptr
+    bool a_vec, b_vec;      // scale rows start on 8-byte boundaries
+};
+
+// mxf4 descriptor: e2m1 x e2m1, e8m0 scales, both K-major, M = 128, N = n; which half of a scale
+// word (two blocks) the MMA takes, for both operands
+__device__ __forceinline__ uint32_t umma_idesc_mxf4(int n, int half)
+{
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(kMmRows >> 7) << 27) |
+           ((uint32_t)(2 * half) << 4) | ((uint32_t)(2 * half) << 29);
+}
+__device__ __forceinline__ void umma_mxf4(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                          bool accumulate)
+{
+    asm volatile(
+        "{.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;}"
+        :
+        : "r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// 32 rows x 16 bytes of shared memory into four columns, repeated in each quarter of the lanes
+__device__ __forceinline__ void umma_copy_scales(uint32_t tmem, uint32_t smem)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(umma_desc(smem, 128, 128)) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16])
+{
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// eight scale bytes of a row from block kb on; blocks past the end read as 1.0 (their codes are
+// zero, and zero times a NaN scale would not be)
+__device__ __forceinline__ uint2 load_scales8(const uint8_t *row, int kb, int blocks, bool vec)
+{
+    uint2 v = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+    if (vec && kb + 8 <= blocks) return __ldg(reinterpret_cast<const uint2 *>(row + kb));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (kb + i < blocks) {
+            const uint32_t b = __ldg(row + kb + i);
+            uint32_t &w = i < 4 ? v.x : v.y;
+            w = (w & ~(0xffu << (8 * (i & 3)))) | (b << (8 * (i & 3)));
+        }
+    return v;
+}
+
+// Which rows a task multiplies.
+struct Mx4Task {
+    int expert, row0;      // matrix of b and its first row
+    int tok0, count;       // first token and how many of the tile's are this expert's
+};
+
+// s_off: first token of every group (groups + 1 entries), s_tile: token tiles before it
+__device__ __forceinline__ Mx4Task mm_task(const Mx4MatmulArgs &a, const int *s_off, const int *s_tile, int task)
+{
+    const int wt = (a.n + kMmRows - 1) / kMmRows;
+    const int t = task / wt;  // which token tile the task would be if every group's came first
+    int lo = 0, hi = a.groups - 1;
+    while (lo < hi) {         // last group with s_tile[g] <= t and tiles of its own
+        const int mid = (lo + hi + 1) / 2;
+        if (s_tile[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    // a group's tasks: its row tiles, and for each of them its token tiles, so that a tile of b is
+    // read by consecutive tasks
+    const int tiles = s_tile[lo + 1] - s_tile[lo], r = task - s_tile[lo] * wt;
+    Mx4Task k;
+    k.expert = lo;
+    k.row0 = (r / tiles) * kMmRows;
+    k.tok0 = s_off[lo] + (r % tiles) * a.bn;
+    k.count = min(a.bn, s_off[lo + 1] - k.tok0);
+    return k;
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_cluster(uint32_t smem, int rank)
+{
+    uint32_t remote;
+    float v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+    return v;
+}
+
+template <int ODT>
+__global__ void __launch_bounds__(kMmThreads, 1)
+mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Mx4MatmulArgs a)
+{
+    using E = Elem<ODT>;
+    extern __shared__ uint8_t dsm_raw[];
+    __shared__ uint64_t full[kMmMaxStages], empty[kMmMaxStages], tfull[2], tempty[2];
+    __shared__ int s_off[kMmMaxGroups + 1], s_tile[kMmMaxGroups + 1];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_dead;
+    const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp;
+    uint8_t *dsm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dsm_raw) + 1023) & ~(uintptr_t)1023);
+    const int NS = mm_stages(a.bn), slot = mm_slot_bytes(a.bn), bn = a.bn;
+    const int sfa_at = kMmABytes + bn * 128, sfb_at = sfa_at + 1024, atoms = mm_token_atoms(bn);
+
+    if (tid == 0) {
+        s_dead = 0;
+        for (int s = 0; s < NS; ++s) dmbar_init(&full[s], 1 + 4), dmbar_init(&empty[s], 1);
+        for (int b = 0; b < 2; ++b) dmbar_init(&tfull[b], 1), dmbar_init(&tempty[b], 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dsmem_u32(&s_tmem)), "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (warp == 2) {  // group offsets; a count that is negative or leaves the rows of a is cut
+        int off = 0, tiles = 0;
+        if (lane == 0) s_off[0] = s_tile[0] = 0;
+        for (int g0 = 0; g0 < a.groups; g0 += kWarp) {
+            const int g = g0 + lane;
+            int c = g < a.groups ? (a.counts ? max(0, a.counts[g]) : a.m) : 0;
+            c = min(c, a.m);
+            long long at = c;
+#pragma unroll
+            for (int o = 1; o < kWarp; o <<= 1) {
+                const long long t = __shfl_up_sync(kFull, at, o);
+                if (lane >= o) at += t;
+            }
+            const int end = (int)min((long long)a.m, off + at);
+            const int beg = (int)min((long long)a.m, off + at - c);
+            int t = (end - beg + bn - 1) / bn;
+#pragma unroll
+            for (int o = 1; o < kWarp; o <<= 1) {
+                const int u = __shfl_up_sync(kFull, t, o);
+                if (lane >= o) t += u;
+            }
+            if (g < a.groups) s_off[g + 1] = end, s_tile[g + 1] = tiles + t;
+            off = __shfl_sync(kFull, end, kWarp - 1);
+            tiles += __shfl_sync(kFull, t, kWarp - 1);
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    volatile int *dead = &s_dead;
+
+    const int n_tasks = s_tile[a.groups] * ((a.n + kMmRows - 1) / kMmRows);
+    const int rank = blockIdx.x % a.splits, first = blockIdx.x / a.splits, step = gridDim.x / a.splits;
+    const int n_steps = (a.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
+    const int k_beg = (int)((long long)n_steps * rank / a.splits), k_end = (int)((long long)n_steps * (rank + 1) / a.splits);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0, issued = 0;
+            uint32_t par = 0;
+            for (int task = first; task < n_tasks && !*dead; task += step) {
+                const Mx4Task t = mm_task(a, s_off, s_tile, task);
+                for (int k = k_beg; k < k_end; ++k, ++issued) {
+                    if (!dmbar_wait(&empty[s], par ^ 1u, dead)) break;
+                    uint8_t *st = dsm + (size_t)s * slot;
+                    dmbar_expect_tx(&full[s], (uint32_t)(kMmABytes + bn * 128));
+                    tma_load_2d(st, &map_b, k * 128, t.expert * a.n + t.row0, &full[s]);
+                    tma_load_2d(st + kMmABytes, &map_a, k * 128, t.tok0, &full[s]);
+                    if (++s == NS) s = 0, par ^= 1u;
+                }
+            }
+            // every load that was issued lands before the CTA may exit, after an error too (the wait
+            // then has an end of its own: the error word would cut it short)
+            int none = 0;
+            for (int i = 0; i < min(issued, NS); ++i) {
+                if (s == 0) s = NS, par ^= 1u;
+                --s;
+                dmbar_wait(&full[s], par, &none, 1 << 14);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t id0 = umma_idesc_mxf4(bn, 0), id1 = umma_idesc_mxf4(bn, 1);
+            const int cols = mm_scale_cols(bn);
+            int s = 0, it = 0;
+            uint32_t par = 0;
+            for (int task = first; task < n_tasks && !*dead; task += step, ++it) {
+                const int ab = it & 1;
+                if (!dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t acc = tmem + ab * kMmAccStride;
+                bool ok = true;
+                for (int k = k_beg; k < k_end; ++k) {
+                    if (!(ok = dmbar_wait(&full[s], par, dead))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t st = dsmem_u32(dsm + (size_t)s * slot);
+                    const uint32_t sf = tmem + kMmScaleCol + s * cols;  // this stage's set of scale columns
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {                       // four blocks each
+                        umma_copy_scales(sf + 4 * q, st + sfa_at + 512 * q);
+                        for (int r = 0; r < atoms; ++r)
+                            umma_copy_scales(sf + 8 + 4 * (q * atoms + r), st + sfb_at + 512 * (q * atoms + r));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        umma_mxf4(acc, umma_desc_sw128(st, j), umma_desc_sw128(st + kMmABytes, j), j & 1 ? id1 : id0,
+                                  sf + 4 * (j / 2), sf + 8 + 4 * (j / 2) * atoms, k > k_beg || j > 0);
+                    umma_commit(&empty[s]);
+                    if (++s == NS) s = 0, par ^= 1u;
+                }
+                if (!ok) break;
+                umma_commit(&tfull[ab]);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 6) {
+        const int lg = warp % 4;  // the quarter of the lanes this warp may read
+        int it = 0;
+        for (int task = first; task < n_tasks; task += step, ++it) {
+            const int ab = it & 1;
+            const Mx4Task t = mm_task(a, s_off, s_tile, task);
+            const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], (uint32_t)(it >> 1) & 1u, dead));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + ab * kMmAccStride + ((uint32_t)(lg * kWarp) << 16);
+            const int row = t.row0 + lg * kWarp + lane;
+            if (a.splits == 1) {
+                typename E::T *out = reinterpret_cast<typename E::T *>(a.out) + (long long)t.tok0 * a.out_stride + row;
+                for (int j0 = 0; j0 < t.count; j0 += 16) {
+                    float v[16];
+                    tmem_ld16(acc + j0, v);
+                    if (row < a.n)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (j0 + j < t.count)
+                                out[(long long)(j0 + j) * a.out_stride] = E::from_f32(ok ? v[j] : __uint_as_float(0x7fffffffu));
+                }
+            } else {
+                // the ring is idle once the last MMA has been committed: the partial tile takes its place
+                float *part = reinterpret_cast<float *>(dsm);
+                for (int j0 = 0; j0 < bn; j0 += 16) {
+                    float v[16];
+                    tmem_ld16(acc + j0, v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) part[(j0 + j) * kMmRows + lg * kWarp + lane] = ok ? v[j] : __uint_as_float(0x7fffffffu);
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) dmbar_arrive(&tempty[ab]);
+            if (!ok) break;
+        }
+    } else {
+        // scales: thread = row of the tile of b, and up to two tokens
+        const int r = tid - 6 * kWarp;
+        const uint32_t at = (uint32_t)((r % 32) * 16 + (r / 32) * 4);
+        int s = 0;
+        uint32_t par = 0;
+        bool ok = true;
+        for (int task = first; task < n_tasks && ok; task += step) {
+            const Mx4Task t = mm_task(a, s_off, s_tile, task);
+            const uint8_t *pb = a.b_scales + ((long long)t.expert * a.n + min(t.row0 + r, a.n - 1)) * a.b_scale_stride;
+            const uint8_t *pa0 = a.a_scales + (long long)min(t.tok0 + r, a.m - 1) * a.a_scale_stride;
+            const uint8_t *pa1 = a.a_scales + (long long)min(t.tok0 + 128 + r, a.m - 1) * a.a_scale_stride;
+            for (int k0 = k_beg; k0 < k_end && ok; k0 += 4) {
+                uint2 vb[4], v0[4], v1[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int kb = min(k0 + i, n_steps - 1) * kMmStageBlocks;
+                    vb[i] = load_scales8(pb, kb, a.blocks, a.b_vec);
+                    if (r < bn) v0[i] = load_scales8(pa0, kb, a.blocks, a.a_vec);
+                    if (128 + r < bn) v1[i] = load_scales8(pa1, kb, a.blocks, a.a_vec);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (k0 + i < k_end && ok) {
+                        ok = __all_sync(kFull, dmbar_wait(&empty[s], par ^ 1u, dead));
+                        uint8_t *st = dsm + (size_t)s * slot;
+                        *reinterpret_cast<uint32_t *>(st + sfa_at + at) = vb[i].x;
+                        *reinterpret_cast<uint32_t *>(st + sfa_at + 512 + at) = vb[i].y;
+                        if (r < bn) {
+                            *reinterpret_cast<uint32_t *>(st + sfb_at + at) = v0[i].x;
+                            *reinterpret_cast<uint32_t *>(st + sfb_at + 512 * atoms + at) = v0[i].y;
+                        }
+                        if (128 + r < bn) {
+                            *reinterpret_cast<uint32_t *>(st + sfb_at + 512 + at) = v1[i].x;
+                            *reinterpret_cast<uint32_t *>(st + sfb_at + 512 * atoms + 512 + at) = v1[i].y;
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) dmbar_arrive(&full[s]);
+                        if (++s == NS) s = 0, par ^= 1u;
+                    }
+                }
+            }
+        }
+    }
+    if (a.splits > 1 && first < n_tasks) {  // one task per cluster, the same for all its CTAs
+        __syncwarp();
+        cluster_sync();
+        const Mx4Task t = mm_task(a, s_off, s_tile, first);
+        const uint32_t part = dsmem_u32(dsm);
+        for (int i = tid; i < kMmRows * bn; i += kMmThreads) {
+            const int j = i / kMmRows, row = t.row0 + i % kMmRows;
+            if (j % a.splits != rank || j >= t.count || row >= a.n) continue;
+            float y = 0.f;
+            for (int z = 0; z < a.splits; ++z) y += ld_cluster(part + (uint32_t)i * 4, z);
+            reinterpret_cast<typename E::T *>(a.out)[(long long)(t.tok0 + j) * a.out_stride + row] = E::from_f32(y);
+        }
+        cluster_sync();  // nobody leaves while its partial tile is read
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+    if (tid == 0 && s_dead && a.err) *a.err = 1u;
+}
+
+}  // namespace stmoe_dev

@@ -1,0 +1,134 @@
+// C entry points of the router's balance loss (router_balance.cuh).
+#include "../../include/stmoe.h"
+
+#include <algorithm>
+
+#include "router_balance.cuh"
+
+using namespace stmoe_dev;
+
+namespace {
+
+bool bal_args_ok(const void *logits, int dtype, int64_t stride, int64_t tokens, int n_experts, int top_k)
+{
+    return logits && (dtype == STMOE_F32 || dtype == STMOE_BF16 || dtype == STMOE_F16) && tokens >= 0 && n_experts >= 1 &&
+           n_experts <= kBalMaxExperts && top_k >= 1 && top_k <= n_experts && (tokens <= 1 || stride >= n_experts) &&
+           tokens <= INT32_MAX / top_k && ((uintptr_t)logits & (dtype == STMOE_F32 ? 3 : 1)) == 0;
+}
+bool rows_vec(const void *p, int dtype, int64_t stride, int n_experts)
+{
+    const int v = dtype == STMOE_F32 ? 4 : 8;
+    return ((uintptr_t)p & 15) == 0 && stride % v == 0 && n_experts % v == 0;
+}
+bool overlap(const void *p, int64_t p_stride, const void *q, int64_t q_stride, int64_t tokens, int n_experts, int dtype)
+{
+    const int64_t eb = dtype == STMOE_F32 ? 4 : 2;
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+    const uintptr_t a_end = a + eb * ((tokens - 1) * p_stride + n_experts), b_end = b + eb * ((tokens - 1) * q_stride + n_experts);
+    return a < b_end && b < a_end;
+}
+// lanes that share a row: a power of two with eight logits each
+int lanes_per_row(int n_experts)
+{
+    int l = 1;
+    while (l * 8 < n_experts) l *= 2;
+    return l;
+}
+int bal_grid(int64_t tokens, int lpr)
+{
+    const int64_t rows = (int64_t)(kBalThreads / kWarp) * (kWarp / lpr);
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(tokens + rows - 1) / rows, (int64_t)sms * 4, kBalMaxCtas}));
+}
+
+template <int DT, int LPR> void launch(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+{
+    if (backward)
+        router_balance_backward_kernel<DT, LPR><<<grid, kBalThreads, 0, st>>>(a);
+    else
+        router_balance_kernel<DT, LPR><<<grid, kBalThreads, 0, st>>>(a);
+}
+template <int DT> void launch_lanes(int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+{
+    switch (lpr) {
+    case 1: launch<DT, 1>(backward, a, grid, st); break;
+    case 2: launch<DT, 2>(backward, a, grid, st); break;
+    case 4: launch<DT, 4>(backward, a, grid, st); break;
+    case 8: launch<DT, 8>(backward, a, grid, st); break;
+    case 16: launch<DT, 16>(backward, a, grid, st); break;
+    default: launch<DT, 32>(backward, a, grid, st); break;
+    }
+}
+int launch_typed(int dtype, int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+{
+    if (dtype == STMOE_F32) launch_lanes<0>(lpr, backward, a, grid, st);
+    else if (dtype == STMOE_BF16) launch_lanes<1>(lpr, backward, a, grid, st);
+    else launch_lanes<4>(lpr, backward, a, grid, st);
+    if (cudaGetLastError() != cudaSuccess) return STMOE_ERR_CUDA;
+    return STMOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t stmoe_router_balance_scratch_bytes(int n_experts)
+{
+    if (n_experts < 1 || n_experts > kBalMaxExperts) return 0;
+    return sizeof(float) * (size_t)kBalMaxCtas * bal_part_words(n_experts);
+}
+
+int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const int32_t *ids, const uint8_t *mask, int64_t tokens,
+                         int n_experts, int top_k, float *loss, int32_t *counts, int32_t *rows, void *scratch,
+                         size_t scratch_bytes, void *cuda_stream)
+{
+    if (!bal_args_ok(logits, dtype, stride, tokens, n_experts, top_k) || !ids || !loss || !counts || !rows || !scratch ||
+        ((uintptr_t)scratch & 3) || scratch_bytes < stmoe_router_balance_scratch_bytes(n_experts))
+        return STMOE_ERR_BAD_ARG;
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr);
+    if (!grid) return STMOE_ERR_CUDA;
+    BalanceArgs a{};
+    a.logits = logits, a.stride = stride, a.ids = ids, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
+    a.vec = rows_vec(logits, dtype, stride, n_experts);
+    a.part = (float *)scratch, a.ctas = grid, a.loss = loss, a.counts = counts, a.rows = rows;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const int rc = launch_typed(dtype, lpr, false, a, grid, st);
+    if (rc != STMOE_OK) return rc;
+    // may start while the first kernel drains; it waits for that kernel's results itself
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1), cfg.blockDim = dim3(1024), cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at, cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, router_balance_finish_kernel, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return STMOE_ERR_CUDA;
+    }
+    return STMOE_OK;
+}
+
+int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride, const uint8_t *mask, int64_t tokens,
+                                  int n_experts, int top_k, const int32_t *counts, const int32_t *rows, const float *grad_loss,
+                                  void *grad_logits, int64_t grad_stride, void *cuda_stream)
+{
+    if (!bal_args_ok(logits, dtype, stride, tokens, n_experts, top_k) || !counts || !rows || !grad_loss ||
+        !bal_args_ok(grad_logits, dtype, grad_stride, tokens, n_experts, top_k))
+        return STMOE_ERR_BAD_ARG;
+    if (tokens == 0) return STMOE_OK;
+    if (overlap(logits, stride, grad_logits, grad_stride, tokens, n_experts, dtype)) return STMOE_ERR_BAD_ARG;
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr);
+    if (!grid) return STMOE_ERR_CUDA;
+    BalanceArgs a{};
+    a.logits = logits, a.stride = stride, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
+    a.vec = rows_vec(logits, dtype, stride, n_experts);
+    a.counts = (int *)counts, a.rows = (int *)rows, a.grad = grad_loss;
+    a.dlogits = grad_logits, a.dstride = grad_stride, a.dvec = rows_vec(grad_logits, dtype, grad_stride, n_experts);
+    return launch_typed(dtype, lpr, true, a, grid, (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"

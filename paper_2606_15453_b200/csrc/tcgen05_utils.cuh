@@ -1,0 +1,93 @@
+// Shared-memory barriers, TMA loads, tensor-memory reads and operand descriptors used by every
+// tensor-core kernel of the library (tcgen05, sm_100a).
+#pragma once
+#include <cuda.h>
+
+#include "device_utils.cuh"
+
+namespace stmoe_dev {
+
+constexpr int kDenseSpinLimit = 1 << 22;
+
+__device__ __forceinline__ uint32_t dsmem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void dmbar_init(uint64_t *bar, int count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(dsmem_u32(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void dmbar_arrive(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(dsmem_u32(bar)) : "memory");
+}
+// bounded wait on a phase parity; false when the limit ran out or another thread gave up
+__device__ __forceinline__ bool dmbar_wait(uint64_t *bar, uint32_t parity, volatile int *dead,
+                                           int spin_limit = kDenseSpinLimit)
+{
+    for (int spins = 0; spins < spin_limit; ++spins) {
+        uint32_t done;
+        asm volatile(
+            "{.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;}"
+            : "=r"(done)
+            : "r"(dsmem_u32(bar)), "r"(parity)
+            : "memory");
+        if (done) return true;
+        if (*dead) return false;
+    }
+    *dead = 1;
+    return false;
+}
+
+// K-major, no-swizzle shared-memory matrix descriptor: 8-row groups `sbo` bytes apart, the two
+// 16-byte K chunks of one MMA `lbo` bytes apart (descriptor version 1 = sm_100).
+__device__ __forceinline__ uint64_t umma_desc(uint32_t smem_addr, uint32_t lbo, uint32_t sbo)
+{
+    return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) |
+           ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) | (1ull << 46);
+}
+__device__ __forceinline__ void umma_commit(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(dsmem_u32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&v)[8])
+{
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+__device__ __forceinline__ void dmbar_expect_tx(uint64_t *bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(dsmem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dsmem_u32(dst)), "l"(map), "r"(dsmem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, int c0, int c1, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dsmem_u32(dst)), "l"(map), "r"(dsmem_u32(bar)), "r"(c0), "r"(c1)
+        : "memory");
+}
+// K-major operand tile in the 128-byte swizzled layout (rows of 128 bytes, 8-row groups 1024
+// bytes apart, tile base 1024-byte aligned); kstep = which 32-byte slice of the row (one MMA's
+// reduction depth: 16 two-byte or 32 one-byte elements).
+__device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t smem_addr, int kstep)
+{
+    return (uint64_t)(((smem_addr + kstep * 32) >> 4) & 0x3FFFu) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+}  // namespace stmoe_dev
