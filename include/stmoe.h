@@ -83,8 +83,8 @@ typedef struct {
     int32_t n_experts;      /* routed experts per layer, <= 256 (8-bit ids in the CCT) */
     int32_t top_k;          /* K of the gating network = candidates per CCT row, <= 32 */
     int32_t n_shared;       /* always-on experts per layer (weight 1, not predicted)   */
-    int32_t hidden;         /* H, multiple of 16                                       */
-    int32_t inter;          /* I, multiple of 16                                       */
+    int32_t hidden;         /* H, multiple of 16 (STMOE_MX4: of 32)                     */
+    int32_t inter;          /* I, multiple of 16 (STMOE_MX4: of 32)                     */
     int32_t max_batch;      /* sequences decoded together, <= 64                       */
     int32_t weight_dtype;   /* expert weights; the router is fp32 for STMOE_F32, else bf16 */
     int64_t cache_slots;    /* 0: all experts resident in HBM; else number of HBM expert
@@ -138,7 +138,8 @@ int stmoe_load_router(stmoe_t *s, int layer, const void *w);
 /* Weights of experts first_expert .. first_expert+count-1 of one layer (is_shared: the
  * always-on experts).  gate, up: [count][I][H]; down: [count][H][I]; row-major in
  * weight_dtype.  scales (fp8 only, else NULL): [count][2I+H] bf16 = gate rows, up rows,
- * down rows.  Pointers may be host or device.  Synchronous: the sources are read during the call
+ * down rows.  STMOE_MX4: gate, up [count][I][H/2] and down [count][H][I/2] bytes of codes, scales
+ * [count][3*H*I/32] bytes = the scale bytes of gate, of up, of down.  Pointers may be host or device.  Synchronous: the sources are read during the call
  * (a device source must be complete: synchronise the stream that produced it first). */
 int stmoe_load_experts(stmoe_t *s, int layer, int first_expert, int count, const void *gate,
                        const void *up, const void *down, const void *scales, int is_shared);
@@ -320,9 +321,19 @@ int stmoe_predictor_step(stmoe_t *s, int layer, int batch, const int32_t *routed
  * experts: device array of n_experts expert images, each `stmoe_expert_image_bytes` long:
  * gate [I][H], up [I][H], down [H][I], then (fp8) bf16 scales [2I+H].
  * scratch: device, stmoe_moe_ffn_scratch_bytes(batch, top_k, hidden, inter) bytes,
- * 256-byte aligned; contents need not be initialised. */
+ * 256-byte aligned; contents need not be initialised.
+ *
+ * STMOE_MX4: an image is the codes of gate [I][H/2], up [I][H/2], down [H][I/2] bytes, then the scale
+ * bytes of gate, up, down; hidden and inter multiples of 32, experts 16-byte aligned, scratch
+ * stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter) bytes.  The weights go to the tensor cores
+ * as stored; an activation is held as a sum of eight 4-bit values that leaves less than 2^-22 of the
+ * largest magnitude among its 32 neighbours, and sums are fp32, so results have the precision of fp32
+ * activations.  A non-finite activation makes the 32 neighbours, and what depends on them, NaN; pairs
+ * whose id is outside [0, n_experts) add nothing.  Should a bounded wait inside a kernel run out, the
+ * outputs that depend on it are NaN. */
 size_t stmoe_expert_image_bytes(int hidden, int inter, int weight_dtype);
 size_t stmoe_moe_ffn_scratch_bytes(int batch, int top_k, int hidden, int inter);
+size_t stmoe_mx4_ffn_scratch_bytes(int batch, int top_k, int hidden, int inter);
 int stmoe_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const float *w,
                   const void *experts, int weight_dtype, int batch, int n_experts, int top_k,
                   int hidden, int inter, float residual_scale, float *h_out, void *scratch,
@@ -337,7 +348,7 @@ int stmoe_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, cons
  *   - Same arguments, layout and results as stmoe_moe_ffn; inputs and outputs stay with the
  *     caller.  Calls no cudaMalloc/cudaFree or other allocating routine.
  *   - Returns STMOE_ERR_TOO_LARGE when stmoe_moe_ffn_scratch_bytes(batch, top_k, hidden, inter)
- *     exceeds 8 MiB (for example batch 64, top_k 8, hidden 4096, inter 14336).
+ *     (STMOE_MX4: stmoe_mx4_ffn_scratch_bytes) exceeds 8 MiB (for example batch 64, top_k 8, hidden 4096, inter 14336).
  *   - The first call on each device looks up the area's device address (with that device
  *     current); make that first call before starting any stream capture, and from one host
  *     thread (later calls may come from any thread).

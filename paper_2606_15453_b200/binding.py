@@ -87,6 +87,8 @@ def lib():
         L.stmoe_expert_image_bytes.argtypes = [i32, i32, i32]
         L.stmoe_moe_ffn_scratch_bytes.restype = sz
         L.stmoe_moe_ffn_scratch_bytes.argtypes = [i32, i32, i32, i32]
+        L.stmoe_mx4_ffn_scratch_bytes.restype = sz
+        L.stmoe_mx4_ffn_scratch_bytes.argtypes = [i32, i32, i32, i32]
         L.stmoe_moe_ffn.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, f32, vp, vp, sz, vp]
         L.stmoe_moe_ffn_static.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, f32, vp, vp]
         L.stmoe_expert_ffn_dense_scratch_bytes.restype = sz
@@ -133,7 +135,7 @@ class Stack:
                  dtype="bf16", cache_slots=0, profile_tokens=0, mode="st", flags=0,
                  prefetch_limit=0, rms_eps=1e-6, residual_scale=0.1):
         self.cfg = Config(n_layers, n_experts, top_k, n_shared, hidden, inter, max_batch,
-                          DTYPE[dtype], cache_slots, profile_tokens, MODE[mode], flags,
+                          WEIGHT_DTYPE[dtype], cache_slots, profile_tokens, MODE[mode], flags,
                           prefetch_limit, rms_eps, residual_scale)
         self._h = C.c_void_p()
         _check(lib().stmoe_create(C.byref(self.cfg), C.byref(self._h)), "stmoe_create")
@@ -162,7 +164,8 @@ class Stack:
         _check(lib().stmoe_load_router(self._h, layer, _ptr(w)), "stmoe_load_router")
 
     def load_experts(self, layer, first_expert, gate, up, down, scales=None, shared=False) -> None:
-        """gate/up [n][I][H], down [n][H][I] (or 2-D for one expert), host or device.  The call copies
+        """gate/up [n][I][H], down [n][H][I] (or 2-D for one expert), host or device; dtype "mx4": uint8
+        codes [n][I][H/2], [n][H][I/2] and scales (mx4_expert).  The call copies
         at once and does not know torch's streams: synchronise the stream that produced a device
         source before calling."""
         count = 1 if gate.dim() == 2 else gate.shape[0]
@@ -270,10 +273,12 @@ def router_topk(h, w_router, top_k, rms_eps=1e-6, renorm=False, stream=None):
 
 
 def expert_image_bytes(hidden, inter, dtype) -> int:
-    return lib().stmoe_expert_image_bytes(hidden, inter, DTYPE[dtype])
+    return lib().stmoe_expert_image_bytes(hidden, inter, WEIGHT_DTYPE[dtype])
 
 
-def moe_ffn_scratch_bytes(batch, top_k, hidden, inter) -> int:
+def moe_ffn_scratch_bytes(batch, top_k, hidden, inter, dtype="bf16") -> int:
+    if dtype == "mx4":
+        return lib().stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter)
     return lib().stmoe_moe_ffn_scratch_bytes(batch, top_k, hidden, inter)
 
 
@@ -284,7 +289,7 @@ def moe_ffn(h, inv_rms, ids, w, experts, dtype, n_experts, hidden, inter, residu
     B, K = ids.shape
     fn = getattr(lib(), entry)
     _check(fn(_dev(h, torch.float32), _ptr(inv_rms), _dev(ids, torch.int32), _dev(w, torch.float32),
-              _dev(experts), DTYPE[dtype], B, n_experts, K, hidden, inter, residual_scale,
+              _dev(experts), WEIGHT_DTYPE[dtype], B, n_experts, K, hidden, inter, residual_scale,
               _dev(h_out, torch.float32), _dev(scratch), scratch.numel() * scratch.element_size(),
               _stream(stream)), entry)
     return h_out
@@ -297,7 +302,7 @@ def moe_ffn_static(h, inv_rms, ids, w, experts, dtype, n_experts, hidden, inter,
     device (order calls that could overlap).  Raises StmoeError when the problem needs more."""
     B, K = ids.shape
     _check(lib().stmoe_moe_ffn_static(_dev(h, torch.float32), _ptr(inv_rms), _dev(ids, torch.int32),
-                                      _dev(w, torch.float32), _dev(experts), DTYPE[dtype], B, n_experts, K,
+                                      _dev(w, torch.float32), _dev(experts), WEIGHT_DTYPE[dtype], B, n_experts, K,
                                       hidden, inter, residual_scale, _dev(h_out, torch.float32),
                                       _stream(stream)), "stmoe_moe_ffn_static")
     return h_out
@@ -393,6 +398,29 @@ def mx4_dequantize(codes, scales, cols, dtype=torch.float32, out=None, stream=No
                                               y.data_ptr(), _ELEM[dtype], y.stride(0), st), "stmoe_mx4_dequantize")
         return y
     return _on_device(codes, stream, call)
+
+
+def mx4_expert(gate, up, down, stream=None):
+    """One expert's matrices (gate, up [I][H], down [H][I]; fp32, bf16 or fp16; H and I multiples of 32)
+    quantised: dict(gate, up, down: codes; scales: those of the three, one after the other) for
+    Stack.load_experts, and image: the same as one expert image for moe_ffn (the others are views
+    into it)."""
+    I, H = _rows2(gate, "gate").shape
+    _need(H % 32 == 0 and I % 32 == 0, "hidden and inter have to be multiples of 32")
+    _need(tuple(up.shape) == (I, H) and tuple(down.shape) == (H, I), "gate and up are [I][H], down is [H][I]")
+    _same_device(gate, up, down)
+
+    def call(st):
+        n, nc, ns = expert_image_bytes(H, I, "mx4"), H * I // 2, H * I // 32
+        image = torch.empty(n, dtype=torch.uint8, device=gate.device)
+        image[3 * (nc + ns):].zero_()
+        parts = {"image": image, "scales": image[3 * nc:3 * (nc + ns)]}
+        for i, (name, w) in enumerate((("gate", gate), ("up", up), ("down", down))):
+            r, c = w.shape
+            parts[name] = image[i * nc:(i + 1) * nc].view(r, c // 2)
+            mx4_quantize(w, parts[name], image[3 * nc + i * ns:3 * nc + (i + 1) * ns].view(r, c // 32))
+        return parts
+    return _on_device(gate, stream, call)
 
 
 def mx4_matmul(a, b, counts=None, dtype=torch.bfloat16, out=None, flags=None, stream=None):

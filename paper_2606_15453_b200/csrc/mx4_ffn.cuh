@@ -1,0 +1,508 @@
+// Routed SwiGLU expert FFN over 4-bit expert images (MX4 weights, fp32 hidden state):
+//
+//   h'[b] = h[b] + r * sum_k w[b][k] * W_d ( silu(W_g x_b) * (W_u x_b) ),   x_b = h[b] * inv_rms[b]
+//
+// A decode step is bound by reading the routed experts' images once (51/32 bytes per hidden x inter
+// element).  The codes go from HBM to the tensor cores as they are (tcgen05.mma kind::mxf4, TMA in
+// the 128-byte swizzled layout, block scales through tensor memory as in mx4_matmul.cuh): unpacking
+// them to fp32 would cost the CUDA cores two conversions and an FMA per weight and token, three times
+// what they can issue at 6.5 TB/s of 4-bit weights.
+//
+// The tensor cores' 4-bit form takes 4-bit activations, which alone would be far too coarse.  So an
+// activation is written as a sum of eight e2m1 values (planes) under scales that fall by a fixed
+// amount, a fixed-point expansion of the block:
+//   e_0: the smallest exponent with amax <= 6 * 2^e_0;   e_1 = e_0 - 2;   e_p = e_(p-1) - 3
+// Rounding at plane 0 leaves at most 2^e_0 = 4 * 2^e_1 (e2m1 steps by 2 up to 6), rounding a value of
+// at most 4 leaves at most 1/2, which is 4 units three binary orders below.  After eight planes the
+// residue is at most 2^(e_0 - 21), below 2^-22 of the block's largest magnitude: the precision of the
+// fp32 values they stand for.  The exponents do not depend on the residues, so all planes of a block
+// follow from one maximum.  The planes are further columns of the MMA's N: a token is eight of them,
+// and eight rows of 128 bytes are exactly one atom of the swizzled operand layout, so an entry's
+// tokens are gathered by one TMA load each.  The epilogue adds a token's eight columns in fp32,
+// smallest plane first.
+//
+//   mx4_planes_kernel    hidden state -> planes (and, for the stand-alone call, the work list)
+//   mx4_ffn_kernel<2>    gate and up tiles of 128 rows; epilogue: SiLU(g) * u as planes (a warp's 32
+//                        rows are one block of the next reduction, so a block maximum is one
+//                        warp reduction)
+//   mx4_ffn_kernel<1>    down tiles -> partial sums [pair][split][H]
+//   mx4_combine_kernel   weighted sum and residual in a fixed order
+// Every launch may start while the one before drains (programmatic dependent launch) and waits for
+// its results itself.  Sums have a fixed order: the same call gives the same bits.
+#pragma once
+#include "ffn.cuh"
+#include "mx4.cuh"
+#include "mx4_matmul.cuh"
+
+namespace stmoe_dev {
+
+constexpr int kPlanes = 8;
+constexpr int kMxfTokens = 12;                          // tokens of a work-list entry: 96 MMA columns
+constexpr int kMxfCols = kMxfTokens * kPlanes;
+constexpr int kMxfAccStride = 2 * kMxfCols;             // two accumulator buffers of (gate, up)
+constexpr int kMxfScaleCol = 2 * kMxfAccStride;
+constexpr int kMxfMaxStages = 12;
+
+// the B tile of a launch whose entries hold at most mt tokens: N is a multiple of 16
+__host__ __device__ constexpr int mxf_cols(int tokens) { return (tokens * kPlanes + 15) / 16 * 16; }
+__host__ __device__ constexpr int mxf_slot_bytes(int nmat, int mt)
+{
+    return nmat * (kMmABytes + 1024) + mxf_cols(mt) * 128 + 1024;   // codes and scales of both operands
+}
+__host__ __device__ constexpr int mxf_stages(int nmat, int mt)
+{
+    const int by_smem = (kMmSmemBytes - 1024) / mxf_slot_bytes(nmat, mt), by_tmem = (512 - kMxfScaleCol) / (8 * nmat + 8);
+    const int n = by_smem < by_tmem ? by_smem : by_tmem;
+    return n < kMxfMaxStages ? n : kMxfMaxStages;
+}
+
+// Byte offsets inside an MX4 expert image: codes of gate [I][H/2], up, down [H][I/2], then the
+// scales of the three in the same order.
+__host__ __device__ inline size_t mx4_image_codes(int H, int I, int mat) { return (size_t)mat * ((size_t)H * I / 2); }
+__host__ __device__ inline size_t mx4_image_scales(int H, int I, int mat)
+{
+    return 3 * ((size_t)H * I / 2) + (size_t)mat * ((size_t)H * I / 32);
+}
+
+// ---- activations as planes ---------------------------------------------------------------------
+
+// The planes of one block: every lane holds one element, returns the word of its eight codes (plane p
+// in bits 4p) and the scale byte of plane 0.
+__device__ __forceinline__ uint32_t planes_of(float v, uint32_t &byte)
+{
+    const uint32_t m = __reduce_max_sync(kFull, __float_as_uint(v) & 0x7fffffffu);
+    const int ef = (int)(m >> 23);
+    if (ef == 255) {  // infinity or NaN: the block is NaN in every plane
+        byte = 255;
+        return 0;
+    }
+    // amax = f * 2^(ef-127), f in [1,2): f <= 1.5 fits under 6 * 2^(ef-129), else one binary order more
+    byte = (uint32_t)max(ef - 2 + ((m & 0x7fffffu) > 0x400000u ? 1 : 0), 0);
+    uint32_t codes = 0;
+    const int b = (int)byte;
+    const float up = __uint_as_float((uint32_t)(254 - b) << 23);   // 2^-(b-127): b <= 253, so a normal number
+    v *= up;
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p) {
+        uint32_t c, f;
+        asm("{.reg .b8 q;\n\t"
+            "cvt.rn.satfinite.e2m1x2.f32 q, %2, %2;\n\t"
+            "cvt.rn.f16x2.e2m1x2 %1, q;\n\t"
+            "cvt.u32.u8 %0, q;}"
+            : "=r"(c), "=r"(f)
+            : "f"(v));
+        const int off = p == 0 ? 0 : 3 * p - 1;
+        if (b >= off) codes |= (c & 15u) << (4 * p);   // a plane below the smallest scale is dropped
+        v -= __low2float(*reinterpret_cast<const __half2 *>(&f));   // exact: at most half a step is left
+        v *= p == 0 ? 4.f : 8.f;                                    // to the next plane's units
+    }
+    return codes;
+}
+// scale byte of plane p: exponents fall by 2, then by 3
+__device__ __forceinline__ uint32_t plane_byte(uint32_t byte, int p)
+{
+    return byte == 255 ? 255u : (uint32_t)max((int)byte - (p == 0 ? 0 : 3 * p - 1), 0);
+}
+// lane l: eight codes of element l -> the four bytes of plane l%8 that hold elements 8*(l/8) .. +7
+__device__ __forceinline__ uint32_t planes_transpose(uint32_t x, int lane)
+{
+    uint32_t r = __shfl_xor_sync(kFull, x, 4);
+    x = lane & 4 ? (r >> 16) | (x & 0xffff0000u) : (x & 0x0000ffffu) | (r << 16);
+    r = __shfl_xor_sync(kFull, x, 2);
+    x = lane & 2 ? ((r >> 8) & 0x00ff00ffu) | (x & 0xff00ff00u) : (x & 0x00ff00ffu) | ((r << 8) & 0xff00ff00u);
+    r = __shfl_xor_sync(kFull, x, 1);
+    x = lane & 1 ? ((r >> 4) & 0x0f0f0f0fu) | (x & 0xf0f0f0f0u) : (x & 0x0f0f0f0fu) | ((r << 4) & 0xf0f0f0f0u);
+    return x;
+}
+// A warp stores block `blk` of row `row` (token or pair): codes [row][8][blocks*16], scales [row][8][blocks].
+__device__ __forceinline__ void planes_store(float v, uint8_t *codes, uint8_t *scales, long long row, int blk, int blocks, int lane)
+{
+    uint32_t byte;
+    const uint32_t w = planes_transpose(planes_of(v, byte), lane);
+    const int p = lane % kPlanes;
+    *reinterpret_cast<uint32_t *>(codes + ((row * kPlanes + p) * blocks + blk) * 16 + 4 * (lane / kPlanes)) = w;
+    if (lane < kPlanes) scales[(row * kPlanes + lane) * blocks + blk] = (uint8_t)plane_byte(byte, lane);
+}
+
+struct Mx4PlanesArgs {
+    const float *h;
+    int B, H;
+    uint8_t *codes, *scales;
+    // stand-alone call: the work list of given routing (n_group_ctas = 1), else 0
+    int group_ctas;
+    const int32_t *ids;
+    int E, K, mt;
+    WorkList wl;
+    const uint8_t *experts;
+    size_t img_bytes;
+    const uint8_t **table;
+};
+
+// Entries of at most mt tokens per expert from given ids, pairs of an expert in index order.  ids
+// outside [0, E) have no entry.  One CTA of 256 threads, one thread an expert; s_ids: B*K ints.
+__device__ __forceinline__ void group_ids(const Mx4PlanesArgs &a, int *s_ids, int *s_g, int *s_p)
+{
+    const int e = threadIdx.x, n = a.B * a.K;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) s_ids[i] = a.ids[i];
+    __syncthreads();
+    int cnt = 0;
+    if (e < a.E)
+        for (int i = 0; i < n; ++i) cnt += s_ids[i] == e;
+    const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+    int g = (cnt + a.mt - 1) / a.mt, p = cnt;   // inclusive prefix sums over the experts
+#pragma unroll
+    for (int o = 1; o < kWarp; o <<= 1) {
+        const int tg = __shfl_up_sync(kFull, g, o), tp = __shfl_up_sync(kFull, p, o);
+        if (lane >= o) g += tg, p += tp;
+    }
+    if (lane == kWarp - 1) s_g[warp] = g, s_p[warp] = p;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) g += s_g[w], p += s_p[w];
+    if (e == 255) *a.wl.n_groups = g;
+    g -= (cnt + a.mt - 1) / a.mt, p -= cnt;
+    if (e < a.E) {
+        a.table[e] = a.experts + (size_t)e * a.img_bytes;
+        for (int t = 0, q = g; t < cnt; t += a.mt, ++q)
+            a.wl.g_expert[q] = e, a.wl.g_start[q] = p + t, a.wl.g_count[q] = min(a.mt, cnt - t);
+        for (int i = 0; cnt && i < n; ++i)
+            if (s_ids[i] == e) a.wl.pair_token[p] = i / a.K, a.wl.pair_slot[p] = i, ++p;
+    }
+}
+
+__global__ void __launch_bounds__(256) mx4_planes_kernel(const Mx4PlanesArgs a)
+{
+    extern __shared__ int s_ids[];
+    __shared__ int s_g[8], s_p[8];
+    pdl_launch_dependents();
+    pdl_wait();
+    if ((int)blockIdx.x < a.group_ctas) {
+        group_ids(a, s_ids, s_g, s_p);
+        return;
+    }
+    const int blocks = a.H / kMxBlock, lane = threadIdx.x % kWarp;
+    const int n = a.B * blocks, step = ((int)gridDim.x - a.group_ctas) * (256 / kWarp);
+    for (int i = ((int)blockIdx.x - a.group_ctas) * (256 / kWarp) + threadIdx.x / kWarp; i < n; i += step) {
+        const int b = i / blocks, blk = i % blocks;
+        planes_store(a.h[(size_t)b * a.H + blk * kMxBlock + lane], a.codes, a.scales, b, blk, blocks, lane);
+    }
+}
+
+// ---- the two projections ------------------------------------------------------------------------
+
+struct Mx4FfnArgs {
+    WorkList wl;
+    int E;
+    const uint8_t *const *blob;          // image of every expert of the step
+    const uint8_t *store[2];             // first image of the maps: routed experts, experts >= E
+    unsigned long long img_bytes;
+    long long scale_off[2];              // scales of the one or two matrices inside an image
+    int rows, blocks;                    // rows of a matrix, scale blocks of its row
+    int mt, splits;                      // splits: of the reduction, over a cluster (gate/up) or over tasks (down)
+    const uint8_t *x_scales;             // planes of the activations, [row][8][blocks]
+    // gate/up
+    const float *inv_rms;
+    uint8_t *act_codes, *act_scales;     // [pair][8][rows/32 * 16], [pair][8][rows/32]
+    // down
+    float *part;                         // [pair][splits][rows]
+    unsigned *err;
+    int w_align;                         // alignment of a weight matrix's scale rows: 8, 4 or 1
+};
+
+// eight scale bytes from block kb on, by the widest loads the rows' alignment allows
+__device__ __forceinline__ uint2 load_scales8_by(const uint8_t *row, int kb, int blocks, int align)
+{
+    if (align == 4 && kb + 8 <= blocks)
+        return make_uint2(__ldg(reinterpret_cast<const uint32_t *>(row + kb)), __ldg(reinterpret_cast<const uint32_t *>(row + kb) + 1));
+    return load_scales8(row, kb, blocks, align == 8);
+}
+
+struct Mx4FfnTask {
+    int g, row0, z;
+};
+template <int NMAT> __device__ __forceinline__ Mx4FfnTask mxf_task(const Mx4FfnArgs &a, int task)
+{
+    const int tiles = (a.rows + kMmRows - 1) / kMmRows, zs = NMAT == 1 ? a.splits : 1;
+    Mx4FfnTask t;
+    t.g = task / (tiles * zs);
+    const int r = task - t.g * tiles * zs;
+    t.row0 = (r / zs) * kMmRows;
+    t.z = r % zs;
+    return t;
+}
+
+// SiLU(g) * u for 32 consecutive rows of one pair, as planes
+__device__ __forceinline__ void mxf_store_act(const Mx4FfnArgs &a, float g, float u, int pair, int row, int lane)
+{
+    const int slot = a.wl.pair_slot[pair];
+    const float inv = a.inv_rms ? a.inv_rms[a.wl.pair_token[pair]] : 1.f;  // W (inv * h) = inv * (W h)
+    g *= inv, u *= inv;
+    planes_store(g / (1.f + expf(-g)) * u, a.act_codes, a.act_scales, slot, row / kMxBlock, a.rows / kMxBlock, lane);
+}
+
+template <int NMAT>
+__global__ void __launch_bounds__(kMmThreads, 1)
+mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1,
+               const __grid_constant__ CUtensorMap map_s0, const __grid_constant__ CUtensorMap map_s1,
+               const __grid_constant__ CUtensorMap map_x, const Mx4FfnArgs a)
+{
+    extern __shared__ uint8_t dsm_raw[];
+    __shared__ uint64_t full[kMxfMaxStages], empty[kMxfMaxStages], tfull[2], tempty[2];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_dead;
+    const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp;
+    uint8_t *dsm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dsm_raw) + 1023) & ~(uintptr_t)1023);
+    const int NS = mxf_stages(NMAT, a.mt), slot = mxf_slot_bytes(NMAT, a.mt);
+    const int x_at = NMAT * kMmABytes, sfa_at = x_at + mxf_cols(a.mt) * 128, sfb_at = sfa_at + NMAT * 1024;
+    constexpr int kSetCols = 8 * NMAT + 8;   // tensor-memory columns of a stage's scales
+
+    pdl_launch_dependents();
+    if (tid == 0) {
+        s_dead = 0;
+        for (int s = 0; s < NS; ++s) dmbar_init(&full[s], 1 + 4), dmbar_init(&empty[s], 1);
+        for (int b = 0; b < 2; ++b) dmbar_init(&tfull[b], 1), dmbar_init(&tempty[b], 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dsmem_u32(&s_tmem)), "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    volatile int *dead = &s_dead;
+    pdl_wait();   // the work list and the planes are the kernel before's
+
+    const int ranks = NMAT == 2 ? a.splits : 1;   // CTAs of a cluster that share a task's reduction
+    const int tiles = (a.rows + kMmRows - 1) / kMmRows;
+    const int n_tasks = *a.wl.n_groups * tiles * (NMAT == 1 ? a.splits : 1);
+    const int rank = blockIdx.x % ranks, first = blockIdx.x / ranks, step = gridDim.x / ranks;
+    const int n_steps = (a.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
+    auto k_range = [&](int z, int &beg, int &end) {
+        const int q = NMAT == 2 ? rank : z;
+        beg = (int)((long long)n_steps * q / a.splits), end = (int)((long long)n_steps * (q + 1) / a.splits);
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0, issued = 0;
+            uint32_t par = 0;
+            for (int task = first; task < n_tasks && !*dead; task += step) {
+                const Mx4FfnTask t = mxf_task<NMAT>(a, task);
+                const int ge = a.wl.g_expert[t.g], start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
+                const bool shared = ge >= a.E;
+                const int img = (int)((unsigned long long)(a.blob[ge] - a.store[shared]) / a.img_bytes);
+                const CUtensorMap *w0 = shared ? &map_s0 : &map_w0, *w1 = shared ? &map_s1 : &map_w1;
+                int row[kMxfTokens];
+#pragma unroll
+                for (int i = 0; i < kMxfTokens; ++i)
+                    if (i < cnt) row[i] = kPlanes * (NMAT == 2 ? a.wl.pair_token[start + i] : a.wl.pair_slot[start + i]);
+                int k_beg, k_end;
+                k_range(t.z, k_beg, k_end);
+                for (int k = k_beg; k < k_end; ++k, ++issued) {
+                    if (!dmbar_wait(&empty[s], par ^ 1u, dead)) break;
+                    uint8_t *st = dsm + (size_t)s * slot;
+                    dmbar_expect_tx(&full[s], (uint32_t)(NMAT * kMmABytes + cnt * kPlanes * 128));
+                    tma_load_3d(st, w0, k * 128, t.row0, img, &full[s]);
+                    if (NMAT == 2) tma_load_3d(st + kMmABytes, w1, k * 128, t.row0, img, &full[s]);
+#pragma unroll
+                    for (int i = 0; i < kMxfTokens; ++i)
+                        if (i < cnt) tma_load_2d(st + x_at + i * kPlanes * 128, &map_x, k * 128, row[i], &full[s]);
+                    if (++s == NS) s = 0, par ^= 1u;
+                }
+            }
+            int none = 0;   // every load that was issued lands before the CTA may exit, after an error too
+            for (int i = 0; i < min(issued, NS); ++i) {
+                if (s == 0) s = NS, par ^= 1u;
+                --s;
+                dmbar_wait(&full[s], par, &none, 1 << 14);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int s = 0, it = 0;
+            uint32_t par = 0;
+            for (int task = first; task < n_tasks && !*dead; task += step, ++it) {
+                const Mx4FfnTask t = mxf_task<NMAT>(a, task);
+                const int n = mxf_cols(a.wl.g_count[t.g]);
+                const uint32_t id0 = umma_idesc_mxf4(n, 0), id1 = umma_idesc_mxf4(n, 1);
+                const int ab = it & 1;
+                if (!dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t acc = tmem + ab * kMxfAccStride;
+                int k_beg, k_end;
+                k_range(t.z, k_beg, k_end);
+                bool ok = true;
+                for (int k = k_beg; k < k_end; ++k) {
+                    if (!(ok = dmbar_wait(&full[s], par, dead))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t st = dsmem_u32(dsm + (size_t)s * slot);
+                    const uint32_t sf = tmem + kMxfScaleCol + s * kSetCols, sfb = sf + 8 * NMAT;
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                        for (int m = 0; m < NMAT; ++m) umma_copy_scales(sf + 8 * m + 4 * q, st + sfa_at + 1024 * m + 512 * q);
+                        umma_copy_scales(sfb + 4 * q, st + sfb_at + 512 * q);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int m = 0; m < NMAT; ++m)
+                            umma_mxf4(acc + m * kMxfCols, umma_desc_sw128(st + m * kMmABytes, j), umma_desc_sw128(st + x_at, j),
+                                      j & 1 ? id1 : id0, sf + 8 * m + 4 * (j / 2), sfb + 4 * (j / 2), k > k_beg || j > 0);
+                    umma_commit(&empty[s]);
+                    if (++s == NS) s = 0, par ^= 1u;
+                }
+                if (!ok) break;
+                umma_commit(&tfull[ab]);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 6) {
+        const int lg = warp % 4;
+        float *part = reinterpret_cast<float *>(dsm);   // cluster: this rank's sums [mat][token][128], in the idle ring
+        int it = 0;
+        for (int task = first; task < n_tasks; task += step, ++it) {
+            const int ab = it & 1;
+            const Mx4FfnTask t = mxf_task<NMAT>(a, task);
+            const int start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
+            const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], (uint32_t)(it >> 1) & 1u, dead));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + ab * kMxfAccStride + ((uint32_t)(lg * kWarp) << 16);
+            const int row = t.row0 + lg * kWarp + lane;
+            for (int i = 0; i < cnt; ++i) {
+                float y[NMAT];
+#pragma unroll
+                for (int m = 0; m < NMAT; ++m) {
+                    float v[8];
+                    tmem_ld8(acc + m * kMxfCols + i * kPlanes, v);
+                    y[m] = v[7];
+#pragma unroll
+                    for (int p = 6; p >= 0; --p) y[m] += v[p];
+                    if (!ok) y[m] = __uint_as_float(0x7fffffffu);
+                }
+                if (NMAT == 1) {
+                    if (row < a.rows)
+                        a.part[((long long)a.wl.pair_slot[start + i] * a.splits + t.z) * a.rows + row] = y[0];
+                } else if (ranks > 1) {
+#pragma unroll
+                    for (int m = 0; m < NMAT; ++m) part[(m * kMxfTokens + i) * kMmRows + lg * kWarp + lane] = y[m];
+                } else if (t.row0 + lg * kWarp < a.rows) {   // rows are a multiple of 32: the whole warp or none of it
+                    mxf_store_act(a, y[0], y[NMAT - 1], start + i, row, lane);
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) dmbar_arrive(&tempty[ab]);
+            if (!ok) break;
+        }
+    } else {
+        // scales: thread = row of the weight tiles, and a plane of a token
+        const int r = tid - 6 * kWarp;
+        const uint32_t at = (uint32_t)((r % 32) * 16 + (r / 32) * 4);
+        int s = 0;
+        uint32_t par = 0;
+        bool ok = true;
+        for (int task = first; task < n_tasks && ok; task += step) {
+            const Mx4FfnTask t = mxf_task<NMAT>(a, task);
+            const int ge = a.wl.g_expert[t.g], start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
+            const uint8_t *img = a.blob[ge];
+            const long long wrow = (long long)min(t.row0 + r, a.rows - 1) * a.blocks;
+            const uint8_t *pw[NMAT];
+#pragma unroll
+            for (int m = 0; m < NMAT; ++m) pw[m] = img + a.scale_off[m] + wrow;
+            const bool has_x = r < cnt * kPlanes;
+            const uint8_t *px = nullptr;
+            if (has_x) {
+                const int pair = start + r / kPlanes;
+                px = a.x_scales + ((long long)(NMAT == 2 ? a.wl.pair_token[pair] : a.wl.pair_slot[pair]) * kPlanes + r % kPlanes) * a.blocks;
+            }
+            const int x_align = a.blocks % 8 == 0 ? 8 : a.blocks % 4 == 0 ? 4 : 1;
+            int k_beg, k_end;
+            k_range(t.z, k_beg, k_end);
+            for (int k0 = k_beg; k0 < k_end && ok; k0 += 4) {
+                uint2 vw[4][NMAT], vx[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int kb = min(k0 + i, n_steps - 1) * kMmStageBlocks;
+#pragma unroll
+                    for (int m = 0; m < NMAT; ++m) vw[i][m] = load_scales8_by(pw[m], kb, a.blocks, a.w_align);
+                    if (has_x) vx[i] = load_scales8_by(px, kb, a.blocks, x_align);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (k0 + i < k_end && ok) {
+                        ok = __all_sync(kFull, dmbar_wait(&empty[s], par ^ 1u, dead));
+                        uint8_t *st = dsm + (size_t)s * slot;
+#pragma unroll
+                        for (int m = 0; m < NMAT; ++m) {
+                            *reinterpret_cast<uint32_t *>(st + sfa_at + 1024 * m + at) = vw[i][m].x;
+                            *reinterpret_cast<uint32_t *>(st + sfa_at + 1024 * m + 512 + at) = vw[i][m].y;
+                        }
+                        if (has_x) {
+                            *reinterpret_cast<uint32_t *>(st + sfb_at + at) = vx[i].x;
+                            *reinterpret_cast<uint32_t *>(st + sfb_at + 512 + at) = vx[i].y;
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) dmbar_arrive(&full[s]);
+                        if (++s == NS) s = 0, par ^= 1u;
+                    }
+                }
+            }
+        }
+    }
+    if (NMAT == 2 && ranks > 1 && first < n_tasks) {   // one task per cluster
+        __syncwarp();
+        cluster_sync();
+        const Mx4FfnTask t = mxf_task<NMAT>(a, first);
+        const int start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
+        const uint32_t part = dsmem_u32(dsm);
+        // (token, 32 rows) units, dealt to the ranks and their warps
+        for (int u = rank + ranks * warp; u < cnt * 4; u += ranks * (kMmThreads / kWarp)) {
+            const int i = u / 4, r0 = (u % 4) * kWarp;
+            if (t.row0 + r0 >= a.rows) continue;
+            float g = 0.f, v = 0.f;
+            for (int z = 0; z < ranks; ++z) {
+                g += ld_cluster(part + (uint32_t)(i * kMmRows + r0 + lane) * 4, z);
+                v += ld_cluster(part + (uint32_t)((kMxfTokens + i) * kMmRows + r0 + lane) * 4, z);
+            }
+            mxf_store_act(a, g, v, start + i, t.row0 + r0 + lane, lane);
+        }
+        cluster_sync();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+    if (tid == 0 && s_dead && a.err) *a.err = 1u;
+}
+
+// h_out[b][c] = h[b][c] + r * (weighted sum of the down projection's partial sums), in a fixed order:
+// shared experts, then routed ones, splits innermost.  ids (stand-alone call): a pair whose id names
+// no expert has no partial sums and adds nothing.
+__global__ void __launch_bounds__(256) mx4_combine_kernel(const FfnArgs a, const int32_t *ids)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int KS = a.K + a.n_shared;
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < a.B * a.H; i += gridDim.x * blockDim.x) {
+        const int b = i / a.H, c = i % a.H;
+        float y = 0.f;
+        for (int q = 0; q < KS; ++q) {
+            const int k = q < a.n_shared ? a.K + q : q - a.n_shared;
+            if (ids && (unsigned)ids[b * a.K + k] >= (unsigned)a.E) continue;
+            const float *part = a.part + ((long long)(b * KS + k) * a.S) * a.H + c;
+            float p = 0.f;
+#pragma unroll 4
+            for (int z = 0; z < a.S; ++z) p += __ldcg(part + (long long)z * a.H);
+            y = q < a.n_shared ? y + p : fmaf(a.w[b * a.K + k], p, y);
+        }
+        a.h_out[i] = fmaf(a.residual_scale, y, a.h[i]);
+    }
+}
+
+}  // namespace stmoe_dev

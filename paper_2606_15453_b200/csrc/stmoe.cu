@@ -2,6 +2,7 @@
 // tables, the HBM slot cache with its copy stream and event fences, kernel launches.
 #include "../../include/stmoe.h"
 
+#include <algorithm>
 #include <atomic>
 #include <chrono>
 #include <cstdio>
@@ -18,6 +19,7 @@
 #include "dense_group.cuh"
 #include "device_utils.cuh"
 #include "ffn.cuh"
+#include "mx4_ffn.cuh"
 #include "predictor.cuh"
 #include "router.cuh"
 #include "token_dense_kernel.cuh"
@@ -57,6 +59,7 @@ int down_splits(int I, int dt)
 
 size_t image_bytes(int H, int I, int dt)
 {
+    if (dt == STMOE_MX4) return round_up(3 * ((size_t)H * I / 2 + (size_t)H * I / 32), 256);
     size_t n = 3 * (size_t)H * I * dtype_bytes(dt);
     if (dt == STMOE_FP8_E4M3) n += 2 * (size_t)(2 * I + H);
     return round_up(n, 256);
@@ -323,6 +326,161 @@ struct SlotCache {
     }
 };
 
+// ---- 4-bit expert FFN (mx4_ffn.cuh) -------------------------------------------------------
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+struct Mx4FfnMaps {
+    CUtensorMap gate[2], up[2], down[2];   // [0]: images of the routed experts, [1]: of the shared ones
+    const uint8_t *store[2];               // first image of either
+    CUtensorMap x, act;
+};
+struct Mx4FfnBufs {
+    uint8_t *x_codes, *x_scales, *act_codes, *act_scales;
+    float *part;
+};
+// splits of the down projection's reduction that the partial sums have room for
+int mx4_max_splits(int pairs, int I)
+{
+    const int steps = (I / kMxBlock + kMmStageBlocks - 1) / kMmStageBlocks, cap = pairs <= 32 ? 8 : pairs <= 128 ? 4 : 2;
+    return std::min(steps, cap);
+}
+// lays the buffers out behind base (nullptr: only the size)
+size_t mx4_buffers(uint8_t *base, int B, int pairs, int H, int I, Mx4FfnBufs *b)
+{
+    size_t o = 0;
+    auto take = [&](size_t n) {
+        uint8_t *p = base ? base + o : nullptr;
+        o += round_up(n, 256);
+        return p;
+    };
+    b->x_codes = take((size_t)B * kPlanes * H / 2);
+    b->x_scales = take((size_t)B * kPlanes * H / kMxBlock);
+    b->act_codes = take((size_t)pairs * kPlanes * I / 2);
+    b->act_scales = take((size_t)pairs * kPlanes * I / kMxBlock);
+    b->part = (float *)take(sizeof(float) * (size_t)pairs * mx4_max_splits(pairs, I) * H);
+    return o;
+}
+int mx4_entry_tokens(int B) { return std::min(B, kMxfTokens); }
+
+EncodeTiledFn encode_tiled_fn()
+{
+    static EncodeTiledFn fn = nullptr;   // the same value whoever fills it
+    if (!fn) {
+        void *sym = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = (EncodeTiledFn)sym;
+        (void)cudaGetLastError();
+    }
+    return fn;
+}
+// codes in rows of row_bytes: boxes of 128 bytes x box_rows rows, 128-byte swizzle, zeros outside;
+// images > 0: a third dimension, img_bytes apart
+int mx4_map(CUtensorMap *m, const uint8_t *base, int64_t row_bytes, int64_t rows, int box_rows, int64_t images, int64_t img_bytes)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)row_bytes, (cuuint64_t)rows, (cuuint64_t)images};
+    const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)img_bytes};
+    const cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1}, es[3] = {1, 1, 1};
+    EncodeTiledFn fn = encode_tiled_fn();
+    return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, images > 0 ? 3 : 2, (void *)base, dims, strides, box, es,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? STMOE_OK
+               : STMOE_ERR_CUDA;
+}
+int mx4_weight_maps(Mx4FfnMaps *m, int which, const uint8_t *store, int64_t images, size_t img_bytes, int H, int I)
+{
+    m->store[which] = store;
+    ST_TRY(mx4_map(&m->gate[which], store + mx4_image_codes(H, I, 0), H / 2, I, kMmRows, images, img_bytes));
+    ST_TRY(mx4_map(&m->up[which], store + mx4_image_codes(H, I, 1), H / 2, I, kMmRows, images, img_bytes));
+    return mx4_map(&m->down[which], store + mx4_image_codes(H, I, 2), I / 2, H, kMmRows, images, img_bytes);
+}
+int mx4_act_maps(Mx4FfnMaps *m, const Mx4FfnBufs &b, int B, int pairs, int H, int I)
+{
+    ST_TRY(mx4_map(&m->x, b.x_codes, H / 2, (int64_t)B * kPlanes, kPlanes, 0, 0));
+    return mx4_map(&m->act, b.act_codes, I / 2, (int64_t)pairs * kPlanes, kPlanes, 0, 0);
+}
+
+// launch behind the kernel before it in the stream (programmatic dependent launch), in clusters
+template <typename... P, typename... A>
+int mx4_launch(void (*kernel)(P...), int grid, int block, size_t smem, int cluster, cudaStream_t st, const A &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
+    CU_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    return STMOE_OK;
+}
+int mx4_prepare_kernels(int dev)
+{
+    static bool ready[64];
+    if (dev < 0 || dev >= 64) return STMOE_ERR_BAD_ARG;
+    if (!ready[dev]) {
+        CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        ready[dev] = true;
+    }
+    return STMOE_OK;
+}
+
+// The FFN of one layer step; pa: the planes kernel's arguments (with grouping for the stand-alone
+// call, fa: inputs, outputs and work list as for the other formats; mark(i): called before the first
+// launch, between the projections and behind the last launch.
+template <typename Mark>
+int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnArgs fa, size_t img_bytes, unsigned *err, int sms,
+            cudaStream_t st, Mark mark)
+{
+    ST_TRY(mark(0));
+    const int H = fa.H, I = fa.I, pairs = fa.B * (fa.K + fa.n_shared), mt = mx4_entry_tokens(fa.B);
+    pa.h = fa.h, pa.B = fa.B, pa.H = H, pa.codes = b.x_codes, pa.scales = b.x_scales;
+    const int blocks = fa.B * H / kMxBlock;
+    ST_TRY(mx4_launch(mx4_planes_kernel, pa.group_ctas + std::min(sms * 4, (blocks + 7) / 8), 256,
+                      pa.group_ctas ? sizeof(int) * (size_t)fa.B * fa.K : 0, 1, st, pa));
+
+    // at most this many entries: an expert's pairs fill its entries but for the last
+    const int entries = std::min(pairs, fa.E + fa.n_shared + pairs / mt);
+    Mx4FfnArgs g{};
+    g.wl = fa.wl, g.E = fa.E, g.blob = fa.blob, g.store[0] = maps.store[0], g.store[1] = maps.store[1], g.img_bytes = img_bytes;
+    g.scale_off[0] = (long long)mx4_image_scales(H, I, 0), g.scale_off[1] = (long long)mx4_image_scales(H, I, 1);
+    g.rows = I, g.blocks = H / kMxBlock, g.mt = mt;
+    g.x_scales = b.x_scales, g.inv_rms = fa.inv_rms, g.act_codes = b.act_codes, g.act_scales = b.act_scales, g.err = err;
+    g.w_align = g.blocks % 8 == 0 ? 8 : g.blocks % 4 == 0 ? 4 : 1;
+    const int gu_steps = (g.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
+    const int gu_tasks = entries * ((I + kMmRows - 1) / kMmRows);
+    // fewer tiles than SMs: a cluster shares a tile's reduction
+    g.splits = std::max(1, std::min({sms / gu_tasks, gu_steps, kMmMaxSplits}));
+    ST_TRY(mx4_launch(mx4_ffn_kernel<2>, g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMmThreads, kMmSmemBytes,
+                      g.splits, st, maps.gate[0], maps.up[0], maps.gate[1], maps.up[1], maps.x, g));
+
+    ST_TRY(mark(1));
+    Mx4FfnArgs d = g;
+    d.rows = H, d.blocks = I / kMxBlock, d.x_scales = b.act_scales, d.part = b.part;
+    d.scale_off[0] = (long long)mx4_image_scales(H, I, 2);
+    d.w_align = d.blocks % 8 == 0 ? 8 : d.blocks % 4 == 0 ? 4 : 1;
+    const int d_tiles = entries * ((H + kMmRows - 1) / kMmRows);
+    // split the reduction where it evens the last round of tasks out; every split is one more
+    // partial sum to write and read
+    double best = 1e30;
+    for (int z = 1; z <= mx4_max_splits(pairs, I); ++z) {
+        const double t = (double)((d_tiles * z + sms - 1) / sms) / z * (1 + 0.03 * z);
+        if (t < best) best = t, d.splits = z;
+    }
+    ST_TRY(mx4_launch(mx4_ffn_kernel<1>, std::min(d_tiles * d.splits, sms), kMmThreads, kMmSmemBytes, 1, st, maps.down[0],
+                      maps.down[0], maps.down[1], maps.down[1], maps.act, d));
+
+    fa.part = b.part, fa.S = d.splits;
+    ST_TRY(mx4_launch(mx4_combine_kernel, std::min(sms * 4, (fa.B * H + 255) / 256), 256, 0, 1, st, fa, pa.ids));
+    return mark(2);
+}
+
 struct TimedSpan {
     cudaEvent_t a, b;
     int kind;  // 0 transfer, 1 exposed wait, 2 gate/up kernel, 3 down kernel, 4 router kernel
@@ -399,6 +557,9 @@ struct stmoe {
     bool dense8 = false;            // fp8 stacks: e4m3 weight tiles x three e5m2 activation planes
     CUtensorMap map8_gate{}, map8_up{}, map8_down{}, map8_x[4]{}, map8_act[4]{};
     uint8_t *d_x8 = nullptr, *d_act8 = nullptr;  // [3][64][H], [3][pairs + 64][I]
+    Mx4FfnMaps mx4_maps{};          // MX4 stacks (mx4_ffn.cuh)
+    Mx4FfnBufs mx4{};
+    uint8_t *d_mx4 = nullptr;       // the buffers behind mx4
     float *d_host_io = nullptr;     // stmoe_decode_token_host: [2][max_batch][H] staging of h_in / h_out
     int32_t *d_host_ids = nullptr;  // and [L][max_batch][K] of the routed ids
     bool dense_persistent = false;  // one cooperative kernel per decode step (token_dense_kernel.cuh)
@@ -677,10 +838,6 @@ constexpr int kTokenDenseDynBytes = 220 * 1024;
 
 bool use_dense(const stmoe *s, int batch) { return (s->dense || s->dense8) && batch >= s->dense_min_batch; }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // bf16 tensor of `rank` dimensions (dims[0] innermost, strides in bytes for dims 1..), boxes of
 // 64 columns x box_rows rows (x 1 image), 128-byte swizzle, zero fill outside
 int encode_map(EncodeTiledFn fn, CUtensorMap *m, void *base, int rank, const cuuint64_t *dims,
@@ -945,6 +1102,24 @@ int run_ffn(stmoe *s, int dt, int mt, const FfnPlan &plan, const FfnArgs &fa, cu
     return STMOE_OK;
 }
 
+int mx4_layer_ffn(stmoe *s, const FfnArgs &fa, cudaStream_t st)
+{
+    cudaEvent_t e[3] = {};
+    if (s->time_kernels)
+        for (cudaEvent_t &x : e) ST_TRY(get_event(s, &x));
+    ST_TRY(mx4_ffn(s->mx4_maps, s->mx4, Mx4PlanesArgs{}, fa, s->img_bytes, s->d_err, s->persistent_grid, st, [&](int i) {
+        if (e[i]) CU_TRY(cudaEventRecord(e[i], st));
+        return STMOE_OK;
+    }));
+    if (s->time_kernels) {
+        s->spans.push_back(TimedSpan{e[0], e[1], 2});
+        s->spans.push_back(TimedSpan{e[1], e[2], 3});
+        s->timed_ffn += 1;
+    }
+    s->launches += 4;
+    return STMOE_OK;
+}
+
 int layer_step(stmoe *s, int layer, int batch, const float *h_in, float *h_out, int32_t *routed_ids,
                float *routed_w, int32_t *predicted_ids, int32_t *n_predicted, uint32_t *flags,
                cudaStream_t st, bool chained = false)
@@ -952,7 +1127,8 @@ int layer_step(stmoe *s, int layer, int batch, const float *h_in, float *h_out, 
     const stmoe_config_t &c = s->cfg;
     const int E = c.n_experts, K = c.top_k, H = c.hidden;
     const bool dense = use_dense(s, batch);
-    const int mt = batch == 1 ? 1 : dense ? kDenseMaxTokens : 4;
+    const bool mx4 = c.weight_dtype == STMOE_MX4;
+    const int mt = mx4 ? mx4_entry_tokens(batch) : batch == 1 ? 1 : dense ? kDenseMaxTokens : 4;
     int32_t *ids = s->d_ids + (size_t)layer * c.max_batch * K;
     const int32_t *prev = layer > 0 ? s->d_ids + (size_t)(layer - 1) * c.max_batch * K : nullptr;
 
@@ -1008,7 +1184,9 @@ int layer_step(stmoe *s, int layer, int batch, const float *h_in, float *h_out, 
         fa.blob = s->d_blob_table + (size_t)layer * (E + c.n_shared);
     }
     s->launches += 1;
-    if (dense && s->dense8)
+    if (mx4)
+        ST_TRY(mx4_layer_ffn(s, fa, st));
+    else if (dense && s->dense8)
         ST_TRY(dense8_ffn(s, layer, batch, chained, fa, st));
     else if (dense)
         ST_TRY(dense_ffn(s, layer, batch, chained, fa, st));
@@ -1238,7 +1416,7 @@ int stmoe_destroy(stmoe_t *s)
                    s->pst.pred_valid, s->pst.stats, s->d_rpart, s->d_sspart, s->d_arrivals, s->d_tile_done, s->d_hbuf, s->d_rpart_all, s->d_sspart_all,
                    s->d_act_all, s->d_part_all, s->d_tiles_all, s->d_barrier, s->d_err, s->d_inv, s->d_logits, s->d_w, s->d_act, s->d_part,
                    s->d_ids, s->d_queue, s->d_xb, s->d_actb, s->d_part_dense, s->d_x8, s->d_act8, s->d_host_io, s->d_host_ids, s->d_gu_done,
-                   s->d_down_t, s->d_zpart, s->d_acc};
+                   s->d_down_t, s->d_zpart, s->d_acc, s->d_mx4};
     if (s->d_shared && s->d_resident && s->d_shared > s->d_resident) dev[2] = nullptr;  // one allocation
     for (void *p : dev)
         if (p) cudaFree(p);
@@ -1260,7 +1438,8 @@ int stmoe_create(const stmoe_config_t *cfg, stmoe_t **out)
     if (c.n_layers < 1 || c.n_experts < 1 || c.n_experts > kMaxExperts || c.top_k < 1 || c.top_k > kMaxTopK ||
         c.top_k > c.n_experts || c.n_shared < 0 || c.n_shared > 8 || c.hidden < 16 || c.hidden % 16 ||
         c.inter < 16 || c.inter % 16 || c.max_batch < 1 || c.max_batch > kMaxBatch ||
-        c.weight_dtype < STMOE_F32 || c.weight_dtype > STMOE_FP8_E4M3 || c.cache_slots < 0 ||
+        c.weight_dtype < STMOE_F32 || c.weight_dtype > STMOE_MX4 || c.cache_slots < 0 ||
+        (c.weight_dtype == STMOE_MX4 && (c.hidden % kMxBlock || c.inter % kMxBlock)) ||
         c.profile_tokens < 0 || c.predictor_mode < 0 || c.predictor_mode > 3 || c.prefetch_limit < 0 ||
         (c.cache_slots > 0 && c.cache_slots < (int64_t)c.max_batch * c.top_k) ||
         c.cache_slots > (int64_t)c.n_layers * c.n_experts)
@@ -1370,7 +1549,31 @@ int stmoe_create(const stmoe_config_t *cfg, stmoe_t **out)
     if (s->wlm.alloc(B * s->KS) != STMOE_OK) return fail(STMOE_ERR_OOM);
     s->plan1 = make_plan(c.weight_dtype, 1);
     s->plan4 = make_plan(c.weight_dtype, 4);
-    if (c.cache_slots == 0 && !(c.flags & STMOE_FLAG_NO_PERSISTENT)) {
+    if (c.weight_dtype == STMOE_MX4) {
+        // its own kernels at every batch, launched layer by layer (replayed as a CUDA graph)
+        const int pairs = B * s->KS;
+        int dev = 0;
+        CR_TRY(cudaGetDevice(&dev));
+        int rc = mx4_prepare_kernels(dev);
+        if (rc != STMOE_OK) return fail(rc);
+        CR_TRY(cudaMalloc(&s->d_mx4, mx4_buffers(nullptr, B, pairs, H, I, &s->mx4)));
+        mx4_buffers(s->d_mx4, B, pairs, H, I, &s->mx4);
+        rc = mx4_act_maps(&s->mx4_maps, s->mx4, B, pairs, H, I);
+        const bool off = c.cache_slots > 0;
+        if (rc == STMOE_OK)
+            rc = mx4_weight_maps(&s->mx4_maps, 0, off ? s->d_slots : s->d_resident,
+                                 off ? c.cache_slots : (int64_t)L * (E + c.n_shared), s->img_bytes, H, I);
+        if (rc == STMOE_OK)   // shared experts of an offloaded stack live in an allocation of their own
+            rc = off && c.n_shared ? mx4_weight_maps(&s->mx4_maps, 1, s->d_shared, (int64_t)L * c.n_shared, s->img_bytes, H, I)
+                                   : STMOE_OK;
+        if (rc != STMOE_OK) return fail(rc);
+        if (!(off && c.n_shared)) {
+            Mx4FfnMaps &m = s->mx4_maps;
+            m.gate[1] = m.gate[0], m.up[1] = m.up[0], m.down[1] = m.down[0], m.store[1] = m.store[0];
+        }
+        s->persistent_grid = sm_count();
+    }
+    if (c.cache_slots == 0 && c.weight_dtype != STMOE_MX4 && !(c.flags & STMOE_FLAG_NO_PERSISTENT)) {
         int dev = 0, coop = 0;
         cudaGetDevice(&dev);
         cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev);
@@ -1565,7 +1768,19 @@ int stmoe_load_experts(stmoe_t *s, int layer, int first_expert, int count, const
         return STMOE_ERR_BAD_ARG;
     const stmoe_config_t &c = s->cfg;
     if (first_expert + count > (is_shared ? c.n_shared : c.n_experts)) return STMOE_ERR_BAD_ARG;
-    if ((c.weight_dtype == STMOE_FP8_E4M3) != (scales != nullptr)) return STMOE_ERR_BAD_ARG;
+    const bool mx4 = c.weight_dtype == STMOE_MX4;
+    if ((c.weight_dtype == STMOE_FP8_E4M3 || mx4) != (scales != nullptr)) return STMOE_ERR_BAD_ARG;
+    if (mx4) {  // codes of the three matrices, then their scales, one after the other as in the image
+        const size_t nc = (size_t)c.hidden * c.inter / 2, ns = 3 * ((size_t)c.hidden * c.inter / kMxBlock);
+        const void *codes[3] = {gate, up, down};
+        for (int i = 0; i < count; ++i) {
+            uint8_t *img = image_ptr(s, layer, first_expert + i, is_shared != 0);
+            for (int m = 0; m < 3; ++m)
+                CU_TRY(cudaMemcpy(img + mx4_image_codes(c.hidden, c.inter, m), (const uint8_t *)codes[m] + i * nc, nc, cudaMemcpyDefault));
+            CU_TRY(cudaMemcpy(img + mx4_image_scales(c.hidden, c.inter, 0), (const uint8_t *)scales + i * ns, ns, cudaMemcpyDefault));
+        }
+        return STMOE_OK;
+    }
     const int wb = dtype_bytes(c.weight_dtype);
     const size_t mat = (size_t)c.hidden * c.inter * wb, sc = 2 * (size_t)(2 * c.inter + c.hidden);
     for (int i = 0; i < count; ++i) {
@@ -1894,6 +2109,61 @@ group_given_ids_kernel(const int32_t *ids, int B, int E, int K, int mt, WorkList
 
 }  // namespace
 
+namespace {
+
+bool mx4_ffn_args_ok(const void *experts, int hidden, int inter)
+{
+    return hidden % kMxBlock == 0 && inter % kMxBlock == 0 && ((uintptr_t)experts & 15) == 0;
+}
+// scratch of a stand-alone MX4 call: work list | image table | planes and partial sums
+size_t mx4_scratch_layout(int B, int K, size_t *o_tab)
+{
+    *o_tab = round_up(sizeof(int) * (4 + 5 * (size_t)B * K), 256);
+    return *o_tab + round_up(sizeof(void *) * (size_t)kMaxExperts, 256);
+}
+
+int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const float *w, const void *experts, int batch,
+                int n_experts, int top_k, int hidden, int inter, float residual_scale, float *h_out, void *scratch,
+                size_t scratch_bytes, cudaStream_t st)
+{
+    if (!mx4_ffn_args_ok(experts, hidden, inter) || scratch_bytes < stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter))
+        return STMOE_ERR_BAD_ARG;
+    static int sms[64];   // per device ordinal; a racing fill writes the same value
+    int dev = 0;
+    CU_TRY(cudaGetDevice(&dev));
+    ST_TRY(mx4_prepare_kernels(dev));
+    if (!sms[dev]) sms[dev] = sm_count();
+    uint8_t *sc = (uint8_t *)scratch;
+    size_t o_tab;
+    const size_t o_buf = mx4_scratch_layout(batch, top_k, &o_tab), img = image_bytes(hidden, inter, STMOE_MX4);
+    Mx4FfnBufs b;
+    mx4_buffers(sc + o_buf, batch, batch * top_k, hidden, inter, &b);
+    Mx4FfnMaps maps;
+    ST_TRY(mx4_weight_maps(&maps, 0, (const uint8_t *)experts, n_experts, img, hidden, inter));
+    maps.gate[1] = maps.gate[0], maps.up[1] = maps.up[0], maps.down[1] = maps.down[0], maps.store[1] = maps.store[0];
+    ST_TRY(mx4_act_maps(&maps, b, batch, batch * top_k, hidden, inter));
+    WorkListMem wlm;
+    wlm.bind((int *)sc, batch * top_k);
+    Mx4PlanesArgs pa{};
+    pa.group_ctas = 1, pa.ids = ids, pa.E = n_experts, pa.K = top_k, pa.mt = mx4_entry_tokens(batch), pa.wl = wlm.wl;
+    pa.experts = (const uint8_t *)experts, pa.img_bytes = img, pa.table = (const uint8_t **)(sc + o_tab);
+    FfnArgs fa{};
+    fa.h = h, fa.inv_rms = inv_rms, fa.wl = wlm.wl, fa.blob = pa.table;
+    fa.H = hidden, fa.I = inter, fa.E = n_experts, fa.w = w, fa.h_out = h_out;
+    fa.B = batch, fa.K = top_k, fa.n_shared = 0, fa.residual_scale = residual_scale;
+    return mx4_ffn(maps, b, pa, fa, img, nullptr, sms[dev], st, [](int) { return STMOE_OK; });
+}
+
+}  // namespace
+
+extern "C" size_t stmoe_mx4_ffn_scratch_bytes(int batch, int top_k, int hidden, int inter)
+{
+    if (batch < 1 || batch > kMaxBatch || top_k < 1 || top_k > kMaxTopK || hidden < kMxBlock || inter < kMxBlock) return 0;
+    size_t o_tab;
+    Mx4FfnBufs b;
+    return mx4_scratch_layout(batch, top_k, &o_tab) + mx4_buffers(nullptr, batch, batch * top_k, hidden, inter, &b);
+}
+
 extern "C" int stmoe_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const float *w,
                              const void *experts, int weight_dtype, int batch, int n_experts, int top_k,
                              int hidden, int inter, float residual_scale, float *h_out, void *scratch,
@@ -1901,9 +2171,12 @@ extern "C" int stmoe_moe_ffn(const float *h, const float *inv_rms, const int32_t
 {
     if (!h || !ids || !w || !experts || !h_out || !scratch || batch < 1 || batch > kMaxBatch || n_experts < 1 ||
         n_experts > kMaxExperts || top_k < 1 || top_k > kMaxTopK || top_k > n_experts || hidden < 16 ||
-        hidden % 16 || inter < 16 || inter % 16 || weight_dtype < STMOE_F32 || weight_dtype > STMOE_FP8_E4M3 ||
+        hidden % 16 || inter < 16 || inter % 16 || weight_dtype < STMOE_F32 || weight_dtype > STMOE_MX4 ||
         ((uintptr_t)scratch & 255))
         return STMOE_ERR_BAD_ARG;
+    if (weight_dtype == STMOE_MX4)
+        return mx4_moe_ffn(h, inv_rms, ids, w, experts, batch, n_experts, top_k, hidden, inter, residual_scale, h_out, scratch,
+                           scratch_bytes, (cudaStream_t)cuda_stream);
     size_t o_tab, o_act, o_part, o_tiles;
     const int S = down_splits(inter, weight_dtype);
     if (scratch_bytes < ffn_scratch_layout(batch, top_k, hidden, inter, kMaxExperts, down_splits(inter, STMOE_F32), &o_tab, &o_act, &o_part, &o_tiles))
@@ -1952,9 +2225,11 @@ extern "C" int stmoe_moe_ffn_static(const float *h, const float *inv_rms, const 
     // call reads as a bad argument and the size below is computed from values in range
     if (!h || !ids || !w || !experts || !h_out || batch < 1 || batch > kMaxBatch || n_experts < 1 ||
         n_experts > kMaxExperts || top_k < 1 || top_k > kMaxTopK || top_k > n_experts || hidden < 16 ||
-        hidden % 16 || inter < 16 || inter % 16 || weight_dtype < STMOE_F32 || weight_dtype > STMOE_FP8_E4M3)
+        hidden % 16 || inter < 16 || inter % 16 || weight_dtype < STMOE_F32 || weight_dtype > STMOE_MX4 ||
+        (weight_dtype == STMOE_MX4 && !mx4_ffn_args_ok(experts, hidden, inter)))
         return STMOE_ERR_BAD_ARG;
-    if (stmoe_moe_ffn_scratch_bytes(batch, top_k, hidden, inter) > (size_t)STMOE_STATIC_SCRATCH_BYTES)
+    if ((weight_dtype == STMOE_MX4 ? stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter)
+                                   : stmoe_moe_ffn_scratch_bytes(batch, top_k, hidden, inter)) > (size_t)STMOE_STATIC_SCRATCH_BYTES)
         return STMOE_ERR_TOO_LARGE;
     int dev = -1;
     CU_TRY(cudaGetDevice(&dev));
