@@ -124,8 +124,12 @@ def _dev(t, dtype=None):
     return t.data_ptr()
 
 
+# torch's current stream of a device as a bare handle; the Stream object costs microseconds to make
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
 def _stream(stream):
-    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+    return stream.cuda_stream if stream is not None else _raw_stream(torch.cuda.current_device())
 
 
 class Stack:
@@ -324,80 +328,89 @@ def expert_ffn_dense(h, inv_rms, image, hidden, inter, stream=None):
 
 
 # ---- microscaled 4-bit floating point and router statistics --------------------------------------
+# These calls take microseconds on the device, so the host side is kept short: one condition in front
+# of each call, messages made only when it fails.
 
 _ELEM = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 4}
+_U8, _I32, _F32 = torch.uint8, torch.int32, torch.float32
 
 
-def _need(ok, what: str) -> None:
-    if not ok:
-        raise StmoeError(what)
+def _refuse(what: str):
+    raise StmoeError(what)
 
 
-def _rows2(t, what: str, dtype=None):
-    """A CUDA matrix whose rows are contiguous; any row stride."""
-    _need(t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{what}: expected a 2-D CUDA tensor with contiguous rows")
-    _need(dtype is None or t.dtype == dtype, f"{what}: expected {dtype}, got {t.dtype}")
-    return t
+def _is_rows(t, dtype=None) -> bool:
+    """A CUDA matrix with contiguous rows, any row stride."""
+    return t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1) and (dtype is None or t.dtype == dtype)
 
 
-def _same_device(first, *rest) -> None:
-    _need(all(t is None or t.device == first.device for t in rest), "all tensors have to be on one CUDA device")
+def _stream_of(ref, stream):
+    """Handle of the stream a call goes to: torch's current one, if ref lives on the current device and no
+    stream was given; else None (see _there)."""
+    i = ref.get_device()
+    return _raw_stream(i) if stream is None and i == torch.cuda.current_device() else None
 
 
-def _on_device(ref, stream, call):
-    """call(stream handle) with ref's device current; tensors it allocates belong to that stream."""
-    if stream is None and ref.device.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream().cuda_stream)
+def _there(ref, stream, fn, *args, **kw):
+    """fn again with ref's device current, on the given stream or that device's current one; tensors it
+    allocates belong to that stream."""
     with torch.cuda.device(ref.device):
         s = stream if stream is not None else torch.cuda.current_stream()
-        _need(s.device == ref.device, "the stream belongs to another device than the tensors")
+        if s.device != ref.device:
+            _refuse("the stream belongs to another device than the tensors")
         with torch.cuda.stream(s):
-            return call(s.cuda_stream)
+            return fn(*args, **kw)
 
 
 def mx4_quantize(x, codes=None, scales=None, stream=None):
     """stmoe_mx4_quantize: x [rows][cols] (fp32, bf16 or fp16, any row stride) -> (codes uint8
     [rows][ceil(cols/32)*16], scales uint8 [rows][ceil(cols/32)]), into given tensors or new ones."""
-    _rows2(x, "x")
-    _need(x.dtype in _ELEM, f"x: fp32, bf16 or fp16, got {x.dtype}")
+    elem = _ELEM.get(x.dtype)
+    if elem is None or not _is_rows(x) or x.shape[1] < 1:
+        _refuse("x: expected a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows")
     rows, cols = x.shape
-    _need(cols >= 1, "x has no columns")
     nb = (cols + 31) // 32
-    _same_device(x, codes, scales)
-    if codes is not None:
-        _need(tuple(_rows2(codes, "codes", torch.uint8).shape) == (rows, nb * 16), f"codes: expected {(rows, nb * 16)}")
-    if scales is not None:
-        _need(tuple(_rows2(scales, "scales", torch.uint8).shape) == (rows, nb), f"scales: expected {(rows, nb)}")
-
-    def call(st):
-        c = torch.empty(rows, nb * 16, dtype=torch.uint8, device=x.device) if codes is None else codes
-        s = torch.empty(rows, nb, dtype=torch.uint8, device=x.device) if scales is None else scales
-        if rows:
-            _check(lib().stmoe_mx4_quantize(x.data_ptr(), _ELEM[x.dtype], rows, cols, x.stride(0), c.data_ptr(), c.stride(0),
-                                            s.data_ptr(), s.stride(0), st), "stmoe_mx4_quantize")
-        return c, s
-    return _on_device(x, stream, call)
+    for t, n in ((codes, nb * 16), (scales, nb)):
+        if t is not None and not (_is_rows(t, _U8) and t.shape[0] == rows and t.shape[1] == n and t.device == x.device):
+            _refuse(f"codes and scales: expected uint8 {(rows, nb * 16)} and {(rows, nb)} on x's device")
+    st = _stream_of(x, stream)
+    if st is None:
+        return _there(x, stream, mx4_quantize, x, codes, scales)
+    if codes is None:
+        codes = torch.empty(rows, nb * 16, dtype=_U8, device=x.device)
+    if scales is None:
+        scales = torch.empty(rows, nb, dtype=_U8, device=x.device)
+    if rows:
+        rc = lib().stmoe_mx4_quantize(x.data_ptr(), elem, rows, cols, x.stride(0), codes.data_ptr(), codes.stride(0),
+                                      scales.data_ptr(), scales.stride(0), st)
+        if rc:
+            _check(rc, "stmoe_mx4_quantize")
+    return codes, scales
 
 
 def mx4_dequantize(codes, scales, cols, dtype=torch.float32, out=None, stream=None):
     """stmoe_mx4_dequantize: the first `cols` values of every row, in dtype (or in out's)."""
-    _rows2(codes, "codes", torch.uint8), _rows2(scales, "scales", torch.uint8)
-    rows, nb = scales.shape
-    _need(tuple(codes.shape) == (rows, nb * 16) and cols >= 1 and (cols + 31) // 32 == nb,
-          "codes, scales and cols do not belong together")
-    _same_device(codes, scales, out)
     if out is not None:
-        _need(tuple(_rows2(out, "out").shape) == (rows, cols), f"out: expected {(rows, cols)}")
         dtype = out.dtype
-    _need(dtype in _ELEM, f"fp32, bf16 or fp16, got {dtype}")
-
-    def call(st):
-        y = torch.empty(rows, cols, dtype=dtype, device=codes.device) if out is None else out
-        if rows:
-            _check(lib().stmoe_mx4_dequantize(codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0), rows, cols,
-                                              y.data_ptr(), _ELEM[dtype], y.stride(0), st), "stmoe_mx4_dequantize")
-        return y
-    return _on_device(codes, stream, call)
+    elem = _ELEM.get(dtype)
+    if elem is None or not (_is_rows(codes, _U8) and _is_rows(scales, _U8)):
+        _refuse("expected 2-D uint8 CUDA tensors with contiguous rows, and fp32, bf16 or fp16 values")
+    rows, nb = scales.shape
+    if codes.shape[0] != rows or codes.shape[1] != nb * 16 or cols < 1 or (cols + 31) // 32 != nb or codes.device != scales.device:
+        _refuse("codes, scales and cols do not belong together")
+    if out is not None and not (_is_rows(out) and out.shape[0] == rows and out.shape[1] == cols and out.device == codes.device):
+        _refuse(f"out: expected {(rows, cols)} with contiguous rows on the codes' device")
+    st = _stream_of(codes, stream)
+    if st is None:
+        return _there(codes, stream, mx4_dequantize, codes, scales, cols, dtype, out)
+    if out is None:
+        out = torch.empty(rows, cols, dtype=dtype, device=codes.device)
+    if rows:
+        rc = lib().stmoe_mx4_dequantize(codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0), rows, cols,
+                                        out.data_ptr(), elem, out.stride(0), st)
+        if rc:
+            _check(rc, "stmoe_mx4_dequantize")
+    return out
 
 
 def mx4_expert(gate, up, down, stream=None):
@@ -405,22 +418,22 @@ def mx4_expert(gate, up, down, stream=None):
     quantised: dict(gate, up, down: codes; scales: those of the three, one after the other) for
     Stack.load_experts, and image: the same as one expert image for moe_ffn (the others are views
     into it)."""
-    I, H = _rows2(gate, "gate").shape
-    _need(H % 32 == 0 and I % 32 == 0, "hidden and inter have to be multiples of 32")
-    _need(tuple(up.shape) == (I, H) and tuple(down.shape) == (H, I), "gate and up are [I][H], down is [H][I]")
-    _same_device(gate, up, down)
-
-    def call(st):
-        n, nc, ns = expert_image_bytes(H, I, "mx4"), H * I // 2, H * I // 32
-        image = torch.empty(n, dtype=torch.uint8, device=gate.device)
-        image[3 * (nc + ns):].zero_()
-        parts = {"image": image, "scales": image[3 * nc:3 * (nc + ns)]}
-        for i, (name, w) in enumerate((("gate", gate), ("up", up), ("down", down))):
-            r, c = w.shape
-            parts[name] = image[i * nc:(i + 1) * nc].view(r, c // 2)
-            mx4_quantize(w, parts[name], image[3 * nc + i * ns:3 * nc + (i + 1) * ns].view(r, c // 32))
-        return parts
-    return _on_device(gate, stream, call)
+    if not (_is_rows(gate) and _is_rows(up) and _is_rows(down)):
+        _refuse("expected 2-D CUDA tensors with contiguous rows")
+    I, H = gate.shape
+    if H % 32 or I % 32 or H < 32 or I < 32 or up.shape != gate.shape or tuple(down.shape) != (H, I):
+        _refuse("gate and up are [I][H], down is [H][I]; hidden and inter multiples of 32")
+    if _stream_of(gate, stream) is None:
+        return _there(gate, stream, mx4_expert, gate, up, down)
+    n, nc, ns = expert_image_bytes(H, I, "mx4"), H * I // 2, H * I // 32
+    image = torch.empty(n, dtype=_U8, device=gate.device)
+    image[3 * (nc + ns):].zero_()
+    parts = {"image": image, "scales": image[3 * nc:3 * (nc + ns)]}
+    for i, (name, w) in enumerate((("gate", gate), ("up", up), ("down", down))):
+        r, c = w.shape
+        parts[name] = image[i * nc:(i + 1) * nc].view(r, c // 2)
+        mx4_quantize(w, parts[name], image[3 * nc + i * ns:3 * nc + (i + 1) * ns].view(r, c // 32))
+    return parts
 
 
 def mx4_matmul(a, b, counts=None, dtype=torch.bfloat16, out=None, flags=None, stream=None):
@@ -428,98 +441,115 @@ def mx4_matmul(a, b, counts=None, dtype=torch.bfloat16, out=None, flags=None, st
     returns them.  a: [m] rows; b: [n] rows, or [groups][n] rows with counts (int32 [groups], on the
     device: how many rows of a belong to each group, in order; rows behind their sum are not written).
     flags: optional int32 [1], caller-zeroed; non-zero = a bounded wait inside the kernel ran out."""
-    a_codes, a_scales = _rows2(a[0], "a codes", torch.uint8), _rows2(a[1], "a scales", torch.uint8)
-    b_codes, b_scales = b
-    _need(b_codes.dim() == b_scales.dim() and b_codes.dim() in (2, 3), "b: codes and scales of [n] or [groups][n] rows")
-    groups = 1
-    if b_codes.dim() == 3:
+    (a_codes, a_scales), (b_codes, b_scales) = a, b
+    groups, dims = 1, b_codes.dim()
+    if dims not in (2, 3) or b_scales.dim() != dims:
+        _refuse("b: codes and scales of [n] or [groups][n] rows")
+    if dims == 3:
         groups, n = b_codes.shape[:2]
-        _need(groups >= 1 and n >= 1, "b has no rows")
-        for t in (b_codes, b_scales):
-            _need(groups == 1 or t.stride(0) == n * t.stride(1), "b: the groups' rows have to follow one another")
-        _need(b_scales.shape[:2] == b_codes.shape[:2], "b: codes and scales do not belong together")
+        if groups < 1 or n < 1 or b_scales.shape[:2] != b_codes.shape[:2]:
+            _refuse("b: codes and scales do not belong together")
+        if groups > 1 and not (b_codes.stride(0) == n * b_codes.stride(1) and b_scales.stride(0) == n * b_scales.stride(1)):
+            _refuse("b: the groups' rows have to follow one another")
         b_codes, b_scales = b_codes[0], b_scales[0]
-    _rows2(b_codes, "b codes", torch.uint8), _rows2(b_scales, "b scales", torch.uint8)
+    if not (_is_rows(a_codes, _U8) and _is_rows(a_scales, _U8) and _is_rows(b_codes, _U8) and _is_rows(b_scales, _U8)):
+        _refuse("codes and scales: expected uint8 CUDA tensors with contiguous rows")
     m, nb = a_scales.shape
     n = b_scales.shape[0]
-    _need(tuple(a_codes.shape) == (m, nb * 16) and tuple(b_codes.shape) == (n, nb * 16) and b_scales.shape[1] == nb and n >= 1 and nb >= 1,
-          "the operands' shapes do not belong together")
-    _same_device(a_codes, a_scales, b_codes, b_scales, counts, out, flags)
-    _need(counts is not None or groups == 1, "several groups need counts")
-    if counts is not None:
-        _need(counts.dtype == torch.int32 and counts.is_contiguous() and counts.numel() == groups, "counts: contiguous int32 [groups]")
+    if not (n and nb and a_codes.shape[0] == m and a_codes.shape[1] == nb * 16 and b_codes.shape[0] == n
+            and b_codes.shape[1] == nb * 16 and b_scales.shape[1] == nb):
+        _refuse("the operands' shapes do not belong together")
+    dev = a_codes.device
+    for t in (a_scales, b_codes, b_scales, counts, out, flags):
+        if t is not None and t.device != dev:
+            _refuse("all tensors have to be on one CUDA device")
+    if counts is None:
+        if groups != 1:
+            _refuse("several groups need counts")
+    elif counts.dtype != _I32 or counts.numel() != groups or not counts.is_contiguous():
+        _refuse("counts: contiguous int32 [groups]")
     if out is not None:
-        _need(tuple(_rows2(out, "out").shape) == (m, n), f"out: expected {(m, n)}")
+        if not (_is_rows(out) and out.shape[0] == m and out.shape[1] == n):
+            _refuse(f"out: expected {(m, n)} with contiguous rows")
         dtype = out.dtype
-    _need(dtype in _ELEM, f"fp32, bf16 or fp16, got {dtype}")
-    _need(flags is None or (flags.dtype == torch.int32 and flags.numel() >= 1), "flags: int32")
+    elem = _ELEM.get(dtype)
+    if elem is None or (flags is not None and (flags.dtype != _I32 or flags.numel() < 1)):
+        _refuse("out is fp32, bf16 or fp16; flags is int32")
+    st = _stream_of(a_codes, stream)
+    if st is None:
+        return _there(a_codes, stream, mx4_matmul, a, b, counts, dtype, out, flags)
+    if out is None:
+        out = torch.empty(m, n, dtype=dtype, device=dev)
+    if m:
+        rc = lib().stmoe_mx4_matmul(a_codes.data_ptr(), a_codes.stride(0), a_scales.data_ptr(), a_scales.stride(0), m,
+                                    b_codes.data_ptr(), b_codes.stride(0), b_scales.data_ptr(), b_scales.stride(0),
+                                    groups, n, nb, None if counts is None else counts.data_ptr(), out.data_ptr(),
+                                    elem, out.stride(0), None if flags is None else flags.data_ptr(), st)
+        if rc:
+            _check(rc, "stmoe_mx4_matmul")
+    return out
 
-    def call(st):
-        y = torch.empty(m, n, dtype=dtype, device=a_codes.device) if out is None else out
-        if m:
-            _check(lib().stmoe_mx4_matmul(a_codes.data_ptr(), a_codes.stride(0), a_scales.data_ptr(), a_scales.stride(0), m,
-                                          b_codes.data_ptr(), b_codes.stride(0), b_scales.data_ptr(), b_scales.stride(0),
-                                          groups, n, nb, None if counts is None else counts.data_ptr(), y.data_ptr(),
-                                          _ELEM[dtype], y.stride(0), None if flags is None else flags.data_ptr(), st),
-                   "stmoe_mx4_matmul")
-        return y
-    return _on_device(a_codes, stream, call)
 
-
-def _balance_args(logits, mask):
-    _rows2(logits, "logits")
-    _need(logits.dtype in _ELEM, f"logits: fp32, bf16 or fp16, got {logits.dtype}")
-    T, E = logits.shape
-    if mask is not None:
-        _need(mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and mask.numel() == T, "mask: contiguous bool [tokens]")
-    return T, E
+def _balance_elem(logits, mask):
+    elem = _ELEM.get(logits.dtype)
+    if elem is None or not _is_rows(logits):
+        _refuse("logits: expected a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows")
+    if mask is not None and not (mask.dtype in (torch.bool, _U8) and mask.is_contiguous() and mask.numel() == logits.shape[0]
+                                 and mask.device == logits.device):
+        _refuse("mask: contiguous bool [tokens] on the logits' device")
+    return elem
 
 
 def router_balance(logits, ids, mask=None, stream=None):
     """stmoe_router_balance: losses and per-expert counts for logits [tokens][n_experts] and the
     chosen experts ids int32 [tokens][top_k] (-1: dropped); mask [tokens]: rows that count.
     Returns dict(loss fp32 [2] = balance, z; counts int32 [n_experts]; rows int32 [1]; top_k)."""
-    T, E = _balance_args(logits, mask)
-    _need(ids.is_cuda and ids.dtype == torch.int32 and ids.dim() == 2 and ids.is_contiguous() and ids.shape[0] == T,
-          "ids: contiguous int32 CUDA tensor [tokens][top_k]")
-    _same_device(logits, ids, mask)
+    elem = _balance_elem(logits, mask)
+    T, E = logits.shape
+    if not (ids.dtype == _I32 and ids.dim() == 2 and ids.is_contiguous() and ids.shape[0] == T and ids.device == logits.device):
+        _refuse("ids: contiguous int32 [tokens][top_k] on the logits' device")
     K = ids.shape[1]
-
-    def call(st):
-        n = lib().stmoe_router_balance_scratch_bytes(E)
-        _need(n > 0, f"{E} experts are out of range")
-        scratch = torch.empty(n, dtype=torch.uint8, device=logits.device)
-        loss = torch.empty(2, dtype=torch.float32, device=logits.device)
-        ints = torch.empty(E + 1, dtype=torch.int32, device=logits.device)
-        counts, rows = ints[:E], ints[E:]
-        # an empty tensor has no address; nothing of it is read
-        src, idp = (logits.data_ptr(), ids.data_ptr()) if T else (scratch.data_ptr(), scratch.data_ptr())
-        _check(lib().stmoe_router_balance(src, _ELEM[logits.dtype], logits.stride(0), idp,
-                                          None if mask is None else mask.data_ptr(), T, E, K, loss.data_ptr(), counts.data_ptr(),
-                                          rows.data_ptr(), scratch.data_ptr(), n, st), "stmoe_router_balance")
-        return dict(loss=loss, counts=counts, rows=rows, top_k=K)
-    return _on_device(logits, stream, call)
+    st = _stream_of(logits, stream)
+    if st is None:
+        return _there(logits, stream, router_balance, logits, ids, mask)
+    L = lib()
+    n = L.stmoe_router_balance_scratch_bytes(E)
+    if n == 0:
+        _refuse(f"{E} experts are out of range")
+    # one allocation: loss | counts | rows | scratch of the call
+    buf = torch.empty(n // 4 + E + 3, dtype=_F32, device=logits.device)
+    head, ptr = buf[:E + 3], buf.data_ptr()
+    ints = head.view(_I32)
+    # an empty tensor has no address; nothing of it is read
+    src, idp = (logits.data_ptr(), ids.data_ptr()) if T else (ptr, ptr)
+    rc = L.stmoe_router_balance(src, elem, logits.stride(0), idp, None if mask is None else mask.data_ptr(), T, E, K, ptr, ptr + 8,
+                                ptr + 8 + 4 * E, ptr + 12 + 4 * E, n, st)
+    if rc:
+        _check(rc, "stmoe_router_balance")
+    return {"loss": head[:2], "counts": ints[2:E + 2], "rows": ints[E + 2:], "top_k": K}
 
 
 def router_balance_backward(logits, forward, grad_loss, mask=None, out=None, stream=None):
     """stmoe_router_balance_backward: gradient of grad_loss . loss with respect to the logits, from
     the dict that router_balance returned for the same logits and mask; grad_loss: fp32 [2]."""
-    T, E = _balance_args(logits, mask)
-    counts, rows = forward["counts"], forward["rows"]
-    _need(counts.dtype == torch.int32 and counts.numel() == E and counts.is_contiguous() and rows.dtype == torch.int32,
-          "forward does not belong to these logits")
-    _need(grad_loss.is_cuda and grad_loss.dtype == torch.float32 and grad_loss.numel() == 2 and grad_loss.is_contiguous(),
-          "grad_loss: fp32 CUDA tensor [2]")
-    _same_device(logits, mask, counts, rows, grad_loss, out)
-    if out is not None:
-        _need(tuple(_rows2(out, "out", logits.dtype).shape) == (T, E), f"out: expected {(T, E)}")
-
-    def call(st):
-        d = torch.empty(T, E, dtype=logits.dtype, device=logits.device) if out is None else out
-        if T:
-            _check(lib().stmoe_router_balance_backward(logits.data_ptr(), _ELEM[logits.dtype], logits.stride(0),
-                                                       None if mask is None else mask.data_ptr(), T, E, forward["top_k"],
-                                                       counts.data_ptr(), rows.data_ptr(), grad_loss.data_ptr(), d.data_ptr(),
-                                                       d.stride(0), st), "stmoe_router_balance_backward")
-        return d
-    return _on_device(logits, stream, call)
+    elem = _balance_elem(logits, mask)
+    T, E = logits.shape
+    counts, rows, dev = forward["counts"], forward["rows"], logits.device
+    if not (counts.dtype == _I32 and counts.numel() == E and counts.is_contiguous() and rows.dtype == _I32 and counts.device == dev and rows.device == dev):
+        _refuse("forward does not belong to these logits")
+    if not (grad_loss.dtype == _F32 and grad_loss.numel() == 2 and grad_loss.is_contiguous() and grad_loss.device == dev):
+        _refuse("grad_loss: fp32 [2] on the logits' device")
+    if out is not None and not (_is_rows(out, logits.dtype) and out.shape == logits.shape and out.device == dev):
+        _refuse("out: expected the logits' shape and type")
+    st = _stream_of(logits, stream)
+    if st is None:
+        return _there(logits, stream, router_balance_backward, logits, forward, grad_loss, mask, out)
+    if out is None:
+        out = torch.empty(T, E, dtype=logits.dtype, device=dev)
+    if T:
+        rc = lib().stmoe_router_balance_backward(logits.data_ptr(), elem, logits.stride(0), None if mask is None else mask.data_ptr(),
+                                                 T, E, forward["top_k"], counts.data_ptr(), rows.data_ptr(), grad_loss.data_ptr(),
+                                                 out.data_ptr(), out.stride(0), st)
+        if rc:
+            _check(rc, "stmoe_router_balance_backward")
+    return out

@@ -45,6 +45,14 @@ int sm_count(int *dev_out)
 bool elem_type(int dtype) { return dtype == STMOE_F32 || dtype == STMOE_BF16 || dtype == STMOE_F16; }
 long long elem_bytes(int dtype) { return dtype == STMOE_F32 ? 4 : 2; }
 
+template <int DT> void launch_rows(bool quantize, const Mx4Rows &a, int grid, cudaStream_t st)
+{
+    if (quantize && a.vec) mx4_quantize_kernel<DT, true><<<grid, kMxThreads, 0, st>>>(a);
+    else if (quantize) mx4_quantize_kernel<DT, false><<<grid, kMxThreads, 0, st>>>(a);
+    else if (a.vec) mx4_dequantize_kernel<DT, true><<<grid, kMxThreads, 0, st>>>(a);
+    else mx4_dequantize_kernel<DT, false><<<grid, kMxThreads, 0, st>>>(a);
+}
+
 int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int64_t x_stride, uint8_t *codes,
              int64_t code_stride, uint8_t *scales, int64_t scale_stride, void *cuda_stream)
 {
@@ -68,15 +76,9 @@ int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int6
     const int64_t tasks = a.rows * ((a.cols - 1) / kMxSeg + 1), warps = kMxThreads / kWarp;
     const int grid = (int)std::min<int64_t>((tasks + warps - 1) / warps, (int64_t)sms * 8);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (quantize) {
-        if (dtype == STMOE_F32) mx4_quantize_kernel<0><<<grid, kMxThreads, 0, st>>>(a);
-        else if (dtype == STMOE_BF16) mx4_quantize_kernel<1><<<grid, kMxThreads, 0, st>>>(a);
-        else mx4_quantize_kernel<4><<<grid, kMxThreads, 0, st>>>(a);
-    } else {
-        if (dtype == STMOE_F32) mx4_dequantize_kernel<0><<<grid, kMxThreads, 0, st>>>(a);
-        else if (dtype == STMOE_BF16) mx4_dequantize_kernel<1><<<grid, kMxThreads, 0, st>>>(a);
-        else mx4_dequantize_kernel<4><<<grid, kMxThreads, 0, st>>>(a);
-    }
+    if (dtype == STMOE_F32) launch_rows<0>(quantize, a, grid, st);
+    else if (dtype == STMOE_BF16) launch_rows<1>(quantize, a, grid, st);
+    else launch_rows<4>(quantize, a, grid, st);
     CU_TRY(cudaGetLastError());
     return STMOE_OK;
 }
@@ -168,8 +170,11 @@ int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_
     a.a_scales = a_scales, a.b_scales = b_scales, a.a_scale_stride = a_scale_stride, a.b_scale_stride = b_scale_stride;
     a.counts = counts, a.groups = n_groups, a.m = (int)m, a.n = n, a.blocks = k_blocks;
     a.out = out, a.out_stride = out_stride, a.err = flags;
-    a.a_vec = ((uintptr_t)a_scales & 7) == 0 && a_scale_stride % 8 == 0;
-    a.b_vec = ((uintptr_t)b_scales & 7) == 0 && b_scale_stride % 8 == 0;
+    const auto align = [](const void *p, int64_t stride) {
+        const uint64_t bits = (uint64_t)(uintptr_t)p | (uint64_t)stride;
+        return bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : 1;
+    };
+    a.a_align = align(a_scales, m > 1 ? a_scale_stride : 0), a.b_align = align(b_scales, b_scale_stride);
     const int64_t mean = (m + n_groups - 1) / n_groups;
     a.bn = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 ? 64 : mean <= 128 ? 128 : kMmMaxTokens;
     const int64_t row_tiles = (n + kMmRows - 1) / kMmRows;

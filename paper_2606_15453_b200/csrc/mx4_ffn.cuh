@@ -56,6 +56,8 @@ __host__ __device__ constexpr int mxf_stages(int nmat, int mt)
     return n < kMxfMaxStages ? n : kMxfMaxStages;
 }
 
+static_assert(mxf_stages(2, kMxfTokens) >= 4 && mxf_stages(1, kMxfTokens) >= 4 && mxf_stages(2, 1) >= 4, "");  // scale warps
+
 // Byte offsets inside an MX4 expert image: codes of gate [I][H/2], up, down [H][I/2], then the
 // scales of the three in the same order.
 __host__ __device__ inline size_t mx4_image_codes(int H, int I, int mat) { return (size_t)mat * ((size_t)H * I / 2); }
@@ -139,16 +141,29 @@ struct Mx4PlanesArgs {
 };
 
 // Entries of at most mt tokens per expert from given ids, pairs of an expert in index order.  ids
-// outside [0, E) have no entry.  One CTA of 256 threads, one thread an expert; s_ids: B*K ints.
-__device__ __forceinline__ void group_ids(const Mx4PlanesArgs &a, int *s_ids, int *s_g, int *s_p)
+// outside [0, E) have no entry.  One CTA of 256 threads.  A pair's place among its expert's pairs is its
+// rank in its chunk of 32 (one match per warp) behind the chunks before it: a thread per expert that
+// walked all pairs took 40 us at 64 sequences x 6 experts.
+// s_cnt: [chunks][256], pairs of an expert in a chunk, then behind all chunks before it.
+__device__ __forceinline__ void group_ids(const Mx4PlanesArgs &a, uint16_t *s_cnt, int *s_g, int *s_p, int *s_first)
 {
-    const int e = threadIdx.x, n = a.B * a.K;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) s_ids[i] = a.ids[i];
+    const int e = threadIdx.x, n = a.B * a.K, chunks = (n + kWarp - 1) / kWarp;
+    const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+    for (int c = 0; c < chunks; ++c) s_cnt[c * 256 + e] = 0;
+    __syncthreads();
+    for (int c = warp; c < chunks; c += 8) {
+        const int i = c * kWarp + lane;
+        const int id = i < n ? a.ids[i] : -1;
+        const unsigned same = __match_any_sync(kFull, id);
+        if ((unsigned)id < (unsigned)a.E && lane == __ffs(same) - 1) s_cnt[c * 256 + id] = (uint16_t)__popc(same);
+    }
     __syncthreads();
     int cnt = 0;
-    if (e < a.E)
-        for (int i = 0; i < n; ++i) cnt += s_ids[i] == e;
-    const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+    for (int c = 0; c < chunks; ++c) {
+        const int k = s_cnt[c * 256 + e];
+        s_cnt[c * 256 + e] = (uint16_t)cnt;   // at most 64 * 32 pairs
+        cnt += k;
+    }
     int g = (cnt + a.mt - 1) / a.mt, p = cnt;   // inclusive prefix sums over the experts
 #pragma unroll
     for (int o = 1; o < kWarp; o <<= 1) {
@@ -160,23 +175,32 @@ __device__ __forceinline__ void group_ids(const Mx4PlanesArgs &a, int *s_ids, in
     for (int w = 0; w < warp; ++w) g += s_g[w], p += s_p[w];
     if (e == 255) *a.wl.n_groups = g;
     g -= (cnt + a.mt - 1) / a.mt, p -= cnt;
+    s_first[e] = p;
     if (e < a.E) {
         a.table[e] = a.experts + (size_t)e * a.img_bytes;
         for (int t = 0, q = g; t < cnt; t += a.mt, ++q)
             a.wl.g_expert[q] = e, a.wl.g_start[q] = p + t, a.wl.g_count[q] = min(a.mt, cnt - t);
-        for (int i = 0; cnt && i < n; ++i)
-            if (s_ids[i] == e) a.wl.pair_token[p] = i / a.K, a.wl.pair_slot[p] = i, ++p;
+    }
+    __syncthreads();
+    for (int c = warp; c < chunks; c += 8) {
+        const int i = c * kWarp + lane;
+        const int id = i < n ? a.ids[i] : -1;
+        const unsigned same = __match_any_sync(kFull, id);
+        if ((unsigned)id < (unsigned)a.E) {
+            const int at = s_first[id] + s_cnt[c * 256 + id] + __popc(same & ((1u << lane) - 1));
+            a.wl.pair_token[at] = i / a.K, a.wl.pair_slot[at] = i;
+        }
     }
 }
 
 __global__ void __launch_bounds__(256) mx4_planes_kernel(const Mx4PlanesArgs a)
 {
-    extern __shared__ int s_ids[];
-    __shared__ int s_g[8], s_p[8];
+    extern __shared__ uint16_t s_cnt[];   // [chunks of 32 pairs][256]; only where a CTA groups
+    __shared__ int s_g[8], s_p[8], s_first[256];
     pdl_launch_dependents();
     pdl_wait();
     if ((int)blockIdx.x < a.group_ctas) {
-        group_ids(a, s_ids, s_g, s_p);
+        group_ids(a, s_cnt, s_g, s_p, s_first);
         return;
     }
     const int blocks = a.H / kMxBlock, lane = threadIdx.x % kWarp;
@@ -205,16 +229,8 @@ struct Mx4FfnArgs {
     // down
     float *part;                         // [pair][splits][rows]
     unsigned *err;
-    int w_align;                         // alignment of a weight matrix's scale rows: 8, 4 or 1
+    int w_align;                         // what a weight matrix's scale rows are aligned to: 8, 4 or 1
 };
-
-// eight scale bytes from block kb on, by the widest loads the rows' alignment allows
-__device__ __forceinline__ uint2 load_scales8_by(const uint8_t *row, int kb, int blocks, int align)
-{
-    if (align == 4 && kb + 8 <= blocks)
-        return make_uint2(__ldg(reinterpret_cast<const uint32_t *>(row + kb)), __ldg(reinterpret_cast<const uint32_t *>(row + kb) + 1));
-    return load_scales8(row, kb, blocks, align == 8);
-}
 
 struct Mx4FfnTask {
     int g, row0, z;
@@ -258,7 +274,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
     pdl_launch_dependents();
     if (tid == 0) {
         s_dead = 0;
-        for (int s = 0; s < NS; ++s) dmbar_init(&full[s], 1 + 4), dmbar_init(&empty[s], 1);
+        for (int s = 0; s < NS; ++s) dmbar_init(&full[s], 2), dmbar_init(&empty[s], 1);
         for (int b = 0; b < 2; ++b) dmbar_init(&tfull[b], 1), dmbar_init(&tempty[b], 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -285,34 +301,29 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
     };
 
     if (warp == 0) {
-        if (lane == 0) {
+        if (elect_one()) {
             int s = 0, issued = 0;
             uint32_t par = 0;
             for (int task = first; task < n_tasks && !*dead; task += step) {
                 const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-                const int ge = a.wl.g_expert[t.g], start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
+                const int ge = a.wl.g_expert[t.g];
                 const bool shared = ge >= a.E;
                 const int img = (int)((unsigned long long)(a.blob[ge] - a.store[shared]) / a.img_bytes);
                 const CUtensorMap *w0 = shared ? &map_s0 : &map_w0, *w1 = shared ? &map_s1 : &map_w1;
-                int row[kMxfTokens];
-#pragma unroll
-                for (int i = 0; i < kMxfTokens; ++i)
-                    if (i < cnt) row[i] = kPlanes * (NMAT == 2 ? a.wl.pair_token[start + i] : a.wl.pair_slot[start + i]);
                 int k_beg, k_end;
                 k_range(t.z, k_beg, k_end);
                 for (int k = k_beg; k < k_end; ++k, ++issued) {
                     if (!dmbar_wait(&empty[s], par ^ 1u, dead)) break;
                     uint8_t *st = dsm + (size_t)s * slot;
-                    dmbar_expect_tx(&full[s], (uint32_t)(NMAT * kMmABytes + cnt * kPlanes * 128));
+                    dmbar_expect_tx(&full[s], (uint32_t)(NMAT * kMmABytes));
                     tma_load_3d(st, w0, k * 128, t.row0, img, &full[s]);
                     if (NMAT == 2) tma_load_3d(st + kMmABytes, w1, k * 128, t.row0, img, &full[s]);
-#pragma unroll
-                    for (int i = 0; i < kMxfTokens; ++i)
-                        if (i < cnt) tma_load_2d(st + x_at + i * kPlanes * 128, &map_x, k * 128, row[i], &full[s]);
                     if (++s == NS) s = 0, par ^= 1u;
                 }
             }
-            int none = 0;   // every load that was issued lands before the CTA may exit, after an error too
+            // every load that was issued lands before the CTA may exit, after an error too; the token
+            // loads of a stage complete on the same barrier
+            int none = 0;
             for (int i = 0; i < min(issued, NS); ++i) {
                 if (s == 0) s = NS, par ^= 1u;
                 --s;
@@ -321,7 +332,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (elect_one()) {
             int s = 0, it = 0;
             uint32_t par = 0;
             for (int task = first; task < n_tasks && !*dead; task += step, ++it) {
@@ -399,59 +410,84 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             if (!ok) break;
         }
     } else {
-        // scales: thread = row of the weight tiles, and a plane of a token
-        const int r = tid - 6 * kWarp;
-        const uint32_t at = (uint32_t)((r % 32) * 16 + (r / 32) * 4);
-        int s = 0;
-        uint32_t par = 0;
-        bool ok = true;
-        for (int task = first; task < n_tasks && ok; task += step) {
-            const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-            const int ge = a.wl.g_expert[t.g], start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
+        // scales and the tokens' codes, a warp every fourth stage (see mx4_matmul.cuh; up to twelve loads a
+        // stage by one thread would hold the weights' back).  A task's steps may differ by one between
+        // splits, so the position is walked, not computed
+        const int w = warp - 6;
+        const int x_align = a.blocks % 8 == 0 ? 8 : a.blocks % 4 == 0 ? 4 : 1;
+        struct Pos {
+            int task, k, end;
+        };
+        auto enter = [&](Pos &p) {   // first step of task p.task
+            if (p.task >= n_tasks) return;
+            k_range(mxf_task<NMAT>(a, p.task).z, p.k, p.end);
+        };
+        auto forward = [&](Pos &p, int by) {
+            p.k += by;
+            while (p.task < n_tasks && p.k >= p.end) {
+                const int over = p.k - p.end;
+                p.task += step;
+                enter(p);
+                p.k += over;
+            }
+        };
+        auto load = [&](const Pos &p, uint2 (&vw)[NMAT][4], uint2 (&vx)[3], int &cnt, int &xrow) {
+            if (p.task >= n_tasks) return false;
+            const Mx4FfnTask t = mxf_task<NMAT>(a, p.task);
+            const int ge = a.wl.g_expert[t.g], start = a.wl.g_start[t.g];
+            cnt = a.wl.g_count[t.g];
+            xrow = 0;   // lane i: first plane of token i
+            if (lane < cnt) xrow = kPlanes * (NMAT == 2 ? a.wl.pair_token[start + lane] : a.wl.pair_slot[start + lane]);
             const uint8_t *img = a.blob[ge];
-            const long long wrow = (long long)min(t.row0 + r, a.rows - 1) * a.blocks;
-            const uint8_t *pw[NMAT];
+            const int kb = p.k * kMmStageBlocks;
 #pragma unroll
-            for (int m = 0; m < NMAT; ++m) pw[m] = img + a.scale_off[m] + wrow;
-            const bool has_x = r < cnt * kPlanes;
-            const uint8_t *px = nullptr;
-            if (has_x) {
-                const int pair = start + r / kPlanes;
-                px = a.x_scales + ((long long)(NMAT == 2 ? a.wl.pair_token[pair] : a.wl.pair_slot[pair]) * kPlanes + r % kPlanes) * a.blocks;
+            for (int m = 0; m < NMAT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    vw[m][r] = load_scales8(img + a.scale_off[m] + (long long)min(t.row0 + 32 * r + lane, a.rows - 1) * a.blocks, kb, a.blocks, a.w_align);
+#pragma unroll
+            for (int r = 0; r < 3; ++r) {
+                const int q = 32 * r + lane;   // row of the B tile: plane q % 8 of token q / 8
+                vx[r] = make_uint2(0u, 0u);
+                const long long row = __shfl_sync(kFull, xrow, q / kPlanes) + q % kPlanes;
+                if (q < cnt * kPlanes) vx[r] = load_scales8(a.x_scales + row * a.blocks, kb, a.blocks, x_align);
             }
-            const int x_align = a.blocks % 8 == 0 ? 8 : a.blocks % 4 == 0 ? 4 : 1;
-            int k_beg, k_end;
-            k_range(t.z, k_beg, k_end);
-            for (int k0 = k_beg; k0 < k_end && ok; k0 += 4) {
-                uint2 vw[4][NMAT], vx[4];
+            return true;
+        };
+        uint2 vw[NMAT][4], vx[3], nw[NMAT][4], nx[3];
+        Pos p = {first, 0, 0};
+        enter(p);
+        forward(p, w);
+        int i = w;
+        int cnt = 0, xrow = 0, n_cnt = 0, n_xrow = 0;
+        bool more = load(p, vw, vx, cnt, xrow);
+        while (more) {
+            const int k = p.k;
+            forward(p, 4);
+            more = load(p, nw, nx, n_cnt, n_xrow);
+            const int s = i % NS;
+            const bool ok = __all_sync(kFull, dmbar_wait(&empty[s], ((uint32_t)(i / NS) & 1u) ^ 1u, dead));
+            uint8_t *st = dsm + (size_t)s * slot;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int kb = min(k0 + i, n_steps - 1) * kMmStageBlocks;
-#pragma unroll
-                    for (int m = 0; m < NMAT; ++m) vw[i][m] = load_scales8_by(pw[m], kb, a.blocks, a.w_align);
-                    if (has_x) vx[i] = load_scales8_by(px, kb, a.blocks, x_align);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (k0 + i < k_end && ok) {
-                        ok = __all_sync(kFull, dmbar_wait(&empty[s], par ^ 1u, dead));
-                        uint8_t *st = dsm + (size_t)s * slot;
-#pragma unroll
-                        for (int m = 0; m < NMAT; ++m) {
-                            *reinterpret_cast<uint32_t *>(st + sfa_at + 1024 * m + at) = vw[i][m].x;
-                            *reinterpret_cast<uint32_t *>(st + sfa_at + 1024 * m + 512 + at) = vw[i][m].y;
-                        }
-                        if (has_x) {
-                            *reinterpret_cast<uint32_t *>(st + sfb_at + at) = vx[i].x;
-                            *reinterpret_cast<uint32_t *>(st + sfb_at + 512 + at) = vx[i].y;
-                        }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) dmbar_arrive(&full[s]);
-                        if (++s == NS) s = 0, par ^= 1u;
-                    }
-                }
+            for (int m = 0; m < NMAT; ++m) store_scales<4>(st + sfa_at + 1024 * m, 512, lane, vw[m]);
+            store_scales<3>(st + sfb_at, 512, lane, vx);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (!ok) break;   // nothing is waited for any more, and nothing may be loaded behind the drain
+            const uint32_t xst = dsmem_u32(st + x_at);
+            if (elect_one()) dmbar_expect_tx(&full[s], (uint32_t)(cnt * kPlanes * 128));
+            for (int q = 0; q < cnt; ++q) {
+                const int row = __shfl_sync(kFull, xrow, q);
+                if (elect_one()) tma_load_2d_at(xst + q * kPlanes * 128, &map_x, k * 128, row, &full[s]);
             }
+#pragma unroll
+            for (int m = 0; m < NMAT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) vw[m][r] = nw[m][r];
+#pragma unroll
+            for (int r = 0; r < 3; ++r) vx[r] = nx[r];
+            cnt = n_cnt, xrow = n_xrow;
+            i += 4;
         }
     }
     if (NMAT == 2 && ranks > 1 && first < n_tasks) {   // one task per cluster
@@ -491,17 +527,30 @@ __global__ void __launch_bounds__(256) mx4_combine_kernel(const FfnArgs a, const
     const int KS = a.K + a.n_shared;
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < a.B * a.H; i += gridDim.x * blockDim.x) {
         const int b = i / a.H, c = i % a.H;
-        float y = 0.f;
-        for (int q = 0; q < KS; ++q) {
-            const int k = q < a.n_shared ? a.K + q : q - a.n_shared;
-            if (ids && (unsigned)ids[b * a.K + k] >= (unsigned)a.E) continue;
-            const float *part = a.part + ((long long)(b * KS + k) * a.S) * a.H + c;
-            float p = 0.f;
-#pragma unroll 4
-            for (int z = 0; z < a.S; ++z) p += __ldcg(part + (long long)z * a.H);
-            y = q < a.n_shared ? y + p : fmaf(a.w[b * a.K + k], p, y);
+        const float h = a.h[i];
+        float y = 0.f, p = 0.f;
+        const int terms = KS * a.S;
+        for (int t0 = 0; t0 < terms; t0 += 8) {   // eight terms' loads together (each is a trip to L2)
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int t = t0 + j, q = t / a.S, k = q < a.n_shared ? a.K + q : q - a.n_shared;
+                v[j] = t < terms && !(ids && (unsigned)ids[b * a.K + k] >= (unsigned)a.E)
+                           ? __ldcg(a.part + ((long long)(b * KS + k) * a.S + (t - q * a.S)) * a.H + c) : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int t = t0 + j, q = t / a.S;
+                if (t < terms) {
+                    p += v[j];
+                    if (t - q * a.S == a.S - 1) {
+                        y = q < a.n_shared ? y + p : fmaf(a.w[b * a.K + q - a.n_shared], p, y);
+                        p = 0.f;
+                    }
+                }
+            }
         }
-        a.h_out[i] = fmaf(a.residual_scale, y, a.h[i]);
+        a.h_out[i] = fmaf(a.residual_scale, y, h);
     }
 }
 

@@ -14,9 +14,12 @@
 //   warp 1      one thread copies a stage's scales into tensor memory (tcgen05.cp), issues its four
 //               MMAs and frees the stage; the warp owns the tensor-memory allocation
 //   warps 2-5   epilogue, from two accumulator buffers
-//   warps 6-9   scales: a thread reads a row's eight scale bytes of a stage (four stages ahead, in
-//               registers) and writes them where the copy expects them: for 128 rows and four blocks
-//               512 bytes, row r at (r % 32) * 16 + (r / 32) * 4
+//   warps 6-9   scales, a warp every fourth stage: a lane reads eight scale bytes of the rows lane,
+//               lane + 32, ... (its next stage's before it waits for this one's place in the ring) and
+//               writes them where the copy expects them: for 128 rows and four blocks 512 bytes, row r
+//               at (r % 32) * 16 + (r / 32) * 4, so four rows of a lane are one 16-byte store.  With the
+//               four warps on one stage, a row a thread, the loads' latency and the proxy fence of every
+//               stage came one after the other and bounded the kernel (1600 cycles a stage).
 // The scales of a stage have their own columns in tensor memory, as many sets as there are stages:
 // a set is rewritten only after the commit that frees its stage, so no copy can overtake an MMA
 // that still reads the set.
@@ -56,6 +59,10 @@ __host__ __device__ constexpr int mm_stages(int bn)
     return n < kMmMaxStages ? n : kMmMaxStages;
 }
 
+// a scale warp waits for step i + 4 knowing that step i - NS has been consumed: with four stages or more
+// it is never two phases ahead of a barrier, whose parity would then deceive it
+static_assert(mm_stages(16) >= 4 && mm_stages(128) >= 4 && mm_stages(kMmMaxTokens) >= 4, "");
+
 struct Mx4MatmulArgs {
     const uint8_t *a_scales, *b_scales;
     long long a_scale_stride, b_scale_stride;  // bytes
@@ -66,7 +73,7 @@ struct Mx4MatmulArgs {
     void *out;
     long long out_stride;   // elements
     unsigned *err;          // may be nullptr
-    bool a_vec, b_vec;      // scale rows start on 8-byte boundaries
+    int a_align, b_align;   // what scale rows are aligned to: 8, 4 or 1 bytes
 };
 
 // mxf4 descriptor: e2m1 x e2m1, e8m0 scales, both K-major, M = 128, N = n; which half of a scale
@@ -105,12 +112,15 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16])
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// eight scale bytes of a row from block kb on; blocks past the end read as 1.0 (their codes are
-// zero, and zero times a NaN scale would not be)
-__device__ __forceinline__ uint2 load_scales8(const uint8_t *row, int kb, int blocks, bool vec)
+// eight scale bytes of a row from block kb on, by the widest loads the rows' alignment allows; blocks
+// past the end read as 1.0 (their codes are zero, and zero times a NaN scale would not be)
+__device__ __forceinline__ uint2 load_scales8(const uint8_t *row, int kb, int blocks, int align)
 {
+    if (align >= 4 && kb + 8 <= blocks) {
+        if (align == 8) return __ldg(reinterpret_cast<const uint2 *>(row + kb));
+        return make_uint2(__ldg(reinterpret_cast<const uint32_t *>(row + kb)), __ldg(reinterpret_cast<const uint32_t *>(row + kb) + 1));
+    }
     uint2 v = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
-    if (vec && kb + 8 <= blocks) return __ldg(reinterpret_cast<const uint2 *>(row + kb));
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (kb + i < blocks) {
@@ -119,6 +129,22 @@ __device__ __forceinline__ uint2 load_scales8(const uint8_t *row, int kb, int bl
             w = (w & ~(0xffu << (8 * (i & 3)))) | (b << (8 * (i & 3)));
         }
     return v;
+}
+// What a lane has read of G row groups (rows lane, lane + 32, ...), into the atoms of 128 rows x four
+// blocks: first half at st, second half of the stage's blocks `half` bytes behind it
+template <int G> __device__ __forceinline__ void store_scales(uint8_t *st, int half, int lane, const uint2 (&v)[G])
+{
+#pragma unroll
+    for (int a = 0; a < (G + 3) / 4; ++a) {
+        uint32_t x[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = 4 * a + i < G ? v[(4 * a + i) % G].x : 0u;   // (no index past the array, even unused)
+            y[i] = 4 * a + i < G ? v[(4 * a + i) % G].y : 0u;
+        }
+        *reinterpret_cast<uint4 *>(st + 512 * a + 16 * lane) = make_uint4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<uint4 *>(st + half + 512 * a + 16 * lane) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
 }
 
 // Which rows a task multiplies.
@@ -178,7 +204,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 
     if (tid == 0) {
         s_dead = 0;
-        for (int s = 0; s < NS; ++s) dmbar_init(&full[s], 1 + 4), dmbar_init(&empty[s], 1);
+        for (int s = 0; s < NS; ++s) dmbar_init(&full[s], 2), dmbar_init(&empty[s], 1);
         for (int b = 0; b < 2; ++b) dmbar_init(&tfull[b], 1), dmbar_init(&tempty[b], 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -225,7 +251,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const int k_beg = (int)((long long)n_steps * rank / a.splits), k_end = (int)((long long)n_steps * (rank + 1) / a.splits);
 
     if (warp == 0) {
-        if (lane == 0) {
+        if (elect_one()) {
             int s = 0, issued = 0;
             uint32_t par = 0;
             for (int task = first; task < n_tasks && !*dead; task += step) {
@@ -250,7 +276,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t id0 = umma_idesc_mxf4(bn, 0), id1 = umma_idesc_mxf4(bn, 1);
             const int cols = mm_scale_cols(bn);
             int s = 0, it = 0;
@@ -321,48 +347,49 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             if (!ok) break;
         }
     } else {
-        // scales: thread = row of the tile of b, and up to two tokens
-        const int r = tid - 6 * kWarp;
-        const uint32_t at = (uint32_t)((r % 32) * 16 + (r / 32) * 4);
-        int s = 0;
-        uint32_t par = 0;
-        bool ok = true;
-        for (int task = first; task < n_tasks && ok; task += step) {
+        // scales: this warp's stages are the CTA's steps w, w + 4, ... across its tasks
+        const int w = warp - 6, per_task = k_end - k_beg;
+        int task = first, k = k_beg + w;   // step i of the CTA, and the next of this warp's
+        auto load = [&](uint2 (&vb)[4], uint2 (&va)[6]) {
+            for (; task < n_tasks && k >= k_end; task += step) k -= per_task;
+            if (task >= n_tasks) return false;
             const Mx4Task t = mm_task(a, s_off, s_tile, task);
-            const uint8_t *pb = a.b_scales + ((long long)t.expert * a.n + min(t.row0 + r, a.n - 1)) * a.b_scale_stride;
-            const uint8_t *pa0 = a.a_scales + (long long)min(t.tok0 + r, a.m - 1) * a.a_scale_stride;
-            const uint8_t *pa1 = a.a_scales + (long long)min(t.tok0 + 128 + r, a.m - 1) * a.a_scale_stride;
-            for (int k0 = k_beg; k0 < k_end && ok; k0 += 4) {
-                uint2 vb[4], v0[4], v1[4];
+            const int kb = k * kMmStageBlocks;
+            k += 4;
+            const uint8_t *pb = a.b_scales + (long long)t.expert * a.n * a.b_scale_stride;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int kb = min(k0 + i, n_steps - 1) * kMmStageBlocks;
-                    vb[i] = load_scales8(pb, kb, a.blocks, a.b_vec);
-                    if (r < bn) v0[i] = load_scales8(pa0, kb, a.blocks, a.a_vec);
-                    if (128 + r < bn) v1[i] = load_scales8(pa1, kb, a.blocks, a.a_vec);
-                }
+            for (int r = 0; r < 4; ++r)
+                vb[r] = load_scales8(pb + (long long)min(t.row0 + 32 * r + lane, a.n - 1) * a.b_scale_stride, kb, a.blocks, a.b_align);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (k0 + i < k_end && ok) {
-                        ok = __all_sync(kFull, dmbar_wait(&empty[s], par ^ 1u, dead));
-                        uint8_t *st = dsm + (size_t)s * slot;
-                        *reinterpret_cast<uint32_t *>(st + sfa_at + at) = vb[i].x;
-                        *reinterpret_cast<uint32_t *>(st + sfa_at + 512 + at) = vb[i].y;
-                        if (r < bn) {
-                            *reinterpret_cast<uint32_t *>(st + sfb_at + at) = v0[i].x;
-                            *reinterpret_cast<uint32_t *>(st + sfb_at + 512 * atoms + at) = v0[i].y;
-                        }
-                        if (128 + r < bn) {
-                            *reinterpret_cast<uint32_t *>(st + sfb_at + 512 + at) = v1[i].x;
-                            *reinterpret_cast<uint32_t *>(st + sfb_at + 512 * atoms + 512 + at) = v1[i].y;
-                        }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) dmbar_arrive(&full[s]);
-                        if (++s == NS) s = 0, par ^= 1u;
-                    }
-                }
+            for (int r = 0; r < 6; ++r)
+                if (32 * r < bn)
+                    va[r] = load_scales8(a.a_scales + (long long)min(t.tok0 + 32 * r + lane, a.m - 1) * a.a_scale_stride, kb, a.blocks, a.a_align);
+            return true;
+        };
+        uint2 vb[4], va[6], nb[4], na[6];
+        uint32_t i = w;
+        bool more = load(vb, va);
+        while (more) {
+            more = load(nb, na);
+            const int s = (int)(i % NS);
+            const bool ok = __all_sync(kFull, dmbar_wait(&empty[s], ((i / NS) & 1u) ^ 1u, dead));
+            uint8_t *st = dsm + (size_t)s * slot;
+            store_scales<4>(st + sfa_at, 512, lane, vb);
+            if (atoms == 1) {
+                const uint2 v4[4] = {va[0], va[1], va[2], va[3]};
+                store_scales<4>(st + sfb_at, 512, lane, v4);
+            } else {
+                store_scales<6>(st + sfb_at, 1024, lane, va);
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) dmbar_arrive(&full[s]);
+            if (!ok) break;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vb[r] = nb[r];
+#pragma unroll
+            for (int r = 0; r < 6; ++r) va[r] = na[r];
+            i += 4;
         }
     }
     if (a.splits > 1 && first < n_tasks) {  // one task per cluster, the same for all its CTAs

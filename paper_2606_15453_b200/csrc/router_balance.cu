@@ -36,7 +36,7 @@ int lanes_per_row(int n_experts)
 }
 int bal_grid(int64_t tokens, int lpr)
 {
-    const int64_t rows = (int64_t)(kBalThreads / kWarp) * (kWarp / lpr);
+    const int64_t rows = (int64_t)(kBalThreads / kWarp) * (kWarp / lpr) * kBalRows;
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
         (void)cudaGetLastError();

@@ -24,6 +24,7 @@ namespace stmoe_dev {
 
 constexpr int kBalThreads = 256;
 constexpr int kBalMaxExperts = 256;
+constexpr int kBalRows = 4;         // rows of a lane in flight
 constexpr int kBalMaxCtas = 592;   // four a SM: rows of the partial-sum workspace
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -104,18 +105,15 @@ template <int LPR> __device__ __forceinline__ float lanes_sum(float v)
 template <int LPR> __device__ __forceinline__ float bal_softmax(float (&z)[8], bool &live)
 {
     float m = -INFINITY;
-    int any = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, z[i]), any |= !(z[i] == -INFINITY);
-#pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) any |= __shfl_xor_sync(kFull, any, o);
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, z[i]);
     m = lanes_max<LPR>(m);
-    live = any != 0;
     const float m2 = m == -INFINITY ? 0.f : m * kLog2e;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) z[i] = ex2(fmaf(z[i], kLog2e, -m2)), sum += z[i];
     sum = lanes_sum<LPR>(sum);
+    live = sum != 0.f;   // 0 where all logits are -infinity (a NaN is not 0)
     const float inv = 1.f / sum;
 #pragma unroll
     for (int i = 0; i < 8; ++i) z[i] *= inv;
@@ -135,26 +133,37 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kBalThreads) router
     __syncthreads();
     float p[8] = {}, zz = 0.f;
     int n = 0;
-    const int stepr = gridDim.x * W * RPW;
-    for (long long t0 = (long long)(blockIdx.x * W + warp) * RPW; t0 < a.T; t0 += stepr) {
-        const long long t = t0 + sub;
-        bool on = t < a.T && (!a.mask || a.mask[t]);
-        float z[8];
-        if (on) {
-            bal_load<DT, LPR>(reinterpret_cast<const T *>(a.logits) + t * a.stride, a.E, l, a.vec, z);
-        } else {
+    // kBalRows rows of a lane in flight: one alone leaves the loads' latency bare
+    const int stepr = gridDim.x * W * RPW * kBalRows;
+    for (long long t0 = (long long)(blockIdx.x * W + warp) * RPW * kBalRows + sub; t0 - sub < a.T; t0 += stepr) {
+        float z[kBalRows][8];
+        bool on[kBalRows];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = -INFINITY;
+        for (int r = 0; r < kBalRows; ++r) {
+            const long long t = t0 + r * RPW;
+            on[r] = t < a.T && (!a.mask || a.mask[t]);
         }
-        bool live;
-        const float lse = bal_softmax<LPR>(z, live);
-        if (on && live) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] += z[i];
-            if (l == 0) zz = fmaf(lse, lse, zz), ++n;
-            for (int k = l; k < a.K; k += LPR) {
-                const int e = __ldg(a.ids + t * a.K + k);
-                if ((unsigned)e < (unsigned)a.E) atomicAdd(&s_cnt[e], 1);
+        for (int r = 0; r < kBalRows; ++r) {
+            if (on[r]) {
+                bal_load<DT, LPR>(reinterpret_cast<const T *>(a.logits) + (t0 + r * RPW) * a.stride, a.E, l, a.vec, z[r]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[r][i] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kBalRows; ++r) {
+            bool live;
+            const float lse = bal_softmax<LPR>(z[r], live);
+            if (on[r] && live) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] += z[r][i];
+                if (l == 0) zz = fmaf(lse, lse, zz), ++n;
+                for (int k = l; k < a.K; k += LPR) {
+                    const int e = __ldg(a.ids + (t0 + r * RPW) * a.K + k);
+                    if ((unsigned)e < (unsigned)a.E) atomicAdd(&s_cnt[e], 1);
+                }
             }
         }
     }
@@ -200,10 +209,18 @@ __global__ void __launch_bounds__(1024) router_balance_finish_kernel(const Balan
     double v = 0.;
     int c = 0;
     if (g < G)
-        for (int b = g; b < a.ctas; b += G) {
-            const float *part = a.part + (size_t)b * words;
-            v += (double)__ldcg(part + e);
-            c += __ldcg(reinterpret_cast<const int *>(part) + cols + e);
+        for (int b0 = g; b0 < a.ctas; b0 += 8 * G) {   // eight CTAs' words in flight
+            float x[8];
+            int y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float *part = a.part + (size_t)(b0 + j * G) * words;
+                x[j] = 0.f, y[j] = 0;
+                if (b0 + j * G < a.ctas)
+                    x[j] = __ldcg(part + e), y[j] = __ldcg(reinterpret_cast<const int *>(part) + cols + e);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v += (double)x[j], c += y[j];
         }
     s_sum[tid] = v, s_int[tid] = c;
     __syncthreads();
@@ -250,27 +267,37 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kBalThreads) router
         const int e = bal_index<DT, LPR>(l, i, vec);
         f[i] = e < a.E ? (float)a.counts[e] * rn / (float)a.K : 0.f;
     }
-    const int stepr = gridDim.x * W * RPW;
-    for (long long t0 = (long long)(blockIdx.x * W + warp) * RPW; t0 < a.T; t0 += stepr) {
-        const long long t = t0 + sub;
-        const bool on = t < a.T && (!a.mask || a.mask[t]);
-        float z[8];
-        if (on) {
-            bal_load<DT, LPR>(reinterpret_cast<const T *>(a.logits) + t * a.stride, a.E, l, vec, z);
-        } else {
+    const int stepr = gridDim.x * W * RPW * kBalRows;
+    for (long long t0 = (long long)(blockIdx.x * W + warp) * RPW * kBalRows + sub; t0 - sub < a.T; t0 += stepr) {
+        float z[kBalRows][8];
+        bool on[kBalRows];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = -INFINITY;
+        for (int r = 0; r < kBalRows; ++r) {
+            const long long t = t0 + r * RPW;
+            on[r] = t < a.T && (!a.mask || a.mask[t]);
         }
-        bool live;
-        const float lse = bal_softmax<LPR>(z, live);
-        float dot = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dot = fmaf(f[i], z[i], dot);
-        dot = lanes_sum<LPR>(dot);
-        const float c = fmaf(gz, lse, -gb * dot);   // dz = p (gb f + gz lse - gb dot)
+        for (int r = 0; r < kBalRows; ++r) {
+            if (on[r]) {
+                bal_load<DT, LPR>(reinterpret_cast<const T *>(a.logits) + (t0 + r * RPW) * a.stride, a.E, l, vec, z[r]);
+            } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = on && live ? z[i] * fmaf(gb, f[i], c) : 0.f;
-        if (t < a.T) {
+                for (int i = 0; i < 8; ++i) z[r][i] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kBalRows; ++r) {
+            bool live;
+            const float lse = bal_softmax<LPR>(z[r], live);
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dot = fmaf(f[i], z[r][i], dot);
+            dot = lanes_sum<LPR>(dot);
+            const float c = fmaf(gz, lse, -gb * dot);   // dz = p (gb f + gz lse - gb dot)
+            const long long t = t0 + r * RPW;
+            if (t >= a.T) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[r][i] = on[r] && live ? z[r][i] * fmaf(gb, f[i], c) : 0.f;
             T *out = reinterpret_cast<T *>(a.dlogits) + t * a.dstride;
             if (vec) {
 #pragma unroll
@@ -278,13 +305,13 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kBalThreads) router
                     const int e = bal_index<DT, LPR>(l, g * El::kVec, true);
                     T o[El::kVec];
 #pragma unroll
-                    for (int i = 0; i < El::kVec; ++i) o[i] = El::from_f32(z[g * El::kVec + i]);
+                    for (int i = 0; i < El::kVec; ++i) o[i] = El::from_f32(z[r][g * El::kVec + i]);
                     if (e < a.E) *reinterpret_cast<uint4 *>(out + e) = *reinterpret_cast<const uint4 *>(o);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (i * LPR + l < a.E) out[i * LPR + l] = El::from_f32(z[i]);
+                    if (i * LPR + l < a.E) out[i * LPR + l] = El::from_f32(z[r][i]);
             }
         }
     }

@@ -443,7 +443,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
     pa.h = fa.h, pa.B = fa.B, pa.H = H, pa.codes = b.x_codes, pa.scales = b.x_scales;
     const int blocks = fa.B * H / kMxBlock;
     ST_TRY(mx4_launch(mx4_planes_kernel, pa.group_ctas + std::min(sms * 4, (blocks + 7) / 8), 256,
-                      pa.group_ctas ? sizeof(int) * (size_t)fa.B * fa.K : 0, 1, st, pa));
+                      pa.group_ctas ? sizeof(uint16_t) * 256 * (size_t)((fa.B * fa.K + kWarp - 1) / kWarp) : 0, 1, st, pa));
 
     // at most this many entries: an expert's pairs fill its entries but for the last
     const int entries = std::min(pairs, fa.E + fa.n_shared + pairs / mt);

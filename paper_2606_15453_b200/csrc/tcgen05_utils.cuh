@@ -19,6 +19,19 @@ __device__ __forceinline__ void dmbar_arrive(uint64_t *bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(dsmem_u32(bar)) : "memory");
 }
+// One lane of a converged warp.  The TMA and tcgen05 instructions take their operands from uniform
+// registers: under a plain `lane == 0` the compiler cannot tell that one lane is left and wraps each of
+// them in a loop over the active lanes' values (measured: 75-130 cycles an instruction).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t mine;
+    asm volatile(
+        "{.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;}"
+        : "=r"(mine));
+    return mine != 0;
+}
 // bounded wait on a phase parity; false when the limit ran out or another thread gave up
 __device__ __forceinline__ bool dmbar_wait(uint64_t *bar, uint32_t parity, volatile int *dead,
                                            int spin_limit = kDenseSpinLimit)
@@ -75,12 +88,16 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, i
         ::"r"(dsmem_u32(dst)), "l"(map), "r"(dsmem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
         : "memory");
 }
-__device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, int c0, int c1, uint64_t *bar)
+__device__ __forceinline__ void tma_load_2d_at(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint64_t *bar)
 {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-        ::"r"(dsmem_u32(dst)), "l"(map), "r"(dsmem_u32(bar)), "r"(c0), "r"(c1)
+        ::"r"(dst), "l"(map), "r"(dsmem_u32(bar)), "r"(c0), "r"(c1)
         : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, int c0, int c1, uint64_t *bar)
+{
+    tma_load_2d_at(dsmem_u32(dst), map, c0, c1, bar);
 }
 // K-major operand tile in the 128-byte swizzled layout (rows of 128 bytes, 8-row groups 1024
 // bytes apart, tile base 1024-byte aligned); kstep = which 32-byte slice of the row (one MMA's
