@@ -246,11 +246,10 @@ template <int NMAT> __device__ __forceinline__ Mx4FfnTask mxf_task(const Mx4FfnA
     return t;
 }
 
-// SiLU(g) * u for 32 consecutive rows of one pair, as planes
-__device__ __forceinline__ void mxf_store_act(const Mx4FfnArgs &a, float g, float u, int pair, int row, int lane)
+// SiLU(g) * u for 32 consecutive rows of one pair, as planes; inv: the token's RMSNorm factor, applied
+// to the sums: W (inv * h) = inv * (W h)
+__device__ __forceinline__ void mxf_store_act(const Mx4FfnArgs &a, float g, float u, int slot, float inv, int row, int lane)
 {
-    const int slot = a.wl.pair_slot[pair];
-    const float inv = a.inv_rms ? a.inv_rms[a.wl.pair_token[pair]] : 1.f;  // W (inv * h) = inv * (W h)
     g *= inv, u *= inv;
     planes_store(g / (1.f + expf(-g)) * u, a.act_codes, a.act_scales, slot, row / kMxBlock, a.rows / kMxBlock, lane);
 }
@@ -332,43 +331,44 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (elect_one()) {
-            int s = 0, it = 0;
-            uint32_t par = 0;
-            for (int task = first; task < n_tasks && !*dead; task += step, ++it) {
-                const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-                const int n = mxf_cols(a.wl.g_count[t.g]);
-                const uint32_t id0 = umma_idesc_mxf4(n, 0), id1 = umma_idesc_mxf4(n, 1);
-                const int ab = it & 1;
-                if (!dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)) break;
+        const bool leader = elect_one();   // the whole warp walks the loop, one lane issues
+        const uint32_t ring = dsmem_u32(dsm);
+        int s = 0, it = 0;
+        uint32_t par = 0;
+        bool ok = true;
+        for (int task = first; task < n_tasks && ok; task += step, ++it) {
+            const Mx4FfnTask t = mxf_task<NMAT>(a, task);
+            const int n = mxf_cols(a.wl.g_count[t.g]);
+            const uint32_t id0 = umma_idesc_mxf4(n, 0), id1 = umma_idesc_mxf4(n, 1);
+            const int ab = it & 1;
+            if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + ab * kMxfAccStride;
+            int k_beg, k_end;
+            k_range(t.z, k_beg, k_end);
+            for (int k = k_beg; k < k_end; ++k) {
+                if (!(ok = __all_sync(kFull, dmbar_wait(&full[s], par, dead)))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t acc = tmem + ab * kMxfAccStride;
-                int k_beg, k_end;
-                k_range(t.z, k_beg, k_end);
-                bool ok = true;
-                for (int k = k_beg; k < k_end; ++k) {
-                    if (!(ok = dmbar_wait(&full[s], par, dead))) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t st = dsmem_u32(dsm + (size_t)s * slot);
-                    const uint32_t sf = tmem + kMxfScaleCol + s * kSetCols, sfb = sf + 8 * NMAT;
+                const uint32_t st = ring + s * slot;
+                const uint32_t sf = tmem + kMxfScaleCol + s * kSetCols, sfb = sf + 8 * NMAT;
+                const uint32_t dw = desc_low_sw128(st), dx = desc_low_sw128(st + x_at);
+                const uint32_t dsw = desc_low_scales(st + sfa_at), dsx = desc_low_scales(st + sfb_at);
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
+                for (int q = 0; q < 2; ++q) {
 #pragma unroll
-                        for (int m = 0; m < NMAT; ++m) umma_copy_scales(sf + 8 * m + 4 * q, st + sfa_at + 1024 * m + 512 * q);
-                        umma_copy_scales(sfb + 4 * q, st + sfb_at + 512 * q);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int m = 0; m < NMAT; ++m)
-                            umma_mxf4(acc + m * kMxfCols, umma_desc_sw128(st + m * kMmABytes, j), umma_desc_sw128(st + x_at, j),
-                                      j & 1 ? id1 : id0, sf + 8 * m + 4 * (j / 2), sfb + 4 * (j / 2), k > k_beg || j > 0);
-                    umma_commit(&empty[s]);
-                    if (++s == NS) s = 0, par ^= 1u;
+                    for (int m = 0; m < NMAT; ++m) umma_copy_scales(leader, sf + 8 * m + 4 * q, dsw + 64 * m + 32 * q);
+                    umma_copy_scales(leader, sfb + 4 * q, dsx + 32 * q);
                 }
-                if (!ok) break;
-                umma_commit(&tfull[ab]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int m = 0; m < NMAT; ++m)
+                        umma_mxf4(leader, acc + m * kMxfCols, dw + m * (kMmABytes >> 4) + 2 * j, dx + 2 * j, j & 1 ? id1 : id0,
+                                  sf + 8 * m + 4 * (j / 2), sfb + 4 * (j / 2), k > k_beg || j > 0);
+                umma_commit_if(leader, &empty[s]);
+                if (++s == NS) s = 0, par ^= 1u;
             }
+            if (ok) umma_commit_if(leader, &tfull[ab]);
         }
         __syncwarp();
     } else if (warp < 6) {
@@ -379,11 +379,19 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             const int ab = it & 1;
             const Mx4FfnTask t = mxf_task<NMAT>(a, task);
             const int start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
+            int slot_l = 0;      // lane i: the i-th pair's slot and RMSNorm factor, fetched while the MMAs run
+            float inv_l = 1.f;
+            if (lane < cnt) {
+                slot_l = a.wl.pair_slot[start + lane];
+                if (NMAT == 2 && a.inv_rms) inv_l = a.inv_rms[a.wl.pair_token[start + lane]];
+            }
             const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], (uint32_t)(it >> 1) & 1u, dead));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + ab * kMxfAccStride + ((uint32_t)(lg * kWarp) << 16);
             const int row = t.row0 + lg * kWarp + lane;
             for (int i = 0; i < cnt; ++i) {
+                const int slot_i = __shfl_sync(kFull, slot_l, i);
+                const float inv_i = __shfl_sync(kFull, inv_l, i);
                 float y[NMAT];
 #pragma unroll
                 for (int m = 0; m < NMAT; ++m) {
@@ -396,12 +404,12 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                 }
                 if (NMAT == 1) {
                     if (row < a.rows)
-                        a.part[((long long)a.wl.pair_slot[start + i] * a.splits + t.z) * a.rows + row] = y[0];
+                        a.part[((long long)slot_i * a.splits + t.z) * a.rows + row] = y[0];
                 } else if (ranks > 1) {
 #pragma unroll
                     for (int m = 0; m < NMAT; ++m) part[(m * kMxfTokens + i) * kMmRows + lg * kWarp + lane] = y[m];
                 } else if (t.row0 + lg * kWarp < a.rows) {   // rows are a multiple of 32: the whole warp or none of it
-                    mxf_store_act(a, y[0], y[NMAT - 1], start + i, row, lane);
+                    mxf_store_act(a, y[0], y[NMAT - 1], slot_i, inv_i, row, lane);
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -500,12 +508,14 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         for (int u = rank + ranks * warp; u < cnt * 4; u += ranks * (kMmThreads / kWarp)) {
             const int i = u / 4, r0 = (u % 4) * kWarp;
             if (t.row0 + r0 >= a.rows) continue;
+            const int slot_i = a.wl.pair_slot[start + i];
+            const float inv_i = a.inv_rms ? a.inv_rms[a.wl.pair_token[start + i]] : 1.f;
             float g = 0.f, v = 0.f;
             for (int z = 0; z < ranks; ++z) {
                 g += ld_cluster(part + (uint32_t)(i * kMmRows + r0 + lane) * 4, z);
                 v += ld_cluster(part + (uint32_t)((kMxfTokens + i) * kMmRows + r0 + lane) * 4, z);
             }
-            mxf_store_act(a, g, v, start + i, t.row0 + r0 + lane, lane);
+            mxf_store_act(a, g, v, slot_i, inv_i, t.row0 + r0 + lane, lane);
         }
         cluster_sync();
     }

@@ -44,6 +44,7 @@ constexpr int kMmMaxStages = 12;
 constexpr int kMmMaxSplits = 8;           // portable cluster size
 constexpr int kMmMaxGroups = 256;
 constexpr int kMmSmemBytes = 224 * 1024;  // dynamic; one CTA per SM
+constexpr int kMmStageOut = 2048;         // epilogue: bytes of shared memory of a warp
 constexpr int kMmAccStride = kMmMaxTokens;
 constexpr int kMmScaleCol = 2 * kMmAccStride;   // scale sets start behind the accumulators
 
@@ -54,7 +55,7 @@ __host__ __device__ constexpr int mm_scale_cols(int bn) { return 8 + 8 * mm_toke
 __host__ __device__ constexpr int mm_slot_bytes(int bn) { return (mm_stage_bytes(bn) + 1023) / 1024 * 1024; }
 __host__ __device__ constexpr int mm_stages(int bn)
 {
-    const int by_smem = (kMmSmemBytes - 1024) / mm_slot_bytes(bn), by_tmem = (512 - kMmScaleCol) / mm_scale_cols(bn);
+    const int by_smem = (kMmSmemBytes - 1024 - 4 * kMmStageOut) / mm_slot_bytes(bn), by_tmem = (512 - kMmScaleCol) / mm_scale_cols(bn);
     const int n = by_smem < by_tmem ? by_smem : by_tmem;
     return n < kMmMaxStages ? n : kMmMaxStages;
 }
@@ -72,6 +73,7 @@ struct Mx4MatmulArgs {
     int bn, splits;
     void *out;
     long long out_stride;   // elements
+    bool out_wide;          // rows of out start on 16-byte boundaries
     unsigned *err;          // may be nullptr
     int a_align, b_align;   // what scale rows are aligned to: 8, 4 or 1 bytes
 };
@@ -83,21 +85,34 @@ __device__ __forceinline__ uint32_t umma_idesc_mxf4(int n, int half)
     return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(kMmRows >> 7) << 27) |
            ((uint32_t)(2 * half) << 4) | ((uint32_t)(2 * half) << 29);
 }
-__device__ __forceinline__ void umma_mxf4(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                          bool accumulate)
+// from a whole warp, issued by the lane that `leader` names; a, b: low words of swizzled descriptors
+__device__ __forceinline__ void umma_mxf4(bool leader, uint32_t tmem_d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sfa,
+                                          uint32_t sfb, bool accumulate)
 {
     asm volatile(
-        "{.reg .pred p;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;}"
+        "{.reg .pred p, q;\n\t"
+        ".reg .b64 da, db;\n\t"
+        "setp.ne.b32 q, %0, 0;\n\t"
+        "setp.ne.b32 p, %7, 0;\n\t"
+        "mov.b64 da, {%2, %8};\n\t"
+        "mov.b64 db, {%3, %8};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%1], da, db, %4, [%5], [%6], p;}"
         :
-        : "r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
+        : "r"((uint32_t)leader), "r"(tmem_d), "r"(a), "r"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate),
+          "n"(kDescHighSw128)
         : "memory");
 }
-// 32 rows x 16 bytes of shared memory into four columns, repeated in each quarter of the lanes
-__device__ __forceinline__ void umma_copy_scales(uint32_t tmem, uint32_t smem)
+// 32 rows x 16 bytes of shared memory into four columns, repeated in each quarter of the lanes; low:
+// low word of the descriptor
+__device__ __forceinline__ void umma_copy_scales(bool leader, uint32_t tmem, uint32_t low)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(umma_desc(smem, 128, 128)) : "memory");
+    asm volatile(
+        "{.reg .pred q;\n\t"
+        ".reg .b64 d;\n\t"
+        "setp.ne.b32 q, %0, 0;\n\t"
+        "mov.b64 d, {%2, %3};\n\t"
+        "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%1], d;}" ::"r"((uint32_t)leader), "r"(tmem), "r"(low), "n"(kDescHighScales)
+        : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16])
 {
@@ -200,6 +215,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp;
     uint8_t *dsm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dsm_raw) + 1023) & ~(uintptr_t)1023);
     const int NS = mm_stages(a.bn), slot = mm_slot_bytes(a.bn), bn = a.bn;
+    uint8_t *stage_out = dsm + NS * slot;
     const int sfa_at = kMmABytes + bn * 128, sfb_at = sfa_at + 1024, atoms = mm_token_atoms(bn);
 
     if (tid == 0) {
@@ -276,38 +292,40 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (elect_one()) {
-            const uint32_t id0 = umma_idesc_mxf4(bn, 0), id1 = umma_idesc_mxf4(bn, 1);
-            const int cols = mm_scale_cols(bn);
-            int s = 0, it = 0;
-            uint32_t par = 0;
-            for (int task = first; task < n_tasks && !*dead; task += step, ++it) {
-                const int ab = it & 1;
-                if (!dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)) break;
+        // the whole warp walks the loop, one lane issues
+        const bool leader = elect_one();
+        const uint32_t id0 = umma_idesc_mxf4(bn, 0), id1 = umma_idesc_mxf4(bn, 1);
+        const int cols = mm_scale_cols(bn);
+        const uint32_t ring = dsmem_u32(dsm);
+        int s = 0, it = 0;
+        uint32_t par = 0;
+        bool ok = true;
+        for (int task = first; task < n_tasks && ok; task += step, ++it) {
+            const int ab = it & 1;
+            if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + ab * kMmAccStride;
+            for (int k = k_beg; k < k_end; ++k) {
+                if (!(ok = __all_sync(kFull, dmbar_wait(&full[s], par, dead)))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t acc = tmem + ab * kMmAccStride;
-                bool ok = true;
-                for (int k = k_beg; k < k_end; ++k) {
-                    if (!(ok = dmbar_wait(&full[s], par, dead))) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t st = dsmem_u32(dsm + (size_t)s * slot);
-                    const uint32_t sf = tmem + kMmScaleCol + s * cols;  // this stage's set of scale columns
+                const uint32_t st = ring + s * slot;
+                const uint32_t sf = tmem + kMmScaleCol + s * cols;  // this stage's set of scale columns
+                const uint32_t da = desc_low_sw128(st), db = desc_low_sw128(st + kMmABytes);
+                const uint32_t ds = desc_low_scales(st + sfa_at);   // 512 bytes a copy: 32 address units
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {                       // four blocks each
-                        umma_copy_scales(sf + 4 * q, st + sfa_at + 512 * q);
-                        for (int r = 0; r < atoms; ++r)
-                            umma_copy_scales(sf + 8 + 4 * (q * atoms + r), st + sfb_at + 512 * (q * atoms + r));
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        umma_mxf4(acc, umma_desc_sw128(st, j), umma_desc_sw128(st + kMmABytes, j), j & 1 ? id1 : id0,
-                                  sf + 4 * (j / 2), sf + 8 + 4 * (j / 2) * atoms, k > k_beg || j > 0);
-                    umma_commit(&empty[s]);
-                    if (++s == NS) s = 0, par ^= 1u;
+                for (int q = 0; q < 2; ++q) {                       // four blocks each
+                    umma_copy_scales(leader, sf + 4 * q, ds + 32 * q);
+                    umma_copy_scales(leader, sf + 8 + 4 * q * atoms, ds + 64 + 32 * q * atoms);
+                    if (atoms == 2) umma_copy_scales(leader, sf + 12 + 8 * q, ds + 96 + 64 * q);
                 }
-                if (!ok) break;
-                umma_commit(&tfull[ab]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    umma_mxf4(leader, acc, da + 2 * j, db + 2 * j, j & 1 ? id1 : id0, sf + 4 * (j / 2), sf + 8 + 4 * (j / 2) * atoms,
+                              k > k_beg || j > 0);
+                umma_commit_if(leader, &empty[s]);
+                if (++s == NS) s = 0, par ^= 1u;
             }
+            if (ok) umma_commit_if(leader, &tfull[ab]);
         }
         __syncwarp();
     } else if (warp < 6) {
@@ -321,15 +339,45 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             const uint32_t acc = tmem + ab * kMmAccStride + ((uint32_t)(lg * kWarp) << 16);
             const int row = t.row0 + lg * kWarp + lane;
             if (a.splits == 1) {
-                typename E::T *out = reinterpret_cast<typename E::T *>(a.out) + (long long)t.tok0 * a.out_stride + row;
-                for (int j0 = 0; j0 < t.count; j0 += 16) {
-                    float v[16];
-                    tmem_ld16(acc + j0, v);
-                    if (row < a.n)
+                using T = typename E::T;
+                T *out = reinterpret_cast<T *>(a.out) + (long long)t.tok0 * a.out_stride + (row - lane);
+                if (a.out_wide && row - lane + kWarp <= a.n) {
+                    // A lane has one column of out for every token.  Stored like that, 192 tokens are 192
+                    // two-byte stores of a warp (17000 cycles, twice the tile's MMAs); through shared memory
+                    // the warp's 32 columns of a token become whole 16-byte pieces.
+                    constexpr int kRow = kWarp * (int)sizeof(T), kLanes = kRow / 16, kTok = kMmStageOut / kRow;  // 64 or 128 bytes a token
+                    T *mine = reinterpret_cast<T *>(stage_out + lg * kMmStageOut);
+                    const int tk = lane / kLanes, piece = (lane % kLanes) * (16 / (int)sizeof(T));
+                    T *to = out + (long long)tk * a.out_stride + piece;
+                    const long long hop = (long long)(kWarp / kLanes) * a.out_stride;
+                    for (int j0 = 0; j0 < t.count; j0 += kTok) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (j0 + j < t.count)
-                                out[(long long)(j0 + j) * a.out_stride] = E::from_f32(ok ? v[j] : __uint_as_float(0x7fffffffu));
+                        for (int h = 0; h < kTok; h += 16) {
+                            float v[16];
+                            tmem_ld16(acc + j0 + h, v);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) mine[(h + j) * kWarp + lane] = E::from_f32(ok ? v[j] : __uint_as_float(0x7fffffffu));
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int h = 0; h < kTok; h += kWarp / kLanes) {
+                            if (j0 + h + tk < t.count)
+                                *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(mine + (h + tk) * kWarp + piece);
+                            to += hop;
+                        }
+                        __syncwarp();
+                    }
+                } else {
+                    T *to = out + lane;
+                    for (int j0 = 0; j0 < t.count; j0 += 16) {
+                        float v[16];
+                        tmem_ld16(acc + j0, v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            if (row < a.n && j0 + j < t.count) *to = E::from_f32(ok ? v[j] : __uint_as_float(0x7fffffffu));
+                            to += a.out_stride;
+                        }
+                    }
                 }
             } else {
                 // the ring is idle once the last MMA has been committed: the partial tile takes its place

@@ -21,7 +21,10 @@ __device__ __forceinline__ void dmbar_arrive(uint64_t *bar)
 }
 // One lane of a converged warp.  The TMA and tcgen05 instructions take their operands from uniform
 // registers: under a plain `lane == 0` the compiler cannot tell that one lane is left and wraps each of
-// them in a loop over the active lanes' values (measured: 75-130 cycles an instruction).
+// them in a loop over the active lanes' values (measured: 75-130 cycles an instruction).  Where such
+// instructions follow one another closely (the MMA loop) even one elected lane is slow, because inside
+// its branch every operand is moved to a uniform register first; there the whole warp walks the loop
+// and the elected lane is a predicate of the instruction.
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t mine;
@@ -32,20 +35,24 @@ __device__ __forceinline__ bool elect_one()
         : "=r"(mine));
     return mine != 0;
 }
+__device__ __forceinline__ bool dmbar_try(uint64_t *bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile(
+        "{.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;}"
+        : "=r"(done)
+        : "r"(dsmem_u32(bar)), "r"(parity)
+        : "memory");
+    return done != 0;
+}
 // bounded wait on a phase parity; false when the limit ran out or another thread gave up
 __device__ __forceinline__ bool dmbar_wait(uint64_t *bar, uint32_t parity, volatile int *dead,
                                            int spin_limit = kDenseSpinLimit)
 {
     for (int spins = 0; spins < spin_limit; ++spins) {
-        uint32_t done;
-        asm volatile(
-            "{.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;}"
-            : "=r"(done)
-            : "r"(dsmem_u32(bar)), "r"(parity)
-            : "memory");
-        if (done) return true;
+        if (dmbar_try(bar, parity)) return true;
         if (*dead) return false;
     }
     *dead = 1;
@@ -63,6 +70,16 @@ __device__ __forceinline__ void umma_commit(uint64_t *bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(dsmem_u32(bar))
                  : "memory");
+}
+// the same from a whole warp, by the lane that `leader` names
+__device__ __forceinline__ void umma_commit_if(bool leader, uint64_t *bar)
+{
+    asm volatile(
+        "{.reg .pred q;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];}" ::"r"(dsmem_u32(bar)),
+        "r"((uint32_t)leader)
+        : "memory");
 }
 __device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&v)[8])
 {
@@ -107,4 +124,9 @@ __device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t smem_addr, int kste
     return (uint64_t)(((smem_addr + kstep * 32) >> 4) & 0x3FFFu) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) |
            (1ull << 46) | (2ull << 61);
 }
+// The two descriptor forms by their low words (address and leading offset); the high words are constant.
+constexpr uint32_t kDescHighSw128 = (1024u >> 4) | (1u << 14) | (2u << 29);
+constexpr uint32_t kDescHighScales = (128u >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t desc_low_sw128(uint32_t smem_addr) { return ((smem_addr >> 4) & 0x3FFFu) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_low_scales(uint32_t smem_addr) { return ((smem_addr >> 4) & 0x3FFFu) | ((128u >> 4) << 16); }
 }  // namespace stmoe_dev
