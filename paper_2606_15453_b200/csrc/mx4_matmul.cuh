@@ -189,10 +189,6 @@ __device__ __forceinline__ Mx4Task mm_task(const Mx4MatmulArgs &a, const int *s_
     return k;
 }
 
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ float ld_cluster(uint32_t smem, int rank)
 {
     uint32_t remote;

@@ -27,14 +27,16 @@ bool overlap(const void *p, int64_t p_stride, const void *q, int64_t q_stride, i
     const uintptr_t a_end = a + eb * ((tokens - 1) * p_stride + n_experts), b_end = b + eb * ((tokens - 1) * q_stride + n_experts);
     return a < b_end && b < a_end;
 }
-// lanes that share a row: a power of two with eight logits each
+// lanes that share a row: a power of two with sixteen logits each (one lane with eight for up to eight)
 int lanes_per_row(int n_experts)
 {
     int l = 1;
-    while (l * 8 < n_experts) l *= 2;
+    while (l * 16 < n_experts) l *= 2;
     return l;
 }
-int bal_grid(int64_t tokens, int lpr)
+// per_sm: CTAs that fit an SM (the kernels' launch bounds).  Up to two steps of rows are left to one CTA,
+// which then needs no second launch to add partial sums up.
+int bal_grid(int64_t tokens, int lpr, int per_sm)
 {
     const int64_t rows = (int64_t)(kBalThreads / kWarp) * (kWarp / lpr) * kBalRows;
     int dev = 0, sms = 0;
@@ -42,25 +44,26 @@ int bal_grid(int64_t tokens, int lpr)
         (void)cudaGetLastError();
         return 0;
     }
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(tokens + rows - 1) / rows, (int64_t)sms * 4, kBalMaxCtas}));
+    const int64_t steps = (tokens + rows - 1) / rows;
+    if (steps <= 2) return 1;
+    return (int)std::min<int64_t>({steps, (int64_t)sms * per_sm, kBalMaxCtas});
 }
 
-template <int DT, int LPR> void launch(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+template <int DT, int LPR, int N> void launch(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {
     if (backward)
-        router_balance_backward_kernel<DT, LPR><<<grid, kBalThreads, 0, st>>>(a);
+        router_balance_backward_kernel<DT, LPR, N><<<grid, kBalThreads, 0, st>>>(a);
     else
-        router_balance_kernel<DT, LPR><<<grid, kBalThreads, 0, st>>>(a);
+        router_balance_kernel<DT, LPR, N><<<grid, kBalThreads, 0, st>>>(a);
 }
 template <int DT> void launch_lanes(int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {
     switch (lpr) {
-    case 1: launch<DT, 1>(backward, a, grid, st); break;
-    case 2: launch<DT, 2>(backward, a, grid, st); break;
-    case 4: launch<DT, 4>(backward, a, grid, st); break;
-    case 8: launch<DT, 8>(backward, a, grid, st); break;
-    case 16: launch<DT, 16>(backward, a, grid, st); break;
-    default: launch<DT, 32>(backward, a, grid, st); break;
+    case 1: a.E <= 8 ? launch<DT, 1, 8>(backward, a, grid, st) : launch<DT, 1, 16>(backward, a, grid, st); break;
+    case 2: launch<DT, 2, 16>(backward, a, grid, st); break;
+    case 4: launch<DT, 4, 16>(backward, a, grid, st); break;
+    case 8: launch<DT, 8, 16>(backward, a, grid, st); break;
+    default: launch<DT, 16, 16>(backward, a, grid, st); break;
     }
 }
 int launch_typed(int dtype, int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
@@ -89,7 +92,7 @@ int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const in
     if (!bal_args_ok(logits, dtype, stride, tokens, n_experts, top_k) || !ids || !loss || !counts || !rows || !scratch ||
         ((uintptr_t)scratch & 3) || scratch_bytes < stmoe_router_balance_scratch_bytes(n_experts))
         return STMOE_ERR_BAD_ARG;
-    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr);
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, 3);
     if (!grid) return STMOE_ERR_CUDA;
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.ids = ids, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
@@ -97,14 +100,16 @@ int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const in
     a.part = (float *)scratch, a.ctas = grid, a.loss = loss, a.counts = counts, a.rows = rows;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const int rc = launch_typed(dtype, lpr, false, a, grid, st);
-    if (rc != STMOE_OK) return rc;
+    if (rc != STMOE_OK || grid == 1) return rc;
     // may start while the first kernel drains; it waits for that kernel's results itself
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(1), cfg.blockDim = dim3(1024), cfg.stream = st;
-    cudaLaunchAttribute at[1];
+    cfg.gridDim = dim3(kBalFinish), cfg.blockDim = dim3(1024), cfg.stream = st;
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at, cfg.numAttrs = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = kBalFinish, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = 2;
     if (cudaLaunchKernelEx(&cfg, router_balance_finish_kernel, a) != cudaSuccess) {
         (void)cudaGetLastError();
         return STMOE_ERR_CUDA;
@@ -121,7 +126,7 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
         return STMOE_ERR_BAD_ARG;
     if (tokens == 0) return STMOE_OK;
     if (overlap(logits, stride, grad_logits, grad_stride, tokens, n_experts, dtype)) return STMOE_ERR_BAD_ARG;
-    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr);
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, 3);
     if (!grid) return STMOE_ERR_CUDA;
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
