@@ -49,30 +49,43 @@ int bal_grid(int64_t tokens, int lpr, int per_sm)
     return (int)std::min<int64_t>({steps, (int64_t)sms * per_sm, kBalMaxCtas});
 }
 
-template <int DT, int LPR, int N> void launch(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+template <int DT, int LPR, int N, bool kVec> int launch_as(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {
-    if (backward)
-        router_balance_backward_kernel<DT, LPR, N><<<grid, kBalThreads, 0, st>>>(a);
-    else
-        router_balance_kernel<DT, LPR, N><<<grid, kBalThreads, 0, st>>>(a);
+    // more than the default 48 KB of dynamic shared memory: asked for once per device
+    static bool ready[64][2];
+    void (*kernel)(BalanceArgs) = backward ? router_balance_backward_kernel<DT, LPR, N, kVec> : router_balance_kernel<DT, LPR, N, kVec>;
+    const int smem = !kVec ? 0 : kBalDepth * (backward ? BalWalk<DT, LPR, N, kVec, false>::stage_bytes() : BalWalk<DT, LPR, N, kVec, true>::stage_bytes());
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return STMOE_ERR_CUDA;
+    if (smem && !ready[dev][backward]) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return STMOE_ERR_CUDA;
+        }
+        ready[dev][backward] = true;
+    }
+    kernel<<<grid, kBalThreads, smem, st>>>(a);
+    return cudaGetLastError() == cudaSuccess ? STMOE_OK : STMOE_ERR_CUDA;
 }
-template <int DT> void launch_lanes(int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+template <int DT, int LPR, int N> int launch(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+{
+    return a.vec ? launch_as<DT, LPR, N, true>(backward, a, grid, st) : launch_as<DT, LPR, N, false>(backward, a, grid, st);
+}
+template <int DT> int launch_lanes(int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {
     switch (lpr) {
-    case 1: a.E <= 8 ? launch<DT, 1, 8>(backward, a, grid, st) : launch<DT, 1, 16>(backward, a, grid, st); break;
-    case 2: launch<DT, 2, 16>(backward, a, grid, st); break;
-    case 4: launch<DT, 4, 16>(backward, a, grid, st); break;
-    case 8: launch<DT, 8, 16>(backward, a, grid, st); break;
-    default: launch<DT, 16, 16>(backward, a, grid, st); break;
+    case 1: return a.E <= 8 ? launch<DT, 1, 8>(backward, a, grid, st) : launch<DT, 1, 16>(backward, a, grid, st);
+    case 2: return launch<DT, 2, 16>(backward, a, grid, st);
+    case 4: return launch<DT, 4, 16>(backward, a, grid, st);
+    case 8: return launch<DT, 8, 16>(backward, a, grid, st);
+    default: return launch<DT, 16, 16>(backward, a, grid, st);
     }
 }
 int launch_typed(int dtype, int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {
-    if (dtype == STMOE_F32) launch_lanes<0>(lpr, backward, a, grid, st);
-    else if (dtype == STMOE_BF16) launch_lanes<1>(lpr, backward, a, grid, st);
-    else launch_lanes<4>(lpr, backward, a, grid, st);
-    if (cudaGetLastError() != cudaSuccess) return STMOE_ERR_CUDA;
-    return STMOE_OK;
+    if (dtype == STMOE_F32) return launch_lanes<0>(lpr, backward, a, grid, st);
+    if (dtype == STMOE_BF16) return launch_lanes<1>(lpr, backward, a, grid, st);
+    return launch_lanes<4>(lpr, backward, a, grid, st);
 }
 
 }  // namespace
@@ -130,9 +143,9 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
     if (!grid) return STMOE_ERR_CUDA;
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
-    a.vec = rows_vec(logits, dtype, stride, n_experts);
+    a.vec = rows_vec(logits, dtype, stride, n_experts) && rows_vec(grad_logits, dtype, grad_stride, n_experts);
     a.counts = (int *)counts, a.rows = (int *)rows, a.grad = grad_loss;
-    a.dlogits = grad_logits, a.dstride = grad_stride, a.dvec = rows_vec(grad_logits, dtype, grad_stride, n_experts);
+    a.dlogits = grad_logits, a.dstride = grad_stride;
     return launch_typed(dtype, lpr, true, a, grid, (cudaStream_t)cuda_stream);
 }
 

@@ -29,6 +29,7 @@ namespace stmoe_dev {
 constexpr int kBalThreads = 256;
 constexpr int kBalMaxExperts = 256;
 constexpr int kBalRows = 2;         // rows of a lane in flight
+constexpr int kBalDepth = 3;        // steps of rows in shared memory: one in use, two under way
 constexpr int kBalFinish = 8;       // CTAs of the cluster that adds the partial sums up
 constexpr int kBalMaxCtas = 592;   // four a SM: rows of the partial-sum workspace
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -42,7 +43,7 @@ struct BalanceArgs {
     const int *ids;         // [T][K]
     const uint8_t *mask;    // [T] or nullptr
     int T, E, K;
-    bool vec;               // rows are 16-byte aligned and E is a multiple of the vector width
+    bool vec;               // rows (of the gradient too) are 16-byte aligned, E a multiple of the vector width
     float *part;            // forward: [gridDim.x][bal_part_words(E)]
     int ctas;               // finish: rows of part
     float *loss;            // [2]
@@ -51,7 +52,6 @@ struct BalanceArgs {
     const float *grad;      // backward: [2]
     void *dlogits;
     long long dstride;
-    bool dvec;
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -59,6 +59,28 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Two fp32 operations in one instruction (each rounded on its own, as the single ones are).
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(r)
+        : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)), "l"(*reinterpret_cast<const uint64_t *>(&c)));
+    return *reinterpret_cast<const float2 *>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)));
+    return *reinterpret_cast<const float2 *>(&r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)));
+    return *reinterpret_cast<const float2 *>(&r);
 }
 
 // Where lane l of a row's LPR lanes finds its N logits: in vector order (groups of 16 bytes, lane after
@@ -69,27 +91,48 @@ template <int DT, int LPR> __device__ __forceinline__ int bal_index(int l, int i
     return vec ? (i / V) * (LPR * V) + l * V + i % V : i * LPR + l;
 }
 
-template <int DT, int LPR, int N>
-__device__ __forceinline__ void bal_load(const typename Elem<DT>::T *row, int E, int l, bool vec, float (&z)[N])
+// A row read element by element (rows without 16-byte alignment), in lane order.
+template <int DT, int LPR, int N> __device__ __forceinline__ void bal_load(const typename Elem<DT>::T *row, int E, int l, float2 (&z)[N / 2])
 {
-    using El = Elem<DT>;
-    if (vec) {
 #pragma unroll
-        for (int g = 0; g < N / El::kVec; ++g) {
-            const int e = bal_index<DT, LPR>(l, g * El::kVec, true);
-            typename El::T t[El::kVec];
-            const bool in = e < E;
-            if (in) *reinterpret_cast<uint4 *>(t) = ld_stream16(row + e);
-#pragma unroll
-            for (int i = 0; i < El::kVec; ++i) z[g * El::kVec + i] = in ? El::to_f32(t[i]) : -INFINITY;
-        }
+    for (int i = 0; i < N; ++i) {
+        const int e = i * LPR + l;
+        (i & 1 ? z[i / 2].y : z[i / 2].x) = e < E ? Elem<DT>::to_f32(row[e]) : -INFINITY;
+    }
+}
+// 16 bytes of a row, widened
+template <int DT> __device__ __forceinline__ void bal_widen(const uint4 &q, float2 *z)
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    if constexpr (DT == 0) {
+        z[0] = make_float2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+        z[1] = make_float2(__uint_as_float(w[2]), __uint_as_float(w[3]));
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int e = i * LPR + l;
-            z[i] = e < E ? El::to_f32(row[e]) : -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (DT == 1) z[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+            else z[i] = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
         }
     }
+}
+template <int DT> __device__ __forceinline__ uint4 bal_narrow(const float2 *z)
+{
+    uint32_t w[4];
+    if constexpr (DT == 0) {
+        w[0] = __float_as_uint(z[0].x), w[1] = __float_as_uint(z[0].y), w[2] = __float_as_uint(z[1].x), w[3] = __float_as_uint(z[1].y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (DT == 1) {
+                const __nv_bfloat162 h = __float22bfloat162_rn(z[i]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                const __half2 h = __float22half2_rn(z[i]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <int LPR> __device__ __forceinline__ float lanes_max(float v)
@@ -107,52 +150,135 @@ template <int LPR> __device__ __forceinline__ float lanes_sum(float v)
 
 // z -> exp(z - max) in place, inv: 1 / their sum; returns lse.  live: the row has a logit above
 // -infinity (NaN included: then the row's results are NaN, as the formulas say).
-template <int LPR, int N> __device__ __forceinline__ float bal_softmax(float (&z)[N], float &inv, bool &live)
+template <int LPR, int P> __device__ __forceinline__ float bal_softmax(float2 (&z)[P], float &inv, bool &live)
 {
-    float m = z[0];
+    float m = fmaxf(z[0].x, z[0].y);
 #pragma unroll
-    for (int i = 1; i < N; ++i) m = fmaxf(m, z[i]);
+    for (int i = 1; i < P; ++i) m = fmaxf(m, fmaxf(z[i].x, z[i].y));
     m = lanes_max<LPR>(m);
     const float m2 = m == -INFINITY ? 0.f : m * kLog2e;
-    float sum = 0.f;
+    const float2 k = make_float2(kLog2e, kLog2e), off = make_float2(-m2, -m2);
+    float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) z[i] = ex2(fmaf(z[i], kLog2e, -m2)), sum += z[i];
-    sum = lanes_sum<LPR>(sum);
+    for (int i = 0; i < P; ++i) {
+        z[i] = fma2(z[i], k, off);
+        z[i] = make_float2(ex2(z[i].x), ex2(z[i].y));
+        s2 = add2(s2, z[i]);
+    }
+    const float sum = lanes_sum<LPR>(s2.x + s2.y);
     live = sum != 0.f;   // 0 where all logits are -infinity (a NaN is not 0)
     inv = __fdividef(1.f, sum);
     return (m2 + __log2f(sum)) * kLn2;
 }
 
-// The rows of a lane: first row, rows between two of its own, and its walk through logits, choices and
-// masks by pointers (a 64-bit product per row and array would cost as much as the row's exponentials).
-template <typename T, int LPR> struct BalWalk {
-    static constexpr int RPW = kWarp / LPR;
-    long long t, step;
-    const T *z;
+// The rows of a lane, kBalRows a step.  With 16-byte rows (kVec) a lane's part of a row goes through
+// shared memory: every lane copies what it will read itself (cp.async, nothing to synchronise), two steps
+// ahead of the one it works on, so the loads' latency is hidden at no cost in registers.  Masks are asked
+// for one step before the copies that depend on them.  kIds: the lane's first choice of a row travels with it.
+template <int DT, int LPR, int N, bool kVec, bool kIds> struct BalWalk {
+    using T = typename Elem<DT>::T;
+    static constexpr int RPW = kWarp / LPR, G = N * (int)sizeof(T) / 16;   // 16-byte pieces of a lane's part
+    long long t, step, t_ahead;      // row of the step in progress, rows between steps, row of the masks held
+    const T *z;                      // kVec: of the next copy; else of the step in progress
     const uint8_t *mask;
-    long long z_row, z_step;
-    bool on[kBalRows];
-    __device__ __forceinline__ BalWalk(const BalanceArgs &a, int warp, int sub)
+    const int *ids;
+    long long z_row, z_step, ids_step;
+    uint32_t on_hist;                // kBalRows bits a step: the steps under way, newest lowest
+    int l, slot;
+    uint8_t *ring;
+
+    __host__ __device__ static constexpr int stage_bytes() { return kBalRows * (G * 16 + (kIds ? 4 : 0)) * kBalThreads; }
+    __device__ __forceinline__ uint32_t ask(const BalanceArgs &a, long long at) const
+    {
+        uint32_t on = 0;
+#pragma unroll
+        for (int r = 0; r < kBalRows; ++r)
+            if (at + r * RPW < a.T && (!a.mask || a.mask[at + r * RPW])) on |= 1u << r;
+        return on;
+    }
+    __device__ __forceinline__ void copy(const BalanceArgs &a, uint32_t on)
+    {
+        uint8_t *st = ring + slot * stage_bytes();
+#pragma unroll
+        for (int r = 0; r < kBalRows; ++r)
+            if (on >> r & 1) {
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const int e = bal_index<DT, LPR>(l, g * Elem<DT>::kVec, true);
+                    if (e < a.E)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(st + ((r * G + g) * kBalThreads + threadIdx.x) * 16)),
+                                     "l"(z + r * z_row + e) : "memory");
+                }
+                if (kIds && l < a.K)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(st + kBalRows * G * 16 * kBalThreads + (r * kBalThreads + threadIdx.x) * 4)),
+                                 "l"(ids + r * RPW * a.K) : "memory");
+            }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        z += z_step;
+        if (kIds) ids += ids_step;
+        if (++slot == kBalDepth) slot = 0;
+    }
+    __device__ __forceinline__ BalWalk(const BalanceArgs &a, int warp, int sub, int l_, uint8_t *ring_) : l(l_), ring(ring_)
     {
         constexpr int W = kBalThreads / kWarp;
         step = (long long)gridDim.x * W * RPW * kBalRows;
         t = (long long)(blockIdx.x * W + warp) * RPW * kBalRows + sub;
         z_row = RPW * a.stride, z_step = step * a.stride;
         z = reinterpret_cast<const T *>(a.logits) + t * a.stride;
-        mask = a.mask ? a.mask + t : nullptr;
-        masks(a);
-    }
-    __device__ __forceinline__ void masks(const BalanceArgs &a)
-    {
+        ids = kIds ? a.ids + t * a.K + l : nullptr, ids_step = step * a.K;
+        on_hist = 0, slot = 0;
+        if (kVec) {
+            uint32_t on[kBalDepth];
 #pragma unroll
-        for (int r = 0; r < kBalRows; ++r) on[r] = t + r * RPW < a.T && (!mask || mask[r * RPW]);
+            for (int i = 0; i < kBalDepth; ++i) on[i] = ask(a, t + i * step);
+#pragma unroll
+            for (int i = 0; i < kBalDepth - 1; ++i) copy(a, on[i]), on_hist = on_hist << kBalRows | on[i];
+            on_hist = on_hist << kBalRows | on[kBalDepth - 1];   // its copy comes with the first step
+            t_ahead = t + kBalDepth * step;
+        } else {
+            on_hist = ask(a, t);
+            t_ahead = t + step;
+        }
     }
-    // to the next rows; their masks are asked for here, a step before the logits that wait for them
-    __device__ __forceinline__ void next(const BalanceArgs &a)
+    __device__ __forceinline__ bool more(const BalanceArgs &a, int sub) const { return t - sub < a.T; }
+    // The rows of the step in progress and the lane's first choices; bit r of the result: row r counts.
+    __device__ __forceinline__ uint32_t rows(const BalanceArgs &a, float2 (&v)[kBalRows][N / 2], int (&id)[kBalRows])
     {
-        t += step, z += z_step;
-        if (mask) mask += step;
-        masks(a);
+        constexpr uint32_t kBits = (1u << kBalRows) - 1;
+        const uint32_t newest = on_hist & kBits, now = kVec ? on_hist >> (kBalRows * (kBalDepth - 1)) & kBits : newest;
+        const uint8_t *st = ring + (slot + 1 == kBalDepth ? 0 : slot + 1) * stage_bytes();   // oldest stage, once the newest is under way
+        if (kVec) copy(a, newest);
+        const uint32_t next = ask(a, t_ahead);
+        if (kVec) asm volatile("cp.async.wait_group %0;" ::"n"(kBalDepth - 1) : "memory");
+#pragma unroll
+        for (int r = 0; r < kBalRows; ++r) {
+            id[r] = -1;
+            if (!(now >> r & 1)) {
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) v[r][i] = make_float2(-INFINITY, -INFINITY);
+            } else if constexpr (kVec) {
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    if (bal_index<DT, LPR>(l, g * Elem<DT>::kVec, true) < a.E) {
+                        bal_widen<DT>(*reinterpret_cast<const uint4 *>(st + ((r * G + g) * kBalThreads + threadIdx.x) * 16), &v[r][g * N / 2 / G]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < N / 2 / G; ++i) v[r][g * N / 2 / G + i] = make_float2(-INFINITY, -INFINITY);
+                    }
+                }
+                if (kIds && l < a.K) id[r] = *reinterpret_cast<const int *>(st + kBalRows * G * 16 * kBalThreads + (r * kBalThreads + threadIdx.x) * 4);
+            } else {
+                bal_load<DT, LPR, N>(z + r * z_row, a.E, l, v[r]);
+                if (kIds && l < a.K) id[r] = __ldg(ids + r * RPW * a.K);
+            }
+        }
+        if (!kVec) {
+            z += z_step;
+            if (kIds) ids += ids_step;
+        }
+        on_hist = on_hist << kBalRows | next;
+        t += step, t_ahead += step;
+        return now;
     }
 };
 
@@ -166,10 +292,10 @@ __device__ __forceinline__ void bal_write(const BalanceArgs &a, double sum, doub
 }
 
 // One CTA's sums over its rows.  Alone (gridDim.x = 1) it writes the results, else its partial sums.
-template <int DT, int LPR, int N> __global__ void __launch_bounds__(kBalThreads, 3) router_balance_kernel(const BalanceArgs a)
+template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(kBalThreads, 3) router_balance_kernel(const BalanceArgs a)
 {
-    using T = typename Elem<DT>::T;
-    constexpr int RPW = kWarp / LPR, W = kBalThreads / kWarp;
+    constexpr int W = kBalThreads / kWarp;
+    extern __shared__ __align__(16) uint8_t ring[];
     __shared__ int s_cnt[kBalMaxExperts];
     __shared__ float s_p[W][LPR * N];
     __shared__ float s_z[W];
@@ -178,57 +304,47 @@ template <int DT, int LPR, int N> __global__ void __launch_bounds__(kBalThreads,
     const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp, l = lane % LPR, sub = lane / LPR;
     for (int e = tid; e < a.E; e += kBalThreads) s_cnt[e] = 0;
     __syncthreads();
-    float p[N] = {}, zz = 0.f;
+    float2 p[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) p[i] = make_float2(0.f, 0.f);
+    float zz = 0.f;
     int n = 0;
-    BalWalk<T, LPR> w(a, warp, sub);
-    const int *ids = a.ids + w.t * a.K + l;
-    const long long ids_step = w.step * a.K;
-    while (w.t - sub < a.T) {
-        float z[kBalRows][N];
+    BalWalk<DT, LPR, N, kVec, true> w(a, warp, sub, l, ring);
+    while (w.more(a, sub)) {
+        float2 z[kBalRows][N / 2];
         int id[kBalRows];
-        bool on[kBalRows];
-#pragma unroll
-        for (int r = 0; r < kBalRows; ++r) {
-            on[r] = w.on[r];
-            id[r] = -1;
-            if (on[r]) {
-                bal_load<DT, LPR>(w.z + r * w.z_row, a.E, l, a.vec, z[r]);
-                if (l < a.K) id[r] = __ldg(ids + r * RPW * a.K);   // the lane's first choice, with the logits
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) z[r][i] = -INFINITY;
-            }
-        }
-        w.next(a);
+        const long long t = w.t;
+        const uint32_t on = w.rows(a, z, id);
 #pragma unroll
         for (int r = 0; r < kBalRows; ++r) {
             bool live;
             float inv;
             const float lse = bal_softmax<LPR>(z[r], inv, live);
-            if (on[r] && live) {
+            if ((on >> r & 1) && live) {
+                const float2 inv2 = make_float2(inv, inv);
 #pragma unroll
-                for (int i = 0; i < N; ++i) p[i] = fmaf(z[r][i], inv, p[i]);
+                for (int i = 0; i < N / 2; ++i) p[i] = fma2(z[r][i], inv2, p[i]);
                 if (l == 0) zz = fmaf(lse, lse, zz), ++n;
                 if ((unsigned)id[r] < (unsigned)a.E) atomicAdd(&s_cnt[id[r]], 1);
-                for (int k = LPR; k + l < a.K; k += LPR) {
-                    const int e = __ldg(ids + r * RPW * a.K + k);
+                for (int k = l + LPR; k < a.K; k += LPR) {
+                    const int e = __ldg(a.ids + (t + r * (kWarp / LPR)) * a.K + k);
                     if ((unsigned)e < (unsigned)a.E) atomicAdd(&s_cnt[e], 1);
                 }
             }
         }
-        ids += ids_step;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     // the rows of a warp first (lanes with the same l), then the warps in order
 #pragma unroll
     for (int o = LPR; o < kWarp; o <<= 1) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) p[i] += __shfl_xor_sync(kFull, p[i], o);
+        for (int i = 0; i < N / 2; ++i) p[i].x += __shfl_xor_sync(kFull, p[i].x, o), p[i].y += __shfl_xor_sync(kFull, p[i].y, o);
         zz += __shfl_xor_sync(kFull, zz, o);
         n += __shfl_xor_sync(kFull, n, o);
     }
     if (sub == 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) s_p[warp][bal_index<DT, LPR>(l, i, a.vec)] = p[i];
+        for (int i = 0; i < N; ++i) s_p[warp][bal_index<DT, LPR>(l, i, kVec)] = i & 1 ? p[i / 2].y : p[i / 2].x;
         if (l == 0) s_z[warp] = zz, s_n[warp] = n;
     }
     __syncthreads();
@@ -333,74 +449,63 @@ __global__ void __launch_bounds__(1024) router_balance_finish_kernel(const Balan
     }
 }
 
-template <int DT, int LPR, int N> __global__ void __launch_bounds__(kBalThreads, 3) router_balance_backward_kernel(const BalanceArgs a)
+// kVec: rows of the logits and of the gradient are both read and written 16 bytes at a time
+template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(kBalThreads, 3) router_balance_backward_kernel(const BalanceArgs a)
 {
     using El = Elem<DT>;
     using T = typename El::T;
-    constexpr int RPW = kWarp / LPR;
+    constexpr int RPW = kWarp / LPR, V = El::kVec;
+    extern __shared__ __align__(16) uint8_t ring[];
     const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp, l = lane % LPR, sub = lane / LPR;
+    BalWalk<DT, LPR, N, kVec, false> w(a, warp, sub, l, ring);
     const int n = *a.rows;
     const float rn = n > 0 ? 1.f / (float)n : 0.f;
     const float gb = a.grad[0] * (float)a.E * rn, gz = a.grad[1] * 2.f * rn;
-    // logits and gradient may be laid out differently; a lane's experts follow the vector order only
-    // where both do
-    const bool vec = a.vec && a.dvec;
-    float f[N];   // g_balance E/n f_e
+    float2 f[N / 2];   // g_balance E/n f_e
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int e = bal_index<DT, LPR>(l, i, vec);
-        f[i] = e < a.E ? gb * ((float)a.counts[e] * rn / (float)a.K) : 0.f;
+        const int e = bal_index<DT, LPR>(l, i, kVec);
+        (i & 1 ? f[i / 2].y : f[i / 2].x) = e < a.E ? gb * ((float)a.counts[e] * rn / (float)a.K) : 0.f;
     }
-    BalWalk<T, LPR> w(a, warp, sub);
     T *out = reinterpret_cast<T *>(a.dlogits) + w.t * a.dstride;
     const long long d_row = RPW * a.dstride, d_step = w.step * a.dstride;
-    while (w.t - sub < a.T) {
-        float z[kBalRows][N];
-        bool on[kBalRows];
+    while (w.more(a, sub)) {
+        float2 z[kBalRows][N / 2];
+        int id[kBalRows];
         const long long t = w.t;
-#pragma unroll
-        for (int r = 0; r < kBalRows; ++r) {
-            on[r] = w.on[r];
-            if (on[r]) {
-                bal_load<DT, LPR>(w.z + r * w.z_row, a.E, l, vec, z[r]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) z[r][i] = -INFINITY;
-            }
-        }
-        w.next(a);
+        const uint32_t on = w.rows(a, z, id);
 #pragma unroll
         for (int r = 0; r < kBalRows; ++r) {
             bool live;
             float inv;
             const float lse = bal_softmax<LPR>(z[r], inv, live);
-            float dot = 0.f;
+            float2 d2 = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < N; ++i) dot = fmaf(f[i], z[r][i], dot);
-            dot = lanes_sum<LPR>(dot);
-            const float c = gz * lse - dot * inv;   // dz = p (gb f + gz lse - gb dot)
-            const bool counts = on[r] && live;
+            for (int i = 0; i < N / 2; ++i) d2 = fma2(f[i], z[r][i], d2);
+            const float dot = lanes_sum<LPR>(d2.x + d2.y);
+            // dz = p (gb f + c), c = gz lse - gb dot, p = z inv; rows that do not count have z = 0
+            float c = gz * lse - dot * inv;
+            if (!(on >> r & 1) || !live) inv = 0.f, c = 0.f;
+            const float2 inv2 = make_float2(inv, inv), c2 = make_float2(c * inv, c * inv);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) z[r][i] = mul2(z[r][i], fma2(f[i], inv2, c2));
             if (t + r * RPW >= a.T) continue;
-#pragma unroll
-            for (int i = 0; i < N; ++i) z[r][i] = counts ? z[r][i] * inv * (f[i] + c) : 0.f;
             T *o = out + r * d_row;
-            if (vec) {
+            if constexpr (kVec) {
 #pragma unroll
-                for (int g = 0; g < N / El::kVec; ++g) {
-                    const int e = bal_index<DT, LPR>(l, g * El::kVec, true);
-                    T v[El::kVec];
-#pragma unroll
-                    for (int i = 0; i < El::kVec; ++i) v[i] = El::from_f32(z[r][g * El::kVec + i]);
-                    if (e < a.E) *reinterpret_cast<uint4 *>(o + e) = *reinterpret_cast<const uint4 *>(v);
+                for (int g = 0; g < N / V; ++g) {
+                    const int e = bal_index<DT, LPR>(l, g * V, true);
+                    if (e < a.E) *reinterpret_cast<uint4 *>(o + e) = bal_narrow<DT>(&z[r][g * V / 2]);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    if (i * LPR + l < a.E) o[i * LPR + l] = El::from_f32(z[r][i]);
+                    if (i * LPR + l < a.E) o[i * LPR + l] = El::from_f32(i & 1 ? z[r][i / 2].y : z[r][i / 2].x);
             }
         }
         out += d_step;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 }  // namespace stmoe_dev
