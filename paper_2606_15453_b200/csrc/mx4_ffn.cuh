@@ -21,7 +21,7 @@
 // tokens are gathered by one TMA load each.  The epilogue adds a token's eight columns in fp32,
 // smallest plane first.
 //
-//   mx4_planes_kernel    hidden state -> planes (and, for the stand-alone call, the work list)
+//   mx4_planes_kernel    hidden state -> planes; the work-list entries, one line of memory each
 //   mx4_ffn_kernel<2>    gate and up tiles of 128 rows; epilogue: SiLU(g) * u as planes (a warp's 32
 //                        rows are one block of the next reduction, so a block maximum is one
 //                        warp reduction)
@@ -126,18 +126,34 @@ __device__ __forceinline__ void planes_store(float v, uint8_t *codes, uint8_t *s
     if (lane < kPlanes) scales[(row * kPlanes + lane) * blocks + blk] = (uint8_t)plane_byte(byte, lane);
 }
 
+// What the projections need to know of a work-list entry (one expert, up to kMxfTokens of its pairs), in
+// one line of memory: gathered from the router's lists it would be a chain of three dependent loads at
+// every task of every warp.
+struct alignas(128) Mx4Entry {
+    const uint8_t *img;            // expert image
+    int32_t img_index;             // its place in the store that the tensor maps cover
+    int16_t count;                 // pairs
+    int16_t shared;                // 1: in the store of the shared experts
+    uint16_t token[kMxfTokens];    // sequence
+    uint16_t slot[kMxfTokens];     // row of the activation and partial-sum buffers
+    float inv[kMxfTokens];         // the sequence's RMSNorm factor
+};
+static_assert(sizeof(Mx4Entry) == 128, "");
+
 struct Mx4PlanesArgs {
-    const float *h;
+    const float *h, *inv_rms;
     int B, H;
     uint8_t *codes, *scales;
-    // stand-alone call: the work list of given routing (n_group_ctas = 1), else 0
-    int group_ctas;
-    const int32_t *ids;
+    Mx4Entry *entries;
+    int *n_entries;
+    const uint8_t *store[2];       // first image of the maps: routed experts, shared ones
+    unsigned long long img_bytes;
     int E, K, mt;
+    // entries from given ids (stand-alone call, by the first CTA) ...
+    const int32_t *ids;
+    // ... or from the router's work list
     WorkList wl;
-    const uint8_t *experts;
-    size_t img_bytes;
-    const uint8_t **table;
+    const uint8_t *const *blob;    // image of every expert of the step
 };
 
 // Entries of at most mt tokens per expert from given ids, pairs of an expert in index order.  ids
@@ -145,7 +161,7 @@ struct Mx4PlanesArgs {
 // rank in its chunk of 32 (one match per warp) behind the chunks before it: a thread per expert that
 // walked all pairs took 40 us at 64 sequences x 6 experts.
 // s_cnt: [chunks][256], pairs of an expert in a chunk, then behind all chunks before it.
-__device__ __forceinline__ void group_ids(const Mx4PlanesArgs &a, uint16_t *s_cnt, int *s_g, int *s_p, int *s_first)
+__device__ __forceinline__ void entries_from_ids(const Mx4PlanesArgs &a, uint16_t *s_cnt, int *s_g, int *s_first)
 {
     const int e = threadIdx.x, n = a.B * a.K, chunks = (n + kWarp - 1) / kWarp;
     const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
@@ -164,22 +180,23 @@ __device__ __forceinline__ void group_ids(const Mx4PlanesArgs &a, uint16_t *s_cn
         s_cnt[c * 256 + e] = (uint16_t)cnt;   // at most 64 * 32 pairs
         cnt += k;
     }
-    int g = (cnt + a.mt - 1) / a.mt, p = cnt;   // inclusive prefix sums over the experts
+    const int mine = (cnt + a.mt - 1) / a.mt;
+    int g = mine;                             // inclusive prefix sum over the experts
 #pragma unroll
     for (int o = 1; o < kWarp; o <<= 1) {
-        const int tg = __shfl_up_sync(kFull, g, o), tp = __shfl_up_sync(kFull, p, o);
-        if (lane >= o) g += tg, p += tp;
+        const int t = __shfl_up_sync(kFull, g, o);
+        if (lane >= o) g += t;
     }
-    if (lane == kWarp - 1) s_g[warp] = g, s_p[warp] = p;
+    if (lane == kWarp - 1) s_g[warp] = g;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) g += s_g[w], p += s_p[w];
-    if (e == 255) *a.wl.n_groups = g;
-    g -= (cnt + a.mt - 1) / a.mt, p -= cnt;
-    s_first[e] = p;
-    if (e < a.E) {
-        a.table[e] = a.experts + (size_t)e * a.img_bytes;
-        for (int t = 0, q = g; t < cnt; t += a.mt, ++q)
-            a.wl.g_expert[q] = e, a.wl.g_start[q] = p + t, a.wl.g_count[q] = min(a.mt, cnt - t);
+    for (int w = 0; w < warp; ++w) g += s_g[w];
+    if (e == 255) *a.n_entries = g;
+    g -= mine;
+    s_first[e] = g;
+    for (int q = 0; q < mine; ++q) {
+        Mx4Entry &x = a.entries[g + q];
+        x.img = a.store[0] + (size_t)e * a.img_bytes, x.img_index = e;
+        x.count = (int16_t)min(a.mt, cnt - q * a.mt), x.shared = 0;
     }
     __syncthreads();
     for (int c = warp; c < chunks; c += 8) {
@@ -187,44 +204,69 @@ __device__ __forceinline__ void group_ids(const Mx4PlanesArgs &a, uint16_t *s_cn
         const int id = i < n ? a.ids[i] : -1;
         const unsigned same = __match_any_sync(kFull, id);
         if ((unsigned)id < (unsigned)a.E) {
-            const int at = s_first[id] + s_cnt[c * 256 + id] + __popc(same & ((1u << lane) - 1));
-            a.wl.pair_token[at] = i / a.K, a.wl.pair_slot[at] = i;
+            const int at = s_cnt[c * 256 + id] + __popc(same & ((1u << lane) - 1)), b = i / a.K;
+            Mx4Entry &x = a.entries[s_first[id] + at / a.mt];
+            const int q = at % a.mt;
+            x.token[q] = (uint16_t)b, x.slot[q] = (uint16_t)i, x.inv[q] = a.inv_rms ? a.inv_rms[b] : 1.f;
         }
+    }
+}
+
+// One warp, one entry of the router's work list.
+__device__ __forceinline__ void entry_from_list(const Mx4PlanesArgs &a, int g, int lane)
+{
+    const int ge = a.wl.g_expert[g], start = a.wl.g_start[g], cnt = a.wl.g_count[g], shared = ge >= a.E;
+    Mx4Entry &x = a.entries[g];
+    if (lane == 0) {
+        const uint8_t *img = a.blob[ge];
+        x.img = img, x.img_index = (int)((unsigned long long)(img - a.store[shared]) / a.img_bytes);
+        x.count = (int16_t)cnt, x.shared = (int16_t)shared;
+    }
+    if (lane < cnt) {
+        const int b = a.wl.pair_token[start + lane];
+        x.token[lane] = (uint16_t)b, x.slot[lane] = (uint16_t)a.wl.pair_slot[start + lane];
+        x.inv[lane] = a.inv_rms ? a.inv_rms[b] : 1.f;
     }
 }
 
 __global__ void __launch_bounds__(256) mx4_planes_kernel(const Mx4PlanesArgs a)
 {
-    extern __shared__ uint16_t s_cnt[];   // [chunks of 32 pairs][256]; only where a CTA groups
-    __shared__ int s_g[8], s_p[8], s_first[256];
+    extern __shared__ uint16_t s_cnt[];   // [chunks of 32 pairs][256]; only with ids
+    __shared__ int s_g[8], s_first[256];
     pdl_launch_dependents();
     pdl_wait();
-    if ((int)blockIdx.x < a.group_ctas) {
-        group_ids(a, s_cnt, s_g, s_p, s_first);
-        return;
+    const int blocks = a.H / kMxBlock, lane = threadIdx.x % kWarp, n = a.B * blocks;
+    int cta = blockIdx.x, ctas = gridDim.x;
+    if (a.ids) {
+        if (cta == 0) {
+            entries_from_ids(a, s_cnt, s_g, s_first);
+            return;
+        }
+        --cta, --ctas;
     }
-    const int blocks = a.H / kMxBlock, lane = threadIdx.x % kWarp;
-    const int n = a.B * blocks, step = ((int)gridDim.x - a.group_ctas) * (256 / kWarp);
-    for (int i = ((int)blockIdx.x - a.group_ctas) * (256 / kWarp) + threadIdx.x / kWarp; i < n; i += step) {
+    const int warp = cta * (256 / kWarp) + threadIdx.x / kWarp, step = ctas * (256 / kWarp);
+    for (int i = warp; i < n; i += step) {
         const int b = i / blocks, blk = i % blocks;
         planes_store(a.h[(size_t)b * a.H + blk * kMxBlock + lane], a.codes, a.scales, b, blk, blocks, lane);
+    }
+    if (!a.ids) {
+        const int entries = *a.wl.n_groups;
+        if (warp == 0 && lane == 0) *a.n_entries = entries;
+        for (int g = warp; g < entries; g += step) entry_from_list(a, g, lane);
     }
 }
 
 // ---- the two projections ------------------------------------------------------------------------
 
 struct Mx4FfnArgs {
-    WorkList wl;
-    int E;
-    const uint8_t *const *blob;          // image of every expert of the step
-    const uint8_t *store[2];             // first image of the maps: routed experts, experts >= E
-    unsigned long long img_bytes;
+    const Mx4Entry *entries;
+    const int *n_entries;
     long long scale_off[2];              // scales of the one or two matrices inside an image
     int rows, blocks;                    // rows of a matrix, scale blocks of its row
+    int last_task;                       // of the most that the call can have
     int mt, splits;                      // splits: of the reduction, over a cluster (gate/up) or over tasks (down)
     const uint8_t *x_scales;             // planes of the activations, [row][8][blocks]
     // gate/up
-    const float *inv_rms;
     uint8_t *act_codes, *act_scales;     // [pair][8][rows/32 * 16], [pair][8][rows/32]
     // down
     float *part;                         // [pair][splits][rows]
@@ -270,7 +312,6 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
     const int x_at = NMAT * kMmABytes, sfa_at = x_at + mxf_cols(a.mt) * 128, sfb_at = sfa_at + NMAT * 1024;
     constexpr int kSetCols = 8 * NMAT + 8;   // tensor-memory columns of a stage's scales
 
-    pdl_launch_dependents();
     if (tid == 0) {
         s_dead = 0;
         for (int s = 0; s < NS; ++s) dmbar_init(&full[s], 2), dmbar_init(&empty[s], 1);
@@ -287,11 +328,15 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     volatile int *dead = &s_dead;
-    pdl_wait();   // the work list and the planes are the kernel before's
+    // Gate/up: the work list and the planes are the kernel before's.  Down: only the activations are (the
+    // gate/up kernel lets its successor start after its own wait, so the work list is complete); its first
+    // weights are on their way while gate/up finishes elsewhere, and the warps that read activations wait.
+    if (NMAT == 2) pdl_wait();
+    pdl_launch_dependents();
 
     const int ranks = NMAT == 2 ? a.splits : 1;   // CTAs of a cluster that share a task's reduction
     const int tiles = (a.rows + kMmRows - 1) / kMmRows;
-    const int n_tasks = *a.wl.n_groups * tiles * (NMAT == 1 ? a.splits : 1);
+    const int n_tasks = *a.n_entries * tiles * (NMAT == 1 ? a.splits : 1);
     const int rank = blockIdx.x % ranks, first = blockIdx.x / ranks, step = gridDim.x / ranks;
     const int n_steps = (a.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
     auto k_range = [&](int z, int &beg, int &end) {
@@ -300,14 +345,17 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
     };
 
     if (warp == 0) {
+        // the scale warps' first loads go ahead of the flood of weights, or the first stage would wait
+        // behind it (measured: 10 us on the gate/up kernel at 64 sequences)
+        asm volatile("bar.sync 1, 160;" ::: "memory");
         if (elect_one()) {
             int s = 0, issued = 0;
             uint32_t par = 0;
             for (int task = first; task < n_tasks && !*dead; task += step) {
                 const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-                const int ge = a.wl.g_expert[t.g];
-                const bool shared = ge >= a.E;
-                const int img = (int)((unsigned long long)(a.blob[ge] - a.store[shared]) / a.img_bytes);
+                const Mx4Entry &en = a.entries[t.g];
+                const int img = en.img_index;
+                const bool shared = en.shared != 0;
                 const CUtensorMap *w0 = shared ? &map_s0 : &map_w0, *w1 = shared ? &map_s1 : &map_w1;
                 int k_beg, k_end;
                 k_range(t.z, k_beg, k_end);
@@ -338,7 +386,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         bool ok = true;
         for (int task = first; task < n_tasks && ok; task += step, ++it) {
             const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-            const int n = mxf_cols(a.wl.g_count[t.g]);
+            const int n = mxf_cols(a.entries[t.g].count);
             const uint32_t id0 = umma_idesc_mxf4(n, 0), id1 = umma_idesc_mxf4(n, 1);
             const int ab = it & 1;
             if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)))) break;
@@ -378,38 +426,49 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         for (int task = first; task < n_tasks; task += step, ++it) {
             const int ab = it & 1;
             const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-            const int start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
-            int slot_l = 0;      // lane i: the i-th pair's slot and RMSNorm factor, fetched while the MMAs run
-            float inv_l = 1.f;
-            if (lane < cnt) {
-                slot_l = a.wl.pair_slot[start + lane];
-                if (NMAT == 2 && a.inv_rms) inv_l = a.inv_rms[a.wl.pair_token[start + lane]];
-            }
+            const Mx4Entry &en = a.entries[t.g];
+            const int cnt = en.count, own = min(lane, kMxfTokens - 1);
+            const int slot_l = en.slot[own];      // lane i: the i-th pair's, fetched while the MMAs run
+            const float inv_l = en.inv[own];
             const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], (uint32_t)(it >> 1) & 1u, dead));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + ab * kMxfAccStride + ((uint32_t)(lg * kWarp) << 16);
             const int row = t.row0 + lg * kWarp + lane;
-            for (int i = 0; i < cnt; ++i) {
-                const int slot_i = __shfl_sync(kFull, slot_l, i);
-                const float inv_i = __shfl_sync(kFull, inv_l, i);
-                float y[NMAT];
+            // two tokens at a time: their chains (loads, reductions, conversions) overlap
+            for (int i0 = 0; i0 < cnt; i0 += 2) {
+                uint32_t raw[2][NMAT][8];
+                float y[2][NMAT];
 #pragma unroll
-                for (int m = 0; m < NMAT; ++m) {
-                    float v[8];
-                    tmem_ld8(acc + m * kMxfCols + i * kPlanes, v);
-                    y[m] = v[7];
+                for (int q = 0; q < 2; ++q)
 #pragma unroll
-                    for (int p = 6; p >= 0; --p) y[m] += v[p];
-                    if (!ok) y[m] = __uint_as_float(0x7fffffffu);
-                }
+                    for (int m = 0; m < NMAT; ++m) tmem_ld8_start(acc + m * kMxfCols + (i0 + q) * kPlanes, raw[q][m]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int m = 0; m < NMAT; ++m) {
+                        y[q][m] = __uint_as_float(raw[q][m][7]);   // smallest plane first
+#pragma unroll
+                        for (int p = 6; p >= 0; --p) y[q][m] += __uint_as_float(raw[q][m][p]);
+                        if (!ok) y[q][m] = __uint_as_float(0x7fffffffu);
+                    }
+                const bool two = i0 + 1 < cnt;   // with an odd count the second has read columns nobody wrote
+                const int slot0 = __shfl_sync(kFull, slot_l, i0), slot1 = __shfl_sync(kFull, slot_l, i0 + 1);
                 if (NMAT == 1) {
-                    if (row < a.rows)
-                        a.part[((long long)slot_i * a.splits + t.z) * a.rows + row] = y[0];
+                    if (row < a.rows) {
+                        a.part[((long long)slot0 * a.splits + t.z) * a.rows + row] = y[0][0];
+                        if (two) a.part[((long long)slot1 * a.splits + t.z) * a.rows + row] = y[1][0];
+                    }
                 } else if (ranks > 1) {
 #pragma unroll
-                    for (int m = 0; m < NMAT; ++m) part[(m * kMxfTokens + i) * kMmRows + lg * kWarp + lane] = y[m];
+                    for (int m = 0; m < NMAT; ++m) {
+                        part[(m * kMxfTokens + i0) * kMmRows + lg * kWarp + lane] = y[0][m];
+                        if (two) part[(m * kMxfTokens + i0 + 1) * kMmRows + lg * kWarp + lane] = y[1][m];
+                    }
                 } else if (t.row0 + lg * kWarp < a.rows) {   // rows are a multiple of 32: the whole warp or none of it
-                    mxf_store_act(a, y[0], y[NMAT - 1], slot_i, inv_i, row, lane);
+                    const float inv0 = __shfl_sync(kFull, inv_l, i0), inv1 = __shfl_sync(kFull, inv_l, i0 + 1);
+                    mxf_store_act(a, y[0][0], y[0][NMAT - 1], slot0, inv0, row, lane);
+                    if (two) mxf_store_act(a, y[1][0], y[1][NMAT - 1], slot1, inv1, row, lane);
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -423,12 +482,39 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         // splits, so the position is walked, not computed
         const int w = warp - 6;
         const int x_align = a.blocks % 8 == 0 ? 8 : a.blocks % 4 == 0 ? 4 : 1;
+        // what a warp knows of the task its next step belongs to, and of the one after (asked for at the
+        // start of this one)
+        struct Info {
+            const uint8_t *img;
+            int cnt, row;                 // row: lane i: token or slot of pair i
+        };
         struct Pos {
-            int task, k, end;
+            int task, k, end, row0;
+            Info in, ahead;
+        };
+        auto ask = [&](int task) {
+            const Mx4Entry &en = a.entries[min(task, a.last_task) / (tiles * (NMAT == 1 ? a.splits : 1))];
+            const int own = min(lane, kMxfTokens - 1);
+            return Info{en.img, en.count, NMAT == 2 ? en.token[own] : en.slot[own]};
+        };
+        // scale rows of a task into L2 while the one before it runs: a lane a row, a warp a quarter of them
+        auto prefetch = [&](int task, const uint8_t *img) {
+            if (task >= n_tasks) return;
+            const Mx4FfnTask t = mxf_task<NMAT>(a, task);
+            int beg, end;
+            k_range(t.z, beg, end);
+            const int row = t.row0 + w * kWarp + lane, lo = beg * kMmStageBlocks, hi = min(end * kMmStageBlocks, a.blocks);
+            if (row < a.rows)
+#pragma unroll
+                for (int m = 0; m < NMAT; ++m)
+                    for (int o = lo; o < hi; o += 128) prefetch_l2(img + a.scale_off[m] + (long long)row * a.blocks + o);
         };
         auto enter = [&](Pos &p) {   // first step of task p.task
             if (p.task >= n_tasks) return;
-            k_range(mxf_task<NMAT>(a, p.task).z, p.k, p.end);
+            const Mx4FfnTask t = mxf_task<NMAT>(a, p.task);
+            p.in = p.ahead, p.row0 = t.row0;
+            p.ahead = ask(p.task + step);
+            k_range(t.z, p.k, p.end);
         };
         auto forward = [&](Pos &p, int by) {
             p.k += by;
@@ -439,40 +525,38 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                 p.k += over;
             }
         };
-        auto load = [&](const Pos &p, uint2 (&vw)[NMAT][4], uint2 (&vx)[3], int &cnt, int &xrow) {
-            if (p.task >= n_tasks) return false;
-            const Mx4FfnTask t = mxf_task<NMAT>(a, p.task);
-            const int ge = a.wl.g_expert[t.g], start = a.wl.g_start[t.g];
-            cnt = a.wl.g_count[t.g];
-            xrow = 0;   // lane i: first plane of token i
-            if (lane < cnt) xrow = kPlanes * (NMAT == 2 ? a.wl.pair_token[start + lane] : a.wl.pair_slot[start + lane]);
-            const uint8_t *img = a.blob[ge];
-            const int kb = p.k * kMmStageBlocks;
+        auto load_w = [&](const Pos &p, uint2 (&vw)[NMAT][4]) {
 #pragma unroll
             for (int m = 0; m < NMAT; ++m)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    vw[m][r] = load_scales8(img + a.scale_off[m] + (long long)min(t.row0 + 32 * r + lane, a.rows - 1) * a.blocks, kb, a.blocks, a.w_align);
+                    vw[m][r] = load_scales8(p.in.img + a.scale_off[m] + (long long)min(p.row0 + 32 * r + lane, a.rows - 1) * a.blocks,
+                                            p.k * kMmStageBlocks, a.blocks, a.w_align);
+        };
+        auto load_x = [&](const Pos &p, uint2 (&vx)[3]) {
 #pragma unroll
             for (int r = 0; r < 3; ++r) {
                 const int q = 32 * r + lane;   // row of the B tile: plane q % 8 of token q / 8
                 vx[r] = make_uint2(0u, 0u);
-                const long long row = __shfl_sync(kFull, xrow, q / kPlanes) + q % kPlanes;
-                if (q < cnt * kPlanes) vx[r] = load_scales8(a.x_scales + row * a.blocks, kb, a.blocks, x_align);
+                const long long row = __shfl_sync(kFull, p.in.row, q / kPlanes) * kPlanes + q % kPlanes;
+                if (q < p.in.cnt * kPlanes) vx[r] = load_scales8(a.x_scales + row * a.blocks, p.k * kMmStageBlocks, a.blocks, x_align);
             }
-            return true;
         };
         uint2 vw[NMAT][4], vx[3], nw[NMAT][4], nx[3];
-        Pos p = {first, 0, 0};
+        Pos p = {first, 0, 0, 0, {}, ask(first)};
         enter(p);
         forward(p, w);
-        int i = w;
-        int cnt = 0, xrow = 0, n_cnt = 0, n_xrow = 0;
-        bool more = load(p, vw, vx, cnt, xrow);
-        while (more) {
-            const int k = p.k;
+        if (p.task < n_tasks) load_w(p, vw);
+        asm volatile("bar.sync 1, 160;" ::: "memory");
+        if (NMAT == 1) pdl_wait();   // the activations
+        if (p.task < n_tasks) load_x(p, vx);
+        int fetched = first;   // tasks whose scales have been asked into L2
+        for (int i = w; p.task < n_tasks; i += 4) {
+            const int k = p.k, cnt = p.in.cnt, xrow = p.in.row;
+            if (fetched == p.task) prefetch(fetched += step, p.ahead.img);
             forward(p, 4);
-            more = load(p, nw, nx, n_cnt, n_xrow);
+            if (fetched < p.task) fetched = p.task;
+            if (p.task < n_tasks) load_w(p, nw), load_x(p, nx);
             const int s = i % NS;
             const bool ok = __all_sync(kFull, dmbar_wait(&empty[s], ((uint32_t)(i / NS) & 1u) ^ 1u, dead));
             uint8_t *st = dsm + (size_t)s * slot;
@@ -485,7 +569,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             const uint32_t xst = dsmem_u32(st + x_at);
             if (elect_one()) dmbar_expect_tx(&full[s], (uint32_t)(cnt * kPlanes * 128));
             for (int q = 0; q < cnt; ++q) {
-                const int row = __shfl_sync(kFull, xrow, q);
+                const int row = __shfl_sync(kFull, xrow, q) * kPlanes;
                 if (elect_one()) tma_load_2d_at(xst + q * kPlanes * 128, &map_x, k * 128, row, &full[s]);
             }
 #pragma unroll
@@ -494,22 +578,21 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                 for (int r = 0; r < 4; ++r) vw[m][r] = nw[m][r];
 #pragma unroll
             for (int r = 0; r < 3; ++r) vx[r] = nx[r];
-            cnt = n_cnt, xrow = n_xrow;
-            i += 4;
         }
     }
     if (NMAT == 2 && ranks > 1 && first < n_tasks) {   // one task per cluster
         __syncwarp();
         cluster_sync();
         const Mx4FfnTask t = mxf_task<NMAT>(a, first);
-        const int start = a.wl.g_start[t.g], cnt = a.wl.g_count[t.g];
+        const Mx4Entry &en = a.entries[t.g];
+        const int cnt = en.count;
         const uint32_t part = dsmem_u32(dsm);
         // (token, 32 rows) units, dealt to the ranks and their warps
         for (int u = rank + ranks * warp; u < cnt * 4; u += ranks * (kMmThreads / kWarp)) {
             const int i = u / 4, r0 = (u % 4) * kWarp;
             if (t.row0 + r0 >= a.rows) continue;
-            const int slot_i = a.wl.pair_slot[start + i];
-            const float inv_i = a.inv_rms ? a.inv_rms[a.wl.pair_token[start + i]] : 1.f;
+            const int slot_i = en.slot[i];
+            const float inv_i = en.inv[i];
             float g = 0.f, v = 0.f;
             for (int z = 0; z < ranks; ++z) {
                 g += ld_cluster(part + (uint32_t)(i * kMmRows + r0 + lane) * 4, z);
@@ -519,6 +602,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         }
         cluster_sync();
     }
+    if (NMAT == 1) pdl_wait();   // a CTA without tasks too: the grid's end then means that gate/up has ended
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (warp == 1) {

@@ -337,6 +337,8 @@ struct Mx4FfnMaps {
     CUtensorMap x, act;
 };
 struct Mx4FfnBufs {
+    Mx4Entry *entries;   // [pairs]
+    int *n_entries;
     uint8_t *x_codes, *x_scales, *act_codes, *act_scales;
     float *part;
 };
@@ -355,6 +357,8 @@ size_t mx4_buffers(uint8_t *base, int B, int pairs, int H, int I, Mx4FfnBufs *b)
         o += round_up(n, 256);
         return p;
     };
+    b->entries = (Mx4Entry *)take(sizeof(Mx4Entry) * (size_t)pairs);
+    b->n_entries = (int *)take(sizeof(int));
     b->x_codes = take((size_t)B * kPlanes * H / 2);
     b->x_scales = take((size_t)B * kPlanes * H / kMxBlock);
     b->act_codes = take((size_t)pairs * kPlanes * I / 2);
@@ -431,8 +435,7 @@ int mx4_prepare_kernels(int dev)
     return STMOE_OK;
 }
 
-// The FFN of one layer step; pa: the planes kernel's arguments (with grouping for the stand-alone
-// call, fa: inputs, outputs and work list as for the other formats; mark(i): called before the first
+// The FFN of one layer step; pa: empty, or with the ids of the stand-alone call; fa: inputs, outputs and work list as for the other formats; mark(i): called before the first
 // launch, between the projections and behind the last launch.
 template <typename Mark>
 int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnArgs fa, size_t img_bytes, unsigned *err, int sms,
@@ -440,21 +443,24 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
 {
     ST_TRY(mark(0));
     const int H = fa.H, I = fa.I, pairs = fa.B * (fa.K + fa.n_shared), mt = mx4_entry_tokens(fa.B);
-    pa.h = fa.h, pa.B = fa.B, pa.H = H, pa.codes = b.x_codes, pa.scales = b.x_scales;
+    pa.h = fa.h, pa.inv_rms = fa.inv_rms, pa.B = fa.B, pa.H = H, pa.codes = b.x_codes, pa.scales = b.x_scales;
+    pa.entries = b.entries, pa.n_entries = b.n_entries, pa.store[0] = maps.store[0], pa.store[1] = maps.store[1];
+    pa.img_bytes = img_bytes, pa.E = fa.E, pa.K = fa.K, pa.mt = mt, pa.wl = fa.wl, pa.blob = fa.blob;
     const int blocks = fa.B * H / kMxBlock;
-    ST_TRY(mx4_launch(mx4_planes_kernel, pa.group_ctas + std::min(sms * 4, (blocks + 7) / 8), 256,
-                      pa.group_ctas ? sizeof(uint16_t) * 256 * (size_t)((fa.B * fa.K + kWarp - 1) / kWarp) : 0, 1, st, pa));
+    ST_TRY(mx4_launch(mx4_planes_kernel, (pa.ids ? 1 : 0) + std::min(sms * 4, (blocks + 7) / 8), 256,
+                      pa.ids ? sizeof(uint16_t) * 256 * (size_t)((fa.B * fa.K + kWarp - 1) / kWarp) : 0, 1, st, pa));
 
     // at most this many entries: an expert's pairs fill its entries but for the last
     const int entries = std::min(pairs, fa.E + fa.n_shared + pairs / mt);
     Mx4FfnArgs g{};
-    g.wl = fa.wl, g.E = fa.E, g.blob = fa.blob, g.store[0] = maps.store[0], g.store[1] = maps.store[1], g.img_bytes = img_bytes;
+    g.entries = b.entries, g.n_entries = b.n_entries;
     g.scale_off[0] = (long long)mx4_image_scales(H, I, 0), g.scale_off[1] = (long long)mx4_image_scales(H, I, 1);
     g.rows = I, g.blocks = H / kMxBlock, g.mt = mt;
-    g.x_scales = b.x_scales, g.inv_rms = fa.inv_rms, g.act_codes = b.act_codes, g.act_scales = b.act_scales, g.err = err;
+    g.x_scales = b.x_scales, g.act_codes = b.act_codes, g.act_scales = b.act_scales, g.err = err;
     g.w_align = g.blocks % 8 == 0 ? 8 : g.blocks % 4 == 0 ? 4 : 1;
     const int gu_steps = (g.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
     const int gu_tasks = entries * ((I + kMmRows - 1) / kMmRows);
+    g.last_task = gu_tasks - 1;
     // fewer tiles than SMs: a cluster shares a tile's reduction
     g.splits = std::max(1, std::min({sms / gu_tasks, gu_steps, kMmMaxSplits}));
     ST_TRY(mx4_launch(mx4_ffn_kernel<2>, g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMmThreads, kMmSmemBytes,
@@ -473,6 +479,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
         const double t = (double)((d_tiles * z + sms - 1) / sms) / z * (1 + 0.03 * z);
         if (t < best) best = t, d.splits = z;
     }
+    d.last_task = d_tiles * d.splits - 1;
     ST_TRY(mx4_launch(mx4_ffn_kernel<1>, std::min(d_tiles * d.splits, sms), kMmThreads, kMmSmemBytes, 1, st, maps.down[0],
                       maps.down[0], maps.down[1], maps.down[1], maps.act, d));
 
@@ -2115,12 +2122,6 @@ bool mx4_ffn_args_ok(const void *experts, int hidden, int inter)
 {
     return hidden % kMxBlock == 0 && inter % kMxBlock == 0 && ((uintptr_t)experts & 15) == 0;
 }
-// scratch of a stand-alone MX4 call: work list | image table | planes and partial sums
-size_t mx4_scratch_layout(int B, int K, size_t *o_tab)
-{
-    *o_tab = round_up(sizeof(int) * (4 + 5 * (size_t)B * K), 256);
-    return *o_tab + round_up(sizeof(void *) * (size_t)kMaxExperts, 256);
-}
 
 int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const float *w, const void *experts, int batch,
                 int n_experts, int top_k, int hidden, int inter, float residual_scale, float *h_out, void *scratch,
@@ -2133,22 +2134,17 @@ int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const 
     CU_TRY(cudaGetDevice(&dev));
     ST_TRY(mx4_prepare_kernels(dev));
     if (!sms[dev]) sms[dev] = sm_count();
-    uint8_t *sc = (uint8_t *)scratch;
-    size_t o_tab;
-    const size_t o_buf = mx4_scratch_layout(batch, top_k, &o_tab), img = image_bytes(hidden, inter, STMOE_MX4);
+    const size_t img = image_bytes(hidden, inter, STMOE_MX4);
     Mx4FfnBufs b;
-    mx4_buffers(sc + o_buf, batch, batch * top_k, hidden, inter, &b);
+    mx4_buffers((uint8_t *)scratch, batch, batch * top_k, hidden, inter, &b);
     Mx4FfnMaps maps;
     ST_TRY(mx4_weight_maps(&maps, 0, (const uint8_t *)experts, n_experts, img, hidden, inter));
     maps.gate[1] = maps.gate[0], maps.up[1] = maps.up[0], maps.down[1] = maps.down[0], maps.store[1] = maps.store[0];
     ST_TRY(mx4_act_maps(&maps, b, batch, batch * top_k, hidden, inter));
-    WorkListMem wlm;
-    wlm.bind((int *)sc, batch * top_k);
     Mx4PlanesArgs pa{};
-    pa.group_ctas = 1, pa.ids = ids, pa.E = n_experts, pa.K = top_k, pa.mt = mx4_entry_tokens(batch), pa.wl = wlm.wl;
-    pa.experts = (const uint8_t *)experts, pa.img_bytes = img, pa.table = (const uint8_t **)(sc + o_tab);
+    pa.ids = ids;
     FfnArgs fa{};
-    fa.h = h, fa.inv_rms = inv_rms, fa.wl = wlm.wl, fa.blob = pa.table;
+    fa.h = h, fa.inv_rms = inv_rms;
     fa.H = hidden, fa.I = inter, fa.E = n_experts, fa.w = w, fa.h_out = h_out;
     fa.B = batch, fa.K = top_k, fa.n_shared = 0, fa.residual_scale = residual_scale;
     return mx4_ffn(maps, b, pa, fa, img, nullptr, sms[dev], st, [](int) { return STMOE_OK; });
@@ -2159,9 +2155,8 @@ int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const 
 extern "C" size_t stmoe_mx4_ffn_scratch_bytes(int batch, int top_k, int hidden, int inter)
 {
     if (batch < 1 || batch > kMaxBatch || top_k < 1 || top_k > kMaxTopK || hidden < kMxBlock || inter < kMxBlock) return 0;
-    size_t o_tab;
     Mx4FfnBufs b;
-    return mx4_scratch_layout(batch, top_k, &o_tab) + mx4_buffers(nullptr, batch, batch * top_k, hidden, inter, &b);
+    return mx4_buffers(nullptr, batch, batch * top_k, hidden, inter, &b);
 }
 
 extern "C" int stmoe_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const float *w,

@@ -81,13 +81,19 @@ __device__ __forceinline__ void umma_commit_if(bool leader, uint64_t *bar)
         "r"((uint32_t)leader)
         : "memory");
 }
-__device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&v)[8])
+// tensor memory -> registers, eight columns of this thread's lane; the values are there after tmem_ld_wait
+__device__ __forceinline__ void tmem_ld8_start(uint32_t addr, uint32_t (&r)[8])
 {
-    uint32_t r[8];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                  : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&v)[8])
+{
+    uint32_t r[8];
+    tmem_ld8_start(addr, r);
+    tmem_ld_wait();
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
