@@ -525,24 +525,23 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                 p.k += over;
             }
         };
-        auto load_w = [&](const Pos &p, uint2 (&vw)[NMAT][4]) {
-#pragma unroll
-            for (int m = 0; m < NMAT; ++m)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    vw[m][r] = load_scales8(p.in.img + a.scale_off[m] + (long long)min(p.row0 + 32 * r + lane, a.rows - 1) * a.blocks,
-                                            p.k * kMmStageBlocks, a.blocks, a.w_align);
+        auto load_w = [&](const Pos &p, uint2 (&vw)[4 * NMAT]) {
+            load_scales<4 * NMAT>(vw, [&](int i) {
+                return p.in.img + a.scale_off[i / 4] + (long long)min(p.row0 + 32 * (i % 4) + lane, a.rows - 1) * a.blocks;
+            }, (1u << (4 * NMAT)) - 1, p.k * kMmStageBlocks, a.blocks, a.w_align);
         };
         auto load_x = [&](const Pos &p, uint2 (&vx)[3]) {
+            int row[3];   // rows of the B tile: plane q % 8 of token q / 8
+            uint32_t on = 0;
 #pragma unroll
             for (int r = 0; r < 3; ++r) {
-                const int q = 32 * r + lane;   // row of the B tile: plane q % 8 of token q / 8
-                vx[r] = make_uint2(0u, 0u);
-                const long long row = __shfl_sync(kFull, p.in.row, q / kPlanes) * kPlanes + q % kPlanes;
-                if (q < p.in.cnt * kPlanes) vx[r] = load_scales8(a.x_scales + row * a.blocks, p.k * kMmStageBlocks, a.blocks, x_align);
+                const int q = 32 * r + lane;
+                row[r] = __shfl_sync(kFull, p.in.row, q / kPlanes) * kPlanes + q % kPlanes;
+                if (q < p.in.cnt * kPlanes) on |= 1u << r;
             }
+            load_scales<3>(vx, [&](int r) { return a.x_scales + (long long)row[r] * a.blocks; }, on, p.k * kMmStageBlocks, a.blocks, x_align);
         };
-        uint2 vw[NMAT][4], vx[3], nw[NMAT][4], nx[3];
+        uint2 vw[4 * NMAT], vx[3], nw[4 * NMAT], nx[3];
         Pos p = {first, 0, 0, 0, {}, ask(first)};
         enter(p);
         forward(p, w);
@@ -561,7 +560,10 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             const bool ok = __all_sync(kFull, dmbar_wait(&empty[s], ((uint32_t)(i / NS) & 1u) ^ 1u, dead));
             uint8_t *st = dsm + (size_t)s * slot;
 #pragma unroll
-            for (int m = 0; m < NMAT; ++m) store_scales<4>(st + sfa_at + 1024 * m, 512, lane, vw[m]);
+            for (int m = 0; m < NMAT; ++m) {
+                const uint2 v[4] = {vw[4 * m], vw[4 * m + 1], vw[4 * m + 2], vw[4 * m + 3]};
+                store_scales<4>(st + sfa_at + 1024 * m, 512, lane, v);
+            }
             store_scales<3>(st + sfb_at, 512, lane, vx);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -573,9 +575,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                 if (elect_one()) tma_load_2d_at(xst + q * kPlanes * 128, &map_x, k * 128, row, &full[s]);
             }
 #pragma unroll
-            for (int m = 0; m < NMAT; ++m)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) vw[m][r] = nw[m][r];
+            for (int r = 0; r < 4 * NMAT; ++r) vw[r] = nw[r];
 #pragma unroll
             for (int r = 0; r < 3; ++r) vx[r] = nx[r];
         }

@@ -127,23 +127,55 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16])
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// eight scale bytes of a row from block kb on, by the widest loads the rows' alignment allows; blocks
-// past the end read as 1.0 (their codes are zero, and zero times a NaN scale would not be)
-__device__ __forceinline__ uint2 load_scales8(const uint8_t *row, int kb, int blocks, int align)
+// Eight scale bytes, from block kb on, of G rows of a lane (row(r): address of row r's first scale; rows
+// whose `on` bit is clear read nothing).  Blocks past the end read as 1.0: their codes are zero, and zero
+// times a NaN scale would not be.  One branch around all loads, and the loads predicated inside: with a
+// branch at each of them they waited for one another (11 cold loads, 8 us in front of the first MMA).
+__device__ __forceinline__ uint2 ld_scales8_if(bool on, const uint8_t *p)
 {
-    if (align >= 4 && kb + 8 <= blocks) {
-        if (align == 8) return __ldg(reinterpret_cast<const uint2 *>(row + kb));
-        return make_uint2(__ldg(reinterpret_cast<const uint32_t *>(row + kb)), __ldg(reinterpret_cast<const uint32_t *>(row + kb) + 1));
-    }
-    uint2 v = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (kb + i < blocks) {
-            const uint32_t b = __ldg(row + kb + i);
-            uint32_t &w = i < 4 ? v.x : v.y;
-            w = (w & ~(0xffu << (8 * (i & 3)))) | (b << (8 * (i & 3)));
-        }
+    uint2 v;
+    asm("{.reg .pred p;\n\t"
+        "setp.ne.b32 p, %3, 0;\n\t"
+        "mov.b32 %0, 0x7f7f7f7f;\n\t"
+        "mov.b32 %1, 0x7f7f7f7f;\n\t"
+        "@p ld.global.nc.v2.u32 {%0, %1}, [%2];}"
+        : "=&r"(v.x), "=&r"(v.y)
+        : "l"(p), "r"((uint32_t)on));
     return v;
+}
+__device__ __forceinline__ uint32_t ld_scales4_if(bool on, const uint8_t *p)
+{
+    uint32_t v;
+    asm("{.reg .pred p;\n\t"
+        "setp.ne.b32 p, %2, 0;\n\t"
+        "mov.b32 %0, 0x7f7f7f7f;\n\t"
+        "@p ld.global.nc.u32 %0, [%1];}"
+        : "=&r"(v)
+        : "l"(p), "r"((uint32_t)on));
+    return v;
+}
+template <int G, typename Row>
+__device__ __forceinline__ void load_scales(uint2 (&v)[G], Row row, uint32_t on, int kb, int blocks, int align)
+{
+    if (align == 8 && kb + 8 <= blocks) {
+#pragma unroll
+        for (int r = 0; r < G; ++r) v[r] = ld_scales8_if(on >> r & 1, row(r) + kb);
+    } else if (align >= 4 && blocks % 4 == 0) {   // whole words, the second perhaps past the end
+#pragma unroll
+        for (int r = 0; r < G; ++r) {
+            v[r].x = ld_scales4_if(on >> r & 1, row(r) + kb);
+            v[r].y = ld_scales4_if((on >> r & 1) && kb + 4 < blocks, row(r) + kb + 4);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < G; ++r) {
+            const uint8_t *p = row(r) + kb;
+            uint32_t b[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = (on >> r & 1) && kb + i < blocks ? (uint32_t)__ldg(p + i) : 0x7fu;
+            v[r] = make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+        }
+    }
 }
 // What a lane has read of G row groups (rows lane, lane + 32, ...), into the atoms of 128 rows x four
 // blocks: first half at st, second half of the stage's blocks `half` bytes behind it
@@ -401,13 +433,10 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             const int kb = k * kMmStageBlocks;
             k += 4;
             const uint8_t *pb = a.b_scales + (long long)t.expert * a.n * a.b_scale_stride;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                vb[r] = load_scales8(pb + (long long)min(t.row0 + 32 * r + lane, a.n - 1) * a.b_scale_stride, kb, a.blocks, a.b_align);
-#pragma unroll
-            for (int r = 0; r < 6; ++r)
-                if (32 * r < bn)
-                    va[r] = load_scales8(a.a_scales + (long long)min(t.tok0 + 32 * r + lane, a.m - 1) * a.a_scale_stride, kb, a.blocks, a.a_align);
+            load_scales<4>(vb, [&](int r) { return pb + (long long)min(t.row0 + 32 * r + lane, a.n - 1) * a.b_scale_stride; }, 15u, kb,
+                           a.blocks, a.b_align);
+            load_scales<6>(va, [&](int r) { return a.a_scales + (long long)min(t.tok0 + 32 * r + lane, a.m - 1) * a.a_scale_stride; },
+                           (1u << ((bn + 31) / 32)) - 1, kb, a.blocks, a.a_align);
             return true;
         };
         uint2 vb[4], va[6], nb[4], na[6];
