@@ -437,11 +437,11 @@ int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_
  *            counted, an expert that stands twice in a row counts twice
  *   mask     uint8 [tokens] or NULL
  *   loss     fp32 [2], counts int32 [n_experts], rows int32 [1] (= n): written
- *   scratch  stmoe_router_balance_scratch_bytes(n_experts) bytes, 4-byte aligned, contents free;
- *            calls that can overlap need scratch of their own
+ *   scratch  stmoe_router_balance_scratch_bytes(tokens, n_experts) bytes (0 for short batches: NULL is
+ *            fine), 4-byte aligned, contents free; calls that can overlap need scratch of their own
  * All pointers device.  n_experts <= 256, top_k <= n_experts, tokens * top_k < 2^31; tokens may be 0.  The same call
  * gives the same bits every time.  Asynchronous on cuda_stream. */
-size_t stmoe_router_balance_scratch_bytes(int n_experts);
+size_t stmoe_router_balance_scratch_bytes(int64_t tokens, int n_experts);
 int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const int32_t *ids, const uint8_t *mask, int64_t tokens,
                          int n_experts, int top_k, float *loss, int32_t *counts, int32_t *rows, void *scratch,
                          size_t scratch_bytes, void *cuda_stream);

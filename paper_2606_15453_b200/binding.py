@@ -98,7 +98,7 @@ def lib():
         L.stmoe_mx4_dequantize.argtypes = [vp, i64, vp, i64, i64, i64, vp, i32, i64, vp]
         L.stmoe_mx4_matmul.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, i64, i32, i32, i32, vp, vp, i32, i64, vp, vp]
         L.stmoe_router_balance_scratch_bytes.restype = sz
-        L.stmoe_router_balance_scratch_bytes.argtypes = [i32]
+        L.stmoe_router_balance_scratch_bytes.argtypes = [i64, i32]
         L.stmoe_router_balance.argtypes = [vp, i32, i64, vp, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
         L.stmoe_router_balance_backward.argtypes = [vp, i32, i64, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp]
         _lib = L
@@ -370,8 +370,9 @@ def mx4_quantize(x, codes=None, scales=None, stream=None):
         _refuse("x: expected a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows")
     rows, cols = x.shape
     nb = (cols + 31) // 32
-    for t, n in ((codes, nb * 16), (scales, nb)):
-        if t is not None and not (_is_rows(t, _U8) and t.shape[0] == rows and t.shape[1] == n and t.device == x.device):
+    if codes is not None or scales is not None:
+        if not all(t is None or (_is_rows(t, _U8) and t.shape[0] == rows and t.shape[1] == n and t.device == x.device)
+                   for t, n in ((codes, nb * 16), (scales, nb))):
             _refuse(f"codes and scales: expected uint8 {(rows, nb * 16)} and {(rows, nb)} on x's device")
     st = _stream_of(x, stream)
     if st is None:
@@ -513,20 +514,17 @@ def router_balance(logits, ids, mask=None, stream=None):
     if st is None:
         return _there(logits, stream, router_balance, logits, ids, mask)
     L = lib()
-    n = L.stmoe_router_balance_scratch_bytes(E)
-    if n == 0:
-        _refuse(f"{E} experts are out of range")
-    # one allocation: loss | counts | rows | scratch of the call
-    buf = torch.empty(n // 4 + E + 3, dtype=_F32, device=logits.device)
-    head, ptr = buf[:E + 3], buf.data_ptr()
-    ints = head.view(_I32)
+    n = L.stmoe_router_balance_scratch_bytes(T, E)
+    dev = logits.device
+    loss, counts, rows = (torch.empty(k, dtype=t, device=dev) for k, t in ((2, _F32), (E, _I32), (1, _I32)))
+    scratch = torch.empty(n, dtype=_U8, device=dev) if n else None
     # an empty tensor has no address; nothing of it is read
-    src, idp = (logits.data_ptr(), ids.data_ptr()) if T else (ptr, ptr)
-    rc = L.stmoe_router_balance(src, elem, logits.stride(0), idp, None if mask is None else mask.data_ptr(), T, E, K, ptr, ptr + 8,
-                                ptr + 8 + 4 * E, ptr + 12 + 4 * E, n, st)
+    src, idp = (logits.data_ptr(), ids.data_ptr()) if T else (loss.data_ptr(), loss.data_ptr())
+    rc = L.stmoe_router_balance(src, elem, logits.stride(0), idp, None if mask is None else mask.data_ptr(), T, E, K, loss.data_ptr(),
+                                counts.data_ptr(), rows.data_ptr(), None if scratch is None else scratch.data_ptr(), n, st)
     if rc:
         _check(rc, "stmoe_router_balance")
-    return {"loss": head[:2], "counts": ints[2:E + 2], "rows": ints[E + 2:], "top_k": K}
+    return {"loss": loss, "counts": counts, "rows": rows, "top_k": K}
 
 
 def router_balance_backward(logits, forward, grad_loss, mask=None, out=None, stream=None):

@@ -45,12 +45,30 @@ int sm_count(int *dev_out)
 bool elem_type(int dtype) { return dtype == STMOE_F32 || dtype == STMOE_BF16 || dtype == STMOE_F16; }
 long long elem_bytes(int dtype) { return dtype == STMOE_F32 ? 4 : 2; }
 
-template <int DT> void launch_rows(bool quantize, const Mx4Rows &a, int grid, cudaStream_t st)
+// Launch that may start while the kernel before it in the stream drains (programmatic dependent
+// launch; the kernels wait for it themselves), in clusters of `cluster` CTAs.
+template <typename... P, typename... A>
+int launch_behind(void (*kernel)(P...), int grid, int block, int smem, int cluster, cudaStream_t st, const A &...args)
 {
-    if (quantize && a.vec) mx4_quantize_kernel<DT, true><<<grid, kMxThreads, 0, st>>>(a);
-    else if (quantize) mx4_quantize_kernel<DT, false><<<grid, kMxThreads, 0, st>>>(a);
-    else if (a.vec) mx4_dequantize_kernel<DT, true><<<grid, kMxThreads, 0, st>>>(a);
-    else mx4_dequantize_kernel<DT, false><<<grid, kMxThreads, 0, st>>>(a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
+    CU_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    return STMOE_OK;
+}
+
+template <int DT> int launch_rows(bool quantize, const Mx4Rows &a, int64_t warps, int sms, cudaStream_t st)
+{
+    const int64_t ctas = (warps + kMxThreads / kWarp - 1) / (kMxThreads / kWarp);
+    const int grid = (int)std::min<int64_t>(ctas, (int64_t)sms * (quantize ? mx4_quantize_ctas<DT>() : 8));
+    if (quantize)
+        return launch_behind(a.vec ? mx4_quantize_kernel<DT, true> : mx4_quantize_kernel<DT, false>, grid, kMxThreads, 0, 1, st, a);
+    return launch_behind(a.vec ? mx4_dequantize_kernel<DT, true> : mx4_dequantize_kernel<DT, false>, grid, kMxThreads, 0, 1, st, a);
 }
 
 int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int64_t x_stride, uint8_t *codes,
@@ -73,14 +91,11 @@ int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int6
     if (rows > 1 && cols % kMxBlock == 0 && x_stride == cols && code_stride == nb * 16 && scale_stride == nb)
         a.rows = 1, a.cols = rows * cols;
     a.vec = ((uintptr_t)x & 15) == 0 && (a.rows == 1 || (x_stride * elem_bytes(dtype)) % 16 == 0);
-    const int64_t tasks = a.rows * ((a.cols - 1) / kMxSeg + 1), warps = kMxThreads / kWarp;
-    const int grid = (int)std::min<int64_t>((tasks + warps - 1) / warps, (int64_t)sms * 8);
+    const int64_t tasks = a.rows * ((a.cols - 1) / kMxSeg + 1);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == STMOE_F32) launch_rows<0>(quantize, a, grid, st);
-    else if (dtype == STMOE_BF16) launch_rows<1>(quantize, a, grid, st);
-    else launch_rows<4>(quantize, a, grid, st);
-    CU_TRY(cudaGetLastError());
-    return STMOE_OK;
+    if (dtype == STMOE_F32) return launch_rows<0>(quantize, a, tasks, sms, st);
+    if (dtype == STMOE_BF16) return launch_rows<1>(quantize, a, tasks, sms, st);
+    return launch_rows<4>(quantize, a, tasks, sms, st);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -120,14 +135,7 @@ int launch_matmul(const CUtensorMap &ma, const CUtensorMap &mb, const Mx4MatmulA
         CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<ODT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
         ready[dev] = true;
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(kMmThreads), cfg.dynamicSmemBytes = kMmSmemBytes, cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = a.splits, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
-    cfg.attrs = at, cfg.numAttrs = 1;
-    CU_TRY(cudaLaunchKernelEx(&cfg, mx4_matmul_kernel<ODT>, ma, mb, a));
-    return STMOE_OK;
+    return launch_behind(mx4_matmul_kernel<ODT>, grid, kMmThreads, kMmSmemBytes, a.splits, st, ma, mb, a);
 }
 
 }  // namespace

@@ -11,8 +11,9 @@
 //
 // Both directions are bound by HBM: one pass, 16-byte loads of the wide side, 4-byte accesses of
 // the codes.  A lane owns 8 consecutive elements of a block, so the block maximum is two shuffles;
-// a warp takes 1024 elements of a row at a time, four independent groups per lane, which keeps
-// enough loads in flight.  The arithmetic is exact: the scale is a power of two, its exponent is
+// a warp takes 1024 elements of a row at a time, four independent groups per lane.  Quantising, it asks
+// for the next 1024 before it works on these (raw, half the registers of the widened values; without
+// that the loads' latency showed: 43 us for 14336 x 4096 bf16).  The arithmetic is exact: the scale is a power of two, its exponent is
 // read from the bits of amax, and the only rounding is the conversion to e2m1.
 #pragma once
 #include <cuda_bf16.h>
@@ -71,31 +72,85 @@ template <> struct Elem<0> {
 };
 template <> struct Elem<1> {
     using T = __nv_bfloat16;
+    using T2 = __nv_bfloat162;
     static constexpr int kVec = 8;
+    __device__ static __forceinline__ T2 from_bits(uint32_t w) { return *reinterpret_cast<const T2 *>(&w); }
+    __device__ static __forceinline__ float2 widen(T2 v)
+    {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(&v);
+        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
     __device__ static __forceinline__ float to_f32(T v) { return __bfloat162float(v); }
     __device__ static __forceinline__ T from_f32(float v) { return __float2bfloat16_rn(v); }
 };
 template <> struct Elem<4> {
     using T = __half;
+    using T2 = __half2;
     static constexpr int kVec = 8;
+    __device__ static __forceinline__ T2 from_bits(uint32_t w) { return *reinterpret_cast<const T2 *>(&w); }
+    __device__ static __forceinline__ float2 widen(T2 v) { return __half22float2(v); }
     __device__ static __forceinline__ float to_f32(T v) { return __half2float(v); }
     __device__ static __forceinline__ T from_f32(float v) { return __float2half_rn(v); }
 };
 
-// 8 elements from the 16-byte aligned p (valid: how many exist, the others read as 0)
-template <int DT> __device__ __forceinline__ void load8(const typename Elem<DT>::T *p, int valid, float (&v)[8])
+// 8 elements as they lie in memory
+template <int DT> struct Raw8 {
+    static constexpr int kPieces = 8 / Elem<DT>::kVec;
+    uint4 q[kPieces];
+};
+// from the 16-byte aligned p (valid: how many exist, the others read as 0)
+template <int DT> __device__ __forceinline__ void load_raw8(const typename Elem<DT>::T *p, int valid, Raw8<DT> &r)
 {
-    using E = Elem<DT>;
-    typename E::T t[8];
+    using T = typename Elem<DT>::T;
     if (valid >= 8) {
 #pragma unroll
-        for (int i = 0; i < 8 / E::kVec; ++i)
-            *reinterpret_cast<uint4 *>(t + i * E::kVec) = ld_stream16(p + i * E::kVec);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = E::to_f32(t[i]);
+        for (int i = 0; i < Raw8<DT>::kPieces; ++i) r.q[i] = ld_stream16(p + i * Elem<DT>::kVec);
     } else {
+        T t[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < valid ? E::to_f32(p[i]) : 0.f;
+        for (int i = 0; i < 8; ++i) t[i] = i < valid ? p[i] : Elem<DT>::from_f32(0.f);
+#pragma unroll
+        for (int i = 0; i < Raw8<DT>::kPieces; ++i) r.q[i] = *reinterpret_cast<const uint4 *>(t + i * Elem<DT>::kVec);
+    }
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// The 8 values, and the bits of the largest magnitude among the 32 of this lane and its three
+// neighbours (infinity and NaN on top).
+template <int DT> __device__ __forceinline__ uint32_t widen8(const Raw8<DT> &r, float (&v)[8])
+{
+    if constexpr (DT == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            v[4 * i] = __uint_as_float(r.q[i].x), v[4 * i + 1] = __uint_as_float(r.q[i].y);
+            v[4 * i + 2] = __uint_as_float(r.q[i].z), v[4 * i + 3] = __uint_as_float(r.q[i].w);
+        }
+        float m = fabsf(v[0]);
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = max_nan(m, fabsf(v[i]));
+        m = max_nan(m, __shfl_xor_sync(kFull, m, 1));
+        m = max_nan(m, __shfl_xor_sync(kFull, m, 2));
+        return __float_as_uint(m) & 0x7fffffffu;
+    } else {
+        // two at a time in the 16-bit type, where a maximum is as exact
+        using T2 = typename Elem<DT>::T2;
+        const uint32_t w[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
+        T2 m = Elem<DT>::from_bits(w[0] & 0x7fff7fffu);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) m = __hmax2_nan(m, Elem<DT>::from_bits(w[i] & 0x7fff7fffu));
+        m = __hmax2_nan(m, __shfl_xor_sync(kFull, m, 1));
+        m = __hmax2_nan(m, __shfl_xor_sync(kFull, m, 2));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = Elem<DT>::widen(Elem<DT>::from_bits(w[i]));
+            v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        }
+        const float2 f = Elem<DT>::widen(m);
+        return __float_as_uint(max_nan(f.x, f.y)) & 0x7fffffffu;
     }
 }
 
@@ -153,41 +208,51 @@ struct Mx4Walk {
     }
 };
 
+// CTAs an SM is to hold: the two sets of raw values of a lane are 32 registers, or 64 for fp32
+template <int DT> constexpr int mx4_quantize_ctas() { return DT == 0 ? 2 : 4; }
+
 // kVec: rows of x on 16-byte boundaries, a lane owns 8 consecutive elements (four lanes a block).
 // Otherwise element by element in lane order, 32 elements (one block) a warp-wide access: with a lane's
 // 8 elements read or written one by one, every access of the warp would touch all sectors of 256
 // elements (1413 f16 columns: dequantisation 20 us against 5).
-template <int DT, bool kVec> __global__ void __launch_bounds__(kMxThreads) mx4_quantize_kernel(const Mx4Rows a)
+template <int DT, bool kVec> __global__ void __launch_bounds__(kMxThreads, mx4_quantize_ctas<DT>()) mx4_quantize_kernel(const Mx4Rows a)
 {
     using T = typename Elem<DT>::T;
     const int lane = threadIdx.x % kWarp;
-    for (Mx4Walk w(a); w.row < a.rows; w.next()) {
+    pdl_wait();
+    pdl_launch_dependents();
+    Raw8<DT> raw[kMxGroups];
+    auto fetch = [&](const Mx4Walk &w) {
+        if (!kVec || w.row >= a.rows) return;
+        const T *x = reinterpret_cast<const T *>(a.x) + w.row * a.x_stride + w.seg * kMxSeg;
+        const int left = (int)min((long long)kMxSeg, a.cols - w.seg * kMxSeg);
+#pragma unroll
+        for (int g = 0; g < kMxGroups; ++g) load_raw8<DT>(x + g * (kWarp * 8) + lane * 8, left - g * (kWarp * 8) - lane * 8, raw[g]);
+    };
+    Mx4Walk w(a);
+    fetch(w);
+    while (w.row < a.rows) {
         const long long c0 = w.seg * kMxSeg;
         const int left = (int)min((long long)kMxSeg, a.cols - c0);          // elements of this segment
         const int padded = (left + kMxBlock - 1) / kMxBlock * kMxBlock;
         const T *x = reinterpret_cast<const T *>(a.x) + w.row * a.x_stride + c0;
         uint8_t *codes = a.codes + w.row * a.code_stride + c0 / 2, *scales = a.scales + w.row * a.scale_stride + c0 / kMxBlock;
+        w.next();
         if constexpr (kVec) {
-            float v[kMxGroups][8];
+            Raw8<DT> now[kMxGroups];
+#pragma unroll
+            for (int g = 0; g < kMxGroups; ++g) now[g] = raw[g];
+            fetch(w);
 #pragma unroll
             for (int g = 0; g < kMxGroups; ++g) {
                 const int c = g * (kWarp * 8) + lane * 8;
-                load8<DT>(x + c, left - c, v[g]);
-            }
-#pragma unroll
-            for (int g = 0; g < kMxGroups; ++g) {
-                const int c = g * (kWarp * 8) + lane * 8;
-                uint32_t m = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[g][i]) & 0x7fffffffu);
-                m = max(m, __shfl_xor_sync(kFull, m, 1));
-                m = max(m, __shfl_xor_sync(kFull, m, 2));
+                float v[8];
                 uint32_t byte;
-                const float inv = mx4_inverse_scale(m, byte);
+                const float inv = mx4_inverse_scale(widen8<DT>(now[g], v), byte);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[g][i] *= inv;
+                for (int i = 0; i < 8; ++i) v[i] *= inv;
                 if (c < padded) {
-                    *reinterpret_cast<uint32_t *>(codes + c / 2) = e2m1_pack8(v[g]);
+                    *reinterpret_cast<uint32_t *>(codes + c / 2) = e2m1_pack8(v);
                     if (lane % 4 == 0) scales[c / kMxBlock] = (uint8_t)byte;
                 }
             }
@@ -224,6 +289,8 @@ template <int DT, bool kVec> __global__ void __launch_bounds__(kMxThreads) mx4_d
 {
     using T = typename Elem<DT>::T;
     const int lane = threadIdx.x % kWarp;
+    pdl_wait();
+    pdl_launch_dependents();
     for (Mx4Walk w(a); w.row < a.rows; w.next()) {
         const long long c0 = w.seg * kMxSeg;
         const int left = (int)min((long long)kMxSeg, a.cols - c0);

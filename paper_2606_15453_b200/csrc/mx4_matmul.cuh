@@ -257,6 +257,8 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    pdl_wait();   // all that is read may be the kernel before's
+    pdl_launch_dependents();
     if (warp == 2) {  // group offsets; a count that is negative or leaves the rows of a is cut
         int off = 0, tiles = 0;
         if (lane == 0) s_off[0] = s_tile[0] = 0;

@@ -34,19 +34,43 @@ int lanes_per_row(int n_experts)
     while (l * 16 < n_experts) l *= 2;
     return l;
 }
-// per_sm: CTAs that fit an SM (the kernels' launch bounds).  Up to two steps of rows are left to one CTA,
-// which then needs no second launch to add partial sums up.
-int bal_grid(int64_t tokens, int lpr, int per_sm)
+// steps of rows that one CTA would take
+int64_t bal_steps(int64_t tokens, int lpr)
 {
     const int64_t rows = (int64_t)(kBalThreads / kWarp) * (kWarp / lpr) * kBalRows;
+    return (tokens + rows - 1) / rows;
+}
+// Up to kBalAlone steps are left to one CTA, which needs no second launch to add partial sums up.
+constexpr int64_t kBalAlone = 2;
+int bal_grid(int64_t tokens, int lpr)
+{
+    const int64_t steps = bal_steps(tokens, lpr);
+    if (steps <= kBalAlone) return 1;
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
         (void)cudaGetLastError();
         return 0;
     }
-    const int64_t steps = (tokens + rows - 1) / rows;
-    if (steps <= 2) return 1;
-    return (int)std::min<int64_t>({steps, (int64_t)sms * per_sm, kBalMaxCtas});
+    return (int)std::min<int64_t>({steps, (int64_t)sms * 3, kBalMaxCtas});   // three CTAs an SM (launch bounds)
+}
+
+// Launch that may start while the kernel before it in the stream drains (the kernels wait for it
+// themselves), in clusters of `cluster` CTAs.
+int launch_behind(void (*kernel)(BalanceArgs), int grid, int block, int smem, int cluster, cudaStream_t st, const BalanceArgs &a)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return STMOE_ERR_CUDA;
+    }
+    return STMOE_OK;
 }
 
 template <int DT, int LPR, int N, bool kVec> int launch_as(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
@@ -64,8 +88,7 @@ template <int DT, int LPR, int N, bool kVec> int launch_as(bool backward, const 
         }
         ready[dev][backward] = true;
     }
-    kernel<<<grid, kBalThreads, smem, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? STMOE_OK : STMOE_ERR_CUDA;
+    return launch_behind(kernel, grid, kBalThreads, smem, 1, st, a);
 }
 template <int DT, int LPR, int N> int launch(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {
@@ -92,9 +115,9 @@ int launch_typed(int dtype, int lpr, bool backward, const BalanceArgs &a, int gr
 
 extern "C" {
 
-size_t stmoe_router_balance_scratch_bytes(int n_experts)
+size_t stmoe_router_balance_scratch_bytes(int64_t tokens, int n_experts)
 {
-    if (n_experts < 1 || n_experts > kBalMaxExperts) return 0;
+    if (n_experts < 1 || n_experts > kBalMaxExperts || tokens < 1 || bal_steps(tokens, lanes_per_row(n_experts)) <= kBalAlone) return 0;
     return sizeof(float) * (size_t)kBalMaxCtas * bal_part_words(n_experts);
 }
 
@@ -102,10 +125,11 @@ int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const in
                          int n_experts, int top_k, float *loss, int32_t *counts, int32_t *rows, void *scratch,
                          size_t scratch_bytes, void *cuda_stream)
 {
-    if (!bal_args_ok(logits, dtype, stride, tokens, n_experts, top_k) || !ids || !loss || !counts || !rows || !scratch ||
-        ((uintptr_t)scratch & 3) || scratch_bytes < stmoe_router_balance_scratch_bytes(n_experts))
+    if (!bal_args_ok(logits, dtype, stride, tokens, n_experts, top_k) || !ids || !loss || !counts || !rows)
         return STMOE_ERR_BAD_ARG;
-    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, 3);
+    const size_t need = stmoe_router_balance_scratch_bytes(tokens, n_experts);
+    if (need && (!scratch || ((uintptr_t)scratch & 3) || scratch_bytes < need)) return STMOE_ERR_BAD_ARG;
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr);
     if (!grid) return STMOE_ERR_CUDA;
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.ids = ids, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
@@ -114,20 +138,7 @@ int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const in
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const int rc = launch_typed(dtype, lpr, false, a, grid, st);
     if (rc != STMOE_OK || grid == 1) return rc;
-    // may start while the first kernel drains; it waits for that kernel's results itself
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kBalFinish), cfg.blockDim = dim3(1024), cfg.stream = st;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = kBalFinish, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
-    cfg.attrs = at, cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, router_balance_finish_kernel, a) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return STMOE_ERR_CUDA;
-    }
-    return STMOE_OK;
+    return launch_behind(router_balance_finish_kernel, kBalFinish, 1024, 0, kBalFinish, st, a);
 }
 
 int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride, const uint8_t *mask, int64_t tokens,
@@ -139,7 +150,7 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
         return STMOE_ERR_BAD_ARG;
     if (tokens == 0) return STMOE_OK;
     if (overlap(logits, stride, grad_logits, grad_stride, tokens, n_experts, dtype)) return STMOE_ERR_BAD_ARG;
-    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, 3);
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr);
     if (!grid) return STMOE_ERR_CUDA;
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;

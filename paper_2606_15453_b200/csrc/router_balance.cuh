@@ -304,6 +304,8 @@ template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(k
     const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp, l = lane % LPR, sub = lane / LPR;
     for (int e = tid; e < a.E; e += kBalThreads) s_cnt[e] = 0;
     __syncthreads();
+    pdl_wait();
+    pdl_launch_dependents();
     float2 p[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) p[i] = make_float2(0.f, 0.f);
@@ -392,6 +394,7 @@ __global__ void __launch_bounds__(1024) router_balance_finish_kernel(const Balan
     const int tid = threadIdx.x, cols = a.E + 1, words = bal_part_words(a.E), rank = blockIdx.x;
     const int G = 1024 / cols, g = tid / cols, e = tid % cols;   // G >= 3: E <= 256
     pdl_wait();
+    pdl_launch_dependents();
     double v = 0.;
     int c = 0;
     if (g < G)
@@ -457,6 +460,8 @@ template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(k
     constexpr int RPW = kWarp / LPR, V = El::kVec;
     extern __shared__ __align__(16) uint8_t ring[];
     const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp, l = lane % LPR, sub = lane / LPR;
+    pdl_wait();
+    pdl_launch_dependents();
     BalWalk<DT, LPR, N, kVec, false> w(a, warp, sub, l, ring);
     const int n = *a.rows;
     const float rn = n > 0 ? 1.f / (float)n : 0.f;

@@ -56,7 +56,7 @@ def test_mx4_matmul_accepts_no_rows_and_refuses_more_tiles_than_an_index_holds()
 
 
 def _bal(**kw):
-    a = dict(z=X, dt=0, st=8, ids=X, mask=None, T=4, E=8, K=2, loss=X, counts=X, rows=X, scratch=X, n=1 << 24)
+    a = dict(z=X, dt=0, st=8, ids=X, mask=None, T=1 << 20, E=8, K=2, loss=X, counts=X, rows=X, scratch=X, n=1 << 24)
     a.update(kw)
     return P.lib().stmoe_router_balance(a["z"], a["dt"], a["st"], a["ids"], a["mask"], a["T"], a["E"], a["K"], a["loss"], a["counts"],
                                         a["rows"], a["scratch"], a["n"], None)
@@ -84,7 +84,8 @@ def test_router_balance_backward_refusals(kw):
 
 def test_scratch_sizes():
     f = P.lib().stmoe_router_balance_scratch_bytes
-    assert f(0) == 0 and f(257) == 0 and f(256) >= 2 * 257 * 4 * 148
+    assert f(1 << 20, 0) == 0 and f(1 << 20, 257) == 0 and f(1 << 20, 256) >= 2 * 257 * 4 * 148
+    assert f(0, 8) == 0 and f(16, 256) == 0           # one CTA alone
 
 
 def test_binding_refuses_before_the_library():
