@@ -73,12 +73,13 @@ int launch_behind(void (*kernel)(BalanceArgs), int grid, int block, int smem, in
     return STMOE_OK;
 }
 
-template <int DT, int LPR, int N, bool kVec> int launch_as(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+template <int DT, int LPR, int N, int kRead> int launch_as(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {
     // more than the default 48 KB of dynamic shared memory: asked for once per device
     static bool ready[64][2];
-    void (*kernel)(BalanceArgs) = backward ? router_balance_backward_kernel<DT, LPR, N, kVec> : router_balance_kernel<DT, LPR, N, kVec>;
-    const int smem = !kVec ? 0 : kBalDepth * (backward ? BalWalk<DT, LPR, N, kVec, false>::stage_bytes() : BalWalk<DT, LPR, N, kVec, true>::stage_bytes());
+    void (*kernel)(BalanceArgs) = backward ? router_balance_backward_kernel<DT, LPR, N, kRead> : router_balance_kernel<DT, LPR, N, kRead>;
+    const int stage = backward ? BalWalk<DT, LPR, N, kRead, false>::stage_bytes() : BalWalk<DT, LPR, N, kRead, true>::stage_bytes();
+    const int smem = kRead == kBalScalar ? 0 : kBalDepth * stage;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return STMOE_ERR_CUDA;
     if (smem && !ready[dev][backward]) {
@@ -92,7 +93,8 @@ template <int DT, int LPR, int N, bool kVec> int launch_as(bool backward, const 
 }
 template <int DT, int LPR, int N> int launch(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {
-    return a.vec ? launch_as<DT, LPR, N, true>(backward, a, grid, st) : launch_as<DT, LPR, N, false>(backward, a, grid, st);
+    if (!a.vec) return launch_as<DT, LPR, N, kBalScalar>(backward, a, grid, st);
+    return a.E == LPR * N ? launch_as<DT, LPR, N, kBalFull>(backward, a, grid, st) : launch_as<DT, LPR, N, kBalVec>(backward, a, grid, st);
 }
 template <int DT> int launch_lanes(int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
 {

@@ -171,68 +171,72 @@ template <int LPR, int P> __device__ __forceinline__ float bal_softmax(float2 (&
     return (m2 + __log2f(sum)) * kLn2;
 }
 
-// The rows of a lane, kBalRows a step.  With 16-byte rows (kVec) a lane's part of a row goes through
-// shared memory: every lane copies what it will read itself (cp.async, nothing to synchronise), two steps
-// ahead of the one it works on, so the loads' latency is hidden at no cost in registers.  Masks are asked
-// for one step before the copies that depend on them.  kIds: the lane's first choice of a row travels with it.
-template <int DT, int LPR, int N, bool kVec, bool kIds> struct BalWalk {
+// How rows are read: element by element; 16 bytes at a time; the same with no lane past the last expert
+// (n_experts = LPR * N), which needs no checks.
+constexpr int kBalScalar = 0, kBalVec = 1, kBalFull = 2;
+
+// The rows of a lane, kBalRows a step.  Where rows are read 16 bytes at a time a lane's part of a row goes
+// through shared memory: every lane copies what it will read itself (cp.async, nothing to synchronise),
+// two steps ahead of the one it works on, so the loads' latency is hidden at no cost in registers.  Masks
+// are asked for one step before the copies that depend on them.  kIds: the lane's first choice of a row
+// travels with it.
+template <int DT, int LPR, int N, int kRead, bool kIds> struct BalWalk {
     using T = typename Elem<DT>::T;
     static constexpr int RPW = kWarp / LPR, G = N * (int)sizeof(T) / 16;   // 16-byte pieces of a lane's part
-    long long t, step, t_ahead;      // row of the step in progress, rows between steps, row of the masks held
-    const T *z;                      // kVec: of the next copy; else of the step in progress
-    const uint8_t *mask;
+    static constexpr bool kRing = kRead != kBalScalar;
+    static constexpr uint32_t kBits = (1u << kBalRows) - 1;
+    uint32_t t, step, t_ahead;       // row of the step in progress, rows between steps, row of the masks held (T < 2^31)
+    const T *z;                      // kRing: of the next copy; else of the step in progress
     const int *ids;
     long long z_row, z_step, ids_step;
-    uint32_t on_hist;                // kBalRows bits a step: the steps under way, newest lowest
-    int l, slot;
-    uint8_t *ring;
+    uint32_t on_hist, next_on;       // kBalRows bits a step: the steps under way, newest lowest
+    uint32_t ring, slot;             // shared-memory address of this thread's pieces, byte offset of the next stage
 
     __host__ __device__ static constexpr int stage_bytes() { return kBalRows * (G * 16 + (kIds ? 4 : 0)) * kBalThreads; }
-    __device__ __forceinline__ uint32_t ask(const BalanceArgs &a, long long at) const
+    __device__ __forceinline__ uint32_t ask(const BalanceArgs &a, uint32_t at) const
     {
         uint32_t on = 0;
 #pragma unroll
         for (int r = 0; r < kBalRows; ++r)
-            if (at + r * RPW < a.T && (!a.mask || a.mask[at + r * RPW])) on |= 1u << r;
+            if (at + r * RPW < (uint32_t)a.T && (!a.mask || a.mask[at + r * RPW])) on |= 1u << r;
         return on;
     }
-    __device__ __forceinline__ void copy(const BalanceArgs &a, uint32_t on)
+    __device__ __forceinline__ uint32_t id_at(int r) const { return ring + kBalRows * G * 16 * kBalThreads - threadIdx.x * 12 + r * kBalThreads * 4; }
+    __device__ __forceinline__ void copy(const BalanceArgs &a, int l, uint32_t on)
     {
-        uint8_t *st = ring + slot * stage_bytes();
 #pragma unroll
         for (int r = 0; r < kBalRows; ++r)
             if (on >> r & 1) {
+                const T *row = z + r * z_row;
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const int e = bal_index<DT, LPR>(l, g * Elem<DT>::kVec, true);
-                    if (e < a.E)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(st + ((r * G + g) * kBalThreads + threadIdx.x) * 16)),
-                                     "l"(z + r * z_row + e) : "memory");
+                    if (kRead == kBalFull || e < a.E)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot + (r * G + g) * kBalThreads * 16), "l"(row + e) : "memory");
                 }
-                if (kIds && l < a.K)
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(st + kBalRows * G * 16 * kBalThreads + (r * kBalThreads + threadIdx.x) * 4)),
-                                 "l"(ids + r * RPW * a.K) : "memory");
+                if (kIds && l < a.K) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(id_at(r) + slot), "l"(ids + r * RPW * a.K) : "memory");
             }
         asm volatile("cp.async.commit_group;" ::: "memory");
         z += z_step;
         if (kIds) ids += ids_step;
-        if (++slot == kBalDepth) slot = 0;
+        slot = slot == (kBalDepth - 1) * stage_bytes() ? 0 : slot + stage_bytes();
     }
-    __device__ __forceinline__ BalWalk(const BalanceArgs &a, int warp, int sub, int l_, uint8_t *ring_) : l(l_), ring(ring_)
+    __device__ __forceinline__ BalWalk(const BalanceArgs &a, int warp, int sub, int l, uint8_t *smem)
     {
         constexpr int W = kBalThreads / kWarp;
-        step = (long long)gridDim.x * W * RPW * kBalRows;
-        t = (long long)(blockIdx.x * W + warp) * RPW * kBalRows + sub;
+        step = gridDim.x * W * RPW * kBalRows;
+        t = (blockIdx.x * W + warp) * RPW * kBalRows + sub;
         z_row = RPW * a.stride, z_step = step * a.stride;
         z = reinterpret_cast<const T *>(a.logits) + t * a.stride;
-        ids = kIds ? a.ids + t * a.K + l : nullptr, ids_step = step * a.K;
-        on_hist = 0, slot = 0;
-        if (kVec) {
+        ids = kIds ? a.ids + (long long)t * a.K + l : nullptr, ids_step = (long long)step * a.K;
+        ring = (uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * 16, slot = 0;
+        on_hist = 0;
+        if (kRing) {
             uint32_t on[kBalDepth];
 #pragma unroll
             for (int i = 0; i < kBalDepth; ++i) on[i] = ask(a, t + i * step);
 #pragma unroll
-            for (int i = 0; i < kBalDepth - 1; ++i) copy(a, on[i]), on_hist = on_hist << kBalRows | on[i];
+            for (int i = 0; i < kBalDepth - 1; ++i) copy(a, l, on[i]), on_hist = on_hist << kBalRows | on[i];
             on_hist = on_hist << kBalRows | on[kBalDepth - 1];   // its copy comes with the first step
             t_ahead = t + kBalDepth * step;
         } else {
@@ -240,45 +244,46 @@ template <int DT, int LPR, int N, bool kVec, bool kIds> struct BalWalk {
             t_ahead = t + step;
         }
     }
-    __device__ __forceinline__ bool more(const BalanceArgs &a, int sub) const { return t - sub < a.T; }
-    // The rows of the step in progress and the lane's first choices; bit r of the result: row r counts.
-    __device__ __forceinline__ uint32_t rows(const BalanceArgs &a, float2 (&v)[kBalRows][N / 2], int (&id)[kBalRows])
+    __device__ __forceinline__ bool more(const BalanceArgs &a, int sub) const { return t - sub < (uint32_t)a.T; }
+    // Begins a step; bit r of the result: row r counts.
+    __device__ __forceinline__ uint32_t begin(const BalanceArgs &a, int l)
     {
-        constexpr uint32_t kBits = (1u << kBalRows) - 1;
-        const uint32_t newest = on_hist & kBits, now = kVec ? on_hist >> (kBalRows * (kBalDepth - 1)) & kBits : newest;
-        const uint8_t *st = ring + (slot + 1 == kBalDepth ? 0 : slot + 1) * stage_bytes();   // oldest stage, once the newest is under way
-        if (kVec) copy(a, newest);
-        const uint32_t next = ask(a, t_ahead);
-        if (kVec) asm volatile("cp.async.wait_group %0;" ::"n"(kBalDepth - 1) : "memory");
+        const uint32_t newest = on_hist & kBits, now = kRing ? on_hist >> (kBalRows * (kBalDepth - 1)) & kBits : newest;
+        if (kRing) copy(a, l, newest);
+        next_on = ask(a, t_ahead);
+        if (kRing) asm volatile("cp.async.wait_group %0;" ::"n"(kBalDepth - 1) : "memory");
+        return now;
+    }
+    // Row r of the step, which counts, and the lane's first choice.
+    __device__ __forceinline__ void row(const BalanceArgs &a, int r, int l, float2 (&v)[N / 2], int &id) const
+    {
+        if constexpr (kRing) {   // the oldest stage, which the next copy will overwrite
 #pragma unroll
-        for (int r = 0; r < kBalRows; ++r) {
-            id[r] = -1;
-            if (!(now >> r & 1)) {
+            for (int g = 0; g < G; ++g) {
+                if (kRead == kBalFull || bal_index<DT, LPR>(l, g * Elem<DT>::kVec, true) < a.E) {
+                    uint4 q;
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(ring + slot + (r * G + g) * kBalThreads * 16));
+                    bal_widen<DT>(q, &v[g * N / 2 / G]);
+                } else {
 #pragma unroll
-                for (int i = 0; i < N / 2; ++i) v[r][i] = make_float2(-INFINITY, -INFINITY);
-            } else if constexpr (kVec) {
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    if (bal_index<DT, LPR>(l, g * Elem<DT>::kVec, true) < a.E) {
-                        bal_widen<DT>(*reinterpret_cast<const uint4 *>(st + ((r * G + g) * kBalThreads + threadIdx.x) * 16), &v[r][g * N / 2 / G]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < N / 2 / G; ++i) v[r][g * N / 2 / G + i] = make_float2(-INFINITY, -INFINITY);
-                    }
+                    for (int i = 0; i < N / 2 / G; ++i) v[g * N / 2 / G + i] = make_float2(-INFINITY, -INFINITY);
                 }
-                if (kIds && l < a.K) id[r] = *reinterpret_cast<const int *>(st + kBalRows * G * 16 * kBalThreads + (r * kBalThreads + threadIdx.x) * 4);
-            } else {
-                bal_load<DT, LPR, N>(z + r * z_row, a.E, l, v[r]);
-                if (kIds && l < a.K) id[r] = __ldg(ids + r * RPW * a.K);
             }
+            if (kIds && l < a.K) asm volatile("ld.shared.s32 %0, [%1];" : "=r"(id) : "r"(id_at(r) + slot));
+        } else {
+            bal_load<DT, LPR, N>(z + r * z_row, a.E, l, v);
+            if (kIds && l < a.K) id = __ldg(ids + r * RPW * a.K);
         }
-        if (!kVec) {
+    }
+    __device__ __forceinline__ void end()
+    {
+        if (!kRing) {
             z += z_step;
             if (kIds) ids += ids_step;
         }
-        on_hist = on_hist << kBalRows | next;
+        on_hist = on_hist << kBalRows | next_on;
         t += step, t_ahead += step;
-        return now;
     }
 };
 
@@ -292,7 +297,7 @@ __device__ __forceinline__ void bal_write(const BalanceArgs &a, double sum, doub
 }
 
 // One CTA's sums over its rows.  Alone (gridDim.x = 1) it writes the results, else its partial sums.
-template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(kBalThreads, 3) router_balance_kernel(const BalanceArgs a)
+template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(kBalThreads, 3) router_balance_kernel(const BalanceArgs a)
 {
     constexpr int W = kBalThreads / kWarp;
     extern __shared__ __align__(16) uint8_t ring[];
@@ -311,29 +316,35 @@ template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(k
     for (int i = 0; i < N / 2; ++i) p[i] = make_float2(0.f, 0.f);
     float zz = 0.f;
     int n = 0;
-    BalWalk<DT, LPR, N, kVec, true> w(a, warp, sub, l, ring);
+    BalWalk<DT, LPR, N, kRead, true> w(a, warp, sub, l, ring);
     while (w.more(a, sub)) {
-        float2 z[kBalRows][N / 2];
-        int id[kBalRows];
-        const long long t = w.t;
-        const uint32_t on = w.rows(a, z, id);
+        const uint32_t on = w.begin(a, l);
 #pragma unroll
         for (int r = 0; r < kBalRows; ++r) {
+            float2 z[N / 2];
+            int id = -1;
+            if (on >> r & 1) {
+                w.row(a, r, l, z, id);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) z[i] = make_float2(-INFINITY, -INFINITY);
+            }
             bool live;
             float inv;
-            const float lse = bal_softmax<LPR>(z[r], inv, live);
+            const float lse = bal_softmax<LPR>(z, inv, live);
             if ((on >> r & 1) && live) {
                 const float2 inv2 = make_float2(inv, inv);
 #pragma unroll
-                for (int i = 0; i < N / 2; ++i) p[i] = fma2(z[r][i], inv2, p[i]);
+                for (int i = 0; i < N / 2; ++i) p[i] = fma2(z[i], inv2, p[i]);
                 if (l == 0) zz = fmaf(lse, lse, zz), ++n;
-                if ((unsigned)id[r] < (unsigned)a.E) atomicAdd(&s_cnt[id[r]], 1);
+                if ((unsigned)id < (unsigned)a.E) atomicAdd(&s_cnt[id], 1);
                 for (int k = l + LPR; k < a.K; k += LPR) {
-                    const int e = __ldg(a.ids + (t + r * (kWarp / LPR)) * a.K + k);
+                    const int e = __ldg(a.ids + (long long)(w.t + r * (kWarp / LPR)) * a.K + k);
                     if ((unsigned)e < (unsigned)a.E) atomicAdd(&s_cnt[e], 1);
                 }
             }
         }
+        w.end();
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     // the rows of a warp first (lanes with the same l), then the warps in order
@@ -346,7 +357,7 @@ template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(k
     }
     if (sub == 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) s_p[warp][bal_index<DT, LPR>(l, i, kVec)] = i & 1 ? p[i / 2].y : p[i / 2].x;
+        for (int i = 0; i < N; ++i) s_p[warp][bal_index<DT, LPR>(l, i, kRead != kBalScalar)] = i & 1 ? p[i / 2].y : p[i / 2].x;
         if (l == 0) s_z[warp] = zz, s_n[warp] = n;
     }
     __syncthreads();
@@ -452,17 +463,18 @@ __global__ void __launch_bounds__(1024) router_balance_finish_kernel(const Balan
     }
 }
 
-// kVec: rows of the logits and of the gradient are both read and written 16 bytes at a time
-template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(kBalThreads, 3) router_balance_backward_kernel(const BalanceArgs a)
+// kRead: how rows of the logits are read and rows of the gradient written
+template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(kBalThreads, 3) router_balance_backward_kernel(const BalanceArgs a)
 {
     using El = Elem<DT>;
     using T = typename El::T;
     constexpr int RPW = kWarp / LPR, V = El::kVec;
+    constexpr bool kVec = kRead != kBalScalar;
     extern __shared__ __align__(16) uint8_t ring[];
     const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp, l = lane % LPR, sub = lane / LPR;
     pdl_wait();
     pdl_launch_dependents();
-    BalWalk<DT, LPR, N, kVec, false> w(a, warp, sub, l, ring);
+    BalWalk<DT, LPR, N, kRead, false> w(a, warp, sub, l, ring);
     const int n = *a.rows;
     const float rn = n > 0 ? 1.f / (float)n : 0.f;
     const float gb = a.grad[0] * (float)a.E * rn, gz = a.grad[1] * 2.f * rn;
@@ -475,39 +487,45 @@ template <int DT, int LPR, int N, bool kVec> __global__ void __launch_bounds__(k
     T *out = reinterpret_cast<T *>(a.dlogits) + w.t * a.dstride;
     const long long d_row = RPW * a.dstride, d_step = w.step * a.dstride;
     while (w.more(a, sub)) {
-        float2 z[kBalRows][N / 2];
-        int id[kBalRows];
-        const long long t = w.t;
-        const uint32_t on = w.rows(a, z, id);
+        const uint32_t on = w.begin(a, l);
 #pragma unroll
         for (int r = 0; r < kBalRows; ++r) {
+            float2 z[N / 2];
+            int id;
+            if (on >> r & 1) {
+                w.row(a, r, l, z, id);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) z[i] = make_float2(-INFINITY, -INFINITY);
+            }
             bool live;
             float inv;
-            const float lse = bal_softmax<LPR>(z[r], inv, live);
+            const float lse = bal_softmax<LPR>(z, inv, live);
             float2 d2 = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) d2 = fma2(f[i], z[r][i], d2);
+            for (int i = 0; i < N / 2; ++i) d2 = fma2(f[i], z[i], d2);
             const float dot = lanes_sum<LPR>(d2.x + d2.y);
             // dz = p (gb f + c), c = gz lse - gb dot, p = z inv; rows that do not count have z = 0
             float c = gz * lse - dot * inv;
             if (!(on >> r & 1) || !live) inv = 0.f, c = 0.f;
             const float2 inv2 = make_float2(inv, inv), c2 = make_float2(c * inv, c * inv);
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) z[r][i] = mul2(z[r][i], fma2(f[i], inv2, c2));
-            if (t + r * RPW >= a.T) continue;
+            for (int i = 0; i < N / 2; ++i) z[i] = mul2(z[i], fma2(f[i], inv2, c2));
+            if (w.t + r * RPW >= (uint32_t)a.T) continue;
             T *o = out + r * d_row;
             if constexpr (kVec) {
 #pragma unroll
                 for (int g = 0; g < N / V; ++g) {
                     const int e = bal_index<DT, LPR>(l, g * V, true);
-                    if (e < a.E) *reinterpret_cast<uint4 *>(o + e) = bal_narrow<DT>(&z[r][g * V / 2]);
+                    if (kRead == kBalFull || e < a.E) *reinterpret_cast<uint4 *>(o + e) = bal_narrow<DT>(&z[g * V / 2]);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    if (i * LPR + l < a.E) o[i * LPR + l] = El::from_f32(i & 1 ? z[r][i / 2].y : z[r][i / 2].x);
+                    if (i * LPR + l < a.E) o[i * LPR + l] = El::from_f32(i & 1 ? z[i / 2].y : z[i / 2].x);
             }
         }
+        w.end();
         out += d_step;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
