@@ -371,31 +371,31 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             if (a.splits == 1) {
                 using T = typename E::T;
                 T *out = reinterpret_cast<T *>(a.out) + (long long)t.tok0 * a.out_stride + (row - lane);
-                if (a.out_wide && row - lane + kWarp <= a.n) {
+                if (a.out_wide && t.row0 + kMmRows <= a.n) {
                     // A lane has one column of out for every token.  Stored like that, 192 tokens are 192
                     // two-byte stores of a warp (17000 cycles, twice the tile's MMAs); through shared memory
-                    // the warp's 32 columns of a token become whole 16-byte pieces.
-                    constexpr int kRow = kWarp * (int)sizeof(T), kLanes = kRow / 16, kTok = kMmStageOut / kRow;  // 64 or 128 bytes a token
-                    T *mine = reinterpret_cast<T *>(stage_out + lg * kMmStageOut);
-                    const int tk = lane / kLanes, piece = (lane % kLanes) * (16 / (int)sizeof(T));
-                    T *to = out + (long long)tk * a.out_stride + piece;
-                    const long long hop = (long long)(kWarp / kLanes) * a.out_stride;
+                    // the four warps' 128 columns of a token become whole lines.
+                    constexpr int kRow = kMmRows * (int)sizeof(T), kLanes = kRow / 16, kTok = 4 * kMmStageOut / kRow;  // 256 or 512 bytes a token
+                    T *tile = reinterpret_cast<T *>(stage_out);
+                    const int id = lg * kWarp + lane, tk = id / kLanes, piece = (id % kLanes) * (16 / (int)sizeof(T));
+                    constexpr int kHop = 4 * kWarp / kLanes;   // tokens that the four warps store at a time
+                    T *to = reinterpret_cast<T *>(a.out) + (long long)(t.tok0 + tk) * a.out_stride + t.row0 + piece;
                     for (int j0 = 0; j0 < t.count; j0 += kTok) {
 #pragma unroll
                         for (int h = 0; h < kTok; h += 16) {
                             float v[16];
                             tmem_ld16(acc + j0 + h, v);
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) mine[(h + j) * kWarp + lane] = E::from_f32(ok ? v[j] : __uint_as_float(0x7fffffffu));
+                            for (int j = 0; j < 16; ++j) tile[(h + j) * kMmRows + id] = E::from_f32(ok ? v[j] : __uint_as_float(0x7fffffffu));
                         }
-                        __syncwarp();
+                        asm volatile("bar.sync 2, 128;" ::: "memory");
 #pragma unroll
-                        for (int h = 0; h < kTok; h += kWarp / kLanes) {
+                        for (int h = 0; h < kTok; h += kHop) {
                             if (j0 + h + tk < t.count)
-                                *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(mine + (h + tk) * kWarp + piece);
-                            to += hop;
+                                *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(tile + (h + tk) * kMmRows + piece);
+                            to += kHop * a.out_stride;
                         }
-                        __syncwarp();
+                        asm volatile("bar.sync 2, 128;" ::: "memory");
                     }
                 } else {
                     T *to = out + lane;
