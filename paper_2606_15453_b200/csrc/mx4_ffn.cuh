@@ -42,6 +42,10 @@ constexpr int kMxfCols = kMxfTokens * kPlanes;
 constexpr int kMxfAccStride = 2 * kMxfCols;             // two accumulator buffers of (gate, up)
 constexpr int kMxfScaleCol = 2 * kMxfAccStride;
 constexpr int kMxfMaxStages = 12;
+// warps: 0 weights, 1 MMA, 2-5 and 6-9 epilogues (a group an accumulator buffer: with few reduction steps
+// a task, as in the down projection of narrow experts, one group was slower than the MMAs), 10-13 scales
+constexpr int kMxfThreads = 448;
+constexpr int kMxfScaleWarp = 10;
 
 // the B tile of a launch whose entries hold at most mt tokens: N is a multiple of 16
 __host__ __device__ constexpr int mxf_cols(int tokens) { return (tokens * kPlanes + 15) / 16 * 16; }
@@ -297,7 +301,7 @@ __device__ __forceinline__ void mxf_store_act(const Mx4FfnArgs &a, float g, floa
 }
 
 template <int NMAT>
-__global__ void __launch_bounds__(kMmThreads, 1)
+__global__ void __launch_bounds__(kMxfThreads, 1)
 mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1,
                const __grid_constant__ CUtensorMap map_s0, const __grid_constant__ CUtensorMap map_s1,
                const __grid_constant__ CUtensorMap map_x, const Mx4FfnArgs a)
@@ -419,32 +423,33 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             if (ok) umma_commit_if(leader, &tfull[ab]);
         }
         __syncwarp();
-    } else if (warp < 6) {
-        const int lg = warp % 4;
+    } else if (warp < kMxfScaleWarp) {
+        const int lg = warp % 4, ab = (warp - 2) / 4;   // quarter of the lanes, accumulator buffer
         float *part = reinterpret_cast<float *>(dsm);   // cluster: this rank's sums [mat][token][128], in the idle ring
-        int it = 0;
-        for (int task = first; task < n_tasks; task += step, ++it) {
-            const int ab = it & 1;
+        uint32_t use = 0;
+        for (int task = first + ab * step; task < n_tasks; task += 2 * step, ++use) {
             const Mx4FfnTask t = mxf_task<NMAT>(a, task);
             const Mx4Entry &en = a.entries[t.g];
             const int cnt = en.count, own = min(lane, kMxfTokens - 1);
             const int slot_l = en.slot[own];      // lane i: the i-th pair's, fetched while the MMAs run
             const float inv_l = en.inv[own];
-            const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], (uint32_t)(it >> 1) & 1u, dead));
+            const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], use & 1u, dead));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + ab * kMxfAccStride + ((uint32_t)(lg * kWarp) << 16);
             const int row = t.row0 + lg * kWarp + lane;
-            // two tokens at a time: their chains (loads, reductions, conversions) overlap
-            for (int i0 = 0; i0 < cnt; i0 += 2) {
-                uint32_t raw[2][NMAT][8];
-                float y[2][NMAT];
+            // a few tokens at a time: their chains (loads, sums, reductions, conversions) overlap
+            constexpr int kTok = NMAT == 1 ? 4 : 2;
+            const long long hop = (long long)a.splits * a.rows;
+            for (int i0 = 0; i0 < cnt; i0 += kTok) {
+                uint32_t raw[kTok][NMAT][8];
+                float y[kTok][NMAT];
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
+                for (int q = 0; q < kTok; ++q)
 #pragma unroll
                     for (int m = 0; m < NMAT; ++m) tmem_ld8_start(acc + m * kMxfCols + (i0 + q) * kPlanes, raw[q][m]);
                 tmem_ld_wait();
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
+                for (int q = 0; q < kTok; ++q)
 #pragma unroll
                     for (int m = 0; m < NMAT; ++m) {
                         y[q][m] = __uint_as_float(raw[q][m][7]);   // smallest plane first
@@ -452,23 +457,19 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                         for (int p = 6; p >= 0; --p) y[q][m] += __uint_as_float(raw[q][m][p]);
                         if (!ok) y[q][m] = __uint_as_float(0x7fffffffu);
                     }
-                const bool two = i0 + 1 < cnt;   // with an odd count the second has read columns nobody wrote
-                const int slot0 = __shfl_sync(kFull, slot_l, i0), slot1 = __shfl_sync(kFull, slot_l, i0 + 1);
-                if (NMAT == 1) {
-                    if (row < a.rows) {
-                        a.part[((long long)slot0 * a.splits + t.z) * a.rows + row] = y[0][0];
-                        if (two) a.part[((long long)slot1 * a.splits + t.z) * a.rows + row] = y[1][0];
-                    }
-                } else if (ranks > 1) {
+                // behind the last pair the columns hold what nobody wrote: not used
 #pragma unroll
-                    for (int m = 0; m < NMAT; ++m) {
-                        part[(m * kMxfTokens + i0) * kMmRows + lg * kWarp + lane] = y[0][m];
-                        if (two) part[(m * kMxfTokens + i0 + 1) * kMmRows + lg * kWarp + lane] = y[1][m];
+                for (int q = 0; q < kTok; ++q) {
+                    const int slot = __shfl_sync(kFull, slot_l, i0 + q);
+                    if (i0 + q >= cnt) break;
+                    if (NMAT == 1) {
+                        if (row < a.rows) a.part[slot * hop + (long long)t.z * a.rows + row] = y[q][0];
+                    } else if (ranks > 1) {
+#pragma unroll
+                        for (int m = 0; m < NMAT; ++m) part[(m * kMxfTokens + i0 + q) * kMmRows + lg * kWarp + lane] = y[q][m];
+                    } else if (t.row0 + lg * kWarp < a.rows) {   // rows are a multiple of 32: the whole warp or none of it
+                        mxf_store_act(a, y[q][0], y[q][NMAT - 1], slot, __shfl_sync(kFull, inv_l, i0 + q), row, lane);
                     }
-                } else if (t.row0 + lg * kWarp < a.rows) {   // rows are a multiple of 32: the whole warp or none of it
-                    const float inv0 = __shfl_sync(kFull, inv_l, i0), inv1 = __shfl_sync(kFull, inv_l, i0 + 1);
-                    mxf_store_act(a, y[0][0], y[0][NMAT - 1], slot0, inv0, row, lane);
-                    if (two) mxf_store_act(a, y[1][0], y[1][NMAT - 1], slot1, inv1, row, lane);
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -480,7 +481,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         // scales and the tokens' codes, a warp every fourth stage (see mx4_matmul.cuh; up to twelve loads a
         // stage by one thread would hold the weights' back).  A task's steps may differ by one between
         // splits, so the position is walked, not computed
-        const int w = warp - 6;
+        const int w = warp - kMxfScaleWarp;
         const int x_align = a.blocks % 8 == 0 ? 8 : a.blocks % 4 == 0 ? 4 : 1;
         // what a warp knows of the task its next step belongs to, and of the one after (asked for at the
         // start of this one)
@@ -588,7 +589,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         const int cnt = en.count;
         const uint32_t part = dsmem_u32(dsm);
         // (token, 32 rows) units, dealt to the ranks and their warps
-        for (int u = rank + ranks * warp; u < cnt * 4; u += ranks * (kMmThreads / kWarp)) {
+        for (int u = rank + ranks * warp; u < cnt * 4; u += ranks * (kMxfThreads / kWarp)) {
             const int i = u / 4, r0 = (u % 4) * kWarp;
             if (t.row0 + r0 >= a.rows) continue;
             const int slot_i = en.slot[i];

@@ -463,7 +463,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
     g.last_task = gu_tasks - 1;
     // fewer tiles than SMs: a cluster shares a tile's reduction
     g.splits = std::max(1, std::min({sms / gu_tasks, gu_steps, kMmMaxSplits}));
-    ST_TRY(mx4_launch(mx4_ffn_kernel<2>, g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMmThreads, kMmSmemBytes,
+    ST_TRY(mx4_launch(mx4_ffn_kernel<2>, g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMxfThreads, kMmSmemBytes,
                       g.splits, st, maps.gate[0], maps.up[0], maps.gate[1], maps.up[1], maps.x, g));
 
     ST_TRY(mark(1));
@@ -480,7 +480,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
         if (t < best) best = t, d.splits = z;
     }
     d.last_task = d_tiles * d.splits - 1;
-    ST_TRY(mx4_launch(mx4_ffn_kernel<1>, std::min(d_tiles * d.splits, sms), kMmThreads, kMmSmemBytes, 1, st, maps.down[0],
+    ST_TRY(mx4_launch(mx4_ffn_kernel<1>, std::min(d_tiles * d.splits, sms), kMxfThreads, kMmSmemBytes, 1, st, maps.down[0],
                       maps.down[0], maps.down[1], maps.down[1], maps.act, d));
 
     fa.part = b.part, fa.S = d.splits;
