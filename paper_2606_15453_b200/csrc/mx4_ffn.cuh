@@ -341,11 +341,12 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
     const int ranks = NMAT == 2 ? a.splits : 1;   // CTAs of a cluster that share a task's reduction
     const int tiles = (a.rows + kMmRows - 1) / kMmRows;
     const int n_tasks = *a.n_entries * tiles * (NMAT == 1 ? a.splits : 1);
+    const int per_entry = tiles * (NMAT == 1 ? a.splits : 1);
     const int rank = blockIdx.x % ranks, first = blockIdx.x / ranks, step = gridDim.x / ranks;
     const int n_steps = (a.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
     auto k_range = [&](int z, int &beg, int &end) {
         const int q = NMAT == 2 ? rank : z;
-        beg = (int)((long long)n_steps * q / a.splits), end = (int)((long long)n_steps * (q + 1) / a.splits);
+        beg = n_steps * q / a.splits, end = n_steps * (q + 1) / a.splits;   // at most 2^20 steps, 8 splits
     };
 
     if (warp == 0) {
@@ -353,13 +354,19 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         // behind it (measured: 10 us on the gate/up kernel at 64 sequences)
         asm volatile("bar.sync 1, 160;" ::: "memory");
         if (elect_one()) {
-            int s = 0, issued = 0;
+            int s = 0, issued = 0, img_next = 0;
+            bool shared_next = false;
             uint32_t par = 0;
+            auto fetch = [&](int task) {   // a task's entry is asked for one task ahead
+                const Mx4Entry &en = a.entries[min(task, a.last_task) / per_entry];
+                img_next = en.img_index, shared_next = en.shared != 0;
+            };
+            fetch(first);
             for (int task = first; task < n_tasks && !*dead; task += step) {
                 const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-                const Mx4Entry &en = a.entries[t.g];
-                const int img = en.img_index;
-                const bool shared = en.shared != 0;
+                const int img = img_next;
+                const bool shared = shared_next;
+                fetch(task + step);
                 const CUtensorMap *w0 = shared ? &map_s0 : &map_w0, *w1 = shared ? &map_s1 : &map_w1;
                 int k_beg, k_end;
                 k_range(t.z, k_beg, k_end);
@@ -388,9 +395,11 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         int s = 0, it = 0;
         uint32_t par = 0;
         bool ok = true;
+        int count = a.entries[min(first, a.last_task) / per_entry].count;
         for (int task = first; task < n_tasks && ok; task += step, ++it) {
             const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-            const int n = mxf_cols(a.entries[t.g].count);
+            const int n = mxf_cols(count);
+            count = a.entries[min(task + step, a.last_task) / per_entry].count;   // the next task's
             const uint32_t id0 = umma_idesc_mxf4(n, 0), id1 = umma_idesc_mxf4(n, 1);
             const int ab = it & 1;
             if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)))) break;
@@ -494,7 +503,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             Info in, ahead;
         };
         auto ask = [&](int task) {
-            const Mx4Entry &en = a.entries[min(task, a.last_task) / (tiles * (NMAT == 1 ? a.splits : 1))];
+            const Mx4Entry &en = a.entries[min(task, a.last_task) / per_entry];
             const int own = min(lane, kMxfTokens - 1);
             return Info{en.img, en.count, NMAT == 2 ? en.token[own] : en.slot[own]};
         };
