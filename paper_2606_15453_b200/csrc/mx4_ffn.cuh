@@ -623,36 +623,52 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
 
 // h_out[b][c] = h[b][c] + r * (weighted sum of the down projection's partial sums), in a fixed order:
 // shared experts, then routed ones, splits innermost.  ids (stand-alone call): a pair whose id names
-// no expert has no partial sums and adds nothing.
+// no expert has no partial sums and adds nothing; what lies in its place is read and dropped, so that no
+// load waits for another.
+template <int S> __device__ __forceinline__ float mx4_combine_sum(const FfnArgs &a, const int32_t *ids, int b, int c)
+{
+    constexpr int Q = S >= 8 ? 1 : 8 / S;   // slots whose loads are under way together
+    const int KS = a.K + a.n_shared;
+    const float *part = a.part + (long long)b * KS * S * a.H + c;
+    float y = 0.f;
+    for (int q0 = 0; q0 < KS; q0 += Q) {
+        float v[Q][S], w[Q];
+        bool in[Q];
+#pragma unroll
+        for (int j = 0; j < Q; ++j) {
+            const int q = min(q0 + j, KS - 1), k = q < a.n_shared ? a.K + q : q - a.n_shared;
+            in[j] = q0 + j < KS && !(ids && (unsigned)__ldg(ids + b * a.K + k) >= (unsigned)a.E);
+            w[j] = q < a.n_shared ? 1.f : __ldg(a.w + b * a.K + k);
+#pragma unroll
+            for (int z = 0; z < S; ++z) v[j][z] = __ldcg(part + (long long)(k * S + z) * a.H);
+        }
+#pragma unroll
+        for (int j = 0; j < Q; ++j) {
+            float p = v[j][0];
+#pragma unroll
+            for (int z = 1; z < S; ++z) p += v[j][z];
+            if (in[j]) y = fmaf(w[j], p, y);
+        }
+    }
+    return y;
+}
 __global__ void __launch_bounds__(256) mx4_combine_kernel(const FfnArgs a, const int32_t *ids)
 {
     pdl_launch_dependents();
     pdl_wait();
-    const int KS = a.K + a.n_shared;
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < a.B * a.H; i += gridDim.x * blockDim.x) {
         const int b = i / a.H, c = i % a.H;
         const float h = a.h[i];
-        float y = 0.f, p = 0.f;
-        const int terms = KS * a.S;
-        for (int t0 = 0; t0 < terms; t0 += 8) {   // eight terms' loads together (each is a trip to L2)
-            float v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int t = t0 + j, q = t / a.S, k = q < a.n_shared ? a.K + q : q - a.n_shared;
-                v[j] = t < terms && !(ids && (unsigned)ids[b * a.K + k] >= (unsigned)a.E)
-                           ? __ldcg(a.part + ((long long)(b * KS + k) * a.S + (t - q * a.S)) * a.H + c) : 0.f;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int t = t0 + j, q = t / a.S;
-                if (t < terms) {
-                    p += v[j];
-                    if (t - q * a.S == a.S - 1) {
-                        y = q < a.n_shared ? y + p : fmaf(a.w[b * a.K + q - a.n_shared], p, y);
-                        p = 0.f;
-                    }
-                }
-            }
+        float y;
+        switch (a.S) {
+        case 1: y = mx4_combine_sum<1>(a, ids, b, c); break;
+        case 2: y = mx4_combine_sum<2>(a, ids, b, c); break;
+        case 3: y = mx4_combine_sum<3>(a, ids, b, c); break;
+        case 4: y = mx4_combine_sum<4>(a, ids, b, c); break;
+        case 5: y = mx4_combine_sum<5>(a, ids, b, c); break;
+        case 6: y = mx4_combine_sum<6>(a, ids, b, c); break;
+        case 7: y = mx4_combine_sum<7>(a, ids, b, c); break;
+        default: y = mx4_combine_sum<8>(a, ids, b, c); break;
         }
         a.h_out[i] = fmaf(a.residual_scale, y, h);
     }
