@@ -127,14 +127,28 @@ int encode_codes(EncodeTiledFn fn, CUtensorMap *m, const uint8_t *base, int64_t 
                : STMOE_ERR_CUDA;
 }
 
-template <int ODT>
-int launch_matmul(const CUtensorMap &ma, const CUtensorMap &mb, const Mx4MatmulArgs &a, int grid, int dev, cudaStream_t st)
+// once per device (a racing fill writes the same values): the kernels' shared memory, and how many of
+// their clusters run at a time (the same for the three output types)
+int matmul_clusters(int dev, MmClusters *c)
 {
+    static MmClusters kept[kMaxDevices];
     static bool ready[kMaxDevices];
     if (!ready[dev]) {
-        CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<ODT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        MmClusters m;
+        if (!mm_clusters(mx4_matmul_kernel<0>, kMmThreads, &m)) return STMOE_ERR_CUDA;
+        kept[dev] = m;
         ready[dev] = true;
     }
+    *c = kept[dev];
+    return STMOE_OK;
+}
+
+template <int ODT>
+int launch_matmul(const CUtensorMap &ma, const CUtensorMap &mb, const Mx4MatmulArgs &a, int grid, cudaStream_t st)
+{
     return launch_behind(mx4_matmul_kernel<ODT>, grid, kMmThreads, kMmSmemBytes, a.splits, st, ma, mb, a);
 }
 
@@ -192,9 +206,10 @@ int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_
     const int64_t tasks = row_tiles * tok_tiles;
     if (tasks > INT32_MAX - 4096) return STMOE_ERR_TOO_LARGE;
     const int steps = (k_blocks + kMmStageBlocks - 1) / kMmStageBlocks;
-    // too few tiles for the SMs: split the reduction over a cluster
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({sms / std::max<int64_t>(tasks, 1), steps, kMmMaxSplits}));
-    if (a.bn > 64) a.splits = 1;
+    MmClusters clusters;
+    const int rc = matmul_clusters(dev, &clusters);
+    if (rc != STMOE_OK) return rc;
+    a.splits = mm_splits(tasks, steps, clusters);   // too few tiles for the SMs: a cluster shares a tile's reduction
     const int grid = a.splits > 1 ? (int)tasks * a.splits : (int)std::min<int64_t>(tasks, sms);
 
     CUtensorMap ma, mb;
@@ -204,9 +219,9 @@ int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_
         encode_codes(fn, &mb, b_codes, b_rows, row_bytes, b_rows > 1 ? b_code_stride : row_bytes, kMmRows) != STMOE_OK)
         return STMOE_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (out_dtype == STMOE_F32) return launch_matmul<0>(ma, mb, a, grid, dev, st);
-    if (out_dtype == STMOE_BF16) return launch_matmul<1>(ma, mb, a, grid, dev, st);
-    return launch_matmul<4>(ma, mb, a, grid, dev, st);
+    if (out_dtype == STMOE_F32) return launch_matmul<0>(ma, mb, a, grid, st);
+    if (out_dtype == STMOE_BF16) return launch_matmul<1>(ma, mb, a, grid, st);
+    return launch_matmul<4>(ma, mb, a, grid, st);
 }
 
 }  // extern "C"

@@ -603,11 +603,17 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             if (t.row0 + r0 >= a.rows) continue;
             const int slot_i = en.slot[i];
             const float inv_i = en.inv[i];
-            float g = 0.f, v = 0.f;
-            for (int z = 0; z < ranks; ++z) {
-                g += ld_cluster(part + (uint32_t)(i * kMmRows + r0 + lane) * 4, z);
-                v += ld_cluster(part + (uint32_t)((kMxfTokens + i) * kMmRows + r0 + lane) * 4, z);
-            }
+            float gz[kMmMaxSplits], vz[kMmMaxSplits];   // the ranks' loads are under way together
+#pragma unroll
+            for (int z = 0; z < kMmMaxSplits; ++z)
+                if (z < ranks) {
+                    gz[z] = ld_cluster(part + (uint32_t)(i * kMmRows + r0 + lane) * 4, z);
+                    vz[z] = ld_cluster(part + (uint32_t)((kMxfTokens + i) * kMmRows + r0 + lane) * 4, z);
+                }
+            float g = gz[0], v = vz[0];
+#pragma unroll
+            for (int z = 1; z < kMmMaxSplits; ++z)
+                if (z < ranks) g += gz[z], v += vz[z];
             mxf_store_act(a, g, v, slot_i, inv_i, t.row0 + r0 + lane, lane);
         }
         cluster_sync();

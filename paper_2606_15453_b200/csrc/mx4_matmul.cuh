@@ -221,13 +221,58 @@ __device__ __forceinline__ Mx4Task mm_task(const Mx4MatmulArgs &a, const int *s_
     return k;
 }
 
+// the float4 (or float) at this CTA's shared-memory address, read from CTA `rank` of the cluster
+__device__ __forceinline__ float4 ld_cluster4(uint32_t smem, int rank)
+{
+    uint32_t remote;
+    float4 v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote));
+    return v;
+}
 __device__ __forceinline__ float ld_cluster(uint32_t smem, int rank)
 {
     uint32_t remote;
     float v;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote));
     return v;
+}
+// How many clusters of 2, 4 and 8 CTAs of a kernel run at a time: fewer than the SMs would suggest, as a
+// cluster has to fit one of the GPU's processor clusters.
+struct MmClusters {
+    int fit[3];
+};
+template <typename... P> inline bool mm_clusters(void (*kernel)(P...), int threads, MmClusters *c)
+{
+    for (int i = 0; i < 3; ++i) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = 2u << i, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3(2u << i), cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = kMmSmemBytes;
+        cfg.attrs = at, cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&c->fit[i], kernel, &cfg) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return false;
+        }
+    }
+    return true;
+}
+// Splits of a reduction of `steps` stages over a cluster, for `tasks` tiles: a power of two whose clusters
+// all run at once, as long as the stages saved (0.26 us each, latency) outweigh the exchange (about
+// 1 us).  Measured at 5 x 2816 outputs: reduction 2048 (8 stages) 6.1 us unsplit, 5.3 by 4; 16 x 512,
+// reduction 14336: 17.3 and 7.0 by 8; 60 x 2048, reduction 2048, 16 clusters of 8 in two rounds: 6.6 and 12.4.
+inline int mm_splits(int64_t tasks, int steps, const MmClusters &c)
+{
+    int best = 1;
+    float cost = 0.26f * steps;
+    for (int i = 0; i < 3; ++i) {
+        const int z = 2 << i;
+        const float t = 0.26f * ((steps + z - 1) / z) + 1.f;
+        if (z <= steps && tasks <= c.fit[i] && t < cost) cost = t, best = z;
+    }
+    return best;
 }
 
 template <int ODT>
@@ -472,12 +517,30 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         cluster_sync();
         const Mx4Task t = mm_task(a, s_off, s_tile, first);
         const uint32_t part = dsmem_u32(dsm);
-        for (int i = tid; i < kMmRows * bn; i += kMmThreads) {
-            const int j = i / kMmRows, row = t.row0 + i % kMmRows;
-            if (j % a.splits != rank || j >= t.count || row >= a.n) continue;
-            float y = 0.f;
-            for (int z = 0; z < a.splits; ++z) y += ld_cluster(part + (uint32_t)i * 4, z);
-            reinterpret_cast<typename E::T *>(a.out)[(long long)(t.tok0 + j) * a.out_stride + row] = E::from_f32(y);
+        // a warp a token, four rows a lane; the ranks' loads are under way together
+        using T = typename E::T;
+        const int row = t.row0 + 4 * lane;
+        for (int j = rank + a.splits * warp; j < t.count; j += a.splits * (kMmThreads / kWarp)) {
+            float4 v[kMmMaxSplits];
+#pragma unroll
+            for (int z = 0; z < kMmMaxSplits; ++z)
+                if (z < a.splits) v[z] = ld_cluster4(part + (uint32_t)(j * kMmRows + 4 * lane) * 4, z);
+            float y[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+            for (int z = 1; z < kMmMaxSplits; ++z)
+                if (z < a.splits) y[0] += v[z].x, y[1] += v[z].y, y[2] += v[z].z, y[3] += v[z].w;
+            T *to = reinterpret_cast<T *>(a.out) + (long long)(t.tok0 + j) * a.out_stride + row;
+            T q[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) q[r] = E::from_f32(y[r]);
+            if (a.out_wide && row + 4 <= a.n) {
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(q);
+                else *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(q);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (row + r < a.n) to[r] = q[r];
+            }
         }
         cluster_sync();  // nobody leaves while its partial tile is read
     }

@@ -423,24 +423,38 @@ int mx4_launch(void (*kernel)(P...), int grid, int block, size_t smem, int clust
     CU_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     return STMOE_OK;
 }
-int mx4_prepare_kernels(int dev)
+// what a call has to know of its device, found out once per device ordinal (a racing fill writes the
+// same values): the kernels' shared memory is asked for on the way
+struct Mx4Device {
+    int sms;
+    MmClusters clusters;
+};
+int mx4_device(int dev, Mx4Device *d)
 {
+    static Mx4Device kept[64];
     static bool ready[64];
     if (dev < 0 || dev >= 64) return STMOE_ERR_BAD_ARG;
     if (!ready[dev]) {
         CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
         CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        Mx4Device m;
+        m.sms = sm_count();
+        if (!mm_clusters(mx4_ffn_kernel<2>, kMxfThreads, &m.clusters)) return STMOE_ERR_CUDA;
+        kept[dev] = m;
         ready[dev] = true;
     }
+    *d = kept[dev];
     return STMOE_OK;
 }
 
-// The FFN of one layer step; pa: empty, or with the ids of the stand-alone call; fa: inputs, outputs and work list as for the other formats; mark(i): called before the first
-// launch, between the projections and behind the last launch.
+// The FFN of one layer step; pa: empty, or with the ids of the stand-alone call; fa: inputs, outputs and
+// work list as for the other formats; mark(i): called before the first launch, between the projections
+// and behind the last launch.
 template <typename Mark>
-int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnArgs fa, size_t img_bytes, unsigned *err, int sms,
-            cudaStream_t st, Mark mark)
+int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnArgs fa, size_t img_bytes, unsigned *err,
+            const Mx4Device &dev, cudaStream_t st, Mark mark)
 {
+    const int sms = dev.sms;
     ST_TRY(mark(0));
     const int H = fa.H, I = fa.I, pairs = fa.B * (fa.K + fa.n_shared), mt = mx4_entry_tokens(fa.B);
     pa.h = fa.h, pa.inv_rms = fa.inv_rms, pa.B = fa.B, pa.H = H, pa.codes = b.x_codes, pa.scales = b.x_scales;
@@ -461,8 +475,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
     const int gu_steps = (g.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
     const int gu_tasks = entries * ((I + kMmRows - 1) / kMmRows);
     g.last_task = gu_tasks - 1;
-    // fewer tiles than SMs: a cluster shares a tile's reduction
-    g.splits = std::max(1, std::min({sms / gu_tasks, gu_steps, kMmMaxSplits}));
+    g.splits = mm_splits(gu_tasks, gu_steps, dev.clusters);   // fewer tiles than SMs: a cluster shares a tile's reduction
     ST_TRY(mx4_launch(mx4_ffn_kernel<2>, g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMxfThreads, kMmSmemBytes,
                       g.splits, st, maps.gate[0], maps.up[0], maps.gate[1], maps.up[1], maps.x, g));
 
@@ -567,6 +580,7 @@ struct stmoe {
     Mx4FfnMaps mx4_maps{};          // MX4 stacks (mx4_ffn.cuh)
     Mx4FfnBufs mx4{};
     uint8_t *d_mx4 = nullptr;       // the buffers behind mx4
+    Mx4Device mx4_dev{};
     float *d_host_io = nullptr;     // stmoe_decode_token_host: [2][max_batch][H] staging of h_in / h_out
     int32_t *d_host_ids = nullptr;  // and [L][max_batch][K] of the routed ids
     bool dense_persistent = false;  // one cooperative kernel per decode step (token_dense_kernel.cuh)
@@ -1114,7 +1128,7 @@ int mx4_layer_ffn(stmoe *s, const FfnArgs &fa, cudaStream_t st)
     cudaEvent_t e[3] = {};
     if (s->time_kernels)
         for (cudaEvent_t &x : e) ST_TRY(get_event(s, &x));
-    ST_TRY(mx4_ffn(s->mx4_maps, s->mx4, Mx4PlanesArgs{}, fa, s->img_bytes, s->d_err, s->persistent_grid, st, [&](int i) {
+    ST_TRY(mx4_ffn(s->mx4_maps, s->mx4, Mx4PlanesArgs{}, fa, s->img_bytes, s->d_err, s->mx4_dev, st, [&](int i) {
         if (e[i]) CU_TRY(cudaEventRecord(e[i], st));
         return STMOE_OK;
     }));
@@ -1561,7 +1575,7 @@ int stmoe_create(const stmoe_config_t *cfg, stmoe_t **out)
         const int pairs = B * s->KS;
         int dev = 0;
         CR_TRY(cudaGetDevice(&dev));
-        int rc = mx4_prepare_kernels(dev);
+        int rc = mx4_device(dev, &s->mx4_dev);
         if (rc != STMOE_OK) return fail(rc);
         CR_TRY(cudaMalloc(&s->d_mx4, mx4_buffers(nullptr, B, pairs, H, I, &s->mx4)));
         mx4_buffers(s->d_mx4, B, pairs, H, I, &s->mx4);
@@ -1578,7 +1592,6 @@ int stmoe_create(const stmoe_config_t *cfg, stmoe_t **out)
             Mx4FfnMaps &m = s->mx4_maps;
             m.gate[1] = m.gate[0], m.up[1] = m.up[0], m.down[1] = m.down[0], m.store[1] = m.store[0];
         }
-        s->persistent_grid = sm_count();
     }
     if (c.cache_slots == 0 && c.weight_dtype != STMOE_MX4 && !(c.flags & STMOE_FLAG_NO_PERSISTENT)) {
         int dev = 0, coop = 0;
@@ -2129,11 +2142,10 @@ int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const 
 {
     if (!mx4_ffn_args_ok(experts, hidden, inter) || scratch_bytes < stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter))
         return STMOE_ERR_BAD_ARG;
-    static int sms[64];   // per device ordinal; a racing fill writes the same value
     int dev = 0;
     CU_TRY(cudaGetDevice(&dev));
-    ST_TRY(mx4_prepare_kernels(dev));
-    if (!sms[dev]) sms[dev] = sm_count();
+    Mx4Device on;
+    ST_TRY(mx4_device(dev, &on));
     const size_t img = image_bytes(hidden, inter, STMOE_MX4);
     Mx4FfnBufs b;
     mx4_buffers((uint8_t *)scratch, batch, batch * top_k, hidden, inter, &b);
@@ -2147,7 +2159,7 @@ int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const 
     fa.h = h, fa.inv_rms = inv_rms;
     fa.H = hidden, fa.I = inter, fa.E = n_experts, fa.w = w, fa.h_out = h_out;
     fa.B = batch, fa.K = top_k, fa.n_shared = 0, fa.residual_scale = residual_scale;
-    return mx4_ffn(maps, b, pa, fa, img, nullptr, sms[dev], st, [](int) { return STMOE_OK; });
+    return mx4_ffn(maps, b, pa, fa, img, nullptr, on, st, [](int) { return STMOE_OK; });
 }
 
 }  // namespace
