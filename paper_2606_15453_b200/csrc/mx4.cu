@@ -62,13 +62,17 @@ int launch_behind(void (*kernel)(P...), int grid, int block, int smem, int clust
     return STMOE_OK;
 }
 
-template <int DT> int launch_rows(bool quantize, const Mx4Rows &a, int64_t warps, int sms, cudaStream_t st)
+template <int DT, bool kVec, bool kPack> int launch_rows_as(bool quantize, const Mx4Rows &a, int64_t warps, int sms, cudaStream_t st)
 {
     const int64_t ctas = (warps + kMxThreads / kWarp - 1) / (kMxThreads / kWarp);
-    const int grid = (int)std::min<int64_t>(ctas, (int64_t)sms * (quantize ? mx4_quantize_ctas<DT>() : 8));
-    if (quantize)
-        return launch_behind(a.vec ? mx4_quantize_kernel<DT, true> : mx4_quantize_kernel<DT, false>, grid, kMxThreads, 0, 1, st, a);
-    return launch_behind(a.vec ? mx4_dequantize_kernel<DT, true> : mx4_dequantize_kernel<DT, false>, grid, kMxThreads, 0, 1, st, a);
+    const int grid = (int)std::min<int64_t>(ctas, (int64_t)sms * (quantize ? mx4_quantize_ctas<DT, kVec>() : 8));
+    return launch_behind(quantize ? mx4_quantize_kernel<DT, kVec, kPack> : mx4_dequantize_kernel<DT, kVec, kPack>, grid, kMxThreads, 0, 1, st, a);
+}
+template <int DT> int launch_rows(bool quantize, const Mx4Rows &a, int64_t warps, int sms, cudaStream_t st)
+{
+    if (a.vec)
+        return a.pack > 1 ? launch_rows_as<DT, true, true>(quantize, a, warps, sms, st) : launch_rows_as<DT, true, false>(quantize, a, warps, sms, st);
+    return a.pack > 1 ? launch_rows_as<DT, false, true>(quantize, a, warps, sms, st) : launch_rows_as<DT, false, false>(quantize, a, warps, sms, st);
 }
 
 int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int64_t x_stride, uint8_t *codes,
@@ -91,7 +95,9 @@ int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int6
     if (rows > 1 && cols % kMxBlock == 0 && x_stride == cols && code_stride == nb * 16 && scale_stride == nb)
         a.rows = 1, a.cols = rows * cols;
     a.vec = ((uintptr_t)x & 15) == 0 && (a.rows == 1 || (x_stride * elem_bytes(dtype)) % 16 == 0);
-    const int64_t tasks = a.rows * ((a.cols - 1) / kMxSeg + 1);
+    const int64_t padded = (a.cols + kMxBlock - 1) / kMxBlock * kMxBlock;
+    a.pack = padded <= kMxSeg / 2 ? (int)(kMxSeg / padded) : 1;
+    const int64_t tasks = (a.rows + a.pack - 1) / a.pack * ((a.cols - 1) / kMxSeg + 1);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (dtype == STMOE_F32) return launch_rows<0>(quantize, a, tasks, sms, st);
     if (dtype == STMOE_BF16) return launch_rows<1>(quantize, a, tasks, sms, st);

@@ -11,7 +11,7 @@
 //
 // Both directions are bound by HBM: one pass, 16-byte loads of the wide side, 4-byte accesses of
 // the codes.  A lane owns 8 consecutive elements of a block, so the block maximum is two shuffles;
-// a warp takes 1024 elements of a row at a time, four independent groups per lane.  Quantising, it asks
+// a warp takes 1024 elements of a row, or several short rows, at a time, four independent groups per lane.  Quantising, it asks
 // for the next 1024 before it works on these (raw, half the registers of the widened values; without
 // that the loads' latency showed: 43 us for 14336 x 4096 bf16).  The arithmetic is exact: the scale is a power of two, its exponent is
 // read from the bits of amax, and the only rounding is the conversion to e2m1.
@@ -187,129 +187,185 @@ struct Mx4Rows {
     long long x_stride;       // elements
     long long code_stride, scale_stride;  // bytes
     bool vec;                 // rows of x start on 16-byte boundaries
+    int pack;                 // rows of a task: as many as 1024 elements hold, at least one
 };
 
-// A warp's tasks: segment after segment of 1024 elements, `step` tasks apart.  The divisions behind a
-// task's row are done once; from then on the position moves by (rows, segments).
+// A warp's tasks: `pack` short rows, or segments of 1024 elements of a long one, `step` tasks apart.  The
+// divisions behind a task's place are done once; from then on it moves by (rows, segments).
 struct Mx4Walk {
     long long row, seg, segs, d_row, d_seg;
-    __device__ __forceinline__ Mx4Walk(const Mx4Rows &a)
+    int pack;
+    __device__ __forceinline__ Mx4Walk(const Mx4Rows &a) : pack(a.pack)
     {
-        segs = (a.cols + kMxSeg - 1) / kMxSeg;
+        segs = (a.cols + kMxSeg - 1) / kMxSeg;   // 1 where pack > 1
         const long long task = (long long)blockIdx.x * (kMxThreads / kWarp) + threadIdx.x / kWarp;
         const long long step = (long long)gridDim.x * (kMxThreads / kWarp);
-        row = task / segs, seg = task - row * segs;
-        d_row = step / segs, d_seg = step - d_row * segs;
+        row = task / segs, seg = task - row * segs, row *= pack;
+        d_row = step / segs, d_seg = step - d_row * segs, d_row *= pack;
     }
     __device__ __forceinline__ void next()
     {
         row += d_row, seg += d_seg;
-        if (seg >= segs) seg -= segs, ++row;
+        if (seg >= segs) seg -= segs, row += pack;
     }
 };
 
+// A task as its warp sees it: pointers to its first row, elements of a row, rows, blocks of a row.
+template <typename T> struct Mx4Piece {
+    T *x;
+    uint8_t *codes, *scales;
+    int cols, rows, per_row;
+    __device__ __forceinline__ Mx4Piece(const Mx4Rows &a, const Mx4Walk &w)
+    {
+        const long long c0 = w.seg * kMxSeg;
+        x = reinterpret_cast<T *>(a.x) + w.row * a.x_stride + c0;
+        codes = a.codes + w.row * a.code_stride + c0 / 2, scales = a.scales + w.row * a.scale_stride + c0 / kMxBlock;
+        cols = (int)min((long long)kMxSeg, a.cols - c0);
+        rows = (int)min((long long)w.pack, a.rows - w.row);
+        per_row = (cols + kMxBlock - 1) / kMxBlock;
+    }
+};
+// Row and first column of a lane's g-th group of 8 elements (kPack: of a task of several rows; the
+// same for all tasks, as they differ in the number of rows alone).
+template <bool kPack> struct Mx4Lane {
+    int row[kMxGroups], col[kMxGroups];
+    __device__ __forceinline__ Mx4Lane(const Mx4Rows &a, int lane)
+    {
+        const int per_row = kPack ? (int)((a.cols + kMxBlock - 1) / kMxBlock) * 4 : kMxSeg / 8;
+#pragma unroll
+        for (int g = 0; g < kMxGroups; ++g) {
+            const int j = g * kWarp + lane;
+            row[g] = kPack ? j / per_row : 0, col[g] = (j - row[g] * per_row) * 8;
+        }
+    }
+};
+// 8 x 8 nibbles among eight neighbouring lanes: nibble i of lane l <-> nibble l%8 of lane (l & ~7) + i
+__device__ __forceinline__ uint32_t transpose_nibbles(uint32_t x, int lane)
+{
+    uint32_t r = __shfl_xor_sync(kFull, x, 4);
+    x = lane & 4 ? (r >> 16) | (x & 0xffff0000u) : (x & 0x0000ffffu) | (r << 16);
+    r = __shfl_xor_sync(kFull, x, 2);
+    x = lane & 2 ? ((r >> 8) & 0x00ff00ffu) | (x & 0xff00ff00u) : (x & 0x00ff00ffu) | ((r << 8) & 0xff00ff00u);
+    r = __shfl_xor_sync(kFull, x, 1);
+    x = lane & 1 ? ((r >> 4) & 0x0f0f0f0fu) | (x & 0xf0f0f0f0u) : (x & 0x0f0f0f0fu) | ((r << 4) & 0xf0f0f0f0u);
+    return x;
+}
+
 // CTAs an SM is to hold: the two sets of raw values of a lane are 32 registers, or 64 for fp32
-template <int DT> constexpr int mx4_quantize_ctas() { return DT == 0 ? 2 : 4; }
+template <int DT, bool kVec> constexpr int mx4_quantize_ctas() { return !kVec ? 5 : DT == 0 ? 2 : 4; }
 
 // kVec: rows of x on 16-byte boundaries, a lane owns 8 consecutive elements (four lanes a block).
 // Otherwise element by element in lane order, 32 elements (one block) a warp-wide access: with a lane's
 // 8 elements read or written one by one, every access of the warp would touch all sectors of 256
-// elements (1413 f16 columns: dequantisation 20 us against 5).
-template <int DT, bool kVec> __global__ void __launch_bounds__(kMxThreads, mx4_quantize_ctas<DT>()) mx4_quantize_kernel(const Mx4Rows a)
+// elements.  Eight blocks go together there: a lane has its element of each of them, and one exchange of
+// nibbles among eight lanes makes (or takes apart) the words of codes.
+// kPack: several short rows a task.
+template <int DT, bool kVec, bool kPack>
+__global__ void __launch_bounds__(kMxThreads, mx4_quantize_ctas<DT, kVec>()) mx4_quantize_kernel(const Mx4Rows a)
 {
     using T = typename Elem<DT>::T;
     const int lane = threadIdx.x % kWarp;
     pdl_wait();
     pdl_launch_dependents();
-    Raw8<DT> raw[kMxGroups];
-    auto fetch = [&](const Mx4Walk &w) {
-        if (!kVec || w.row >= a.rows) return;
-        const T *x = reinterpret_cast<const T *>(a.x) + w.row * a.x_stride + w.seg * kMxSeg;
-        const int left = (int)min((long long)kMxSeg, a.cols - w.seg * kMxSeg);
-#pragma unroll
-        for (int g = 0; g < kMxGroups; ++g) load_raw8<DT>(x + g * (kWarp * 8) + lane * 8, left - g * (kWarp * 8) - lane * 8, raw[g]);
-    };
     Mx4Walk w(a);
-    fetch(w);
-    while (w.row < a.rows) {
-        const long long c0 = w.seg * kMxSeg;
-        const int left = (int)min((long long)kMxSeg, a.cols - c0);          // elements of this segment
-        const int padded = (left + kMxBlock - 1) / kMxBlock * kMxBlock;
-        const T *x = reinterpret_cast<const T *>(a.x) + w.row * a.x_stride + c0;
-        uint8_t *codes = a.codes + w.row * a.code_stride + c0 / 2, *scales = a.scales + w.row * a.scale_stride + c0 / kMxBlock;
-        w.next();
-        if constexpr (kVec) {
+    if constexpr (kVec) {
+        const Mx4Lane<kPack> at(a, lane);
+        Raw8<DT> raw[kMxGroups];
+        auto fetch = [&]() {
+            const Mx4Piece<const T> t(a, w);
+#pragma unroll
+            for (int g = 0; g < kMxGroups; ++g)
+                load_raw8<DT>(t.x + (kPack ? at.row[g] * a.x_stride : 0) + at.col[g], at.row[g] < t.rows ? t.cols - at.col[g] : 0, raw[g]);
+        };
+        if (w.row < a.rows) fetch();
+        while (w.row < a.rows) {
+            const Mx4Piece<const T> t(a, w);
+            w.next();
             Raw8<DT> now[kMxGroups];
 #pragma unroll
             for (int g = 0; g < kMxGroups; ++g) now[g] = raw[g];
-            fetch(w);
+            if (w.row < a.rows) fetch();
 #pragma unroll
             for (int g = 0; g < kMxGroups; ++g) {
-                const int c = g * (kWarp * 8) + lane * 8;
                 float v[8];
                 uint32_t byte;
                 const float inv = mx4_inverse_scale(widen8<DT>(now[g], v), byte);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] *= inv;
-                if (c < padded) {
-                    *reinterpret_cast<uint32_t *>(codes + c / 2) = e2m1_pack8(v);
-                    if (lane % 4 == 0) scales[c / kMxBlock] = (uint8_t)byte;
+                if (at.col[g] < t.per_row * kMxBlock && at.row[g] < t.rows) {
+                    *reinterpret_cast<uint32_t *>(t.codes + (kPack ? at.row[g] * a.code_stride : 0) + at.col[g] / 2) = e2m1_pack8(v);
+                    if (lane % 4 == 0) t.scales[(kPack ? at.row[g] * a.scale_stride : 0) + at.col[g] / kMxBlock] = (uint8_t)byte;
                 }
             }
-        } else {
+        }
+    } else {
+        for (; w.row < a.rows; w.next()) {
+            const Mx4Piece<const T> t(a, w);
+            const int blocks = t.per_row * t.rows;
+            // the next eight blocks are asked for before these are worked on
+            T raw[8];
+            int row = 0, blk = 0;   // of the next block to ask for
+            auto fetch = [&](int b) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = blk * kMxBlock + lane;
+                    raw[i] = b + i < blocks && c < t.cols ? t.x[(kPack ? row * a.x_stride : 0) + c] : Elem<DT>::from_f32(0.f);
+                    if (++blk == t.per_row && kPack) blk = 0, ++row;
+                }
+            };
+            fetch(0);
 #pragma unroll 1
-            for (int g = 0; g < padded; g += 8 * kMxBlock) {
+            for (int b = 0; b < blocks; b += 8) {
                 float v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int c = g + i * kMxBlock + lane;
-                    v[i] = c < left ? Elem<DT>::to_f32(x[c]) : 0.f;
-                }
+                for (int i = 0; i < 8; ++i) v[i] = Elem<DT>::to_f32(raw[i]);
+                fetch(b + 8);
+                uint32_t word = 0, mine = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int c = g + i * kMxBlock + lane;
-                    uint32_t byte;
+                    uint32_t byte, code;
                     const float inv = mx4_inverse_scale(__reduce_max_sync(kFull, __float_as_uint(v[i]) & 0x7fffffffu), byte);
-                    const float q[8] = {v[i] * inv};
-                    uint32_t code = (e2m1_pack8(q) & 15u) << (4 * (lane & 7));   // then the eight lanes' codes in one word
-                    code |= __shfl_xor_sync(kFull, code, 1);
-                    code |= __shfl_xor_sync(kFull, code, 2);
-                    code |= __shfl_xor_sync(kFull, code, 4);
-                    if (c < padded) {
-                        if (lane % 8 == 0) *reinterpret_cast<uint32_t *>(codes + c / 2) = code;
-                        if (lane == 0) scales[c / kMxBlock] = (uint8_t)byte;
-                    }
+                    asm("{.reg .b8 q;\n\t"
+                        "cvt.rn.satfinite.e2m1x2.f32 q, %1, %1;\n\t"
+                        "cvt.u32.u8 %0, q;}"
+                        : "=r"(code)
+                        : "f"(v[i] * inv));
+                    word |= (code & 15u) << (4 * i);
+                    mine = lane % 8 == i ? byte : mine;
+                }
+                word = transpose_nibbles(word, lane);   // elements 8 (lane/8) .. +7 of block b + lane%8
+                const int q = b + lane % 8, r = kPack ? q / t.per_row : 0, c = q - r * t.per_row;
+                if (q < blocks) {
+                    *reinterpret_cast<uint32_t *>(t.codes + (kPack ? r * a.code_stride : 0) + c * 16 + 4 * (lane / 8)) = word;
+                    if (lane < 8) t.scales[(kPack ? r * a.scale_stride : 0) + c] = (uint8_t)mine;
                 }
             }
         }
     }
 }
 
-template <int DT, bool kVec> __global__ void __launch_bounds__(kMxThreads) mx4_dequantize_kernel(const Mx4Rows a)
+template <int DT, bool kVec, bool kPack> __global__ void __launch_bounds__(kMxThreads) mx4_dequantize_kernel(const Mx4Rows a)
 {
     using T = typename Elem<DT>::T;
     const int lane = threadIdx.x % kWarp;
     pdl_wait();
     pdl_launch_dependents();
-    for (Mx4Walk w(a); w.row < a.rows; w.next()) {
-        const long long c0 = w.seg * kMxSeg;
-        const int left = (int)min((long long)kMxSeg, a.cols - c0);
-        T *x = reinterpret_cast<T *>(a.x) + w.row * a.x_stride + c0;
-        const uint8_t *codes = a.codes + w.row * a.code_stride + c0 / 2, *scales = a.scales + w.row * a.scale_stride + c0 / kMxBlock;
-        if constexpr (kVec) {
+    Mx4Walk w(a);
+    if constexpr (kVec) {
+        const Mx4Lane<kPack> at(a, lane);
+        for (; w.row < a.rows; w.next()) {
+            const Mx4Piece<T> t(a, w);
             uint32_t word[kMxGroups], byte[kMxGroups];
 #pragma unroll
             for (int g = 0; g < kMxGroups; ++g) {
-                const int c = g * (kWarp * 8) + lane * 8;
                 word[g] = byte[g] = 0;
-                if (c < left) {
-                    word[g] = __ldg(reinterpret_cast<const uint32_t *>(codes + c / 2));
-                    byte[g] = __ldg(scales + c / kMxBlock);
+                if (at.col[g] < t.cols && at.row[g] < t.rows) {
+                    word[g] = __ldg(reinterpret_cast<const uint32_t *>(t.codes + (kPack ? at.row[g] * a.code_stride : 0) + at.col[g] / 2));
+                    byte[g] = __ldg(t.scales + (kPack ? at.row[g] * a.scale_stride : 0) + at.col[g] / kMxBlock);
                 }
             }
 #pragma unroll
             for (int g = 0; g < kMxGroups; ++g) {
-                const int c = g * (kWarp * 8) + lane * 8;
                 uint32_t h[4];
                 e2m1_unpack8(word[g], h);
                 const float s = e8m0_value(byte[g]);
@@ -319,28 +375,36 @@ template <int DT, bool kVec> __global__ void __launch_bounds__(kMxThreads) mx4_d
                     const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[i]));
                     v[2 * i] = f.x * s, v[2 * i + 1] = f.y * s;
                 }
-                store8<DT>(x + c, left - c, v);
+                store8<DT>(t.x + (kPack ? at.row[g] * a.x_stride : 0) + at.col[g], at.row[g] < t.rows ? t.cols - at.col[g] : 0, v);
             }
-        } else {
+        }
+    } else {
+        for (; w.row < a.rows; w.next()) {
+            const Mx4Piece<T> t(a, w);
+            const int blocks = t.per_row * t.rows;
+            int row = 0, blk = 0;
 #pragma unroll 1
-            for (int g = 0; g < left; g += 8 * kMxBlock) {
-                uint32_t word[8], byte[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int c = g + i * kMxBlock;
-                    word[i] = byte[i] = 0;
-                    if (c < left) {
-                        word[i] = __ldg(reinterpret_cast<const uint32_t *>(codes + c / 2) + lane / 8);
-                        byte[i] = __ldg(scales + c / kMxBlock);
-                    }
+            for (int b = 0; b < blocks; b += 8) {
+                const int q = b + lane % 8, qr = kPack ? q / t.per_row : 0, qc = q - qr * t.per_row;
+                uint32_t word = 0, byte = 0;
+                if (q < blocks) {
+                    word = __ldg(reinterpret_cast<const uint32_t *>(t.codes + (kPack ? qr * a.code_stride : 0) + qc * 16 + 4 * (lane / 8)));
+                    byte = __ldg(t.scales + (kPack ? qr * a.scale_stride : 0) + qc);
                 }
+                const float scale = e8m0_value(byte);
+                word = transpose_nibbles(word, lane);   // this lane's element of blocks b .. b+7
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int c = g + i * kMxBlock + lane;
-                    uint32_t h[4];
-                    e2m1_unpack8(word[i] >> (4 * (lane & 7)), h);
-                    const float v = __low2float(*reinterpret_cast<const __half2 *>(&h[0])) * e8m0_value(byte[i]);
-                    if (c < left) x[c] = Elem<DT>::from_f32(v);
+                    uint32_t h;
+                    asm("{.reg .b8 q;\n\t"
+                        "cvt.u8.u32 q, %1;\n\t"
+                        "cvt.rn.f16x2.e2m1x2 %0, q;}"
+                        : "=r"(h)
+                        : "r"(word >> (4 * i) & 15u));
+                    const float v = __low2float(*reinterpret_cast<const __half2 *>(&h)) * __shfl_sync(kFull, scale, i);
+                    const int c = blk * kMxBlock + lane;
+                    if (b + i < blocks && c < t.cols) t.x[(kPack ? row * a.x_stride : 0) + c] = Elem<DT>::from_f32(v);
+                    if (++blk == t.per_row && kPack) blk = 0, ++row;
                 }
             }
         }

@@ -109,22 +109,11 @@ __device__ __forceinline__ uint32_t plane_byte(uint32_t byte, int p)
 {
     return byte == 255 ? 255u : (uint32_t)max((int)byte - (p == 0 ? 0 : 3 * p - 1), 0);
 }
-// lane l: eight codes of element l -> the four bytes of plane l%8 that hold elements 8*(l/8) .. +7
-__device__ __forceinline__ uint32_t planes_transpose(uint32_t x, int lane)
-{
-    uint32_t r = __shfl_xor_sync(kFull, x, 4);
-    x = lane & 4 ? (r >> 16) | (x & 0xffff0000u) : (x & 0x0000ffffu) | (r << 16);
-    r = __shfl_xor_sync(kFull, x, 2);
-    x = lane & 2 ? ((r >> 8) & 0x00ff00ffu) | (x & 0xff00ff00u) : (x & 0x00ff00ffu) | ((r << 8) & 0xff00ff00u);
-    r = __shfl_xor_sync(kFull, x, 1);
-    x = lane & 1 ? ((r >> 4) & 0x0f0f0f0fu) | (x & 0xf0f0f0f0u) : (x & 0x0f0f0f0fu) | ((r << 4) & 0xf0f0f0f0u);
-    return x;
-}
 // A warp stores block `blk` of row `row` (token or pair): codes [row][8][blocks*16], scales [row][8][blocks].
 __device__ __forceinline__ void planes_store(float v, uint8_t *codes, uint8_t *scales, long long row, int blk, int blocks, int lane)
 {
     uint32_t byte;
-    const uint32_t w = planes_transpose(planes_of(v, byte), lane);
+    const uint32_t w = transpose_nibbles(planes_of(v, byte), lane);   // plane lane%8 of elements 8 (lane/8) .. +7
     const int p = lane % kPlanes;
     *reinterpret_cast<uint32_t *>(codes + ((row * kPlanes + p) * blocks + blk) * 16 + 4 * (lane / kPlanes)) = w;
     if (lane < kPlanes) scales[(row * kPlanes + lane) * blocks + blk] = (uint8_t)plane_byte(byte, lane);

@@ -35,7 +35,8 @@ def _check_quantized(x):
 
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("rows,cols,pad,offset", [(1, 1, 0, 0), (3, 31, 0, 0), (2, 32, 0, 0), (5, 33, 3, 1), (7, 1024, 8, 8), (1, 4096, 0, 0),
-                                                  (4, 1413, 11, 0), (130, 96, 0, 0), (3, 2049, 0, 0), (600, 64, 64, 0)])
+                                                  (4, 1413, 11, 0), (130, 96, 0, 0), (3, 2049, 0, 0), (600, 64, 64, 0),
+                                                  (700, 33, 7, 0), (41, 7, 1, 1), (333, 200, 8, 0), (35, 992, 0, 0), (34, 993, 31, 0), (65, 500, 4, 0), (1025, 1, 0, 0)])
 def test_quantize_and_back(dt, rows, cols, pad, offset):
     g = _gen(rows * 7 + cols)
     x = torch.randn(rows, cols, generator=g) * torch.exp(2 * torch.randn(rows, 1, generator=g))
