@@ -238,3 +238,37 @@ def test_product_on_another_stream_and_replayed():
         x.copy_(torch.randn(24, 1280, generator=_gen(seed)))
         graph.replay()
         assert torch.equal(y, P.mx4_matmul(P.mx4_quantize(x), b))
+
+
+# ---- sizes whose offsets pass 32 bits ------------------------------------------------------------
+
+def test_quantize_and_back_behind_four_billion_elements():
+    """70000 x 65536 bf16 (9 GB): elements, and with a row of padding bytes too, beyond 2^32."""
+    rows, cols = 70000, 65536
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV)
+    x[:8].normal_()
+    x[8:] = 1.0
+    x[-4:] = x[:4]
+    x[rows // 2] = x[5]
+    codes, scales = P.mx4_quantize(x)
+    few_c, few_s = P.mx4_quantize(x[:8].clone())
+    for big, few in ((slice(0, 8), slice(0, 8)), (slice(rows - 4, rows), slice(0, 4)), (slice(rows // 2, rows // 2 + 1), slice(5, 6))):
+        assert torch.equal(codes[big], few_c[few]) and torch.equal(scales[big], few_s[few])
+    del x
+    y = P.mx4_dequantize(codes, scales, cols, dtype=torch.bfloat16)
+    z = P.mx4_dequantize(few_c, few_s, cols, dtype=torch.bfloat16)
+    assert torch.equal(y[-4:], z[:4]) and torch.equal(y[rows // 2], z[5])
+    del y
+    wide = torch.empty(rows, 65540, dtype=torch.bfloat16, device=DEV)[:, :cols]   # rows off the 16-byte grid
+    P.mx4_dequantize(codes, scales, cols, out=wide)
+    assert torch.equal(wide[-4:], z[:4]) and torch.equal(wide[:8], z)
+
+
+def test_product_with_more_than_two_billion_outputs():
+    m, n, nb = 40003, 60001, 1
+    g = _gen(41)
+    a, b = _operand(g, m, nb), _operand(g, n, nb)
+    out = P.mx4_matmul(_dev(a), _dev(b), dtype=torch.bfloat16)
+    rows = [0, 1, 17777, 35791, 35792, m - 2, m - 1]          # 35792 * 60001 passes 2^31
+    want = _product([t[rows] for t in a], b)
+    assert torch.equal(out[rows].cpu(), torch.from_numpy(want).float().bfloat16())

@@ -265,6 +265,29 @@ def test_stack_whole_tokens_and_host_buffers(B, slots):
     st.close()
 
 
+@pytest.mark.parametrize("B", [1, 7, 33])
+def test_stack_replayed_steps_have_the_bits_of_single_layers(B):
+    """Many layers whose launches overlap and share the work list's and the planes' buffers, against
+    the same layers one at a time with a synchronisation behind each."""
+    cfg = stacks.CONFIGS["C2"].scaled(n_layers=10, profile_tokens=0, hidden=192, inter=160, n_experts=20, top_k=3, n_shared=1)
+    a, _ = _stack_pair(cfg, B)
+    b, _ = _stack_pair(cfg, B)
+    x = stacks.token_inputs(cfg, B, 12)
+    side = torch.cuda.Stream()
+    h, out, one = (torch.empty(B, cfg.hidden, device=DEV) for _ in range(3))
+    for t in range(12):
+        h.copy_(x[t])
+        torch.cuda.synchronize()
+        a.decode_token(h, out, stream=side)
+        side.synchronize()
+        one.copy_(h)
+        for l in range(cfg.n_layers):
+            b.decode_step(l, one, one)
+            torch.cuda.synchronize()
+        assert torch.equal(out, one), t
+    a.close(), b.close()
+
+
 def test_stack_kernel_timing_covers_the_projections():
     cfg = stacks.CONFIGS["C2"].scaled(n_layers=2, profile_tokens=0, hidden=128, inter=96, n_experts=8, top_k=2, n_shared=0)
     st, _ = _stack_pair(cfg, 2)

@@ -185,3 +185,24 @@ def test_same_bits_every_time_on_streams_and_replayed():
     torch.cuda.synchronize()
     f2 = P.router_balance(zd, idd, mask=md)
     assert torch.equal(f["loss"], f2["loss"]) and torch.equal(d, P.router_balance_backward(zd, f2, g, mask=md))
+
+
+def test_more_than_two_billion_logits():
+    """2^24 + 5 rows of 132 experts: the last rows against the formulas, the counts as a whole."""
+    T, E, K = (1 << 24) + 5, 132, 2
+    few = torch.randn(4096, E, generator=torch.Generator().manual_seed(3)).to(DEV).bfloat16()
+    z = few.repeat(T // 4096 + 1, 1)[:T]
+    ids = torch.arange(T * K, dtype=torch.int64, device=DEV).remainder_(E).to(torch.int32).view(T, K)
+    f = P.router_balance(z, ids)
+    assert f["rows"].item() == T
+    assert torch.equal(f["counts"].long(), torch.bincount(ids.flatten().long(), minlength=E))
+    g = torch.tensor([float(T), 0.1 * T], device=DEV)
+    d = P.router_balance_backward(z, f, g)
+    tail = slice(T - 4, T)
+    p = torch.softmax(z[tail].double(), 1)
+    share = f["counts"].double() / (T * K)
+    lse = torch.logsumexp(z[tail].double(), 1, keepdim=True)
+    want = E * p * (share - (p * share).sum(1, keepdim=True)) + 0.2 * lse * p
+    size = p * (E * share.max() + 0.2 * lse.abs())
+    assert ((d[tail].double() - want).abs() <= P_TOL * size + 2.0 ** -8 * want.abs()).all()
+    assert torch.equal(d[:4096], d[4096:8192])               # the same rows, the same gradient
