@@ -473,10 +473,23 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         // scales: this warp's stages are the CTA's steps w, w + 4, ... across its tasks
         const int w = warp - 6, per_task = k_end - k_beg;
         int task = first, k = k_beg + w;   // step i of the CTA, and the next of this warp's
+        Mx4Task t = {0, 0, 0, 0};
+        if (first < n_tasks) t = mm_task(a, s_off, s_tile, first);
         auto load = [&](uint2 (&vb)[4], uint2 (&va)[6]) {
-            for (; task < n_tasks && k >= k_end; task += step) k -= per_task;
+            bool entered = false;
+            for (; task < n_tasks && k >= k_end; task += step) k -= per_task, entered = true;
             if (task >= n_tasks) return false;
-            const Mx4Task t = mm_task(a, s_off, s_tile, task);
+            if (entered) t = mm_task(a, s_off, s_tile, task);
+            if ((entered || k < k_beg + 4) && task + step < n_tasks) {
+                // the next task's scale rows of b into L2, a lane a row, a warp a quarter of them: asked for
+                // one stage ahead alone they would hold every task up by a trip to HBM (2000 of 5600 cycles
+                // at 64 experts of 2816 x 2048)
+                const Mx4Task u = mm_task(a, s_off, s_tile, task + step);
+                const int row = u.row0 + 32 * w + lane;
+                const uint8_t *p = a.b_scales + ((long long)u.expert * a.n + row) * a.b_scale_stride;
+                if (row < a.n)
+                    for (int o = k_beg * kMmStageBlocks; o < min(k_end * kMmStageBlocks, a.blocks); o += 128) prefetch_l2(p + o);
+            }
             const int kb = k * kMmStageBlocks;
             k += 4;
             const uint8_t *pb = a.b_scales + (long long)t.expert * a.n * a.b_scale_stride;
@@ -486,11 +499,8 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                            (1u << ((bn + 31) / 32)) - 1, kb, a.blocks, a.a_align);
             return true;
         };
-        uint2 vb[4], va[6], nb[4], na[6];
         uint32_t i = w;
-        bool more = load(vb, va);
-        while (more) {
-            more = load(nb, na);
+        auto put = [&](const uint2 (&vb)[4], const uint2 (&va)[6]) {   // step i
             const int s = (int)(i % NS);
             const bool ok = __all_sync(kFull, dmbar_wait(&empty[s], ((i / NS) & 1u) ^ 1u, dead));
             uint8_t *st = dsm + (size_t)s * slot;
@@ -504,12 +514,17 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) dmbar_arrive(&full[s]);
-            if (!ok) break;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) vb[r] = nb[r];
-#pragma unroll
-            for (int r = 0; r < 6; ++r) va[r] = na[r];
             i += 4;
+            return ok;
+        };
+        // two sets of registers in turn: copying one into the other would wait for its loads
+        uint2 b0[4], a0[6], b1[4], a1[6];
+        bool more = load(b0, a0);
+        while (more) {
+            const bool next = load(b1, a1);
+            if (!put(b0, a0) || !next) break;
+            more = load(b0, a0);
+            if (!put(b1, a1)) break;
         }
     }
     if (a.splits > 1 && first < n_tasks) {  // one task per cluster, the same for all its CTAs
