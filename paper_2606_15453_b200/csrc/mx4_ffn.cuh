@@ -496,18 +496,6 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             const int own = min(lane, kMxfTokens - 1);
             return Info{en.img, en.count, NMAT == 2 ? en.token[own] : en.slot[own]};
         };
-        // scale rows of a task into L2 while the one before it runs: a lane a row, a warp a quarter of them
-        auto prefetch = [&](int task, const uint8_t *img) {
-            if (task >= n_tasks) return;
-            const Mx4FfnTask t = mxf_task<NMAT>(a, task);
-            int beg, end;
-            k_range(t.z, beg, end);
-            const int row = t.row0 + w * kWarp + lane, lo = beg * kMmStageBlocks, hi = min(end * kMmStageBlocks, a.blocks);
-            if (row < a.rows)
-#pragma unroll
-                for (int m = 0; m < NMAT; ++m)
-                    for (int o = lo; o < hi; o += 128) prefetch_l2(img + a.scale_off[m] + (long long)row * a.blocks + o);
-        };
         auto enter = [&](Pos &p) {   // first step of task p.task
             if (p.task >= n_tasks) return;
             const Mx4FfnTask t = mxf_task<NMAT>(a, p.task);
@@ -548,12 +536,9 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         asm volatile("bar.sync 1, 160;" ::: "memory");
         if (NMAT == 1) pdl_wait();   // the activations
         if (p.task < n_tasks) load_x(p, vx);
-        int fetched = first;   // tasks whose scales have been asked into L2
         for (int i = w; p.task < n_tasks; i += 4) {
             const int k = p.k, cnt = p.in.cnt, xrow = p.in.row;
-            if (fetched == p.task) prefetch(fetched += step, p.ahead.img);
             forward(p, 4);
-            if (fetched < p.task) fetched = p.task;
             if (p.task < n_tasks) load_w(p, nw), load_x(p, nx);
             const int s = i % NS;
             const bool ok = __all_sync(kFull, dmbar_wait(&empty[s], ((uint32_t)(i / NS) & 1u) ^ 1u, dead));

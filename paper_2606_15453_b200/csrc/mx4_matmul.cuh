@@ -480,16 +480,6 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             for (; task < n_tasks && k >= k_end; task += step) k -= per_task, entered = true;
             if (task >= n_tasks) return false;
             if (entered) t = mm_task(a, s_off, s_tile, task);
-            if ((entered || k < k_beg + 4) && task + step < n_tasks) {
-                // the next task's scale rows of b into L2, a lane a row, a warp a quarter of them: asked for
-                // one stage ahead alone they would hold every task up by a trip to HBM (2000 of 5600 cycles
-                // at 64 experts of 2816 x 2048)
-                const Mx4Task u = mm_task(a, s_off, s_tile, task + step);
-                const int row = u.row0 + 32 * w + lane;
-                const uint8_t *p = a.b_scales + ((long long)u.expert * a.n + row) * a.b_scale_stride;
-                if (row < a.n)
-                    for (int o = k_beg * kMmStageBlocks; o < min(k_end * kMmStageBlocks, a.blocks); o += 128) prefetch_l2(p + o);
-            }
             const int kb = k * kMmStageBlocks;
             k += 4;
             const uint8_t *pb = a.b_scales + (long long)t.expert * a.n * a.b_scale_stride;
