@@ -251,6 +251,8 @@ __global__ void __launch_bounds__(256) mx4_planes_kernel(const Mx4PlanesArgs a)
 
 // ---- the two projections ------------------------------------------------------------------------
 
+inline int mxf_align(int blocks) { return blocks % 8 == 0 ? 8 : blocks % 4 == 0 ? 4 : 1; }
+
 struct Mx4FfnArgs {
     const Mx4Entry *entries;
     const int *n_entries;
@@ -264,7 +266,6 @@ struct Mx4FfnArgs {
     // down
     float *part;                         // [pair][splits][rows]
     unsigned *err;
-    int w_align;                         // what a weight matrix's scale rows are aligned to: 8, 4 or 1
 };
 
 struct Mx4FfnTask {
@@ -289,7 +290,9 @@ __device__ __forceinline__ void mxf_store_act(const Mx4FfnArgs &a, float g, floa
     planes_store(g / (1.f + expf(-g)) * u, a.act_codes, a.act_scales, slot, row / kMxBlock, a.rows / kMxBlock, lane);
 }
 
-template <int NMAT>
+// kAlign: what scale rows are aligned to (mxf_align), of weights and planes alike; as a template
+// parameter because a kernel of some tens of microseconds pays for every line of code it fetches
+template <int NMAT, int kAlign>
 __global__ void __launch_bounds__(kMxfThreads, 1)
 mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1,
                const __grid_constant__ CUtensorMap map_s0, const __grid_constant__ CUtensorMap map_s1,
@@ -480,7 +483,6 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         // stage by one thread would hold the weights' back).  A task's steps may differ by one between
         // splits, so the position is walked, not computed
         const int w = warp - kMxfScaleWarp;
-        const int x_align = a.blocks % 8 == 0 ? 8 : a.blocks % 4 == 0 ? 4 : 1;
         // what a warp knows of the task its next step belongs to, and of the one after (asked for at the
         // start of this one)
         struct Info {
@@ -515,7 +517,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         auto load_w = [&](const Pos &p, uint2 (&vw)[4 * NMAT]) {
             load_scales<4 * NMAT>(vw, [&](int i) {
                 return p.in.img + a.scale_off[i / 4] + (long long)min(p.row0 + 32 * (i % 4) + lane, a.rows - 1) * a.blocks;
-            }, (1u << (4 * NMAT)) - 1, p.k * kMmStageBlocks, a.blocks, a.w_align);
+            }, (1u << (4 * NMAT)) - 1, p.k * kMmStageBlocks, a.blocks, kAlign);
         };
         auto load_x = [&](const Pos &p, uint2 (&vx)[3]) {
             int row[3];   // rows of the B tile: plane q % 8 of token q / 8
@@ -526,7 +528,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                 row[r] = __shfl_sync(kFull, p.in.row, q / kPlanes) * kPlanes + q % kPlanes;
                 if (q < p.in.cnt * kPlanes) on |= 1u << r;
             }
-            load_scales<3>(vx, [&](int r) { return a.x_scales + (long long)row[r] * a.blocks; }, on, p.k * kMmStageBlocks, a.blocks, x_align);
+            load_scales<3>(vx, [&](int r) { return a.x_scales + (long long)row[r] * a.blocks; }, on, p.k * kMmStageBlocks, a.blocks, kAlign);
         };
         uint2 vw[4 * NMAT], vx[3], nw[4 * NMAT], nx[3];
         Pos p = {first, 0, 0, 0, {}, ask(first)};

@@ -423,6 +423,12 @@ int mx4_launch(void (*kernel)(P...), int grid, int block, size_t smem, int clust
     CU_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     return STMOE_OK;
 }
+template <int NMAT> auto mx4_ffn_kernel_for(int blocks)
+{
+    const int align = mxf_align(blocks);
+    return align == 8 ? mx4_ffn_kernel<NMAT, 8> : align == 4 ? mx4_ffn_kernel<NMAT, 4> : mx4_ffn_kernel<NMAT, 1>;
+}
+
 // what a call has to know of its device, found out once per device ordinal (a racing fill writes the
 // same values): the kernels' shared memory is asked for on the way
 struct Mx4Device {
@@ -435,11 +441,13 @@ int mx4_device(int dev, Mx4Device *d)
     static bool ready[64];
     if (dev < 0 || dev >= 64) return STMOE_ERR_BAD_ARG;
     if (!ready[dev]) {
-        CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
-        CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        for (int blocks : {8, 4, 1}) {
+            CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel_for<2>(blocks), cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+            CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel_for<1>(blocks), cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
+        }
         Mx4Device m;
         m.sms = sm_count();
-        if (!mm_clusters(mx4_ffn_kernel<2>, kMxfThreads, &m.clusters)) return STMOE_ERR_CUDA;
+        if (!mm_clusters(mx4_ffn_kernel_for<2>(8), kMxfThreads, &m.clusters)) return STMOE_ERR_CUDA;
         kept[dev] = m;
         ready[dev] = true;
     }
@@ -471,19 +479,17 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
     g.scale_off[0] = (long long)mx4_image_scales(H, I, 0), g.scale_off[1] = (long long)mx4_image_scales(H, I, 1);
     g.rows = I, g.blocks = H / kMxBlock, g.mt = mt;
     g.x_scales = b.x_scales, g.act_codes = b.act_codes, g.act_scales = b.act_scales, g.err = err;
-    g.w_align = g.blocks % 8 == 0 ? 8 : g.blocks % 4 == 0 ? 4 : 1;
     const int gu_steps = (g.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
     const int gu_tasks = entries * ((I + kMmRows - 1) / kMmRows);
     g.last_task = gu_tasks - 1;
     g.splits = mm_splits(gu_tasks, gu_steps, dev.clusters);   // fewer tiles than SMs: a cluster shares a tile's reduction
-    ST_TRY(mx4_launch(mx4_ffn_kernel<2>, g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMxfThreads, kMmSmemBytes,
+    ST_TRY(mx4_launch(mx4_ffn_kernel_for<2>(g.blocks), g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMxfThreads, kMmSmemBytes,
                       g.splits, st, maps.gate[0], maps.up[0], maps.gate[1], maps.up[1], maps.x, g));
 
     ST_TRY(mark(1));
     Mx4FfnArgs d = g;
     d.rows = H, d.blocks = I / kMxBlock, d.x_scales = b.act_scales, d.part = b.part;
     d.scale_off[0] = (long long)mx4_image_scales(H, I, 2);
-    d.w_align = d.blocks % 8 == 0 ? 8 : d.blocks % 4 == 0 ? 4 : 1;
     const int d_tiles = entries * ((H + kMmRows - 1) / kMmRows);
     // split the reduction where it evens the last round of tasks out; every split is one more
     // partial sum to write and read
@@ -493,7 +499,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
         if (t < best) best = t, d.splits = z;
     }
     d.last_task = d_tiles * d.splits - 1;
-    ST_TRY(mx4_launch(mx4_ffn_kernel<1>, std::min(d_tiles * d.splits, sms), kMxfThreads, kMmSmemBytes, 1, st, maps.down[0],
+    ST_TRY(mx4_launch(mx4_ffn_kernel_for<1>(d.blocks), std::min(d_tiles * d.splits, sms), kMxfThreads, kMmSmemBytes, 1, st, maps.down[0],
                       maps.down[0], maps.down[1], maps.down[1], maps.act, d));
 
     fa.part = b.part, fa.S = d.splits;
