@@ -360,8 +360,8 @@ template <int DT, bool kVec, bool kPack> __global__ void __launch_bounds__(kMxTh
             for (int g = 0; g < kMxGroups; ++g) {
                 word[g] = byte[g] = 0;
                 if (at.col[g] < t.cols && at.row[g] < t.rows) {
-                    word[g] = __ldg(reinterpret_cast<const uint32_t *>(t.codes + (kPack ? at.row[g] * a.code_stride : 0) + at.col[g] / 2));
-                    byte[g] = __ldg(t.scales + (kPack ? at.row[g] * a.scale_stride : 0) + at.col[g] / kMxBlock);
+                    word[g] = (*reinterpret_cast<const uint32_t *>(t.codes + (kPack ? at.row[g] * a.code_stride : 0) + at.col[g] / 2));
+                    byte[g] = t.scales[(kPack ? at.row[g] * a.scale_stride : 0) + at.col[g] / kMxBlock];
                 }
             }
 #pragma unroll
@@ -388,8 +388,8 @@ template <int DT, bool kVec, bool kPack> __global__ void __launch_bounds__(kMxTh
                 const int q = b + lane % 8, qr = kPack ? q / t.per_row : 0, qc = q - qr * t.per_row;
                 uint32_t word = 0, byte = 0;
                 if (q < blocks) {
-                    word = __ldg(reinterpret_cast<const uint32_t *>(t.codes + (kPack ? qr * a.code_stride : 0) + qc * 16 + 4 * (lane / 8)));
-                    byte = __ldg(t.scales + (kPack ? qr * a.scale_stride : 0) + qc);
+                    word = (*reinterpret_cast<const uint32_t *>(t.codes + (kPack ? qr * a.code_stride : 0) + qc * 16 + 4 * (lane / 8)));
+                    byte = t.scales[(kPack ? qr * a.scale_stride : 0) + qc];
                 }
                 const float scale = e8m0_value(byte);
                 word = transpose_nibbles(word, lane);   // this lane's element of blocks b .. b+7

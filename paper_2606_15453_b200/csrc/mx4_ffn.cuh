@@ -327,12 +327,13 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
     // Gate/up: the work list and the planes are the kernel before's.  Down: only the activations are (the
     // gate/up kernel lets its successor start after its own wait, so the work list is complete); its first
     // weights are on their way while gate/up finishes elsewhere, and the warps that read activations wait.
+    // The work list is read from L2, as an L1 line could be older than this launch.
     if (NMAT == 2) pdl_wait();
     pdl_launch_dependents();
 
     const int ranks = NMAT == 2 ? a.splits : 1;   // CTAs of a cluster that share a task's reduction
     const int tiles = (a.rows + kMmRows - 1) / kMmRows;
-    const int n_tasks = *a.n_entries * tiles * (NMAT == 1 ? a.splits : 1);
+    const int n_tasks = __ldcg(a.n_entries) * tiles * (NMAT == 1 ? a.splits : 1);
     const int per_entry = tiles * (NMAT == 1 ? a.splits : 1);
     const int rank = blockIdx.x % ranks, first = blockIdx.x / ranks, step = gridDim.x / ranks;
     const int n_steps = (a.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
@@ -343,7 +344,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
 
     if (warp == 0) {
         // the scale warps' first loads go ahead of the flood of weights, or the first stage would wait
-        // behind it (measured: 10 us on the gate/up kernel at 64 sequences)
+        // behind it
         asm volatile("bar.sync 1, 160;" ::: "memory");
         if (elect_one()) {
             int s = 0, issued = 0, img_next = 0;
@@ -351,7 +352,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             uint32_t par = 0;
             auto fetch = [&](int task) {   // a task's entry is asked for one task ahead
                 const Mx4Entry &en = a.entries[min(task, a.last_task) / per_entry];
-                img_next = en.img_index, shared_next = en.shared != 0;
+                img_next = __ldcg(&en.img_index), shared_next = __ldcg(&en.shared) != 0;
             };
             fetch(first);
             for (int task = first; task < n_tasks && !*dead; task += step) {
@@ -387,11 +388,11 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         int s = 0, it = 0;
         uint32_t par = 0;
         bool ok = true;
-        int count = a.entries[min(first, a.last_task) / per_entry].count;
+        int count = __ldcg(&a.entries[min(first, a.last_task) / per_entry].count);
         for (int task = first; task < n_tasks && ok; task += step, ++it) {
             const Mx4FfnTask t = mxf_task<NMAT>(a, task);
             const int n = mxf_cols(count);
-            count = a.entries[min(task + step, a.last_task) / per_entry].count;   // the next task's
+            count = __ldcg(&a.entries[min(task + step, a.last_task) / per_entry].count);   // the next task's
             const uint32_t id0 = umma_idesc_mxf4(n, 0), id1 = umma_idesc_mxf4(n, 1);
             const int ab = it & 1;
             if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)))) break;
@@ -431,8 +432,8 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         for (int task = first + ab * step; task < n_tasks; task += 2 * step, ++use) {
             const Mx4FfnTask t = mxf_task<NMAT>(a, task);
             const Mx4Entry &en = a.entries[t.g];
-            const int cnt = en.count, own = min(lane, kMxfTokens - 1);
-            const int slot_l = en.slot[own];      // lane i: the i-th pair's, fetched while the MMAs run
+            const int cnt = __ldcg(&en.count), own = min(lane, kMxfTokens - 1);
+            const int slot_l = __ldcg(&en.slot[own]);      // lane i: the i-th pair's, fetched while the MMAs run
             const float inv_l = en.inv[own];
             const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], use & 1u, dead));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -496,7 +497,8 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         auto ask = [&](int task) {
             const Mx4Entry &en = a.entries[min(task, a.last_task) / per_entry];
             const int own = min(lane, kMxfTokens - 1);
-            return Info{en.img, en.count, NMAT == 2 ? en.token[own] : en.slot[own]};
+            const auto img = __ldcg(reinterpret_cast<const unsigned long long *>(&en.img));
+            return Info{reinterpret_cast<const uint8_t *>(img), __ldcg(&en.count), __ldcg(NMAT == 2 ? &en.token[own] : &en.slot[own])};
         };
         auto enter = [&](Pos &p) {   // first step of task p.task
             if (p.task >= n_tasks) return;
@@ -619,8 +621,8 @@ template <int S> __device__ __forceinline__ float mx4_combine_sum(const FfnArgs 
 #pragma unroll
         for (int j = 0; j < Q; ++j) {
             const int q = min(q0 + j, KS - 1), k = q < a.n_shared ? a.K + q : q - a.n_shared;
-            in[j] = q0 + j < KS && !(ids && (unsigned)__ldg(ids + b * a.K + k) >= (unsigned)a.E);
-            w[j] = q < a.n_shared ? 1.f : __ldg(a.w + b * a.K + k);
+            in[j] = q0 + j < KS && !(ids && (unsigned)ids[b * a.K + k] >= (unsigned)a.E);
+            w[j] = q < a.n_shared ? 1.f : a.w[b * a.K + k];
 #pragma unroll
             for (int z = 0; z < S; ++z) v[j][z] = __ldcg(part + (long long)(k * S + z) * a.H);
         }

@@ -273,7 +273,7 @@ template <int DT, int LPR, int N, int kRead, bool kIds> struct BalWalk {
             if (kIds && l < a.K) asm volatile("ld.shared.s32 %0, [%1];" : "=r"(id) : "r"(id_at(r) + slot));
         } else {
             bal_load<DT, LPR, N>(z + r * z_row, a.E, l, v);
-            if (kIds && l < a.K) id = __ldg(ids + r * RPW * a.K);
+            if (kIds && l < a.K) id = ids[r * RPW * a.K];
         }
     }
     __device__ __forceinline__ void end()
@@ -339,7 +339,7 @@ template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(k
                 if (l == 0) zz = fmaf(lse, lse, zz), ++n;
                 if ((unsigned)id < (unsigned)a.E) atomicAdd(&s_cnt[id], 1);
                 for (int k = l + LPR; k < a.K; k += LPR) {
-                    const int e = __ldg(a.ids + (long long)(w.t + r * (kWarp / LPR)) * a.K + k);
+                    const int e = a.ids[(long long)(w.t + r * (kWarp / LPR)) * a.K + k];
                     if ((unsigned)e < (unsigned)a.E) atomicAdd(&s_cnt[e], 1);
                 }
             }

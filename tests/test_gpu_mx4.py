@@ -272,3 +272,30 @@ def test_product_with_more_than_two_billion_outputs():
     rows = [0, 1, 17777, 35791, 35792, m - 2, m - 1]          # 35792 * 60001 passes 2^31
     want = _product([t[rows] for t in a], b)
     assert torch.equal(out[rows].cpu(), torch.from_numpy(want).float().bfloat16())
+
+
+@pytest.mark.parametrize("blocks", [16, 12, 35])   # scale rows on 8, 4 and 1 bytes: a read path each
+def test_chain_through_the_same_buffers_sees_each_step_s_values(blocks):
+    """Each product reads what the quantisation just before it wrote over the last step's operand."""
+    g = torch.Generator(device="cuda").manual_seed(blocks)
+    rows, n, cols, steps = 700, 256, blocks * 32, 24
+    xs = torch.randn(steps, rows, cols, device="cuda", generator=g, dtype=torch.bfloat16)
+    b = P.mx4_quantize(torch.randn(n, cols, device="cuda", generator=g))
+    want_x, want_y = [], []
+    for x in xs:   # operands of their own, one step at a time
+        q = P.mx4_quantize(x)
+        torch.cuda.synchronize()
+        want_x.append(P.mx4_dequantize(*q, cols))
+        want_y.append(P.mx4_matmul(q, b))
+        torch.cuda.synchronize()
+    codes = torch.empty(rows, blocks * 16, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(rows, blocks, dtype=torch.uint8, device="cuda")
+    back = torch.empty(steps, rows, cols, device="cuda")
+    out = torch.empty(steps, rows, n, dtype=torch.bfloat16, device="cuda")
+    for i, x in enumerate(xs):
+        P.mx4_quantize(x, codes, scales)
+        P.mx4_matmul((codes, scales), b, out=out[i])
+        P.mx4_quantize(x.flip(0).contiguous(), codes, scales)
+        P.mx4_dequantize(codes, scales, cols, out=back[i])
+    assert all(torch.equal(out[i], want_y[i]) for i in range(steps))
+    assert all(torch.equal(back[i], want_x[i].flip(0)) for i in range(steps))
