@@ -325,7 +325,8 @@ int stmoe_predictor_step(stmoe_t *s, int layer, int batch, const int32_t *routed
  *
  * STMOE_MX4: an image is the codes of gate [I][H/2], up [I][H/2], down [H][I/2] bytes, then the scale
  * bytes of gate, up, down; hidden and inter multiples of 32, experts 16-byte aligned, scratch
- * stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter) bytes.  The weights go to the tensor cores
+ * stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter) bytes, which also serve every smaller batch
+ * and top_k (a call of exactly that size may take less).  The weights go to the tensor cores
  * as stored; an activation is held as a sum of eight 4-bit values that leaves less than 2^-22 of the
  * largest magnitude among its 32 neighbours, and sums are fp32, so results have the precision of fp32
  * activations.  A non-finite activation makes the 32 neighbours, and what depends on them, NaN; pairs
@@ -348,7 +349,7 @@ int stmoe_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, cons
  *   - Same arguments, layout and results as stmoe_moe_ffn; inputs and outputs stay with the
  *     caller.  Calls no cudaMalloc/cudaFree or other allocating routine.
  *   - Returns STMOE_ERR_TOO_LARGE when stmoe_moe_ffn_scratch_bytes(batch, top_k, hidden, inter)
- *     (STMOE_MX4: stmoe_mx4_ffn_scratch_bytes) exceeds 8 MiB (for example batch 64, top_k 8, hidden 4096, inter 14336).
+ *     (STMOE_MX4: what a call of exactly that size takes) exceeds 8 MiB (for example batch 64, top_k 8, hidden 4096, inter 14336).
  *   - The first call on each device looks up the area's device address (with that device
  *     current); make that first call before starting any stream capture, and from one host
  *     thread (later calls may come from any thread).

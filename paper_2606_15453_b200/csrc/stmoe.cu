@@ -342,14 +342,23 @@ struct Mx4FfnBufs {
     uint8_t *x_codes, *x_scales, *act_codes, *act_scales;
     float *part;
 };
-// splits of the down projection's reduction that the partial sums have room for
+// most splits of the down projection's reduction that a call with this many pairs may choose
 int mx4_max_splits(int pairs, int I)
 {
     const int steps = (I / kMxBlock + kMmStageBlocks - 1) / kMmStageBlocks, cap = pairs <= 32 ? 8 : pairs <= 128 ? 4 : 2;
     return std::min(steps, cap);
 }
-// lays the buffers out behind base (nullptr: only the size)
-size_t mx4_buffers(uint8_t *base, int B, int pairs, int H, int I, Mx4FfnBufs *b)
+// Rows of partial sums that a call with this many pairs may write, and that any call with up to as many
+// may: the splits fall as the pairs grow, so fewer pairs can need more rows (32 of them 256, 40 only 160).
+int mx4_part_rows(int pairs, int I) { return pairs * mx4_max_splits(pairs, I); }
+int mx4_part_rows_up_to(int pairs, int I)
+{
+    int rows = 0;
+    for (int p = 1; p <= pairs; ++p) rows = std::max(rows, mx4_part_rows(p, I));
+    return rows;
+}
+// lays the buffers out behind base (nullptr: only the size), with room for part_rows rows of partial sums
+size_t mx4_buffers(uint8_t *base, int B, int pairs, int H, int I, int part_rows, Mx4FfnBufs *b)
 {
     size_t o = 0;
     auto take = [&](size_t n) {
@@ -363,7 +372,7 @@ size_t mx4_buffers(uint8_t *base, int B, int pairs, int H, int I, Mx4FfnBufs *b)
     b->x_scales = take((size_t)B * kPlanes * H / kMxBlock);
     b->act_codes = take((size_t)pairs * kPlanes * I / 2);
     b->act_scales = take((size_t)pairs * kPlanes * I / kMxBlock);
-    b->part = (float *)take(sizeof(float) * (size_t)pairs * mx4_max_splits(pairs, I) * H);
+    b->part = (float *)take(sizeof(float) * (size_t)part_rows * H);
     return o;
 }
 int mx4_entry_tokens(int B) { return std::min(B, kMxfTokens); }
@@ -1583,8 +1592,9 @@ int stmoe_create(const stmoe_config_t *cfg, stmoe_t **out)
         CR_TRY(cudaGetDevice(&dev));
         int rc = mx4_device(dev, &s->mx4_dev);
         if (rc != STMOE_OK) return fail(rc);
-        CR_TRY(cudaMalloc(&s->d_mx4, mx4_buffers(nullptr, B, pairs, H, I, &s->mx4)));
-        mx4_buffers(s->d_mx4, B, pairs, H, I, &s->mx4);
+        const int part_rows = mx4_part_rows_up_to(pairs, I);   // a step may have fewer sequences than max_batch
+        CR_TRY(cudaMalloc(&s->d_mx4, mx4_buffers(nullptr, B, pairs, H, I, part_rows, &s->mx4)));
+        mx4_buffers(s->d_mx4, B, pairs, H, I, part_rows, &s->mx4);
         rc = mx4_act_maps(&s->mx4_maps, s->mx4, B, pairs, H, I);
         const bool off = c.cache_slots > 0;
         if (rc == STMOE_OK)
@@ -2137,6 +2147,12 @@ group_given_ids_kernel(const int32_t *ids, int B, int E, int K, int mt, WorkList
 
 namespace {
 
+// what a stand-alone call lays out behind its scratch (nullptr: only the size)
+size_t mx4_call_buffers(uint8_t *scratch, int batch, int top_k, int hidden, int inter, Mx4FfnBufs *b)
+{
+    return mx4_buffers(scratch, batch, batch * top_k, hidden, inter, mx4_part_rows(batch * top_k, inter), b);
+}
+
 bool mx4_ffn_args_ok(const void *experts, int hidden, int inter)
 {
     return hidden % kMxBlock == 0 && inter % kMxBlock == 0 && ((uintptr_t)experts & 15) == 0;
@@ -2146,15 +2162,14 @@ int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const 
                 int n_experts, int top_k, int hidden, int inter, float residual_scale, float *h_out, void *scratch,
                 size_t scratch_bytes, cudaStream_t st)
 {
-    if (!mx4_ffn_args_ok(experts, hidden, inter) || scratch_bytes < stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter))
+    Mx4FfnBufs b;
+    if (!mx4_ffn_args_ok(experts, hidden, inter) || scratch_bytes < mx4_call_buffers((uint8_t *)scratch, batch, top_k, hidden, inter, &b))
         return STMOE_ERR_BAD_ARG;
     int dev = 0;
     CU_TRY(cudaGetDevice(&dev));
     Mx4Device on;
     ST_TRY(mx4_device(dev, &on));
     const size_t img = image_bytes(hidden, inter, STMOE_MX4);
-    Mx4FfnBufs b;
-    mx4_buffers((uint8_t *)scratch, batch, batch * top_k, hidden, inter, &b);
     Mx4FfnMaps maps;
     ST_TRY(mx4_weight_maps(&maps, 0, (const uint8_t *)experts, n_experts, img, hidden, inter));
     maps.gate[1] = maps.gate[0], maps.up[1] = maps.up[0], maps.down[1] = maps.down[0], maps.store[1] = maps.store[0];
@@ -2174,7 +2189,7 @@ extern "C" size_t stmoe_mx4_ffn_scratch_bytes(int batch, int top_k, int hidden, 
 {
     if (batch < 1 || batch > kMaxBatch || top_k < 1 || top_k > kMaxTopK || hidden < kMxBlock || inter < kMxBlock) return 0;
     Mx4FfnBufs b;
-    return mx4_buffers(nullptr, batch, batch * top_k, hidden, inter, &b);
+    return mx4_buffers(nullptr, batch, batch * top_k, hidden, inter, mx4_part_rows_up_to(batch * top_k, inter), &b);
 }
 
 extern "C" int stmoe_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const float *w,
@@ -2241,7 +2256,8 @@ extern "C" int stmoe_moe_ffn_static(const float *h, const float *inv_rms, const 
         hidden % 16 || inter < 16 || inter % 16 || weight_dtype < STMOE_F32 || weight_dtype > STMOE_MX4 ||
         (weight_dtype == STMOE_MX4 && !mx4_ffn_args_ok(experts, hidden, inter)))
         return STMOE_ERR_BAD_ARG;
-    if ((weight_dtype == STMOE_MX4 ? stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter)
+    Mx4FfnBufs b;
+    if ((weight_dtype == STMOE_MX4 ? mx4_call_buffers(nullptr, batch, top_k, hidden, inter, &b)
                                    : stmoe_moe_ffn_scratch_bytes(batch, top_k, hidden, inter)) > (size_t)STMOE_STATIC_SCRATCH_BYTES)
         return STMOE_ERR_TOO_LARGE;
     int dev = -1;
