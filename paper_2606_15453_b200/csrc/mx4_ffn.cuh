@@ -372,8 +372,9 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                     if (++s == NS) s = 0, par ^= 1u;
                 }
             }
-            // every load that was issued lands before the CTA may exit, after an error too; the token
-            // loads of a stage complete on the same barrier
+            // every load that was issued lands before the CTA may exit; the token loads of a stage complete
+            // on the same barrier (behind an error, where a stage may have token loads and no weights, its
+            // barrier never completes: see settle_in_flight)
             int none = 0;
             for (int i = 0; i < min(issued, NS); ++i) {
                 if (s == 0) s = NS, par ^= 1u;
@@ -599,6 +600,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
     if (NMAT == 1) pdl_wait();   // a CTA without tasks too: the grid's end then means that gate/up has ended
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (s_dead) settle_in_flight();
     if (warp == 1) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }

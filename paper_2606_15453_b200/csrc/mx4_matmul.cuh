@@ -359,8 +359,8 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     if (++s == NS) s = 0, par ^= 1u;
                 }
             }
-            // every load that was issued lands before the CTA may exit, after an error too (the wait
-            // then has an end of its own: the error word would cut it short)
+            // every load that was issued lands before the CTA may exit (the wait has an end of its own, as
+            // the error word would cut it short; behind an error settle_in_flight has the last word)
             int none = 0;
             for (int i = 0; i < min(issued, NS); ++i) {
                 if (s == 0) s = NS, par ^= 1u;
@@ -554,6 +554,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (s_dead) settle_in_flight();
     if (warp == 1) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }

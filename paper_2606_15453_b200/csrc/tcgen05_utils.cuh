@@ -59,6 +59,20 @@ __device__ __forceinline__ bool dmbar_wait(uint64_t *bar, uint32_t parity, volat
     return false;
 }
 
+// Behind a wait that ran out, before a block gives its shared and tensor memory back: time for the copies
+// and MMAs that it still has in flight, whose barriers may never complete any more (a copy takes
+// microseconds; 1 ms by the clock, and a bounded number of looks at it).
+__device__ __forceinline__ void settle_in_flight()
+{
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    for (int i = 0; i < 1 << 16; ++i) {
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+        if (t - t0 > 1000000ull) break;
+        __nanosleep(1000);
+    }
+}
+
 // K-major, no-swizzle shared-memory matrix descriptor: 8-row groups `sbo` bytes apart, the two
 // 16-byte K chunks of one MMA `lbo` bytes apart (descriptor version 1 = sm_100).
 __device__ __forceinline__ uint64_t umma_desc(uint32_t smem_addr, uint32_t lbo, uint32_t sbo)
