@@ -249,13 +249,17 @@ int stmoe_set_copy_throttle(stmoe_t *s, int64_t chunk_bytes, int gap_us);
  *   HOST_WAIT_MS ms   limit of the host's wait for a layer's routing (default 20000); when it
  *                     runs out the step returns STMOE_ERR_TIMEOUT
  * Any stack: POLL_LIMIT n = polls after which a grid-barrier wait of the single-sequence
- * persistent kernel gives up (default 2^22). */
+ * persistent kernel gives up (default 2^22).
+ * No stack (s NULL): MX4_POLL_LIMIT n = polls, of about 4 us each, after which a wait inside the MX4
+ * product and FFN kernels gives up, in every launch of the process from then on (default and most 2^22;
+ * 0: at once; a captured graph keeps the limit it was captured with). */
 #define STMOE_HOOK_DROP_PREFETCH 1
 #define STMOE_HOOK_FAIL_COPY 2
 #define STMOE_HOOK_DELAY_COPY_US 3
 #define STMOE_HOOK_CORRUPT_TAG 4
 #define STMOE_HOOK_HOST_WAIT_MS 5
 #define STMOE_HOOK_POLL_LIMIT 6
+#define STMOE_HOOK_MX4_POLL_LIMIT 7
 int stmoe_test_hook(stmoe_t *s, int what, int64_t value);
 
 /* Runs the bounded waits of the persistent kernels on barriers that nobody completes, with a poll

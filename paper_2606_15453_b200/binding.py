@@ -22,6 +22,7 @@ FLAG_NO_PERSISTENT = 2
 FLAG_NO_DENSE = 4
 FLAG_NO_FUSED = 8
 HOOK_DROP_PREFETCH, HOOK_FAIL_COPY, HOOK_DELAY_COPY_US, HOOK_CORRUPT_TAG, HOOK_HOST_WAIT_MS, HOOK_POLL_LIMIT = 1, 2, 3, 4, 5, 6
+HOOK_MX4_POLL_LIMIT = 7
 
 
 class StmoeError(RuntimeError):
@@ -435,6 +436,11 @@ def mx4_expert(gate, up, down, stream=None):
         parts[name] = image[i * nc:(i + 1) * nc].view(r, c // 2)
         mx4_quantize(w, parts[name], image[3 * nc + i * ns:3 * nc + (i + 1) * ns].view(r, c // 32))
     return parts
+
+
+def mx4_poll_limit(polls: int) -> None:
+    """For tests: polls after which a wait inside the MX4 kernels gives up (STMOE_HOOK_MX4_POLL_LIMIT)."""
+    _check(lib().stmoe_test_hook(None, HOOK_MX4_POLL_LIMIT, int(polls)), "stmoe_test_hook")
 
 
 def mx4_matmul(a, b, counts=None, dtype=torch.bfloat16, out=None, flags=None, stream=None):

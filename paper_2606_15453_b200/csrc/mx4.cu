@@ -197,7 +197,7 @@ int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_
     Mx4MatmulArgs a{};
     a.a_scales = a_scales, a.b_scales = b_scales, a.a_scale_stride = a_scale_stride, a.b_scale_stride = b_scale_stride;
     a.counts = counts, a.groups = n_groups, a.m = (int)m, a.n = n, a.blocks = k_blocks;
-    a.out = out, a.out_stride = out_stride, a.err = flags;
+    a.out = out, a.out_stride = out_stride, a.err = flags, a.polls = g_mx4_polls.load(std::memory_order_relaxed);
     a.out_wide = ((uintptr_t)out & 15) == 0 && (m == 1 || (out_stride * elem_bytes(out_dtype)) % 16 == 0);
     const auto align = [](const void *p, int64_t stride) {
         const uint64_t bits = (uint64_t)(uintptr_t)p | (uint64_t)stride;

@@ -29,8 +29,13 @@
 // reduction is split over a cluster of CTAs that exchange their partial sums through distributed
 // shared memory and add them in the order of the ranks (no workspace, no atomics, the same bits
 // every time).
-// Every wait is bounded; where one runs out the error word is set and the affected outputs are NaN.
+// Every wait is bounded; where one runs out the error word is set and the affected outputs are NaN: the
+// loaders, the scale warps and the MMA warp stop, and an epilogue warp that has given up walks the tasks
+// that are left and writes NaN.  It arrives at no barrier of the pipeline any more, so no accumulator is
+// overwritten under a warp that still reads it, and it meets the others at every barrier of theirs.
 #pragma once
+#include <atomic>
+
 #include "mx4.cuh"
 #include "tcgen05_utils.cuh"
 
@@ -65,6 +70,9 @@ __host__ __device__ constexpr int mm_stages(int bn)
 // it is never two phases ahead of a barrier, whose parity would then deceive it
 static_assert(mm_stages(16) >= 4 && mm_stages(128) >= 4 && mm_stages(kMmMaxTokens) >= 4, "");
 
+// Polls after which a wait gives up, for the launches to come (tests lower it).
+inline std::atomic<int> g_mx4_polls{kDenseSpinLimit};
+
 struct Mx4MatmulArgs {
     const uint8_t *a_scales, *b_scales;
     long long a_scale_stride, b_scale_stride;  // bytes
@@ -77,6 +85,7 @@ struct Mx4MatmulArgs {
     bool out_wide;          // rows of out start on 16-byte boundaries
     unsigned *err;          // may be nullptr
     int a_align, b_align;   // what scale rows are aligned to: 8, 4 or 1 bytes
+    int polls;              // limit of every wait
 };
 
 // mxf4 descriptor: e2m1 x e2m1, e8m0 scales, both K-major, M = 128, N = n; which half of a scale
@@ -351,7 +360,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             for (int task = first; task < n_tasks && !*dead; task += step) {
                 const Mx4Task t = mm_task(a, s_off, s_tile, task);
                 for (int k = k_beg; k < k_end; ++k, ++issued) {
-                    if (!dmbar_wait(&empty[s], par ^ 1u, dead)) break;
+                    if (!dmbar_wait(&empty[s], par ^ 1u, dead, a.polls)) break;
                     uint8_t *st = dsm + (size_t)s * slot;
                     dmbar_expect_tx(&full[s], (uint32_t)(kMmABytes + bn * 128));
                     tma_load_2d(st, &map_b, k * 128, t.expert * a.n + t.row0, &full[s]);
@@ -380,11 +389,11 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         bool ok = true;
         for (int task = first; task < n_tasks && ok; task += step, ++it) {
             const int ab = it & 1;
-            if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)))) break;
+            if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead, a.polls)))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + ab * kMmAccStride;
             for (int k = k_beg; k < k_end; ++k) {
-                if (!(ok = __all_sync(kFull, dmbar_wait(&full[s], par, dead)))) break;
+                if (!(ok = __all_sync(kFull, dmbar_wait(&full[s], par, dead, a.polls)))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t st = ring + s * slot;
                 const uint32_t sf = tmem + kMmScaleCol + s * cols;  // this stage's set of scale columns
@@ -409,10 +418,11 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     } else if (warp < 6) {
         const int lg = warp % 4;  // the quarter of the lanes this warp may read
         int it = 0;
+        bool ok = true;
         for (int task = first; task < n_tasks; task += step, ++it) {
             const int ab = it & 1;
             const Mx4Task t = mm_task(a, s_off, s_tile, task);
-            const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], (uint32_t)(it >> 1) & 1u, dead));
+            ok = ok && __all_sync(kFull, dmbar_wait(&tfull[ab], (uint32_t)(it >> 1) & 1u, dead, a.polls));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + ab * kMmAccStride + ((uint32_t)(lg * kWarp) << 16);
             const int row = t.row0 + lg * kWarp + lane;
@@ -459,6 +469,8 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 }
             } else {
                 // the ring is idle once the last MMA has been committed: the partial tile takes its place
+                // (NaN, where that was not waited for, once nothing can land on top of it)
+                if (!ok) settle_in_flight();
                 float *part = reinterpret_cast<float *>(dsm);
                 for (int j0 = 0; j0 < bn; j0 += 16) {
                     float v[16];
@@ -469,8 +481,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) dmbar_arrive(&tempty[ab]);
-            if (!ok) break;
+            if (ok && lane == 0) dmbar_arrive(&tempty[ab]);
         }
     } else {
         // scales: this warp's stages are the CTA's steps w, w + 4, ... across its tasks
@@ -495,7 +506,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         uint32_t i = w;
         auto put = [&](const uint2 (&vb)[4], const uint2 (&va)[6]) {   // step i
             const int s = (int)(i % NS);
-            const bool ok = __all_sync(kFull, dmbar_wait(&empty[s], ((i / NS) & 1u) ^ 1u, dead));
+            if (!__all_sync(kFull, dmbar_wait(&empty[s], ((i / NS) & 1u) ^ 1u, dead, a.polls))) return false;   // its place may be in use
             uint8_t *st = dsm + (size_t)s * slot;
             store_scales<4>(st + sfa_at, 512, lane, vb);
             if (atoms == 1) {
@@ -508,7 +519,7 @@ mx4_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             __syncwarp();
             if (lane == 0) dmbar_arrive(&full[s]);
             i += 4;
-            return ok;
+            return true;
         };
         // two sets of registers in turn: copying one into the other would wait for its loads
         uint2 b0[4], a0[6], b1[4], a1[6];

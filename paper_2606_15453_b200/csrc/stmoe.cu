@@ -1737,6 +1737,11 @@ int stmoe_set_copy_throttle(stmoe_t *s, int64_t chunk_bytes, int gap_us)
 
 int stmoe_test_hook(stmoe_t *s, int what, int64_t value)
 {
+    if (what == STMOE_HOOK_MX4_POLL_LIMIT) {   // of the process: the product has no stack
+        if (s || value < 0) return STMOE_ERR_BAD_ARG;
+        g_mx4_polls.store((int)std::min<int64_t>(value, kDenseSpinLimit), std::memory_order_relaxed);
+        return STMOE_OK;
+    }
     if (!s || value < 0 || s->next_layer != 0) return STMOE_ERR_BAD_ARG;
     if (what != STMOE_HOOK_POLL_LIMIT && !offloaded(s)) return STMOE_ERR_BAD_ARG;
     switch (what) {

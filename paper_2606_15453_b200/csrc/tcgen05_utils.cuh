@@ -61,8 +61,9 @@ __device__ __forceinline__ bool dmbar_wait(uint64_t *bar, uint32_t parity, volat
 
 // Behind a wait that ran out, before a block gives its shared and tensor memory back: time for the copies
 // and MMAs that it still has in flight, whose barriers may never complete any more (a copy takes
-// microseconds; 1 ms by the clock, and a bounded number of looks at it).
-__device__ __forceinline__ void settle_in_flight()
+// microseconds; 1 ms by the clock, and a bounded number of looks at it).  Not inlined: kernels that it is
+// never called in pay for every line of code that they fetch.
+inline __device__ __noinline__ void settle_in_flight()
 {
     unsigned long long t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));

@@ -94,3 +94,9 @@ def test_binding_refuses_before_the_library():
                  lambda: P.router_balance(x, torch.zeros(4, 2, dtype=torch.int32))):
         with pytest.raises(P.StmoeError):
             call()
+
+
+def test_mx4_poll_limit_is_set_without_a_stack():
+    hook = P.lib().stmoe_test_hook
+    assert hook(None, 7, -1) == BAD and hook(X, 7, 4) == BAD and hook(None, 6, 4) == BAD
+    assert hook(None, 7, 16) == 0 and hook(None, 7, 1 << 40) == 0      # the second: back to the default
