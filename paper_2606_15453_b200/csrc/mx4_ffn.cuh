@@ -266,6 +266,7 @@ struct Mx4FfnArgs {
     // down
     float *part;                         // [pair][splits][rows]
     unsigned *err;
+    int polls;                           // limit of every wait
 };
 
 struct Mx4FfnTask {
@@ -364,7 +365,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
                 int k_beg, k_end;
                 k_range(t.z, k_beg, k_end);
                 for (int k = k_beg; k < k_end; ++k, ++issued) {
-                    if (!dmbar_wait(&empty[s], par ^ 1u, dead)) break;
+                    if (!dmbar_wait(&empty[s], par ^ 1u, dead, a.polls)) break;
                     uint8_t *st = dsm + (size_t)s * slot;
                     dmbar_expect_tx(&full[s], (uint32_t)(NMAT * kMmABytes));
                     tma_load_3d(st, w0, k * 128, t.row0, img, &full[s]);
@@ -396,13 +397,13 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             count = __ldcg(&a.entries[min(task + step, a.last_task) / per_entry].count);   // the next task's
             const uint32_t id0 = umma_idesc_mxf4(n, 0), id1 = umma_idesc_mxf4(n, 1);
             const int ab = it & 1;
-            if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead)))) break;
+            if (!(ok = __all_sync(kFull, dmbar_wait(&tempty[ab], ((uint32_t)(it >> 1) & 1u) ^ 1u, dead, a.polls)))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + ab * kMxfAccStride;
             int k_beg, k_end;
             k_range(t.z, k_beg, k_end);
             for (int k = k_beg; k < k_end; ++k) {
-                if (!(ok = __all_sync(kFull, dmbar_wait(&full[s], par, dead)))) break;
+                if (!(ok = __all_sync(kFull, dmbar_wait(&full[s], par, dead, a.polls)))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t st = ring + s * slot;
                 const uint32_t sf = tmem + kMxfScaleCol + s * kSetCols, sfb = sf + 8 * NMAT;
@@ -430,13 +431,15 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
         const int lg = warp % 4, ab = (warp - 2) / 4;   // quarter of the lanes, accumulator buffer
         float *part = reinterpret_cast<float *>(dsm);   // cluster: this rank's sums [mat][token][128], in the idle ring
         uint32_t use = 0;
+        bool ok = true;   // once false, this warp's tasks that are left are NaN (see mx4_matmul.cuh)
         for (int task = first + ab * step; task < n_tasks; task += 2 * step, ++use) {
             const Mx4FfnTask t = mxf_task<NMAT>(a, task);
             const Mx4Entry &en = a.entries[t.g];
             const int cnt = __ldcg(&en.count), own = min(lane, kMxfTokens - 1);
             const int slot_l = __ldcg(&en.slot[own]);      // lane i: the i-th pair's, fetched while the MMAs run
             const float inv_l = en.inv[own];
-            const bool ok = __all_sync(kFull, dmbar_wait(&tfull[ab], use & 1u, dead));
+            ok = ok && __all_sync(kFull, dmbar_wait(&tfull[ab], use & 1u, dead, a.polls));
+            if (NMAT == 2 && ranks > 1 && !ok) settle_in_flight();   // its sums take the ring's place
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + ab * kMxfAccStride + ((uint32_t)(lg * kWarp) << 16);
             const int row = t.row0 + lg * kWarp + lane;
@@ -477,8 +480,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) dmbar_arrive(&tempty[ab]);
-            if (!ok) break;
+            if (ok && lane == 0) dmbar_arrive(&tempty[ab]);
         }
     } else {
         // scales and the tokens' codes, a warp every fourth stage (see mx4_matmul.cuh; up to twelve loads a
@@ -546,7 +548,7 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             forward(p, 4);
             if (p.task < n_tasks) load_w(p, nw), load_x(p, nx);
             const int s = i % NS;
-            const bool ok = __all_sync(kFull, dmbar_wait(&empty[s], ((uint32_t)(i / NS) & 1u) ^ 1u, dead));
+            if (!__all_sync(kFull, dmbar_wait(&empty[s], ((uint32_t)(i / NS) & 1u) ^ 1u, dead, a.polls))) break;   // its place may be in use
             uint8_t *st = dsm + (size_t)s * slot;
 #pragma unroll
             for (int m = 0; m < NMAT; ++m) {
@@ -556,7 +558,6 @@ mx4_ffn_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             store_scales<3>(st + sfb_at, 512, lane, vx);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (!ok) break;   // nothing is waited for any more, and nothing may be loaded behind the drain
             const uint32_t xst = dsmem_u32(st + x_at);
             if (elect_one()) dmbar_expect_tx(&full[s], (uint32_t)(cnt * kPlanes * 128));
             for (int q = 0; q < cnt; ++q) {

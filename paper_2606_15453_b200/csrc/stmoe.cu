@@ -488,6 +488,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
     g.scale_off[0] = (long long)mx4_image_scales(H, I, 0), g.scale_off[1] = (long long)mx4_image_scales(H, I, 1);
     g.rows = I, g.blocks = H / kMxBlock, g.mt = mt;
     g.x_scales = b.x_scales, g.act_codes = b.act_codes, g.act_scales = b.act_scales, g.err = err;
+    g.polls = g_mx4_polls.load(std::memory_order_relaxed);
     const int gu_steps = (g.blocks + kMmStageBlocks - 1) / kMmStageBlocks;
     const int gu_tasks = entries * ((I + kMmRows - 1) / kMmRows);
     g.last_task = gu_tasks - 1;
