@@ -436,7 +436,8 @@ int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_
  *   counts[e] = how often e stands in ids of those rows;  f_e = counts[e] / (n top_k);
  *   loss[0] = n_experts * sum_e f_e * (1/n) sum_t p_te;   loss[1] = (1/n) sum_t lse_t^2.
  * A row does not count where its mask byte is 0 (it may then hold anything, NaN included) or where
- * all its logits are -infinity.  With n = 0 everything is 0.
+ * all its logits are -infinity; a row filled with any finite value counts, with uniform p.  A NaN or
+ * +infinity in a row that counts makes both losses and the row's gradient NaN.  With n = 0 everything is 0.
  *   logits   [tokens][n_experts] in dtype (STMOE_F32, STMOE_BF16, STMOE_F16), stride in elements
  *   ids      int32 [tokens][top_k]; entries outside [0, n_experts) (-1 for a dropped choice) are not
  *            counted, an expert that stands twice in a row counts twice

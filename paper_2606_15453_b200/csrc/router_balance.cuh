@@ -14,10 +14,12 @@
 // maximum, sum and probabilities, and a row of 8 experts does not leave 31 lanes idle.  What competes
 // with the loads is issue slots: with eight logits a lane, library reciprocal and logarithm and 64-bit
 // row arithmetic the forward kernel issued 210 instructions per two rows of 128 experts and took 92 us
-// for 524288 rows that HBM delivers in 23.  The exponential is exp2 of one fused multiply-add per logit
-// (relative error 2^-22 for the terms that matter; the row's sum is formed from the same rounded
-// exponents, so a common error of the maximum cancels); reciprocal and logarithm of the sum, which lies
-// in [1, 256], are the hardware's (2^-23 relative, 2^-22 absolute).
+// for 524288 rows that HBM delivers in 23.  The exponential is exp2 of one fused multiply-add per logit,
+// z log2(e) - fl(m log2(e)) with m the row's maximum (relative error 2^-22 for the terms that matter; the
+// row's sum is formed from the same exponents, so what the rounded product of m is off by, less than 0.1
+// up to |m| = 2^20, cancels).  Beyond that it would become an exponent of its own and then overflow, so such
+// rows, a mask's fill value as a rule, have m subtracted first.  Reciprocal and logarithm of the sum, which
+// lies in [0.9, 280], are the hardware's (2^-23 relative, 2^-22 absolute).
 // Sums over tokens: a lane adds the probabilities of its experts in fp32 over the few hundred rows it
 // sees, a CTA adds its lanes in a fixed order, and the CTAs' partial sums are added in fp64 in a fixed
 // order by a second launch: no floating-point atomics, the same bits every time.
@@ -32,6 +34,7 @@ constexpr int kBalRows = 2;         // rows of a lane in flight
 constexpr int kBalDepth = 3;        // steps of rows in shared memory: one in use, two under way
 constexpr int kBalFinish = 8;       // CTAs of the cluster that adds the partial sums up
 constexpr int kBalMaxCtas = 592;   // four a SM: rows of the partial-sum workspace
+constexpr float kBalPlainMax = 1048576.f;   // 2^20: largest |maximum| of a row without a subtraction of its own
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // a CTA's partial sums: [E] probabilities, lse^2, then (int) [E] counts, rows
@@ -156,7 +159,15 @@ template <int LPR, int P> __device__ __forceinline__ float bal_softmax(float2 (&
 #pragma unroll
     for (int i = 1; i < P; ++i) m = fmaxf(m, fmaxf(z[i].x, z[i].y));
     m = lanes_max<LPR>(m);
-    const float m2 = m == -INFINITY ? 0.f : m * kLog2e;
+    if (m == -INFINITY) m = 0.f;
+    float shift = 0.f;
+    // a branch of the whole warp (one of the row's lanes cost 3 % of 524288 x 128, this one 0.8 %)
+    if (__any_sync(kFull, fabsf(m) > kBalPlainMax)) {
+        if (fabsf(m) > kBalPlainMax) shift = m, m = 0.f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) z[i] = add2(z[i], make_float2(-shift, -shift));
+    }
+    const float m2 = m * kLog2e;
     const float2 k = make_float2(kLog2e, kLog2e), off = make_float2(-m2, -m2);
     float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
@@ -168,7 +179,7 @@ template <int LPR, int P> __device__ __forceinline__ float bal_softmax(float2 (&
     const float sum = lanes_sum<LPR>(s2.x + s2.y);
     live = sum != 0.f;   // 0 where all logits are -infinity (a NaN is not 0)
     inv = __fdividef(1.f, sum);
-    return (m2 + __log2f(sum)) * kLn2;
+    return fmaf(m2 + __log2f(sum), kLn2, shift);
 }
 
 // How rows are read: element by element; 16 bytes at a time; the same with no lane past the last expert
