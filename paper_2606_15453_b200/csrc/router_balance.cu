@@ -40,9 +40,14 @@ int64_t bal_steps(int64_t tokens, int lpr)
     const int64_t rows = (int64_t)(kBalThreads / kWarp) * (kWarp / lpr) * kBalRows;
     return (tokens + rows - 1) / rows;
 }
+// CTAs that a batch is spread over where each has few steps: rows of the workspace, which knows no device
+constexpr int kBalOnceCtas = 592;
 // Up to kBalAlone steps are left to one CTA, which needs no second launch to add partial sums up.
 constexpr int64_t kBalAlone = 2;
-int bal_grid(int64_t tokens, int lpr)
+// CTAs that it takes for no lane to add more than kBalLaneSteps steps of rows in fp32
+int64_t bal_least_ctas(int64_t steps) { return (steps + kBalLaneSteps - 1) / kBalLaneSteps; }
+// three CTAs an SM (launch bounds); forward: whole multiples of that where rows are many
+int bal_grid(int64_t tokens, int lpr, bool backward)
 {
     const int64_t steps = bal_steps(tokens, lpr);
     if (steps <= kBalAlone) return 1;
@@ -51,7 +56,8 @@ int bal_grid(int64_t tokens, int lpr)
         (void)cudaGetLastError();
         return 0;
     }
-    return (int)std::min<int64_t>({steps, (int64_t)sms * 3, kBalMaxCtas});   // three CTAs an SM (launch bounds)
+    const int64_t once = std::min<int64_t>(steps, std::min(sms * 3, kBalOnceCtas));
+    return (int)(backward ? once : (bal_least_ctas(steps) + once - 1) / once * once);
 }
 
 // Launch that may start while the kernel before it in the stream drains (the kernels wait for it
@@ -120,7 +126,9 @@ extern "C" {
 size_t stmoe_router_balance_scratch_bytes(int64_t tokens, int n_experts)
 {
     if (n_experts < 1 || n_experts > kBalMaxExperts || tokens < 1 || bal_steps(tokens, lanes_per_row(n_experts)) <= kBalAlone) return 0;
-    return sizeof(float) * (size_t)kBalMaxCtas * bal_part_words(n_experts);
+    // the multiple that the grid is rounded up to depends on the device
+    const int64_t rows = bal_least_ctas(bal_steps(tokens, lanes_per_row(n_experts))) + kBalOnceCtas;
+    return sizeof(float) * (size_t)rows * bal_part_words(n_experts);
 }
 
 int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const int32_t *ids, const uint8_t *mask, int64_t tokens,
@@ -131,7 +139,7 @@ int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const in
         return STMOE_ERR_BAD_ARG;
     const size_t need = stmoe_router_balance_scratch_bytes(tokens, n_experts);
     if (need && (!scratch || ((uintptr_t)scratch & 3) || scratch_bytes < need)) return STMOE_ERR_BAD_ARG;
-    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr);
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, false);
     if (!grid) return STMOE_ERR_CUDA;
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.ids = ids, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
@@ -152,7 +160,7 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
         return STMOE_ERR_BAD_ARG;
     if (tokens == 0) return STMOE_OK;
     if (overlap(logits, stride, grad_logits, grad_stride, tokens, n_experts, dtype)) return STMOE_ERR_BAD_ARG;
-    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr);
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, true);
     if (!grid) return STMOE_ERR_CUDA;
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;

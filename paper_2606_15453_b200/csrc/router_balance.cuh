@@ -20,9 +20,12 @@
 // up to |m| = 2^20, cancels).  Beyond that it would become an exponent of its own and then overflow, so such
 // rows, a mask's fill value as a rule, have m subtracted first.  Reciprocal and logarithm of the sum, which
 // lies in [0.9, 280], are the hardware's (2^-23 relative, 2^-22 absolute).
-// Sums over tokens: a lane adds the probabilities of its experts in fp32 over the few hundred rows it
-// sees, a CTA adds its lanes in a fixed order, and the CTAs' partial sums are added in fp64 in a fixed
-// order by a second launch: no floating-point atomics, the same bits every time.
+// Sums over tokens: a lane adds the probabilities of its experts in fp32 over at most 256 rows (batches that
+// would give it more have more CTAs), a CTA adds its lanes in a fixed order, and the CTAs' partial sums are
+// added in fp64 in a fixed order by a second launch: no floating-point atomics, the same bits every time, and
+// an error that does not grow with the tokens.  (Moving a lane's sums to fp64 inside the loop took nine
+// registers that the loads need: 91.4 -> 93.9 us for 524288 x 128.)  lse^2 is summed in fp64 throughout: a
+// row at a fill value of 1e20 has one that fp32 does not hold, while the mean over the rows may.
 #pragma once
 #include "mx4.cuh"
 
@@ -33,12 +36,13 @@ constexpr int kBalMaxExperts = 256;
 constexpr int kBalRows = 2;         // rows of a lane in flight
 constexpr int kBalDepth = 3;        // steps of rows in shared memory: one in use, two under way
 constexpr int kBalFinish = 8;       // CTAs of the cluster that adds the partial sums up
-constexpr int kBalMaxCtas = 592;   // four a SM: rows of the partial-sum workspace
+constexpr int kBalLaneSteps = 128; // steps of a CTA at most: so many times kBalRows rows a lane
 constexpr float kBalPlainMax = 1048576.f;   // 2^20: largest |maximum| of a row without a subtraction of its own
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// a CTA's partial sums: [E] probabilities, lse^2, then (int) [E] counts, rows
-__host__ __device__ inline int bal_part_words(int E) { return 2 * (E + 1); }
+// a CTA's partial sums: [E] probabilities, the low word of lse^2 (fp64), then (int) [E] counts, rows, and
+// the high word
+__host__ __device__ inline int bal_part_words(int E) { return 2 * (E + 1) + 1; }
 
 struct BalanceArgs {
     const void *logits;
@@ -314,7 +318,7 @@ template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(k
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ int s_cnt[kBalMaxExperts];
     __shared__ float s_p[W][LPR * N];
-    __shared__ float s_z[W];
+    __shared__ double s_z[W];
     __shared__ int s_n[W];
     __shared__ double s_bal[W];
     const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp, l = lane % LPR, sub = lane / LPR;
@@ -325,7 +329,7 @@ template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(k
     float2 p[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) p[i] = make_float2(0.f, 0.f);
-    float zz = 0.f;
+    double zz = 0.;
     int n = 0;
     BalWalk<DT, LPR, N, kRead, true> w(a, warp, sub, l, ring);
     while (w.more(a, sub)) {
@@ -347,7 +351,7 @@ template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(k
                 const float2 inv2 = make_float2(inv, inv);
 #pragma unroll
                 for (int i = 0; i < N / 2; ++i) p[i] = fma2(z[i], inv2, p[i]);
-                if (l == 0) zz = fmaf(lse, lse, zz), ++n;
+                if (l == 0) zz = fma((double)lse, (double)lse, zz), ++n;
                 if ((unsigned)id < (unsigned)a.E) atomicAdd(&s_cnt[id], 1);
                 for (int k = l + LPR; k < a.K; k += LPR) {
                     const int e = a.ids[(long long)(w.t + r * (kWarp / LPR)) * a.K + k];
@@ -375,15 +379,18 @@ template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(k
     if (gridDim.x > 1) {
         float *part = a.part + (size_t)blockIdx.x * bal_part_words(a.E);
         int *ipart = reinterpret_cast<int *>(part) + a.E + 1;
-        for (int e = tid; e <= a.E; e += kBalThreads) {
+        for (int e = tid; e < a.E; e += kBalThreads) {
             float v = 0.f;
-            int c = 0;
-            for (int q = 0; q < W; ++q) {
-                v += e < a.E ? s_p[q][e] : s_z[q];
-                if (e == a.E) c += s_n[q];
-            }
+            for (int q = 0; q < W; ++q) v += s_p[q][e];
             part[e] = v;
-            ipart[e] = e < a.E ? s_cnt[e] : c;
+            ipart[e] = s_cnt[e];
+        }
+        if (tid == 0) {
+            double v = 0.;
+            int c = 0;
+            for (int q = 0; q < W; ++q) v += s_z[q], c += s_n[q];
+            part[a.E] = __int_as_float(__double2loint(v));
+            ipart[a.E] = c, ipart[a.E + 1] = __double2hiint(v);
         }
         return;
     }
@@ -401,7 +408,7 @@ template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(k
     if (tid == 0) {
         double sum = 0., sq = 0.;
         int rows = 0;
-        for (int q = 0; q < W; ++q) sum += s_bal[q], sq += (double)s_z[q], rows += s_n[q];
+        for (int q = 0; q < W; ++q) sum += s_bal[q], sq += s_z[q], rows += s_n[q];
         bal_write(a, sum, sq, rows);
     }
 }
@@ -422,16 +429,17 @@ __global__ void __launch_bounds__(1024) router_balance_finish_kernel(const Balan
     if (g < G)
         for (int b0 = rank + kBalFinish * g; b0 < a.ctas; b0 += 8 * kBalFinish * G) {   // eight rows' words in flight
             float x[8];
-            int y[8];
+            int y[8], hi[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int b = b0 + j * kBalFinish * G;
                 const float *part = a.part + (size_t)b * words;
-                x[j] = 0.f, y[j] = 0;
+                x[j] = 0.f, y[j] = hi[j] = 0;
                 if (b < a.ctas) x[j] = __ldcg(part + e), y[j] = __ldcg(reinterpret_cast<const int *>(part) + cols + e);
+                if (b < a.ctas && e == a.E) hi[j] = __ldcg(reinterpret_cast<const int *>(part) + cols + e + 1);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v += (double)x[j], c += y[j];
+            for (int j = 0; j < 8; ++j) v += e == a.E ? __hiloint2double(hi[j], __float_as_int(x[j])) : (double)x[j], c += y[j];
         }
     s_sum[tid] = v, s_int[tid] = c;
     __syncthreads();

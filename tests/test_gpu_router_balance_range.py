@@ -111,3 +111,38 @@ def test_large_batch_with_rows_at_fill_values():
         z, ids = _ordinary(4, 6000, 64, 4, dt)
         z[::7] = fill
         _check(z, ids, (6000.0, 0.0), dt)
+
+
+@pytest.mark.parametrize("fill", [-1e19, 1e19, 3e20])
+def test_z_loss_is_finite_where_its_mean_is(fill):
+    """lse^2 of one row passes the largest fp32 value, its mean over the rows does not."""
+    for T in (300, 9000):                                     # one CTA, and many with the second launch
+        z, ids = _ordinary(6, T, 16, 2, "f32")
+        z[T // 2, :] = fill if abs(fill) < 1e20 else 0.
+        z[3, 5] = fill
+        loss = _formula(z, ids, (0.0, 0.0))[0]
+        got = P.router_balance(z.to(DEV), ids.to(DEV))["loss"].double().cpu()
+        if loss[1] < F32_MAX:
+            assert abs(got[1] - loss[1]) <= 4 * P_TOL * loss[1]
+        else:
+            assert got[1] == math.inf
+        assert abs(got[0] - loss[0]) <= 4 * P_TOL * loss[0]
+
+
+@pytest.mark.parametrize("logit", [1.5625, 3.0625, 3.5])
+def test_losses_do_not_drift_with_the_tokens(logit):
+    """2^28 equal rows; with all of an SM's CTAs at work once, 2362 to a lane.  Added one by one in fp32 their
+    probability drifts by 3.2e-5 (the same rounding every time: followed on the CPU).  In groups of 256 rows it may
+    drift by 255 2^-24, then 5 additions of lanes, 8 of warps and the store of a CTA's sum, 2^-24 each, on top of
+    the probability's own 2^-20 (a row's exponents are below 6, where 2^-22 of exp2 and a few 2^-24 are all there
+    is); an lse is off by 2^-21."""
+    T, E = 1 << 28, 8
+    row = torch.zeros(E, dtype=torch.bfloat16, device=DEV)
+    row[0] = logit
+    z = row.repeat(T, 1)
+    f = P.router_balance(z, torch.zeros(T, 1, dtype=torch.int32, device=DEV))
+    p, lse = math.exp(logit) / (math.exp(logit) + 7), math.log(math.exp(logit) + 7)
+    assert f["rows"].item() == T and f["counts"].tolist() == [T] + [0] * 7
+    got = f["loss"].double().cpu()
+    assert abs(got[0] - 8 * p) <= (269 * 2.0 ** -24 + 2.0 ** -20) * 8 * p
+    assert abs(got[1] - lse ** 2) <= 2 * lse * 2.0 ** -21 + 2.0 ** -23 * lse ** 2

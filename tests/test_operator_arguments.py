@@ -100,3 +100,13 @@ def test_mx4_poll_limit_is_set_without_a_stack():
     hook = P.lib().stmoe_test_hook
     assert hook(None, 7, -1) == BAD and hook(X, 7, 4) == BAD and hook(None, 6, 4) == BAD
     assert hook(None, 7, 16) == 0 and hook(None, 7, 1 << 40) == 0      # the second: back to the default
+
+
+def test_balance_scratch_grows_with_the_tokens_and_never_falls():
+    f = P.lib().stmoe_router_balance_scratch_bytes
+    for E in (2, 8, 9, 64, 100, 256):
+        sizes = [f(t, E) for t in sorted({1 << i for i in range(31)} | {(1 << i) + 7 for i in range(30)})]
+        assert sizes == sorted(sizes)
+        # one row of sums, 2 E + 3 words, to every 256 rows of a lane at most: 256 lanes' worth of rows a CTA
+        lanes = next(l for l in (1, 2, 4, 8, 16) if 16 * l >= E)
+        assert sizes[-1] >= 4 * (2 * E + 3) * ((1 << 30) // (256 * 256 // lanes))
