@@ -524,13 +524,16 @@ template <int DT, int LPR, int N, int kRead> __global__ void __launch_bounds__(k
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) d2 = fma2(f[i], z[i], d2);
             const float dot = lanes_sum<LPR>(d2.x + d2.y);
-            // dz = p (gb f + c), c = gz lse - gb dot, p = z inv; rows that do not count have z = 0
-            float c = gz * lse - dot * inv;
-            if (!(on >> r & 1) || !live) inv = 0.f, c = 0.f;
+            // dz = p (gb f + c), c = gz lse - gb dot, p = z inv
+            const float c = gz * lse - dot * inv;
             const float2 inv2 = make_float2(inv, inv), c2 = make_float2(c * inv, c * inv);
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) z[i] = mul2(z[i], fma2(f[i], inv2, c2));
             if (w.t + r * RPW >= (uint32_t)a.T) continue;
+            if (!(on >> r & 1) || !live) {   // 0 whatever the losses' gradient is: an infinite one times 0 is NaN
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) z[i] = make_float2(0.f, 0.f);
+            }
             T *o = out + r * d_row;
             if constexpr (kVec) {
 #pragma unroll

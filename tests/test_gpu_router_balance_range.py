@@ -146,3 +146,23 @@ def test_losses_do_not_drift_with_the_tokens(logit):
     got = f["loss"].double().cpu()
     assert abs(got[0] - 8 * p) <= (269 * 2.0 ** -24 + 2.0 ** -20) * 8 * p
     assert abs(got[1] - lse ** 2) <= 2 * lse * 2.0 ** -21 + 2.0 ** -23 * lse ** 2
+
+
+@pytest.mark.parametrize("grad", [(math.inf, 1.0), (1.0, -math.inf), (math.nan, 1.0), (1.0, math.nan), (math.inf, math.inf)])
+@pytest.mark.parametrize("dt,E", [("f32", 12), ("f32", 7), ("bf16", 64), ("f16", 16), ("bf16", 200)])
+def test_rows_that_do_not_count_have_zero_gradient_whatever_the_losses_have(dt, E, grad):
+    """An overflowed loss scale, for example: padding stays out of what the caller's network sees."""
+    z, ids = _ordinary(8, 70, E, 2, dt)
+    mask = torch.ones(70, dtype=torch.bool)
+    mask[1::3] = False
+    z[1] = math.nan
+    z[2::9] = -math.inf
+    f = P.router_balance(z.to(DEV), ids.to(DEV), mask=mask.to(DEV))
+    out = torch.full((70, E), 3.0, dtype=z.dtype, device=DEV)
+    P.router_balance_backward(z.to(DEV), f, torch.tensor(grad, device=DEV), mask=mask.to(DEV), out=out)
+    counts = mask & (z != -math.inf).any(1)
+    assert (out[~counts.to(DEV)] == 0).all()
+    assert not out[counts.to(DEV)].isfinite().all()
+    f = P.router_balance(z.to(DEV), ids.to(DEV), mask=torch.zeros_like(mask).to(DEV))
+    P.router_balance_backward(z.to(DEV), f, torch.tensor(grad, device=DEV), mask=torch.zeros_like(mask).to(DEV), out=out)
+    assert (out == 0).all()
