@@ -507,10 +507,33 @@ def _balance_elem(logits, mask):
     return elem
 
 
+class _RouterBalance(torch.autograd.Function):
+    """router_balance as a step of torch's graph; the gradient is router_balance_backward's."""
+
+    @staticmethod
+    def forward(ctx, logits, ids, mask):
+        f = router_balance(logits, ids, mask)
+        ctx.save_for_backward(logits, mask, f["counts"], f["rows"])
+        ctx.top_k = f["top_k"]
+        ctx.mark_non_differentiable(f["counts"], f["rows"])
+        ctx.set_materialize_grads(False)
+        return f["loss"], f["counts"], f["rows"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss, *_):
+        if grad_loss is None:
+            return None, None, None
+        logits, mask, counts, rows = ctx.saved_tensors
+        f = {"counts": counts, "rows": rows, "top_k": ctx.top_k}
+        return router_balance_backward(logits, f, grad_loss.to(_F32).contiguous(), mask), None, None
+
+
 def router_balance(logits, ids, mask=None, stream=None):
     """stmoe_router_balance: losses and per-expert counts for logits [tokens][n_experts] and the
     chosen experts ids int32 [tokens][top_k] (-1: dropped); mask [tokens]: rows that count.
-    Returns dict(loss fp32 [2] = balance, z; counts int32 [n_experts]; rows int32 [1]; top_k)."""
+    Returns dict(loss fp32 [2] = balance, z; counts int32 [n_experts]; rows int32 [1]; top_k).
+    Where logits require a gradient (and torch records one) the loss carries it, once differentiable."""
     elem = _balance_elem(logits, mask)
     T, E = logits.shape
     if not (ids.dtype == _I32 and ids.dim() == 2 and ids.is_contiguous() and ids.shape[0] == T and ids.device == logits.device):
@@ -519,6 +542,9 @@ def router_balance(logits, ids, mask=None, stream=None):
     st = _stream_of(logits, stream)
     if st is None:
         return _there(logits, stream, router_balance, logits, ids, mask)
+    if logits.requires_grad and torch.is_grad_enabled():
+        loss, counts, rows = _RouterBalance.apply(logits, ids, mask)
+        return {"loss": loss, "counts": counts, "rows": rows, "top_k": K}
     L = lib()
     n = L.stmoe_router_balance_scratch_bytes(T, E)
     dev = logits.device
