@@ -3,64 +3,17 @@
 
 #include <algorithm>
 
+#include "host_utils.cuh"
 #include "mx4.cuh"
 #include "mx4_matmul.cuh"
 
 using namespace stmoe_dev;
+using namespace stmoe_host;
 
 namespace {
 
-#define CU_TRY(expr)                                  \
-    do {                                              \
-        cudaError_t e_ = (expr);                      \
-        if (e_ != cudaSuccess) {                      \
-            (void)cudaGetLastError();                 \
-            return e_ == cudaErrorMemoryAllocation ? STMOE_ERR_OOM : STMOE_ERR_CUDA; \
-        }                                             \
-    } while (0)
-
-constexpr int kMaxDevices = 64;
-
-// SMs of the current device, asked once per device ordinal (a racing fill writes the same value)
-int sm_count(int *dev_out)
-{
-    static int sms[kMaxDevices];
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
-        (void)cudaGetLastError();
-        return 0;
-    }
-    *dev_out = dev;
-    if (!sms[dev]) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return 0;
-        }
-        sms[dev] = n;
-    }
-    return sms[dev];
-}
-
 bool elem_type(int dtype) { return dtype == STMOE_F32 || dtype == STMOE_BF16 || dtype == STMOE_F16; }
 long long elem_bytes(int dtype) { return dtype == STMOE_F32 ? 4 : 2; }
-
-// Launch that may start while the kernel before it in the stream drains (programmatic dependent
-// launch; the kernels wait for it themselves), in clusters of `cluster` CTAs.
-template <typename... P, typename... A>
-int launch_behind(void (*kernel)(P...), int grid, int block, int smem, int cluster, cudaStream_t st, const A &...args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = st;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
-    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
-    CU_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
-    return STMOE_OK;
-}
 
 template <int DT, bool kVec, bool kPack> int launch_rows_as(bool quantize, const Mx4Rows &a, int64_t warps, int sms, cudaStream_t st)
 {
@@ -84,9 +37,8 @@ int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int6
         ((uintptr_t)codes & 3) || ((uintptr_t)x & (elem_bytes(dtype) - 1)))
         return STMOE_ERR_BAD_ARG;
     if (rows == 0) return STMOE_OK;
-    int dev = 0;
-    const int sms = sm_count(&dev);
-    if (!sms) return STMOE_ERR_CUDA;
+    int dev = 0, sms = 0;
+    if (const int rc = current_device(&dev, &sms)) return rc;
     Mx4Rows a{};
     a.x = x, a.codes = codes, a.scales = scales, a.rows = rows, a.cols = cols;
     a.x_stride = x_stride, a.code_stride = code_stride, a.scale_stride = scale_stride;
@@ -104,24 +56,6 @@ int mx4_rows(bool quantize, void *x, int dtype, int64_t rows, int64_t cols, int6
     return launch_rows<4>(quantize, a, tasks, sms, st);
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn()
-{
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void *sym = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = (EncodeTiledFn)sym;
-        (void)cudaGetLastError();
-    }
-    return fn;
-}
-
 // codes [rows][row_bytes]: boxes of 128 bytes x box_rows rows, 128-byte swizzle, zeros outside
 int encode_codes(EncodeTiledFn fn, CUtensorMap *m, const uint8_t *base, int64_t rows, int64_t row_bytes, int64_t stride, int box_rows)
 {
@@ -133,23 +67,16 @@ int encode_codes(EncodeTiledFn fn, CUtensorMap *m, const uint8_t *base, int64_t 
                : STMOE_ERR_CUDA;
 }
 
-// once per device (a racing fill writes the same values): the kernels' shared memory, and how many of
-// their clusters run at a time (the same for the three output types)
+// once per device: the kernels' shared memory, and how many of their clusters run at a time (the same for
+// the three output types)
 int matmul_clusters(int dev, MmClusters *c)
 {
-    static MmClusters kept[kMaxDevices];
-    static bool ready[kMaxDevices];
-    if (!ready[dev]) {
-        CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
-        CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
-        CU_TRY(cudaFuncSetAttribute(mx4_matmul_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
-        MmClusters m;
-        if (!mm_clusters(mx4_matmul_kernel<0>, kMmThreads, &m)) return STMOE_ERR_CUDA;
-        kept[dev] = m;
-        ready[dev] = true;
-    }
-    *c = kept[dev];
-    return STMOE_OK;
+    static PerDevice<MmClusters> kept;
+    return kept.get(dev, c, [](MmClusters &m) {
+        for (const void *k : {(const void *)mx4_matmul_kernel<0>, (const void *)mx4_matmul_kernel<1>, (const void *)mx4_matmul_kernel<4>})
+            if (const int rc = cuda_status(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes))) return rc;
+        return mm_clusters(mx4_matmul_kernel<0>, kMmThreads, &m) ? STMOE_OK : STMOE_ERR_CUDA;
+    });
 }
 
 template <int ODT>
@@ -189,10 +116,10 @@ int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_
         ((int64_t)n_groups * n > 1 && b_scale_stride < k_blocks) || (m > 1 && out_stride < n) || ((uintptr_t)out & (elem_bytes(out_dtype) - 1)))
         return STMOE_ERR_BAD_ARG;
     if (m == 0) return STMOE_OK;
-    int dev = 0;
-    const int sms = sm_count(&dev);
-    EncodeTiledFn fn = encode_fn();
-    if (!sms || !fn) return STMOE_ERR_CUDA;
+    int dev = 0, sms = 0;
+    if (const int rc = current_device(&dev, &sms)) return rc;
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return STMOE_ERR_CUDA;
 
     Mx4MatmulArgs a{};
     a.a_scales = a_scales, a.b_scales = b_scales, a.a_scale_stride = a_scale_stride, a.b_scale_stride = b_scale_stride;

@@ -3,9 +3,11 @@
 
 #include <algorithm>
 
+#include "host_utils.cuh"
 #include "router_balance.cuh"
 
 using namespace stmoe_dev;
+using namespace stmoe_host;
 
 namespace {
 
@@ -47,76 +49,49 @@ constexpr int64_t kBalAlone = 2;
 // CTAs that it takes for no lane to add more than kBalLaneSteps steps of rows in fp32
 int64_t bal_least_ctas(int64_t steps) { return (steps + kBalLaneSteps - 1) / kBalLaneSteps; }
 // three CTAs an SM (launch bounds); forward: whole multiples of that where rows are many
-int bal_grid(int64_t tokens, int lpr, bool backward)
+int bal_grid(int64_t tokens, int lpr, int sms, bool backward)
 {
     const int64_t steps = bal_steps(tokens, lpr);
     if (steps <= kBalAlone) return 1;
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return 0;
-    }
     const int64_t once = std::min<int64_t>(steps, std::min(sms * 3, kBalOnceCtas));
     return (int)(backward ? once : (bal_least_ctas(steps) + once - 1) / once * once);
 }
 
-// Launch that may start while the kernel before it in the stream drains (the kernels wait for it
-// themselves), in clusters of `cluster` CTAs.
-int launch_behind(void (*kernel)(BalanceArgs), int grid, int block, int smem, int cluster, cudaStream_t st, const BalanceArgs &a)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = st;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
-    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return STMOE_ERR_CUDA;
-    }
-    return STMOE_OK;
-}
-
-template <int DT, int LPR, int N, int kRead> int launch_as(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+template <int DT, int LPR, int N, int kRead> int launch_as(bool backward, const BalanceArgs &a, int grid, int dev, cudaStream_t st)
 {
     // more than the default 48 KB of dynamic shared memory: asked for once per device
-    static bool ready[64][2];
+    static PerDevice<bool> asked[2];
     void (*kernel)(BalanceArgs) = backward ? router_balance_backward_kernel<DT, LPR, N, kRead> : router_balance_kernel<DT, LPR, N, kRead>;
     const int stage = backward ? BalWalk<DT, LPR, N, kRead, false>::stage_bytes() : BalWalk<DT, LPR, N, kRead, true>::stage_bytes();
     const int smem = kRead == kBalScalar ? 0 : kBalDepth * stage;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return STMOE_ERR_CUDA;
-    if (smem && !ready[dev][backward]) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return STMOE_ERR_CUDA;
-        }
-        ready[dev][backward] = true;
-    }
+    bool done = false;
+    if (smem)
+        if (const int rc = asked[backward].get(dev, &done, [=](bool &) {
+                return cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+            }))
+            return rc;
     return launch_behind(kernel, grid, kBalThreads, smem, 1, st, a);
 }
-template <int DT, int LPR, int N> int launch(bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+template <int DT, int LPR, int N> int launch(bool backward, const BalanceArgs &a, int grid, int dev, cudaStream_t st)
 {
-    if (!a.vec) return launch_as<DT, LPR, N, kBalScalar>(backward, a, grid, st);
-    return a.E == LPR * N ? launch_as<DT, LPR, N, kBalFull>(backward, a, grid, st) : launch_as<DT, LPR, N, kBalVec>(backward, a, grid, st);
+    if (!a.vec) return launch_as<DT, LPR, N, kBalScalar>(backward, a, grid, dev, st);
+    return a.E == LPR * N ? launch_as<DT, LPR, N, kBalFull>(backward, a, grid, dev, st) : launch_as<DT, LPR, N, kBalVec>(backward, a, grid, dev, st);
 }
-template <int DT> int launch_lanes(int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+template <int DT> int launch_lanes(int lpr, bool backward, const BalanceArgs &a, int grid, int dev, cudaStream_t st)
 {
     switch (lpr) {
-    case 1: return a.E <= 8 ? launch<DT, 1, 8>(backward, a, grid, st) : launch<DT, 1, 16>(backward, a, grid, st);
-    case 2: return launch<DT, 2, 16>(backward, a, grid, st);
-    case 4: return launch<DT, 4, 16>(backward, a, grid, st);
-    case 8: return launch<DT, 8, 16>(backward, a, grid, st);
-    default: return launch<DT, 16, 16>(backward, a, grid, st);
+    case 1: return a.E <= 8 ? launch<DT, 1, 8>(backward, a, grid, dev, st) : launch<DT, 1, 16>(backward, a, grid, dev, st);
+    case 2: return launch<DT, 2, 16>(backward, a, grid, dev, st);
+    case 4: return launch<DT, 4, 16>(backward, a, grid, dev, st);
+    case 8: return launch<DT, 8, 16>(backward, a, grid, dev, st);
+    default: return launch<DT, 16, 16>(backward, a, grid, dev, st);
     }
 }
-int launch_typed(int dtype, int lpr, bool backward, const BalanceArgs &a, int grid, cudaStream_t st)
+int launch_typed(int dtype, int lpr, bool backward, const BalanceArgs &a, int grid, int dev, cudaStream_t st)
 {
-    if (dtype == STMOE_F32) return launch_lanes<0>(lpr, backward, a, grid, st);
-    if (dtype == STMOE_BF16) return launch_lanes<1>(lpr, backward, a, grid, st);
-    return launch_lanes<4>(lpr, backward, a, grid, st);
+    if (dtype == STMOE_F32) return launch_lanes<0>(lpr, backward, a, grid, dev, st);
+    if (dtype == STMOE_BF16) return launch_lanes<1>(lpr, backward, a, grid, dev, st);
+    return launch_lanes<4>(lpr, backward, a, grid, dev, st);
 }
 
 }  // namespace
@@ -139,14 +114,15 @@ int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const in
         return STMOE_ERR_BAD_ARG;
     const size_t need = stmoe_router_balance_scratch_bytes(tokens, n_experts);
     if (need && (!scratch || ((uintptr_t)scratch & 3) || scratch_bytes < need)) return STMOE_ERR_BAD_ARG;
-    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, false);
-    if (!grid) return STMOE_ERR_CUDA;
+    int dev = 0, sms = 0;
+    if (const int rc = current_device(&dev, &sms)) return rc;
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, sms, false);
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.ids = ids, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
     a.vec = rows_vec(logits, dtype, stride, n_experts);
     a.part = (float *)scratch, a.ctas = grid, a.loss = loss, a.counts = counts, a.rows = rows;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const int rc = launch_typed(dtype, lpr, false, a, grid, st);
+    const int rc = launch_typed(dtype, lpr, false, a, grid, dev, st);
     if (rc != STMOE_OK || grid == 1) return rc;
     return launch_behind(router_balance_finish_kernel, kBalFinish, 1024, 0, kBalFinish, st, a);
 }
@@ -160,14 +136,15 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
         return STMOE_ERR_BAD_ARG;
     if (tokens == 0) return STMOE_OK;
     if (overlap(logits, stride, grad_logits, grad_stride, tokens, n_experts, dtype)) return STMOE_ERR_BAD_ARG;
-    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, true);
-    if (!grid) return STMOE_ERR_CUDA;
+    int dev = 0, sms = 0;
+    if (const int rc = current_device(&dev, &sms)) return rc;
+    const int lpr = lanes_per_row(n_experts), grid = bal_grid(tokens, lpr, sms, true);
     BalanceArgs a{};
     a.logits = logits, a.stride = stride, a.mask = mask, a.T = (int)tokens, a.E = n_experts, a.K = top_k;
     a.vec = rows_vec(logits, dtype, stride, n_experts) && rows_vec(grad_logits, dtype, grad_stride, n_experts);
     a.counts = (int *)counts, a.rows = (int *)rows, a.grad = grad_loss;
     a.dlogits = grad_logits, a.dstride = grad_stride;
-    return launch_typed(dtype, lpr, true, a, grid, (cudaStream_t)cuda_stream);
+    return launch_typed(dtype, lpr, true, a, grid, dev, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

@@ -19,6 +19,7 @@
 #include "dense_group.cuh"
 #include "device_utils.cuh"
 #include "ffn.cuh"
+#include "host_utils.cuh"
 #include "mx4_ffn.cuh"
 #include "predictor.cuh"
 #include "router.cuh"
@@ -27,6 +28,7 @@
 #include "token_kernel.cuh"
 
 using namespace stmoe_dev;
+using namespace stmoe_host;
 
 #define CU_TRY(expr)                                  \
     do {                                              \
@@ -327,10 +329,6 @@ struct SlotCache {
 };
 
 // ---- 4-bit expert FFN (mx4_ffn.cuh) -------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 struct Mx4FfnMaps {
     CUtensorMap gate[2], up[2], down[2];   // [0]: images of the routed experts, [1]: of the shared ones
     const uint8_t *store[2];               // first image of either
@@ -377,19 +375,6 @@ size_t mx4_buffers(uint8_t *base, int B, int pairs, int H, int I, int part_rows,
 }
 int mx4_entry_tokens(int B) { return std::min(B, kMxfTokens); }
 
-EncodeTiledFn encode_tiled_fn()
-{
-    static EncodeTiledFn fn = nullptr;   // the same value whoever fills it
-    if (!fn) {
-        void *sym = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = (EncodeTiledFn)sym;
-        (void)cudaGetLastError();
-    }
-    return fn;
-}
 // codes in rows of row_bytes: boxes of 128 bytes x box_rows rows, 128-byte swizzle, zeros outside;
 // images > 0: a third dimension, img_bytes apart
 int mx4_map(CUtensorMap *m, const uint8_t *base, int64_t row_bytes, int64_t rows, int box_rows, int64_t images, int64_t img_bytes)
@@ -417,51 +402,30 @@ int mx4_act_maps(Mx4FfnMaps *m, const Mx4FfnBufs &b, int B, int pairs, int H, in
     return mx4_map(&m->act, b.act_codes, I / 2, (int64_t)pairs * kPlanes, kPlanes, 0, 0);
 }
 
-// launch behind the kernel before it in the stream (programmatic dependent launch), in clusters
-template <typename... P, typename... A>
-int mx4_launch(void (*kernel)(P...), int grid, int block, size_t smem, int cluster, cudaStream_t st, const A &...args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = st;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
-    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
-    CU_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
-    return STMOE_OK;
-}
 template <int NMAT> auto mx4_ffn_kernel_for(int blocks)
 {
     const int align = mxf_align(blocks);
     return align == 8 ? mx4_ffn_kernel<NMAT, 8> : align == 4 ? mx4_ffn_kernel<NMAT, 4> : mx4_ffn_kernel<NMAT, 1>;
 }
 
-// what a call has to know of its device, found out once per device ordinal (a racing fill writes the
-// same values): the kernels' shared memory is asked for on the way
+// what a call has to know of its device, found out once: the kernels' shared memory is asked for on the way
 struct Mx4Device {
     int sms;
     MmClusters clusters;
 };
-int mx4_device(int dev, Mx4Device *d)
+int mx4_device(Mx4Device *d)
 {
-    static Mx4Device kept[64];
-    static bool ready[64];
-    if (dev < 0 || dev >= 64) return STMOE_ERR_BAD_ARG;
-    if (!ready[dev]) {
+    static PerDevice<Mx4Device> kept;
+    int dev = 0, sms = 0;
+    ST_TRY(current_device(&dev, &sms));
+    return kept.get(dev, d, [sms](Mx4Device &m) {
         for (int blocks : {8, 4, 1}) {
             CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel_for<2>(blocks), cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
             CU_TRY(cudaFuncSetAttribute(mx4_ffn_kernel_for<1>(blocks), cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmemBytes));
         }
-        Mx4Device m;
-        m.sms = sm_count();
-        if (!mm_clusters(mx4_ffn_kernel_for<2>(8), kMxfThreads, &m.clusters)) return STMOE_ERR_CUDA;
-        kept[dev] = m;
-        ready[dev] = true;
-    }
-    *d = kept[dev];
-    return STMOE_OK;
+        m.sms = sms;
+        return mm_clusters(mx4_ffn_kernel_for<2>(8), kMxfThreads, &m.clusters) ? STMOE_OK : STMOE_ERR_CUDA;
+    });
 }
 
 // The FFN of one layer step; pa: empty, or with the ids of the stand-alone call; fa: inputs, outputs and
@@ -478,7 +442,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
     pa.entries = b.entries, pa.n_entries = b.n_entries, pa.store[0] = maps.store[0], pa.store[1] = maps.store[1];
     pa.img_bytes = img_bytes, pa.E = fa.E, pa.K = fa.K, pa.mt = mt, pa.wl = fa.wl, pa.blob = fa.blob;
     const int blocks = fa.B * H / kMxBlock;
-    ST_TRY(mx4_launch(mx4_planes_kernel, (pa.ids ? 1 : 0) + std::min(sms * 4, (blocks + 7) / 8), 256,
+    ST_TRY(launch_behind(mx4_planes_kernel, (pa.ids ? 1 : 0) + std::min(sms * 4, (blocks + 7) / 8), 256,
                       pa.ids ? sizeof(uint16_t) * 256 * (size_t)((fa.B * fa.K + kWarp - 1) / kWarp) : 0, 1, st, pa));
 
     // at most this many entries: an expert's pairs fill its entries but for the last
@@ -493,7 +457,7 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
     const int gu_tasks = entries * ((I + kMmRows - 1) / kMmRows);
     g.last_task = gu_tasks - 1;
     g.splits = mm_splits(gu_tasks, gu_steps, dev.clusters);   // fewer tiles than SMs: a cluster shares a tile's reduction
-    ST_TRY(mx4_launch(mx4_ffn_kernel_for<2>(g.blocks), g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMxfThreads, kMmSmemBytes,
+    ST_TRY(launch_behind(mx4_ffn_kernel_for<2>(g.blocks), g.splits > 1 ? gu_tasks * g.splits : std::min(gu_tasks, sms), kMxfThreads, kMmSmemBytes,
                       g.splits, st, maps.gate[0], maps.up[0], maps.gate[1], maps.up[1], maps.x, g));
 
     ST_TRY(mark(1));
@@ -509,11 +473,11 @@ int mx4_ffn(const Mx4FfnMaps &maps, const Mx4FfnBufs &b, Mx4PlanesArgs pa, FfnAr
         if (t < best) best = t, d.splits = z;
     }
     d.last_task = d_tiles * d.splits - 1;
-    ST_TRY(mx4_launch(mx4_ffn_kernel_for<1>(d.blocks), std::min(d_tiles * d.splits, sms), kMxfThreads, kMmSmemBytes, 1, st, maps.down[0],
+    ST_TRY(launch_behind(mx4_ffn_kernel_for<1>(d.blocks), std::min(d_tiles * d.splits, sms), kMxfThreads, kMmSmemBytes, 1, st, maps.down[0],
                       maps.down[0], maps.down[1], maps.down[1], maps.act, d));
 
     fa.part = b.part, fa.S = d.splits;
-    ST_TRY(mx4_launch(mx4_combine_kernel, std::min(sms * 4, (fa.B * H + 255) / 256), 256, 0, 1, st, fa, pa.ids));
+    ST_TRY(launch_behind(mx4_combine_kernel, std::min(sms * 4, (fa.B * H + 255) / 256), 256, 0, 1, st, fa, pa.ids));
     return mark(2);
 }
 
@@ -1589,9 +1553,7 @@ int stmoe_create(const stmoe_config_t *cfg, stmoe_t **out)
     if (c.weight_dtype == STMOE_MX4) {
         // its own kernels at every batch, launched layer by layer (replayed as a CUDA graph)
         const int pairs = B * s->KS;
-        int dev = 0;
-        CR_TRY(cudaGetDevice(&dev));
-        int rc = mx4_device(dev, &s->mx4_dev);
+        int rc = mx4_device(&s->mx4_dev);
         if (rc != STMOE_OK) return fail(rc);
         const int part_rows = mx4_part_rows_up_to(pairs, I);   // a step may have fewer sequences than max_batch
         CR_TRY(cudaMalloc(&s->d_mx4, mx4_buffers(nullptr, B, pairs, H, I, part_rows, &s->mx4)));
@@ -2171,10 +2133,8 @@ int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const 
     Mx4FfnBufs b;
     if (!mx4_ffn_args_ok(experts, hidden, inter) || scratch_bytes < mx4_call_buffers((uint8_t *)scratch, batch, top_k, hidden, inter, &b))
         return STMOE_ERR_BAD_ARG;
-    int dev = 0;
-    CU_TRY(cudaGetDevice(&dev));
     Mx4Device on;
-    ST_TRY(mx4_device(dev, &on));
+    ST_TRY(mx4_device(&on));
     const size_t img = image_bytes(hidden, inter, STMOE_MX4);
     Mx4FfnMaps maps;
     ST_TRY(mx4_weight_maps(&maps, 0, (const uint8_t *)experts, n_experts, img, hidden, inter));
