@@ -12,6 +12,7 @@
  * Conventions
  *   - Every function returns STMOE_OK (0) or a negative STMOE_ERR_* code; no
  *     exception, abort or output crosses this boundary.
+ *   - Pointers are aligned to their element type; the MX4 and balance entry points refuse others.
  *   - "device" pointers are CUDA global memory of the device that was current
  *     in stmoe_create; "host" pointers are ordinary or pinned host memory.
  *   - load_* calls copy what they are given; the caller keeps its buffers.
@@ -332,7 +333,7 @@ int stmoe_predictor_step(stmoe_t *s, int layer, int batch, const int32_t *routed
  * stmoe_mx4_ffn_scratch_bytes(batch, top_k, hidden, inter) bytes, which also serve every smaller batch
  * and top_k (a call of exactly that size may take less).  The weights go to the tensor cores
  * as stored; an activation is held as a sum of eight 4-bit values that leaves less than 2^-22 of the
- * largest magnitude among its 32 neighbours, and sums are fp32, so results have the precision of fp32
+ * largest magnitude among its 32 neighbours (or 2^-128, where that is more: 4-bit scales end at 2^-127), and sums are fp32, so results have the precision of fp32
  * activations.  A non-finite activation makes the 32 neighbours, and what depends on them, NaN; pairs
  * whose id is outside [0, n_experts) add nothing.  Should a bounded wait inside a kernel run out, the
  * outputs that depend on it are NaN. */

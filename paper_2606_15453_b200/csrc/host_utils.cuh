@@ -16,6 +16,9 @@ inline int cuda_status(cudaError_t e)
     return e == cudaErrorMemoryAllocation ? STMOE_ERR_OOM : STMOE_ERR_CUDA;
 }
 
+// whether every one of these is NULL or on a boundary of its element type's size
+template <typename... T> bool aligned(const T *...p) { return ((((uintptr_t)p & (sizeof(T) - 1)) == 0) && ...); }
+
 // ordinal of the current device, and how many SMs it has
 inline int current_device(int *dev, int *sms)
 {

@@ -113,7 +113,8 @@ int stmoe_mx4_matmul(const uint8_t *a_codes, int64_t a_code_stride, const uint8_
         (n_groups > 1 && !counts) || (int64_t)n_groups * n > INT32_MAX - 256 || ((uintptr_t)a_codes & 15) ||
         ((uintptr_t)b_codes & 15) || (m > 1 && (a_code_stride % 16 || a_code_stride < row_bytes)) ||
         ((int64_t)n_groups * n > 1 && (b_code_stride % 16 || b_code_stride < row_bytes)) || (m > 1 && a_scale_stride < k_blocks) ||
-        ((int64_t)n_groups * n > 1 && b_scale_stride < k_blocks) || (m > 1 && out_stride < n) || ((uintptr_t)out & (elem_bytes(out_dtype) - 1)))
+        ((int64_t)n_groups * n > 1 && b_scale_stride < k_blocks) || (m > 1 && out_stride < n) || ((uintptr_t)out & (elem_bytes(out_dtype) - 1)) ||
+        !aligned(counts, flags))
         return STMOE_ERR_BAD_ARG;
     if (m == 0) return STMOE_OK;
     int dev = 0, sms = 0;

@@ -110,7 +110,8 @@ int stmoe_router_balance(const void *logits, int dtype, int64_t stride, const in
                          int n_experts, int top_k, float *loss, int32_t *counts, int32_t *rows, void *scratch,
                          size_t scratch_bytes, void *cuda_stream)
 {
-    if (!bal_args_ok(logits, dtype, stride, tokens, n_experts, top_k) || !ids || !loss || !counts || !rows)
+    if (!bal_args_ok(logits, dtype, stride, tokens, n_experts, top_k) || !ids || !loss || !counts || !rows ||
+        !aligned(ids, loss, counts, rows))
         return STMOE_ERR_BAD_ARG;
     const size_t need = stmoe_router_balance_scratch_bytes(tokens, n_experts);
     if (need && (!scratch || ((uintptr_t)scratch & 3) || scratch_bytes < need)) return STMOE_ERR_BAD_ARG;
@@ -132,7 +133,7 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
                                   void *grad_logits, int64_t grad_stride, void *cuda_stream)
 {
     if (!bal_args_ok(logits, dtype, stride, tokens, n_experts, top_k) || !counts || !rows || !grad_loss ||
-        !bal_args_ok(grad_logits, dtype, grad_stride, tokens, n_experts, top_k))
+        !bal_args_ok(grad_logits, dtype, grad_stride, tokens, n_experts, top_k) || !aligned(counts, rows, grad_loss))
         return STMOE_ERR_BAD_ARG;
     if (tokens == 0) return STMOE_OK;
     if (overlap(logits, stride, grad_logits, grad_stride, tokens, n_experts, dtype)) return STMOE_ERR_BAD_ARG;

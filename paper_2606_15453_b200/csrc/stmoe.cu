@@ -2131,7 +2131,7 @@ int mx4_moe_ffn(const float *h, const float *inv_rms, const int32_t *ids, const 
                 size_t scratch_bytes, cudaStream_t st)
 {
     Mx4FfnBufs b;
-    if (!mx4_ffn_args_ok(experts, hidden, inter) || scratch_bytes < mx4_call_buffers((uint8_t *)scratch, batch, top_k, hidden, inter, &b))
+    if (!mx4_ffn_args_ok(experts, hidden, inter) || !aligned(h, inv_rms, ids, w, h_out) || scratch_bytes < mx4_call_buffers((uint8_t *)scratch, batch, top_k, hidden, inter, &b))
         return STMOE_ERR_BAD_ARG;
     Mx4Device on;
     ST_TRY(mx4_device(&on));

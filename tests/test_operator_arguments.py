@@ -69,6 +69,12 @@ def test_router_balance_refusals(kw):
     assert _bal(**kw) == BAD
 
 
+@pytest.mark.parametrize("name", ["ids", "loss", "counts", "rows"])
+@pytest.mark.parametrize("off", [1, 2])
+def test_router_balance_refuses_addresses_off_their_type(name, off):
+    assert _bal(**{name: C.c_void_p((1 << 20) + off)}) == BAD
+
+
 def _balb(**kw):
     a = dict(z=X, dt=0, st=8, mask=None, T=4, E=8, K=2, counts=X, rows=X, g=X, d=C.c_void_p(1 << 21), ds=8)
     a.update(kw)
@@ -110,3 +116,23 @@ def test_balance_scratch_grows_with_the_tokens_and_never_falls():
         # one row of sums, 2 E + 3 words, to every 256 rows of a lane at most: 256 lanes' worth of rows a CTA
         lanes = next(l for l in (1, 2, 4, 8, 16) if 16 * l >= E)
         assert sizes[-1] >= 4 * (2 * E + 3) * ((1 << 30) // (256 * 256 // lanes))
+
+
+@pytest.mark.parametrize("name", ["counts", "rows", "g"])
+def test_router_balance_backward_refuses_addresses_off_their_type(name):
+    assert _balb(**{name: C.c_void_p((1 << 20) + 2)}) == BAD
+
+
+def test_mx4_matmul_refuses_addresses_off_their_type():
+    off = C.c_void_p((1 << 20) + 2)
+    assert _mm(counts=off) == BAD
+    assert P.lib().stmoe_mx4_matmul(X, 32, X, 2, 4, X, 32, X, 2, 1, 8, 2, None, X, 1, 8, off, None) == BAD
+
+
+@pytest.mark.parametrize("name", ["h", "inv", "ids", "w", "out", "experts", "scratch"])
+def test_mx4_ffn_refuses_addresses_off_their_type(name):
+    a = dict(h=X, inv=X, ids=X, w=X, experts=X, out=X, scratch=X)
+    a[name] = C.c_void_p((1 << 20) + (8 if name == "experts" else 128 if name == "scratch" else 2))
+    rc = P.lib().stmoe_moe_ffn(a["h"], a["inv"], a["ids"], a["w"], a["experts"], 3, 2, 4, 2, 64, 64, 0.1, a["out"], a["scratch"],
+                               1 << 24, None)
+    assert rc == BAD
