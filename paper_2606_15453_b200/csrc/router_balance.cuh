@@ -23,8 +23,8 @@
 // Sums over tokens: a lane adds the probabilities of its experts in fp32 over at most 256 rows (batches that
 // would give it more have more CTAs), a CTA adds its lanes in a fixed order, and the CTAs' partial sums are
 // added in fp64 in a fixed order by a second launch: no floating-point atomics, the same bits every time, and
-// an error that does not grow with the tokens.  (Moving a lane's sums to fp64 inside the loop took nine
-// registers that the loads need: 91.4 -> 93.9 us for 524288 x 128.)  lse^2 is summed in fp64 throughout: a
+// an error that does not grow with the tokens.  (Moving a lane's sums to fp64 inside the loop cost
+// registers that the loads need: 92.3 -> 93.9 us for 524288 x 128, both directions.)  lse^2 is summed in fp64 throughout: a
 // row at a fill value of 1e20 has one that fp32 does not hold, while the mean over the rows may.
 #pragma once
 #include "mx4.cuh"
