@@ -461,6 +461,97 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
                                   int n_experts, int top_k, const int32_t *counts, const int32_t *rows, const float *grad_loss,
                                   void *grad_logits, int64_t grad_stride, void *cuda_stream);
 
+/* ---- choice of experts for many tokens ---------------------------------------------------------- */
+
+#define STMOE_SELECT_SIGMOID 1 /* scores are sigmoids of the logits (off: their softmax)    */
+#define STMOE_SELECT_RENORM 2  /* weights are divided by the sum of the chosen scores       */
+
+/* The gating network's choice from given logits z [tokens][n_experts] (stmoe_router_topk makes them for a decode
+ * step), for routers beyond the plain softmax of Section 2:
+ *   s = softmax(z) or sigmoid(z);  v = s + bias;  groups of n_experts / n_groups neighbouring experts are ranked
+ *   by the sum of their group_best (1 or 2) largest v and the best top_groups stay;  ids = the top_k largest v in
+ *   them, ascending;  w = scale * s[ids], divided by the sum of s[ids] with STMOE_SELECT_RENORM.
+ * Equal values: the lower index, of groups too; values are compared as the formula's in 64 bits, so the choice
+ * does not depend on their rounding to 32.  A logit or bias of -infinity, or a NaN, is never chosen and counts as -infinity in
+ * its group's sum; a row with fewer than top_k left has id -1 and weight 0 behind the last.  So has a row whose mask byte is 0, which may hold
+ * anything.  A NaN in a row that counts (softmax: +infinity too) makes its weights NaN.
+ *   logits  STMOE_F32, STMOE_BF16 or STMOE_F16, stride in elements;  bias fp32 [n_experts] or NULL;  mask uint8 [tokens] or NULL
+ *   ids     int32 [tokens][top_k], w fp32 [tokens][top_k]: written
+ * n_experts <= 256 and a multiple of n_groups <= 32, top_k <= 32, tokens * top_k < 2^31; tokens may be 0.  Asynchronous on cuda_stream. */
+int stmoe_router_select(const void *logits, int dtype, int64_t stride, const float *bias, const uint8_t *mask, int64_t tokens, int n_experts,
+                        int top_k, int n_groups, int top_groups, int group_best, int flags, float scale, int32_t *ids, float *w, void *cuda_stream);
+/* Gradient of sum grad_w . w with respect to the logits (the choice held constant), from the forward call's ids and w, flags and
+ * scale: 0 for experts that were not chosen, except under a softmax without STMOE_SELECT_RENORM.  Rows without a choice have zero
+ * gradient, rows with NaN weights NaN.  grad_w: fp32 [tokens][top_k], not read where the id is -1.  grad_logits: dtype as the logits,
+ * every element written; the two may not overlap. */
+int stmoe_router_select_backward(const void *logits, int dtype, int64_t stride, int64_t tokens, int n_experts, int top_k, int flags, float scale,
+                                 const int32_t *ids, const float *w, const float *grad_w, void *grad_logits, int64_t grad_stride, void *cuda_stream);
+
+/* ---- rows grouped by expert, there and back --------------------------------------------------- */
+
+/* Grouping of the pairs (t, k) of ids [rows][top_k] by id, in 0 .. n_groups - 1 (others have no group):
+ *   counts [n_groups], starts [n_groups + 1]   pairs of each group, and where it begins (last: pairs in groups)
+ *   order  [rows * top_k]   the pair t * top_k + k at each slot: groups one after the other, pairs of a group in their order,
+ *                           pairs without a group behind the last
+ *   slots  [rows][top_k]    slot of each pair, -1 without a group
+ * All int32, device.  The counts are what stmoe_mx4_matmul takes, the grouping of rows by adapter (top_k 1) what stmoe_lora takes.
+ *   scratch  stmoe_group_rows_scratch_bytes(rows, top_k, n_groups) bytes (0 for few pairs: NULL is fine), 4-byte
+ *            aligned, contents free; calls that can overlap need scratch of their own
+ * n_groups <= 1024, rows * top_k < 2^31; rows may be 0.  Asynchronous on cuda_stream. */
+size_t stmoe_group_rows_scratch_bytes(int64_t rows, int top_k, int n_groups);
+int stmoe_group_rows(const int32_t *ids, int64_t rows, int top_k, int n_groups, int32_t *counts, int32_t *starts, int32_t *order,
+                     int32_t *slots, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/* out[slots[t][k]] = x[t], rows of row_bytes bytes (of any type; strides in bytes).  Slots outside [0, out_rows) are left out.
+ *   n_rows  int32 [1]: rows of out from there to rows * top_k become 0 (starts[n_groups] of the grouping); NULL: they stay as they were
+ * x and out may not overlap.  Asynchronous on cuda_stream. */
+int stmoe_dispatch_rows(const void *x, int64_t row_bytes, int64_t x_stride, int64_t rows, int top_k, const int32_t *slots, const int32_t *n_rows,
+                        void *out, int64_t out_rows, int64_t out_stride, void *cuda_stream);
+
+/* out[t] = residual[t] + scale * sum_k w[t][k] y[slots[t][k]], summed in fp32 in the order of k and rounded once.
+ *   y        [y_rows][cols] in y_dtype (STMOE_F32, STMOE_BF16, STMOE_F16); slots outside [0, y_rows) add nothing, whatever their weight
+ *   w        fp32 [tokens][top_k], or NULL: 1
+ *   residual, out  [tokens][cols] in out_dtype (y's or STMOE_F32); residual may be NULL (0) or out itself; nothing else may overlap
+ * Strides in elements.  With w NULL and scale 1 it is the gradient of stmoe_dispatch_rows.  Asynchronous on cuda_stream. */
+int stmoe_combine_rows(const void *y, int y_dtype, int64_t y_stride, int64_t y_rows, const int32_t *slots, const float *w, const void *residual,
+                       int64_t residual_stride, float scale, int64_t tokens, int top_k, int64_t cols, void *out, int out_dtype,
+                       int64_t out_stride, void *cuda_stream);
+/* Its gradients: grad_y[slots[t][k]] = scale * w[t][k] * grad[t] and grad_w[t][k] = scale * <grad[t], y[slots[t][k]]> (0 without a slot;
+ * grad_w NULL: not wanted); the residual's gradient is grad itself.  grad [tokens][cols] in grad_dtype (y's or STMOE_F32), grad_y in y's type.
+ *   n_rows  as in stmoe_dispatch_rows, for the rows of grad_y.  grad_y may overlap neither y nor grad. */
+int stmoe_combine_rows_backward(const void *grad, int grad_dtype, int64_t grad_stride, const void *y, int y_dtype, int64_t y_stride, int64_t y_rows,
+                                const int32_t *slots, const float *w, float scale, int64_t tokens, int top_k, int64_t cols, const int32_t *n_rows,
+                                void *grad_y, int64_t grad_y_stride, float *grad_w, void *cuda_stream);
+
+/* ---- low-rank adapters of many requests beside a shared projection ----------------------------- */
+
+/* out[t] = base[t] + alpha * scale[g] * (x[t] A_g^T) B_g^T, g = ids[t]; rows whose id is outside [0, n_adapters): out = base.
+ *   x      [tokens][inner] in dtype (STMOE_BF16 or STMOE_F16); A [n_adapters][rank][inner], B [n_adapters][outer][rank] in the same type
+ *   ids    int32 [tokens];  order: the permutation that stmoe_group_rows makes of them (top_k 1, n_adapters groups); ids[order[.]] has to
+ *          hold each adapter's rows side by side.  Rows that order does not name are left as they were
+ *   scale  fp32 [n_adapters], or NULL: 1
+ *   base, out  [tokens][outer] in out_dtype (dtype or STMOE_F32); base may be NULL (0) or out itself; nothing else may overlap
+ *   hidden fp32 [tokens][rank], or NULL: receives x A^T (0 for rows without an adapter), which the gradient of B needs
+ *   scratch  stmoe_lora_scratch_bytes(...) bytes, 16-byte aligned, contents free; calls that can overlap need scratch of their own
+ * Strides in elements; a_group, b_group: from one adapter to the next.  Sums in fp32, one rounding of out; x A^T is kept to 2^-17 (out fp32:
+ * 2^-24) of itself.  n_adapters <= 1024, rank <= 256, inner and outer <= 2^24; tokens may be 0 (or 1: a decode step).  The same call gives the same bits every
+ * time.  16-byte aligned rows (rank a multiple of 8 for B) are read 16 bytes at a time, others element by element.  Asynchronous on cuda_stream. */
+size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer);
+int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,
+               int64_t b_row, int n_adapters, int rank, int inner, int outer, const int32_t *ids, const int32_t *order, const float *scale,
+               float alpha, const void *base, int64_t base_stride, void *out, int out_dtype, int64_t out_stride, float *hidden, void *scratch,
+               size_t scratch_bytes, void *cuda_stream);
+/* Gradients for grad [tokens][outer] in dtype: grad_x [tokens][inner] = c u A with u = grad B (0 for rows without an adapter; the base's gradient
+ * is grad itself), grad_a [n][rank][inner] = c sum_t u^T x, grad_b [n][outer][rank] = c sum_t grad^T hidden, c = alpha * scale[g]; contiguous, in dtype,
+ * each rounded once, 0 for adapters without rows; grad_a and grad_b may be NULL.  counts, starts: of the grouping that made order.
+ * scale is held constant.  scratch: stmoe_lora_backward_scratch_bytes(...) bytes, 256-byte aligned.  grad_x may overlap neither grad nor x. */
+size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer);
+int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const void *x, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group,
+                        int64_t a_row, const void *b, int64_t b_group, int64_t b_row, int n_adapters, int rank, int inner, int outer,
+                        const int32_t *ids, const int32_t *order, const int32_t *counts, const int32_t *starts, const float *scale, float alpha,
+                        const float *hidden, void *grad_x, int64_t grad_x_stride, void *grad_a, void *grad_b, void *scratch, size_t scratch_bytes,
+                        void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

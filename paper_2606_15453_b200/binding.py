@@ -102,6 +102,20 @@ def lib():
         L.stmoe_router_balance_scratch_bytes.argtypes = [i64, i32]
         L.stmoe_router_balance.argtypes = [vp, i32, i64, vp, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
         L.stmoe_router_balance_backward.argtypes = [vp, i32, i64, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp]
+        L.stmoe_router_select.argtypes = [vp, i32, i64, vp, vp, i64, i32, i32, i32, i32, i32, i32, f32, vp, vp, vp]
+        L.stmoe_router_select_backward.argtypes = [vp, i32, i64, i64, i32, i32, i32, f32, vp, vp, vp, vp, i64, vp]
+        L.stmoe_group_rows_scratch_bytes.restype = sz
+        L.stmoe_group_rows_scratch_bytes.argtypes = [i64, i32, i32]
+        L.stmoe_group_rows.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.stmoe_dispatch_rows.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, i64, i64, vp]
+        L.stmoe_combine_rows.argtypes = [vp, i32, i64, i64, vp, vp, vp, i64, f32, i64, i32, i64, vp, i32, i64, vp]
+        L.stmoe_combine_rows_backward.argtypes = [vp, i32, i64, vp, i32, i64, i64, vp, vp, f32, i64, i32, i64, vp, vp, i64, vp, vp]
+        L.stmoe_lora_scratch_bytes.restype = L.stmoe_lora_backward_scratch_bytes.restype = sz
+        L.stmoe_lora_scratch_bytes.argtypes = L.stmoe_lora_backward_scratch_bytes.argtypes = [i64, i32, i32, i32, i32]
+        L.stmoe_lora.argtypes = [vp, i32, i64, i64, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, f32, vp, i64, vp, i32,
+                                 i64, vp, vp, sz, vp]
+        L.stmoe_lora_backward.argtypes = [vp, i32, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp,
+                                          f32, vp, vp, i64, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -583,3 +597,355 @@ def router_balance_backward(logits, forward, grad_loss, mask=None, out=None, str
         if rc:
             _check(rc, "stmoe_router_balance_backward")
     return out
+
+
+# ---- around the experts' products: choice of experts, rows in their order and back, adapters ------------
+
+SELECT_SIGMOID, SELECT_RENORM = 1, 2
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _wants_grad(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _is_vector(t, n, dtype, dev) -> bool:
+    return t.dtype == dtype and t.numel() == n and t.is_contiguous() and t.device == dev
+
+
+class _RouterSelect(torch.autograd.Function):
+    """router_select as a step of torch's graph; the gradient is router_select_backward's."""
+
+    @staticmethod
+    def forward(ctx, logits, *how):
+        f = router_select(logits, *how)
+        ctx.save_for_backward(logits, f["ids"], f["w"])
+        ctx.how = f["flags"], f["scale"]
+        ctx.mark_non_differentiable(f["ids"])
+        ctx.set_materialize_grads(False)
+        return f["ids"], f["w"], f["flags"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, _, grad_w, __):
+        if grad_w is None:
+            return (None,) * 10
+        logits, ids, w = ctx.saved_tensors
+        f = {"ids": ids, "w": w, "flags": ctx.how[0], "scale": ctx.how[1]}
+        return (router_select_backward(logits, f, grad_w.to(_F32).contiguous()),) + (None,) * 9
+
+
+def router_select(logits, top_k, scores="softmax", bias=None, groups=1, top_groups=None, group_best=1, renorm=False, scale=1.0, mask=None,
+                  stream=None):
+    """stmoe_router_select: the experts of every row of logits [tokens][n_experts] (fp32, bf16 or fp16) and their weights.
+    scores: "softmax" or "sigmoid"; bias fp32 [n_experts]: added to the scores for the choice only; groups, top_groups, group_best: the
+    choice is made among the best top_groups groups, ranked by their group_best best members; renorm: weights of a row sum to scale;
+    mask bool [tokens]: rows to choose for.  Returns dict(ids int32 [tokens][top_k], ascending, -1 behind the last; w fp32
+    [tokens][top_k]; flags, scale: what the gradient has to know).  Where logits require a gradient w carries it, once differentiable."""
+    elem = _balance_elem(logits, mask)
+    T, E = logits.shape
+    if scores not in ("softmax", "sigmoid"):
+        _refuse("scores: softmax or sigmoid")
+    if bias is not None and not _is_vector(bias, E, _F32, logits.device):
+        _refuse("bias: contiguous fp32 [n_experts] on the logits' device")
+    if not 1 <= top_k <= E:
+        _refuse("top_k: 1 to the number of experts")
+    st = _stream_of(logits, stream)
+    if st is None:
+        return _there(logits, stream, router_select, logits, top_k, scores, bias, groups, top_groups, group_best, renorm, scale, mask)
+    if _wants_grad(logits):
+        ids, w, flags = _RouterSelect.apply(logits, top_k, scores, bias, groups, top_groups, group_best, renorm, scale, mask)
+        return {"ids": ids, "w": w, "flags": flags, "scale": scale}
+    flags = (SELECT_SIGMOID if scores == "sigmoid" else 0) | (SELECT_RENORM if renorm else 0)
+    ids = torch.empty(T, top_k, dtype=_I32, device=logits.device)
+    w = torch.empty(T, top_k, dtype=_F32, device=logits.device)
+    # an empty tensor has no address; nothing of it is read
+    src, idp, wp = (logits.data_ptr(), ids.data_ptr(), w.data_ptr()) if T else (256, 256, 256)
+    rc = lib().stmoe_router_select(src, elem, logits.stride(0), _addr(bias), _addr(mask), T, E, top_k, groups,
+                                   groups if top_groups is None else top_groups, group_best, flags, scale, idp, wp, st)
+    if rc:
+        _check(rc, "stmoe_router_select")
+    return {"ids": ids, "w": w, "flags": flags, "scale": scale}
+
+
+def router_select_backward(logits, forward, grad_w, out=None, stream=None):
+    """stmoe_router_select_backward: gradient of sum(grad_w * w) with respect to the logits, from the dict that
+    router_select returned for them; grad_w: fp32 [tokens][top_k]."""
+    elem = _balance_elem(logits, None)
+    T, E = logits.shape
+    ids, w, dev = forward["ids"], forward["w"], logits.device
+    K = ids.shape[1]
+    if not (ids.shape[0] == T and _is_vector(ids, T * K, _I32, dev) and _is_vector(w, T * K, _F32, dev)):
+        _refuse("forward does not belong to these logits")
+    if not _is_vector(grad_w, T * K, _F32, dev):
+        _refuse("grad_w: contiguous fp32 [tokens][top_k] on the logits' device")
+    if out is not None and not (_is_rows(out, logits.dtype) and out.shape == logits.shape and out.device == dev):
+        _refuse("out: expected the logits' shape and type")
+    st = _stream_of(logits, stream)
+    if st is None:
+        return _there(logits, stream, router_select_backward, logits, forward, grad_w, out)
+    if out is None:
+        out = torch.empty(T, E, dtype=logits.dtype, device=dev)
+    if T:
+        rc = lib().stmoe_router_select_backward(logits.data_ptr(), elem, logits.stride(0), T, E, K, forward["flags"], forward["scale"],
+                                                ids.data_ptr(), w.data_ptr(), grad_w.data_ptr(), out.data_ptr(), out.stride(0), st)
+        if rc:
+            _check(rc, "stmoe_router_select_backward")
+    return out
+
+
+def group_rows(ids, n_groups, stream=None):
+    """stmoe_group_rows: the grouping of ids int32 [rows][top_k] (or [rows]) by id; ids outside [0, n_groups) have no group.
+    Returns the plan that dispatch_rows, combine_rows and (for ids [rows]) lora take: dict(counts int32 [n_groups], for mx4_matmul;
+    starts [n_groups + 1]; order [rows * top_k]; slots, shaped as ids; ids, groups)."""
+    if not (ids.is_cuda and ids.dtype == _I32 and ids.dim() in (1, 2) and ids.is_contiguous()):
+        _refuse("ids: contiguous int32 [rows][top_k] or [rows] on a CUDA device")
+    T, K = (ids.shape[0], 1) if ids.dim() == 1 else ids.shape
+    if K < 1 or not 1 <= n_groups <= 1024:
+        _refuse("top_k at least 1, 1 to 1024 groups")
+    st = _stream_of(ids, stream)
+    if st is None:
+        return _there(ids, stream, group_rows, ids, n_groups)
+    L = lib()
+    P, n = T * K, L.stmoe_group_rows_scratch_bytes(T, K, n_groups)
+    counts, starts, order, slots, scratch = torch.empty(2 * n_groups + 1 + 2 * P + n // 4, dtype=_I32, device=ids.device).split(
+        [n_groups, n_groups + 1, P, P, n // 4])
+    idp = ids.data_ptr() if T else counts.data_ptr()
+    c = counts.data_ptr()
+    at = c + 4 * (2 * n_groups + 1)
+    rc = L.stmoe_group_rows(idp, T, K, n_groups, c, c + 4 * n_groups, at, at + 4 * P, at + 8 * P, n, st)
+    if rc:
+        _check(rc, "stmoe_group_rows")
+    return {"counts": counts, "starts": starts, "order": order, "slots": slots.view(ids.shape), "ids": ids, "groups": n_groups}
+
+
+def _plan_of(plan, T, dev):
+    """top_k of a plan for T rows."""
+    slots = plan["slots"]
+    if slots.shape[0] != T or slots.device != dev:
+        _refuse("the plan belongs to other rows")
+    return 1 if slots.dim() == 1 else slots.shape[1]
+
+
+class _Dispatch(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, plan):
+        ctx.plan = plan
+        return dispatch_rows(x, plan)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        return combine_rows(grad.contiguous(), ctx.plan), None
+
+
+def dispatch_rows(x, plan, out=None, stream=None):
+    """stmoe_dispatch_rows: rows of x [rows][cols] (any type) in the order of group_rows' plan, [rows * top_k][cols].  Rows
+    behind the last group are 0; in a given out they stay as they were.  Takes part in autograd (without out)."""
+    if not _is_rows(x) or x.shape[1] < 1:
+        _refuse("x: expected a 2-D CUDA tensor with contiguous rows")
+    T, C = x.shape
+    K = _plan_of(plan, T, x.device)
+    if out is not None and not (_is_rows(out, x.dtype) and out.shape[0] == T * K and out.shape[1] == C and out.device == x.device):
+        _refuse(f"out: expected {(T * K, C)} of x's type with contiguous rows on x's device")
+    if out is not None and _wants_grad(x, out):
+        _refuse("out is not part of torch's graph: leave it away where x requires a gradient")
+    st = _stream_of(x, stream)
+    if st is None:
+        return _there(x, stream, dispatch_rows, x, plan, out)
+    if _wants_grad(x):
+        return _Dispatch.apply(x, plan)
+    fresh = out is None
+    if fresh:
+        out = torch.empty(T * K, C, dtype=x.dtype, device=x.device)
+    if T:
+        b = x.element_size()
+        rc = lib().stmoe_dispatch_rows(x.data_ptr(), C * b, x.stride(0) * b, T, K, plan["slots"].data_ptr(),
+                                       plan["starts"].data_ptr() + 4 * plan["groups"] if fresh else None, out.data_ptr(), T * K,
+                                       out.stride(0) * b, st)
+        if rc:
+            _check(rc, "stmoe_dispatch_rows")
+    return out
+
+
+class _Combine(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, y, w, residual, plan, scale):
+        ctx.save_for_backward(y, w)
+        ctx.plan, ctx.scale, ctx.wants = plan, scale, (y.requires_grad, w is not None and w.requires_grad)
+        return combine_rows(y, plan, w, residual, scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        y, w = ctx.saved_tensors
+        dy = dw = None
+        if any(ctx.wants):
+            dy, dw = combine_rows_backward(grad.contiguous(), y, ctx.plan, w, ctx.scale)
+        return dy, dw, grad if ctx.needs_input_grad[2] else None, None, None
+
+
+def _combine_args(y, plan, w, other, what):
+    T = plan["slots"].shape[0]
+    elem = _ELEM.get(y.dtype)
+    if elem is None or not _is_rows(y) or y.shape[1] < 1:
+        _refuse("y: expected a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows")
+    K = _plan_of(plan, T, y.device)
+    if y.shape[0] != T * K:
+        _refuse("y has other rows than the plan")
+    if w is not None and not _is_vector(w, T * K, _F32, y.device):
+        _refuse("w: contiguous fp32 [rows][top_k] on y's device")
+    for t in other:
+        if t is not None and not (_is_rows(t) and t.dtype in (y.dtype, _F32) and t.shape[0] == T and t.shape[1] == y.shape[1] and t.device == y.device):
+            _refuse(f"{what}: expected [rows][cols] of y's type or fp32 with contiguous rows on y's device")
+    return T, K, elem
+
+
+def combine_rows(y, plan, w=None, residual=None, scale=1.0, out=None, stream=None):
+    """stmoe_combine_rows: residual + scale * sum_k w[:, k] y[slot of (row, k)] for y [rows * top_k][cols] in the plan's order; the result
+    has the residual's type (y's or fp32; without a residual out's or y's); out may be the residual.  Takes part in autograd (without out)."""
+    T, K, elem = _combine_args(y, plan, w, (residual, out), "residual, out")
+    if residual is not None and out is not None and residual.dtype != out.dtype:
+        _refuse("residual and out have to be of one type")
+    if out is not None and _wants_grad(y, w, residual, out):
+        _refuse("out is not part of torch's graph: leave it away where an input requires a gradient")
+    st = _stream_of(y, stream)
+    if st is None:
+        return _there(y, stream, combine_rows, y, plan, w, residual, scale, out)
+    if _wants_grad(y, w, residual):
+        return _Combine.apply(y, w, residual, plan, scale)
+    C = y.shape[1]
+    if out is None:
+        out = torch.empty(T, C, dtype=y.dtype if residual is None else residual.dtype, device=y.device)
+    if T:
+        rc = lib().stmoe_combine_rows(y.data_ptr(), elem, y.stride(0), T * K, plan["slots"].data_ptr(), _addr(w), _addr(residual),
+                                      0 if residual is None else residual.stride(0), scale, T, K, C, out.data_ptr(), _ELEM[out.dtype],
+                                      out.stride(0), st)
+        if rc:
+            _check(rc, "stmoe_combine_rows")
+    return out
+
+
+def combine_rows_backward(grad, y, plan, w=None, scale=1.0, stream=None):
+    """stmoe_combine_rows_backward: (gradient of y, of w) for grad [rows][cols]; rows of the first behind the last group
+    are 0.  The second is None where w is."""
+    T, K, elem = _combine_args(y, plan, w, (grad,), "grad")
+    st = _stream_of(y, stream)
+    if st is None:
+        return _there(y, stream, combine_rows_backward, grad, y, plan, w, scale)
+    C = y.shape[1]
+    dy = torch.empty(T * K, C, dtype=y.dtype, device=y.device)
+    dw = None if w is None else torch.empty_like(w)
+    if T:
+        rc = lib().stmoe_combine_rows_backward(grad.data_ptr(), _ELEM[grad.dtype], grad.stride(0), y.data_ptr(), elem, y.stride(0), T * K,
+                                               plan["slots"].data_ptr(), _addr(w), scale, T, K, C,
+                                               plan["starts"].data_ptr() + 4 * plan["groups"], dy.data_ptr(), C, _addr(dw), st)
+        if rc:
+            _check(rc, "stmoe_combine_rows_backward")
+    return dy, dw
+
+
+class _Lora(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, a, b, base, plan, scale, alpha):
+        hidden = torch.empty(x.shape[0], a.shape[1], dtype=_F32, device=x.device)
+        out = lora(x, a, b, plan, scale, alpha, base, hidden=hidden)
+        ctx.save_for_backward(x, a, b, scale, hidden)
+        ctx.plan, ctx.alpha, ctx.dtype = plan, alpha, out.dtype
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, a, b, scale, hidden = ctx.saved_tensors
+        dx = da = db = None
+        if any(ctx.needs_input_grad[:3]):
+            dx, da, db = lora_backward(grad.to(x.dtype).contiguous(), x, a, b, ctx.plan, hidden, scale, ctx.alpha)
+        return dx, da, db, grad if ctx.needs_input_grad[3] else None, None, None, None
+
+
+def _lora_args(x, a, b, plan, scale, hidden):
+    elem = _ELEM.get(x.dtype)
+    if not elem or not _is_rows(x) or x.shape[1] < 1:
+        _refuse("x: expected a 2-D CUDA tensor of bf16 or fp16 with contiguous rows")
+    T, I = x.shape
+    if a.dim() != 3 or b.dim() != 3 or a.dtype != x.dtype or b.dtype != x.dtype or a.device != x.device or b.device != x.device:
+        _refuse("a [n][rank][inner] and b [n][outer][rank]: expected x's type and device")
+    n, r, O = a.shape[0], a.shape[1], b.shape[1]
+    if a.shape[2] != I or b.shape[0] != n or b.shape[2] != r or n < 1 or O < 1 or not 1 <= r <= 256:
+        _refuse("the adapters' shapes do not belong together, or rank is not in 1..256")
+    if (a.stride(2) != 1 and I > 1) or (b.stride(2) != 1 and r > 1):
+        _refuse("a and b: expected contiguous rows")
+    if _plan_of(plan, T, x.device) != 1 or plan["groups"] != n:
+        _refuse("plan: group_rows of ids [rows], one group an adapter")
+    if scale is not None and not _is_vector(scale, n, _F32, x.device):
+        _refuse("scale: contiguous fp32 [n] on x's device")
+    if hidden is not None and not (_is_vector(hidden, T * r, _F32, x.device)):
+        _refuse("hidden: contiguous fp32 [rows][rank] on x's device")
+    return elem, T, I, n, r, O
+
+
+def lora(x, a, b, plan, scale=None, alpha=1.0, base=None, out=None, hidden=None, stream=None):
+    """stmoe_lora: base + alpha * scale[g] * (x A_g^T) B_g^T, g the adapter of each row of x [rows][inner] (bf16 or fp16), a [n][rank][inner],
+    b [n][outer][rank], plan = group_rows(ids [rows], n) (one plan serves all projections of a step; rows without a group keep the base).
+    base [rows][outer]: the shared projection's result, in x's type or fp32, which is the result's type (without a base out's or
+    x's); None: 0.  out may be the base.  hidden fp32 [rows][rank]: receives x A_g^T, for lora_backward.  Takes part in autograd (without out);
+    the gradient of an fp32 result is rounded to x's type for those of x, a and b."""
+    elem, T, I, n, r, O = _lora_args(x, a, b, plan, scale, hidden)
+    for t in (base, out):
+        if t is not None and not (_is_rows(t) and t.dtype in (x.dtype, _F32) and t.shape[0] == T and t.shape[1] == O and t.device == x.device):
+            _refuse(f"base, out: expected {(T, O)} of x's type or fp32 with contiguous rows on x's device")
+    if base is not None and out is not None and base.dtype != out.dtype:
+        _refuse("base and out have to be of one type")
+    if _wants_grad(x, a, b, base, out) and (out is not None or hidden is not None):
+        _refuse("out and hidden are not part of torch's graph: leave them away where an input requires a gradient")
+    if _wants_grad(scale):
+        _refuse("scale is held constant")
+    st = _stream_of(x, stream)
+    if st is None:
+        return _there(x, stream, lora, x, a, b, plan, scale, alpha, base, out, hidden)
+    if _wants_grad(x, a, b, base):
+        return _Lora.apply(x, a, b, base, plan, scale, alpha)
+    if out is None:
+        out = torch.empty(T, O, dtype=x.dtype if base is None else base.dtype, device=x.device)
+    if T:
+        L = lib()
+        size = L.stmoe_lora_scratch_bytes(T, n, r, I, O)
+        scratch = torch.empty(size, dtype=_U8, device=x.device)
+        rc = L.stmoe_lora(x.data_ptr(), elem, x.stride(0), T, a.data_ptr(), a.stride(0), a.stride(1), b.data_ptr(), b.stride(0), b.stride(1), n, r, I, O,
+                          plan["ids"].data_ptr(), plan["order"].data_ptr(), _addr(scale), alpha, _addr(base),
+                          0 if base is None else base.stride(0), out.data_ptr(), _ELEM[out.dtype], out.stride(0), _addr(hidden),
+                          scratch.data_ptr(), size, st)
+        if rc:
+            _check(rc, "stmoe_lora")
+    return out
+
+
+def lora_backward(grad, x, a, b, plan, hidden, scale=None, alpha=1.0, stream=None):
+    """stmoe_lora_backward: gradients (of x, a, b) for grad [rows][outer] in x's type, from the hidden that lora wrote."""
+    elem, T, I, n, r, O = _lora_args(x, a, b, plan, scale, hidden)
+    if not (_is_rows(grad, x.dtype) and grad.shape[0] == T and grad.shape[1] == O and grad.device == x.device):
+        _refuse(f"grad: expected {(T, O)} of x's type with contiguous rows on x's device")
+    if hidden is None:
+        _refuse("hidden: what lora wrote is needed")
+    st = _stream_of(x, stream)
+    if st is None:
+        return _there(x, stream, lora_backward, grad, x, a, b, plan, hidden, scale, alpha)
+    dx = torch.empty(T, I, dtype=x.dtype, device=x.device)
+    da, db = torch.empty(n, r, I, dtype=x.dtype, device=x.device), torch.empty(n, O, r, dtype=x.dtype, device=x.device)
+    L = lib()
+    size = L.stmoe_lora_backward_scratch_bytes(T, n, r, I, O)
+    scratch = torch.empty(size, dtype=_U8, device=x.device)
+    if T:
+        rc = L.stmoe_lora_backward(grad.data_ptr(), elem, grad.stride(0), x.data_ptr(), x.stride(0), T, a.data_ptr(), a.stride(0), a.stride(1),
+                                   b.data_ptr(), b.stride(0), b.stride(1), n, r, I, O, plan["ids"].data_ptr(), plan["order"].data_ptr(),
+                                   plan["counts"].data_ptr(), plan["starts"].data_ptr(), _addr(scale), alpha, hidden.data_ptr(), dx.data_ptr(),
+                                   I, da.data_ptr(), db.data_ptr(), scratch.data_ptr(), size, st)
+        if rc:
+            _check(rc, "stmoe_lora_backward")
+    else:
+        da.zero_(), db.zero_()
+    return dx, da, db

@@ -1,0 +1,311 @@
+// Rows grouped by expert (or by adapter), carried into that order and back.
+//
+//   group      ids [T][K] -> counts[g], starts[g] = where group g begins, order[s] = which pair t K + k stands at slot s (stable: pairs of a group in their
+//              order; pairs without a group behind the last), slots[t][k] = its slot, -1 without a group
+//   dispatch   out[slots[t][k]] = x[t]
+//   combine    out[t] = r[t] + c sum_k w[t][k] y[slots[t][k]], in fp32 in the order of k, rounded once
+//   backward   dy[slots[t][k]] = c w[t][k] g[t];  dw[t][k] = c <g[t], y[slots[t][k]]>
+//
+// Grouping is a counting sort.  Every warp owns a stretch of pairs and counts it into its own row of a table in
+// shared memory, 32 pairs at a time: lanes with the same id find one another, the first adds their number, so
+// neither pass has an atomic and equal ids keep their order.  Running sums down the table and across the groups
+// give each warp its place in each group, and a second walk hands the places out.  Few pairs are one CTA's
+// work; more are spread over CTAs that count in a first launch and place in a second.
+//
+// The copies are HBM's work: a row of x is read once and written K times, a row of y is read once.
+#pragma once
+#include "row_utils.cuh"
+
+namespace stmoe_dev {
+
+constexpr int kGrpMaxGroups = 1024;
+constexpr int kGrpThreads = 512, kGrpWarps = kGrpThreads / kWarp;
+constexpr int kGrpCtaPairs = 4096;  // pairs of a CTA where there are several
+constexpr int kGrpMaxCtas = 128;
+
+struct GroupArgs {
+    const int *ids;
+    int pairs, G;
+    int per_warp;           // pairs of a warp, a multiple of 32
+    int *counts, *starts, *order, *slots;
+    int *hist;              // [ctas][G + 1], or nullptr for one CTA
+};
+
+// Counts of a warp's stretch in its row of the table (columns 0..G, the last one for pairs without a group).
+__device__ __forceinline__ int grp_id(const GroupArgs &a, int p)
+{
+    const int e = a.ids[p];
+    return (unsigned)e < (unsigned)a.G ? e : a.G;
+}
+__device__ __forceinline__ void grp_count(const GroupArgs &a, int first, int lane, int *row)
+{
+    const int end = min(first + a.per_warp, a.pairs);
+    for (int p = first + lane; p - lane < end; p += kWarp) {
+        const int e = p < end ? grp_id(a, p) : -1;
+        const unsigned same = __match_any_sync(kFull, e);
+        if (e >= 0 && lane == __ffs(same) - 1) row[e] += __popc(same);
+        __syncwarp();
+    }
+}
+__device__ __forceinline__ int grp_first(const GroupArgs &a, int warp)
+{
+    const long long p = ((long long)blockIdx.x * kGrpWarps + warp) * a.per_warp;
+    return p < a.pairs ? (int)p : a.pairs;
+}
+// Exclusive running sums over the columns 0..G of total, in place, by the whole CTA.
+__device__ __forceinline__ void grp_scan(int *total, int n, int *part)
+{
+    const int tid = threadIdx.x, lane = tid % kWarp, warp = tid / kWarp;
+    int carry = 0;
+    for (int at = 0; at < n; at += kGrpThreads) {
+        const int v = at + tid < n ? total[at + tid] : 0;
+        int s = v;
+#pragma unroll
+        for (int o = 1; o < kWarp; o <<= 1) {
+            const int t = __shfl_up_sync(kFull, s, o);
+            if (lane >= o) s += t;
+        }
+        if (lane == kWarp - 1) part[warp] = s;
+        __syncthreads();
+        int before = carry, all = carry;
+#pragma unroll
+        for (int w = 0; w < kGrpWarps; ++w) {
+            if (w < warp) before += part[w];
+            all += part[w];
+        }
+        if (at + tid < n) total[at + tid] = before + s - v;
+        carry = all;
+        __syncthreads();
+    }
+}
+
+__global__ void __launch_bounds__(kGrpThreads) group_count_kernel(const GroupArgs a)
+{
+    extern __shared__ int table[];              // [kGrpWarps][G + 1]
+    const int n = a.G + 1, tid = threadIdx.x, warp = tid / kWarp;
+    for (int i = tid; i < kGrpWarps * n; i += kGrpThreads) table[i] = 0;
+    __syncthreads();
+    pdl_wait();
+    pdl_launch_dependents();
+    grp_count(a, grp_first(a, warp), tid % kWarp, table + warp * n);
+    __syncthreads();
+    for (int g = tid; g < n; g += kGrpThreads) {
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < kGrpWarps; ++w) sum += table[w * n + g];
+        a.hist[blockIdx.x * n + g] = sum;
+    }
+}
+
+__global__ void __launch_bounds__(kGrpThreads) group_place_kernel(const GroupArgs a)
+{
+    extern __shared__ int table[];              // [kGrpWarps][G + 1], [G + 1] starts
+    __shared__ int part[kGrpWarps];
+    const int n = a.G + 1, tid = threadIdx.x, lane = tid % kWarp, warp = tid / kWarp;
+    int *const start = table + kGrpWarps * n, *const mine = table + warp * n;
+    for (int i = tid; i < kGrpWarps * n; i += kGrpThreads) table[i] = 0;
+    __syncthreads();
+    pdl_wait();
+    pdl_launch_dependents();
+    const int first = grp_first(a, warp), end = min(first + a.per_warp, a.pairs);
+    grp_count(a, first, lane, mine);
+    __syncthreads();
+    for (int g = tid; g < n; g += kGrpThreads) {
+        int before = 0, total = 0;              // in this group: pairs of the CTAs before this one, of all
+        if (a.hist) {
+#pragma unroll 8
+            for (int c = 0; c < (int)gridDim.x; ++c) {
+                const int h = a.hist[c * n + g];
+                before += c < (int)blockIdx.x ? h : 0;
+                total += h;
+            }
+        }
+        int run = before;
+#pragma unroll
+        for (int w = 0; w < kGrpWarps; ++w) {
+            const int c = table[w * n + g];
+            table[w * n + g] = run;
+            run += c;
+        }
+        if (!a.hist) total = run;
+        start[g] = total;
+        if (blockIdx.x == 0 && g < a.G) a.counts[g] = total;
+    }
+    __syncthreads();
+    grp_scan(start, n, part);
+    if (blockIdx.x == 0)
+        for (int g = tid; g < n; g += kGrpThreads) a.starts[g] = start[g];
+    for (int p = first + lane; p - lane < end; p += kWarp) {
+        const int e = p < end ? grp_id(a, p) : -1;
+        const unsigned same = __match_any_sync(kFull, e);
+        if (e >= 0) {
+            const int s = start[e] + mine[e] + __popc(same & ((1u << lane) - 1));
+            a.order[s] = p;
+            a.slots[p] = e < a.G ? s : -1;
+        }
+        __syncwarp();
+        if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+        __syncwarp();
+    }
+}
+
+// ---- rows there and back -------------------------------------------------------------------------
+
+constexpr int kRowThreads = 256;
+
+struct DispatchArgs {
+    const uint8_t *x;
+    long long x_stride, out_stride, row_bytes;   // bytes
+    const int *slots;       // [T][K]
+    const int *rows;        // rows in groups; those behind become 0 (nullptr: stay as they were)
+    int T, K, out_rows;
+    unsigned parts;         // warps that share a row; T * parts < 2^31
+    uint8_t *out;
+};
+
+// U: widest type that every address of the rows is a multiple of.
+template <typename U> __global__ void __launch_bounds__(kRowThreads) dispatch_rows_kernel(const DispatchArgs a)
+{
+    constexpr int kAtOnce = 4;
+    const int lane = threadIdx.x % kWarp;
+    pdl_wait();
+    pdl_launch_dependents();
+    const unsigned task = blockIdx.x * (kRowThreads / kWarp) + threadIdx.x / kWarp, t32 = task / a.parts;
+    const long long t = t32;
+    if (t >= a.T) return;
+    const int n = (int)(a.row_bytes / (int)sizeof(U));
+    const int first = (int)(task - t32 * a.parts) * kWarp * kAtOnce, step = (int)a.parts * kWarp * kAtOnce;
+    const U *const src = reinterpret_cast<const U *>(a.x + t * a.x_stride);
+    const int *const slots = a.slots + t * a.K;
+    const int behind = a.rows ? *a.rows : a.out_rows;
+    for (int at = first; at < n; at += step) {
+        U v[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+            if (at + i * kWarp + lane < n) v[i] = src[at + i * kWarp + lane];
+        for (int k = 0; k < a.K; ++k) {
+            const int s = slots[k];
+            if ((unsigned)s >= (unsigned)a.out_rows) continue;
+            U *const dst = reinterpret_cast<U *>(a.out + s * a.out_stride);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                if (at + i * kWarp + lane < n) dst[at + i * kWarp + lane] = v[i];
+        }
+        for (long long r = max(t * a.K, (long long)behind); r < min((t + 1) * a.K, (long long)a.out_rows); ++r) {
+            U *const dst = reinterpret_cast<U *>(a.out + r * a.out_stride);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                if (at + i * kWarp + lane < n) dst[at + i * kWarp + lane] = U{};
+        }
+    }
+}
+
+struct CombineArgs {
+    const void *y;          // [y_rows][C]
+    long long y_stride;     // elements, as all strides here
+    const int *slots;       // [T][K]
+    const float *w;         // [T][K] or nullptr (1)
+    const void *res;        // combine: [T][C] or nullptr; backward: the gradient
+    long long res_stride;
+    void *out;              // combine: [T][C]; backward: gradient of y
+    long long out_stride;
+    float *dw;              // backward: [T][K] or nullptr
+    const int *rows;        // backward: as in DispatchArgs
+    float scale;
+    int T, K, C, y_rows;
+    unsigned parts;         // warps that share a row; T * parts < 2^31
+    bool vec;               // every row is 16-byte aligned
+};
+
+// DY: type of y, DO: of the residual and the result.
+template <int DY, int DO> __global__ void __launch_bounds__(kRowThreads) combine_rows_kernel(const CombineArgs a)
+{
+    using TY = typename Elem<DY>::T;
+    using TO = typename Elem<DO>::T;
+    const int lane = threadIdx.x % kWarp;
+    pdl_wait();
+    pdl_launch_dependents();
+    const unsigned task = blockIdx.x * (kRowThreads / kWarp) + threadIdx.x / kWarp, t32 = task / a.parts;
+    const long long t = t32;
+    if (t >= a.T) return;
+    const TY *const y = reinterpret_cast<const TY *>(a.y);
+    const TO *const res = a.res ? reinterpret_cast<const TO *>(a.res) + t * a.res_stride : nullptr;
+    TO *const out = reinterpret_cast<TO *>(a.out) + t * a.out_stride;
+    const int *const slots = a.slots + t * a.K;
+    for (int c = ((int)(task - t32 * a.parts) * kWarp + lane) * 8; c < a.C; c += (int)a.parts * kWarp * 8) {
+        float sum[8];
+        if (res) row_load8<DO>(res, c, a.C, a.vec, sum);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+        }
+#pragma unroll 4
+        for (int k = 0; k < a.K; ++k) {
+            const int s = slots[k];
+            if ((unsigned)s >= (unsigned)a.y_rows) continue;
+            const float w = a.w ? a.scale * a.w[t * a.K + k] : a.scale;
+            float v[8];
+            row_load8<DY>(y + s * a.y_stride, c, a.C, a.vec, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
+        }
+        row_store8<DO>(out, c, a.C, a.vec, sum);
+    }
+}
+
+// WPT warps share a token (and reduce its inner products through shared memory, in a fixed order).
+template <int DY, int DG, int WPT> __global__ void __launch_bounds__(kRowThreads) combine_rows_backward_kernel(const CombineArgs a)
+{
+    using TY = typename Elem<DY>::T;
+    using TG = typename Elem<DG>::T;
+    constexpr int kTokens = kRowThreads / kWarp / WPT;
+    __shared__ float s_dot[kRowThreads / kWarp];
+    const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp, part = warp % WPT;
+    pdl_wait();
+    pdl_launch_dependents();
+    const long long t = (long long)blockIdx.x * kTokens + warp / WPT;
+    if (WPT == 1 && t >= a.T) return;           // WPT > 1: all warps of the CTA share one token
+    const TY *const y = reinterpret_cast<const TY *>(a.y);
+    TY *const dy = reinterpret_cast<TY *>(a.out);
+    const TG *const g = reinterpret_cast<const TG *>(a.res) + t * a.res_stride;
+    for (int k = 0; k < a.K; ++k) {
+        const int s = a.slots[t * a.K + k];
+        const bool there = (unsigned)s < (unsigned)a.y_rows;
+        float dot = 0.f;
+        if (there) {
+            const float w = a.w ? a.scale * a.w[t * a.K + k] : a.scale;
+#pragma unroll 2
+            for (int c = (part * kWarp + lane) * 8; c < a.C; c += WPT * kWarp * 8) {
+                float gv[8], v[8];
+                row_load8<DG>(g, c, a.C, a.vec, gv);
+                if (a.dw) {
+                    row_load8<DY>(y + s * a.y_stride, c, a.C, a.vec, v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dot = fmaf(gv[i], v[i], dot);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = w * gv[i];
+                row_store8<DY>(dy + s * a.out_stride, c, a.C, a.vec, v);
+            }
+        }
+        if (a.dw) {
+            dot = warp_sum(dot);
+            if (WPT > 1) {
+                __syncthreads();
+                if (lane == 0) s_dot[warp] = dot;
+                __syncthreads();
+                dot = 0.f;
+#pragma unroll
+                for (int i = 0; i < WPT; ++i) dot += s_dot[i];
+            }
+            if (part == 0 && lane == 0) a.dw[t * a.K + k] = there ? a.scale * dot : 0.f;
+        }
+    }
+    if (a.rows) {
+        const float zero[8] = {};
+        for (long long r = max(t * a.K, (long long)*a.rows); r < min((t + 1) * a.K, (long long)a.y_rows); ++r)
+            for (int c = (part * kWarp + lane) * 8; c < a.C; c += WPT * kWarp * 8) row_store8<DY>(dy + r * a.out_stride, c, a.C, a.vec, zero);
+    }
+}
+
+}  // namespace stmoe_dev

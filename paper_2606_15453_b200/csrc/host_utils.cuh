@@ -19,6 +19,16 @@ inline int cuda_status(cudaError_t e)
 // whether every one of these is NULL or on a boundary of its element type's size
 template <typename... T> bool aligned(const T *...p) { return ((((uintptr_t)p & (sizeof(T) - 1)) == 0) && ...); }
 
+// A matrix in memory (stride in elements of so many bytes), and whether two of them share some, seen from their first to
+// their last element.
+struct Span {
+    const void *p;
+    int64_t stride, rows, cols;
+    int bytes;
+    uintptr_t end() const { return (uintptr_t)p + bytes * ((rows > 1 ? (rows - 1) * stride : 0) + cols); }
+};
+inline bool overlap(const Span &a, const Span &b) { return a.rows && b.rows && (uintptr_t)a.p < b.end() && (uintptr_t)b.p < a.end(); }
+
 // ordinal of the current device, and how many SMs it has
 inline int current_device(int *dev, int *sms)
 {
@@ -32,10 +42,10 @@ inline int current_device(int *dev, int *sms)
 // Launch that may start while the kernel before it in the stream drains (programmatic dependent
 // launch; the kernels wait for it themselves), in clusters of `cluster` CTAs.
 template <typename... P, typename... A>
-int launch_behind(void (*kernel)(P...), int grid, int block, size_t smem, int cluster, cudaStream_t st, const A &...args)
+int launch_behind(void (*kernel)(P...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t st, const A &...args)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = st;
+    cfg.gridDim = grid, cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;

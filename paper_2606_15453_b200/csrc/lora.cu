@@ -1,0 +1,188 @@
+// C entry points of the adapters of many requests (lora.cuh).
+#include "../../include/stmoe.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "host_utils.cuh"
+#include "lora.cuh"
+
+using namespace stmoe_dev;
+using namespace stmoe_host;
+
+namespace {
+
+bool half_ok(int dtype) { return dtype == STMOE_BF16 || dtype == STMOE_F16; }
+int elem_bytes(int dtype) { return dtype == STMOE_F32 ? 4 : 2; }
+bool rows_ok(const void *p, int dtype, int64_t stride, int64_t rows, int64_t cols)
+{
+    return p && (rows <= 1 || stride >= cols) && ((uintptr_t)p & (elem_bytes(dtype) - 1)) == 0;
+}
+bool rows_vec(const void *p, int dtype, int64_t stride) { return ((uintptr_t)p & 15) == 0 && stride * elem_bytes(dtype) % 16 == 0; }
+int64_t up_to(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+constexpr int kMaxLength = 1 << 24;       // of inner and outer
+bool sizes_ok(int64_t tokens, int n, int rank, int inner, int outer)
+{
+    return tokens >= 0 && tokens <= INT32_MAX / 2 && n >= 1 && n <= kLoraMaxAdapters && rank >= 1 && rank <= kLoraMaxRank && inner >= 1 &&
+           inner <= kMaxLength && outer >= 1 && outer <= kMaxLength;
+}
+// Parts of the inner dimension: enough CTAs for the GPU where rows are few, two steps to a warp at least.
+int down_splits(int64_t tokens, int inner)
+{
+    const int64_t steps = (inner + kLoraStep - 1) / kLoraStep;
+    const int64_t most = std::min<int64_t>(16, (steps + 2 * kLoraWarps - 1) / (2 * kLoraWarps));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(most, 592 / std::max<int64_t>(1, tokens)));
+}
+int64_t part_bytes(int64_t tokens, int rank, int inner) { return up_to((int64_t)sizeof(float) * down_splits(tokens, inner) * tokens * up_to(rank, 8), 256); }
+int grad_task_rows(int64_t tokens) { return (int)std::max<int64_t>(512, up_to((tokens + 15) / 16, kGradPos)); }
+int grad_parts(int64_t tokens) { return (int)(2 * tokens / grad_task_rows(tokens)); }
+
+int launch_down(const LoraArgs &a, int dtype, cudaStream_t st)
+{
+    const bool vec = rows_vec(a.x, dtype, a.T > 1 ? a.x_stride : 0) && rows_vec(a.a, dtype, a.a_row) && a.a_group % 8 == 0 && a.I % 8 == 0;
+    const dim3 grid(a.T, a.splits, (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
+    if (dtype == STMOE_BF16)
+        return vec ? launch_behind(lora_down_kernel<1, true>, grid, kLoraThreads, 0, 1, st, a) : launch_behind(lora_down_kernel<1, false>, grid, kLoraThreads, 0, 1, st, a);
+    return vec ? launch_behind(lora_down_kernel<4, true>, grid, kLoraThreads, 0, 1, st, a) : launch_behind(lora_down_kernel<4, false>, grid, kLoraThreads, 0, 1, st, a);
+}
+template <int DT, int DO, int PL> int launch_up_as(const LoraArgs &a, bool vec, cudaStream_t st)
+{
+    const dim3 grid(a.T, (a.O + kLoraOutBlock - 1) / kLoraOutBlock);
+    return vec ? launch_behind(lora_up_kernel<DT, DO, PL, true>, grid, kLoraThreads, 0, 1, st, a)
+               : launch_behind(lora_up_kernel<DT, DO, PL, false>, grid, kLoraThreads, 0, 1, st, a);
+}
+int launch_up(LoraArgs &a, int dtype, int out_dtype, cudaStream_t st)
+{
+    const int64_t tall = a.T > 1;
+    a.out_vec = rows_vec(a.out, out_dtype, tall * a.out_stride) && (!a.base || rows_vec(a.base, out_dtype, tall * a.base_stride));
+    const bool vec = rows_vec(a.b, dtype, a.b_row) && a.b_group % 8 == 0 && a.r % 8 == 0;
+    if (dtype == STMOE_BF16) return out_dtype == STMOE_F32 ? launch_up_as<1, 0, 3>(a, vec, st) : launch_up_as<1, 1, 2>(a, vec, st);
+    return out_dtype == STMOE_F32 ? launch_up_as<4, 0, 3>(a, vec, st) : launch_up_as<4, 4, 2>(a, vec, st);
+}
+int launch_transpose(const void *b, int64_t group, int64_t row, int rows, int cols, int n, uint16_t *t, int64_t t_row, cudaStream_t st)
+{
+    LoraTransposeArgs a{};
+    a.b = (const uint16_t *)b, a.b_group = group, a.b_row = row, a.rows = rows, a.cols = cols;
+    a.t = t, a.t_row = t_row, a.t_group = t_row * cols;
+    return launch_behind(lora_transpose_kernel, dim3((rows + 31) / 32, (cols + 31) / 32, n), kLoraThreads, 0, 1, st, a);
+}
+template <int DT> int launch_grad(const LoraGradArgs &a, int dev, cudaStream_t st)
+{
+    constexpr int smem = (int)sizeof(float) * kLoraRankBlock * (kGradCols + 1);
+    static PerDevice<bool> asked;       // more than 48 KB of shared memory: asked for once per device
+    bool done = false;
+    if (const int rc = asked.get(dev, &done, [](bool &) {
+            return cuda_status(cudaFuncSetAttribute(lora_grad_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        }))
+        return rc;
+    const dim3 grid(a.n + a.T / a.task_rows, (a.C + kGradCols - 1) / kGradCols, (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
+    if (const int rc = launch_behind(lora_grad_kernel<DT>, grid, kLoraThreads, smem, 1, st, a)) return rc;
+    if (a.T <= a.task_rows) return STMOE_OK;    // no adapter has several tasks
+    const int64_t size = (int64_t)a.r * a.C;
+    return launch_behind(lora_grad_sum_kernel<DT>, dim3(a.n, (unsigned)std::min<int64_t>(256, (size + kLoraThreads - 1) / kLoraThreads)), kLoraThreads, 0, 1, st, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer)
+{
+    return sizes_ok(tokens, n_adapters, rank, inner, outer) ? (size_t)part_bytes(tokens, rank, inner) : 0;
+}
+
+int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,
+               int64_t b_row, int n_adapters, int rank, int inner, int outer, const int32_t *ids, const int32_t *order, const float *scale,
+               float alpha, const void *base, int64_t base_stride, void *out, int out_dtype, int64_t out_stride, float *hidden, void *scratch,
+               size_t scratch_bytes, void *cuda_stream)
+{
+    if (!half_ok(dtype) || (out_dtype != dtype && out_dtype != STMOE_F32) || !sizes_ok(tokens, n_adapters, rank, inner, outer) ||
+        !rows_ok(x, dtype, x_stride, tokens, inner) || !rows_ok(a, dtype, a_row, rank, inner) || !rows_ok(b, dtype, b_row, outer, rank) ||
+        (n_adapters > 1 && (a_group < 0 || b_group < 0)) || !rows_ok(out, out_dtype, out_stride, tokens, outer) ||
+        (base && !rows_ok(base, out_dtype, base_stride, tokens, outer)) || !ids || !order || !aligned(ids, order) || !aligned(scale, (const float *)hidden))
+        return STMOE_ERR_BAD_ARG;
+    if (tokens == 0) return STMOE_OK;
+    if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < stmoe_lora_scratch_bytes(tokens, n_adapters, rank, inner, outer)) return STMOE_ERR_BAD_ARG;
+    const int xb = elem_bytes(dtype), ob = elem_bytes(out_dtype);
+    const bool same = base == out && (tokens == 1 || base_stride == out_stride);
+    const Span to{out, out_stride, tokens, outer, ob};
+    if (overlap({x, x_stride, tokens, inner, xb}, to) || (base && !same && overlap({base, base_stride, tokens, outer, ob}, to))) return STMOE_ERR_BAD_ARG;
+    int dev = 0, sms = 0;
+    if (const int rc = current_device(&dev, &sms)) return rc;
+    LoraArgs k{};
+    k.x = x, k.x_stride = x_stride, k.a = a, k.b = b, k.a_group = a_group, k.a_row = a_row, k.b_group = b_group, k.b_row = b_row;
+    k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.I = inner, k.O = outer;
+    k.splits = down_splits(tokens, inner), k.rp = (int)up_to(rank, 8), k.part = (float *)scratch;
+    k.steps = ((inner + kLoraStep - 1) / kLoraStep + k.splits - 1) / k.splits;
+    k.splits = ((inner + kLoraStep - 1) / kLoraStep + k.steps - 1) / k.steps;
+    k.base = base, k.base_stride = base_stride, k.out = out, k.out_stride = out_stride, k.keep = same, k.hidden = hidden;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (const int rc = launch_down(k, dtype, st)) return rc;
+    return launch_up(k, dtype, out_dtype, st);
+}
+
+size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer)
+{
+    if (!sizes_ok(tokens, n_adapters, rank, inner, outer)) return 0;
+    int64_t n = up_to((int64_t)2 * n_adapters * rank * up_to(outer, 8), 256) + up_to((int64_t)2 * n_adapters * inner * up_to(rank, 8), 256);
+    n += part_bytes(tokens, rank, outer) + up_to((int64_t)sizeof(float) * tokens * rank, 256);
+    return (size_t)(n + (int64_t)sizeof(float) * grad_parts(tokens) * rank * std::max(inner, outer));
+}
+
+int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const void *x, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group,
+                        int64_t a_row, const void *b, int64_t b_group, int64_t b_row, int n_adapters, int rank, int inner, int outer,
+                        const int32_t *ids, const int32_t *order, const int32_t *counts, const int32_t *starts, const float *scale, float alpha,
+                        const float *hidden, void *grad_x, int64_t grad_x_stride, void *grad_a, void *grad_b, void *scratch, size_t scratch_bytes,
+                        void *cuda_stream)
+{
+    if (!half_ok(dtype) || !sizes_ok(tokens, n_adapters, rank, inner, outer) || !rows_ok(grad, dtype, grad_stride, tokens, outer) ||
+        !rows_ok(x, dtype, x_stride, tokens, inner) || !rows_ok(a, dtype, a_row, rank, inner) || !rows_ok(b, dtype, b_row, outer, rank) ||
+        (n_adapters > 1 && (a_group < 0 || b_group < 0)) || !rows_ok(grad_x, dtype, grad_x_stride, tokens, inner) ||
+        !ids || !order || !counts || !starts || (grad_b && !hidden) || !aligned(ids, order, counts, starts) || !aligned(scale, hidden) ||
+        !aligned((const uint16_t *)grad_a, (const uint16_t *)grad_b))
+        return STMOE_ERR_BAD_ARG;
+    const size_t need = stmoe_lora_backward_scratch_bytes(tokens, n_adapters, rank, inner, outer);
+    if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < need) return STMOE_ERR_BAD_ARG;
+    const Span to{grad_x, grad_x_stride, tokens, inner, 2};
+    if (overlap({x, x_stride, tokens, inner, 2}, to) || overlap({grad, grad_stride, tokens, outer, 2}, to)) return STMOE_ERR_BAD_ARG;
+    int dev = 0, sms = 0;
+    if (const int rc = current_device(&dev, &sms)) return rc;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    uint8_t *at = (uint8_t *)scratch;
+    auto take = [&](int64_t bytes) { uint8_t *p = at; at += up_to(bytes, 256); return p; };
+    const int64_t outer8 = up_to(outer, 8), rank8 = up_to(rank, 8);
+    uint16_t *const bt = (uint16_t *)take((int64_t)2 * n_adapters * rank * outer8), *const a_t = (uint16_t *)take((int64_t)2 * n_adapters * inner * rank8);
+    float *const part = (float *)take(part_bytes(tokens, rank, outer)), *const u = (float *)take((int64_t)sizeof(float) * tokens * rank);
+    float *const parts = (float *)at;
+    if (tokens) {
+        if (const int rc = launch_transpose(b, b_group, b_row, outer, rank, n_adapters, bt, outer8, st)) return rc;
+        if (const int rc = launch_transpose(a, a_group, a_row, rank, inner, n_adapters, a_t, rank8, st)) return rc;
+        // the forward kernels with the roles of A and B exchanged
+        LoraArgs k{};
+        k.x = grad, k.x_stride = grad_stride, k.a = bt, k.a_row = outer8, k.a_group = rank * outer8, k.b = a_t, k.b_row = rank8, k.b_group = inner * rank8;
+        k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.I = outer, k.O = inner;
+        k.splits = down_splits(tokens, outer), k.rp = (int)up_to(rank, 8), k.part = part;
+        k.steps = ((outer + kLoraStep - 1) / kLoraStep + k.splits - 1) / k.splits;
+        k.splits = ((outer + kLoraStep - 1) / kLoraStep + k.steps - 1) / k.steps;
+        k.out = grad_x, k.out_stride = grad_x_stride, k.hidden = u;
+        if (const int rc = launch_down(k, dtype, st)) return rc;
+        if (const int rc = launch_up(k, dtype, dtype, st)) return rc;
+    }
+    LoraGradArgs g{};
+    g.order = order, g.counts = counts, g.starts = starts, g.scale = scale, g.alpha = alpha, g.T = (int)tokens, g.n = n_adapters, g.r = rank;
+    g.task_rows = grad_task_rows(tokens), g.parts = grad_parts(tokens), g.part = parts;
+    if (grad_a) {
+        g.u = u, g.z = x, g.z_stride = x_stride, g.C = inner, g.by_col = false, g.grad = grad_a;
+        g.vec = rows_vec(x, dtype, tokens > 1 ? x_stride : 0);
+        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, dev, st) : launch_grad<4>(g, dev, st)) return rc;
+    }
+    if (grad_b) {
+        g.u = hidden, g.z = grad, g.z_stride = grad_stride, g.C = outer, g.by_col = true, g.grad = grad_b;
+        g.vec = rows_vec(grad, dtype, tokens > 1 ? grad_stride : 0);
+        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, dev, st) : launch_grad<4>(g, dev, st)) return rc;
+    }
+    return STMOE_OK;
+}
+
+}  // extern "C"

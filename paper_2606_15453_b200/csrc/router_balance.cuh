@@ -27,7 +27,7 @@
 // registers that the loads need: 92.3 -> 93.9 us for 524288 x 128, both directions.)  lse^2 is summed in fp64 throughout: a
 // row at a fill value of 1e20 has one that fp32 does not hold, while the mean over the rows may.
 #pragma once
-#include "mx4.cuh"
+#include "row_utils.cuh"
 
 namespace stmoe_dev {
 
@@ -38,7 +38,6 @@ constexpr int kBalDepth = 3;        // steps of rows in shared memory: one in us
 constexpr int kBalFinish = 8;       // CTAs of the cluster that adds the partial sums up
 constexpr int kBalLaneSteps = 128; // steps of a CTA at most: so many times kBalRows rows a lane
 constexpr float kBalPlainMax = 1048576.f;   // 2^20: largest |maximum| of a row without a subtraction of its own
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // a CTA's partial sums: [E] probabilities, the low word of lse^2 (fp64), then (int) [E] counts, rows, and
 // the high word
@@ -61,35 +60,6 @@ struct BalanceArgs {
     long long dstride;
 };
 
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// Two fp32 operations in one instruction (each rounded on its own, as the single ones are).
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(r)
-        : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)), "l"(*reinterpret_cast<const uint64_t *>(&c)));
-    return *reinterpret_cast<const float2 *>(&r);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)));
-    return *reinterpret_cast<const float2 *>(&r);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)));
-    return *reinterpret_cast<const float2 *>(&r);
-}
-
 // Where lane l of a row's LPR lanes finds its N logits: in vector order (groups of 16 bytes, lane after
 // lane) or one by one.
 template <int DT, int LPR> __device__ __forceinline__ int bal_index(int l, int i, bool vec)
@@ -107,54 +77,6 @@ template <int DT, int LPR, int N> __device__ __forceinline__ void bal_load(const
         (i & 1 ? z[i / 2].y : z[i / 2].x) = e < E ? Elem<DT>::to_f32(row[e]) : -INFINITY;
     }
 }
-// 16 bytes of a row, widened
-template <int DT> __device__ __forceinline__ void bal_widen(const uint4 &q, float2 *z)
-{
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    if constexpr (DT == 0) {
-        z[0] = make_float2(__uint_as_float(w[0]), __uint_as_float(w[1]));
-        z[1] = make_float2(__uint_as_float(w[2]), __uint_as_float(w[3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (DT == 1) z[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
-            else z[i] = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-        }
-    }
-}
-template <int DT> __device__ __forceinline__ uint4 bal_narrow(const float2 *z)
-{
-    uint32_t w[4];
-    if constexpr (DT == 0) {
-        w[0] = __float_as_uint(z[0].x), w[1] = __float_as_uint(z[0].y), w[2] = __float_as_uint(z[1].x), w[3] = __float_as_uint(z[1].y);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (DT == 1) {
-                const __nv_bfloat162 h = __float22bfloat162_rn(z[i]);
-                w[i] = *reinterpret_cast<const uint32_t *>(&h);
-            } else {
-                const __half2 h = __float22half2_rn(z[i]);
-                w[i] = *reinterpret_cast<const uint32_t *>(&h);
-            }
-        }
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-template <int LPR> __device__ __forceinline__ float lanes_max(float v)
-{
-#pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
-    return v;
-}
-template <int LPR> __device__ __forceinline__ float lanes_sum(float v)
-{
-#pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
-    return v;
-}
-
 // z -> exp(z - max) in place, inv: 1 / their sum; returns lse.  live: the row has a logit above
 // -infinity (NaN included: then the row's results are NaN, as the formulas say).
 template <int LPR, int P> __device__ __forceinline__ float bal_softmax(float2 (&z)[P], float &inv, bool &live)
