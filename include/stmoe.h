@@ -252,7 +252,7 @@ int stmoe_set_copy_throttle(stmoe_t *s, int64_t chunk_bytes, int gap_us);
  * Any stack: POLL_LIMIT n = polls after which a grid-barrier wait of the single-sequence
  * persistent kernel gives up (default 2^22).
  * No stack (s NULL): MX4_POLL_LIMIT n = polls, of about 4 us each, after which a wait inside the MX4
- * product and FFN kernels gives up, in every launch of the process from then on (default and most 2^22;
+ * product and FFN kernels and the adapters' tile kernels gives up, in every launch of the process from then on (default and most 2^22;
  * 0: at once; a captured graph keeps the limit it was captured with). */
 #define STMOE_HOOK_DROP_PREFETCH 1
 #define STMOE_HOOK_FAIL_COPY 2
@@ -527,23 +527,22 @@ int stmoe_combine_rows_backward(const void *grad, int grad_dtype, int64_t grad_s
 
 /* out[t] = base[t] + alpha * scale[g] * (x[t] A_g^T) B_g^T, g = ids[t]; rows whose id is outside [0, n_adapters): out = base.
  *   x      [tokens][inner] in dtype (STMOE_BF16 or STMOE_F16); A [n_adapters][rank][inner], B [n_adapters][outer][rank] in the same type
- *   ids    int32 [tokens];  order: the permutation that stmoe_group_rows makes of them (top_k 1, n_adapters groups); ids[order[.]] has to
- *          hold each adapter's rows side by side.  Rows that order does not name are left as they were
+ *   ids    int32 [tokens];  order, counts, starts: what stmoe_group_rows makes of them (top_k 1, n_adapters groups)
  *   scale  fp32 [n_adapters], or NULL: 1
  *   base, out  [tokens][outer] in out_dtype (dtype or STMOE_F32); base may be NULL (0) or out itself; nothing else may overlap
  *   hidden fp32 [tokens][rank], or NULL: receives x A^T (0 for rows without an adapter), which the gradient of B needs
  *   scratch  stmoe_lora_scratch_bytes(...) bytes, 16-byte aligned, contents free; calls that can overlap need scratch of their own
  * Strides in elements; a_group, b_group: from one adapter to the next.  Sums in fp32, one rounding of out; x A^T is kept to 2^-17 (out fp32:
  * 2^-24) of itself.  n_adapters <= 1024, rank <= 256, inner and outer <= 2^24; tokens may be 0 (or 1: a decode step).  The same call gives the same bits every
- * time.  16-byte aligned rows (rank a multiple of 8 for B) are read 16 bytes at a time, others element by element.  Asynchronous on cuda_stream. */
+ * time.  16-byte aligned rows (rank a multiple of 8 for B) are read 16 bytes at a time, others element by element.  Should a bounded wait inside a kernel run out, the outputs that depend on it are NaN.  Asynchronous on cuda_stream. */
 size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer);
 int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,
-               int64_t b_row, int n_adapters, int rank, int inner, int outer, const int32_t *ids, const int32_t *order, const float *scale,
-               float alpha, const void *base, int64_t base_stride, void *out, int out_dtype, int64_t out_stride, float *hidden, void *scratch,
+               int64_t b_row, int n_adapters, int rank, int inner, int outer, const int32_t *ids, const int32_t *order,
+               const int32_t *counts, const int32_t *starts, const float *scale, float alpha, const void *base, int64_t base_stride, void *out, int out_dtype, int64_t out_stride, float *hidden, void *scratch,
                size_t scratch_bytes, void *cuda_stream);
 /* Gradients for grad [tokens][outer] in dtype: grad_x [tokens][inner] = c u A with u = grad B (0 for rows without an adapter; the base's gradient
  * is grad itself), grad_a [n][rank][inner] = c sum_t u^T x, grad_b [n][outer][rank] = c sum_t grad^T hidden, c = alpha * scale[g]; contiguous, in dtype,
- * each rounded once, 0 for adapters without rows; grad_a and grad_b may be NULL.  counts, starts: of the grouping that made order.
+ * each rounded once, 0 for adapters without rows; grad_a and grad_b may be NULL.
  * scale is held constant.  scratch: stmoe_lora_backward_scratch_bytes(...) bytes, 256-byte aligned.  grad_x may overlap neither grad nor x. */
 size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer);
 int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const void *x, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group,

@@ -112,7 +112,7 @@ def lib():
         L.stmoe_combine_rows_backward.argtypes = [vp, i32, i64, vp, i32, i64, i64, vp, vp, f32, i64, i32, i64, vp, vp, i64, vp, vp]
         L.stmoe_lora_scratch_bytes.restype = L.stmoe_lora_backward_scratch_bytes.restype = sz
         L.stmoe_lora_scratch_bytes.argtypes = L.stmoe_lora_backward_scratch_bytes.argtypes = [i64, i32, i32, i32, i32]
-        L.stmoe_lora.argtypes = [vp, i32, i64, i64, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, f32, vp, i64, vp, i32,
+        L.stmoe_lora.argtypes = [vp, i32, i64, i64, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, f32, vp, i64, vp, i32,
                                  i64, vp, vp, sz, vp]
         L.stmoe_lora_backward.argtypes = [vp, i32, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp,
                                           f32, vp, vp, i64, vp, vp, vp, sz, vp]
@@ -916,8 +916,8 @@ def lora(x, a, b, plan, scale=None, alpha=1.0, base=None, out=None, hidden=None,
         size = L.stmoe_lora_scratch_bytes(T, n, r, I, O)
         scratch = torch.empty(size, dtype=_U8, device=x.device)
         rc = L.stmoe_lora(x.data_ptr(), elem, x.stride(0), T, a.data_ptr(), a.stride(0), a.stride(1), b.data_ptr(), b.stride(0), b.stride(1), n, r, I, O,
-                          plan["ids"].data_ptr(), plan["order"].data_ptr(), _addr(scale), alpha, _addr(base),
-                          0 if base is None else base.stride(0), out.data_ptr(), _ELEM[out.dtype], out.stride(0), _addr(hidden),
+                          plan["ids"].data_ptr(), plan["order"].data_ptr(), plan["counts"].data_ptr(), plan["starts"].data_ptr(), _addr(scale), alpha,
+                          _addr(base), 0 if base is None else base.stride(0), out.data_ptr(), _ELEM[out.dtype], out.stride(0), _addr(hidden),
                           scratch.data_ptr(), size, st)
         if rc:
             _check(rc, "stmoe_lora")

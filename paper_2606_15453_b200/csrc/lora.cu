@@ -5,7 +5,7 @@
 #include <cmath>
 
 #include "host_utils.cuh"
-#include "lora.cuh"
+#include "lora_tile.cuh"
 
 using namespace stmoe_dev;
 using namespace stmoe_host;
@@ -27,38 +27,78 @@ bool sizes_ok(int64_t tokens, int n, int rank, int inner, int outer)
     return tokens >= 0 && tokens <= INT32_MAX / 2 && n >= 1 && n <= kLoraMaxAdapters && rank >= 1 && rank <= kLoraMaxRank && inner >= 1 &&
            inner <= kMaxLength && outer >= 1 && outer <= kMaxLength;
 }
-// Parts of the inner dimension: enough CTAs for the GPU where rows are few, two steps to a warp at least.
-int down_splits(int64_t tokens, int inner)
+// The tile kernels' share: MEASURED
+bool by_tiles(int64_t tokens, int rank) { return tokens >= 256 && rank <= kTileMaxRank; }
+// Parts of the inner dimension: enough CTAs for the GPU where rows are few, two steps to a warp (four to a tile) at least.
+int down_splits(int64_t tokens, int rank, int inner)
 {
+    if (by_tiles(tokens, rank)) {
+        const int64_t most = std::min<int64_t>(8, (inner + 255) / 256);
+        return (int)std::max<int64_t>(1, std::min<int64_t>(most, 296 / ((tokens + kTileRows - 1) / kTileRows)));
+    }
     const int64_t steps = (inner + kLoraStep - 1) / kLoraStep;
     const int64_t most = std::min<int64_t>(16, (steps + 2 * kLoraWarps - 1) / (2 * kLoraWarps));
     return (int)std::max<int64_t>(1, std::min<int64_t>(most, 592 / std::max<int64_t>(1, tokens)));
 }
-int64_t part_bytes(int64_t tokens, int rank, int inner) { return up_to((int64_t)sizeof(float) * down_splits(tokens, inner) * tokens * up_to(rank, 8), 256); }
+int64_t part_bytes(int64_t tokens, int rank, int inner) { return up_to((int64_t)sizeof(float) * down_splits(tokens, rank, inner) * tokens * up_to(rank, 8), 256); }
 int grad_task_rows(int64_t tokens) { return (int)std::max<int64_t>(512, up_to((tokens + 15) / 16, kGradPos)); }
 int grad_parts(int64_t tokens) { return (int)(2 * tokens / grad_task_rows(tokens)); }
 
-int launch_down(const LoraArgs &a, int dtype, cudaStream_t st)
+// more than the default 48 KB of shared memory: asked for once per device
+template <typename K> int smem_of(PerDevice<bool> &asked, int dev, K kernel, int bytes)
 {
-    const bool vec = rows_vec(a.x, dtype, a.T > 1 ? a.x_stride : 0) && rows_vec(a.a, dtype, a.a_row) && a.a_group % 8 == 0 && a.I % 8 == 0;
-    const dim3 grid(a.T, a.splits, (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
-    if (dtype == STMOE_BF16)
-        return vec ? launch_behind(lora_down_kernel<1, true>, grid, kLoraThreads, 0, 1, st, a) : launch_behind(lora_down_kernel<1, false>, grid, kLoraThreads, 0, 1, st, a);
-    return vec ? launch_behind(lora_down_kernel<4, true>, grid, kLoraThreads, 0, 1, st, a) : launch_behind(lora_down_kernel<4, false>, grid, kLoraThreads, 0, 1, st, a);
+    bool done = false;
+    return asked.get(dev, &done, [=](bool &) { return cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)); });
 }
-template <int DT, int DO, int PL> int launch_up_as(const LoraArgs &a, bool vec, cudaStream_t st)
+template <int DT, bool XVEC, bool WVEC> int launch_down_tiles(const LoraArgs &a, int dev, cudaStream_t st)
 {
+    static PerDevice<bool> asked;
+    if (const int rc = smem_of(asked, dev, lora_down_tile_kernel<DT, XVEC, WVEC>, 97 * 1024)) return rc;
+    const int tiles = (int)std::min<int64_t>(a.T, a.T / kTileRows + a.n);
+    return launch_behind(lora_down_tile_kernel<DT, XVEC, WVEC>, dim3(tiles, a.splits), kDownTileThreads, 1024 + down_stages(a.r) * down_stage_bytes(a.r), 1, st, a);
+}
+template <int DT> int launch_down_as(const LoraArgs &a, bool xvec, bool wvec, int dev, cudaStream_t st)
+{
+    if (by_tiles(a.T, a.r)) {
+        if (xvec) return wvec ? launch_down_tiles<DT, true, true>(a, dev, st) : launch_down_tiles<DT, true, false>(a, dev, st);
+        return wvec ? launch_down_tiles<DT, false, true>(a, dev, st) : launch_down_tiles<DT, false, false>(a, dev, st);
+    }
+    const dim3 grid(a.T, a.splits, (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
+    return xvec && wvec ? launch_behind(lora_down_kernel<DT, true>, grid, kLoraThreads, 0, 1, st, a) : launch_behind(lora_down_kernel<DT, false>, grid, kLoraThreads, 0, 1, st, a);
+}
+int launch_down(LoraArgs &a, int dtype, int dev, cudaStream_t st)
+{
+    a.splits = down_splits(a.T, a.r, a.I);
+    const int step = by_tiles(a.T, a.r) ? 64 : kLoraStep, steps = (a.I + step - 1) / step;
+    a.steps = (steps + a.splits - 1) / a.splits;
+    a.splits = (steps + a.steps - 1) / a.steps;
+    const bool xvec = rows_vec(a.x, dtype, a.T > 1 ? a.x_stride : 0) && a.I % 8 == 0;
+    const bool wvec = rows_vec(a.a, dtype, a.r > 1 ? a.a_row : 0) && (a.n == 1 || a.a_group % 8 == 0) && a.I % 8 == 0;
+    return dtype == STMOE_BF16 ? launch_down_as<1>(a, xvec, wvec, dev, st) : launch_down_as<4>(a, xvec, wvec, dev, st);
+}
+template <int DT, int DO, int PL, bool WVEC> int launch_up_tiles(const LoraArgs &a, int dev, int sms, cudaStream_t st)
+{
+    static PerDevice<bool> asked;
+    if (const int rc = smem_of(asked, dev, lora_up_tile_kernel<DT, DO, PL, WVEC>, up_smem(kTileMaxRank, PL))) return rc;
+    const int smem = up_smem(a.r, PL), sm = smem <= 110 * 1024 ? 2 : 1;
+    const int64_t units = std::min<int64_t>(a.T, a.T / kTileRows + a.n + 1) * ((a.O + kUpCols - 1) / kUpCols);
+    if (units > INT32_MAX) return STMOE_ERR_TOO_LARGE;
+    return launch_behind(lora_up_tile_kernel<DT, DO, PL, WVEC>, (int)std::min<int64_t>(units, sms * sm), kUpTileThreads, smem, 1, st, a);
+}
+template <int DT, int DO, int PL> int launch_up_as(const LoraArgs &a, bool vec, int dev, int sms, cudaStream_t st)
+{
+    if (by_tiles(a.T, a.r)) return vec ? launch_up_tiles<DT, DO, PL, true>(a, dev, sms, st) : launch_up_tiles<DT, DO, PL, false>(a, dev, sms, st);
     const dim3 grid(a.T, (a.O + kLoraOutBlock - 1) / kLoraOutBlock);
     return vec ? launch_behind(lora_up_kernel<DT, DO, PL, true>, grid, kLoraThreads, 0, 1, st, a)
                : launch_behind(lora_up_kernel<DT, DO, PL, false>, grid, kLoraThreads, 0, 1, st, a);
 }
-int launch_up(LoraArgs &a, int dtype, int out_dtype, cudaStream_t st)
+int launch_up(LoraArgs &a, int dtype, int out_dtype, int dev, int sms, cudaStream_t st)
 {
     const int64_t tall = a.T > 1;
     a.out_vec = rows_vec(a.out, out_dtype, tall * a.out_stride) && (!a.base || rows_vec(a.base, out_dtype, tall * a.base_stride));
-    const bool vec = rows_vec(a.b, dtype, a.b_row) && a.b_group % 8 == 0 && a.r % 8 == 0;
-    if (dtype == STMOE_BF16) return out_dtype == STMOE_F32 ? launch_up_as<1, 0, 3>(a, vec, st) : launch_up_as<1, 1, 2>(a, vec, st);
-    return out_dtype == STMOE_F32 ? launch_up_as<4, 0, 3>(a, vec, st) : launch_up_as<4, 4, 2>(a, vec, st);
+    const bool vec = rows_vec(a.b, dtype, a.O > 1 ? a.b_row : 0) && (a.n == 1 || a.b_group % 8 == 0) && a.r % 8 == 0;
+    if (dtype == STMOE_BF16) return out_dtype == STMOE_F32 ? launch_up_as<1, 0, 3>(a, vec, dev, sms, st) : launch_up_as<1, 1, 2>(a, vec, dev, sms, st);
+    return out_dtype == STMOE_F32 ? launch_up_as<4, 0, 3>(a, vec, dev, sms, st) : launch_up_as<4, 4, 2>(a, vec, dev, sms, st);
 }
 int launch_transpose(const void *b, int64_t group, int64_t row, int rows, int cols, int n, uint16_t *t, int64_t t_row, cudaStream_t st)
 {
@@ -70,12 +110,8 @@ int launch_transpose(const void *b, int64_t group, int64_t row, int rows, int co
 template <int DT> int launch_grad(const LoraGradArgs &a, int dev, cudaStream_t st)
 {
     constexpr int smem = (int)sizeof(float) * kLoraRankBlock * (kGradCols + 1);
-    static PerDevice<bool> asked;       // more than 48 KB of shared memory: asked for once per device
-    bool done = false;
-    if (const int rc = asked.get(dev, &done, [](bool &) {
-            return cuda_status(cudaFuncSetAttribute(lora_grad_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        }))
-        return rc;
+    static PerDevice<bool> asked;
+    if (const int rc = smem_of(asked, dev, lora_grad_kernel<DT>, smem)) return rc;
     const dim3 grid(a.n + a.T / a.task_rows, (a.C + kGradCols - 1) / kGradCols, (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
     if (const int rc = launch_behind(lora_grad_kernel<DT>, grid, kLoraThreads, smem, 1, st, a)) return rc;
     if (a.T <= a.task_rows) return STMOE_OK;    // no adapter has several tasks
@@ -93,14 +129,15 @@ size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int in
 }
 
 int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,
-               int64_t b_row, int n_adapters, int rank, int inner, int outer, const int32_t *ids, const int32_t *order, const float *scale,
-               float alpha, const void *base, int64_t base_stride, void *out, int out_dtype, int64_t out_stride, float *hidden, void *scratch,
+               int64_t b_row, int n_adapters, int rank, int inner, int outer, const int32_t *ids, const int32_t *order,
+               const int32_t *counts, const int32_t *starts, const float *scale, float alpha, const void *base, int64_t base_stride, void *out, int out_dtype, int64_t out_stride, float *hidden, void *scratch,
                size_t scratch_bytes, void *cuda_stream)
 {
     if (!half_ok(dtype) || (out_dtype != dtype && out_dtype != STMOE_F32) || !sizes_ok(tokens, n_adapters, rank, inner, outer) ||
         !rows_ok(x, dtype, x_stride, tokens, inner) || !rows_ok(a, dtype, a_row, rank, inner) || !rows_ok(b, dtype, b_row, outer, rank) ||
         (n_adapters > 1 && (a_group < 0 || b_group < 0)) || !rows_ok(out, out_dtype, out_stride, tokens, outer) ||
-        (base && !rows_ok(base, out_dtype, base_stride, tokens, outer)) || !ids || !order || !aligned(ids, order) || !aligned(scale, (const float *)hidden))
+        (base && !rows_ok(base, out_dtype, base_stride, tokens, outer)) || !ids || !order || !counts || !starts ||
+        !aligned(ids, order, counts, starts) || !aligned(scale, (const float *)hidden))
         return STMOE_ERR_BAD_ARG;
     if (tokens == 0) return STMOE_OK;
     if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < stmoe_lora_scratch_bytes(tokens, n_adapters, rank, inner, outer)) return STMOE_ERR_BAD_ARG;
@@ -113,13 +150,11 @@ int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const
     LoraArgs k{};
     k.x = x, k.x_stride = x_stride, k.a = a, k.b = b, k.a_group = a_group, k.a_row = a_row, k.b_group = b_group, k.b_row = b_row;
     k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.I = inner, k.O = outer;
-    k.splits = down_splits(tokens, inner), k.rp = (int)up_to(rank, 8), k.part = (float *)scratch;
-    k.steps = ((inner + kLoraStep - 1) / kLoraStep + k.splits - 1) / k.splits;
-    k.splits = ((inner + kLoraStep - 1) / kLoraStep + k.steps - 1) / k.steps;
+    k.counts = counts, k.starts = starts, k.polls = g_mx4_polls.load(std::memory_order_relaxed), k.rp = (int)up_to(rank, 8), k.part = (float *)scratch;
     k.base = base, k.base_stride = base_stride, k.out = out, k.out_stride = out_stride, k.keep = same, k.hidden = hidden;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (const int rc = launch_down(k, dtype, st)) return rc;
-    return launch_up(k, dtype, out_dtype, st);
+    if (const int rc = launch_down(k, dtype, dev, st)) return rc;
+    return launch_up(k, dtype, out_dtype, dev, sms, st);
 }
 
 size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer)
@@ -162,12 +197,10 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
         LoraArgs k{};
         k.x = grad, k.x_stride = grad_stride, k.a = bt, k.a_row = outer8, k.a_group = rank * outer8, k.b = a_t, k.b_row = rank8, k.b_group = inner * rank8;
         k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.I = outer, k.O = inner;
-        k.splits = down_splits(tokens, outer), k.rp = (int)up_to(rank, 8), k.part = part;
-        k.steps = ((outer + kLoraStep - 1) / kLoraStep + k.splits - 1) / k.splits;
-        k.splits = ((outer + kLoraStep - 1) / kLoraStep + k.steps - 1) / k.steps;
+        k.counts = counts, k.starts = starts, k.polls = g_mx4_polls.load(std::memory_order_relaxed), k.rp = (int)up_to(rank, 8), k.part = part;
         k.out = grad_x, k.out_stride = grad_x_stride, k.hidden = u;
-        if (const int rc = launch_down(k, dtype, st)) return rc;
-        if (const int rc = launch_up(k, dtype, dtype, st)) return rc;
+        if (const int rc = launch_down(k, dtype, dev, st)) return rc;
+        if (const int rc = launch_up(k, dtype, dtype, dev, sms, st)) return rc;
     }
     LoraGradArgs g{};
     g.order = order, g.counts = counts, g.starts = starts, g.scale = scale, g.alpha = alpha, g.T = (int)tokens, g.n = n_adapters, g.r = rank;

@@ -48,6 +48,7 @@ struct LoraArgs {
     bool out_vec;           // rows of base and out are 16-byte aligned
     bool keep;              // out is base: rows without an adapter are there already
     float *hidden;          // [T][r] or nullptr: h by row
+    int polls;              // limit of every wait of the tile kernels
 };
 
 // D += A B for one 16 x 8 x 16 step (A 16 x 16 by rows, B 16 x 8 by columns); F32 accumulators.

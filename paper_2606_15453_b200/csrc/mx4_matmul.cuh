@@ -70,9 +70,6 @@ __host__ __device__ constexpr int mm_stages(int bn)
 // it is never two phases ahead of a barrier, whose parity would then deceive it
 static_assert(mm_stages(16) >= 4 && mm_stages(128) >= 4 && mm_stages(kMmMaxTokens) >= 4, "");
 
-// Polls after which a wait gives up, for the launches to come (tests lower it).
-inline std::atomic<int> g_mx4_polls{kDenseSpinLimit};
-
 struct Mx4MatmulArgs {
     const uint8_t *a_scales, *b_scales;
     long long a_scale_stride, b_scale_stride;  // bytes

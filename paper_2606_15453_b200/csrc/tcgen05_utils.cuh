@@ -3,11 +3,15 @@
 #pragma once
 #include <cuda.h>
 
+#include <atomic>
+
 #include "device_utils.cuh"
 
 namespace stmoe_dev {
 
 constexpr int kDenseSpinLimit = 1 << 22;
+// Polls after which a wait of the operators' kernels gives up, for the launches to come (tests lower it).
+inline std::atomic<int> g_mx4_polls{kDenseSpinLimit};
 
 __device__ __forceinline__ uint32_t dsmem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 

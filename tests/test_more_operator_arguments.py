@@ -103,13 +103,13 @@ def test_combine_rows_backward_refusals(kw):
 
 
 def _lora(**kw):
-    a = dict(x=X, dt=1, xs=64, T=4, a=X, ag=1024, ar=64, b=X, bg=1024, br=16, n=2, r=16, I=64, O=64, ids=X, order=X, scale=None, alpha=1.0, base=None, bs=64,
+    a = dict(x=X, dt=1, xs=64, T=4, a=X, ag=1024, ar=64, b=X, bg=1024, br=16, n=2, r=16, I=64, O=64, ids=X, order=X, counts=X, starts=X, scale=None, alpha=1.0, base=None, bs=64,
              out=Y, odt=1, os=64, hidden=None, scratch=X, size=1 << 20)
     a.update(kw)
     return P.lib().stmoe_lora(*a.values(), None)
 
 
-@pytest.mark.parametrize("kw", [dict(x=None), dict(a=None), dict(b=None), dict(ids=None), dict(order=None), dict(out=None), dict(scratch=None), dict(size=64),
+@pytest.mark.parametrize("kw", [dict(x=None), dict(a=None), dict(b=None), dict(ids=None), dict(order=None), dict(counts=None), dict(starts=None), dict(out=None), dict(scratch=None), dict(size=64),
                                 dict(dt=0), dict(dt=2), dict(odt=4), dict(xs=63), dict(ar=63), dict(br=15), dict(os=63), dict(base=Z, bs=63), dict(T=-1), dict(n=0),
                                 dict(n=1025), dict(r=0), dict(r=257, br=300), dict(I=0), dict(O=0), dict(I=1 << 25, xs=1 << 25, ar=1 << 25), dict(ag=-1), dict(out=X),
                                 dict(base=C.c_void_p((1 << 24) + 128)), dict(x=ODD), dict(a=ODD), dict(b=ODD), dict(ids=TWO), dict(order=TWO), dict(scale=TWO),
