@@ -76,14 +76,19 @@ int launch_down(LoraArgs &a, int dtype, int dev, cudaStream_t st)
     const bool wvec = rows_vec(a.a, dtype, a.r > 1 ? a.a_row : 0) && (a.n == 1 || a.a_group % 8 == 0) && a.I % 8 == 0;
     return dtype == STMOE_BF16 ? launch_down_as<1>(a, xvec, wvec, dev, st) : launch_down_as<4>(a, xvec, wvec, dev, st);
 }
-template <int DT, int DO, int PL, bool WVEC> int launch_up_tiles(const LoraArgs &a, int dev, int sms, cudaStream_t st)
+template <int DT, int DO, int PL, bool WVEC, bool OVEC> int launch_up_tiles(const LoraArgs &a, int dev, int sms, cudaStream_t st)
 {
     static PerDevice<bool> asked;
-    if (const int rc = smem_of(asked, dev, lora_up_tile_kernel<DT, DO, PL, WVEC>, up_smem(kTileMaxRank, PL))) return rc;
-    const int smem = up_smem(a.r, PL), sm = smem <= 110 * 1024 ? 2 : 1;
-    const int64_t units = std::min<int64_t>(a.T, a.T / kTileRows + a.n + 1) * ((a.O + kUpCols - 1) / kUpCols);
+    constexpr auto kernel = lora_up_tile_kernel<DT, DO, PL, WVEC, OVEC>;
+    if (const int rc = smem_of(asked, dev, kernel, std::max(up_smem<DO, PL>(64), up_smem<DO, PL>(kTileMaxRank)))) return rc;
+    const int64_t units = std::min<int64_t>(a.T, a.T / kTileRows + a.n + 1) * ((a.O + up_cols<DO>() - 1) / up_cols<DO>());
     if (units > INT32_MAX) return STMOE_ERR_TOO_LARGE;
-    return launch_behind(lora_up_tile_kernel<DT, DO, PL, WVEC>, (int)std::min<int64_t>(units, sms * sm), kUpTileThreads, smem, 1, st, a);
+    return launch_behind(kernel, (int)std::min<int64_t>(units, sms), kUpTileThreads, up_smem<DO, PL>(a.r), 1, st, a);
+}
+template <int DT, int DO, int PL, bool WVEC> int launch_up_tiles(const LoraArgs &a, int dev, int sms, cudaStream_t st)
+{
+    const bool ovec = a.out_vec && a.O % Elem<DO>::kVec == 0;
+    return ovec ? launch_up_tiles<DT, DO, PL, WVEC, true>(a, dev, sms, st) : launch_up_tiles<DT, DO, PL, WVEC, false>(a, dev, sms, st);
 }
 template <int DT, int DO, int PL> int launch_up_as(const LoraArgs &a, bool vec, int dev, int sms, cudaStream_t st)
 {
