@@ -105,20 +105,10 @@ int launch_up(LoraArgs &a, int dtype, int out_dtype, int dev, int sms, cudaStrea
     if (dtype == STMOE_BF16) return out_dtype == STMOE_F32 ? launch_up_as<1, 0, 3>(a, vec, dev, sms, st) : launch_up_as<1, 1, 2>(a, vec, dev, sms, st);
     return out_dtype == STMOE_F32 ? launch_up_as<4, 0, 3>(a, vec, dev, sms, st) : launch_up_as<4, 4, 2>(a, vec, dev, sms, st);
 }
-int launch_transpose(const void *b, int64_t group, int64_t row, int rows, int cols, int n, uint16_t *t, int64_t t_row, cudaStream_t st)
+template <int DT> int launch_grad(const LoraGradArgs &a, cudaStream_t st)
 {
-    LoraTransposeArgs a{};
-    a.b = (const uint16_t *)b, a.b_group = group, a.b_row = row, a.rows = rows, a.cols = cols;
-    a.t = t, a.t_row = t_row, a.t_group = t_row * cols;
-    return launch_behind(lora_transpose_kernel, dim3((rows + 31) / 32, (cols + 31) / 32, n), kLoraThreads, 0, 1, st, a);
-}
-template <int DT> int launch_grad(const LoraGradArgs &a, int dev, cudaStream_t st)
-{
-    constexpr int smem = (int)sizeof(float) * kLoraRankBlock * (kGradCols + 1);
-    static PerDevice<bool> asked;
-    if (const int rc = smem_of(asked, dev, lora_grad_kernel<DT>, smem)) return rc;
     const dim3 grid(a.n + a.T / a.task_rows, (a.C + kGradCols - 1) / kGradCols, (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
-    if (const int rc = launch_behind(lora_grad_kernel<DT>, grid, kLoraThreads, smem, 1, st, a)) return rc;
+    if (const int rc = launch_behind(lora_grad_kernel<DT>, grid, kLoraThreads, kGradSmem, 1, st, a)) return rc;
     if (a.T <= a.task_rows) return STMOE_OK;    // no adapter has several tasks
     const int64_t size = (int64_t)a.r * a.C;
     return launch_behind(lora_grad_sum_kernel<DT>, dim3(a.n, (unsigned)std::min<int64_t>(256, (size + kLoraThreads - 1) / kLoraThreads)), kLoraThreads, 0, 1, st, a);
@@ -196,8 +186,9 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
     float *const part = (float *)take(part_bytes(tokens, rank, outer)), *const u = (float *)take((int64_t)sizeof(float) * tokens * rank);
     float *const parts = (float *)at;
     if (tokens) {
-        if (const int rc = launch_transpose(b, b_group, b_row, outer, rank, n_adapters, bt, outer8, st)) return rc;
-        if (const int rc = launch_transpose(a, a_group, a_row, rank, inner, n_adapters, a_t, rank8, st)) return rc;
+        LoraTransposeArgs t{{(const uint16_t *)b, (const uint16_t *)a}, {bt, a_t}, {b_group, a_group}, {b_row, a_row}, {outer8, rank8}, {outer, rank}, {rank, inner}, {}};
+        for (int w = 0; w < 2; ++w) t.tiles[w] = ((t.rows[w] + 31) / 32) * ((t.cols[w] + 31) / 32);
+        if (const int rc = launch_behind(lora_transpose_kernel, dim3(t.tiles[0] + t.tiles[1], n_adapters), kLoraThreads, 0, 1, st, t)) return rc;
         // the forward kernels with the roles of A and B exchanged
         LoraArgs k{};
         k.x = grad, k.x_stride = grad_stride, k.a = bt, k.a_row = outer8, k.a_group = rank * outer8, k.b = a_t, k.b_row = rank8, k.b_group = inner * rank8;
@@ -209,16 +200,16 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
     }
     LoraGradArgs g{};
     g.order = order, g.counts = counts, g.starts = starts, g.scale = scale, g.alpha = alpha, g.T = (int)tokens, g.n = n_adapters, g.r = rank;
-    g.task_rows = grad_task_rows(tokens), g.parts = grad_parts(tokens), g.part = parts;
+    g.u_vec = rank % 4 == 0, g.task_rows = grad_task_rows(tokens), g.parts = grad_parts(tokens), g.part = parts;
     if (grad_a) {
         g.u = u, g.z = x, g.z_stride = x_stride, g.C = inner, g.by_col = false, g.grad = grad_a;
         g.vec = rows_vec(x, dtype, tokens > 1 ? x_stride : 0);
-        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, dev, st) : launch_grad<4>(g, dev, st)) return rc;
+        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, st) : launch_grad<4>(g, st)) return rc;
     }
     if (grad_b) {
-        g.u = hidden, g.z = grad, g.z_stride = grad_stride, g.C = outer, g.by_col = true, g.grad = grad_b;
+        g.u = hidden, g.u_vec = g.u_vec && ((uintptr_t)hidden & 15) == 0, g.z = grad, g.z_stride = grad_stride, g.C = outer, g.by_col = true, g.grad = grad_b;
         g.vec = rows_vec(grad, dtype, tokens > 1 ? grad_stride : 0);
-        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, dev, st) : launch_grad<4>(g, dev, st)) return rc;
+        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, st) : launch_grad<4>(g, st)) return rc;
     }
     return STMOE_OK;
 }

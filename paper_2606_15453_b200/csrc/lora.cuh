@@ -272,30 +272,34 @@ template <int DT, int DO, int PL, bool VEC> __global__ void __launch_bounds__(kL
 
 // ---- gradients of A and B ------------------------------------------------------------------------
 
-// b [n][rows][cols] -> t [n][cols][ld]
+// m [n][rows][cols] -> t [n][cols][ld], two such in one launch
 struct LoraTransposeArgs {
-    const uint16_t *b;
-    uint16_t *t;
-    long long b_group, b_row, t_group, t_row;
-    int rows, cols;
+    const uint16_t *m[2];
+    uint16_t *t[2];
+    long long m_group[2], m_row[2], t_row[2];
+    int rows[2], cols[2], tiles[2];     // tiles of 32 x 32 in one of the n matrices
 };
 __global__ void __launch_bounds__(kLoraThreads) lora_transpose_kernel(const LoraTransposeArgs a)
 {
     __shared__ uint16_t s[32][33];
     pdl_wait();
     pdl_launch_dependents();
-    const int r0 = blockIdx.x * 32, c0 = blockIdx.y * 32, x = threadIdx.x % 32, y = threadIdx.x / 32;
-    const uint16_t *const b = a.b + blockIdx.z * a.b_group;
-    uint16_t *const t = a.t + blockIdx.z * a.t_group;
+    const int w = (int)blockIdx.x >= a.tiles[0], tile = blockIdx.x - (w ? a.tiles[0] : 0), across = (a.cols[w] + 31) / 32;
+    const int r0 = tile / across * 32, c0 = tile % across * 32, x = threadIdx.x % 32, y = threadIdx.x / 32;
+    const uint16_t *const m = a.m[w] + blockIdx.y * a.m_group[w];
+    uint16_t *const t = a.t[w] + blockIdx.y * a.t_row[w] * a.cols[w];
+#pragma unroll
     for (int i = y; i < 32; i += kLoraWarps)
-        if (r0 + i < a.rows && c0 + x < a.cols) s[i][x] = b[(r0 + i) * a.b_row + c0 + x];
+        if (r0 + i < a.rows[w] && c0 + x < a.cols[w]) s[i][x] = m[(r0 + i) * a.m_row[w] + c0 + x];
     __syncthreads();
+#pragma unroll
     for (int i = y; i < 32; i += kLoraWarps)
-        if (c0 + i < a.cols && r0 + x < a.rows) t[(c0 + i) * a.t_row + r0 + x] = s[x][i];
+        if (c0 + i < a.cols[w] && r0 + x < a.rows[w]) t[(c0 + i) * a.t_row[w] + r0 + x] = s[x][i];
 }
 
 constexpr int kGradCols = 128;      // columns of a CTA: 16 a warp
 constexpr int kGradPos = 32;        // positions of a step
+constexpr int kGradSmem = 47 * 1024;
 
 struct LoraGradArgs {
     const float *u;         // [T][r] by row
@@ -307,6 +311,7 @@ struct LoraGradArgs {
     int T, n, r, C;
     int task_rows;          // positions of a task, a multiple of kGradPos
     bool vec;               // rows of z are 16-byte aligned
+    bool u_vec;             // rows of u are
     bool by_col;            // grad [n][C][r], else [n][r][C]
     void *grad;
     float *part;            // [parts][r * C], laid out as grad: tasks of adapters that have several
@@ -358,15 +363,22 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t (&r)[4])
 }
 
 // One task's sum over its positions of z[p][c] u[p][r] for 128 columns and up to 64 ranks.  Columns are the MMA's rows, positions its inner
-// dimension: z lies in shared memory as in memory and is read transposed, u as planes by rank.
-template <int DT> __global__ void __launch_bounds__(kLoraThreads) lora_grad_kernel(const LoraGradArgs a)
+// dimension: z lies in shared memory as in memory and is read transposed, u as planes by rank.  A step of 32 positions costs one barrier: behind
+// barrier i the MMAs of step i run while z is fetched for step i + 2, u is turned into planes for step i + 1 and asked for for
+// step i + 2, whose largest magnitude (fp16 planes) the next barrier publishes, and the rows of step i + 3 are looked up.
+template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_kernel(const LoraGradArgs a)
 {
     using T = typename Elem<DT>::T;
-    constexpr int PL = 2, kTiles = kLoraRankBlock / 8, kZ = kGradCols + 8, kU = kGradPos + 8;
-    __shared__ __align__(16) T s_z[2][kGradPos][kZ];
-    __shared__ __align__(16) uint16_t s_u[PL][kLoraRankBlock][kU];
-    __shared__ float s_most[kLoraWarps];
-    extern __shared__ float s_out[];    // [64][kGradCols + 1]
+    constexpr int PL = 2, kTiles = kLoraRankBlock / 8, kZ = kGradCols + 8, kU = kGradPos + 8, kRing = 3;
+    struct Steps {
+        T z[kRing][kGradPos][kZ];
+        uint16_t u[2][PL][kLoraRankBlock][kU];
+    };
+    extern __shared__ __align__(16) uint8_t smem[];
+    Steps &s = *reinterpret_cast<Steps *>(smem);
+    float *const s_out = reinterpret_cast<float *>(smem);       // [64][kGradCols + 1], behind the last step
+    static_assert(sizeof(Steps) <= kGradSmem && kLoraRankBlock * (kGradCols + 1) * 4 <= kGradSmem, "");
+    __shared__ float s_most[2][kLoraWarps];
     const int tid = threadIdx.x, lane = tid % kWarp, warp = tid / kWarp, q = lane % 4, o = lane / 4;
     pdl_wait();
     pdl_launch_dependents();
@@ -375,81 +387,112 @@ template <int DT> __global__ void __launch_bounds__(kLoraThreads) lora_grad_kern
     if (task.tasks > 1 && task.several + task.index >= a.parts) return;   // counts of more rows than there are
     const int c0 = blockIdx.y * kGradCols, r0 = blockIdx.z * kLoraRankBlock, here = min(kGradCols, a.C - c0), ranks = min(kLoraRankBlock, a.r - r0);
     const int begin = a.starts[task.g] + task.index * a.task_rows;
-    const int count = max(0, min(a.task_rows, a.counts[task.g] - task.index * a.task_rows));
+    const int count = max(0, min(a.task_rows, a.counts[task.g] - task.index * a.task_rows)), steps = (count + kGradPos - 1) / kGradPos;
     const T *const z = reinterpret_cast<const T *>(a.z);
     auto row_at = [&](int i) {           // row of the task's position i, -1 behind its last
         const int row = i < count && (unsigned)(begin + i) < (unsigned)a.T ? a.order[begin + i] : -1;
         return (unsigned)row < (unsigned)a.T ? row : -1;
     };
-    auto fetch = [&](int buf, int i0) {  // 32 positions x 128 columns, zeros where there is nothing
-        for (int i = tid; i < kGradPos * kGradCols / 8; i += kLoraThreads) {
-            const int pos = i / (kGradCols / 8), c = i % (kGradCols / 8) * 8, row = row_at(i0 + pos);
-            T *const dst = &s_z[buf][pos][c];
-            if (a.vec && row >= 0 && c + 8 <= here) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dsmem_u32(dst)), "l"(z + row * a.z_stride + c0 + c) : "memory");
+    // z: sixteen lanes a row, rows tid / 16 and 16 further; u: eight ranks of position lane
+    const int zp = tid / 16, zc = tid % 16 * 8, ur = warp * 8;
+    struct Rows {
+        int z[2], u;
+    };
+    auto rows_of = [&](int i) { return Rows{{row_at(i * kGradPos + zp), row_at(i * kGradPos + zp + 16)}, row_at(i * kGradPos + lane)}; };
+    auto fetch = [&](int i, const Rows &rows) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            T *const dst = &s.z[i % kRing][zp + 16 * j][zc];
+            const T *const src = z + (rows.z[j] >= 0 ? rows.z[j] : 0) * a.z_stride + c0 + zc;
+            if (a.vec && zc + 8 <= here) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dsmem_u32(dst)), "l"(src), "r"(rows.z[j] >= 0 ? 16 : 0) : "memory");
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dst[j] = row >= 0 && c + j < here ? z[row * a.z_stride + c0 + c + j] : Elem<DT>::from_f32(0.f);
+                for (int e = 0; e < 8; ++e) dst[e] = rows.z[j] >= 0 && zc + e < here ? src[e] : Elem<DT>::from_f32(0.f);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    float sum[kTiles][4] = {};
-    fetch(0, 0);
-    for (int i0 = 0, buf = 0; i0 < count; i0 += kGradPos, buf ^= 1) {
-        // u of this step: a thread has eight ranks of one position
-        float u[8], most = 0.f;
-        const int pos = tid % kGradPos, ur = tid / kGradPos * 8, row = row_at(i0 + pos);
+    auto load_u = [&](const Rows &rows, float (&u)[8]) {
+        const float *const p = a.u + (long long)(rows.u >= 0 ? rows.u : 0) * a.r + r0 + ur;
+        if (a.u_vec && ur + 8 <= ranks) {
+            const float4 x = rows.u >= 0 ? ld_f4(p) : float4{}, y = rows.u >= 0 ? ld_f4(p + 4) : float4{};
+            u[0] = x.x, u[1] = x.y, u[2] = x.z, u[3] = x.w, u[4] = y.x, u[5] = y.y, u[6] = y.z, u[7] = y.w;
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            u[j] = row >= 0 && ur + j < ranks ? a.u[(long long)row * a.r + r0 + ur + j] : 0.f;
-            most = fmaxf(most, fabsf(u[j]));
+            for (int j = 0; j < 8; ++j) u[j] = rows.u >= 0 && ur + j < ranks ? p[j] : 0.f;
         }
-        float up = 1.f;
-        if (DT != 1) {                  // one power of two for the whole step
-            most = warp_max(most);
-            if (lane == 0) s_most[warp] = most;
-            __syncthreads();
-            most = 0.f;
+    };
+    auto publish = [&](int i, const float (&u)[8]) {
+        if (DT == 1) return;
+        float most = 0.f;
 #pragma unroll
-            for (int w = 0; w < kLoraWarps; ++w) most = fmaxf(most, s_most[w]);
-            up = plane_scale<DT>(most);
-        }
-        fetch(buf ^ 1, i0 + kGradPos);
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(u[j]));
+        most = warp_max(most);
+        if (lane == 0) s_most[i & 1][warp] = most;
+    };
+    auto scale_of = [&](int i) {         // one power of two for the whole step
+        if (DT == 1) return 1.f;
+        float most = 0.f;
+#pragma unroll
+        for (int w = 0; w < kLoraWarps; ++w) most = fmaxf(most, s_most[i & 1][w]);
+        return plane_scale<DT>(most);
+    };
+    auto put_planes = [&](int i, float up, const float (&u)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             uint16_t pl[PL];
             planes_of<DT, PL>(u[j] * up, pl);
 #pragma unroll
-            for (int i = 0; i < PL; ++i) s_u[i][ur + j][pos] = pl[i];
+            for (int p = 0; p < PL; ++p) s.u[i & 1][p][ur + j][lane] = pl[p];
         }
+    };
+    float sum[kTiles][4] = {}, u[8];
+    Rows rows = rows_of(0), next = rows_of(1), after = rows_of(2);
+    fetch(0, rows);
+    fetch(1, next);
+    load_u(rows, u);
+    publish(0, u);
+    __syncthreads();
+    float up = scale_of(0), up_next;
+    put_planes(0, up, u);
+    load_u(next, u);
+    publish(1, u);
+    for (int i = 0; i < steps; ++i) {
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncthreads();
+        fetch(i + 2, after);
+        up_next = scale_of(i + 1);
+        put_planes(i + 1, up_next, u);
+        load_u(after, u);
+        after = rows_of(i + 3);
         float d[kTiles][4] = {};
 #pragma unroll
         for (int k = 0; k < kGradPos; k += 16) {
             uint32_t za[4];
-            ldmatrix4t(dsmem_u32(&s_z[buf][k + (lane & 7) + (lane & 16) / 2][warp * 16 + (lane & 8)]), za);
+            ldmatrix4t(dsmem_u32(&s.z[i % kRing][k + (lane & 7) + (lane & 16) / 2][warp * 16 + (lane & 8)]), za);
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-                if (i * 8 < ranks) {
+            for (int j = 0; j < kTiles; ++j)
+                if (j * 8 < ranks) {
 #pragma unroll
-                    for (int j = 0; j < PL; ++j) {
-                        const uint16_t *const col = &s_u[j][i * 8 + o][k + 2 * q];
-                        mma16<DT>(DT == 1 ? sum[i] : d[i], za[0], za[1], za[2], za[3], *reinterpret_cast<const uint32_t *>(col), *reinterpret_cast<const uint32_t *>(col + 8));
+                    for (int p = 0; p < PL; ++p) {
+                        const uint16_t *const col = &s.u[i & 1][p][j * 8 + o][k + 2 * q];
+                        mma16<DT>(DT == 1 ? sum[j] : d[j], za[0], za[1], za[2], za[3], *reinterpret_cast<const uint32_t *>(col), *reinterpret_cast<const uint32_t *>(col + 8));
                     }
                 }
         }
         if (DT != 1) {
             const float down = 1.f / up;
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i)
+            for (int j = 0; j < kTiles; ++j)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum[i][j] = fmaf(d[i][j], down, sum[i][j]);
+                for (int e = 0; e < 4; ++e) sum[j][e] = fmaf(d[j][e], down, sum[j][e]);
         }
-        __syncthreads();
+        up = up_next;
+        publish(i + 2, u);
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
     const float c = a.alpha * (a.scale ? a.scale[task.g] : 1.f);
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
