@@ -33,14 +33,17 @@ bool by_tiles(int64_t tokens, int rank) { return tokens >= 256 && rank <= kTileM
 int down_splits(int64_t tokens, int rank, int inner)
 {
     if (by_tiles(tokens, rank)) {
-        const int64_t most = std::min<int64_t>(8, (inner + 255) / 256);
+        const int64_t most = std::min<int64_t>(kDownMaxSplits, (inner + 255) / 256);
         return (int)std::max<int64_t>(1, std::min<int64_t>(most, 296 / ((tokens + kTileRows - 1) / kTileRows)));
     }
     const int64_t steps = (inner + kLoraStep - 1) / kLoraStep;
     const int64_t most = std::min<int64_t>(16, (steps + 2 * kLoraWarps - 1) / (2 * kLoraWarps));
     return (int)std::max<int64_t>(1, std::min<int64_t>(most, 592 / std::max<int64_t>(1, tokens)));
 }
-int64_t part_bytes(int64_t tokens, int rank, int inner) { return up_to((int64_t)sizeof(float) * down_splits(tokens, rank, inner) * tokens * up_to(rank, 8), 256); }
+int64_t part_bytes(int64_t tokens, int rank, int inner)
+{
+    return up_to((int64_t)sizeof(float) * (by_tiles(tokens, rank) ? 1 : down_splits(tokens, rank, inner)) * tokens * up_to(rank, 8), 256);
+}
 int grad_task_rows(int64_t tokens) { return (int)std::max<int64_t>(512, up_to((tokens + 15) / 16, kGradPos)); }
 int grad_parts(int64_t tokens) { return (int)(2 * tokens / grad_task_rows(tokens)); }
 
@@ -55,7 +58,9 @@ template <int DT, bool XVEC, bool WVEC> int launch_down_tiles(const LoraArgs &a,
     static PerDevice<bool> asked;
     if (const int rc = smem_of(asked, dev, lora_down_tile_kernel<DT, XVEC, WVEC>, 97 * 1024)) return rc;
     const int tiles = (int)std::min<int64_t>(a.T, a.T / kTileRows + a.n);
-    return launch_behind(lora_down_tile_kernel<DT, XVEC, WVEC>, dim3(tiles, a.splits), kDownTileThreads, 1024 + down_stages(a.r) * down_stage_bytes(a.r), 1, st, a);
+    if ((int64_t)tiles * a.splits > INT32_MAX) return STMOE_ERR_TOO_LARGE;
+    // the parts of a tile are a cluster, which adds them up: one part is left in memory
+    return launch_behind(lora_down_tile_kernel<DT, XVEC, WVEC>, tiles * a.splits, kDownTileThreads, 1024 + down_stages(a.r) * down_stage_bytes(a.r), a.splits, st, a);
 }
 template <int DT> int launch_down_as(const LoraArgs &a, bool xvec, bool wvec, int dev, cudaStream_t st)
 {
@@ -105,8 +110,10 @@ int launch_up(LoraArgs &a, int dtype, int out_dtype, int dev, int sms, cudaStrea
     if (dtype == STMOE_BF16) return out_dtype == STMOE_F32 ? launch_up_as<1, 0, 3>(a, vec, dev, sms, st) : launch_up_as<1, 1, 2>(a, vec, dev, sms, st);
     return out_dtype == STMOE_F32 ? launch_up_as<4, 0, 3>(a, vec, dev, sms, st) : launch_up_as<4, 4, 2>(a, vec, dev, sms, st);
 }
-template <int DT> int launch_grad(const LoraGradArgs &a, cudaStream_t st)
+template <int DT> int launch_grad(const LoraGradArgs &a, int dev, cudaStream_t st)
 {
+    static PerDevice<bool> asked;
+    if (const int rc = smem_of(asked, dev, lora_grad_kernel<DT>, kGradSmem)) return rc;
     const dim3 grid(a.n + a.T / a.task_rows, (a.C + kGradCols - 1) / kGradCols, (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
     if (const int rc = launch_behind(lora_grad_kernel<DT>, grid, kLoraThreads, kGradSmem, 1, st, a)) return rc;
     if (a.T <= a.task_rows) return STMOE_OK;    // no adapter has several tasks
@@ -204,12 +211,12 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
     if (grad_a) {
         g.u = u, g.z = x, g.z_stride = x_stride, g.C = inner, g.by_col = false, g.grad = grad_a;
         g.vec = rows_vec(x, dtype, tokens > 1 ? x_stride : 0);
-        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, st) : launch_grad<4>(g, st)) return rc;
+        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, dev, st) : launch_grad<4>(g, dev, st)) return rc;
     }
     if (grad_b) {
         g.u = hidden, g.u_vec = g.u_vec && ((uintptr_t)hidden & 15) == 0, g.z = grad, g.z_stride = grad_stride, g.C = outer, g.by_col = true, g.grad = grad_b;
         g.vec = rows_vec(grad, dtype, tokens > 1 ? grad_stride : 0);
-        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, st) : launch_grad<4>(g, st)) return rc;
+        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, dev, st) : launch_grad<4>(g, dev, st)) return rc;
     }
     return STMOE_OK;
 }

@@ -40,7 +40,7 @@ struct LoraArgs {
     int splits;             // of I
     int steps;              // steps of a split
     int rp;                 // ranks of a row of part: r rounded up to 8
-    float *part;            // [splits][T][rp], by position
+    float *part;            // [splits][T][rp], by position (tile kernels: [T][rp], the parts added up)
     const void *base;       // [T][O] or nullptr
     long long base_stride;
     void *out;              // [T][O]
@@ -207,8 +207,11 @@ template <int DT, int DO, int PL, bool VEC> __global__ void __launch_bounds__(kL
         for (int i = 0; i < kLoraMaxRank / kWarp; ++i) {
             const int r = i * kWarp + lane;
             h[i] = 0.f;
-            if (warp < count && r < a.r)
-                for (int s = 0; s < a.splits; ++s) h[i] += a.part[((long long)s * a.T + p + warp) * a.rp + r];
+            if (warp < count && r < a.r) {
+                const float *const part = a.part + (long long)(p + warp) * a.rp + r;
+#pragma unroll 8
+                for (int s = 0; s < a.splits; ++s) h[i] += part[(long long)s * a.T * a.rp];
+            }
             most = fmaxf(most, fabsf(h[i]));
         }
         most = warp_max(most);
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(kLoraThreads) lora_transpose_kernel(const Lora
 
 constexpr int kGradCols = 128;      // columns of a CTA: 16 a warp
 constexpr int kGradPos = 32;        // positions of a step
-constexpr int kGradSmem = 47 * 1024;
+constexpr int kGradRing = 5, kGradSmem = 104 * 1024;
 
 struct LoraGradArgs {
     const float *u;         // [T][r] by row
@@ -364,14 +367,15 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t (&r)[4])
 
 // One task's sum over its positions of z[p][c] u[p][r] for 128 columns and up to 64 ranks.  Columns are the MMA's rows, positions its inner
 // dimension: z lies in shared memory as in memory and is read transposed, u as planes by rank.  A step of 32 positions costs one barrier: behind
-// barrier i the MMAs of step i run while z is fetched for step i + 2, u is turned into planes for step i + 1 and asked for for
-// step i + 2, whose largest magnitude (fp16 planes) the next barrier publishes, and the rows of step i + 3 are looked up.
+// barrier i the MMAs of step i run while z and u are on their way for steps up to i + 4, u is turned into planes for step i + 1, and the
+// largest magnitude of step i + 2 is found (fp16 planes), which the next barrier publishes.  A thread copies the u that it reads itself.
 template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_kernel(const LoraGradArgs a)
 {
     using T = typename Elem<DT>::T;
-    constexpr int PL = 2, kTiles = kLoraRankBlock / 8, kZ = kGradCols + 8, kU = kGradPos + 8, kRing = 3;
+    constexpr int PL = 2, kTiles = kLoraRankBlock / 8, kZ = kGradCols + 8, kU = kGradPos + 8, kRing = kGradRing;
     struct Steps {
         T z[kRing][kGradPos][kZ];
+        float4 own[kRing][2][kLoraThreads];     // u: eight ranks of a position, a thread's own
         uint16_t u[2][PL][kLoraRankBlock][kU];
     };
     extern __shared__ __align__(16) uint8_t smem[];
@@ -411,17 +415,23 @@ template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_k
                 for (int e = 0; e < 8; ++e) dst[e] = rows.z[j] >= 0 && zc + e < here ? src[e] : Elem<DT>::from_f32(0.f);
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    auto load_u = [&](const Rows &rows, float (&u)[8]) {
+        float4 *const own = &s.own[i % kRing][0][tid];
         const float *const p = a.u + (long long)(rows.u >= 0 ? rows.u : 0) * a.r + r0 + ur;
         if (a.u_vec && ur + 8 <= ranks) {
-            const float4 x = rows.u >= 0 ? ld_f4(p) : float4{}, y = rows.u >= 0 ? ld_f4(p + 4) : float4{};
-            u[0] = x.x, u[1] = x.y, u[2] = x.z, u[3] = x.w, u[4] = y.x, u[5] = y.y, u[6] = y.z, u[7] = y.w;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dsmem_u32(own + j * kLoraThreads)), "l"(p + 4 * j), "r"(rows.u >= 0 ? 16 : 0) : "memory");
         } else {
+            float u[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) u[j] = rows.u >= 0 && ur + j < ranks ? p[j] : 0.f;
+            own[0] = make_float4(u[0], u[1], u[2], u[3]), own[kLoraThreads] = make_float4(u[4], u[5], u[6], u[7]);
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto load_u = [&](int i, float (&u)[8]) {
+        const float4 x = s.own[i % kRing][0][tid], y = s.own[i % kRing][1][tid];
+        u[0] = x.x, u[1] = x.y, u[2] = x.z, u[3] = x.w, u[4] = y.x, u[5] = y.y, u[6] = y.z, u[7] = y.w;
     };
     auto publish = [&](int i, const float (&u)[8]) {
         if (DT == 1) return;
@@ -448,24 +458,27 @@ template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_k
         }
     };
     float sum[kTiles][4] = {}, u[8];
-    Rows rows = rows_of(0), next = rows_of(1), after = rows_of(2);
-    fetch(0, rows);
-    fetch(1, next);
-    load_u(rows, u);
+    Rows after;
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) fetch(i, rows_of(i));
+    after = rows_of(kRing - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 3) : "memory");     // steps 0 and 1
+    load_u(0, u);
     publish(0, u);
     __syncthreads();
     float up = scale_of(0), up_next;
     put_planes(0, up, u);
-    load_u(next, u);
+    load_u(1, u);
     publish(1, u);
     for (int i = 0; i < steps; ++i) {
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 4) : "memory"); // step i + 2
         __syncthreads();
-        fetch(i + 2, after);
+        fetch(i + kRing - 1, after);
+        after = rows_of(i + kRing);
         up_next = scale_of(i + 1);
         put_planes(i + 1, up_next, u);
-        load_u(after, u);
-        after = rows_of(i + 3);
+        load_u(i + 2, u);
+        publish(i + 2, u);
         float d[kTiles][4] = {};
 #pragma unroll
         for (int k = 0; k < kGradPos; k += 16) {
@@ -489,7 +502,6 @@ template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_k
                 for (int e = 0; e < 4; ++e) sum[j][e] = fmaf(d[j][e], down, sum[j][e]);
         }
         up = up_next;
-        publish(i + 2, u);
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();

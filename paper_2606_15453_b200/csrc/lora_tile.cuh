@@ -24,6 +24,7 @@
 namespace stmoe_dev {
 
 constexpr int kTileRows = 128, kTileMaxRank = 128;
+constexpr int kDownMaxSplits = 8;          // parts of the inner dimension: a portable cluster
 constexpr int kDownTileThreads = 160;       // warps 0-3 copy and store, warp 4 issues
 constexpr int kUpTileThreads = 416;         // warps 0-7 add and store, 8-11 copy B and the base, 12 issues
 constexpr int kUpRowBytes = 256, kUpPitch = kUpRowBytes + 16;   // of a unit's row, and from one to the next in shared memory
@@ -169,9 +170,10 @@ template <int DT, bool XVEC, bool WVEC> __global__ void __launch_bounds__(kDownT
     pdl_wait();
     pdl_launch_dependents();
     lora_tiles(a, s_tile, s_sum);
-    const int from = blockIdx.y * a.steps, to = min(from + a.steps, (a.I + 63) / 64);
-    if ((int)blockIdx.x >= s_tile[a.n] || from >= to) return;
-    const LoraTile t = lora_tile_at(a, s_tile, blockIdx.x);
+    // the parts of a tile's inner dimension are a cluster
+    const int rank = blockIdx.x % a.splits, from = rank * a.steps, to = min(from + a.steps, (a.I + 63) / 64);
+    if ((int)blockIdx.x / a.splits >= s_tile[a.n]) return;
+    const LoraTile t = lora_tile_at(a, s_tile, blockIdx.x / a.splits);
     uint8_t *const dsm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dsm_raw) + 1023) & ~(uintptr_t)1023);
     if (tid == 0) {
         s_dead = 0;
@@ -230,17 +232,17 @@ template <int DT, bool XVEC, bool WVEC> __global__ void __launch_bounds__(kDownT
             }
         ok = ok && __all_sync(kFull, dmbar_wait(&done, 0, dead, a.polls));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        // a thread a position
+        // a thread a position: one part goes to memory, several to shared memory, where every stage has been read
         const int i = warp * kWarp + lane;
-        float *const part = a.part + ((long long)blockIdx.y * a.T + t.begin + i) * a.rp;
+        float *const to_row = a.splits == 1 ? a.part + (long long)(t.begin + i) * a.rp : reinterpret_cast<float *>(dsm) + i * (r16 + 4);
         for (int r = 0; r < a.rp; r += 8) {
             float v[8];
             if (ok) tmem_ld8(tmem + ((uint32_t)(warp * kWarp) << 16) + r, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = ok ? v[j] : NAN;
             if (i < t.count) {
-                *reinterpret_cast<float4 *>(part + r) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4 *>(part + r + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                *reinterpret_cast<float4 *>(to_row + r) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4 *>(to_row + r + 4) = make_float4(v[4], v[5], v[6], v[7]);
             }
         }
     } else {
@@ -257,6 +259,24 @@ template <int DT, bool XVEC, bool WVEC> __global__ void __launch_bounds__(kDownT
             if (++s == NS) s = 0, par ^= 1;
         }
         if (ok) umma_commit_if(leader, &done);
+    }
+    if (a.splits > 1) {
+        __syncwarp();
+        cluster_sync();
+        const int pieces = a.rp / 4;
+        for (int e = rank * kDownTileThreads + tid; e < t.count * pieces; e += a.splits * kDownTileThreads) {
+            const int i = e / pieces, r = e % pieces * 4;
+            const uint32_t at = dsmem_u32(dsm) + (i * (r16 + 4) + r) * 4;
+            float4 v[kDownMaxSplits];
+#pragma unroll
+            for (int z = 0; z < kDownMaxSplits; ++z)
+                if (z < a.splits) v[z] = ld_cluster4(at, z);
+#pragma unroll
+            for (int z = 1; z < kDownMaxSplits; ++z)
+                if (z < a.splits) v[0].x += v[z].x, v[0].y += v[z].y, v[0].z += v[z].z, v[0].w += v[z].w;
+            *reinterpret_cast<float4 *>(a.part + (long long)(t.begin + i) * a.rp + r) = v[0];
+        }
+        cluster_sync();                     // nobody leaves while its part is read
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
@@ -360,17 +380,10 @@ template <int DT, int DO, int PL, bool WVEC, bool OVEC> __global__ void __launch
                     const float c = a.alpha * (a.scale ? a.scale[t.g] : 1.f);
                     for (int i0 = tid / lanes; i0 < kTileRows; i0 += 8 * rows) {
                         float4 sum[8];
+                        const float *const p = a.part + (long long)(t.begin + i0) * a.rp + k;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        const float *p = a.part + (long long)(t.begin + i0) * a.rp + k;
-                        for (int s = 0; s < a.splits; ++s, p += (long long)a.T * a.rp) {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (i0 + j * rows < t.count && k < a.rp) {
-                                    const float4 v = *reinterpret_cast<const float4 *>(p + j * rows * a.rp);
-                                    sum[j].x += v.x, sum[j].y += v.y, sum[j].z += v.z, sum[j].w += v.w;
-                                }
-                        }
+                        for (int j = 0; j < 8; ++j)
+                            sum[j] = i0 + j * rows < t.count && k < a.rp ? ld_f4(p + j * rows * a.rp) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const int pos = i0 + j * rows;

@@ -230,23 +230,6 @@ __device__ __forceinline__ Mx4Task mm_task(const Mx4MatmulArgs &a, const int *s_
     return k;
 }
 
-// the float4 (or float) at this CTA's shared-memory address, read from CTA `rank` of the cluster
-__device__ __forceinline__ float4 ld_cluster4(uint32_t smem, int rank)
-{
-    uint32_t remote;
-    float4 v;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem), "r"(rank));
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote));
-    return v;
-}
-__device__ __forceinline__ float ld_cluster(uint32_t smem, int rank)
-{
-    uint32_t remote;
-    float v;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote));
-    return v;
-}
 // How many clusters of 2, 4 and 8 CTAs of a kernel run at a time: fewer than the SMs would suggest, as a
 // cluster has to fit one of the GPU's processor clusters.
 struct MmClusters {

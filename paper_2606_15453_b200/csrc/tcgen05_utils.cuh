@@ -9,6 +9,24 @@
 
 namespace stmoe_dev {
 
+// the float4 (or float) at this CTA's shared-memory address, read from CTA `rank` of the cluster
+__device__ __forceinline__ float4 ld_cluster4(uint32_t smem, int rank)
+{
+    uint32_t remote;
+    float4 v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote));
+    return v;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t smem, int rank)
+{
+    uint32_t remote;
+    float v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote));
+    return v;
+}
+
 constexpr int kDenseSpinLimit = 1 << 22;
 // Polls after which a wait of the operators' kernels gives up, for the launches to come (tests lower it).
 inline std::atomic<int> g_mx4_polls{kDenseSpinLimit};
