@@ -44,7 +44,7 @@ int64_t part_bytes(int64_t tokens, int rank, int inner)
 {
     return up_to((int64_t)sizeof(float) * (by_tiles(tokens, rank) ? 1 : down_splits(tokens, rank, inner)) * tokens * up_to(rank, 8), 256);
 }
-int grad_task_rows(int64_t tokens) { return (int)std::max<int64_t>(512, up_to((tokens + 15) / 16, kGradPos)); }
+int grad_task_rows(int64_t tokens) { return (int)std::max<int64_t>(256, up_to((tokens + 15) / 16, kGradPos)); }
 int grad_parts(int64_t tokens) { return (int)(2 * tokens / grad_task_rows(tokens)); }
 
 // more than the default 48 KB of shared memory: asked for once per device
@@ -201,7 +201,7 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
         k.x = grad, k.x_stride = grad_stride, k.a = bt, k.a_row = outer8, k.a_group = rank * outer8, k.b = a_t, k.b_row = rank8, k.b_group = inner * rank8;
         k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.I = outer, k.O = inner;
         k.counts = counts, k.starts = starts, k.polls = g_mx4_polls.load(std::memory_order_relaxed), k.rp = (int)up_to(rank, 8), k.part = part;
-        k.out = grad_x, k.out_stride = grad_x_stride, k.hidden = u;
+        k.out = grad_x, k.out_stride = grad_x_stride, k.hidden = u, k.early = true;
         if (const int rc = launch_down(k, dtype, dev, st)) return rc;
         if (const int rc = launch_up(k, dtype, dtype, dev, sms, st)) return rc;
     }

@@ -49,7 +49,13 @@ struct LoraArgs {
     bool keep;              // out is base: rows without an adapter are there already
     float *hidden;          // [T][r] or nullptr: h by row
     int polls;              // limit of every wait of the tile kernels
+    bool early;             // the kernel before in the stream is one of this call's (see below)
 };
+
+// Ahead of pdl_wait: every kernel here waits for the one before it and only then lets the one behind it start.  So when a kernel of this
+// call starts behind another one of this call, all that ran before that other one is complete, and the grouping, the operands and
+// the base, which none of them writes, can be read at once; only what the kernel before wrote, and all writing, stays behind
+// the wait.
 
 // D += A B for one 16 x 8 x 16 step (A 16 x 16 by rows, B 16 x 8 by columns); F32 accumulators.
 template <int DT> __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -192,11 +198,22 @@ template <int DT, int DO, int PL, bool VEC> __global__ void __launch_bounds__(kL
     __shared__ float s_factor[kLoraPos];
     __shared__ int s_row[kLoraPos];
     const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp, q = lane % 4, o = lane / 4;
-    pdl_wait();
-    pdl_launch_dependents();
     const int p = blockIdx.x, o0 = blockIdx.y * kLoraOutBlock;
     int row8, g8, g;
     const int count = lora_tile(a, p, lane, row8, g8, g);
+    const T *const w = reinterpret_cast<const T *>(a.b) + max(g, 0) * a.b_group;
+    uint4 lo[kTiles], hi[kTiles];
+    auto load_b = [&](int k) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+            const int oa = o0 + (warp + i * kLoraWarps) * 16 + o, ob = oa + 8;
+            lo[i] = lora_load8<DT, VEC>(w + oa * a.b_row, k + q * 8, a.r, oa < a.O);
+            hi[i] = lora_load8<DT, VEC>(w + ob * a.b_row, k + q * 8, a.r, ob < a.O);
+        }
+    };
+    if (count > 0 && g >= 0) load_b(0);
+    pdl_wait();
+    pdl_launch_dependents();
     if (count == 0 || (g < 0 && a.keep)) return;
     if (warp == 0 && lane < kLoraPos) s_row[lane] = row8;
     if (g >= 0) {
@@ -230,16 +247,9 @@ template <int DT, int DO, int PL, bool VEC> __global__ void __launch_bounds__(kL
         }
         if (lane == 0) s_factor[warp] = a.alpha * (a.scale ? a.scale[g] : 1.f) / up;
         __syncthreads();
-        const T *const w = reinterpret_cast<const T *>(a.b) + g * a.b_group;
         float d[kTiles][4] = {};
         for (int k0 = 0; k0 < wide; k0 += kLoraStep) {
-            uint4 lo[kTiles], hi[kTiles];
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
-                const int oa = o0 + (warp + i * kLoraWarps) * 16 + o, ob = oa + 8;
-                lo[i] = lora_load8<DT, VEC>(w + oa * a.b_row, k0 + q * 8, a.r, oa < a.O);
-                hi[i] = lora_load8<DT, VEC>(w + ob * a.b_row, k0 + q * 8, a.r, ob < a.O);
-            }
+            if (k0 > 0) load_b(k0);
 #pragma unroll
             for (int j = 0; j < PL; ++j) {
                 const uint4 hv = *reinterpret_cast<const uint4 *>(&s_h[j][o][k0 + q * 8]);
@@ -300,9 +310,9 @@ __global__ void __launch_bounds__(kLoraThreads) lora_transpose_kernel(const Lora
         if (c0 + i < a.cols[w] && r0 + x < a.rows[w]) t[(c0 + i) * a.t_row[w] + r0 + x] = s[x][i];
 }
 
-constexpr int kGradCols = 128;      // columns of a CTA: 16 a warp
+constexpr int kGradCols = 256;      // columns of a CTA: 32 a warp
 constexpr int kGradPos = 32;        // positions of a step
-constexpr int kGradRing = 5, kGradSmem = 104 * 1024;
+constexpr int kGradSmem = 87 * 1024;
 
 struct LoraGradArgs {
     const float *u;         // [T][r] by row
@@ -365,73 +375,65 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t (&r)[4])
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 
-// One task's sum over its positions of z[p][c] u[p][r] for 128 columns and up to 64 ranks.  Columns are the MMA's rows, positions its inner
-// dimension: z lies in shared memory as in memory and is read transposed, u as planes by rank.  A step of 32 positions costs one barrier: behind
-// barrier i the MMAs of step i run while z and u are on their way for steps up to i + 4, u is turned into planes for step i + 1, and the
-// largest magnitude of step i + 2 is found (fp16 planes), which the next barrier publishes.  A thread copies the u that it reads itself.
+// One task's sum over its positions of z[p][c] u[p][r] for 256 columns and up to 64 ranks.  Columns are the MMA's rows, positions its inner
+// dimension: z lies in shared memory as in memory and is read transposed, u as planes by rank, 32 columns a warp.  What bounds it is issue
+// slots: every CTA turns the same u into planes, which 256 columns share (with 128, and all 64 ranks converted where there were 24, 4099 rows of 2048
+// and 2816 columns took 26 and 37 us, now GRADTIME).  A step of 32 positions costs one barrier: behind barrier i the MMAs of step i run while z
+// is on its way for steps up to i + 3, u is turned into planes for step i + 1, the largest magnitude of step i + 2 is found (fp16 planes), which the
+// next barrier publishes, and u is asked for for step i + 3.  The planes' power of two follows the largest u so far, the sums with it.
 template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_kernel(const LoraGradArgs a)
 {
     using T = typename Elem<DT>::T;
-    constexpr int PL = 2, kTiles = kLoraRankBlock / 8, kZ = kGradCols + 8, kU = kGradPos + 8, kRing = kGradRing;
+    constexpr int PL = 2, kTiles = kLoraRankBlock / 8, kZ = kGradCols + 8, kU = kGradPos + 8, kRing = 4;
     struct Steps {
         T z[kRing][kGradPos][kZ];
-        float4 own[kRing][2][kLoraThreads];     // u: eight ranks of a position, a thread's own
         uint16_t u[2][PL][kLoraRankBlock][kU];
     };
     extern __shared__ __align__(16) uint8_t smem[];
     Steps &s = *reinterpret_cast<Steps *>(smem);
     float *const s_out = reinterpret_cast<float *>(smem);       // [64][kGradCols + 1], behind the last step
     static_assert(sizeof(Steps) <= kGradSmem && kLoraRankBlock * (kGradCols + 1) * 4 <= kGradSmem, "");
+    static_assert(kGradPos == kWarp && kGradCols == 8 * kWarp, "a lane is a position of u, and a piece of a row of z");
     __shared__ float s_most[2][kLoraWarps];
     const int tid = threadIdx.x, lane = tid % kWarp, warp = tid / kWarp, q = lane % 4, o = lane / 4;
-    pdl_wait();
-    pdl_launch_dependents();
     LoraTask task;
-    if (!lora_task(a, blockIdx.x, task)) return;
-    if (task.tasks > 1 && task.several + task.index >= a.parts) return;   // counts of more rows than there are
+    if (!lora_task(a, blockIdx.x, task) || (task.tasks > 1 && task.several + task.index >= a.parts)) {   // behind the last; counts of more rows than there are
+        pdl_wait();
+        return;
+    }
     const int c0 = blockIdx.y * kGradCols, r0 = blockIdx.z * kLoraRankBlock, here = min(kGradCols, a.C - c0), ranks = min(kLoraRankBlock, a.r - r0);
     const int begin = a.starts[task.g] + task.index * a.task_rows;
     const int count = max(0, min(a.task_rows, a.counts[task.g] - task.index * a.task_rows)), steps = (count + kGradPos - 1) / kGradPos;
-    const T *const z = reinterpret_cast<const T *>(a.z);
-    auto row_at = [&](int i) {           // row of the task's position i, -1 behind its last
-        const int row = i < count && (unsigned)(begin + i) < (unsigned)a.T ? a.order[begin + i] : -1;
+    const T *const z = reinterpret_cast<const T *>(a.z) + c0 + lane * 8;
+    const int ur = warp * 8;             // u: a lane a position, a warp eight ranks
+    auto row_of = [&](int i) {           // row of the lane's position of step i, -1 behind the task's last
+        const int at = i * kGradPos + lane, row = at < count && (unsigned)(begin + at) < (unsigned)a.T ? a.order[begin + at] : -1;
         return (unsigned)row < (unsigned)a.T ? row : -1;
     };
-    // z: sixteen lanes a row, rows tid / 16 and 16 further; u: eight ranks of position lane
-    const int zp = tid / 16, zc = tid % 16 * 8, ur = warp * 8;
-    struct Rows {
-        int z[2], u;
-    };
-    auto rows_of = [&](int i) { return Rows{{row_at(i * kGradPos + zp), row_at(i * kGradPos + zp + 16)}, row_at(i * kGradPos + lane)}; };
-    auto fetch = [&](int i, const Rows &rows) {
+    auto fetch = [&](int i, int row) {   // z: a warp a row, positions warp + 8 j
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            T *const dst = &s.z[i % kRing][zp + 16 * j][zc];
-            const T *const src = z + (rows.z[j] >= 0 ? rows.z[j] : 0) * a.z_stride + c0 + zc;
-            if (a.vec && zc + 8 <= here) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dsmem_u32(dst)), "l"(src), "r"(rows.z[j] >= 0 ? 16 : 0) : "memory");
+        for (int j = 0; j < kGradPos / kLoraWarps; ++j) {
+            const int pos = warp + j * kLoraWarps, of = __shfl_sync(kFull, row, pos);
+            T *const dst = &s.z[i % kRing][pos][lane * 8];
+            const T *const src = z + (of >= 0 ? of : 0) * a.z_stride;
+            if (a.vec && lane * 8 + 8 <= here) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dsmem_u32(dst)), "l"(src), "r"(of >= 0 ? 16 : 0) : "memory");
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e] = rows.z[j] >= 0 && zc + e < here ? src[e] : Elem<DT>::from_f32(0.f);
+                for (int e = 0; e < 8; ++e) dst[e] = of >= 0 && lane * 8 + e < here ? src[e] : Elem<DT>::from_f32(0.f);
             }
-        }
-        float4 *const own = &s.own[i % kRing][0][tid];
-        const float *const p = a.u + (long long)(rows.u >= 0 ? rows.u : 0) * a.r + r0 + ur;
-        if (a.u_vec && ur + 8 <= ranks) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dsmem_u32(own + j * kLoraThreads)), "l"(p + 4 * j), "r"(rows.u >= 0 ? 16 : 0) : "memory");
-        } else {
-            float u[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = rows.u >= 0 && ur + j < ranks ? p[j] : 0.f;
-            own[0] = make_float4(u[0], u[1], u[2], u[3]), own[kLoraThreads] = make_float4(u[4], u[5], u[6], u[7]);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto load_u = [&](int i, float (&u)[8]) {
-        const float4 x = s.own[i % kRing][0][tid], y = s.own[i % kRing][1][tid];
-        u[0] = x.x, u[1] = x.y, u[2] = x.z, u[3] = x.w, u[4] = y.x, u[5] = y.y, u[6] = y.z, u[7] = y.w;
+    auto load_u = [&](int row, float (&u)[8]) {
+        const float *const p = a.u + (long long)(row >= 0 ? row : 0) * a.r + r0 + ur;
+        if (a.u_vec && ur + 8 <= ranks) {
+            const float4 x = row >= 0 ? ld_f4(p) : float4{}, y = row >= 0 ? ld_f4(p + 4) : float4{};
+            u[0] = x.x, u[1] = x.y, u[2] = x.z, u[3] = x.w, u[4] = y.x, u[5] = y.y, u[6] = y.z, u[7] = y.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = row >= 0 && ur + j < ranks ? p[j] : 0.f;
+        }
     };
     auto publish = [&](int i, const float (&u)[8]) {
         if (DT == 1) return;
@@ -441,14 +443,17 @@ template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_k
         most = warp_max(most);
         if (lane == 0) s_most[i & 1][warp] = most;
     };
-    auto scale_of = [&](int i) {         // one power of two for the whole step
-        if (DT == 1) return 1.f;
-        float most = 0.f;
+    float largest = 0.f;                 // |u| of the steps up to the one whose planes are next
+    auto scale_of = [&](int i) {
+        if constexpr (DT == 1) return 1.f;
+        else {
 #pragma unroll
-        for (int w = 0; w < kLoraWarps; ++w) most = fmaxf(most, s_most[i & 1][w]);
-        return plane_scale<DT>(most);
+            for (int w = 0; w < kLoraWarps; ++w) largest = fmaxf(largest, s_most[i & 1][w]);
+            return plane_scale<DT>(largest);
+        }
     };
     auto put_planes = [&](int i, float up, const float (&u)[8]) {
+        if (ur >= ranks) return;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             uint16_t pl[PL];
@@ -457,59 +462,71 @@ template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_k
             for (int p = 0; p < PL; ++p) s.u[i & 1][p][ur + j][lane] = pl[p];
         }
     };
-    float sum[kTiles][4] = {}, u[8];
-    Rows after;
-#pragma unroll
-    for (int i = 0; i < kRing - 1; ++i) fetch(i, rows_of(i));
-    after = rows_of(kRing - 1);
-    asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 3) : "memory");     // steps 0 and 1
-    load_u(0, u);
-    publish(0, u);
+    float sum[2][kTiles][4] = {}, u0[8], u1[8];
+    const int row0 = row_of(0), row1 = row_of(1);
+    int row = row_of(2);
+    fetch(0, row0), fetch(1, row1), fetch(2, row);
+    pdl_wait();                          // u and the parts' room may be the kernel before's
+    pdl_launch_dependents();
+    load_u(row0, u0), load_u(row1, u1);
+    publish(0, u0), publish(1, u1);
     __syncthreads();
-    float up = scale_of(0), up_next;
-    put_planes(0, up, u);
-    load_u(1, u);
-    publish(1, u);
-    for (int i = 0; i < steps; ++i) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 4) : "memory"); // step i + 2
+    float up = scale_of(0), scaled = up;          // of the planes that are next for the MMAs, and of the sums
+    put_planes(0, up, u0);
+    load_u(row, u0);
+    row = row_of(3);
+    // convert: u of step i + 1, then of step i + 3; ahead: of step i + 2
+    auto step = [&](int i, float (&convert)[8], const float (&ahead)[8]) {
+        asm volatile("cp.async.wait_group 2;" ::: "memory");
         __syncthreads();
-        fetch(i + kRing - 1, after);
-        after = rows_of(i + kRing);
-        up_next = scale_of(i + 1);
-        put_planes(i + 1, up_next, u);
-        load_u(i + 2, u);
-        publish(i + 2, u);
-        float d[kTiles][4] = {};
+        fetch(i + 3, row);
+        const float next = scale_of(i + 1);
+        put_planes(i + 1, next, convert);
+        load_u(row, convert);
+        row = row_of(i + 4);
+        publish(i + 2, ahead);
+        if (DT != 1 && up != scaled) {            // a larger u than any before
+            const float f = up / scaled;
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[m][j][e] *= f;
+            scaled = up;
+        }
+        up = next;
 #pragma unroll
         for (int k = 0; k < kGradPos; k += 16) {
-            uint32_t za[4];
-            ldmatrix4t(dsmem_u32(&s.z[i % kRing][k + (lane & 7) + (lane & 16) / 2][warp * 16 + (lane & 8)]), za);
+            uint32_t za[2][4];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) ldmatrix4t(dsmem_u32(&s.z[i % kRing][k + (lane & 7) + (lane & 16) / 2][warp * 32 + m * 16 + (lane & 8)]), za[m]);
 #pragma unroll
             for (int j = 0; j < kTiles; ++j)
                 if (j * 8 < ranks) {
 #pragma unroll
                     for (int p = 0; p < PL; ++p) {
                         const uint16_t *const col = &s.u[i & 1][p][j * 8 + o][k + 2 * q];
-                        mma16<DT>(DT == 1 ? sum[j] : d[j], za[0], za[1], za[2], za[3], *reinterpret_cast<const uint32_t *>(col), *reinterpret_cast<const uint32_t *>(col + 8));
+                        const uint32_t b0 = *reinterpret_cast<const uint32_t *>(col), b1 = *reinterpret_cast<const uint32_t *>(col + 8);
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) mma16<DT>(sum[m][j], za[m][0], za[m][1], za[m][2], za[m][3], b0, b1);
                     }
                 }
         }
-        if (DT != 1) {
-            const float down = 1.f / up;
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum[j][e] = fmaf(d[j][e], down, sum[j][e]);
-        }
-        up = up_next;
+    };
+    for (int i = 0; i < steps; i += 2) {
+        step(i, u1, u0);
+        if (i + 1 < steps) step(i + 1, u0, u1);
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
-    const float c = a.alpha * (a.scale ? a.scale[task.g] : 1.f);
+    const float c = a.alpha * (a.scale ? a.scale[task.g] : 1.f) / scaled;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s_out[(i * 8 + 2 * q + (j & 1)) * (kGradCols + 1) + warp * 16 + o + (j & 2) * 4] = c * sum[i][j];
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) s_out[(i * 8 + 2 * q + (j & 1)) * (kGradCols + 1) + warp * 32 + m * 16 + o + (j & 2) * 4] = c * sum[m][i][j];
     __syncthreads();
     const long long size = (long long)a.r * a.C;
     T *const grad = reinterpret_cast<T *>(a.grad) + task.g * size;

@@ -167,9 +167,10 @@ template <int DT, bool XVEC, bool WVEC> __global__ void __launch_bounds__(kDownT
     const int r16 = lora_r16(a.r), NS = down_stages(a.r), slot = down_stage_bytes(a.r);
     int cols = 32;
     while (cols < r16) cols *= 2;
-    pdl_wait();
-    pdl_launch_dependents();
+    if (!a.early) pdl_wait();
     lora_tiles(a, s_tile, s_sum);
+    if (a.early) pdl_wait();
+    pdl_launch_dependents();
     // the parts of a tile's inner dimension are a cluster
     const int rank = blockIdx.x % a.splits, from = rank * a.steps, to = min(from + a.steps, (a.I + 63) / 64);
     if ((int)blockIdx.x / a.splits >= s_tile[a.n]) return;
@@ -314,14 +315,15 @@ template <int DT, int DO, int PL, bool WVEC, bool OVEC> __global__ void __launch
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], tfull[4], tempty[4], planes, bfull[kUnits], bfree[kUnits];
     const int tid = threadIdx.x, warp = tid / kWarp, lane = tid % kWarp;
     const int slabs = lora_slabs(a.r), r16 = lora_r16(a.r), NS = up_stages(a.r), NU = up_units(a.r);
-    pdl_wait();
-    pdl_launch_dependents();
     lora_tiles(a, s_tile, s_sum);
     // units of this CTA: whole tiles' columns, tile after tile
     const int per_tile = (a.O + kCols - 1) / kCols;
     const int units = s_tile[a.keep && !a.hidden ? a.n : a.n + 1] * per_tile;      // < 2^31: checked by the host
     const int first = (int)((long long)units * blockIdx.x / gridDim.x), count = (int)((long long)units * (blockIdx.x + 1) / gridDim.x) - first;
-    if (count <= 0) return;
+    if (count <= 0) {
+        pdl_wait();
+        return;
+    }
     uint8_t *const dsm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dsm_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t h_at = dsmem_u32(dsm), b_at = h_at + PL * slabs * kSlabBytes;
     uint8_t *const units_at = dsm + PL * slabs * kSlabBytes + NS * up_b_bytes<DO>(a.r);
@@ -359,6 +361,8 @@ template <int DT, int DO, int PL, bool WVEC, bool OVEC> __global__ void __launch
         // OVEC: a lane's four rows are o + 8 j + 16 h of its warp's 32, where its sixteen outputs of each 64 begin at 16 q
         const int q = lane % 4, o = lane / 4;
         TO *to[2][2];
+        pdl_wait();                                          // h is the kernel before's
+        pdl_launch_dependents();
         for (int u = 0; u < count; step(u), ++u) {
             const bool some = t.g < a.n;
             if (fresh) {
