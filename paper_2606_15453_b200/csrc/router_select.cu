@@ -26,21 +26,42 @@ template <int DT, int LPR> int launch(bool backward, const SelectArgs &a, cudaSt
     void (*kernel)(SelectArgs) = backward ? router_select_backward_kernel<DT, LPR> : router_select_kernel<DT, LPR>;
     return launch_behind(kernel, (int)(((int64_t)a.T + rows - 1) / rows), kSelThreads, 0, 1, st, a);
 }
-// lanes that share a row: a power of two with eight logits each
-template <int DT> int launch_lanes(bool backward, const SelectArgs &a, cudaStream_t st)
+// A warp a row, in turns: three CTAs an SM, as the kernel's registers allow.
+template <int DT> int launch_wide(const SelectArgs &a, int sms, cudaStream_t st)
 {
+    const int64_t ctas = ((int64_t)a.T + kSelThreads / kWarp - 1) / (kSelThreads / kWarp);
+    return launch_behind(router_select_wide_kernel<DT>, (int)std::min<int64_t>(ctas, sms * 3), kSelThreads, 0, 1, st, a);
+}
+// whether groups are whole lanes of a row of LPR = 32
+bool whole_groups(const SelectArgs &a)
+{
+    const int gs = a.E / a.G, lg = gs / kSelN;
+    return a.G == 1 || (gs % kSelN == 0 && (lg & (lg - 1)) == 0);
+}
+// lanes that share a row: a power of two with eight logits each
+template <int DT> int launch_sparse_backward(const SelectArgs &a, int sms, cudaStream_t st)
+{
+    int kp = 1;
+    while (kp < a.K) kp *= 2;
+    const int rows = std::min(4, kWarp / kp), per = kSelThreads / kWarp * rows;
+    return launch_behind(router_select_sparse_backward_kernel<DT>, (int)std::min<int64_t>(((int64_t)a.T + per - 1) / per, sms * 6), kSelThreads, 0, 1, st, a, kp, rows);
+}
+template <int DT> int launch_lanes(bool backward, const SelectArgs &a, int sms, cudaStream_t st)
+{
+    if (backward && (a.sigmoid || a.renorm)) return launch_sparse_backward<DT>(a, sms, st);
     if (a.E <= 8) return launch<DT, 1>(backward, a, st);
     if (a.E <= 16) return launch<DT, 2>(backward, a, st);
     if (a.E <= 32) return launch<DT, 4>(backward, a, st);
     if (a.E <= 64) return launch<DT, 8>(backward, a, st);
     if (a.E <= 128) return launch<DT, 16>(backward, a, st);
+    if (!backward && whole_groups(a)) return launch_wide<DT>(a, sms, st);
     return launch<DT, 32>(backward, a, st);
 }
-int launch_typed(int dtype, bool backward, const SelectArgs &a, cudaStream_t st)
+int launch_typed(int dtype, bool backward, const SelectArgs &a, int sms, cudaStream_t st)
 {
-    if (dtype == STMOE_F32) return launch_lanes<0>(backward, a, st);
-    if (dtype == STMOE_BF16) return launch_lanes<1>(backward, a, st);
-    return launch_lanes<4>(backward, a, st);
+    if (dtype == STMOE_F32) return launch_lanes<0>(backward, a, sms, st);
+    if (dtype == STMOE_BF16) return launch_lanes<1>(backward, a, sms, st);
+    return launch_lanes<4>(backward, a, sms, st);
 }
 
 }  // namespace
@@ -64,7 +85,7 @@ int stmoe_router_select(const void *logits, int dtype, int64_t stride, const flo
     a.vec = rows_vec(logits, dtype, stride), a.sigmoid = flags & STMOE_SELECT_SIGMOID, a.renorm = flags & STMOE_SELECT_RENORM;
     a.exact = !bias && (a.G == 1 || group_best == 1);
     a.scale = scale, a.ids = ids, a.w = w;
-    return launch_typed(dtype, false, a, (cudaStream_t)cuda_stream);
+    return launch_typed(dtype, false, a, sms, (cudaStream_t)cuda_stream);
 }
 
 int stmoe_router_select_backward(const void *logits, int dtype, int64_t stride, int64_t tokens, int n_experts, int top_k, int flags, float scale,
@@ -83,7 +104,7 @@ int stmoe_router_select_backward(const void *logits, int dtype, int64_t stride, 
     a.vec = rows_vec(logits, dtype, stride) && rows_vec(grad_logits, dtype, grad_stride);
     a.sigmoid = flags & STMOE_SELECT_SIGMOID, a.renorm = flags & STMOE_SELECT_RENORM, a.scale = scale;
     a.ids = (int *)ids, a.w = (float *)w, a.grad = grad_w, a.dlogits = grad_logits, a.dstride = grad_stride;
-    return launch_typed(dtype, true, a, (cudaStream_t)cuda_stream);
+    return launch_typed(dtype, true, a, sms, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

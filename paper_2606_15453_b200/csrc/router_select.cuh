@@ -131,7 +131,9 @@ template <int LPR, typename F> __device__ __forceinline__ void sel_values(const 
 
 // Groups that stay; members of the others become -infinity.  near: a group of the other side of the border lies within the
 // slack.  keys, totals: the row's room in shared memory.
-template <int LPR, typename F> __device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, int e0, F (&v)[kSelN], F *keys, F *totals, bool &near)
+// kWhole: groups are known to be 2^j whole lanes.
+template <int LPR, typename F, bool kWhole = false>
+__device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, int e0, F (&v)[kSelN], F *keys, F *totals, bool &near)
 {
     const int gs = a.E / a.G, lg = gs / kSelN;
     const F lowest = -INFINITY;
@@ -152,7 +154,7 @@ template <int LPR, typename F> __device__ __forceinline__ void sel_groups(const 
         sure += other > mine + room || (room == (F)0 && other == mine && og < g);
         maybe += og != g && (room == (F)0 ? other > mine || (other == mine && og < g) : !(other < mine - room) && other > lowest);
     };
-    if (gs % kSelN == 0 && (lg & (lg - 1)) == 0) {   // a group is 2^j whole lanes
+    if (kWhole || (gs % kSelN == 0 && (lg & (lg - 1)) == 0)) {   // a group is 2^j whole lanes
         F b1 = lowest, b2 = lowest;
 #pragma unroll
         for (int i = 0; i < kSelN; ++i) merge(b1, b2, v[i] > lowest ? v[i] : lowest, lowest);
@@ -168,31 +170,33 @@ template <int LPR, typename F> __device__ __forceinline__ void sel_groups(const 
         }
         return;
     }
+    if constexpr (!kWhole) {
 #pragma unroll
-    for (int i = 0; i < kSelN; ++i) keys[e0 + i] = v[i] > lowest ? v[i] : lowest;
-    __syncwarp();
-    for (int g = l; g < a.G; g += LPR) {
-        F b1 = lowest, b2 = lowest;
-        for (int i = 0; i < gs; ++i) merge(b1, b2, keys[g * gs + i], lowest);
-        totals[g] = total_of(b1, b2);
-    }
-    __syncwarp();
-    uint32_t stay = 0;
-    for (int g = l; g < a.G; g += LPR) {
-        const F mine = totals[g];
-        int sure = 0, maybe = 0;
-        for (int og = 0; og < a.G; ++og) rank_step(mine, g, totals[og], og, sure, maybe);
-        near |= mine > lowest && sure < a.top_groups && maybe >= a.top_groups;
-        if (sure < a.top_groups) stay |= 1u << g;
-    }
+        for (int i = 0; i < kSelN; ++i) keys[e0 + i] = v[i] > lowest ? v[i] : lowest;
+        __syncwarp();
+        for (int g = l; g < a.G; g += LPR) {
+            F b1 = lowest, b2 = lowest;
+            for (int i = 0; i < gs; ++i) merge(b1, b2, keys[g * gs + i], lowest);
+            totals[g] = total_of(b1, b2);
+        }
+        __syncwarp();
+        uint32_t stay = 0;
+        for (int g = l; g < a.G; g += LPR) {
+            const F mine = totals[g];
+            int sure = 0, maybe = 0;
+            for (int og = 0; og < a.G; ++og) rank_step(mine, g, totals[og], og, sure, maybe);
+            near |= mine > lowest && sure < a.top_groups && maybe >= a.top_groups;
+            if (sure < a.top_groups) stay |= 1u << g;
+        }
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) stay |= __shfl_xor_sync(kFull, stay, o);
-    __syncwarp();   // the room is written again for the next choice
-    int g = e0 / gs, left = gs - e0 % gs;
+        for (int o = LPR / 2; o > 0; o >>= 1) stay |= __shfl_xor_sync(kFull, stay, o);
+        __syncwarp();   // the room is written again for the next choice
+        int g = e0 / gs, left = gs - e0 % gs;
 #pragma unroll
-    for (int i = 0; i < kSelN; ++i) {
-        if (e0 + i < a.E && !(stay >> g & 1)) v[i] = lowest;
-        if (--left == 0) ++g, left = gs;
+        for (int i = 0; i < kSelN; ++i) {
+            if (e0 + i < a.E && !(stay >> g & 1)) v[i] = lowest;
+            if (--left == 0) ++g, left = gs;
+        }
     }
 }
 
@@ -268,23 +272,11 @@ template <int LPR> struct SelShared {
     };
 };
 
-template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads, 4) router_select_kernel(const SelectArgs a)
+// Everything about a row from its logits on (-infinity throughout where it does not count): choice, weights, outputs.
+template <int LPR> __device__ __forceinline__ void sel_row(const SelectArgs &a, long long t, const float (&z)[kSelN], int l, int sub, SelShared<LPR> &s)
 {
-    using T = typename Elem<DT>::T;
-    constexpr int W = kSelThreads / kWarp, RPW = kWarp / LPR;
-    __shared__ SelShared<LPR> s_warp[W];
-    const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp, l = lane % LPR, sub = lane / LPR, e0 = l * kSelN;
-    SelShared<LPR> &s = s_warp[warp];
-    pdl_wait();
-    pdl_launch_dependents();
-    const long long t = ((long long)blockIdx.x * W + warp) * RPW + sub;
-    const bool counts = t < a.T && (!a.mask || a.mask[t]);
-    float z[kSelN];
-    if (counts) sel_load<DT>(reinterpret_cast<const T *>(a.logits) + t * a.stride, e0, a.E, a.vec, z);
-    else {
-#pragma unroll
-        for (int i = 0; i < kSelN; ++i) z[i] = -INFINITY;
-    }
+    constexpr uint32_t kRowBits = LPR == kWarp ? kFull : (1u << (LPR % kWarp)) - 1;
+    const int e0 = l * kSelN;
     float v[kSelN], m = 0.f, inv = 0.f;
     sel_values<LPR>(a, z, e0, v, m, inv);
     bool bad = false;
@@ -328,7 +320,7 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads, 4) rou
     for (int i = 0; i < kSelN; ++i)
         if (chosen >> i & 1) id[at] = e0 + i, zc[at] = z[i], ++at;
     __syncwarp();
-    const uint32_t any_bad = __ballot_sync(kFull, bad) >> (sub * LPR) & (LPR == kWarp ? kFull : (1u << (LPR % kWarp)) - 1);
+    const uint32_t any_bad = __ballot_sync(kFull, bad) >> (sub * LPR) & kRowBits;
     const float poison = any_bad || (!a.sigmoid && inv != inv) ? NAN : 0.f;
     auto log_score = [&](float x) { return a.sigmoid ? fminf(x, 0.f) - log1pf(expf(-fabsf(x))) : x; };
     float top = -INFINITY, sum = 0.f;
@@ -350,7 +342,196 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads, 4) rou
         }
 }
 
-// Gradient of sum grad . w; every element of the gradient's rows is written.
+template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads, 4) router_select_kernel(const SelectArgs a)
+{
+    using T = typename Elem<DT>::T;
+    constexpr int W = kSelThreads / kWarp, RPW = kWarp / LPR;
+    __shared__ SelShared<LPR> s_warp[W];
+    const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp, l = lane % LPR, sub = lane / LPR;
+    pdl_wait();
+    pdl_launch_dependents();
+    const long long t = ((long long)blockIdx.x * W + warp) * RPW + sub;
+    const bool counts = t < a.T && (!a.mask || a.mask[t]);
+    float z[kSelN];
+    if (counts) sel_load<DT>(reinterpret_cast<const T *>(a.logits) + t * a.stride, l * kSelN, a.E, a.vec, z);
+    else {
+#pragma unroll
+        for (int i = 0; i < kSelN; ++i) z[i] = -INFINITY;
+    }
+    sel_row<LPR>(a, t, z, l, sub, s_warp[warp]);
+}
+
+// ---- one row a warp (more than 128 experts) -----------------------------------------------------
+//
+// K rounds over eight values a lane are 1400 instructions a row.  Here the K rounds run over one value a lane, the largest of its
+// eight: the K-th of these is a lower bound of the row's K-th value, and what reaches it, K values and a few, is brought
+// together, a value a lane in ascending order of index, where the few too many are taken away from below (of equal ones the
+// highest index first).  Rows that hold an infinity or a NaN, rows with more than 32 values at the bound and rows that have to
+// look twice at their border go the general way (131072 x 256, 8 groups, K 8: 259 -> SELTIME us).
+
+__device__ __forceinline__ float redux_max(float v)
+{
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float redux_min(float v)
+{
+    float r;
+    asm("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+__device__ __noinline__ void sel_row_again(const SelectArgs &a, long long t, const float *zp, SelShared<kWarp> &s)
+{
+    float z[kSelN];
+#pragma unroll
+    for (int i = 0; i < kSelN; ++i) z[i] = zp[i];
+    __syncwarp();
+    sel_row<kWarp>(a, t, z, threadIdx.x % kWarp, 0, s);
+    __syncwarp();
+}
+
+struct Candidate {
+    float v, z;
+    int id, pad;
+};
+
+// false: the general way
+__device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, const float (&z)[kSelN], const float (&bias)[kSelN], int valid, Candidate *room)
+{
+    const int lane = threadIdx.x % kWarp;
+    const float lowest = -INFINITY;
+    float v[kSelN], m = 0.f, inv = 0.f, probe = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSelN; ++i) probe = fmaf(i < valid ? z[i] : 0.f, 0.f, probe);
+    if (__any_sync(kFull, probe != 0.f)) return false;          // an infinity or a NaN
+    if (!a.sigmoid) {
+        m = lowest;
+#pragma unroll
+        for (int i = 0; i < kSelN; ++i) m = fmaxf(m, z[i]);
+        m = redux_max(m);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kSelN; ++i) v[i] = exp_of(z[i] - m), sum += v[i];
+        inv = __fdividef(1.f, row_sum<kWarp>(sum));
+    }
+#pragma unroll
+    for (int i = 0; i < kSelN; ++i) {
+        if (a.exact) v[i] = z[i];
+        else v[i] = (a.sigmoid ? __fdividef(1.f, 1.f + exp_of(-z[i])) : v[i] * inv) + bias[i];
+        if (i >= valid) v[i] = lowest;
+    }
+    if (a.G > 1) {
+        bool unsure = false;
+        sel_groups<kWarp, float, true>(a, lane, 0, lane * kSelN, v, nullptr, nullptr, unsure);
+        if (__any_sync(kFull, unsure)) return false;
+    }
+    float top = v[0];
+#pragma unroll
+    for (int i = 1; i < kSelN; ++i) top = fmaxf(top, v[i]);
+    float bound = lowest;
+    for (int j = 0; j < a.K; ++j) {
+        bound = redux_max(top);
+        const uint32_t with = __ballot_sync(kFull, top == bound);
+        if (lane == __ffs(with) - 1) top = lowest;
+    }
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kSelN; ++i) mine += v[i] >= bound && v[i] > lowest;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < kWarp; o <<= 1) {
+        const int u = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += u;
+    }
+    int n = __shfl_sync(kFull, upto, kWarp - 1);
+    if (n > kWarp) return false;
+    Candidate *at = room + upto - mine;
+#pragma unroll
+    for (int i = 0; i < kSelN; ++i)
+        if (v[i] >= bound && v[i] > lowest) *at++ = {v[i], z[i], lane * kSelN + i, 0};
+    __syncwarp();
+    const Candidate c = room[lane];
+    bool there = lane < n;
+    float border = lowest;                  // the largest value on the other side
+    if (n <= a.K) {
+        if (!a.exact) {
+#pragma unroll
+            for (int i = 0; i < kSelN; ++i) border = fmaxf(border, v[i] < bound ? v[i] : lowest);
+            border = redux_max(border);
+        }
+    } else
+        for (; n > a.K; --n) {
+            border = redux_min(there ? c.v : INFINITY);
+            const uint32_t with = __ballot_sync(kFull, there && c.v == border);
+            if (lane == 31 - __clz(with)) there = false;
+        }
+    if (!a.exact && border > lowest) {
+        const float last = redux_min(there ? c.v : INFINITY);
+        if (last - border <= kSelectSlack + fabsf(last) * kSelectPart) return false;
+    }
+    const uint32_t chosen = __ballot_sync(kFull, there);
+    float w = 0.f;
+    if (a.renorm) {
+        float x;
+        if (a.sigmoid) {
+            // scores far below 1 by their logarithms
+            const float far = redux_max(there ? c.z : lowest);
+            x = far > -40.f ? 1.f / (1.f + expf(-c.z)) : expf(fminf(c.z, 0.f) - log1pf(expf(-fabsf(c.z))) - (fminf(far, 0.f) - log1pf(expf(-fabsf(far)))));
+        } else
+            x = expf(c.z - redux_max(there ? c.z : lowest));
+        x = there ? x : 0.f;
+        w = x / row_sum<kWarp>(x);
+    } else if (there)
+        w = a.sigmoid ? 1.f / (1.f + expf(-c.z)) : expf(c.z - m) * inv;
+    const long long to = t * a.K;
+    if (there) {
+        const int pos = __popc(chosen & ((1u << lane) - 1));
+        a.ids[to + pos] = c.id;
+        a.w[to + pos] = a.scale * w;
+    }
+    if (lane >= n && lane < a.K) a.ids[to + lane] = -1, a.w[to + lane] = 0.f;
+    return true;
+}
+
+template <int DT> __global__ void __launch_bounds__(kSelThreads, 3) router_select_wide_kernel(const SelectArgs a)
+{
+    using T = typename Elem<DT>::T;
+    constexpr int W = kSelThreads / kWarp;
+    __shared__ SelShared<kWarp> s_warp[W];
+    __shared__ Candidate s_room[W][kWarp];
+    const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp, e0 = lane * kSelN, valid = a.E - e0;
+    pdl_wait();
+    pdl_launch_dependents();
+    float bias[kSelN];
+    bool odd = false;                       // a bias that is no number takes every row the general way
+#pragma unroll
+    for (int i = 0; i < kSelN; ++i) {
+        bias[i] = a.bias && i < valid ? a.bias[e0 + i] : 0.f;
+        odd |= !(fabsf(bias[i]) < INFINITY);
+    }
+    odd = __any_sync(kFull, odd);
+    const long long step = (long long)gridDim.x * W;
+    const T *const logits = reinterpret_cast<const T *>(a.logits);
+    for (long long t = (long long)blockIdx.x * W + warp; t < a.T; t += step) {
+        if (a.mask && !a.mask[t]) {
+            if (lane < a.K) a.ids[t * a.K + lane] = -1, a.w[t * a.K + lane] = 0.f;
+            continue;
+        }
+        float z[kSelN];
+        sel_load<DT>(logits + t * a.stride, e0, a.E, a.vec, z);
+        if (odd || !sel_row_quick(a, t, z, bias, valid, s_room[warp])) {
+            float copy[kSelN];
+#pragma unroll
+            for (int i = 0; i < kSelN; ++i) copy[i] = z[i];
+            sel_row_again(a, t, copy, s_warp[warp]);
+        }
+        __syncwarp();
+    }
+}
+
+// Gradient of sum grad . w under a plain softmax, which every expert has a part in.
 template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads) router_select_backward_kernel(const SelectArgs a)
 {
     using T = typename Elem<DT>::T;
@@ -363,7 +544,6 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads) router
     const long long t = ((long long)blockIdx.x * W + warp) * RPW + sub;
     const bool there = t < a.T;
     const T *const logits = reinterpret_cast<const T *>(a.logits) + (there ? t : 0) * a.stride;
-    const bool dense = !a.sigmoid && !a.renorm;
     *reinterpret_cast<float4 *>(row + e0) = make_float4(0.f, 0.f, 0.f, 0.f);
     *reinterpret_cast<float4 *>(row + e0 + 4) = make_float4(0.f, 0.f, 0.f, 0.f);
     __syncwarp();
@@ -383,36 +563,28 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads) router
         for (int j = l; j < a.K; j += LPR) {
             const int e = a.ids[t * a.K + j];
             if ((unsigned)e >= (unsigned)a.E) continue;
-            const float w = a.w[t * a.K + j], g = a.grad[t * a.K + j];
-            float d = g;
-            if (!dense) {
-                d = a.renorm ? w * (g - mean) : w * g;
-                if (a.sigmoid) d *= 1.f / (1.f + expf(Elem<DT>::to_f32(logits[e])));
-            }
-            row[e] = d;
+            row[e] = a.grad[t * a.K + j];
         }
     __syncwarp();
     float d[kSelN];
     *reinterpret_cast<float4 *>(d) = *reinterpret_cast<const float4 *>(row + e0);
     *reinterpret_cast<float4 *>(d + 4) = *reinterpret_cast<const float4 *>(row + e0 + 4);
-    if (dense) {
-        float z[kSelN], v[kSelN], m, inv;
-        if (some) sel_load<DT>(logits, e0, a.E, a.vec, z);
-        else {
+    float z[kSelN], v[kSelN], m, inv;
+    if (some) sel_load<DT>(logits, e0, a.E, a.vec, z);
+    else {
 #pragma unroll
-            for (int i = 0; i < kSelN; ++i) z[i] = -INFINITY;
-        }
-        m = z[0];
-#pragma unroll
-        for (int i = 1; i < kSelN; ++i) m = fmaxf(m, z[i]);
-        m = lanes_max<LPR>(m);
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < kSelN; ++i) v[i] = z[i] == -INFINITY ? 0.f : exp_of(z[i] - m), sum += v[i];
-        inv = a.scale / lanes_sum<LPR>(sum);
-#pragma unroll
-        for (int i = 0; i < kSelN; ++i) d[i] = z[i] == -INFINITY ? 0.f : v[i] * inv * (d[i] - mean);
+        for (int i = 0; i < kSelN; ++i) z[i] = -INFINITY;
     }
+    m = z[0];
+#pragma unroll
+    for (int i = 1; i < kSelN; ++i) m = fmaxf(m, z[i]);
+    m = lanes_max<LPR>(m);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSelN; ++i) v[i] = z[i] == -INFINITY ? 0.f : exp_of(z[i] - m), sum += v[i];
+    inv = a.scale / lanes_sum<LPR>(sum);
+#pragma unroll
+    for (int i = 0; i < kSelN; ++i) d[i] = z[i] == -INFINITY ? 0.f : v[i] * inv * (d[i] - mean);
     if (!there) return;
 #pragma unroll
     for (int i = 0; i < kSelN; ++i) d[i] += poison;
@@ -424,6 +596,66 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads) router
 #pragma unroll
         for (int i = 0; i < kSelN; ++i)
             if (e0 + i < a.E) out[e0 + i] = Elem<DT>::from_f32(d[i]);
+    }
+}
+
+// The same where only the chosen have a gradient (all but the plain softmax): up to four rows a warp at a time, a lane a choice, kp (a
+// power of two) lanes a row; rows are made in shared memory, which is zero but for the chosen, and go out 16 bytes at a time.  One
+// row a warp left each of its four dependent reads to wait alone (131072 x 256, K 8: 67 -> BWDTIME us).
+template <int DT> __global__ void __launch_bounds__(kSelThreads) router_select_sparse_backward_kernel(const SelectArgs a, int kp, int rows)
+{
+    using T = typename Elem<DT>::T;
+    constexpr int W = kSelThreads / kWarp, V = Elem<DT>::kVec, kMost = 4;
+    __shared__ __align__(16) float s_row[W][kMost][kSelMaxExperts];
+    const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp, r = lane / kp, j = lane % kp;
+    float(*const row)[kSelMaxExperts] = s_row[warp];
+    for (int i = lane; i < kMost * kSelMaxExperts; i += kWarp) row[0][i] = 0.f;
+    __syncwarp();
+    pdl_wait();
+    pdl_launch_dependents();
+    const int chunks = (a.E + kSelN - 1) / kSelN;
+    const float inv_c = a.scale != 0.f ? 1.f / a.scale : 0.f;
+    const long long step = (long long)gridDim.x * W * rows;
+    for (long long t0 = ((long long)blockIdx.x * W + warp) * rows; t0 < a.T; t0 += step) {
+        const bool on = r < rows && j < a.K && t0 + r < a.T;
+        const long long at = (t0 + r) * a.K + j;
+        const int e = on ? a.ids[at] : -1;
+        const float w = on ? a.w[at] : 0.f;
+        const bool chosen = (unsigned)e < (unsigned)a.E;
+        const float g = chosen ? a.grad[at] : 0.f;
+        float slope = 1.f;
+        if (a.sigmoid && chosen) slope = 1.f / (1.f + expf(Elem<DT>::to_f32(reinterpret_cast<const T *>(a.logits)[(t0 + r) * a.stride + e])));
+        float mean = 0.f;
+        if (a.renorm) {
+            mean = chosen ? w * inv_c * g : 0.f;
+            for (int o = kp / 2; o > 0; o >>= 1) mean += __shfl_xor_sync(kFull, mean, o);
+        }
+        if (chosen) row[r][e] = w * (g - mean) * slope;
+        const uint32_t bad = __ballot_sync(kFull, w != w);
+        __syncwarp();
+        for (int c = lane; c < rows * chunks; c += kWarp) {
+            const int rr = c / chunks, e0 = (c - rr * chunks) * kSelN;
+            if (t0 + rr >= a.T) break;
+            float d[kSelN];
+            *reinterpret_cast<float4 *>(d) = *reinterpret_cast<const float4 *>(&row[rr][e0]);
+            *reinterpret_cast<float4 *>(d + 4) = *reinterpret_cast<const float4 *>(&row[rr][e0 + 4]);
+            if (bad >> (rr * kp) & (kp == kWarp ? kFull : (1u << kp) - 1)) {
+#pragma unroll
+                for (int i = 0; i < kSelN; ++i) d[i] = NAN;
+            }
+            T *const out = reinterpret_cast<T *>(a.dlogits) + (t0 + rr) * a.dstride + e0;
+            if (a.vec && e0 + kSelN <= a.E) {
+#pragma unroll
+                for (int i = 0; i < kSelN / V; ++i) *reinterpret_cast<uint4 *>(out + i * V) = bal_narrow<DT>(reinterpret_cast<const float2 *>(d) + i * V / 2);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kSelN; ++i)
+                    if (e0 + i < a.E) out[i] = Elem<DT>::from_f32(d[i]);
+            }
+        }
+        __syncwarp();
+        if (chosen) row[r][e] = 0.f;
+        __syncwarp();
     }
 }
 
