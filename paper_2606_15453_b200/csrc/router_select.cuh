@@ -22,6 +22,7 @@
 // holds 1 to 32 rows.  Choosing takes K rounds of a maximum over the row; these, not the bytes, bound it.
 #pragma once
 #include "row_utils.cuh"
+#include "tcgen05_utils.cuh"
 
 namespace stmoe_dev {
 
@@ -131,8 +132,7 @@ template <int LPR, typename F> __device__ __forceinline__ void sel_values(const 
 
 // Groups that stay; members of the others become -infinity.  near: a group of the other side of the border lies within the
 // slack.  keys, totals: the row's room in shared memory.
-// kWhole: groups are known to be 2^j whole lanes.
-template <int LPR, typename F, bool kWhole = false>
+template <int LPR, typename F>
 __device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, int e0, F (&v)[kSelN], F *keys, F *totals, bool &near)
 {
     const int gs = a.E / a.G, lg = gs / kSelN;
@@ -154,7 +154,7 @@ __device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, 
         sure += other > mine + room || (room == (F)0 && other == mine && og < g);
         maybe += og != g && (room == (F)0 ? other > mine || (other == mine && og < g) : !(other < mine - room) && other > lowest);
     };
-    if (kWhole || (gs % kSelN == 0 && (lg & (lg - 1)) == 0)) {   // a group is 2^j whole lanes
+    if (gs % kSelN == 0 && (lg & (lg - 1)) == 0) {   // a group is 2^j whole lanes
         F b1 = lowest, b2 = lowest;
 #pragma unroll
         for (int i = 0; i < kSelN; ++i) merge(b1, b2, v[i] > lowest ? v[i] : lowest, lowest);
@@ -170,33 +170,31 @@ __device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, 
         }
         return;
     }
-    if constexpr (!kWhole) {
 #pragma unroll
-        for (int i = 0; i < kSelN; ++i) keys[e0 + i] = v[i] > lowest ? v[i] : lowest;
-        __syncwarp();
-        for (int g = l; g < a.G; g += LPR) {
-            F b1 = lowest, b2 = lowest;
-            for (int i = 0; i < gs; ++i) merge(b1, b2, keys[g * gs + i], lowest);
-            totals[g] = total_of(b1, b2);
-        }
-        __syncwarp();
-        uint32_t stay = 0;
-        for (int g = l; g < a.G; g += LPR) {
-            const F mine = totals[g];
-            int sure = 0, maybe = 0;
-            for (int og = 0; og < a.G; ++og) rank_step(mine, g, totals[og], og, sure, maybe);
-            near |= mine > lowest && sure < a.top_groups && maybe >= a.top_groups;
-            if (sure < a.top_groups) stay |= 1u << g;
-        }
+    for (int i = 0; i < kSelN; ++i) keys[e0 + i] = v[i] > lowest ? v[i] : lowest;
+    __syncwarp();
+    for (int g = l; g < a.G; g += LPR) {
+        F b1 = lowest, b2 = lowest;
+        for (int i = 0; i < gs; ++i) merge(b1, b2, keys[g * gs + i], lowest);
+        totals[g] = total_of(b1, b2);
+    }
+    __syncwarp();
+    uint32_t stay = 0;
+    for (int g = l; g < a.G; g += LPR) {
+        const F mine = totals[g];
+        int sure = 0, maybe = 0;
+        for (int og = 0; og < a.G; ++og) rank_step(mine, g, totals[og], og, sure, maybe);
+        near |= mine > lowest && sure < a.top_groups && maybe >= a.top_groups;
+        if (sure < a.top_groups) stay |= 1u << g;
+    }
 #pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) stay |= __shfl_xor_sync(kFull, stay, o);
-        __syncwarp();   // the room is written again for the next choice
-        int g = e0 / gs, left = gs - e0 % gs;
+    for (int o = LPR / 2; o > 0; o >>= 1) stay |= __shfl_xor_sync(kFull, stay, o);
+    __syncwarp();   // the room is written again for the next choice
+    int g = e0 / gs, left = gs - e0 % gs;
 #pragma unroll
-        for (int i = 0; i < kSelN; ++i) {
-            if (e0 + i < a.E && !(stay >> g & 1)) v[i] = lowest;
-            if (--left == 0) ++g, left = gs;
-        }
+    for (int i = 0; i < kSelN; ++i) {
+        if (e0 + i < a.E && !(stay >> g & 1)) v[i] = lowest;
+        if (--left == 0) ++g, left = gs;
     }
 }
 
@@ -369,6 +367,13 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads, 4) rou
 // highest index first).  Rows that hold an infinity or a NaN, rows with more than 32 values at the bound and rows that have to
 // look twice at their border go the general way (131072 x 256, 8 groups, K 8: 259 -> SELTIME us).
 
+// 1 / x for 1 <= x <= infinity, to 2^-23
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float redux_max(float v)
 {
     float r;
@@ -382,51 +387,75 @@ __device__ __forceinline__ float redux_min(float v)
     return r;
 }
 
-__device__ __noinline__ void sel_row_again(const SelectArgs &a, long long t, const float *zp, SelShared<kWarp> &s)
-{
-    float z[kSelN];
-#pragma unroll
-    for (int i = 0; i < kSelN; ++i) z[i] = zp[i];
-    __syncwarp();
-    sel_row<kWarp>(a, t, z, threadIdx.x % kWarp, 0, s);
-    __syncwarp();
-}
+constexpr int kSelLater = INT32_MIN;    // in place of a row's first id
 
-struct Candidate {
+struct __align__(16) Candidate {
     float v, z;
     int id, pad;
 };
 
-// false: the general way
-__device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, const float (&z)[kSelN], const float (&bias)[kSelN], int valid, Candidate *room)
+// Members of groups that do not stay become -infinity; false where a group's rank is within the error.  A group is lg (2^j) whole lanes.
+__device__ __forceinline__ bool sel_groups_quick(const SelectArgs &a, int lane, float (&v)[kSelN])
+{
+    const int lg = a.E / a.G / kSelN, all = a.E / kSelN;
+    float hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hi[i] = fmaxf(v[2 * i], v[2 * i + 1]), lo[i] = fminf(v[2 * i], v[2 * i + 1]);
+    auto merge = [](float &b1, float &b2, float o1, float o2) {
+        b2 = fmaxf(fminf(b1, o1), fmaxf(b2, o2));
+        b1 = fmaxf(b1, o1);
+    };
+    merge(hi[0], lo[0], hi[1], lo[1]), merge(hi[2], lo[2], hi[3], lo[3]), merge(hi[0], lo[0], hi[2], lo[2]);
+    for (int o = 1; o < lg; o <<= 1) merge(hi[0], lo[0], __shfl_xor_sync(kFull, hi[0], o), __shfl_xor_sync(kFull, lo[0], o));
+    const float mine = a.best == 1 ? hi[0] : hi[0] + lo[0], room = a.exact ? 0.f : 2 * kSelectSlack + fabsf(mine) * kSelectPart;
+    const float above = mine + room, below = mine - room;
+    int sure = 0, maybe = 0, at = lane;
+    for (int g = 1; g < a.G; ++g) {
+        at += lg;
+        if (at >= all) at -= all;
+        const float other = __shfl_sync(kFull, mine, at & (kWarp - 1));
+        sure += other > above || (room == 0.f && other == mine && at < lane);
+        maybe += other >= below;
+    }
+    const bool out = sure >= a.top_groups;
+    if (__any_sync(kFull, lane < all && !a.exact && !out && maybe >= a.top_groups)) return false;
+    if (out) {
+#pragma unroll
+        for (int i = 0; i < kSelN; ++i) v[i] = -INFINITY;
+    }
+    return true;
+}
+
+// false: the general way.  bias: -infinity behind the last expert, where z is the lowest finite number.
+__device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, const float (&z)[kSelN], const float (&bias)[kSelN], Candidate *room)
 {
     const int lane = threadIdx.x % kWarp;
     const float lowest = -INFINITY;
     float v[kSelN], m = 0.f, inv = 0.f, probe = 0.f;
 #pragma unroll
-    for (int i = 0; i < kSelN; ++i) probe = fmaf(i < valid ? z[i] : 0.f, 0.f, probe);
+    for (int i = 0; i < kSelN; ++i) probe = fmaf(z[i], 0.f, probe);
     if (__any_sync(kFull, probe != 0.f)) return false;          // an infinity or a NaN
     if (!a.sigmoid) {
-        m = lowest;
+        m = z[0];
 #pragma unroll
-        for (int i = 0; i < kSelN; ++i) m = fmaxf(m, z[i]);
+        for (int i = 1; i < kSelN; ++i) m = fmaxf(m, z[i]);
         m = redux_max(m);
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < kSelN; ++i) v[i] = exp_of(z[i] - m), sum += v[i];
         inv = __fdividef(1.f, row_sum<kWarp>(sum));
     }
+    if (a.exact) {
 #pragma unroll
-    for (int i = 0; i < kSelN; ++i) {
-        if (a.exact) v[i] = z[i];
-        else v[i] = (a.sigmoid ? __fdividef(1.f, 1.f + exp_of(-z[i])) : v[i] * inv) + bias[i];
-        if (i >= valid) v[i] = lowest;
+        for (int i = 0; i < kSelN; ++i) v[i] = z[i] + bias[i];
+    } else if (a.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < kSelN; ++i) v[i] = rcp(1.f + ex2(z[i] * -kLog2e)) + bias[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kSelN; ++i) v[i] = fmaf(v[i], inv, bias[i]);
     }
-    if (a.G > 1) {
-        bool unsure = false;
-        sel_groups<kWarp, float, true>(a, lane, 0, lane * kSelN, v, nullptr, nullptr, unsure);
-        if (__any_sync(kFull, unsure)) return false;
-    }
+    if (a.G > 1 && !sel_groups_quick(a, lane, v)) return false;
     float top = v[0];
 #pragma unroll
     for (int i = 1; i < kSelN; ++i) top = fmaxf(top, v[i]);
@@ -436,9 +465,10 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
         const uint32_t with = __ballot_sync(kFull, top == bound);
         if (lane == __ffs(with) - 1) top = lowest;
     }
+    bound = fmaxf(bound, -3.402823466e38f);                     // fewer lanes than K with a value: all values
     int mine = 0;
 #pragma unroll
-    for (int i = 0; i < kSelN; ++i) mine += v[i] >= bound && v[i] > lowest;
+    for (int i = 0; i < kSelN; ++i) mine += v[i] >= bound;
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < kWarp; o <<= 1) {
@@ -447,26 +477,31 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
     }
     int n = __shfl_sync(kFull, upto, kWarp - 1);
     if (n > kWarp) return false;
-    Candidate *at = room + upto - mine;
+    uint32_t at = dsmem_u32(room + upto - mine);
 #pragma unroll
     for (int i = 0; i < kSelN; ++i)
-        if (v[i] >= bound && v[i] > lowest) *at++ = {v[i], z[i], lane * kSelN + i, 0};
+        asm volatile(
+            "{.reg .pred p;\n\t"
+            "setp.ge.f32 p, %1, %4;\n\t"
+            "@p st.shared.v4.b32 [%0], {%5, %6, %3, %3};\n\t"
+            "@p add.u32 %0, %0, 16;}"
+            : "+r"(at) : "f"(v[i]), "f"(z[i]), "r"(lane * kSelN + i), "f"(bound), "r"(__float_as_uint(v[i])), "r"(__float_as_uint(z[i])) : "memory");
     __syncwarp();
     const Candidate c = room[lane];
     bool there = lane < n;
-    float border = lowest;                  // the largest value on the other side
-    if (n <= a.K) {
-        if (!a.exact) {
-#pragma unroll
-            for (int i = 0; i < kSelN; ++i) border = fmaxf(border, v[i] < bound ? v[i] : lowest);
-            border = redux_max(border);
-        }
-    } else
-        for (; n > a.K; --n) {
+    float border = lowest;                                      // the largest value on the other side
+    if (n > a.K) {
+        for (int left = n; left > a.K; --left) {
             border = redux_min(there ? c.v : INFINITY);
             const uint32_t with = __ballot_sync(kFull, there && c.v == border);
             if (lane == 31 - __clz(with)) there = false;
         }
+        n = a.K;
+    } else if (!a.exact) {
+#pragma unroll
+        for (int i = 0; i < kSelN; ++i) border = fmaxf(border, v[i] < bound ? v[i] : lowest);
+        border = redux_max(border);
+    }
     if (!a.exact && border > lowest) {
         const float last = redux_min(there ? c.v : INFINITY);
         if (last - border <= kSelectSlack + fabsf(last) * kSelectPart) return false;
@@ -474,13 +509,11 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
     const uint32_t chosen = __ballot_sync(kFull, there);
     float w = 0.f;
     if (a.renorm) {
+        const float far = redux_max(there ? c.z : lowest);
         float x;
-        if (a.sigmoid) {
-            // scores far below 1 by their logarithms
-            const float far = redux_max(there ? c.z : lowest);
-            x = far > -40.f ? 1.f / (1.f + expf(-c.z)) : expf(fminf(c.z, 0.f) - log1pf(expf(-fabsf(c.z))) - (fminf(far, 0.f) - log1pf(expf(-fabsf(far)))));
-        } else
-            x = expf(c.z - redux_max(there ? c.z : lowest));
+        if (!a.sigmoid) x = expf(c.z - far);
+        else if (far > -40.f) x = 1.f / (1.f + expf(-c.z));
+        else x = expf(fminf(c.z, 0.f) - log1pf(expf(-fabsf(c.z))) - far);      // scores far below 1: by their logarithms
         x = there ? x : 0.f;
         w = x / row_sum<kWarp>(x);
     } else if (there)
@@ -498,35 +531,64 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
 template <int DT> __global__ void __launch_bounds__(kSelThreads, 3) router_select_wide_kernel(const SelectArgs a)
 {
     using T = typename Elem<DT>::T;
-    constexpr int W = kSelThreads / kWarp;
+    constexpr int W = kSelThreads / kWarp, V = Elem<DT>::kVec;
     __shared__ SelShared<kWarp> s_warp[W];
     __shared__ Candidate s_room[W][kWarp];
     const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp, e0 = lane * kSelN, valid = a.E - e0;
+    const bool whole = a.vec && valid >= kSelN;
     pdl_wait();
     pdl_launch_dependents();
     float bias[kSelN];
     bool odd = false;                       // a bias that is no number takes every row the general way
 #pragma unroll
     for (int i = 0; i < kSelN; ++i) {
-        bias[i] = a.bias && i < valid ? a.bias[e0 + i] : 0.f;
-        odd |= !(fabsf(bias[i]) < INFINITY);
+        bias[i] = i >= valid ? -INFINITY : a.bias ? a.bias[e0 + i] : 0.f;
+        odd |= i < valid && !(fabsf(bias[i]) < INFINITY);
     }
     odd = __any_sync(kFull, odd);
     const long long step = (long long)gridDim.x * W;
-    const T *const logits = reinterpret_cast<const T *>(a.logits);
-    for (long long t = (long long)blockIdx.x * W + warp; t < a.T; t += step) {
-        if (a.mask && !a.mask[t]) {
+    const T *const logits = reinterpret_cast<const T *>(a.logits) + e0;
+    auto counts = [&](long long t) { return t < a.T && (!a.mask || a.mask[t]); };
+    // 16-byte pieces of the row after the one in work
+    uint4 ahead[kSelN / V];
+    auto ask = [&](long long t, bool on) {
+#pragma unroll
+        for (int g = 0; g < kSelN / V; ++g)
+            if (on && whole) ahead[g] = ld_stream16(logits + t * a.stride + g * V);
+    };
+    long long t = (long long)blockIdx.x * W + warp;
+    bool later = false;                     // rows that were marked for the general way, which would cost the loop its registers
+    bool on = counts(t);
+    ask(t, on);
+    for (; t < a.T; t += step) {
+        const bool row = on;
+        float z[kSelN];
+        if (row && whole) {
+#pragma unroll
+            for (int g = 0; g < kSelN / V; ++g) bal_widen<DT>(ahead[g], reinterpret_cast<float2 *>(z) + g * V / 2);
+        } else if (row) {
+#pragma unroll
+            for (int i = 0; i < kSelN; ++i) z[i] = i < valid ? Elem<DT>::to_f32(logits[t * a.stride + i]) : -3.402823466e38f;
+        }
+        on = counts(t + step);
+        ask(t + step, on);
+        if (!row) {
             if (lane < a.K) a.ids[t * a.K + lane] = -1, a.w[t * a.K + lane] = 0.f;
             continue;
         }
-        float z[kSelN];
-        sel_load<DT>(logits + t * a.stride, e0, a.E, a.vec, z);
-        if (odd || !sel_row_quick(a, t, z, bias, valid, s_room[warp])) {
-            float copy[kSelN];
-#pragma unroll
-            for (int i = 0; i < kSelN; ++i) copy[i] = z[i];
-            sel_row_again(a, t, copy, s_warp[warp]);
+        if (odd || !sel_row_quick(a, t, z, bias, s_room[warp])) {
+            if (lane == 0) a.ids[t * a.K] = kSelLater;
+            later = true;
         }
+        __syncwarp();
+    }
+    if (!later) return;
+    for (t = (long long)blockIdx.x * W + warp; t < a.T; t += step) {
+        if (*(volatile int *)&a.ids[t * a.K] != kSelLater) continue;
+        float z[kSelN];
+        sel_load<DT>(logits - e0 + t * a.stride, e0, a.E, a.vec, z);
+        __syncwarp();                       // all have seen the mark
+        sel_row<kWarp>(a, t, z, lane, 0, s_warp[warp]);
         __syncwarp();
     }
 }
