@@ -21,6 +21,8 @@
 // 2^j lanes share a row, eight neighbouring logits each, so a row is read once, 16 bytes at a time, and a warp
 // holds 1 to 32 rows.  Choosing takes K rounds of a maximum over the row; these, not the bytes, bound it.
 #pragma once
+#include <cstddef>
+
 #include "row_utils.cuh"
 #include "tcgen05_utils.cuh"
 
@@ -374,6 +376,12 @@ __device__ __forceinline__ float rcp(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// the same to the last place or two; 0 for infinity
+__device__ __forceinline__ float rcp_near(float x)
+{
+    const float y = rcp(x);
+    return x < INFINITY ? fmaf(y, fmaf(-x, y, 1.f), y) : 0.f;
+}
 __device__ __forceinline__ float redux_max(float v)
 {
     float r;
@@ -389,15 +397,16 @@ __device__ __forceinline__ float redux_min(float v)
 
 constexpr int kSelLater = INT32_MIN;    // in place of a row's first id
 
-struct __align__(16) Candidate {
-    float v, z;
-    int id, pad;
+struct SelRoom {
+    float z[kWarp * kSelN];     // the row
+    float v[kWarp];             // the candidates
+    int id[kWarp];
 };
 
 // Members of groups that do not stay become -infinity; false where a group's rank is within the error.  A group is lg (2^j) whole lanes.
 __device__ __forceinline__ bool sel_groups_quick(const SelectArgs &a, int lane, float (&v)[kSelN])
 {
-    const int lg = a.E / a.G / kSelN, all = a.E / kSelN;
+    const int lg = a.E / a.G / kSelN;
     float hi[4], lo[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) hi[i] = fmaxf(v[2 * i], v[2 * i + 1]), lo[i] = fminf(v[2 * i], v[2 * i + 1]);
@@ -407,19 +416,30 @@ __device__ __forceinline__ bool sel_groups_quick(const SelectArgs &a, int lane, 
     };
     merge(hi[0], lo[0], hi[1], lo[1]), merge(hi[2], lo[2], hi[3], lo[3]), merge(hi[0], lo[0], hi[2], lo[2]);
     for (int o = 1; o < lg; o <<= 1) merge(hi[0], lo[0], __shfl_xor_sync(kFull, hi[0], o), __shfl_xor_sync(kFull, lo[0], o));
-    const float mine = a.best == 1 ? hi[0] : hi[0] + lo[0], room = a.exact ? 0.f : 2 * kSelectSlack + fabsf(mine) * kSelectPart;
-    const float above = mine + room, below = mine - room;
-    int sure = 0, maybe = 0, at = lane;
-    for (int g = 1; g < a.G; ++g) {
-        at += lg;
-        if (at >= all) at -= all;
-        const float other = __shfl_sync(kFull, mine, at & (kWarp - 1));
-        sure += other > above || (room == 0.f && other == mine && at < lane);
-        maybe += other >= below;
+    float mine = a.best == 1 ? hi[0] : hi[0] + lo[0];
+    // the groups that stay, or those that go, whichever are fewer, one after the other; equal ones: the lower index stays
+    const bool group = lane < a.E / kSelN, adding = 2 * a.top_groups <= a.G;
+    bool stays = !adding;
+    float last, next;           // on either side of the border
+    if (adding) {
+        if (!group) mine = -INFINITY;
+        for (int j = 0; j < a.top_groups; ++j) {
+            last = redux_max(mine);
+            const int first = __ffs(__ballot_sync(kFull, mine == last)) - 1;
+            if ((lane ^ first) < lg) stays = true, mine = -INFINITY;
+        }
+        next = redux_max(mine);
+    } else {
+        if (!group) mine = INFINITY;
+        for (int j = a.top_groups; j < a.G; ++j) {
+            next = redux_min(mine);
+            const int first = 31 - __clz(__ballot_sync(kFull, mine == next));
+            if ((lane ^ first) < lg) stays = false, mine = INFINITY;
+        }
+        last = redux_min(mine);
     }
-    const bool out = sure >= a.top_groups;
-    if (__any_sync(kFull, lane < all && !a.exact && !out && maybe >= a.top_groups)) return false;
-    if (out) {
+    if (!a.exact && last - next <= 2 * kSelectSlack + fabsf(last) * kSelectPart) return false;
+    if (!stays) {
 #pragma unroll
         for (int i = 0; i < kSelN; ++i) v[i] = -INFINITY;
     }
@@ -427,7 +447,7 @@ __device__ __forceinline__ bool sel_groups_quick(const SelectArgs &a, int lane, 
 }
 
 // false: the general way.  bias: -infinity behind the last expert, where z is the lowest finite number.
-__device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, const float (&z)[kSelN], const float (&bias)[kSelN], Candidate *room)
+__device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, const float (&z)[kSelN], const float (&bias)[kSelN], SelRoom &room)
 {
     const int lane = threadIdx.x % kWarp;
     const float lowest = -INFINITY;
@@ -477,23 +497,28 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
     }
     int n = __shfl_sync(kFull, upto, kWarp - 1);
     if (n > kWarp) return false;
-    uint32_t at = dsmem_u32(room + upto - mine);
+    uint32_t at = dsmem_u32(room.v + upto - mine);
 #pragma unroll
     for (int i = 0; i < kSelN; ++i)
         asm volatile(
             "{.reg .pred p;\n\t"
-            "setp.ge.f32 p, %1, %4;\n\t"
-            "@p st.shared.v4.b32 [%0], {%5, %6, %3, %3};\n\t"
-            "@p add.u32 %0, %0, 16;}"
-            : "+r"(at) : "f"(v[i]), "f"(z[i]), "r"(lane * kSelN + i), "f"(bound), "r"(__float_as_uint(v[i])), "r"(__float_as_uint(z[i])) : "memory");
+            "setp.ge.f32 p, %1, %3;\n\t"
+            "@p st.shared.f32 [%0], %1;\n\t"
+            "@p st.shared.b32 [%0+%4], %2;\n\t"
+            "@p add.u32 %0, %0, 4;}"
+            : "+r"(at) : "f"(v[i]), "r"(lane * kSelN + i), "f"(bound), "n"(offsetof(SelRoom, id) - offsetof(SelRoom, v)) : "memory");
+    *reinterpret_cast<float4 *>(room.z + lane * kSelN) = make_float4(z[0], z[1], z[2], z[3]);
+    *reinterpret_cast<float4 *>(room.z + lane * kSelN + 4) = make_float4(z[4], z[5], z[6], z[7]);
     __syncwarp();
-    const Candidate c = room[lane];
+    const float cv = room.v[lane];
+    const int id = room.id[lane] & (kWarp * kSelN - 1);          // behind the n-th: what an earlier row left
+    const float cz = room.z[id];
     bool there = lane < n;
     float border = lowest;                                      // the largest value on the other side
     if (n > a.K) {
         for (int left = n; left > a.K; --left) {
-            border = redux_min(there ? c.v : INFINITY);
-            const uint32_t with = __ballot_sync(kFull, there && c.v == border);
+            border = redux_min(there ? cv : INFINITY);
+            const uint32_t with = __ballot_sync(kFull, there && cv == border);
             if (lane == 31 - __clz(with)) there = false;
         }
         n = a.K;
@@ -503,25 +528,25 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
         border = redux_max(border);
     }
     if (!a.exact && border > lowest) {
-        const float last = redux_min(there ? c.v : INFINITY);
+        const float last = redux_min(there ? cv : INFINITY);
         if (last - border <= kSelectSlack + fabsf(last) * kSelectPart) return false;
     }
     const uint32_t chosen = __ballot_sync(kFull, there);
     float w = 0.f;
     if (a.renorm) {
-        const float far = redux_max(there ? c.z : lowest);
+        const float far = redux_max(there ? cz : lowest);
         float x;
-        if (!a.sigmoid) x = expf(c.z - far);
-        else if (far > -40.f) x = 1.f / (1.f + expf(-c.z));
-        else x = expf(fminf(c.z, 0.f) - log1pf(expf(-fabsf(c.z))) - far);      // scores far below 1: by their logarithms
+        if (!a.sigmoid) x = expf(cz - far);
+        else if (far > -40.f) x = rcp_near(1.f + expf(-cz));
+        else x = expf(fminf(cz, 0.f) - log1pf(expf(-fabsf(cz))) - far);      // scores far below 1: by their logarithms
         x = there ? x : 0.f;
-        w = x / row_sum<kWarp>(x);
+        w = x * rcp_near(row_sum<kWarp>(x));
     } else if (there)
-        w = a.sigmoid ? 1.f / (1.f + expf(-c.z)) : expf(c.z - m) * inv;
+        w = a.sigmoid ? rcp_near(1.f + expf(-cz)) : expf(cz - m) * inv;
     const long long to = t * a.K;
     if (there) {
         const int pos = __popc(chosen & ((1u << lane) - 1));
-        a.ids[to + pos] = c.id;
+        a.ids[to + pos] = id;
         a.w[to + pos] = a.scale * w;
     }
     if (lane >= n && lane < a.K) a.ids[to + lane] = -1, a.w[to + lane] = 0.f;
@@ -533,7 +558,7 @@ template <int DT> __global__ void __launch_bounds__(kSelThreads, 3) router_selec
     using T = typename Elem<DT>::T;
     constexpr int W = kSelThreads / kWarp, V = Elem<DT>::kVec;
     __shared__ SelShared<kWarp> s_warp[W];
-    __shared__ Candidate s_room[W][kWarp];
+    __shared__ __align__(16) SelRoom s_room[W];
     const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp, e0 = lane * kSelN, valid = a.E - e0;
     const bool whole = a.vec && valid >= kSelN;
     pdl_wait();
