@@ -26,11 +26,11 @@ template <int DT, int LPR> int launch(bool backward, const SelectArgs &a, cudaSt
     void (*kernel)(SelectArgs) = backward ? router_select_backward_kernel<DT, LPR> : router_select_kernel<DT, LPR>;
     return launch_behind(kernel, (int)(((int64_t)a.T + rows - 1) / rows), kSelThreads, 0, 1, st, a);
 }
-// A warp a row, in turns: three CTAs an SM, as the kernel's registers allow.
+// A warp a row, in turns: four CTAs an SM, as the kernel's registers allow.
 template <int DT> int launch_wide(const SelectArgs &a, int sms, cudaStream_t st)
 {
     const int64_t ctas = ((int64_t)a.T + kSelThreads / kWarp - 1) / (kSelThreads / kWarp);
-    return launch_behind(router_select_wide_kernel<DT>, (int)std::min<int64_t>(ctas, sms * 3), kSelThreads, 0, 1, st, a);
+    return launch_behind(router_select_wide_kernel<DT>, (int)std::min<int64_t>(ctas, sms * 4), kSelThreads, 0, 1, st, a);
 }
 // whether groups are whole lanes of a row of LPR = 32
 bool whole_groups(const SelectArgs &a)

@@ -553,7 +553,7 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
     return true;
 }
 
-template <int DT> __global__ void __launch_bounds__(kSelThreads, 3) router_select_wide_kernel(const SelectArgs a)
+template <int DT> __global__ void __launch_bounds__(kSelThreads, 4) router_select_wide_kernel(const SelectArgs a)
 {
     using T = typename Elem<DT>::T;
     constexpr int W = kSelThreads / kWarp, V = Elem<DT>::kVec;
