@@ -22,16 +22,30 @@ bool rows_ok(const void *p, int dtype, int64_t stride, int64_t rows, int64_t col
 }
 bool rows_vec(const void *p, int dtype, int64_t stride) { return ((uintptr_t)p & 15) == 0 && stride * elem_bytes(dtype) % 16 == 0; }
 
+// Pieces of 256 columns that a warp has: four, or one where that would leave SMs without work (fewer than a wave of 148 x 8 CTAs)
+int64_t combine_parts(int64_t tokens, int64_t cols, int pieces) { return tokens * ((cols + pieces * 8 * kWarp - 1) / (pieces * 8 * kWarp)); }
+int combine_pieces(int64_t tokens, int64_t cols) { return combine_parts(tokens, cols, 4) >= 148 * 8 * (kRowThreads / kWarp) ? 4 : 1; }
+
 template <int DY, int DO> int launch_combine(const CombineArgs &a, cudaStream_t st)
 {
     const int64_t threads = (int64_t)a.T * a.parts * kWarp;
-    return launch_behind(combine_rows_kernel<DY, DO>, (int)((threads + kRowThreads - 1) / kRowThreads), kRowThreads, 0, 1, st, a);
+    const int ctas = (int)((threads + kRowThreads - 1) / kRowThreads);
+    if (combine_pieces(a.T, a.C) == 4) return launch_behind(combine_rows_kernel<DY, DO, 4>, ctas, kRowThreads, 0, 1, st, a);
+    return launch_behind(combine_rows_kernel<DY, DO, 1>, ctas, kRowThreads, 0, 1, st, a);
 }
+template <int DY, int DG, int WPT> int launch_combine_backward_of(const CombineArgs &a, cudaStream_t st)
+{
+    constexpr int kTokens = kRowThreads / kWarp / WPT;
+    const int ctas = (a.T + kTokens - 1) / kTokens;
+    if (a.K <= 2) return launch_behind(combine_rows_backward_kernel<DY, DG, WPT, 2>, ctas, kRowThreads, 0, 1, st, a);
+    return launch_behind(combine_rows_backward_kernel<DY, DG, WPT, 4>, ctas, kRowThreads, 0, 1, st, a);
+}
+// A CTA a token where rows are long or tokens few, else a warp.
 template <int DY, int DG> int launch_combine_backward(const CombineArgs &a, cudaStream_t st)
 {
     constexpr int kWarps = kRowThreads / kWarp;
-    if (a.parts > 1) return launch_behind(combine_rows_backward_kernel<DY, DG, kWarps>, a.T, kRowThreads, 0, 1, st, a);
-    return launch_behind(combine_rows_backward_kernel<DY, DG, 1>, (a.T + kWarps - 1) / kWarps, kRowThreads, 0, 1, st, a);
+    if (a.C > 4 * 8 * kWarp || (a.C > 8 * kWarp && a.T < 148 * 8)) return launch_combine_backward_of<DY, DG, kWarps>(a, st);
+    return launch_combine_backward_of<DY, DG, 1>(a, st);
 }
 template <bool backward, int DY, int DO> int launch_as(const CombineArgs &a, cudaStream_t st)
 {
@@ -134,7 +148,7 @@ int stmoe_combine_rows(const void *y, int y_dtype, int64_t y_stride, int64_t y_r
     a.y = y, a.y_stride = y_stride, a.y_rows = (int)y_rows, a.slots = slots, a.w = w, a.res = residual, a.res_stride = residual_stride;
     a.scale = scale, a.T = (int)tokens, a.K = top_k, a.C = (int)cols, a.out = out, a.out_stride = out_stride;
     a.vec = rows_vec(y, y_dtype, y_stride) && rows_vec(out, out_dtype, out_stride) && (!residual || rows_vec(residual, out_dtype, residual_stride));
-    a.parts = (unsigned)((cols + 8 * kWarp - 1) / (8 * kWarp));
+    a.parts = (unsigned)(combine_parts(tokens, cols, combine_pieces(tokens, cols)) / tokens);
     if ((int64_t)a.T * a.parts >= INT32_MAX) return STMOE_ERR_TOO_LARGE;
     return launch_typed<false>(y_dtype, out_dtype, a, (cudaStream_t)cuda_stream);
 }
@@ -157,7 +171,6 @@ int stmoe_combine_rows_backward(const void *grad, int grad_dtype, int64_t grad_s
     a.y = y, a.y_stride = y_stride, a.y_rows = (int)y_rows, a.slots = slots, a.w = w, a.res = grad, a.res_stride = grad_stride, a.rows = n_rows;
     a.scale = scale, a.T = (int)tokens, a.K = top_k, a.C = (int)cols, a.out = grad_y, a.out_stride = grad_y_stride, a.dw = grad_w;
     a.vec = rows_vec(y, y_dtype, y_stride) && rows_vec(grad, grad_dtype, grad_stride) && rows_vec(grad_y, y_dtype, grad_y_stride);
-    a.parts = cols > 8 * kWarp ? 2 : 1;        // a CTA a token, or a warp
     return launch_typed<true>(y_dtype, grad_dtype, a, (cudaStream_t)cuda_stream);
 }
 

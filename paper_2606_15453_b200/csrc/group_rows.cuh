@@ -217,8 +217,52 @@ struct CombineArgs {
     bool vec;               // every row is 16-byte aligned
 };
 
-// DY: type of y, DO: of the residual and the result.
-template <int DY, int DO> __global__ void __launch_bounds__(kRowThreads) combine_rows_kernel(const CombineArgs a)
+// Eight elements of a row of C to a lane: neighbours where rows are aligned (columns c + 8 lane and on), else lanes side by side (c + lane + 32 i), so
+// that a row is read in whole lines either way (2047 x 1001 fp16, 16 bytes apart element by element: 49 us both directions, now COMBINEODD).
+template <int DT> struct Lane8 {
+    static constexpr int V = Elem<DT>::kVec, G = 8 / V;
+    uint4 q[G];
+    __device__ __forceinline__ void load(const typename Elem<DT>::T *row, int c, int lane, int C, bool vec, bool on)
+    {
+        using T = typename Elem<DT>::T;
+        if (vec && c + 8 * lane + 8 <= C) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) q[g] = on ? *reinterpret_cast<const uint4 *>(row + c + 8 * lane + g * V) : make_uint4(0, 0, 0, 0);
+        } else {
+            T e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = vec ? c + 8 * lane + i : c + lane + kWarp * i;
+                e[i] = on && at < C ? row[at] : Elem<DT>::from_f32(0.f);
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g) q[g] = *reinterpret_cast<const uint4 *>(e + g * V);
+        }
+    }
+    __device__ __forceinline__ void widen(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int g = 0; g < G; ++g) bal_widen<DT>(q[g], reinterpret_cast<float2 *>(v) + g * V / 2);
+    }
+};
+template <int DT> __device__ __forceinline__ void lane_store8(typename Elem<DT>::T *row, int c, int lane, int C, bool vec, const float (&v)[8])
+{
+    constexpr int V = Elem<DT>::kVec;
+    if (vec && c + 8 * lane + 8 <= C) {
+#pragma unroll
+        for (int g = 0; g < 8 / V; ++g) *reinterpret_cast<uint4 *>(row + c + 8 * lane + g * V) = bal_narrow<DT>(reinterpret_cast<const float2 *>(v) + g * V / 2);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int at = vec ? c + 8 * lane + i : c + lane + kWarp * i;
+            if (at < C) row[at] = Elem<DT>::from_f32(v[i]);
+        }
+    }
+}
+
+// DY: type of y, DO: of the residual and the result.  A warp has J pieces of 256 columns of a token, and asks for two of its rows at a
+// time in all of them: with one piece a warp's loads were too few for its life (16384 x 4096 bf16, K 2: 120 us, now COMBINEFWD).
+template <int DY, int DO, int J> __global__ void __launch_bounds__(kRowThreads) combine_rows_kernel(const CombineArgs a)
 {
     using TY = typename Elem<DY>::T;
     using TO = typename Elem<DO>::T;
@@ -229,37 +273,49 @@ template <int DY, int DO> __global__ void __launch_bounds__(kRowThreads) combine
     const long long t = t32;
     if (t >= a.T) return;
     const TY *const y = reinterpret_cast<const TY *>(a.y);
-    const TO *const res = a.res ? reinterpret_cast<const TO *>(a.res) + t * a.res_stride : nullptr;
-    TO *const out = reinterpret_cast<TO *>(a.out) + t * a.out_stride;
     const int *const slots = a.slots + t * a.K;
-    for (int c = ((int)(task - t32 * a.parts) * kWarp + lane) * 8; c < a.C; c += (int)a.parts * kWarp * 8) {
-        float sum[8];
-        if (res) row_load8<DO>(res, c, a.C, a.vec, sum);
-        else {
+    const int first = (int)(task - t32 * a.parts) * J * kWarp * 8;
+    float sum[J][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-        }
-#pragma unroll 4
-        for (int k = 0; k < a.K; ++k) {
-            const int s = slots[k];
-            if ((unsigned)s >= (unsigned)a.y_rows) continue;
-            const float w = a.w ? a.scale * a.w[t * a.K + k] : a.scale;
-            float v[8];
-            row_load8<DY>(y + s * a.y_stride, c, a.C, a.vec, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
-        }
-        row_store8<DO>(out, c, a.C, a.vec, sum);
+    for (int j = 0; j < J; ++j) {
+        Lane8<DO> r;
+        r.load(reinterpret_cast<const TO *>(a.res) + t * a.res_stride, first + j * kWarp * 8, lane, a.C, a.vec, a.res != nullptr);
+        r.widen(sum[j]);
     }
+    for (int k = 0; k < a.K; k += 2) {
+        Lane8<DY> row[2][J];
+        float w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int s = k + i < a.K ? slots[k + i] : -1;
+            const bool there = (unsigned)s < (unsigned)a.y_rows;
+            w[i] = there ? a.w ? a.scale * a.w[t * a.K + k + i] : a.scale : 0.f;
+#pragma unroll
+            for (int j = 0; j < J; ++j) row[i][j].load(y + (there ? s : 0) * a.y_stride, first + j * kWarp * 8, lane, a.C, a.vec, there);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                float v[8];
+                row[i][j].widen(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[j][e] = fmaf(w[i], v[e], sum[j][e]);
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+        if (first + j * kWarp * 8 < a.C) lane_store8<DO>(reinterpret_cast<TO *>(a.out) + t * a.out_stride, first + j * kWarp * 8, lane, a.C, a.vec, sum[j]);
 }
 
-// WPT warps share a token (and reduce its inner products through shared memory, in a fixed order).
-template <int DY, int DG, int WPT> __global__ void __launch_bounds__(kRowThreads) combine_rows_backward_kernel(const CombineArgs a)
+// WPT warps share a token (and reduce its inner products through shared memory, in a fixed order); KB choices at a time, so that a piece of the
+// gradient is read once for them and their rows are asked for together.
+template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRowThreads) combine_rows_backward_kernel(const CombineArgs a)
 {
     using TY = typename Elem<DY>::T;
     using TG = typename Elem<DG>::T;
     constexpr int kTokens = kRowThreads / kWarp / WPT;
-    __shared__ float s_dot[kRowThreads / kWarp];
+    __shared__ float s_dot[KB][kRowThreads / kWarp];
     const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp, part = warp % WPT;
     pdl_wait();
     pdl_launch_dependents();
@@ -268,43 +324,64 @@ template <int DY, int DG, int WPT> __global__ void __launch_bounds__(kRowThreads
     const TY *const y = reinterpret_cast<const TY *>(a.y);
     TY *const dy = reinterpret_cast<TY *>(a.out);
     const TG *const g = reinterpret_cast<const TG *>(a.res) + t * a.res_stride;
-    for (int k = 0; k < a.K; ++k) {
-        const int s = a.slots[t * a.K + k];
-        const bool there = (unsigned)s < (unsigned)a.y_rows;
-        float dot = 0.f;
-        if (there) {
-            const float w = a.w ? a.scale * a.w[t * a.K + k] : a.scale;
+    for (int k = 0; k < a.K; k += KB) {
+        int s[KB];
+        float w[KB], dot[KB];
+#pragma unroll
+        for (int i = 0; i < KB; ++i) {
+            s[i] = k + i < a.K ? a.slots[t * a.K + k + i] : -1;
+            if ((unsigned)s[i] >= (unsigned)a.y_rows) s[i] = -1;
+            w[i] = s[i] < 0 ? 0.f : a.w ? a.scale * a.w[t * a.K + k + i] : a.scale;
+            dot[i] = 0.f;
+        }
 #pragma unroll 2
-            for (int c = (part * kWarp + lane) * 8; c < a.C; c += WPT * kWarp * 8) {
-                float gv[8], v[8];
-                row_load8<DG>(g, c, a.C, a.vec, gv);
-                if (a.dw) {
-                    row_load8<DY>(y + s * a.y_stride, c, a.C, a.vec, v);
+        for (int c = part * kWarp * 8; c < a.C; c += WPT * kWarp * 8) {
+            Lane8<DG> graw;
+            Lane8<DY> row[KB];
+            graw.load(g, c, lane, a.C, a.vec, true);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) dot = fmaf(gv[i], v[i], dot);
-                }
+            for (int i = 0; i < KB; ++i) row[i].load(y + (s[i] < 0 ? 0 : s[i]) * a.y_stride, c, lane, a.C, a.vec, s[i] >= 0 && a.dw);
+            float gv[8];
+            graw.widen(gv);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = w * gv[i];
-                row_store8<DY>(dy + s * a.out_stride, c, a.C, a.vec, v);
+            for (int i = 0; i < KB; ++i) {
+                float v[8];
+                row[i].widen(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dot[i] = fmaf(gv[e], v[e], dot[i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = w[i] * gv[e];
+                if (s[i] >= 0) lane_store8<DY>(dy + s[i] * a.out_stride, c, lane, a.C, a.vec, v);
             }
         }
         if (a.dw) {
-            dot = warp_sum(dot);
+#pragma unroll
+            for (int i = 0; i < KB; ++i) dot[i] = warp_sum(dot[i]);
             if (WPT > 1) {
                 __syncthreads();
-                if (lane == 0) s_dot[warp] = dot;
-                __syncthreads();
-                dot = 0.f;
+                if (lane == 0) {
 #pragma unroll
-                for (int i = 0; i < WPT; ++i) dot += s_dot[i];
+                    for (int i = 0; i < KB; ++i) s_dot[i][warp] = dot[i];
+                }
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < KB; ++i) {
+                    dot[i] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < WPT; ++j) dot[i] += s_dot[i][j];
+                }
             }
-            if (part == 0 && lane == 0) a.dw[t * a.K + k] = there ? a.scale * dot : 0.f;
+            if (part == 0 && lane == 0) {
+#pragma unroll
+                for (int i = 0; i < KB; ++i)
+                    if (k + i < a.K) a.dw[t * a.K + k + i] = s[i] >= 0 ? a.scale * dot[i] : 0.f;
+            }
         }
     }
     if (a.rows) {
         const float zero[8] = {};
         for (long long r = max(t * a.K, (long long)*a.rows); r < min((t + 1) * a.K, (long long)a.y_rows); ++r)
-            for (int c = (part * kWarp + lane) * 8; c < a.C; c += WPT * kWarp * 8) row_store8<DY>(dy + r * a.out_stride, c, a.C, a.vec, zero);
+            for (int c = part * kWarp * 8; c < a.C; c += WPT * kWarp * 8) lane_store8<DY>(dy + r * a.out_stride, c, lane, a.C, a.vec, zero);
     }
 }
 
