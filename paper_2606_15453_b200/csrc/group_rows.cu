@@ -15,7 +15,13 @@ namespace {
 bool pairs_ok(int64_t rows, int top_k) { return rows >= 0 && top_k >= 1 && rows <= INT32_MAX / top_k; }
 bool elem_ok(int dtype) { return dtype == STMOE_F32 || dtype == STMOE_BF16 || dtype == STMOE_F16; }
 int elem_bytes(int dtype) { return dtype == STMOE_F32 ? 4 : 2; }
-int group_ctas(int64_t pairs) { return (int)std::min<int64_t>(kGrpMaxCtas, (pairs + kGrpCtaPairs - 1) / kGrpCtaPairs); }
+// One CTA, a cluster of up to eight, or CTAs on their own that count in a launch before.  A CTA by itself takes 4096 pairs, one of many 1024.
+bool in_cluster(int64_t pairs) { return pairs <= kGrpCtaPairs * kGrpCluster; }
+int group_ctas(int64_t pairs)
+{
+    if (in_cluster(pairs)) return pairs <= kGrpCtaPairs ? 1 : kGrpCluster;
+    return (int)std::min<int64_t>(kGrpMaxCtas, (pairs + 1023) / 1024);
+}
 bool rows_ok(const void *p, int dtype, int64_t stride, int64_t rows, int64_t cols)
 {
     return p && elem_ok(dtype) && (rows <= 1 || stride >= cols) && ((uintptr_t)p & (elem_bytes(dtype) - 1)) == 0;
@@ -28,8 +34,8 @@ int combine_pieces(int64_t tokens, int64_t cols) { return combine_parts(tokens, 
 
 template <int DY, int DO> int launch_combine(const CombineArgs &a, cudaStream_t st)
 {
-    const int64_t threads = (int64_t)a.T * a.parts * kWarp;
-    const int ctas = (int)((threads + kRowThreads - 1) / kRowThreads);
+    constexpr int kWarps = kRowThreads / kWarp;
+    const int ctas = (int)(((int64_t)a.T * a.parts + kWarps - 1) / kWarps);
     if (combine_pieces(a.T, a.C) == 4) return launch_behind(combine_rows_kernel<DY, DO, 4>, ctas, kRowThreads, 0, 1, st, a);
     return launch_behind(combine_rows_kernel<DY, DO, 1>, ctas, kRowThreads, 0, 1, st, a);
 }
@@ -40,11 +46,11 @@ template <int DY, int DG, int WPT> int launch_combine_backward_of(const CombineA
     if (a.K <= 2) return launch_behind(combine_rows_backward_kernel<DY, DG, WPT, 2>, ctas, kRowThreads, 0, 1, st, a);
     return launch_behind(combine_rows_backward_kernel<DY, DG, WPT, 4>, ctas, kRowThreads, 0, 1, st, a);
 }
-// A CTA a token where rows are long or tokens few, else a warp.
+// Eight warps a token where rows are long, four where tokens are too few to fill the GPU's 148 x 64 warps, else one.
 template <int DY, int DG> int launch_combine_backward(const CombineArgs &a, cudaStream_t st)
 {
-    constexpr int kWarps = kRowThreads / kWarp;
-    if (a.C > 4 * 8 * kWarp || (a.C > 8 * kWarp && a.T < 148 * 8)) return launch_combine_backward_of<DY, DG, kWarps>(a, st);
+    if (a.C > 4 * 8 * kWarp) return launch_combine_backward_of<DY, DG, 8>(a, st);
+    if (a.C > 8 * kWarp && a.T < 148 * 64) return launch_combine_backward_of<DY, DG, 4>(a, st);
     return launch_combine_backward_of<DY, DG, 1>(a, st);
 }
 template <bool backward, int DY, int DO> int launch_as(const CombineArgs &a, cudaStream_t st)
@@ -67,7 +73,7 @@ size_t stmoe_group_rows_scratch_bytes(int64_t rows, int top_k, int n_groups)
 {
     if (!pairs_ok(rows, top_k) || n_groups < 1 || n_groups > kGrpMaxGroups) return 0;
     const int ctas = group_ctas(rows * top_k);
-    return ctas <= 1 ? 0 : sizeof(int) * (size_t)ctas * (n_groups + 1);
+    return in_cluster(rows * top_k) ? 0 : sizeof(int) * (size_t)ctas * (n_groups + 1);
 }
 
 int stmoe_group_rows(const int32_t *ids, int64_t rows, int top_k, int n_groups, int32_t *counts, int32_t *starts, int32_t *order,
@@ -85,20 +91,21 @@ int stmoe_group_rows(const int32_t *ids, int64_t rows, int top_k, int n_groups, 
     a.counts = counts, a.starts = starts, a.order = order, a.slots = slots;
     const int ctas = std::max(1, group_ctas(a.pairs));
     a.per_warp = (int)(((int64_t)a.pairs + (int64_t)ctas * kGrpWarps * kWarp - 1) / ((int64_t)ctas * kGrpWarps * kWarp)) * kWarp;
-    a.hist = ctas > 1 ? (int *)scratch : nullptr;
-    const int smem = (int)sizeof(int) * (kGrpWarps + 1) * (n_groups + 1);
+    const bool cluster = in_cluster(a.pairs);
+    a.hist = cluster ? nullptr : (int *)scratch;
+    const int smem = (int)sizeof(int) * (kGrpWarps + 2) * (n_groups + 1);
     static PerDevice<bool> asked;       // more than 48 KB of dynamic shared memory: asked for once per device
     bool done = false;
     if (const int rc = asked.get(dev, &done, [](bool &) {
-            const int most = (int)sizeof(int) * (kGrpWarps + 1) * (kGrpMaxGroups + 1);
+            const int most = (int)sizeof(int) * (kGrpWarps + 2) * (kGrpMaxGroups + 1);
             if (const int rc = cuda_status(cudaFuncSetAttribute(group_count_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most))) return rc;
             return cuda_status(cudaFuncSetAttribute(group_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
         }))
         return rc;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (ctas > 1)
+    if (!cluster)
         if (const int rc = launch_behind(group_count_kernel, ctas, kGrpThreads, smem, 1, st, a)) return rc;
-    return launch_behind(group_place_kernel, ctas, kGrpThreads, smem, 1, st, a);
+    return launch_behind(group_place_kernel, ctas, kGrpThreads, smem, cluster ? ctas : 1, st, a);
 }
 
 int stmoe_dispatch_rows(const void *x, int64_t row_bytes, int64_t x_stride, int64_t rows, int top_k, const int32_t *slots, const int32_t *n_rows,

@@ -9,26 +9,27 @@
 // Grouping is a counting sort.  Every warp owns a stretch of pairs and counts it into its own row of a table in
 // shared memory, 32 pairs at a time: lanes with the same id find one another, the first adds their number, so
 // neither pass has an atomic and equal ids keep their order.  Running sums down the table and across the groups
-// give each warp its place in each group, and a second walk hands the places out.  Few pairs are one CTA's
-// work; more are spread over CTAs that count in a first launch and place in a second.
+// give each warp its place in each group, and a second walk hands the places out.  Few pairs are one CTA's work, more that of a cluster, whose
+// CTAs read one another's counts from shared memory; beyond that CTAs count in a first launch and place in a second.
 //
 // The copies are HBM's work: a row of x is read once and written K times, a row of y is read once.
 #pragma once
 #include "row_utils.cuh"
+#include "tcgen05_utils.cuh"
 
 namespace stmoe_dev {
 
 constexpr int kGrpMaxGroups = 1024;
 constexpr int kGrpThreads = 512, kGrpWarps = kGrpThreads / kWarp;
-constexpr int kGrpCtaPairs = 4096;  // pairs of a CTA where there are several
-constexpr int kGrpMaxCtas = 128;
+constexpr int kGrpCtaPairs = 4096;  // pairs of a CTA of a cluster, or alone
+constexpr int kGrpCluster = 8, kGrpMaxCtas = 128;
 
 struct GroupArgs {
     const int *ids;
     int pairs, G;
     int per_warp;           // pairs of a warp, a multiple of 32
     int *counts, *starts, *order, *slots;
-    int *hist;              // [ctas][G + 1], or nullptr for one CTA
+    int *hist;              // [ctas][G + 1], or nullptr: one CTA, or the CTAs of a cluster
 };
 
 // Counts of a warp's stretch in its row of the table (columns 0..G, the last one for pairs without a group).
@@ -99,10 +100,11 @@ __global__ void __launch_bounds__(kGrpThreads) group_count_kernel(const GroupArg
 
 __global__ void __launch_bounds__(kGrpThreads) group_place_kernel(const GroupArgs a)
 {
-    extern __shared__ int table[];              // [kGrpWarps][G + 1], [G + 1] starts
+    extern __shared__ int table[];              // [kGrpWarps][G + 1], [G + 1] starts, [G + 1] own counts
     __shared__ int part[kGrpWarps];
-    const int n = a.G + 1, tid = threadIdx.x, lane = tid % kWarp, warp = tid / kWarp;
-    int *const start = table + kGrpWarps * n, *const mine = table + warp * n;
+    __shared__ int2 sums[kGrpThreads];
+    const int n = a.G + 1, tid = threadIdx.x, lane = tid % kWarp, warp = tid / kWarp, ctas = gridDim.x, me = blockIdx.x;
+    int *const start = table + kGrpWarps * n, *const own = start + n, *const mine = table + warp * n;
     for (int i = tid; i < kGrpWarps * n; i += kGrpThreads) table[i] = 0;
     __syncthreads();
     pdl_wait();
@@ -110,26 +112,57 @@ __global__ void __launch_bounds__(kGrpThreads) group_place_kernel(const GroupArg
     const int first = grp_first(a, warp), end = min(first + a.per_warp, a.pairs);
     grp_count(a, first, lane, mine);
     __syncthreads();
-    for (int g = tid; g < n; g += kGrpThreads) {
+    if (!a.hist) {
+        for (int g = tid; g < n; g += kGrpThreads) {
+            int sum = 0;
+#pragma unroll
+            for (int w = 0; w < kGrpWarps; ++w) sum += table[w * n + g];
+            own[g] = sum;
+        }
+        if (ctas > 1) cluster_sync();
+        else __syncthreads();
+    }
+    // the CTAs' counts of a column, by as many threads as there are for one
+    int share = 1;
+    while (2 * share * n <= kGrpThreads && share < 8) share *= 2;
+    const int columns = kGrpThreads / share, col = tid % columns, of = tid / columns;
+    for (int g0 = 0; g0 < n; g0 += columns) {
+        const int g = g0 + col;
         int before = 0, total = 0;              // in this group: pairs of the CTAs before this one, of all
-        if (a.hist) {
-#pragma unroll 8
-            for (int c = 0; c < (int)gridDim.x; ++c) {
-                const int h = a.hist[c * n + g];
-                before += c < (int)blockIdx.x ? h : 0;
-                total += h;
+        if (g < n) {
+            if (a.hist) {
+#pragma unroll 16
+                for (int c = of; c < ctas; c += share) {
+                    const int h = a.hist[c * n + g];
+                    before += c < me ? h : 0;
+                    total += h;
+                }
+            } else {
+                for (int c = of; c < ctas; c += share) {
+                    const int h = ctas == 1 ? own[g] : __float_as_int(ld_cluster(dsmem_u32(own + g), c));
+                    before += c < me ? h : 0;
+                    total += h;
+                }
             }
         }
-        int run = before;
-#pragma unroll
-        for (int w = 0; w < kGrpWarps; ++w) {
-            const int c = table[w * n + g];
-            table[w * n + g] = run;
-            run += c;
+        if (share > 1) {
+            __syncthreads();
+            sums[tid] = make_int2(before, total);
+            __syncthreads();
+            if (of == 0)
+                for (int i = 1; i < share; ++i) before += sums[i * columns + col].x, total += sums[i * columns + col].y;
         }
-        if (!a.hist) total = run;
-        start[g] = total;
-        if (blockIdx.x == 0 && g < a.G) a.counts[g] = total;
+        if (g < n && of == 0) {
+            int run = before;
+#pragma unroll
+            for (int w = 0; w < kGrpWarps; ++w) {
+                const int c = table[w * n + g];
+                table[w * n + g] = run;
+                run += c;
+            }
+            start[g] = total;
+            if (me == 0 && g < a.G) a.counts[g] = total;
+        }
     }
     __syncthreads();
     grp_scan(start, n, part);
@@ -146,6 +179,10 @@ __global__ void __launch_bounds__(kGrpThreads) group_place_kernel(const GroupArg
         __syncwarp();
         if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
         __syncwarp();
+    }
+    if (!a.hist && ctas > 1) {
+        __syncwarp();
+        cluster_sync();                         // nobody leaves while its counts are read
     }
 }
 
@@ -320,7 +357,7 @@ template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRo
     pdl_wait();
     pdl_launch_dependents();
     const long long t = (long long)blockIdx.x * kTokens + warp / WPT;
-    if (WPT == 1 && t >= a.T) return;           // WPT > 1: all warps of the CTA share one token
+    const bool on = t < a.T;                    // the CTA's other tokens go on to its barriers
     const TY *const y = reinterpret_cast<const TY *>(a.y);
     TY *const dy = reinterpret_cast<TY *>(a.out);
     const TG *const g = reinterpret_cast<const TG *>(a.res) + t * a.res_stride;
@@ -329,13 +366,13 @@ template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRo
         float w[KB], dot[KB];
 #pragma unroll
         for (int i = 0; i < KB; ++i) {
-            s[i] = k + i < a.K ? a.slots[t * a.K + k + i] : -1;
+            s[i] = on && k + i < a.K ? a.slots[t * a.K + k + i] : -1;
             if ((unsigned)s[i] >= (unsigned)a.y_rows) s[i] = -1;
             w[i] = s[i] < 0 ? 0.f : a.w ? a.scale * a.w[t * a.K + k + i] : a.scale;
             dot[i] = 0.f;
         }
 #pragma unroll 2
-        for (int c = part * kWarp * 8; c < a.C; c += WPT * kWarp * 8) {
+        for (int c = part * kWarp * 8; on && c < a.C; c += WPT * kWarp * 8) {
             Lane8<DG> graw;
             Lane8<DY> row[KB];
             graw.load(g, c, lane, a.C, a.vec, true);
@@ -368,17 +405,17 @@ template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRo
                 for (int i = 0; i < KB; ++i) {
                     dot[i] = 0.f;
 #pragma unroll
-                    for (int j = 0; j < WPT; ++j) dot[i] += s_dot[i][j];
+                    for (int j = 0; j < WPT; ++j) dot[i] += s_dot[i][warp - part + j];
                 }
             }
-            if (part == 0 && lane == 0) {
+            if (on && part == 0 && lane == 0) {
 #pragma unroll
                 for (int i = 0; i < KB; ++i)
                     if (k + i < a.K) a.dw[t * a.K + k + i] = s[i] >= 0 ? a.scale * dot[i] : 0.f;
             }
         }
     }
-    if (a.rows) {
+    if (a.rows && on) {
         const float zero[8] = {};
         for (long long r = max(t * a.K, (long long)*a.rows); r < min((t + 1) * a.K, (long long)a.y_rows); ++r)
             for (int c = part * kWarp * 8; c < a.C; c += WPT * kWarp * 8) lane_store8<DY>(dy + r * a.out_stride, c, lane, a.C, a.vec, zero);
