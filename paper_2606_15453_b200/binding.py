@@ -609,11 +609,16 @@ def _addr(t):
 
 
 def _wants_grad(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _is_vector(t, n, dtype, dev) -> bool:
-    return t.dtype == dtype and t.numel() == n and t.is_contiguous() and t.device == dev
+    """n contiguous elements of dtype on the CUDA device of ordinal dev."""
+    return t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.get_device() == dev
 
 
 class _RouterSelect(torch.autograd.Function):
@@ -649,7 +654,7 @@ def router_select(logits, top_k, scores="softmax", bias=None, groups=1, top_grou
     T, E = logits.shape
     if scores not in ("softmax", "sigmoid"):
         _refuse("scores: softmax or sigmoid")
-    if bias is not None and not _is_vector(bias, E, _F32, logits.device):
+    if bias is not None and not _is_vector(bias, E, _F32, logits.get_device()):
         _refuse("bias: contiguous fp32 [n_experts] on the logits' device")
     if not 1 <= top_k <= E:
         _refuse("top_k: 1 to the number of experts")
@@ -660,8 +665,9 @@ def router_select(logits, top_k, scores="softmax", bias=None, groups=1, top_grou
         ids, w, flags = _RouterSelect.apply(logits, top_k, scores, bias, groups, top_groups, group_best, renorm, scale, mask)
         return {"ids": ids, "w": w, "flags": flags, "scale": scale}
     flags = (SELECT_SIGMOID if scores == "sigmoid" else 0) | (SELECT_RENORM if renorm else 0)
-    ids = torch.empty(T, top_k, dtype=_I32, device=logits.device)
-    w = torch.empty(T, top_k, dtype=_F32, device=logits.device)
+    dev = logits.device
+    ids = torch.empty(T, top_k, dtype=_I32, device=dev)
+    w = torch.empty(T, top_k, dtype=_F32, device=dev)
     # an empty tensor has no address; nothing of it is read
     src, idp, wp = (logits.data_ptr(), ids.data_ptr(), w.data_ptr()) if T else (256, 256, 256)
     rc = lib().stmoe_router_select(src, elem, logits.stride(0), _addr(bias), _addr(mask), T, E, top_k, groups,
@@ -676,19 +682,19 @@ def router_select_backward(logits, forward, grad_w, out=None, stream=None):
     router_select returned for them; grad_w: fp32 [tokens][top_k]."""
     elem = _balance_elem(logits, None)
     T, E = logits.shape
-    ids, w, dev = forward["ids"], forward["w"], logits.device
+    ids, w, dev = forward["ids"], forward["w"], logits.get_device()
     K = ids.shape[1]
     if not (ids.shape[0] == T and _is_vector(ids, T * K, _I32, dev) and _is_vector(w, T * K, _F32, dev)):
         _refuse("forward does not belong to these logits")
     if not _is_vector(grad_w, T * K, _F32, dev):
         _refuse("grad_w: contiguous fp32 [tokens][top_k] on the logits' device")
-    if out is not None and not (_is_rows(out, logits.dtype) and out.shape == logits.shape and out.device == dev):
+    if out is not None and not (_is_rows(out, logits.dtype) and out.shape == logits.shape and out.get_device() == dev):
         _refuse("out: expected the logits' shape and type")
     st = _stream_of(logits, stream)
     if st is None:
         return _there(logits, stream, router_select_backward, logits, forward, grad_w, out)
     if out is None:
-        out = torch.empty(T, E, dtype=logits.dtype, device=dev)
+        out = torch.empty(T, E, dtype=logits.dtype, device=logits.device)
     if T:
         rc = lib().stmoe_router_select_backward(logits.data_ptr(), elem, logits.stride(0), T, E, K, forward["flags"], forward["scale"],
                                                 ids.data_ptr(), w.data_ptr(), grad_w.data_ptr(), out.data_ptr(), out.stride(0), st)
@@ -719,13 +725,13 @@ def group_rows(ids, n_groups, stream=None):
     rc = L.stmoe_group_rows(idp, T, K, n_groups, c, c + 4 * n_groups, at, at + 4 * P, at + 8 * P, n, st)
     if rc:
         _check(rc, "stmoe_group_rows")
-    return {"counts": counts, "starts": starts, "order": order, "slots": slots.view(ids.shape), "ids": ids, "groups": n_groups}
+    return {"counts": counts, "starts": starts, "order": order, "slots": slots if ids.dim() == 1 else slots.view(T, K), "ids": ids, "groups": n_groups}
 
 
 def _plan_of(plan, T, dev):
     """top_k of a plan for T rows."""
     slots = plan["slots"]
-    if slots.shape[0] != T or slots.device != dev:
+    if slots.shape[0] != T or slots.get_device() != dev:
         _refuse("the plan belongs to other rows")
     return 1 if slots.dim() == 1 else slots.shape[1]
 
@@ -748,8 +754,8 @@ def dispatch_rows(x, plan, out=None, stream=None):
     if not _is_rows(x) or x.shape[1] < 1:
         _refuse("x: expected a 2-D CUDA tensor with contiguous rows")
     T, C = x.shape
-    K = _plan_of(plan, T, x.device)
-    if out is not None and not (_is_rows(out, x.dtype) and out.shape[0] == T * K and out.shape[1] == C and out.device == x.device):
+    K = _plan_of(plan, T, x.get_device())
+    if out is not None and not (_is_rows(out, x.dtype) and out.shape[0] == T * K and out.shape[1] == C and out.get_device() == x.get_device()):
         _refuse(f"out: expected {(T * K, C)} of x's type with contiguous rows on x's device")
     if out is not None and _wants_grad(x, out):
         _refuse("out is not part of torch's graph: leave it away where x requires a gradient")
@@ -793,13 +799,14 @@ def _combine_args(y, plan, w, other, what):
     elem = _ELEM.get(y.dtype)
     if elem is None or not _is_rows(y) or y.shape[1] < 1:
         _refuse("y: expected a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows")
-    K = _plan_of(plan, T, y.device)
+    dev = y.get_device()
+    K = _plan_of(plan, T, dev)
     if y.shape[0] != T * K:
         _refuse("y has other rows than the plan")
-    if w is not None and not _is_vector(w, T * K, _F32, y.device):
+    if w is not None and not _is_vector(w, T * K, _F32, dev):
         _refuse("w: contiguous fp32 [rows][top_k] on y's device")
     for t in other:
-        if t is not None and not (_is_rows(t) and t.dtype in (y.dtype, _F32) and t.shape[0] == T and t.shape[1] == y.shape[1] and t.device == y.device):
+        if t is not None and not (_is_rows(t) and t.dtype in (y.dtype, _F32) and t.shape[0] == T and t.shape[1] == y.shape[1] and t.get_device() == dev):
             _refuse(f"{what}: expected [rows][cols] of y's type or fp32 with contiguous rows on y's device")
     return T, K, elem
 
@@ -872,18 +879,19 @@ def _lora_args(x, a, b, plan, scale, hidden):
     if not elem or not _is_rows(x) or x.shape[1] < 1:
         _refuse("x: expected a 2-D CUDA tensor of bf16 or fp16 with contiguous rows")
     T, I = x.shape
-    if a.dim() != 3 or b.dim() != 3 or a.dtype != x.dtype or b.dtype != x.dtype or a.device != x.device or b.device != x.device:
+    dev, dtype = x.get_device(), x.dtype
+    if a.dim() != 3 or b.dim() != 3 or a.dtype is not dtype or b.dtype is not dtype or a.get_device() != dev or b.get_device() != dev:
         _refuse("a [n][rank][inner] and b [n][outer][rank]: expected x's type and device")
-    n, r, O = a.shape[0], a.shape[1], b.shape[1]
-    if a.shape[2] != I or b.shape[0] != n or b.shape[2] != r or n < 1 or O < 1 or not 1 <= r <= 256:
+    (n, r, inner), (nb, O, rb) = a.shape, b.shape
+    if inner != I or nb != n or rb != r or n < 1 or O < 1 or not 1 <= r <= 256:
         _refuse("the adapters' shapes do not belong together, or rank is not in 1..256")
     if (a.stride(2) != 1 and I > 1) or (b.stride(2) != 1 and r > 1):
         _refuse("a and b: expected contiguous rows")
-    if _plan_of(plan, T, x.device) != 1 or plan["groups"] != n:
+    if _plan_of(plan, T, dev) != 1 or plan["groups"] != n:
         _refuse("plan: group_rows of ids [rows], one group an adapter")
-    if scale is not None and not _is_vector(scale, n, _F32, x.device):
+    if scale is not None and not _is_vector(scale, n, _F32, dev):
         _refuse("scale: contiguous fp32 [n] on x's device")
-    if hidden is not None and not (_is_vector(hidden, T * r, _F32, x.device)):
+    if hidden is not None and not _is_vector(hidden, T * r, _F32, dev):
         _refuse("hidden: contiguous fp32 [rows][rank] on x's device")
     return elem, T, I, n, r, O
 
@@ -896,18 +904,19 @@ def lora(x, a, b, plan, scale=None, alpha=1.0, base=None, out=None, hidden=None,
     the gradient of an fp32 result is rounded to x's type for those of x, a and b."""
     elem, T, I, n, r, O = _lora_args(x, a, b, plan, scale, hidden)
     for t in (base, out):
-        if t is not None and not (_is_rows(t) and t.dtype in (x.dtype, _F32) and t.shape[0] == T and t.shape[1] == O and t.device == x.device):
+        if t is not None and not (_is_rows(t) and t.dtype in (x.dtype, _F32) and t.shape[0] == T and t.shape[1] == O and t.get_device() == x.get_device()):
             _refuse(f"base, out: expected {(T, O)} of x's type or fp32 with contiguous rows on x's device")
     if base is not None and out is not None and base.dtype != out.dtype:
         _refuse("base and out have to be of one type")
-    if _wants_grad(x, a, b, base, out) and (out is not None or hidden is not None):
+    graph = _wants_grad(x, a, b, base, out, scale)
+    if graph and (out is not None or hidden is not None):
         _refuse("out and hidden are not part of torch's graph: leave them away where an input requires a gradient")
-    if _wants_grad(scale):
+    if graph and scale is not None and scale.requires_grad:
         _refuse("scale is held constant")
     st = _stream_of(x, stream)
     if st is None:
         return _there(x, stream, lora, x, a, b, plan, scale, alpha, base, out, hidden)
-    if _wants_grad(x, a, b, base):
+    if graph:
         return _Lora.apply(x, a, b, base, plan, scale, alpha)
     if out is None:
         out = torch.empty(T, O, dtype=x.dtype if base is None else base.dtype, device=x.device)
@@ -927,7 +936,7 @@ def lora(x, a, b, plan, scale=None, alpha=1.0, base=None, out=None, hidden=None,
 def lora_backward(grad, x, a, b, plan, hidden, scale=None, alpha=1.0, stream=None):
     """stmoe_lora_backward: gradients (of x, a, b) for grad [rows][outer] in x's type, from the hidden that lora wrote."""
     elem, T, I, n, r, O = _lora_args(x, a, b, plan, scale, hidden)
-    if not (_is_rows(grad, x.dtype) and grad.shape[0] == T and grad.shape[1] == O and grad.device == x.device):
+    if not (_is_rows(grad, x.dtype) and grad.shape[0] == T and grad.shape[1] == O and grad.get_device() == x.get_device()):
         _refuse(f"grad: expected {(T, O)} of x's type with contiguous rows on x's device")
     if hidden is None:
         _refuse("hidden: what lora wrote is needed")

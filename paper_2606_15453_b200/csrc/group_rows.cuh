@@ -14,6 +14,8 @@
 //
 // The copies are HBM's work: a row of x is read once and written K times, a row of y is read once.
 #pragma once
+#include <type_traits>
+
 #include "row_utils.cuh"
 #include "tcgen05_utils.cuh"
 
@@ -259,10 +261,11 @@ struct CombineArgs {
 template <int DT> struct Lane8 {
     static constexpr int V = Elem<DT>::kVec, G = 8 / V;
     uint4 q[G];
-    __device__ __forceinline__ void load(const typename Elem<DT>::T *row, int c, int lane, int C, bool vec, bool on)
+    // WHOLE: aligned, and all 256 columns are there
+    template <bool WHOLE> __device__ __forceinline__ void load(const typename Elem<DT>::T *row, int c, int lane, int C, bool vec, bool on)
     {
         using T = typename Elem<DT>::T;
-        if (vec && c + 8 * lane + 8 <= C) {
+        if (WHOLE || (vec && c + 8 * lane + 8 <= C)) {
 #pragma unroll
             for (int g = 0; g < G; ++g) q[g] = on ? *reinterpret_cast<const uint4 *>(row + c + 8 * lane + g * V) : make_uint4(0, 0, 0, 0);
         } else {
@@ -282,10 +285,10 @@ template <int DT> struct Lane8 {
         for (int g = 0; g < G; ++g) bal_widen<DT>(q[g], reinterpret_cast<float2 *>(v) + g * V / 2);
     }
 };
-template <int DT> __device__ __forceinline__ void lane_store8(typename Elem<DT>::T *row, int c, int lane, int C, bool vec, const float (&v)[8])
+template <int DT, bool WHOLE> __device__ __forceinline__ void lane_store8(typename Elem<DT>::T *row, int c, int lane, int C, bool vec, const float (&v)[8])
 {
     constexpr int V = Elem<DT>::kVec;
-    if (vec && c + 8 * lane + 8 <= C) {
+    if (WHOLE || (vec && c + 8 * lane + 8 <= C)) {
 #pragma unroll
         for (int g = 0; g < 8 / V; ++g) *reinterpret_cast<uint4 *>(row + c + 8 * lane + g * V) = bal_narrow<DT>(reinterpret_cast<const float2 *>(v) + g * V / 2);
     } else {
@@ -297,26 +300,19 @@ template <int DT> __device__ __forceinline__ void lane_store8(typename Elem<DT>:
     }
 }
 
-// DY: type of y, DO: of the residual and the result.  A warp has J pieces of 256 columns of a token, and asks for two of its rows at a
-// time in all of them: with one piece a warp's loads were too few for its life (16384 x 4096 bf16, K 2: 120 us, now COMBINEFWD).
-template <int DY, int DO, int J> __global__ void __launch_bounds__(kRowThreads) combine_rows_kernel(const CombineArgs a)
+// J pieces of 256 columns of a token, from column `first` on; two of its rows at a time in all of them.
+template <int DY, int DO, int J, bool WHOLE>
+__device__ __forceinline__ void combine_pieces(const CombineArgs &a, long long t, int first, int lane)
 {
     using TY = typename Elem<DY>::T;
     using TO = typename Elem<DO>::T;
-    const int lane = threadIdx.x % kWarp;
-    pdl_wait();
-    pdl_launch_dependents();
-    const unsigned task = blockIdx.x * (kRowThreads / kWarp) + threadIdx.x / kWarp, t32 = task / a.parts;
-    const long long t = t32;
-    if (t >= a.T) return;
     const TY *const y = reinterpret_cast<const TY *>(a.y);
     const int *const slots = a.slots + t * a.K;
-    const int first = (int)(task - t32 * a.parts) * J * kWarp * 8;
     float sum[J][8];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         Lane8<DO> r;
-        r.load(reinterpret_cast<const TO *>(a.res) + t * a.res_stride, first + j * kWarp * 8, lane, a.C, a.vec, a.res != nullptr);
+        r.template load<WHOLE>(reinterpret_cast<const TO *>(a.res) + t * a.res_stride, first + j * kWarp * 8, lane, a.C, a.vec, a.res != nullptr);
         r.widen(sum[j]);
     }
     for (int k = 0; k < a.K; k += 2) {
@@ -328,7 +324,7 @@ template <int DY, int DO, int J> __global__ void __launch_bounds__(kRowThreads) 
             const bool there = (unsigned)s < (unsigned)a.y_rows;
             w[i] = there ? a.w ? a.scale * a.w[t * a.K + k + i] : a.scale : 0.f;
 #pragma unroll
-            for (int j = 0; j < J; ++j) row[i][j].load(y + (there ? s : 0) * a.y_stride, first + j * kWarp * 8, lane, a.C, a.vec, there);
+            for (int j = 0; j < J; ++j) row[i][j].template load<WHOLE>(y + (there ? s : 0) * a.y_stride, first + j * kWarp * 8, lane, a.C, a.vec, there);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -342,7 +338,22 @@ template <int DY, int DO, int J> __global__ void __launch_bounds__(kRowThreads) 
     }
 #pragma unroll
     for (int j = 0; j < J; ++j)
-        if (first + j * kWarp * 8 < a.C) lane_store8<DO>(reinterpret_cast<TO *>(a.out) + t * a.out_stride, first + j * kWarp * 8, lane, a.C, a.vec, sum[j]);
+        if (WHOLE || first + j * kWarp * 8 < a.C)
+            lane_store8<DO, WHOLE>(reinterpret_cast<TO *>(a.out) + t * a.out_stride, first + j * kWarp * 8, lane, a.C, a.vec, sum[j]);
+}
+
+// DY: type of y, DO: of the residual and the result.  With one piece a warp's loads were too few for its life (16384 x 4096 bf16, K 2: 120 us,
+// now COMBINEFWD with four).
+template <int DY, int DO, int J> __global__ void __launch_bounds__(kRowThreads) combine_rows_kernel(const CombineArgs a)
+{
+    const int lane = threadIdx.x % kWarp;
+    pdl_wait();
+    pdl_launch_dependents();
+    const unsigned task = blockIdx.x * (kRowThreads / kWarp) + threadIdx.x / kWarp, t32 = task / a.parts;
+    if (t32 >= (unsigned)a.T) return;
+    const int first = (int)(task - t32 * a.parts) * J * kWarp * 8;
+    if (a.vec && first + J * kWarp * 8 <= a.C) combine_pieces<DY, DO, J, true>(a, t32, first, lane);
+    else combine_pieces<DY, DO, J, false>(a, t32, first, lane);
 }
 
 // WPT warps share a token (and reduce its inner products through shared memory, in a fixed order); KB choices at a time, so that a piece of the
@@ -371,13 +382,13 @@ template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRo
             w[i] = s[i] < 0 ? 0.f : a.w ? a.scale * a.w[t * a.K + k + i] : a.scale;
             dot[i] = 0.f;
         }
-#pragma unroll 2
-        for (int c = part * kWarp * 8; on && c < a.C; c += WPT * kWarp * 8) {
+        auto piece = [&](int c, auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
             Lane8<DG> graw;
             Lane8<DY> row[KB];
-            graw.load(g, c, lane, a.C, a.vec, true);
+            graw.template load<WHOLE>(g, c, lane, a.C, a.vec, true);
 #pragma unroll
-            for (int i = 0; i < KB; ++i) row[i].load(y + (s[i] < 0 ? 0 : s[i]) * a.y_stride, c, lane, a.C, a.vec, s[i] >= 0 && a.dw);
+            for (int i = 0; i < KB; ++i) row[i].template load<WHOLE>(y + (s[i] < 0 ? 0 : s[i]) * a.y_stride, c, lane, a.C, a.vec, s[i] >= 0 && a.dw);
             float gv[8];
             graw.widen(gv);
 #pragma unroll
@@ -388,9 +399,17 @@ template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRo
                 for (int e = 0; e < 8; ++e) dot[i] = fmaf(gv[e], v[e], dot[i]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = w[i] * gv[e];
-                if (s[i] >= 0) lane_store8<DY>(dy + s[i] * a.out_stride, c, lane, a.C, a.vec, v);
+                if (s[i] >= 0) lane_store8<DY, WHOLE>(dy + s[i] * a.out_stride, c, lane, a.C, a.vec, v);
             }
+        };
+        constexpr int kStep = WPT * kWarp * 8;
+        int c = on ? part * kWarp * 8 : a.C;
+        if (a.vec) {
+#pragma unroll 2
+            for (; c + kWarp * 8 <= a.C; c += kStep) piece(c, std::true_type());
         }
+#pragma unroll 2
+        for (; c < a.C; c += kStep) piece(c, std::false_type());
         if (a.dw) {
 #pragma unroll
             for (int i = 0; i < KB; ++i) dot[i] = warp_sum(dot[i]);
@@ -418,7 +437,7 @@ template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRo
     if (a.rows && on) {
         const float zero[8] = {};
         for (long long r = max(t * a.K, (long long)*a.rows); r < min((t + 1) * a.K, (long long)a.y_rows); ++r)
-            for (int c = part * kWarp * 8; c < a.C; c += WPT * kWarp * 8) lane_store8<DY>(dy + r * a.out_stride, c, lane, a.C, a.vec, zero);
+            for (int c = part * kWarp * 8; c < a.C; c += WPT * kWarp * 8) lane_store8<DY, false>(dy + r * a.out_stride, c, lane, a.C, a.vec, zero);
     }
 }
 
