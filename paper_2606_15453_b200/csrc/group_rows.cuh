@@ -258,44 +258,61 @@ struct CombineArgs {
 
 // Eight elements of a row of C to a lane: neighbours where rows are aligned (columns c + 8 lane and on), else lanes side by side (c + lane + 32 i), so
 // that a row is read in whole lines either way (2047 x 1001 fp16, 16 bytes apart element by element: 49 us both directions, now COMBINEODD).
-template <int DT> struct Lane8 {
+// WHOLE: aligned, and all 256 columns are there.
+template <int DT, bool WHOLE> struct Lane8 {
+    using T = typename Elem<DT>::T;
     static constexpr int V = Elem<DT>::kVec, G = 8 / V;
-    uint4 q[G];
-    // WHOLE: aligned, and all 256 columns are there
-    template <bool WHOLE> __device__ __forceinline__ void load(const typename Elem<DT>::T *row, int c, int lane, int C, bool vec, bool on)
+    uint4 q[WHOLE ? G : 1];
+    float f[WHOLE ? 1 : 8];
+    __device__ __forceinline__ void load(const T *row, int c, int lane, int C, bool vec, bool on)
     {
-        using T = typename Elem<DT>::T;
-        if (WHOLE || (vec && c + 8 * lane + 8 <= C)) {
+        if constexpr (WHOLE) {
 #pragma unroll
             for (int g = 0; g < G; ++g) q[g] = on ? *reinterpret_cast<const uint4 *>(row + c + 8 * lane + g * V) : make_uint4(0, 0, 0, 0);
         } else {
-            T e[8];
+            const T *const p = row + c + (vec ? 8 : 1) * lane;
+            const int left = on ? C - c - (vec ? 8 : 1) * lane : 0;
+            if (vec) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = vec ? c + 8 * lane + i : c + lane + kWarp * i;
-                e[i] = on && at < C ? row[at] : Elem<DT>::from_f32(0.f);
+                for (int i = 0; i < 8; ++i) f[i] = i < left ? Elem<DT>::to_f32(p[i]) : 0.f;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = kWarp * i < left ? Elem<DT>::to_f32(p[kWarp * i]) : 0.f;
             }
-#pragma unroll
-            for (int g = 0; g < G; ++g) q[g] = *reinterpret_cast<const uint4 *>(e + g * V);
         }
     }
     __device__ __forceinline__ void widen(float (&v)[8]) const
     {
+        if constexpr (WHOLE) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) bal_widen<DT>(q[g], reinterpret_cast<float2 *>(v) + g * V / 2);
+            for (int g = 0; g < G; ++g) bal_widen<DT>(q[g], reinterpret_cast<float2 *>(v) + g * V / 2);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = f[i];
+        }
     }
 };
 template <int DT, bool WHOLE> __device__ __forceinline__ void lane_store8(typename Elem<DT>::T *row, int c, int lane, int C, bool vec, const float (&v)[8])
 {
+    using T = typename Elem<DT>::T;
     constexpr int V = Elem<DT>::kVec;
-    if (WHOLE || (vec && c + 8 * lane + 8 <= C)) {
+    if constexpr (WHOLE) {
 #pragma unroll
         for (int g = 0; g < 8 / V; ++g) *reinterpret_cast<uint4 *>(row + c + 8 * lane + g * V) = bal_narrow<DT>(reinterpret_cast<const float2 *>(v) + g * V / 2);
     } else {
+        T *const p = row + c + (vec ? 8 : 1) * lane;
+        const int left = C - c - (vec ? 8 : 1) * lane;
+        if (vec && left >= 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int at = vec ? c + 8 * lane + i : c + lane + kWarp * i;
-            if (at < C) row[at] = Elem<DT>::from_f32(v[i]);
+            for (int g = 0; g < 8 / V; ++g) *reinterpret_cast<uint4 *>(p + g * V) = bal_narrow<DT>(reinterpret_cast<const float2 *>(v) + g * V / 2);
+        } else if (vec) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) p[i] = Elem<DT>::from_f32(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (kWarp * i < left) p[kWarp * i] = Elem<DT>::from_f32(v[i]);
         }
     }
 }
@@ -311,12 +328,12 @@ __device__ __forceinline__ void combine_pieces(const CombineArgs &a, long long t
     float sum[J][8];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        Lane8<DO> r;
-        r.template load<WHOLE>(reinterpret_cast<const TO *>(a.res) + t * a.res_stride, first + j * kWarp * 8, lane, a.C, a.vec, a.res != nullptr);
+        Lane8<DO, WHOLE> r;
+        r.load(reinterpret_cast<const TO *>(a.res) + t * a.res_stride, first + j * kWarp * 8, lane, a.C, a.vec, a.res != nullptr);
         r.widen(sum[j]);
     }
     for (int k = 0; k < a.K; k += 2) {
-        Lane8<DY> row[2][J];
+        Lane8<DY, WHOLE> row[2][J];
         float w[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -324,7 +341,7 @@ __device__ __forceinline__ void combine_pieces(const CombineArgs &a, long long t
             const bool there = (unsigned)s < (unsigned)a.y_rows;
             w[i] = there ? a.w ? a.scale * a.w[t * a.K + k + i] : a.scale : 0.f;
 #pragma unroll
-            for (int j = 0; j < J; ++j) row[i][j].template load<WHOLE>(y + (there ? s : 0) * a.y_stride, first + j * kWarp * 8, lane, a.C, a.vec, there);
+            for (int j = 0; j < J; ++j) row[i][j].load(y + (there ? s : 0) * a.y_stride, first + j * kWarp * 8, lane, a.C, a.vec, there);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -384,11 +401,11 @@ template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRo
         }
         auto piece = [&](int c, auto whole) {
             constexpr bool WHOLE = decltype(whole)::value;
-            Lane8<DG> graw;
-            Lane8<DY> row[KB];
-            graw.template load<WHOLE>(g, c, lane, a.C, a.vec, true);
+            Lane8<DG, WHOLE> graw;
+            Lane8<DY, WHOLE> row[KB];
+            graw.load(g, c, lane, a.C, a.vec, true);
 #pragma unroll
-            for (int i = 0; i < KB; ++i) row[i].template load<WHOLE>(y + (s[i] < 0 ? 0 : s[i]) * a.y_stride, c, lane, a.C, a.vec, s[i] >= 0 && a.dw);
+            for (int i = 0; i < KB; ++i) row[i].load(y + (s[i] < 0 ? 0 : s[i]) * a.y_stride, c, lane, a.C, a.vec, s[i] >= 0 && a.dw);
             float gv[8];
             graw.widen(gv);
 #pragma unroll
