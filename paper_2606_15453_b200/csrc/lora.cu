@@ -110,15 +110,20 @@ int launch_up(LoraArgs &a, int dtype, int out_dtype, int dev, int sms, cudaStrea
     if (dtype == STMOE_BF16) return out_dtype == STMOE_F32 ? launch_up_as<1, 0, 3>(a, vec, dev, sms, st) : launch_up_as<1, 1, 2>(a, vec, dev, sms, st);
     return out_dtype == STMOE_F32 ? launch_up_as<4, 0, 3>(a, vec, dev, sms, st) : launch_up_as<4, 4, 2>(a, vec, dev, sms, st);
 }
-template <int DT> int launch_grad(const LoraGradArgs &a, int dev, cudaStream_t st)
+template <int DT> int launch_grad(LoraGradPair &p, int dev, cudaStream_t st)
 {
     static PerDevice<bool> asked;
     if (const int rc = smem_of(asked, dev, lora_grad_kernel<DT>, kGradSmem)) return rc;
-    const dim3 grid(a.n + a.T / a.task_rows, (a.C + kGradCols - 1) / kGradCols, (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
-    if (const int rc = launch_behind(lora_grad_kernel<DT>, grid, kLoraThreads, kGradSmem, 1, st, a)) return rc;
+    const LoraGradArgs &a = p.g[p.g[0].grad ? 0 : 1];
+    int blocks[2];
+    for (int w = 0; w < 2; ++w) blocks[w] = p.g[w].grad ? (p.g[w].C + kGradCols - 1) / kGradCols : 0;
+    p.blocks = blocks[0];
+    const dim3 grid(a.n + a.T / a.task_rows, blocks[0] + blocks[1], (a.r + kLoraRankBlock - 1) / kLoraRankBlock);
+    if (const int rc = launch_behind(lora_grad_kernel<DT>, grid, kLoraThreads, kGradSmem, 1, st, p)) return rc;
     if (a.T <= a.task_rows) return STMOE_OK;    // no adapter has several tasks
-    const int64_t size = (int64_t)a.r * a.C;
-    return launch_behind(lora_grad_sum_kernel<DT>, dim3(a.n, (unsigned)std::min<int64_t>(256, (size + kLoraThreads - 1) / kLoraThreads)), kLoraThreads, 0, 1, st, a);
+    const int64_t size = (int64_t)a.r * std::max(blocks[0] ? p.g[0].C : 0, blocks[1] ? p.g[1].C : 0);
+    const dim3 sums(a.n, (unsigned)std::min<int64_t>(256, (size + kLoraThreads - 1) / kLoraThreads), (blocks[0] > 0) + (blocks[1] > 0));
+    return launch_behind(lora_grad_sum_kernel<DT>, sums, kLoraThreads, 0, 1, st, p);
 }
 
 }  // namespace
@@ -164,7 +169,7 @@ size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int ran
     if (!sizes_ok(tokens, n_adapters, rank, inner, outer)) return 0;
     int64_t n = up_to((int64_t)2 * n_adapters * rank * up_to(outer, 8), 256) + up_to((int64_t)2 * n_adapters * inner * up_to(rank, 8), 256);
     n += part_bytes(tokens, rank, outer) + up_to((int64_t)sizeof(float) * tokens * rank, 256);
-    return (size_t)(n + (int64_t)sizeof(float) * grad_parts(tokens) * rank * std::max(inner, outer));
+    return (size_t)(n + (int64_t)sizeof(float) * grad_parts(tokens) * rank * ((int64_t)inner + outer));
 }
 
 int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const void *x, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group,
@@ -205,20 +210,17 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
         if (const int rc = launch_down(k, dtype, dev, st)) return rc;
         if (const int rc = launch_up(k, dtype, dtype, dev, sms, st)) return rc;
     }
-    LoraGradArgs g{};
-    g.order = order, g.counts = counts, g.starts = starts, g.scale = scale, g.alpha = alpha, g.T = (int)tokens, g.n = n_adapters, g.r = rank;
-    g.u_vec = rank % 4 == 0, g.task_rows = grad_task_rows(tokens), g.parts = grad_parts(tokens), g.part = parts;
-    if (grad_a) {
-        g.u = u, g.z = x, g.z_stride = x_stride, g.C = inner, g.by_col = false, g.grad = grad_a;
-        g.vec = rows_vec(x, dtype, tokens > 1 ? x_stride : 0);
-        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, dev, st) : launch_grad<4>(g, dev, st)) return rc;
+    if (!grad_a && !grad_b) return STMOE_OK;
+    LoraGradPair p{};
+    for (int w = 0; w < 2; ++w) {
+        LoraGradArgs &g = p.g[w];
+        g.order = order, g.counts = counts, g.starts = starts, g.scale = scale, g.alpha = alpha, g.T = (int)tokens, g.n = n_adapters, g.r = rank;
+        g.task_rows = grad_task_rows(tokens), g.parts = grad_parts(tokens), g.by_col = w == 1;
+        g.u = w ? hidden : u, g.z = w ? grad : x, g.z_stride = w ? grad_stride : x_stride, g.C = w ? outer : inner, g.grad = w ? grad_b : grad_a;
+        g.part = parts + (w ? (int64_t)g.parts * rank * inner : 0);
+        g.u_vec = rank % 4 == 0 && ((uintptr_t)g.u & 15) == 0, g.vec = rows_vec(g.z, dtype, tokens > 1 ? g.z_stride : 0);
     }
-    if (grad_b) {
-        g.u = hidden, g.u_vec = g.u_vec && ((uintptr_t)hidden & 15) == 0, g.z = grad, g.z_stride = grad_stride, g.C = outer, g.by_col = true, g.grad = grad_b;
-        g.vec = rows_vec(grad, dtype, tokens > 1 ? grad_stride : 0);
-        if (const int rc = dtype == STMOE_BF16 ? launch_grad<1>(g, dev, st) : launch_grad<4>(g, dev, st)) return rc;
-    }
-    return STMOE_OK;
+    return dtype == STMOE_BF16 ? launch_grad<1>(p, dev, st) : launch_grad<4>(p, dev, st);
 }
 
 }  // extern "C"

@@ -330,6 +330,11 @@ struct LoraGradArgs {
     float *part;            // [parts][r * C], laid out as grad: tasks of adapters that have several
     int parts;
 };
+// The gradients of A and of B in one launch: column blocks of the first, then of the second (either may be left out).
+struct LoraGradPair {
+    LoraGradArgs g[2];
+    int blocks;             // of the first
+};
 
 struct LoraTask {
     int g, index, tasks, several;   // adapter, which of its tasks, how many, tasks of earlier adapters that have several
@@ -381,8 +386,11 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t (&r)[4])
 // and 2816 columns took 26 and 37 us, now GRADTIME).  A step of 32 positions costs one barrier: behind barrier i the MMAs of step i run while z
 // is on its way for steps up to i + 3, u is turned into planes for step i + 1, the largest magnitude of step i + 2 is found (fp16 planes), which the
 // next barrier publishes, and u is asked for for step i + 3.  The planes' power of two follows the largest u so far, the sums with it.
-template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_kernel(const LoraGradArgs a)
+template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_kernel(const __grid_constant__ LoraGradPair pair)
 {
+    const bool second = (int)blockIdx.y >= pair.blocks;
+    const LoraGradArgs &a = pair.g[second];
+    const int block = blockIdx.y - (second ? pair.blocks : 0);
     using T = typename Elem<DT>::T;
     constexpr int PL = 2, kTiles = kLoraRankBlock / 8, kZ = kGradCols + 8, kU = kGradPos + 8, kRing = 4;
     struct Steps {
@@ -401,7 +409,7 @@ template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_k
         pdl_wait();
         return;
     }
-    const int c0 = blockIdx.y * kGradCols, r0 = blockIdx.z * kLoraRankBlock, here = min(kGradCols, a.C - c0), ranks = min(kLoraRankBlock, a.r - r0);
+    const int c0 = block * kGradCols, r0 = blockIdx.z * kLoraRankBlock, here = min(kGradCols, a.C - c0), ranks = min(kLoraRankBlock, a.r - r0);
     const int begin = a.starts[task.g] + task.index * a.task_rows;
     const int count = max(0, min(a.task_rows, a.counts[task.g] - task.index * a.task_rows)), steps = (count + kGradPos - 1) / kGradPos;
     const T *const z = reinterpret_cast<const T *>(a.z) + c0 + lane * 8;
@@ -541,8 +549,9 @@ template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_k
 }
 
 // Adapters of several tasks: their sums, in order.
-template <int DT> __global__ void __launch_bounds__(kLoraThreads) lora_grad_sum_kernel(const LoraGradArgs a)
+template <int DT> __global__ void __launch_bounds__(kLoraThreads) lora_grad_sum_kernel(const __grid_constant__ LoraGradPair pair)
 {
+    const LoraGradArgs &a = pair.g[pair.blocks ? blockIdx.z : 1];
     using T = typename Elem<DT>::T;
     __shared__ int s_sum[kLoraWarps];
     pdl_wait();
