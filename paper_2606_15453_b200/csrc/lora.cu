@@ -27,12 +27,15 @@ bool sizes_ok(int64_t tokens, int n, int rank, int inner, int outer)
     return tokens >= 0 && tokens <= INT32_MAX / 2 && n >= 1 && n <= kLoraMaxAdapters && rank >= 1 && rank <= kLoraMaxRank && inner >= 1 &&
            inner <= kMaxLength && outer >= 1 && outer <= kMaxLength;
 }
-// The tile kernels' share: MEASURED
-bool by_tiles(int64_t tokens, int rank) { return tokens >= 256 && rank <= kTileMaxRank; }
+// The tile kernels' share.  In a graph, rank 16, 4096 -> 4096 (rank 64, 2048 -> 2816), they take 13 us and half of one for every adapter that has rows, however
+// few; the kernels for few rows 7 us and 3 for every 100 rows.  Tiles against few: 256 rows of 1 adapter 13.8 : 14.2 (13.4 : 17.1), of 8
+// adapters 17.9 : 14.2 (17.3 : 17.1), 384 of 8 18.0 : 19.6 (17.4 : 23.8), 1024 of 8 19 : 35 (19 : 38), 1024 of 64 46 : 35 (42 : 38), 1024 of 256
+// 149 : 48 (132 : 63).
+bool by_tiles(int64_t tokens, int n_adapters, int rank) { return tokens >= 20 * ((int64_t)n_adapters + 10) && rank <= kTileMaxRank; }
 // Parts of the inner dimension: enough CTAs for the GPU where rows are few, two steps to a warp (four to a tile) at least.
-int down_splits(int64_t tokens, int rank, int inner)
+int down_splits(int64_t tokens, int n_adapters, int rank, int inner)
 {
-    if (by_tiles(tokens, rank)) {
+    if (by_tiles(tokens, n_adapters, rank)) {
         const int64_t most = std::min<int64_t>(kDownMaxSplits, (inner + 255) / 256);
         return (int)std::max<int64_t>(1, std::min<int64_t>(most, 296 / ((tokens + kTileRows - 1) / kTileRows)));
     }
@@ -40,9 +43,10 @@ int down_splits(int64_t tokens, int rank, int inner)
     const int64_t most = std::min<int64_t>(16, (steps + 2 * kLoraWarps - 1) / (2 * kLoraWarps));
     return (int)std::max<int64_t>(1, std::min<int64_t>(most, 592 / std::max<int64_t>(1, tokens)));
 }
-int64_t part_bytes(int64_t tokens, int rank, int inner)
+int64_t part_bytes(int64_t tokens, int n_adapters, int rank, int inner)
 {
-    return up_to((int64_t)sizeof(float) * (by_tiles(tokens, rank) ? 1 : down_splits(tokens, rank, inner)) * tokens * up_to(rank, 8), 256);
+    const int parts = by_tiles(tokens, n_adapters, rank) ? 1 : down_splits(tokens, n_adapters, rank, inner);
+    return up_to((int64_t)sizeof(float) * parts * tokens * up_to(rank, 8), 256);
 }
 int grad_task_rows(int64_t tokens) { return (int)std::max<int64_t>(256, up_to((tokens + 15) / 16, kGradPos)); }
 int grad_parts(int64_t tokens) { return (int)(2 * tokens / grad_task_rows(tokens)); }
@@ -64,7 +68,7 @@ template <int DT, bool XVEC, bool WVEC> int launch_down_tiles(const LoraArgs &a,
 }
 template <int DT> int launch_down_as(const LoraArgs &a, bool xvec, bool wvec, int dev, cudaStream_t st)
 {
-    if (by_tiles(a.T, a.r)) {
+    if (by_tiles(a.T, a.n, a.r)) {
         if (xvec) return wvec ? launch_down_tiles<DT, true, true>(a, dev, st) : launch_down_tiles<DT, true, false>(a, dev, st);
         return wvec ? launch_down_tiles<DT, false, true>(a, dev, st) : launch_down_tiles<DT, false, false>(a, dev, st);
     }
@@ -73,8 +77,8 @@ template <int DT> int launch_down_as(const LoraArgs &a, bool xvec, bool wvec, in
 }
 int launch_down(LoraArgs &a, int dtype, int dev, cudaStream_t st)
 {
-    a.splits = down_splits(a.T, a.r, a.I);
-    const int step = by_tiles(a.T, a.r) ? 64 : kLoraStep, steps = (a.I + step - 1) / step;
+    a.splits = down_splits(a.T, a.n, a.r, a.I);
+    const int step = by_tiles(a.T, a.n, a.r) ? 64 : kLoraStep, steps = (a.I + step - 1) / step;
     a.steps = (steps + a.splits - 1) / a.splits;
     a.splits = (steps + a.steps - 1) / a.steps;
     const bool xvec = rows_vec(a.x, dtype, a.T > 1 ? a.x_stride : 0) && a.I % 8 == 0;
@@ -97,7 +101,7 @@ template <int DT, int DO, int PL, bool WVEC> int launch_up_tiles(const LoraArgs 
 }
 template <int DT, int DO, int PL> int launch_up_as(const LoraArgs &a, bool vec, int dev, int sms, cudaStream_t st)
 {
-    if (by_tiles(a.T, a.r)) return vec ? launch_up_tiles<DT, DO, PL, true>(a, dev, sms, st) : launch_up_tiles<DT, DO, PL, false>(a, dev, sms, st);
+    if (by_tiles(a.T, a.n, a.r)) return vec ? launch_up_tiles<DT, DO, PL, true>(a, dev, sms, st) : launch_up_tiles<DT, DO, PL, false>(a, dev, sms, st);
     const dim3 grid(a.T, (a.O + kLoraOutBlock - 1) / kLoraOutBlock);
     return vec ? launch_behind(lora_up_kernel<DT, DO, PL, true>, grid, kLoraThreads, 0, 1, st, a)
                : launch_behind(lora_up_kernel<DT, DO, PL, false>, grid, kLoraThreads, 0, 1, st, a);
@@ -132,7 +136,7 @@ extern "C" {
 
 size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer)
 {
-    return sizes_ok(tokens, n_adapters, rank, inner, outer) ? (size_t)part_bytes(tokens, rank, inner) : 0;
+    return sizes_ok(tokens, n_adapters, rank, inner, outer) ? (size_t)part_bytes(tokens, n_adapters, rank, inner) : 0;
 }
 
 int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,
@@ -168,7 +172,7 @@ size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int ran
 {
     if (!sizes_ok(tokens, n_adapters, rank, inner, outer)) return 0;
     int64_t n = up_to((int64_t)2 * n_adapters * rank * up_to(outer, 8), 256) + up_to((int64_t)2 * n_adapters * inner * up_to(rank, 8), 256);
-    n += part_bytes(tokens, rank, outer) + up_to((int64_t)sizeof(float) * tokens * rank, 256);
+    n += part_bytes(tokens, n_adapters, rank, outer) + up_to((int64_t)sizeof(float) * tokens * rank, 256);
     return (size_t)(n + (int64_t)sizeof(float) * grad_parts(tokens) * rank * ((int64_t)inner + outer));
 }
 
@@ -195,7 +199,7 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
     auto take = [&](int64_t bytes) { uint8_t *p = at; at += up_to(bytes, 256); return p; };
     const int64_t outer8 = up_to(outer, 8), rank8 = up_to(rank, 8);
     uint16_t *const bt = (uint16_t *)take((int64_t)2 * n_adapters * rank * outer8), *const a_t = (uint16_t *)take((int64_t)2 * n_adapters * inner * rank8);
-    float *const part = (float *)take(part_bytes(tokens, rank, outer)), *const u = (float *)take((int64_t)sizeof(float) * tokens * rank);
+    float *const part = (float *)take(part_bytes(tokens, n_adapters, rank, outer)), *const u = (float *)take((int64_t)sizeof(float) * tokens * rank);
     float *const parts = (float *)at;
     if (tokens) {
         LoraTransposeArgs t{{(const uint16_t *)b, (const uint16_t *)a}, {bt, a_t}, {b_group, a_group}, {b_row, a_row}, {outer8, rank8}, {outer, rank}, {rank, inner}, {}};

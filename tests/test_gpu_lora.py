@@ -77,7 +77,7 @@ def _within(got, want, name):
 
 SHAPES = [(1, 1, 1, 8, 8), (1, 3, 16, 4096, 4096), (2, 1, 5, 33, 17), (7, 4, 8, 64, 512), (8, 8, 16, 128, 520), (64, 64, 16, 512, 768), (65, 3, 24, 100, 1000),
           (200, 5, 64, 256, 256), (131, 2, 65, 96, 130), (40, 2, 128, 264, 200), (33, 3, 256, 72, 80), (1000, 7, 16, 512, 300), (777, 1, 33, 200, 136), (520, 1024, 4, 32, 40),
-          (1500, 2, 8, 40, 1024)]
+          (1500, 2, 8, 40, 1024), (640, 3, 128, 200, 264), (700, 2, 72, 136, 90), (3000, 20, 16, 64, 48), (450, 12, 16, 192, 130)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
