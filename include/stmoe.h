@@ -531,9 +531,9 @@ int stmoe_combine_rows_backward(const void *grad, int grad_dtype, int64_t grad_s
  *   scale  fp32 [n_adapters], or NULL: 1
  *   base, out  [tokens][outer] in out_dtype (dtype or STMOE_F32); base may be NULL (0) or out itself; nothing else may overlap
  *   hidden fp32 [tokens][rank], or NULL: receives x A^T (0 for rows without an adapter), which the gradient of B needs
- *   scratch  stmoe_lora_scratch_bytes(...) bytes, 16-byte aligned, contents free; calls that can overlap need scratch of their own
+ *   scratch  stmoe_lora_scratch_bytes(...) bytes (which serve fewer tokens too), 16-byte aligned, contents free; calls that can overlap need scratch of their own
  * Strides in elements; a_group, b_group: from one adapter to the next.  Sums in fp32, one rounding of out; x A^T is kept to 2^-17 (out fp32:
- * 2^-24) of itself.  n_adapters <= 1024, rank <= 256, inner and outer <= 2^24; tokens may be 0 (or 1: a decode step).  The same call gives the same bits every
+ * 2^-24) of itself.  n_adapters <= 1024, rank <= 256, inner and outer <= 2^22; tokens may be 0 (or 1: a decode step).  The same call gives the same bits every
  * time.  16-byte aligned rows (rank a multiple of 8 for B) are read 16 bytes at a time, others element by element.  Should a bounded wait inside a kernel run out, the outputs that depend on it are NaN.  Asynchronous on cuda_stream. */
 size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer);
 int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,

@@ -706,7 +706,8 @@ def router_select_backward(logits, forward, grad_w, out=None, stream=None):
 def group_rows(ids, n_groups, stream=None):
     """stmoe_group_rows: the grouping of ids int32 [rows][top_k] (or [rows]) by id; ids outside [0, n_groups) have no group.
     Returns the plan that dispatch_rows, combine_rows and (for ids [rows]) lora take: dict(counts int32 [n_groups], for mx4_matmul;
-    starts [n_groups + 1]; order [rows * top_k]; slots, shaped as ids; ids, groups)."""
+    starts [n_groups + 1]; order [rows * top_k]; slots, shaped as ids; ids, groups).  ids are kept, not copied: leave them as they are while
+    the plan is in use."""
     if not (ids.is_cuda and ids.dtype == _I32 and ids.dim() in (1, 2) and ids.is_contiguous()):
         _refuse("ids: contiguous int32 [rows][top_k] or [rows] on a CUDA device")
     T, K = (ids.shape[0], 1) if ids.dim() == 1 else ids.shape

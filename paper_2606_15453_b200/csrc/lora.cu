@@ -21,7 +21,7 @@ bool rows_ok(const void *p, int dtype, int64_t stride, int64_t rows, int64_t col
 bool rows_vec(const void *p, int dtype, int64_t stride) { return ((uintptr_t)p & 15) == 0 && stride * elem_bytes(dtype) % 16 == 0; }
 int64_t up_to(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
-constexpr int kMaxLength = 1 << 24;       // of inner and outer
+constexpr int kMaxLength = 1 << 22;       // of inner and outer: blocks of both are one grid dimension
 bool sizes_ok(int64_t tokens, int n, int rank, int inner, int outer)
 {
     return tokens >= 0 && tokens <= INT32_MAX / 2 && n >= 1 && n <= kLoraMaxAdapters && rank >= 1 && rank <= kLoraMaxRank && inner >= 1 &&
@@ -43,13 +43,10 @@ int down_splits(int64_t tokens, int n_adapters, int rank, int inner)
     const int64_t most = std::min<int64_t>(16, (steps + 2 * kLoraWarps - 1) / (2 * kLoraWarps));
     return (int)std::max<int64_t>(1, std::min<int64_t>(most, 592 / std::max<int64_t>(1, tokens)));
 }
-int64_t part_bytes(int64_t tokens, int n_adapters, int rank, int inner)
-{
-    const int parts = by_tiles(tokens, n_adapters, rank) ? 1 : down_splits(tokens, n_adapters, rank, inner);
-    return up_to((int64_t)sizeof(float) * parts * tokens * up_to(rank, 8), 256);
-}
+// parts times rows is never more than this, which does not fall as rows grow
+int64_t part_bytes(int64_t tokens, int rank) { return up_to((int64_t)sizeof(float) * std::max<int64_t>(tokens, 592) * up_to(rank, 8), 256); }
 int grad_task_rows(int64_t tokens) { return (int)std::max<int64_t>(256, up_to((tokens + 15) / 16, kGradPos)); }
-int grad_parts(int64_t tokens) { return (int)(2 * tokens / grad_task_rows(tokens)); }
+int grad_parts(int64_t tokens) { return (int)std::min<int64_t>(32, 2 * tokens / 256); }     // 2 tokens / task rows at most, and does not fall
 
 // more than the default 48 KB of shared memory: asked for once per device
 template <typename K> int smem_of(PerDevice<bool> &asked, int dev, K kernel, int bytes)
@@ -136,7 +133,7 @@ extern "C" {
 
 size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer)
 {
-    return sizes_ok(tokens, n_adapters, rank, inner, outer) ? (size_t)part_bytes(tokens, n_adapters, rank, inner) : 0;
+    return sizes_ok(tokens, n_adapters, rank, inner, outer) ? (size_t)part_bytes(tokens, rank) : 0;
 }
 
 int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,
@@ -172,7 +169,7 @@ size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int ran
 {
     if (!sizes_ok(tokens, n_adapters, rank, inner, outer)) return 0;
     int64_t n = up_to((int64_t)2 * n_adapters * rank * up_to(outer, 8), 256) + up_to((int64_t)2 * n_adapters * inner * up_to(rank, 8), 256);
-    n += part_bytes(tokens, n_adapters, rank, outer) + up_to((int64_t)sizeof(float) * tokens * rank, 256);
+    n += part_bytes(tokens, rank) + up_to((int64_t)sizeof(float) * tokens * rank, 256);
     return (size_t)(n + (int64_t)sizeof(float) * grad_parts(tokens) * rank * ((int64_t)inner + outer));
 }
 
@@ -199,7 +196,7 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
     auto take = [&](int64_t bytes) { uint8_t *p = at; at += up_to(bytes, 256); return p; };
     const int64_t outer8 = up_to(outer, 8), rank8 = up_to(rank, 8);
     uint16_t *const bt = (uint16_t *)take((int64_t)2 * n_adapters * rank * outer8), *const a_t = (uint16_t *)take((int64_t)2 * n_adapters * inner * rank8);
-    float *const part = (float *)take(part_bytes(tokens, n_adapters, rank, outer)), *const u = (float *)take((int64_t)sizeof(float) * tokens * rank);
+    float *const part = (float *)take(part_bytes(tokens, rank)), *const u = (float *)take((int64_t)sizeof(float) * tokens * rank);
     float *const parts = (float *)at;
     if (tokens) {
         LoraTransposeArgs t{{(const uint16_t *)b, (const uint16_t *)a}, {bt, a_t}, {b_group, a_group}, {b_row, a_row}, {outer8, rank8}, {outer, rank}, {rank, inner}, {}};

@@ -462,7 +462,7 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
         m = redux_max(m);
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < kSelN; ++i) v[i] = exp_of(z[i] - m), sum += v[i];
+        for (int i = 0; i < kSelN; ++i) v[i] = bias[i] > lowest ? exp_of(z[i] - m) : 0.f, sum += v[i];   // a row may be at the lowest number throughout
         inv = __fdividef(1.f, row_sum<kWarp>(sum));
     }
     if (a.exact) {
@@ -564,11 +564,11 @@ template <int DT> __global__ void __launch_bounds__(kSelThreads, 4) router_selec
     pdl_wait();
     pdl_launch_dependents();
     float bias[kSelN];
-    bool odd = false;                       // a bias that is no number takes every row the general way
+    bool odd = false;                       // a bias that is no number, or so large that sums overflow, takes every row the general way
 #pragma unroll
     for (int i = 0; i < kSelN; ++i) {
         bias[i] = i >= valid ? -INFINITY : a.bias ? a.bias[e0 + i] : 0.f;
-        odd |= i < valid && !(fabsf(bias[i]) < INFINITY);
+        odd |= i < valid && !(fabsf(bias[i]) < 1e30f);
     }
     odd = __any_sync(kFull, odd);
     const long long step = (long long)gridDim.x * W;

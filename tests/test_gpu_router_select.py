@@ -144,6 +144,31 @@ def test_values_next_to_the_border(scores):
     _check(z, 8, scores=scores, bias=bias, groups=8, top_groups=4, group_best=2)
 
 
+@pytest.mark.parametrize("E", [129, 130, 200, 255, 256])
+@pytest.mark.parametrize("scores", ["softmax", "sigmoid"])
+def test_rows_at_a_fill_value_with_bias(E, scores):
+    """Rows of the type's lowest number throughout, or but for a few, where lanes reach past the last expert."""
+    g = torch.Generator().manual_seed(E)
+    bias = 0.1 * torch.randn(E, generator=g)
+    z = torch.full((12, E), torch.finfo(torch.float32).min)
+    z[1, :3], z[2, -2:], z[3, E // 2] = 1., 2., 0.
+    for renorm in (False, True):
+        _check(z, 6, scores=scores, bias=bias, renorm=renorm)
+        _check(z, 6, scores=scores, bias=3e38 * torch.sign(bias), renorm=renorm)
+    if E in (200, 256):
+        _check(z, 6, scores=scores, bias=bias, groups=E // 8, top_groups=3, group_best=2) if E // 8 <= 32 else None
+
+
+@pytest.mark.parametrize("E,K,groups,top", [(256, 8, 8, 1), (256, 8, 8, 7), (256, 20, 16, 2), (256, 32, 2, 1), (192, 8, 3, 2), (160, 12, 20, 3), (256, 1, 32, 31)])
+def test_groups_of_whole_lanes(E, K, groups, top):
+    g = torch.Generator().manual_seed(K)
+    z = _logits(K, 60, E, "bf16")
+    for best in (1, 2):
+        for b in (None, 0.1 * torch.randn(E, generator=g)):
+            _check(z, K, scores="sigmoid", bias=b, groups=groups, top_groups=top, group_best=best, renorm=True)
+            _check(z, K, bias=b, groups=groups, top_groups=top, group_best=best)
+
+
 def test_masks_padding_and_bias_that_closes_an_expert():
     z = _logits(3, 50, 64, "bf16", special=False)
     mask = torch.rand(50, generator=torch.Generator().manual_seed(1)) < 0.7

@@ -62,6 +62,9 @@ def test_scratch_sizes_do_not_fall():
     for f in (P.lib().stmoe_lora_scratch_bytes, P.lib().stmoe_lora_backward_scratch_bytes):
         assert f(4, 0, 16, 64, 64) == f(4, 4, 257, 64, 64) == f(4, 4, 16, 0, 64) == f(4, 1025, 16, 64, 64) == f(-1, 4, 16, 64, 64) == 0
         assert f(4, 4, 16, 4096, 4096) >= 4 * 16 * 4
+        for n in (1, 7, 200):
+            sizes = [f(tokens, n, 24, 1000, 300) for tokens in sorted({1 << i for i in range(18)} | set(range(1, 9000, 37)))]
+            assert sizes == sorted(sizes)
 
 
 def _dispatch(**kw):
