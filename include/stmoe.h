@@ -497,7 +497,7 @@ int stmoe_router_select_backward(const void *logits, int dtype, int64_t stride, 
  * All int32, device.  The counts are what stmoe_mx4_matmul takes, the grouping of rows by adapter (top_k 1) what stmoe_lora takes.
  *   scratch  stmoe_group_rows_scratch_bytes(rows, top_k, n_groups) bytes (0 for few pairs: NULL is fine), 4-byte
  *            aligned, contents free; calls that can overlap need scratch of their own
- * n_groups <= 1024, rows * top_k < 2^31; rows may be 0.  Asynchronous on cuda_stream. */
+ * n_groups <= 1024, rows * top_k <= 2^30; rows may be 0.  Asynchronous on cuda_stream. */
 size_t stmoe_group_rows_scratch_bytes(int64_t rows, int top_k, int n_groups);
 int stmoe_group_rows(const int32_t *ids, int64_t rows, int top_k, int n_groups, int32_t *counts, int32_t *starts, int32_t *order,
                      int32_t *slots, void *scratch, size_t scratch_bytes, void *cuda_stream);

@@ -764,6 +764,8 @@ def dispatch_rows(x, plan, out=None, stream=None):
     if st is None:
         return _there(x, stream, dispatch_rows, x, plan, out)
     if _wants_grad(x):
+        if x.dtype not in _ELEM:
+            _refuse("x: gradients are of fp32, bf16 or fp16 rows")
         return _Dispatch.apply(x, plan)
     fresh = out is None
     if fresh:

@@ -13,6 +13,7 @@ using namespace stmoe_host;
 namespace {
 
 bool pairs_ok(int64_t rows, int top_k) { return rows >= 0 && top_k >= 1 && rows <= INT32_MAX / top_k; }
+bool group_ok(int64_t rows, int top_k) { return pairs_ok(rows, top_k) && rows * top_k <= 1 << 30; }     // a warp's last position stays an int
 bool elem_ok(int dtype) { return dtype == STMOE_F32 || dtype == STMOE_BF16 || dtype == STMOE_F16; }
 int elem_bytes(int dtype) { return dtype == STMOE_F32 ? 4 : 2; }
 // One CTA, a cluster of up to eight, or CTAs on their own that count in a launch before.  A CTA by itself takes 4096 pairs, one of many 1024.
@@ -71,7 +72,7 @@ extern "C" {
 
 size_t stmoe_group_rows_scratch_bytes(int64_t rows, int top_k, int n_groups)
 {
-    if (!pairs_ok(rows, top_k) || n_groups < 1 || n_groups > kGrpMaxGroups) return 0;
+    if (!group_ok(rows, top_k) || n_groups < 1 || n_groups > kGrpMaxGroups) return 0;
     const int ctas = group_ctas(rows * top_k);
     return in_cluster(rows * top_k) ? 0 : sizeof(int) * (size_t)ctas * (n_groups + 1);
 }
@@ -79,7 +80,7 @@ size_t stmoe_group_rows_scratch_bytes(int64_t rows, int top_k, int n_groups)
 int stmoe_group_rows(const int32_t *ids, int64_t rows, int top_k, int n_groups, int32_t *counts, int32_t *starts, int32_t *order,
                      int32_t *slots, void *scratch, size_t scratch_bytes, void *cuda_stream)
 {
-    if (!ids || !pairs_ok(rows, top_k) || n_groups < 1 || n_groups > kGrpMaxGroups || !counts || !starts || !order || !slots ||
+    if (!ids || !group_ok(rows, top_k) || n_groups < 1 || n_groups > kGrpMaxGroups || !counts || !starts || !order || !slots ||
         !aligned(ids, counts, starts, order, slots))
         return STMOE_ERR_BAD_ARG;
     const size_t need = stmoe_group_rows_scratch_bytes(rows, top_k, n_groups);

@@ -257,7 +257,7 @@ struct CombineArgs {
 };
 
 // Eight elements of a row of C to a lane: neighbours where rows are aligned (columns c + 8 lane and on), else lanes side by side (c + lane + 32 i), so
-// that a row is read in whole lines either way (2047 x 1001 fp16, 16 bytes apart element by element: 49 us both directions, now COMBINEODD).
+// that a row is read in whole lines either way (2047 x 1001 fp16, 16 bytes apart element by element: 49 us both directions, now 35).
 // WHOLE: aligned, and all 256 columns are there.
 template <int DT, bool WHOLE> struct Lane8 {
     using T = typename Elem<DT>::T;
@@ -360,7 +360,7 @@ __device__ __forceinline__ void combine_pieces(const CombineArgs &a, long long t
 }
 
 // DY: type of y, DO: of the residual and the result.  With one piece a warp's loads were too few for its life (16384 x 4096 bf16, K 2: 120 us,
-// now COMBINEFWD with four).
+// 84 with four, where the bytes take 62).
 template <int DY, int DO, int J> __global__ void __launch_bounds__(kRowThreads) combine_rows_kernel(const CombineArgs a)
 {
     const int lane = threadIdx.x % kWarp;

@@ -383,7 +383,7 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t (&r)[4])
 // One task's sum over its positions of z[p][c] u[p][r] for 256 columns and up to 64 ranks.  Columns are the MMA's rows, positions its inner
 // dimension: z lies in shared memory as in memory and is read transposed, u as planes by rank, 32 columns a warp.  What bounds it is issue
 // slots: every CTA turns the same u into planes, which 256 columns share (with 128, and all 64 ranks converted where there were 24, 4099 rows of 2048
-// and 2816 columns took 26 and 37 us, now GRADTIME).  A step of 32 positions costs one barrier: behind barrier i the MMAs of step i run while z
+// and 2816 columns took 26 and 37 us, now 31 for both).  A step of 32 positions costs one barrier: behind barrier i the MMAs of step i run while z
 // is on its way for steps up to i + 3, u is turned into planes for step i + 1, the largest magnitude of step i + 2 is found (fp16 planes), which the
 // next barrier publishes, and u is asked for for step i + 3.  The planes' power of two follows the largest u so far, the sums with it.
 template <int DT> __global__ void __launch_bounds__(kLoraThreads, 2) lora_grad_kernel(const __grid_constant__ LoraGradPair pair)

@@ -48,7 +48,7 @@ def _group(**kw):
     return P.lib().stmoe_group_rows(*a.values(), None)
 
 
-@pytest.mark.parametrize("kw", [dict(ids=None), dict(counts=None), dict(starts=None), dict(order=None), dict(slots=None), dict(T=-1), dict(T=1 << 30), dict(K=0),
+@pytest.mark.parametrize("kw", [dict(ids=None), dict(counts=None), dict(starts=None), dict(order=None), dict(slots=None), dict(T=-1), dict(T=1 << 30), dict(T=(1 << 29) + 1), dict(K=0),
                                 dict(n=0), dict(n=1025), dict(T=1 << 20, scratch=None), dict(T=1 << 20, size=64), dict(T=1 << 20, scratch=TWO), dict(ids=TWO),
                                 dict(counts=ODD), dict(starts=TWO), dict(order=TWO), dict(slots=TWO)])
 def test_group_rows_refusals(kw):
