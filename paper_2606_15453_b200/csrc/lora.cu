@@ -107,10 +107,26 @@ int launch_up(LoraArgs &a, int dtype, int out_dtype, int dev, int sms, cudaStrea
 {
     const int64_t tall = a.T > 1;
     a.out_vec = rows_vec(a.out, out_dtype, tall * a.out_stride) && (!a.base || rows_vec(a.base, out_dtype, tall * a.base_stride));
-    const bool vec = rows_vec(a.b, dtype, a.O > 1 ? a.b_row : 0) && (a.n == 1 || a.b_group % 8 == 0) && a.r % 8 == 0;
+    const bool vec = rows_vec(a.b, dtype, a.O > 1 ? a.b_row : 0) && (a.n == 1 || a.b_group % 8 == 0) && (a.r % 8 == 0 || a.b_padded);
     if (dtype == STMOE_BF16) return out_dtype == STMOE_F32 ? launch_up_as<1, 0, 3>(a, vec, dev, sms, st) : launch_up_as<1, 1, 2>(a, vec, dev, sms, st);
     return out_dtype == STMOE_F32 ? launch_up_as<4, 0, 3>(a, vec, dev, sms, st) : launch_up_as<4, 4, 2>(a, vec, dev, sms, st);
 }
+// Adds a matrix to a launch of lora_pack_kernel.
+void pack(LoraPackArgs &p, int w, const void *from, int64_t group, int64_t row, int64_t groups, int64_t rows, int cols, uint16_t *to)
+{
+    LoraPackArgs::Matrix &m = p.m[w];
+    m.from = (const uint16_t *)from, m.to = to, m.group = group, m.row = row, m.rows = (int)rows, m.cols = cols, m.ld = (int)up_to(cols, 8);
+    m.parts = (m.ld + kPackCols - 1) / kPackCols, m.tasks = groups * rows * m.parts;
+}
+int launch_pack(const LoraPackArgs &p, cudaStream_t st)
+{
+    const int64_t ctas = (p.m[0].tasks + p.m[1].tasks + p.m[2].tasks + kLoraWarps - 1) / kLoraWarps;
+    if (ctas > INT32_MAX) return STMOE_ERR_TOO_LARGE;
+    return launch_behind(lora_pack_kernel, (int)ctas, kLoraThreads, 0, 1, st, p);
+}
+// room for packed rows of `cols`, none where they can be aligned as they are
+int64_t pack_bytes(int64_t rows, int cols) { return cols % 8 ? up_to(2 * rows * up_to(cols, 8), 256) : 0; }
+
 template <int DT> int launch_grad(LoraGradPair &p, int dev, cudaStream_t st)
 {
     static PerDevice<bool> asked;
@@ -133,7 +149,8 @@ extern "C" {
 
 size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer)
 {
-    return sizes_ok(tokens, n_adapters, rank, inner, outer) ? (size_t)part_bytes(tokens, rank) : 0;
+    if (!sizes_ok(tokens, n_adapters, rank, inner, outer)) return 0;
+    return (size_t)(part_bytes(tokens, rank) + pack_bytes(tokens, inner) + pack_bytes((int64_t)n_adapters * rank, inner) + pack_bytes((int64_t)n_adapters * outer, rank));
 }
 
 int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,
@@ -161,6 +178,22 @@ int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const
     k.counts = counts, k.starts = starts, k.polls = g_mx4_polls.load(std::memory_order_relaxed), k.rp = (int)up_to(rank, 8), k.part = (float *)scratch;
     k.base = base, k.base_stride = base_stride, k.out = out, k.out_stride = out_stride, k.keep = same, k.hidden = hidden;
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (by_tiles(tokens, n_adapters, rank) && (inner % 8 || rank % 8)) {
+        LoraPackArgs p{};
+        uint8_t *at = (uint8_t *)scratch + part_bytes(tokens, rank);
+        const int64_t i8 = up_to(inner, 8), r8 = up_to(rank, 8);
+        if (inner % 8) {
+            uint16_t *const xs = (uint16_t *)at, *const as = (uint16_t *)(at += pack_bytes(tokens, inner));
+            at += pack_bytes((int64_t)n_adapters * rank, inner);
+            pack(p, 0, x, 0, x_stride, 1, tokens, inner, xs), pack(p, 1, a, a_group, a_row, n_adapters, rank, inner, as);
+            k.x = xs, k.x_stride = i8, k.a = as, k.a_row = i8, k.a_group = rank * i8, k.I = (int)i8;
+        }
+        if (rank % 8) {
+            pack(p, 2, b, b_group, b_row, n_adapters, outer, rank, (uint16_t *)at);
+            k.b = at, k.b_row = r8, k.b_group = outer * r8, k.b_padded = true;
+        }
+        if (const int rc = launch_pack(p, st)) return rc;
+    }
     if (const int rc = launch_down(k, dtype, dev, st)) return rc;
     return launch_up(k, dtype, out_dtype, dev, sms, st);
 }
@@ -169,7 +202,7 @@ size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int ran
 {
     if (!sizes_ok(tokens, n_adapters, rank, inner, outer)) return 0;
     int64_t n = up_to((int64_t)2 * n_adapters * rank * up_to(outer, 8), 256) + up_to((int64_t)2 * n_adapters * inner * up_to(rank, 8), 256);
-    n += part_bytes(tokens, rank) + up_to((int64_t)sizeof(float) * tokens * rank, 256);
+    n += part_bytes(tokens, rank) + up_to((int64_t)sizeof(float) * tokens * rank, 256) + pack_bytes(tokens, inner) + pack_bytes(tokens, outer);
     return (size_t)(n + (int64_t)sizeof(float) * grad_parts(tokens) * rank * ((int64_t)inner + outer));
 }
 
@@ -197,6 +230,21 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
     const int64_t outer8 = up_to(outer, 8), rank8 = up_to(rank, 8);
     uint16_t *const bt = (uint16_t *)take((int64_t)2 * n_adapters * rank * outer8), *const a_t = (uint16_t *)take((int64_t)2 * n_adapters * inner * rank8);
     float *const part = (float *)take(part_bytes(tokens, rank)), *const u = (float *)take((int64_t)sizeof(float) * tokens * rank);
+    const bool tiles = by_tiles(tokens, n_adapters, rank), packed = tiles && outer % 8;
+    if (tiles && (inner % 8 || outer % 8)) {
+        LoraPackArgs p{};
+        if (packed) {
+            uint16_t *const to = (uint16_t *)take(pack_bytes(tokens, outer));
+            pack(p, 0, grad, 0, grad_stride, 1, tokens, outer, to);
+            grad = to, grad_stride = outer8;
+        }
+        if (inner % 8) {
+            uint16_t *const to = (uint16_t *)take(pack_bytes(tokens, inner));
+            pack(p, 1, x, 0, x_stride, 1, tokens, inner, to);
+            x = to, x_stride = up_to(inner, 8);
+        }
+        if (const int rc = launch_pack(p, st)) return rc;
+    }
     float *const parts = (float *)at;
     if (tokens) {
         LoraTransposeArgs t{{(const uint16_t *)b, (const uint16_t *)a}, {bt, a_t}, {b_group, a_group}, {b_row, a_row}, {outer8, rank8}, {outer, rank}, {rank, inner}, {}};
@@ -205,7 +253,8 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
         // the forward kernels with the roles of A and B exchanged
         LoraArgs k{};
         k.x = grad, k.x_stride = grad_stride, k.a = bt, k.a_row = outer8, k.a_group = rank * outer8, k.b = a_t, k.b_row = rank8, k.b_group = inner * rank8;
-        k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.I = outer, k.O = inner;
+        k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.O = inner;
+        k.I = packed ? (int)outer8 : outer, k.b_padded = true;       // zeros behind the rows of bt and a_t, and of grad where it was packed
         k.counts = counts, k.starts = starts, k.polls = g_mx4_polls.load(std::memory_order_relaxed), k.rp = (int)up_to(rank, 8), k.part = part;
         k.out = grad_x, k.out_stride = grad_x_stride, k.hidden = u, k.early = true;
         if (const int rc = launch_down(k, dtype, dev, st)) return rc;
