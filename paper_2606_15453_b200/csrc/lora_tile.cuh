@@ -535,7 +535,7 @@ template <int DT, int DO, int PL, bool WVEC, bool OVEC> __global__ void __launch
         // addresses: made anew for every unit they took 130 cycles a copy, which was the whole kernel's time (230 us).
         const int mine = warp - 8, piece = lane % 16, elem = piece * Elem<DO>::kVec, row0 = mine * kWarp + lane / 16;
         const TO *from[kWarp / 2];
-        int s = 0, par = 0;
+        int s = 0, par = 0, ahead = -1;
         for (int u = 0; u < count; step(u), ++u) {
             const int slot = u % NU, o0 = col * kCols;
             if (t.g < a.n) {
@@ -550,7 +550,20 @@ template <int DT, int DO, int PL, bool WVEC, bool OVEC> __global__ void __launch
                 else dmbar_arrive(&full[s]);
                 if (++s == NS) s = 0, par ^= 1;
             }
-            if (!OVEC || !base) continue;
+            if (!base) continue;
+            if constexpr (!OVEC) {
+                // the base is read by the warps that add, element by element: here it is asked into L2, a lane a row
+                if (fresh) {
+                    const int i = mine * kWarp + lane;
+                    ahead = i < t.count && (t.g < a.n || !a.keep) ? lora_row(a, t.begin + i) : -1;
+                }
+                if (ahead >= 0) {
+                    const TO *const p = base + ahead * a.base_stride + o0;
+                    const int last = min(kCols, a.O - o0) - 1;
+                    prefetch_l2(p), prefetch_l2(p + min(last, kCols / 2)), prefetch_l2(p + last);
+                }
+                continue;
+            }
             if (fresh) {
 #pragma unroll
                 for (int r = 0; r < kWarp / 2; ++r) {
