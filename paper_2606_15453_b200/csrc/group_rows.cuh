@@ -375,7 +375,7 @@ template <int DY, int DO, int J> __global__ void __launch_bounds__(kRowThreads, 
 
 // WPT warps share a token (and reduce its inner products through shared memory, in a fixed order); KB choices at a time, so that a piece of the
 // gradient is read once for them and their rows are asked for together.
-template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRowThreads) combine_rows_backward_kernel(const CombineArgs a)
+template <int DY, int DG, int WPT, int KB> __global__ void __launch_bounds__(kRowThreads, KB == 2 ? 5 : 1) combine_rows_backward_kernel(const CombineArgs a)
 {
     using TY = typename Elem<DY>::T;
     using TG = typename Elem<DG>::T;
