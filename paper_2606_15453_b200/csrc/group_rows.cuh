@@ -360,7 +360,7 @@ __device__ __forceinline__ void combine_pieces(const CombineArgs &a, long long t
 }
 
 // DY: type of y, DO: of the residual and the result.  With one piece a warp's loads were too few for its life (16384 x 4096 bf16, K 2: 120 us,
-// 84 with four, where the bytes take 62).
+// 70 with four, where the bytes take 62, and three CTAs an SM; a fourth cost registers: 92).
 template <int DY, int DO, int J> __global__ void __launch_bounds__(kRowThreads, 3) combine_rows_kernel(const CombineArgs a)
 {
     const int lane = threadIdx.x % kWarp;
