@@ -215,7 +215,8 @@ template <int DT, int DO, int PL, bool VEC> __global__ void __launch_bounds__(kL
     if (count > 0 && g >= 0) load_b(0);
     pdl_wait();
     pdl_launch_dependents();
-    if (count == 0 || (g < 0 && a.keep)) return;
+    const bool keep = g < 0 && a.keep;          // nothing of out to write; hidden still gets its zeros
+    if (count == 0 || (keep && !(a.hidden && blockIdx.y == 0))) return;
     if (warp == 0 && lane < kLoraPos) s_row[lane] = row8;
     if (g >= 0) {
         // a warp a position: its ranks' sum over the parts, then the planes
@@ -267,6 +268,7 @@ template <int DT, int DO, int PL, bool VEC> __global__ void __launch_bounds__(kL
             const int row = lora_row(a, p + i / a.r);
             if (row >= 0) a.hidden[(long long)row * a.r + i % a.r] = 0.f;
         }
+        if (keep) return;
     }
     __syncthreads();
     const int here = min(kLoraOutBlock, a.O - o0);
