@@ -37,7 +37,9 @@ constexpr int kSelN = 8;            // logits of a lane
 // sigmoid is off by less than 2^-21: exp2 of a rounded product (|z| 2^-24 relative, which s(1-s) damps to 2^-26), the
 // hardware's exp2 and reciprocal (2^-22 and 2^-23).  A softmax probability p is off by p (|z-m| 2^-23 + 2^-22) from
 // its exponential, at most 0.37 * 2^-23 + 2^-22, and by 13 * 2^-24 from its sum: less than 2^-19.5.  The sum with the
-// bias adds 2^-24 of itself.  Two values, and twice that for sums of two.
+// bias adds 2^-24 of itself.  So two values are off by 2^-18.5 and 2^-24 of each, and a group's sum of two, its own rounding
+// included, by 2^-18.5 and 2^-23 of the magnitudes of its members, which may cancel in it: two groups are told apart by twice the first
+// constant and the second of the magnitudes of both groups' members (the quick way: of the largest of any group's, where 2^-22 would do).
 constexpr float kSelectSlack = 3.814697265625e-6f, kSelectPart = 4.76837158203125e-7f;   // 2^-18, 2^-21
 
 struct SelectArgs {
@@ -133,13 +135,13 @@ template <int LPR, typename F> __device__ __forceinline__ void sel_values(const 
 }
 
 // Groups that stay; members of the others become -infinity.  near: a group of the other side of the border lies within the
-// slack.  keys, totals: the row's room in shared memory.
+// error.  keys, totals, errors: the row's room in shared memory.
 template <int LPR, typename F>
-__device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, int e0, F (&v)[kSelN], F *keys, F *totals, bool &near)
+__device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, int e0, F (&v)[kSelN], F *keys, F *totals, float *errors, bool &near)
 {
     const int gs = a.E / a.G, lg = gs / kSelN;
     const F lowest = -INFINITY;
-    const F slack = a.exact || sizeof(F) == 8 ? (F)0 : (F)(2 * kSelectSlack);
+    const bool by_order = a.exact || sizeof(F) == 8;      // of the sums as they are: no error to allow for
     auto merge = [&](F &b1, F &b2, F o1, F o2) {
         const F low = b1 < o1 ? b1 : o1;
         b1 = b1 < o1 ? o1 : b1;
@@ -150,11 +152,21 @@ __device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, 
         const F t = a.best == 1 || gs == 1 ? b1 : b1 + b2;
         return t > lowest ? t : lowest;       // infinity - infinity: nothing
     };
-    // more: groups that are, or may be, ahead of this one
-    auto rank_step = [&](F mine, int g, F other, int og, int &sure, int &maybe) {
-        const F room = slack == (F)0 || !(mine > lowest) ? (F)0 : slack + (F)fabsf((float)mine) * (F)kSelectPart;
-        sure += other > mine + room || (room == (F)0 && other == mine && og < g);
-        maybe += og != g && (room == (F)0 ? other > mine || (other == mine && og < g) : !(other < mine - room) && other > lowest);
+    // error of a group's sum: its members' are of their own magnitude, also where they cancel
+    auto error_of = [&](F total, F b1, F b2) {
+        if (by_order || !(total > lowest)) return 0.f;
+        return kSelectSlack + (fabsf((float)b1) + (a.best == 1 || gs == 1 ? 0.f : fabsf((float)b2))) * kSelectPart;
+    };
+    // sure, maybe: groups that are, or may be, ahead of this one
+    auto rank_step = [&](F mine, float error, int g, F other, float other_error, int og, int &sure, int &maybe) {
+        if (by_order || !(mine > lowest)) {
+            const bool ahead = other > mine || (other == mine && og < g);
+            sure += ahead, maybe += ahead;
+            return;
+        }
+        const F room = (F)error + (F)other_error;
+        sure += other > mine + room;
+        maybe += og != g && !(other < mine - room) && other > lowest;
     };
     if (gs % kSelN == 0 && (lg & (lg - 1)) == 0) {   // a group is 2^j whole lanes
         F b1 = lowest, b2 = lowest;
@@ -162,9 +174,14 @@ __device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, 
         for (int i = 0; i < kSelN; ++i) merge(b1, b2, v[i] > lowest ? v[i] : lowest, lowest);
         for (int o = 1; o < lg; o <<= 1) merge(b1, b2, __shfl_xor_sync(kFull, b1, o), __shfl_xor_sync(kFull, b2, o));
         const F mine = total_of(b1, b2);
+        const float error = error_of(mine, b1, b2);
         const int g = l / lg;
         int sure = 0, maybe = 0;
-        for (int og = 0; og < a.G; ++og) rank_step(mine, g, __shfl_sync(kFull, mine, sub * LPR + og * lg), og, sure, maybe);
+        for (int og = 0; og < a.G; ++og) {
+            const int of = sub * LPR + og * lg;
+            const F other = __shfl_sync(kFull, mine, of);
+            rank_step(mine, error, g, other, by_order ? 0.f : __shfl_sync(kFull, error, of), og, sure, maybe);
+        }
         near |= g < a.G && mine > lowest && sure < a.top_groups && maybe >= a.top_groups;
         if (sure >= a.top_groups) {
 #pragma unroll
@@ -178,14 +195,17 @@ __device__ __forceinline__ void sel_groups(const SelectArgs &a, int l, int sub, 
     for (int g = l; g < a.G; g += LPR) {
         F b1 = lowest, b2 = lowest;
         for (int i = 0; i < gs; ++i) merge(b1, b2, keys[g * gs + i], lowest);
-        totals[g] = total_of(b1, b2);
+        const F t = total_of(b1, b2);
+        totals[g] = t;
+        if (!by_order) errors[g] = error_of(t, b1, b2);
     }
     __syncwarp();
     uint32_t stay = 0;
     for (int g = l; g < a.G; g += LPR) {
         const F mine = totals[g];
+        const float error = by_order ? 0.f : errors[g];
         int sure = 0, maybe = 0;
-        for (int og = 0; og < a.G; ++og) rank_step(mine, g, totals[og], og, sure, maybe);
+        for (int og = 0; og < a.G; ++og) rank_step(mine, error, g, totals[og], by_order ? 0.f : errors[og], og, sure, maybe);
         near |= mine > lowest && sure < a.top_groups && maybe >= a.top_groups;
         if (sure < a.top_groups) stay |= 1u << g;
     }
@@ -239,7 +259,7 @@ template <int LPR> __device__ __noinline__ uint32_t sel_again(const SelectArgs &
     for (int i = 0; i < kSelN; ++i) z[i] = zp[i];
     sel_values<LPR>(a, z, l * kSelN, v, m, inv);
     bool near = false;
-    if (a.G > 1) sel_groups<LPR>(a, l, sub, l * kSelN, v, keys, totals, near);
+    if (a.G > 1) sel_groups<LPR>(a, l, sub, l * kSelN, v, keys, totals, nullptr, near);
     unsigned long long k[kSelN], last, next;
 #pragma unroll
     for (int i = 0; i < kSelN; ++i) k[i] = sel_key(v[i]);
@@ -284,7 +304,10 @@ template <int LPR> __device__ __forceinline__ void sel_row(const SelectArgs &a, 
     for (int i = 0; i < kSelN; ++i) bad |= z[i] != z[i];
     bool near = false, unsure = false;     // the choice's border, the groups'
     double *const keys = s.keys + sub * LPR * kSelN, *const totals = s.totals + sub * SelShared<LPR>::kMax;
-    if (a.G > 1) sel_groups<LPR>(a, l, sub, e0, v, reinterpret_cast<float *>(keys), reinterpret_cast<float *>(totals), unsure);
+    if (a.G > 1) {
+        float *const room = reinterpret_cast<float *>(totals);      // as many errors behind the totals
+        sel_groups<LPR>(a, l, sub, e0, v, reinterpret_cast<float *>(keys), room, room + SelShared<LPR>::kMax, unsure);
+    }
     uint32_t k[kSelN], last, next;
 #pragma unroll
     for (int i = 0; i < kSelN; ++i) k[i] = sel_key(v[i]);
@@ -417,6 +440,8 @@ __device__ __forceinline__ bool sel_groups_quick(const SelectArgs &a, int lane, 
     merge(hi[0], lo[0], hi[1], lo[1]), merge(hi[2], lo[2], hi[3], lo[3]), merge(hi[0], lo[0], hi[2], lo[2]);
     for (int o = 1; o < lg; o <<= 1) merge(hi[0], lo[0], __shfl_xor_sync(kFull, hi[0], o), __shfl_xor_sync(kFull, lo[0], o));
     float mine = a.best == 1 ? hi[0] : hi[0] + lo[0];
+    // what a sum's error goes by: its members' sizes, which it may be far below
+    const float size = lane < a.E / kSelN ? fabsf(hi[0]) + (a.best == 1 ? 0.f : fabsf(lo[0])) : 0.f;
     // the groups that stay, or those that go, whichever are fewer, one after the other; equal ones: the lower index stays
     const bool group = lane < a.E / kSelN, adding = 2 * a.top_groups <= a.G;
     bool stays = !adding;
@@ -438,7 +463,7 @@ __device__ __forceinline__ bool sel_groups_quick(const SelectArgs &a, int lane, 
         }
         last = redux_min(mine);
     }
-    if (!a.exact && last - next <= 2 * kSelectSlack + fabsf(last) * kSelectPart) return false;
+    if (!a.exact && last - next <= 2 * kSelectSlack + redux_max(size) * kSelectPart) return false;
     if (!stays) {
 #pragma unroll
         for (int i = 0; i < kSelN; ++i) v[i] = -INFINITY;
