@@ -225,6 +225,12 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
     int dev = 0, sms = 0;
     if (const int rc = current_device(&dev, &sms)) return rc;
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (tokens == 0) {
+        // lora_grad_kernel would write the zeros too, but it reads the counts ahead of its wait, which only a kernel of this call before it makes right
+        if (grad_a)
+            if (const int rc = cuda_status(cudaMemsetAsync(grad_a, 0, (size_t)2 * n_adapters * rank * inner, st))) return rc;
+        return grad_b ? cuda_status(cudaMemsetAsync(grad_b, 0, (size_t)2 * n_adapters * rank * outer, st)) : STMOE_OK;
+    }
     uint8_t *at = (uint8_t *)scratch;
     auto take = [&](int64_t bytes) { uint8_t *p = at; at += up_to(bytes, 256); return p; };
     const int64_t outer8 = up_to(outer, 8), rank8 = up_to(rank, 8);
@@ -246,20 +252,18 @@ int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const 
         if (const int rc = launch_pack(p, st)) return rc;
     }
     float *const parts = (float *)at;
-    if (tokens) {
-        LoraTransposeArgs t{{(const uint16_t *)b, (const uint16_t *)a}, {bt, a_t}, {b_group, a_group}, {b_row, a_row}, {outer8, rank8}, {outer, rank}, {rank, inner}, {}};
-        for (int w = 0; w < 2; ++w) t.tiles[w] = ((t.rows[w] + 31) / 32) * ((t.cols[w] + 31) / 32);
-        if (const int rc = launch_behind(lora_transpose_kernel, dim3(t.tiles[0] + t.tiles[1], n_adapters), kLoraThreads, 0, 1, st, t)) return rc;
-        // the forward kernels with the roles of A and B exchanged
-        LoraArgs k{};
-        k.x = grad, k.x_stride = grad_stride, k.a = bt, k.a_row = outer8, k.a_group = rank * outer8, k.b = a_t, k.b_row = rank8, k.b_group = inner * rank8;
-        k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.O = inner;
-        k.I = packed ? (int)outer8 : outer, k.b_padded = true;       // zeros behind the rows of bt and a_t, and of grad where it was packed
-        k.counts = counts, k.starts = starts, k.polls = g_mx4_polls.load(std::memory_order_relaxed), k.rp = (int)up_to(rank, 8), k.part = part;
-        k.out = grad_x, k.out_stride = grad_x_stride, k.hidden = u, k.early = true;
-        if (const int rc = launch_down(k, dtype, dev, st)) return rc;
-        if (const int rc = launch_up(k, dtype, dtype, dev, sms, st)) return rc;
-    }
+    LoraTransposeArgs t{{(const uint16_t *)b, (const uint16_t *)a}, {bt, a_t}, {b_group, a_group}, {b_row, a_row}, {outer8, rank8}, {outer, rank}, {rank, inner}, {}};
+    for (int w = 0; w < 2; ++w) t.tiles[w] = ((t.rows[w] + 31) / 32) * ((t.cols[w] + 31) / 32);
+    if (const int rc = launch_behind(lora_transpose_kernel, dim3(t.tiles[0] + t.tiles[1], n_adapters), kLoraThreads, 0, 1, st, t)) return rc;
+    // the forward kernels with the roles of A and B exchanged
+    LoraArgs k{};
+    k.x = grad, k.x_stride = grad_stride, k.a = bt, k.a_row = outer8, k.a_group = rank * outer8, k.b = a_t, k.b_row = rank8, k.b_group = inner * rank8;
+    k.order = order, k.ids = ids, k.scale = scale, k.alpha = alpha, k.T = (int)tokens, k.n = n_adapters, k.r = rank, k.O = inner;
+    k.I = packed ? (int)outer8 : outer, k.b_padded = true;       // zeros behind the rows of bt and a_t, and of grad where it was packed
+    k.counts = counts, k.starts = starts, k.polls = g_mx4_polls.load(std::memory_order_relaxed), k.rp = (int)up_to(rank, 8), k.part = part;
+    k.out = grad_x, k.out_stride = grad_x_stride, k.hidden = u, k.early = true;
+    if (const int rc = launch_down(k, dtype, dev, st)) return rc;
+    if (const int rc = launch_up(k, dtype, dtype, dev, sms, st)) return rc;
     if (!grad_a && !grad_b) return STMOE_OK;
     LoraGradPair p{};
     for (int w = 0; w < 2; ++w) {
