@@ -562,8 +562,8 @@ __device__ __forceinline__ bool sel_row_quick(const SelectArgs &a, long long t, 
         const float far = redux_max(there ? cz : lowest);
         float x;
         if (!a.sigmoid) x = expf(cz - far);
-        else if (far > -40.f) x = rcp_near(1.f + expf(-cz));
-        else x = expf(fminf(cz, 0.f) - log1pf(expf(-fabsf(cz))) - far);      // scores far below 1: by their logarithms
+        else if (far > -40.f && !__any_sync(kFull, there && cz < -80.f)) x = rcp_near(1.f + expf(-cz));
+        else x = expf(fminf(cz, 0.f) - log1pf(expf(-fabsf(cz))) - fminf(far, 0.f));     // scores so far below 1 that they or their sum underflow: by their logarithms
         x = there ? x : 0.f;
         w = x * rcp_near(row_sum<kWarp>(x));
     } else if (there)
