@@ -643,6 +643,10 @@ template <int DT> __global__ void __launch_bounds__(kSelThreads, 4) router_selec
     }
 }
 
+// 1 / scale, which turns weights into shares of a row; 0 below 2^-126, where it would overflow: the mean that is left away is below the
+// smallest normal number once the scale is back
+__device__ __forceinline__ float sel_inverse(float scale) { return fabsf(scale) >= 1.17549435e-38f ? 1.f / scale : 0.f; }
+
 // Gradient of sum grad . w under a plain softmax, which every expert has a part in.
 template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads) router_select_backward_kernel(const SelectArgs a)
 {
@@ -659,7 +663,7 @@ template <int DT, int LPR> __global__ void __launch_bounds__(kSelThreads) router
     *reinterpret_cast<float4 *>(row + e0) = make_float4(0.f, 0.f, 0.f, 0.f);
     *reinterpret_cast<float4 *>(row + e0 + 4) = make_float4(0.f, 0.f, 0.f, 0.f);
     __syncwarp();
-    const float inv_c = a.scale != 0.f ? 1.f / a.scale : 0.f;
+    const float inv_c = sel_inverse(a.scale);
     float mean = 0.f, poison = 0.f;
     bool some = false;
     if (there)
@@ -726,7 +730,7 @@ template <int DT> __global__ void __launch_bounds__(kSelThreads) router_select_s
     pdl_wait();
     pdl_launch_dependents();
     const int chunks = (a.E + kSelN - 1) / kSelN;
-    const float inv_c = a.scale != 0.f ? 1.f / a.scale : 0.f;
+    const float inv_c = sel_inverse(a.scale);
     const long long step = (long long)gridDim.x * W * rows;
     for (long long t0 = ((long long)blockIdx.x * W + warp) * rows; t0 < a.T; t0 += step) {
         const bool on = r < rows && j < a.K && t0 + r < a.T;
