@@ -233,7 +233,9 @@ template <int DT, bool XVEC, bool WVEC> __global__ void __launch_bounds__(kDownT
             }
         ok = ok && __all_sync(kFull, dmbar_wait(&done, 0, dead, a.polls));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        // a thread a position: one part goes to memory, several to shared memory, where every stage has been read
+        // a thread a position: one part goes to memory, several to shared memory, where every stage has been read.  Should a wait have run out, a
+        // warp that is still copying would write over the others' NaN: all four are behind their copies first.
+        if (a.splits > 1) asm volatile("bar.sync 1, 128;" ::: "memory");
         const int i = warp * kWarp + lane;
         float *const to_row = a.splits == 1 ? a.part + (long long)(t.begin + i) * a.rp : reinterpret_cast<float *>(dsm) + i * (r16 + 4);
         for (int r = 0; r < a.rp; r += 8) {
