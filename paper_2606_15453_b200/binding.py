@@ -11,6 +11,7 @@ import ctypes as C
 import os
 
 import torch
+from torch.autograd import forward_ad as _forward_ad
 
 from . import build as _build
 
@@ -359,6 +360,14 @@ def _is_rows(t, dtype=None) -> bool:
     return t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1) and (dtype is None or t.dtype == dtype)
 
 
+def _no_tangents(*tensors) -> None:
+    """Refuses forward-mode derivatives, which the kernels would lose without a word."""
+    if _forward_ad._current_level >= 0:
+        for t in tensors:
+            if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+                _refuse("forward-mode derivatives are not provided")
+
+
 def _stream_of(ref, stream):
     """Handle of the stream a call goes to: torch's current one, if ref lives on the current device and no
     stream was given; else None (see _there)."""
@@ -518,6 +527,7 @@ def _balance_elem(logits, mask):
     if mask is not None and not (mask.dtype in (torch.bool, _U8) and mask.is_contiguous() and mask.numel() == logits.shape[0]
                                  and mask.device == logits.device):
         _refuse("mask: contiguous bool [tokens] on the logits' device")
+    _no_tangents(logits)
     return elem
 
 
@@ -583,6 +593,7 @@ def router_balance_backward(logits, forward, grad_loss, mask=None, out=None, str
         _refuse("forward does not belong to these logits")
     if not (grad_loss.dtype == _F32 and grad_loss.numel() == 2 and grad_loss.is_contiguous() and grad_loss.device == dev):
         _refuse("grad_loss: fp32 [2] on the logits' device")
+    _no_tangents(grad_loss)
     if out is not None and not (_is_rows(out, logits.dtype) and out.shape == logits.shape and out.device == dev):
         _refuse("out: expected the logits' shape and type")
     st = _stream_of(logits, stream)
@@ -688,6 +699,7 @@ def router_select_backward(logits, forward, grad_w, out=None, stream=None):
         _refuse("forward does not belong to these logits")
     if not _is_vector(grad_w, T * K, _F32, dev):
         _refuse("grad_w: contiguous fp32 [tokens][top_k] on the logits' device")
+    _no_tangents(grad_w)
     if out is not None and not (_is_rows(out, logits.dtype) and out.shape == logits.shape and out.get_device() == dev):
         _refuse("out: expected the logits' shape and type")
     st = _stream_of(logits, stream)
@@ -760,6 +772,7 @@ def dispatch_rows(x, plan, out=None, stream=None):
         _refuse(f"out: expected {(T * K, C)} of x's type with contiguous rows on x's device")
     if out is not None and _wants_grad(x, out):
         _refuse("out is not part of torch's graph: leave it away where x requires a gradient")
+    _no_tangents(x, out)
     st = _stream_of(x, stream)
     if st is None:
         return _there(x, stream, dispatch_rows, x, plan, out)
@@ -811,6 +824,7 @@ def _combine_args(y, plan, w, other, what):
     for t in other:
         if t is not None and not (_is_rows(t) and t.dtype in (y.dtype, _F32) and t.shape[0] == T and t.shape[1] == y.shape[1] and t.get_device() == dev):
             _refuse(f"{what}: expected [rows][cols] of y's type or fp32 with contiguous rows on y's device")
+    _no_tangents(y, w, *other)
     return T, K, elem
 
 
@@ -896,6 +910,7 @@ def _lora_args(x, a, b, plan, scale, hidden):
         _refuse("scale: contiguous fp32 [n] on x's device")
     if hidden is not None and not _is_vector(hidden, T * r, _F32, dev):
         _refuse("hidden: contiguous fp32 [rows][rank] on x's device")
+    _no_tangents(x, a, b, scale, hidden)
     return elem, T, I, n, r, O
 
 
@@ -911,6 +926,7 @@ def lora(x, a, b, plan, scale=None, alpha=1.0, base=None, out=None, hidden=None,
             _refuse(f"base, out: expected {(T, O)} of x's type or fp32 with contiguous rows on x's device")
     if base is not None and out is not None and base.dtype != out.dtype:
         _refuse("base and out have to be of one type")
+    _no_tangents(base, out)
     graph = _wants_grad(x, a, b, base, out, scale)
     if graph and (out is not None or hidden is not None):
         _refuse("out and hidden are not part of torch's graph: leave them away where an input requires a gradient")
@@ -943,6 +959,7 @@ def lora_backward(grad, x, a, b, plan, hidden, scale=None, alpha=1.0, stream=Non
         _refuse(f"grad: expected {(T, O)} of x's type with contiguous rows on x's device")
     if hidden is None:
         _refuse("hidden: what lora wrote is needed")
+    _no_tangents(grad)
     st = _stream_of(x, stream)
     if st is None:
         return _there(x, stream, lora_backward, grad, x, a, b, plan, hidden, scale, alpha)
