@@ -719,7 +719,7 @@ def group_rows(ids, n_groups, stream=None):
     """stmoe_group_rows: the grouping of ids int32 [rows][top_k] (or [rows]) by id; ids outside [0, n_groups) have no group.
     Returns the plan that dispatch_rows, combine_rows and (for ids [rows]) lora take: dict(counts int32 [n_groups], for mx4_matmul;
     starts [n_groups + 1]; order [rows * top_k]; slots, shaped as ids; ids, groups).  ids are kept, not copied: leave them as they are while
-    the plan is in use."""
+    the plan is in use (a gradient that reads the plan refuses one that torch saw written since the call)."""
     if not (ids.is_cuda and ids.dtype == _I32 and ids.dim() in (1, 2) and ids.is_contiguous()):
         _refuse("ids: contiguous int32 [rows][top_k] or [rows] on a CUDA device")
     T, K = (ids.shape[0], 1) if ids.dim() == 1 else ids.shape
@@ -749,16 +749,32 @@ def _plan_of(plan, T, dev):
     return 1 if slots.dim() == 1 else slots.shape[1]
 
 
+class _KeptPlan:
+    """A plan for a gradient that reads these of its tensors: refused there if they were written in between."""
+
+    def __init__(self, plan, *names):
+        self.plan, self.names = dict(plan), names
+        self.versions = self._versions()
+
+    def _versions(self):
+        return [None if t.is_inference() else t._version for t in map(self.plan.get, self.names)]     # inference tensors have none
+
+    def get(self):
+        if self._versions() != self.versions:
+            _refuse(f"the plan's {', '.join(self.names)} (or what shares their memory) were written between the call and its gradient")
+        return self.plan
+
+
 class _Dispatch(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, plan):
-        ctx.plan = plan
+        ctx.plan = _KeptPlan(plan, "slots")
         return dispatch_rows(x, plan)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
-        return combine_rows(grad.contiguous(), ctx.plan), None
+        return combine_rows(grad.contiguous(), ctx.plan.get()), None
 
 
 def dispatch_rows(x, plan, out=None, stream=None):
@@ -797,7 +813,7 @@ class _Combine(torch.autograd.Function):
     @staticmethod
     def forward(ctx, y, w, residual, plan, scale):
         ctx.save_for_backward(y, w)
-        ctx.plan, ctx.scale, ctx.wants = plan, scale, (y.requires_grad, w is not None and w.requires_grad)
+        ctx.plan, ctx.scale, ctx.wants = _KeptPlan(plan, "slots", "starts"), scale, (y.requires_grad, w is not None and w.requires_grad)
         return combine_rows(y, plan, w, residual, scale)
 
     @staticmethod
@@ -806,7 +822,7 @@ class _Combine(torch.autograd.Function):
         y, w = ctx.saved_tensors
         dy = dw = None
         if any(ctx.wants):
-            dy, dw = combine_rows_backward(grad.contiguous(), y, ctx.plan, w, ctx.scale)
+            dy, dw = combine_rows_backward(grad.contiguous(), y, ctx.plan.get(), w, ctx.scale)
         return dy, dw, grad if ctx.needs_input_grad[2] else None, None, None
 
 
@@ -878,7 +894,7 @@ class _Lora(torch.autograd.Function):
         hidden = torch.empty(x.shape[0], a.shape[1], dtype=_F32, device=x.device)
         out = lora(x, a, b, plan, scale, alpha, base, hidden=hidden)
         ctx.save_for_backward(x, a, b, scale, hidden)
-        ctx.plan, ctx.alpha, ctx.dtype = plan, alpha, out.dtype
+        ctx.plan, ctx.alpha = _KeptPlan(plan, "ids", "order", "counts", "starts"), alpha
         return out
 
     @staticmethod
@@ -887,7 +903,7 @@ class _Lora(torch.autograd.Function):
         x, a, b, scale, hidden = ctx.saved_tensors
         dx = da = db = None
         if any(ctx.needs_input_grad[:3]):
-            dx, da, db = lora_backward(grad.to(x.dtype).contiguous(), x, a, b, ctx.plan, hidden, scale, ctx.alpha)
+            dx, da, db = lora_backward(grad.to(x.dtype).contiguous(), x, a, b, ctx.plan.get(), hidden, scale, ctx.alpha)
         return dx, da, db, grad if ctx.needs_input_grad[3] else None, None, None, None
 
 
