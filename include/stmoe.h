@@ -472,7 +472,9 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
  *   by the sum of their group_best (1 or 2) largest v and the best top_groups stay;  ids = the top_k largest v in
  *   them, ascending;  w = scale * s[ids], divided by the sum of s[ids] with STMOE_SELECT_RENORM.
  * Equal values: the lower index, of groups too; values are compared as the formula's in 64 bits, so the choice
- * does not depend on their rounding to 32.  A logit or bias of -infinity, or a NaN, is never chosen and counts as -infinity in
+ * does not depend on their rounding to 32.  Where the order of the scores is that of the logits (bias NULL, and groups, if any have to go,
+ * ranked by their best one) the logits are compared, which differ also where scores are equal in 64 bits: sigmoids of 40 and 50, a softmax's
+ * values 800 below its largest.  With a bias, be it zeros, such scores are equal and the lower index is chosen.  A logit or bias of -infinity, or a NaN, is never chosen and counts as -infinity in
  * its group's sum; a row with fewer than top_k left has id -1 and weight 0 behind the last.  So has a row whose mask byte is 0, which may hold
  * anything.  A NaN in a row that counts (softmax: +infinity too) makes its weights NaN.
  *   logits  STMOE_F32, STMOE_BF16 or STMOE_F16, stride in elements;  bias fp32 [n_experts] or NULL;  mask uint8 [tokens] or NULL

@@ -657,7 +657,8 @@ class _RouterSelect(torch.autograd.Function):
 def router_select(logits, top_k, scores="softmax", bias=None, groups=1, top_groups=None, group_best=1, renorm=False, scale=1.0, mask=None,
                   stream=None):
     """stmoe_router_select: the experts of every row of logits [tokens][n_experts] (fp32, bf16 or fp16) and their weights.
-    scores: "softmax" or "sigmoid"; bias fp32 [n_experts]: added to the scores for the choice only; groups, top_groups, group_best: the
+    scores: "softmax" or "sigmoid"; bias fp32 [n_experts]: added to the scores for the choice only (without one the order is that of the
+    logits, also where scores are equal in 64 bits; with one, be it zeros, the lower index of such is chosen); groups, top_groups, group_best: the
     choice is made among the best top_groups groups, ranked by their group_best best members; renorm: weights of a row sum to scale;
     mask bool [tokens]: rows to choose for.  Returns dict(ids int32 [tokens][top_k], ascending, -1 behind the last; w fp32
     [tokens][top_k]; flags, scale: what the gradient has to know).  Where logits require a gradient w carries it, once differentiable."""

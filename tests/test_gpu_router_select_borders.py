@@ -50,3 +50,24 @@ def test_a_large_group_beside_a_small_one():
         bias = torch.tensor(bias)
         f = P.router_select(z.to(DEV), 2, scores="sigmoid", bias=bias.to(DEV), groups=2, top_groups=1, group_best=2)
         assert torch.equal(f["ids"].cpu(), _groups_of_two_best(z, bias, 2, 1, 2, "sigmoid")[0])
+
+
+@pytest.mark.parametrize("E", [8, 64, 200, 256])
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+def test_scores_that_are_equal_in_64_bits(E, scores):
+    """Without a bias the logits decide, with one of zeros the lower index: of groups too, which are ranked by their best."""
+    z = torch.full((3, E), -2000.)
+    if scores == "sigmoid":                                # all 1 in 64 bits
+        z[:, 1], z[:, 3], z[:, E - 1] = 40., 50., 45.
+        want, equal = [3, E - 1], [1, 3]
+    else:                                                  # 1, and zeros
+        z[:, 1], z[:, 3], z[:, E - 1] = 900., 0., 50.
+        want, equal = [1, E - 1], [0, 1]
+    z, zeros = z.to(DEV), torch.zeros(E, device=DEV)
+    for groups, top in ((1, 1), (2, 2)):
+        kw = dict(scores=scores, groups=groups, top_groups=top)
+        assert P.router_select(z, 2, **kw)["ids"].tolist() == [want] * 3
+        assert P.router_select(z, 2, bias=zeros, **kw)["ids"].tolist() == [equal] * 3
+    half = dict(scores=scores, groups=2, top_groups=1)
+    assert P.router_select(z, 1, **half)["ids"].tolist() == [[want[0]]] * 3
+    assert P.router_select(z, 1, bias=zeros, **half)["ids"].tolist() == [[1]] * 3
