@@ -474,8 +474,8 @@ int stmoe_router_balance_backward(const void *logits, int dtype, int64_t stride,
  * Equal values: the lower index, of groups too; values are compared as the formula's in 64 bits, so the choice
  * does not depend on their rounding to 32.  Where the order of the scores is that of the logits (bias NULL, and groups, if any have to go,
  * ranked by their best one) the logits are compared, which differ also where scores are equal in 64 bits: sigmoids of 40 and 50, a softmax's
- * values 800 below its largest.  With a bias, be it zeros, such scores are equal and the lower index is chosen.  A logit or bias of -infinity, or a NaN, is never chosen and counts as -infinity in
- * its group's sum; a row with fewer than top_k left has id -1 and weight 0 behind the last.  So has a row whose mask byte is 0, which may hold
+ * values 800 below its largest.  With a bias, be it zeros, such scores are equal and the lower index is chosen.
+ * A logit or bias of -infinity, or a NaN, is never chosen and counts as -infinity in its group's sum; a row with fewer than top_k left has id -1 and weight 0 behind the last.  So has a row whose mask byte is 0, which may hold
  * anything.  A NaN in a row that counts (softmax: +infinity too) makes its weights NaN.
  *   logits  STMOE_F32, STMOE_BF16 or STMOE_F16, stride in elements;  bias fp32 [n_experts] or NULL;  mask uint8 [tokens] or NULL
  *   ids     int32 [tokens][top_k], w fp32 [tokens][top_k]: written
@@ -535,7 +535,7 @@ int stmoe_combine_rows_backward(const void *grad, int grad_dtype, int64_t grad_s
  *   hidden fp32 [tokens][rank], or NULL: receives x A^T (0 for rows without an adapter), which the gradient of B needs
  *   scratch  stmoe_lora_scratch_bytes(...) bytes (which serve fewer tokens too), 16-byte aligned, contents free; calls that can overlap need scratch of their own
  * Strides in elements; a_group, b_group: from one adapter to the next.  Sums in fp32, one rounding of out; x A^T is kept to 2^-17 (out fp32:
- * 2^-24) of itself.  n_adapters <= 1024, rank <= 256, inner and outer <= 2^22; tokens may be 0 (or 1: a decode step).  The same call gives the same bits every
+ * 2^-24) of itself or, fp16, to 2^-38 of the largest of its row, whichever is more.  n_adapters <= 1024, rank <= 256, inner and outer <= 2^22; tokens may be 0 (or 1: a decode step).  The same call gives the same bits every
  * time.  16-byte aligned rows (rank a multiple of 8 for B) are read 16 bytes at a time, others element by element.  Should a bounded wait inside a kernel run out, the outputs that depend on it are NaN.  Asynchronous on cuda_stream. */
 size_t stmoe_lora_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer);
 int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group, int64_t a_row, const void *b, int64_t b_group,
@@ -544,7 +544,8 @@ int stmoe_lora(const void *x, int dtype, int64_t x_stride, int64_t tokens, const
                size_t scratch_bytes, void *cuda_stream);
 /* Gradients for grad [tokens][outer] in dtype: grad_x [tokens][inner] = c u A with u = grad B (0 for rows without an adapter; the base's gradient
  * is grad itself), grad_a [n][rank][inner] = c sum_t u^T x, grad_b [n][outer][rank] = c sum_t grad^T hidden, c = alpha * scale[g]; contiguous, in dtype,
- * each rounded once, 0 for adapters without rows; grad_a and grad_b may be NULL.
+ * each rounded once, 0 for adapters without rows; grad_a and grad_b may be NULL.  u and hidden are kept to 2^-17 of themselves or, fp16, to 2^-38 of
+ * the largest of their row (of all rows of their adapter for grad_a and grad_b), whichever is more.  tokens may be 0: grad_a and grad_b are cleared.
  * scale is held constant.  scratch: stmoe_lora_backward_scratch_bytes(...) bytes, 256-byte aligned.  grad_x may overlap neither grad nor x. */
 size_t stmoe_lora_backward_scratch_bytes(int64_t tokens, int n_adapters, int rank, int inner, int outer);
 int stmoe_lora_backward(const void *grad, int dtype, int64_t grad_stride, const void *x, int64_t x_stride, int64_t tokens, const void *a, int64_t a_group,

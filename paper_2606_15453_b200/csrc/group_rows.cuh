@@ -34,12 +34,13 @@ struct GroupArgs {
     int *hist;              // [ctas][G + 1], or nullptr: one CTA, or the CTAs of a cluster
 };
 
-// Counts of a warp's stretch in its row of the table (columns 0..G, the last one for pairs without a group).
+// Column of a pair: its group, or G without one.
 __device__ __forceinline__ int grp_id(const GroupArgs &a, int p)
 {
     const int e = a.ids[p];
     return (unsigned)e < (unsigned)a.G ? e : a.G;
 }
+// Counts of a warp's stretch in its row of the table, columns 0..G.
 __device__ __forceinline__ void grp_count(const GroupArgs &a, int first, int lane, int *row)
 {
     const int end = min(first + a.per_warp, a.pairs);

@@ -28,7 +28,8 @@ bool sizes_ok(int64_t tokens, int n, int rank, int inner, int outer)
            inner <= kMaxLength && outer >= 1 && outer <= kMaxLength;
 }
 // The tile kernels' share.  In a graph, rank 16, 4096 -> 4096 (rank 64, 2048 -> 2816), they take 13 us and half of one for every adapter that has rows, however
-// few; the kernels for few rows 7 us and 3 for every 100 rows.  Tiles against few: 256 rows of 1 adapter 13.8 : 14.2 (13.4 : 17.1), of 8
+// few; the kernels for few rows 7 us and 3 for every 100 rows.  The host does not know which adapters have rows, so the rule takes all of them to
+// have some: rows enough for tiles beside a large table that few of them use take the kernels for few rows.  Tiles against few, every adapter with rows: 256 rows of 1 adapter 13.8 : 14.2 (13.4 : 17.1), of 8
 // adapters 17.9 : 14.2 (17.3 : 17.1), 384 of 8 18.0 : 19.6 (17.4 : 23.8), 1024 of 8 19 : 35 (19 : 38), 1024 of 64 46 : 35 (42 : 38), 1024 of 256
 // 149 : 48 (132 : 63).
 bool by_tiles(int64_t tokens, int n_adapters, int rank) { return tokens >= 20 * ((int64_t)n_adapters + 10) && rank <= kTileMaxRank; }

@@ -12,7 +12,7 @@
 // first that is stages of x, two CTAs an SM.  In the second the base's rows come by asynchronous copies into a ring of units in shared
 // memory, three units ahead of the one in work, so that they cost neither registers nor waits (8192 rows, 4096 -> 14336: with the rows in
 // the registers of eight warps and two CTAs an SM 215 us, spills and all; as a bulk copy of 256 bytes a row 265 us, a lane's bulk copy
-// taking some 75 cycles to issue; like this 100 us).  Two sets of four warps take units in turn.  B's rows are permuted on their way to
+// taking some 75 cycles to issue; like this 106 us).  Two sets of four warps take units in turn.  B's rows are permuted on their way to
 // shared memory so that a lane finds sixteen neighbouring outputs in its accumulator registers and stores them at once.
 // Rows that are not 16-byte aligned go another way: the sums pass through the same shared memory in fp32, and each warp adds and stores
 // its rows element by element, lanes side by side.

@@ -38,7 +38,7 @@ bool whole_groups(const SelectArgs &a)
     const int gs = a.E / a.G, lg = gs / kSelN;
     return a.G == 1 || (gs % kSelN == 0 && (lg & (lg - 1)) == 0);
 }
-// lanes that share a row: a power of two with eight logits each
+// a lane a choice: up to four rows a warp
 template <int DT> int launch_sparse_backward(const SelectArgs &a, int sms, cudaStream_t st)
 {
     int kp = 1;
@@ -46,6 +46,7 @@ template <int DT> int launch_sparse_backward(const SelectArgs &a, int sms, cudaS
     const int rows = std::min(4, kWarp / kp), per = kSelThreads / kWarp * rows;
     return launch_behind(router_select_sparse_backward_kernel<DT>, (int)std::min<int64_t>(((int64_t)a.T + per - 1) / per, sms * 6), kSelThreads, 0, 1, st, a, kp, rows);
 }
+// lanes that share a row: a power of two with eight logits each
 template <int DT> int launch_lanes(bool backward, const SelectArgs &a, int sms, cudaStream_t st)
 {
     if (backward && (a.sigmoid || a.renorm)) return launch_sparse_backward<DT>(a, sms, st);
