@@ -214,27 +214,32 @@ template <typename U> __global__ void __launch_bounds__(kRowThreads) dispatch_ro
     const long long t = t32;
     if (t >= a.T) return;
     const int n = (int)(a.row_bytes / (int)sizeof(U));
-    const int at = (int)(task - t32 * a.parts) * kWarp * kAtOnce + lane;      // the parts are as many as it takes: one piece each
+    const int first = (int)(task - t32 * a.parts) * kWarp * kAtOnce;
+    const unsigned step = a.parts * kWarp * kAtOnce;           // at least n, at most 2^31: at + step is behind the row, and below 2^32
     const U *const src = reinterpret_cast<const U *>(a.x + t * a.x_stride);
     const int *const slots = a.slots + t * a.K;
     const int behind = a.rows ? *a.rows : a.out_rows;
-    U v[kAtOnce];
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i)
-        if (at + i * kWarp < n) v[i] = src[at + i * kWarp];
-    for (int k = 0; k < a.K; ++k) {
-        const int s = slots[k];
-        if ((unsigned)s >= (unsigned)a.out_rows) continue;
-        U *const dst = reinterpret_cast<U *>(a.out + s * a.out_stride);
+    // one turn, as there are as many parts as it takes; without the loop the compiler asks for fewer registers, and the more CTAs an SM write
+    // less evenly (16384 x 2048 bf16, K 8: 95.8 -> 97.2 us)
+    for (int at = first; (unsigned)at < (unsigned)n; at = (int)(at + step)) {
+        U v[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i)
-            if (at + i * kWarp < n) dst[at + i * kWarp] = v[i];
-    }
-    for (long long r = max(t * a.K, (long long)behind); r < min((t + 1) * a.K, (long long)a.out_rows); ++r) {
-        U *const dst = reinterpret_cast<U *>(a.out + r * a.out_stride);
+            if (at + i * kWarp + lane < n) v[i] = src[at + i * kWarp + lane];
+        for (int k = 0; k < a.K; ++k) {
+            const int s = slots[k];
+            if ((unsigned)s >= (unsigned)a.out_rows) continue;
+            U *const dst = reinterpret_cast<U *>(a.out + s * a.out_stride);
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i)
-            if (at + i * kWarp < n) dst[at + i * kWarp] = U{};
+            for (int i = 0; i < kAtOnce; ++i)
+                if (at + i * kWarp + lane < n) dst[at + i * kWarp + lane] = v[i];
+        }
+        for (long long r = max(t * a.K, (long long)behind); r < min((t + 1) * a.K, (long long)a.out_rows); ++r) {
+            U *const dst = reinterpret_cast<U *>(a.out + r * a.out_stride);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                if (at + i * kWarp + lane < n) dst[at + i * kWarp + lane] = U{};
+        }
     }
 }
 
